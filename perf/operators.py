@@ -134,13 +134,13 @@ def _quantised(v, fmt):
     n = v.shape[-1]
     u = torch.nn.functional.pad(v, (0, -n % GROUP)).unflatten(-1, (-1, GROUP))
     m, k = torch.frexp(u.abs().amax(-1, keepdim=True))
-    if fmt == "int8":      # the smallest scale at which the largest value rounds to no more than 127
-        e = k - 7 + (m * 128 >= 127.5)
+    if fmt == "int8":      # the smallest scale at which the largest value is below 128; codes end at 127
+        e = k - 7
     else:                  # ... is no more than 448, the largest e4m3 value
         e = k - 9 + (m > 0.875)
     e = e.clamp(min=-127)
     q = torch.ldexp(u, -e)
-    q = torch.round(q) if fmt == "int8" else q.to(torch.float8_e4m3fn).float()
+    q = torch.round(q).clamp(-127, 127) if fmt == "int8" else q.to(torch.float8_e4m3fn).float()
     q = torch.ldexp(q, e)
     return q.flatten(-2)[..., :n]
 
@@ -297,16 +297,16 @@ def _exact_eight_bits(v, fmt):
     for c0 in range(0, n, GROUP):
         u = v[..., c0:c0 + GROUP]
         top = u.abs().amax(-1, keepdim=True)
-        # exponent e of the scale: the smallest with top / 2^e below 127.5 (int8) or up to 448 (e4m3)
+        # exponent e of the scale: the smallest with top / 2^e below 128 (int8) or up to 448 (e4m3)
         e = torch.floor(torch.log2(top.clamp(min=2.0 ** -140))) - (8 if fmt == "e4m3" else 6)
         e = e.clamp(min=-127) - 1
-        over = (lambda t: t > 448) if fmt == "e4m3" else (lambda t: t >= 127.5)
+        over = (lambda t: t > 448) if fmt == "e4m3" else (lambda t: t >= 128)
         for _ in range(3):
             e = torch.where(over(top / torch.exp2(e)), e + 1, e)
         e = e.clamp(min=-127)
         q = u / torch.exp2(e)
         if fmt == "int8":
-            q = torch.round(q)
+            q = torch.round(q).clamp(-127, 127)
         else:   # three fraction bits, normal exponents down to -6
             step = torch.exp2(torch.floor(torch.log2(q.abs().clamp(min=2.0 ** -6))) - 3)
             q = torch.round(q / step) * step

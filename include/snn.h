@@ -340,6 +340,77 @@ typedef struct {
 } snn_event_layout;
 snn_status snn_get_event_layout(const snn_net* net, int32_t layer, snn_event_layout* out);
 
+/* ---- sequence-model operators --------------------------------------------------------------
+ * The parts of a recurrent sequence model around the spiking step: a recurrence with learned gates, its inputs kept
+ * in 8 bits for the backward pass, and the soft-max loss over a large vocabulary.  Unlike the training step they are
+ * asynchronous: a call checks its arguments, launches kernels on `stream` and returns; it never synchronises and can be
+ * captured into a CUDA graph.  Data is fp32, bf16 or fp16 as `dtype` says; sums, soft-max statistics and recurrent
+ * states are fp32 inside whatever the type, and results are rounded to it once.  The functions keep nothing between
+ * calls.  Strides are in elements and may be any; the innermost dimension is contiguous.
+ * Common errors, before any launch: SNN_ERR_INVALID_ARG (null pointers, sizes, an unknown dtype, mode or format),
+ * SNN_ERR_UNSUPPORTED (a grid or a size beyond the limits named), SNN_ERR_WORKSPACE_TOO_SMALL; SNN_ERR_CUDA if a
+ * launch is refused. */
+typedef enum { SNN_DTYPE_FP32 = 0, SNN_DTYPE_BF16 = 1, SNN_DTYPE_FP16 = 2 } snn_dtype;
+
+/* Activations in 8 bits.  The last axis is cut into groups of SNN_KEEP_GROUP values (the last group of a row may be
+ * shorter); a group has one scale byte c for the scale 2^(c-127) and one code byte per value: a signed integer
+ * (SNN_KEEP_INT8, rounded to nearest even, at most 127 in magnitude) or a 4-bit-exponent, 3-bit-fraction float
+ * (SNN_KEEP_E4M3, rounded to nearest even).  The scale is the smallest power of two, not below 2^-127, at which the
+ * largest magnitude of the group is below 128 resp. no more than 448.  c = 255: the group held an infinity or a NaN, and
+ * all of it decodes to NaN.  A finite value stays finite: what rounding takes beyond the type's range decodes to its
+ * largest finite value. */
+typedef enum { SNN_KEEP_RAW = 0, SNN_KEEP_INT8 = 1, SNN_KEEP_E4M3 = 2 } snn_keep_format;
+#define SNN_KEEP_GROUP 64
+
+/* Encodes n_rows rows of n_cols values (device; rows `row_stride` elements apart) to codes [n_rows][n_cols] and scales
+ * [n_rows][ceil(n_cols / 64)] (device). */
+snn_status snn_activation_pack(const void* values, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t row_stride,
+                               int32_t format, uint8_t* codes, uint8_t* scales, void* stream);
+/* Decodes them to n_rows rows of n_cols values of the given type. */
+snn_status snn_activation_unpack(const uint8_t* codes, const uint8_t* scales, int32_t format, int64_t n_rows,
+                                 int32_t n_cols, void* values, int32_t dtype, int64_t row_stride, void* stream);
+
+/* The gated linear recurrence, for t = 1..T, each sample b and channel n on its own:
+ *   SNN_SCAN_SIGMOID   h_t = a_t h_{t-1} + (1 - a_t) x_t,   a_t = sigmoid(gate_t)
+ *   SNN_SCAN_DIRECT    h_t = gate_t h_{t-1} + x_t
+ * from h_0 = state (zero if NULL).  The backward pass, for a gradient dh_t of every h_t and dlast of the last state:
+ *   D_t = dh_t + a_{t+1} D_{t+1},  D_{T+1} a_{T+1} = dlast,   dstate = a_1 D_1
+ *   SIGMOID: dx_t = (1 - a_t) D_t,  dgate_t = D_t (h_{t-1} - x_t) a_t (1 - a_t);   DIRECT: dx_t = D_t, dgate_t = D_t h_{t-1}
+ * What a forward pass keeps for it: the state before every SNN_SCAN_CHUNK-th step (the paper's local checkpoints,
+ * Eq. 1, with a fixed chunk) and the inputs, either as they are (SNN_KEEP_RAW: the caller's own x and gate, nothing is
+ * written) or in 8 bits, encoded by the forward pass while it reads them.  The backward pass recomputes the states of
+ * a chunk from its checkpoint and the kept inputs.  The gate of SNN_SCAN_DIRECT is a decay close to one, which 8 bits
+ * do not resolve: its gate_format must be SNN_KEEP_RAW (SNN_ERR_UNSUPPORTED otherwise).
+ * Runs of steps are combined before the state they start from is known: the decays are meant to be at most one in
+ * magnitude, and where a product of consecutive decays leaves the range of fp32 the result may not be finite.
+ * lengths (optional, device int32 [B], clamped to [0, T]): sample b ends after lengths[b] steps.  What x, gate and dh
+ * hold behind that is not read; h, dx and dgate are set to zero there; `last` is the state at the end. */
+typedef enum { SNN_SCAN_SIGMOID = 0, SNN_SCAN_DIRECT = 1 } snn_scan_mode;
+#define SNN_SCAN_CHUNK 64
+typedef struct {
+  int32_t T, B, N;               /* steps, samples, channels: each >= 0; T < 2^30                               */
+  int32_t dtype, mode;           /* snn_dtype of x, gate, h, dh, dx, dgate; snn_scan_mode                       */
+  const void *x, *gate;          /* [T][B][N]; the backward pass reads them only where the format is RAW        */
+  int64_t x_stride[2], gate_stride[2];   /* of T and of B                                                       */
+  const int32_t* lengths;        /* [B] or NULL                                                                 */
+  const float* state;            /* [B][N] or NULL; may be the same buffer as `last`                            */
+  void* h;                       /* [T][B][N], forward                                                          */
+  int64_t h_stride[2];
+  float* last;                   /* [B][N] or NULL, forward                                                     */
+  float* states;                 /* [ceil(T / 64)][B][N]: written by the forward pass (NULL: nothing is kept),
+                                    read by the backward pass                                                   */
+  int32_t x_format, gate_format; /* snn_keep_format of the kept inputs                                          */
+  uint8_t *x_codes, *x_scales, *gate_codes, *gate_scales;   /* [T][B][N] and [T][B][ceil(N / 64)]               */
+  const void* dh;                /* [T][B][N], backward                                                         */
+  int64_t dh_stride[2];
+  const float* dlast;            /* [B][N] or NULL, backward                                                    */
+  void *dx, *dgate;              /* [T][B][N], backward                                                         */
+  int64_t dx_stride[2], dgate_stride[2];
+  float* dstate;                 /* [B][N] or NULL, backward                                                    */
+} snn_scan_args;
+snn_status snn_scan_forward(const snn_scan_args* args, void* stream);
+snn_status snn_scan_backward(const snn_scan_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -20,6 +20,9 @@ SNN_STANDARD, SNN_CHUNK, SNN_REMOTE, SNN_DOUBLE, SNN_HIERARCHICAL, SNN_DOUBLE_LO
 SNN_CELL_LIF, SNN_CELL_GRADED = 0, 1
 SNN_SURR_FAST_SIGMOID, SNN_SURR_SIGMOID, SNN_SURR_TRIANGLE = 0, 1, 2
 SNN_INPUT_BITS, SNN_INPUT_DENSE = 0, 1
+SNN_DTYPE_FP32, SNN_DTYPE_BF16, SNN_DTYPE_FP16 = 0, 1, 2
+SNN_KEEP_RAW, SNN_KEEP_INT8, SNN_KEEP_E4M3, SNN_KEEP_GROUP = 0, 1, 2, 64
+SNN_SCAN_SIGMOID, SNN_SCAN_DIRECT, SNN_SCAN_CHUNK = 0, 1, 64
 SNN_FLAG_INPUT_ON_HOST, SNN_FLAG_FORWARD_ONLY, SNN_FLAG_TIME_PHASES = 1, 2, 4
 SNN_FLAG_BACKWARD_LAYER_BY_LAYER, SNN_FLAG_BACKWARD_WAVEFRONT = 8, 16
 SNN_FLAG_REFORWARD_PER_STEP = 32
@@ -40,7 +43,8 @@ STRATEGY_NAMES = {SNN_STANDARD: "standard", SNN_CHUNK: "chunk", SNN_REMOTE: "rem
 EXPORTS = ["snn_create", "snn_destroy", "snn_alpha", "snn_workspace_query", "snn_workspace_query_flags", "snn_train_step", "snn_peak_memory",
            "snn_memory_stats_get", "snn_last_error", "snn_plan", "snn_compact_spikes", "snn_get_event_layout",
            "snn_phase_times_get", "snn_train_step_static", "snn_suggest_ckpt", "snn_selftest_wait_timeout",
-           "snn_debug_checks_enabled"]
+           "snn_debug_checks_enabled", "snn_activation_pack", "snn_activation_unpack", "snn_scan_forward",
+           "snn_scan_backward"]
 SNN_STATIC_WORKSPACE_BYTES = 32 << 20
 
 
@@ -85,6 +89,17 @@ class snn_event_layout(C.Structure):
                 ("pool_capacity", C.c_size_t), ("mask_off", C.c_size_t), ("mask_words", C.c_int32)]
 
 
+class snn_scan_args(C.Structure):
+    _fields_ = [("T", C.c_int32), ("B", C.c_int32), ("N", C.c_int32), ("dtype", C.c_int32), ("mode", C.c_int32),
+                ("x", C.c_void_p), ("gate", C.c_void_p), ("x_stride", C.c_int64 * 2), ("gate_stride", C.c_int64 * 2),
+                ("lengths", C.c_void_p), ("state", C.c_void_p), ("h", C.c_void_p), ("h_stride", C.c_int64 * 2),
+                ("last", C.c_void_p), ("states", C.c_void_p), ("x_format", C.c_int32), ("gate_format", C.c_int32),
+                ("x_codes", C.c_void_p), ("x_scales", C.c_void_p), ("gate_codes", C.c_void_p),
+                ("gate_scales", C.c_void_p), ("dh", C.c_void_p), ("dh_stride", C.c_int64 * 2), ("dlast", C.c_void_p),
+                ("dx", C.c_void_p), ("dgate", C.c_void_p), ("dx_stride", C.c_int64 * 2),
+                ("dgate_stride", C.c_int64 * 2), ("dstate", C.c_void_p)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2412_11810_b200/build.py` "
@@ -116,6 +131,12 @@ def _load() -> C.CDLL:
                                      C.POINTER(snn_ckpt)]
     lib.snn_get_event_layout.argtypes = [C.c_void_p, C.c_int32, C.POINTER(snn_event_layout)]
     lib.snn_selftest_wait_timeout.argtypes = [C.c_void_p, C.c_uint32, C.c_void_p]
+    lib.snn_activation_pack.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_int32, C.c_void_p,
+                                        C.c_void_p, C.c_void_p]
+    lib.snn_activation_unpack.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_void_p,
+                                          C.c_int32, C.c_int64, C.c_void_p]
+    lib.snn_scan_forward.argtypes = [C.POINTER(snn_scan_args), C.c_void_p]
+    lib.snn_scan_backward.argtypes = [C.POINTER(snn_scan_args), C.c_void_p]
     return lib
 
 
@@ -226,6 +247,24 @@ def snn_get_event_layout(net, layer: int) -> snn_event_layout:
     e = snn_event_layout()
     _check(lib.snn_get_event_layout(net, layer, C.byref(e)), net)
     return e
+
+
+def snn_activation_pack(values_ptr: int, dtype: int, n_rows: int, n_cols: int, row_stride: int, fmt: int, codes_ptr: int,
+                        scales_ptr: int, stream: int = 0) -> None:
+    _check(lib.snn_activation_pack(values_ptr, dtype, n_rows, n_cols, row_stride, fmt, codes_ptr, scales_ptr, stream))
+
+
+def snn_activation_unpack(codes_ptr: int, scales_ptr: int, fmt: int, n_rows: int, n_cols: int, values_ptr: int,
+                          dtype: int, row_stride: int, stream: int = 0) -> None:
+    _check(lib.snn_activation_unpack(codes_ptr, scales_ptr, fmt, n_rows, n_cols, values_ptr, dtype, row_stride, stream))
+
+
+def snn_scan_forward(args: snn_scan_args, stream: int = 0) -> None:
+    _check(lib.snn_scan_forward(C.byref(args), stream))
+
+
+def snn_scan_backward(args: snn_scan_args, stream: int = 0) -> None:
+    _check(lib.snn_scan_backward(C.byref(args), stream))
 
 
 def ptr_array(ptrs: Sequence[Optional[int]]):

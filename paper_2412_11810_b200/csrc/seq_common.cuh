@@ -1,0 +1,101 @@
+// What the sequence-model operators share: element types, pairs of neighbouring values, and the 8-bit format of kept
+// activations.
+//
+// 8-bit format.  The last axis is cut into groups of 64 values (the last one may be shorter).  A group has one scale
+// byte c, standing for 2^(c - 127), and a code byte per value.  The scale is the smallest power of two at which the
+// largest magnitude of the group still rounds to a code: 127 for int8 (round to nearest, ties to even), 448 for e4m3.
+// A power of two costs int8 up to one of its seven bits against a free scale; in return scaling is exact, decoding
+// needs one multiplication, and codes do not depend on how a quotient is rounded.  c = 255 marks a group that holds an
+// infinity or a NaN: all of it decodes to NaN.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "../../include/snn.h"
+
+namespace snnk {
+
+constexpr int KEEP_GROUP = SNN_KEEP_GROUP;
+
+template <typename IO> struct Pair;
+template <> struct Pair<float> { using raw = float2; };
+template <> struct Pair<__nv_bfloat16> { using raw = __nv_bfloat162; };
+template <> struct Pair<__half> { using raw = __half2; };
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float2 to_f32(float2 v) { return v; }
+__device__ __forceinline__ float2 to_f32(__nv_bfloat162 v) { return __bfloat1622float2(v); }
+__device__ __forceinline__ float2 to_f32(__half2 v) { return __half22float2(v); }
+template <typename IO> __device__ __forceinline__ IO from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+__device__ __forceinline__ void set_raw(float2& r, float2 v) { r = v; }
+__device__ __forceinline__ void set_raw(__nv_bfloat162& r, float2 v) { r = __float22bfloat162_rn(v); }
+__device__ __forceinline__ void set_raw(__half2& r, float2 v) { r = __float22half2_rn(v); }
+
+// Values c and c + 1 of a row (`n_ok` of them exist: 0, 1 or 2); `vec`: the address is aligned for one access.
+template <typename IO>
+__device__ __forceinline__ float2 load_pair(const IO* row, int c, int n_ok, bool vec) {
+  if (n_ok == 2 && vec) return to_f32(*reinterpret_cast<const typename Pair<IO>::raw*>(row + c));
+  float2 v = make_float2(0.f, 0.f);
+  if (n_ok > 0) v.x = to_f32(row[c]);
+  if (n_ok > 1) v.y = to_f32(row[c + 1]);
+  return v;
+}
+template <typename IO>
+__device__ __forceinline__ void store_pair(IO* row, int c, int n_ok, bool vec, float2 v) {
+  if (n_ok == 2 && vec) {
+    typename Pair<IO>::raw r;
+    set_raw(r, v);
+    *reinterpret_cast<typename Pair<IO>::raw*>(row + c) = r;
+    return;
+  }
+  if (n_ok > 0) row[c] = from_f32<IO>(v.x);
+  if (n_ok > 1) row[c + 1] = from_f32<IO>(v.y);
+}
+
+// ---- 8-bit codes -------------------------------------------------------------------------------------------
+// Scale byte of a group whose largest magnitude has the bit pattern `top` (NaN sorts above infinity above the rest).
+__device__ __forceinline__ uint32_t keep_scale_byte(uint32_t top, int format) {
+  const int exponent = (int)(top >> 23);
+  const uint32_t fraction = top & 0x7fffffu;
+  if (exponent == 255) return 255u;
+  // top = 1.f x 2^(exponent - 127).  int8: 1.f x 64 is below 128.  e4m3: 1.f x 256 is at most 448 while 1.f <= 1.75, one
+  // scale up beyond that.
+  const int c = format == SNN_KEEP_INT8 ? exponent - 6 : exponent - 8 + (fraction > 0x600000u);
+  return (uint32_t)max(c, 0);
+}
+__device__ __forceinline__ float keep_scale_inverse(uint32_t c) { return __uint_as_float((254u - min(c, 253u)) << 23); }
+__device__ __forceinline__ float keep_scale_value(uint32_t c) {
+  return __uint_as_float(c == 0u ? 0x00400000u : c == 255u ? 0x7fc00000u : c << 23);
+}
+__device__ __forceinline__ uint32_t keep_encode2(float2 v, float inverse, int format) {   // two code bytes, low first
+  const float a = __fmul_rn(v.x, inverse), b = __fmul_rn(v.y, inverse);
+  if (format == SNN_KEEP_INT8) {
+    const int i = min(max(__float2int_rn(a), -127), 127), j = min(max(__float2int_rn(b), -127), 127);
+    return ((uint32_t)i & 255u) | (((uint32_t)j & 255u) << 8);
+  }
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+template <typename IO> __device__ __forceinline__ float largest_finite();
+template <> __device__ __forceinline__ float largest_finite<float>() { return __uint_as_float(0x7f7fffffu); }
+template <> __device__ __forceinline__ float largest_finite<__nv_bfloat16>() { return __uint_as_float(0x7f7f0000u); }
+template <> __device__ __forceinline__ float largest_finite<__half>() { return 65504.f; }
+// The values of two codes, within the range of type IO.
+template <typename IO>
+__device__ __forceinline__ float2 keep_decode2(uint32_t codes, float scale, int format) {
+  if (format == SNN_KEEP_INT8)
+    return make_float2(__fmul_rn((float)(int8_t)(codes & 255u), scale), __fmul_rn((float)(int8_t)((codes >> 8) & 255u), scale));
+  const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3)));
+  const float a = __fmul_rn(v.x, scale), b = __fmul_rn(v.y, scale), top = largest_finite<IO>();
+  return make_float2(fabsf(a) > top ? copysignf(top, a) : a, fabsf(b) > top ? copysignf(top, b) : b);   // NaN stays
+}
+__device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+}  // namespace snnk

@@ -1,0 +1,101 @@
+"""Refusals of the sequence-model operators: before anything is launched, so without a GPU."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import seq_reference as ref
+from paper_2412_11810_b200 import binding as sb
+
+torch = pytest.importorskip("torch")
+from paper_2412_11810_b200 import ops  # noqa: E402
+
+
+def _scan_args(**kw):
+    a = sb.snn_scan_args()
+    a.T, a.B, a.N = 4, 2, 8
+    for name in ("x", "gate", "h", "last", "states", "dh", "dx", "dgate", "dstate"):
+        setattr(a, name, 1 << 20)   # never read: every call below is refused first
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("change", [{"T": -1}, {"B": -1}, {"N": -1}, {"T": 1 << 30}, {"dtype": 3}, {"dtype": -1}, {"mode": 2},
+                                    {"x_format": 3}, {"gate_format": -1}, {"x_format": sb.SNN_KEEP_INT8}, {"gate": None}, {"x": None}])
+def test_scan_refuses_invalid_arguments(change):
+    for call in (sb.lib.snn_scan_forward, sb.lib.snn_scan_backward):
+        assert call(C.byref(_scan_args(**change)), None) == sb.SNN_ERR_INVALID_ARG
+
+
+def test_scan_refuses_missing_buffers():
+    assert sb.lib.snn_scan_forward(None, None) == sb.SNN_ERR_INVALID_ARG
+    assert sb.lib.snn_scan_backward(None, None) == sb.SNN_ERR_INVALID_ARG
+    assert sb.lib.snn_scan_forward(C.byref(_scan_args(h=None)), None) == sb.SNN_ERR_INVALID_ARG
+    # 8-bit copies are made only where states are kept
+    assert sb.lib.snn_scan_forward(C.byref(_scan_args(states=None, x_format=1, x_codes=256, x_scales=256)), None) == sb.SNN_ERR_INVALID_ARG
+    for name in ("dh", "dx", "dgate", "states"):
+        assert sb.lib.snn_scan_backward(C.byref(_scan_args(**{name: None})), None) == sb.SNN_ERR_INVALID_ARG
+    direct = _scan_args(mode=sb.SNN_SCAN_DIRECT, gate_format=sb.SNN_KEEP_INT8, gate_codes=256, gate_scales=256)
+    assert sb.lib.snn_scan_forward(C.byref(direct), None) == sb.SNN_ERR_UNSUPPORTED
+    assert sb.lib.snn_scan_backward(C.byref(direct), None) == sb.SNN_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("rows,cols,dtype,fmt", [(-1, 4, 0, 1), (4, -1, 0, 1), (4, 4, 3, 1), (4, 4, 0, 0), (4, 4, 0, 3), (4, 4, 0, 1)])
+def test_pack_refuses_invalid_arguments(rows, cols, dtype, fmt):
+    assert sb.lib.snn_activation_pack(None, dtype, rows, cols, 4, fmt, None, None, None) == sb.SNN_ERR_INVALID_ARG
+    assert sb.lib.snn_activation_unpack(None, None, fmt, rows, cols, None, dtype, 4, None) == sb.SNN_ERR_INVALID_ARG
+
+
+def test_sequence_operators_need_cuda_tensors():
+    x = torch.zeros(4, 2, 8)
+    for call in (lambda: ops.gated_scan(x, x), lambda: ops.gated_scan_step(x[0], x[0]), lambda: ops.pack_activation(x),
+                 lambda: ops.gated_scan_backward(None, x),
+                 lambda: ops.unpack_activation(ops.PackedActivation(x, x, "int8", torch.float32))):
+        with pytest.raises(ValueError):
+            call()
+
+
+def test_struct_sizes_match_the_header(tmp_path):
+    """The argument structs are spelled twice (include/snn.h and binding.py): same sizes and last offsets."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "s.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "%s/include/snn.h"\nint main(void) {\n'
+                   'printf("%%zu %%zu\\n", sizeof(snn_scan_args), offsetof(snn_scan_args, dstate));\n'
+                   'printf("%%d %%d\\n", SNN_KEEP_GROUP, SNN_SCAN_CHUNK); return 0; }\n' % root)
+    subprocess.run(["gcc", str(src), "-o", str(tmp_path / "s")], check=True)
+    out = subprocess.run([str(tmp_path / "s")], check=True, capture_output=True, text=True).stdout.split()
+    assert [int(v) for v in out] == [C.sizeof(sb.snn_scan_args), sb.snn_scan_args.dstate.offset, ops.KEEP_GROUP, ops.SCAN_CHUNK]
+
+
+# ---- the 64-bit reference itself ---------------------------------------------------------------------------------
+@pytest.mark.parametrize("mode", ["sigmoid", "direct"])
+def test_reference_gradients_against_differences(mode):
+    rng = np.random.default_rng(1)
+    T, B, N = 70, 2, 3
+    lengths = np.array([70, 41])
+    x, gate = rng.standard_normal((T, B, N)), rng.standard_normal((T, B, N))
+    gate = gate if mode == "sigmoid" else 0.9 * np.tanh(gate)
+    state, dh, dlast = rng.standard_normal((B, N)), rng.standard_normal((T, B, N)), rng.standard_normal((B, N))
+    r = ref.scan_backward(x, gate, state, lengths, mode, dh, dlast)
+
+    def loss(p):
+        f = ref.scan_forward(p[0], p[1], p[2], lengths, mode)
+        return (f["h"] * dh).sum() + (f["last"] * dlast).sum()
+
+    point = [x, gate, state]
+    for k, name in enumerate(("dx", "dgate", "dstate")):
+        v = rng.standard_normal(point[k].shape)
+        at = lambda s: [p + s * v if j == k else p for j, p in enumerate(point)]  # noqa: E731
+        slope = (loss(at(1e-6)) - loss(at(-1e-6))) / 2e-6
+        assert abs((r[name] * v).sum() - slope) <= 1e-7 * np.abs(r[name] * v).sum() + 1e-6
+
+
+def test_reference_eight_bits():
+    v = np.array([[127.0, 2.5, -0.49, 63.5], [448.0, 450.0, 17.0, 2.0 ** -10]])
+    q, s = ref.eight_bits(v, "int8")
+    assert np.array_equal(q[0], [127, 2, 0, 64]) and s[0, 0] == 127 and s[1, 0] == 129
+    q, s = ref.eight_bits(v, "e4m3")
+    assert np.array_equal(q, [[128, 2.5, -0.5, 64], [448, 448, 16, 0]]) and s[0, 0] == 126 and s[1, 0] == 128

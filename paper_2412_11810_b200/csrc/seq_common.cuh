@@ -39,21 +39,20 @@ __device__ __forceinline__ void set_raw(float2& r, float2 v) { r = v; }
 __device__ __forceinline__ void set_raw(__nv_bfloat162& r, float2 v) { r = __float22bfloat162_rn(v); }
 __device__ __forceinline__ void set_raw(__half2& r, float2 v) { r = __float22half2_rn(v); }
 
-// Values c and c + 1 of a row (`n_ok` of them exist: 0, 1 or 2); `vec`: the address is aligned for one access.
-template <typename IO>
-__device__ __forceinline__ float2 load_pair(const IO* row, int c, int n_ok, bool vec) {
-  if (n_ok == 2 && vec) return to_f32(*reinterpret_cast<const typename Pair<IO>::raw*>(row + c));
-  float2 v = make_float2(0.f, 0.f);
-  if (n_ok > 0) v.x = to_f32(row[c]);
-  if (n_ok > 1) v.y = to_f32(row[c + 1]);
-  return v;
+// Values c and c + 1 of a row, of which n_ok (0, 1 or 2) exist.  The loads are unconditional, so that many of them are in
+// flight at once: a value that does not exist is read from another place of the row and means nothing.  PAIRS: an access
+// of two values is aligned, and rows have an even number of them.
+template <bool PAIRS, typename IO>
+__device__ __forceinline__ float2 load_pair(const IO* row, int c, int n_ok) {
+  if (PAIRS) return to_f32(*reinterpret_cast<const typename Pair<IO>::raw*>(row + (n_ok ? c : 0)));
+  return make_float2(to_f32(row[n_ok ? c : 0]), to_f32(row[n_ok == 2 ? c + 1 : 0]));
 }
-template <typename IO>
-__device__ __forceinline__ void store_pair(IO* row, int c, int n_ok, bool vec, float2 v) {
-  if (n_ok == 2 && vec) {
+template <bool PAIRS, typename IO>
+__device__ __forceinline__ void store_pair(IO* row, int c, int n_ok, float2 v) {
+  if (PAIRS) {
     typename Pair<IO>::raw r;
     set_raw(r, v);
-    *reinterpret_cast<typename Pair<IO>::raw*>(row + c) = r;
+    if (n_ok) *reinterpret_cast<typename Pair<IO>::raw*>(row + c) = r;
     return;
   }
   if (n_ok > 0) row[c] = from_f32<IO>(v.x);
@@ -62,24 +61,32 @@ __device__ __forceinline__ void store_pair(IO* row, int c, int n_ok, bool vec, f
 
 // ---- 8-bit codes -------------------------------------------------------------------------------------------
 // Scale byte of a group whose largest magnitude has the bit pattern `top` (NaN sorts above infinity above the rest).
-__device__ __forceinline__ uint32_t keep_scale_byte(uint32_t top, int format) {
+template <int FORMAT> __device__ __forceinline__ uint32_t keep_scale_byte(uint32_t top) {
   const int exponent = (int)(top >> 23);
   const uint32_t fraction = top & 0x7fffffu;
   if (exponent == 255) return 255u;
   // top = 1.f x 2^(exponent - 127).  int8: 1.f x 64 is below 128.  e4m3: 1.f x 256 is at most 448 while 1.f <= 1.75, one
   // scale up beyond that.
-  const int c = format == SNN_KEEP_INT8 ? exponent - 6 : exponent - 8 + (fraction > 0x600000u);
+  const int c = FORMAT == SNN_KEEP_INT8 ? exponent - 6 : exponent - 8 + (fraction > 0x600000u);
   return (uint32_t)max(c, 0);
 }
 __device__ __forceinline__ float keep_scale_inverse(uint32_t c) { return __uint_as_float((254u - min(c, 253u)) << 23); }
 __device__ __forceinline__ float keep_scale_value(uint32_t c) {
   return __uint_as_float(c == 0u ? 0x00400000u : c == 255u ? 0x7fc00000u : c << 23);
 }
-__device__ __forceinline__ uint32_t keep_encode2(float2 v, float inverse, int format) {   // two code bytes, low first
+// Two code bytes, low first.  `top` is the group's largest magnitude, as in keep_scale_byte.
+template <int FORMAT> __device__ __forceinline__ uint32_t keep_encode2(float2 v, float inverse, uint32_t top) {
   const float a = __fmul_rn(v.x, inverse), b = __fmul_rn(v.y, inverse);
-  if (format == SNN_KEEP_INT8) {
-    const int i = min(max(__float2int_rn(a), -127), 127), j = min(max(__float2int_rn(b), -127), 127);
-    return ((uint32_t)i & 255u) | (((uint32_t)j & 255u) << 8);
+  if (FORMAT == SNN_KEEP_INT8) {
+    // adding 1.5 x 2^23 rounds to an integer (nearest even) and leaves it in the low bits: no conversion instructions,
+    // which run at a quarter of the rate
+    const float magic = 12582912.f;
+    float i = __fadd_rn(a, magic), j = __fadd_rn(b, magic);
+    if ((top & 0x7fffffu) >= 0x7f0000u) {   // only then can a value round to 128
+      i = fminf(fmaxf(i, magic - 127.f), magic + 127.f);
+      j = fminf(fmaxf(j, magic - 127.f), magic + 127.f);
+    }
+    return __byte_perm(__float_as_uint(i), __float_as_uint(j), 0x0040) & 0xffffu;
   }
   return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
@@ -88,14 +95,22 @@ template <> __device__ __forceinline__ float largest_finite<float>() { return __
 template <> __device__ __forceinline__ float largest_finite<__nv_bfloat16>() { return __uint_as_float(0x7f7f0000u); }
 template <> __device__ __forceinline__ float largest_finite<__half>() { return 65504.f; }
 // The values of two codes, within the range of type IO.
-template <typename IO>
-__device__ __forceinline__ float2 keep_decode2(uint32_t codes, float scale, int format) {
-  if (format == SNN_KEEP_INT8)
-    return make_float2(__fmul_rn((float)(int8_t)(codes & 255u), scale), __fmul_rn((float)(int8_t)((codes >> 8) & 255u), scale));
+template <typename IO, int FORMAT> __device__ __forceinline__ float2 keep_decode2(uint32_t codes, float scale) {
+  if (FORMAT == SNN_KEEP_INT8) {   // code + 128 in the low bits of 2^23: again no conversion instructions
+    const uint32_t u = codes ^ 0x8080u;
+    const float i = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650));
+    const float j = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7651));
+    return make_float2(__fmul_rn(i - 8388736.f, scale), __fmul_rn(j - 8388736.f, scale));
+  }
   const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3)));
   const float a = __fmul_rn(v.x, scale), b = __fmul_rn(v.y, scale), top = largest_finite<IO>();
   return make_float2(fabsf(a) > top ? copysignf(top, a) : a, fabsf(b) > top ? copysignf(top, b) : b);   // NaN stays
 }
-__device__ __forceinline__ uint32_t magnitude_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// The larger magnitude of two values; NaN if one of them is.
+__device__ __forceinline__ float larger_magnitude(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return m;
+}
 
 }  // namespace snnk

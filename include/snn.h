@@ -411,6 +411,46 @@ typedef struct {
 snn_status snn_scan_forward(const snn_scan_args* args, void* stream);
 snn_status snn_scan_backward(const snn_scan_args* args, void* stream);
 
+/* Soft-max cross entropy over a large vocabulary, with the readout product inside (the readout and loss of snn_train_step
+ * for many classes: z = scale * x W_out, x [rows][dim], W_out [dim][classes]) and without storing z:
+ *   lse_n = log sum_v exp(z_nv),   row_loss_n = lse_n - z_{n, target_n},   loss = mean of row_loss over the rows that count
+ *   dx = dz W_out^T scale,   dW_out = x^T dz scale,   dz_nv = dloss (exp(z_nv - lse_n) - [v = target_n]) / (rows that count)
+ * A row with target = ignore_index does not count: its row_loss and lse are 0, its dx is 0, whatever x holds there.  Any
+ * other target outside [0, classes) makes that row_loss and the loss NaN and counts like an ignored row in the gradients;
+ * it is never used as an index.  If no row counts, loss and gradients are 0.
+ * The products run on the tensor cores.  bf16 and fp16 operands are used as they are; fp32 ones are split into three bf16
+ * parts (24 bits in all) of which the six products that matter are summed.  Sums are fp32.  In the backward pass the
+ * derivatives by the logits exist one piece of the vocabulary at a time, rounded to the operands' type (fp32: in three
+ * parts), in the workspace.
+ * W_out is stored by feature (SNN_W_BY_FEATURE: [dim][classes] as everywhere in this library) or by class
+ * (SNN_W_BY_CLASS: [classes][dim], the transpose, as in an embedding table); w_stride is the distance of its rows. dw has
+ * the same layout with its own stride. */
+typedef enum { SNN_W_BY_FEATURE = 0, SNN_W_BY_CLASS = 1 } snn_w_layout;
+typedef struct {
+  int32_t rows, dim, classes;  /* rows >= 0, dim >= 1, classes >= 1; each < 2^30                        */
+  int32_t dtype;               /* snn_dtype of x, w, dx, dw                                             */
+  const void* x; int64_t x_stride;   /* [rows][dim], rows x_stride elements apart                       */
+  const void* w; int64_t w_stride;
+  int32_t w_layout;            /* snn_w_layout                                                          */
+  int32_t target_bits;         /* 32 or 64: targets are int32 or int64                                  */
+  const void* targets;         /* [rows], device                                                        */
+  int64_t ignore_index;
+  float scale;
+  float* row_loss;             /* [rows], forward; may be NULL                                          */
+  float* lse;                  /* [rows]; written by the forward pass, read by the backward pass        */
+  float* loss;                 /* one value, forward                                                    */
+  float dloss;                 /* backward: gradient of the loss, times *dloss_device if that is given  */
+  const float* dloss_device;
+  void* dx; int64_t dx_stride; /* backward                                                              */
+  void* dw; int64_t dw_stride;
+  void* workspace; size_t workspace_bytes;   /* device, 256-byte aligned; calls that may overlap in time need
+                                                workspaces of their own                                 */
+} snn_vocab_loss_args;
+/* Bytes of workspace that the forward (backward = 0) or backward pass (1) with these arguments needs. */
+snn_status snn_vocab_loss_workspace(const snn_vocab_loss_args* args, int32_t backward, size_t* bytes);
+snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* args, void* stream);
+snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

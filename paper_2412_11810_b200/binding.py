@@ -23,6 +23,7 @@ SNN_INPUT_BITS, SNN_INPUT_DENSE = 0, 1
 SNN_DTYPE_FP32, SNN_DTYPE_BF16, SNN_DTYPE_FP16 = 0, 1, 2
 SNN_KEEP_RAW, SNN_KEEP_INT8, SNN_KEEP_E4M3, SNN_KEEP_GROUP = 0, 1, 2, 64
 SNN_SCAN_SIGMOID, SNN_SCAN_DIRECT, SNN_SCAN_CHUNK = 0, 1, 64
+SNN_W_BY_FEATURE, SNN_W_BY_CLASS = 0, 1
 SNN_FLAG_INPUT_ON_HOST, SNN_FLAG_FORWARD_ONLY, SNN_FLAG_TIME_PHASES = 1, 2, 4
 SNN_FLAG_BACKWARD_LAYER_BY_LAYER, SNN_FLAG_BACKWARD_WAVEFRONT = 8, 16
 SNN_FLAG_REFORWARD_PER_STEP = 32
@@ -44,7 +45,7 @@ EXPORTS = ["snn_create", "snn_destroy", "snn_alpha", "snn_workspace_query", "snn
            "snn_memory_stats_get", "snn_last_error", "snn_plan", "snn_compact_spikes", "snn_get_event_layout",
            "snn_phase_times_get", "snn_train_step_static", "snn_suggest_ckpt", "snn_selftest_wait_timeout",
            "snn_debug_checks_enabled", "snn_activation_pack", "snn_activation_unpack", "snn_scan_forward",
-           "snn_scan_backward"]
+           "snn_scan_backward", "snn_vocab_loss_workspace", "snn_vocab_loss_forward", "snn_vocab_loss_backward"]
 SNN_STATIC_WORKSPACE_BYTES = 32 << 20
 
 
@@ -100,6 +101,15 @@ class snn_scan_args(C.Structure):
                 ("dgate_stride", C.c_int64 * 2), ("dstate", C.c_void_p)]
 
 
+class snn_vocab_loss_args(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("dim", C.c_int32), ("classes", C.c_int32), ("dtype", C.c_int32), ("x", C.c_void_p),
+                ("x_stride", C.c_int64), ("w", C.c_void_p), ("w_stride", C.c_int64), ("w_layout", C.c_int32),
+                ("target_bits", C.c_int32), ("targets", C.c_void_p), ("ignore_index", C.c_int64), ("scale", C.c_float),
+                ("row_loss", C.c_void_p), ("lse", C.c_void_p), ("loss", C.c_void_p), ("dloss", C.c_float),
+                ("dloss_device", C.c_void_p), ("dx", C.c_void_p), ("dx_stride", C.c_int64), ("dw", C.c_void_p),
+                ("dw_stride", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2412_11810_b200/build.py` "
@@ -137,6 +147,9 @@ def _load() -> C.CDLL:
                                           C.c_int32, C.c_int64, C.c_void_p]
     lib.snn_scan_forward.argtypes = [C.POINTER(snn_scan_args), C.c_void_p]
     lib.snn_scan_backward.argtypes = [C.POINTER(snn_scan_args), C.c_void_p]
+    lib.snn_vocab_loss_workspace.argtypes = [C.POINTER(snn_vocab_loss_args), C.c_int32, C.POINTER(C.c_size_t)]
+    lib.snn_vocab_loss_forward.argtypes = [C.POINTER(snn_vocab_loss_args), C.c_void_p]
+    lib.snn_vocab_loss_backward.argtypes = [C.POINTER(snn_vocab_loss_args), C.c_void_p]
     return lib
 
 
@@ -265,6 +278,20 @@ def snn_scan_forward(args: snn_scan_args, stream: int = 0) -> None:
 
 def snn_scan_backward(args: snn_scan_args, stream: int = 0) -> None:
     _check(lib.snn_scan_backward(C.byref(args), stream))
+
+
+def snn_vocab_loss_workspace(args: snn_vocab_loss_args, backward: bool) -> int:
+    n = C.c_size_t()
+    _check(lib.snn_vocab_loss_workspace(C.byref(args), int(backward), C.byref(n)))
+    return n.value
+
+
+def snn_vocab_loss_forward(args: snn_vocab_loss_args, stream: int = 0) -> None:
+    _check(lib.snn_vocab_loss_forward(C.byref(args), stream))
+
+
+def snn_vocab_loss_backward(args: snn_vocab_loss_args, stream: int = 0) -> None:
+    _check(lib.snn_vocab_loss_backward(C.byref(args), stream))
 
 
 def ptr_array(ptrs: Sequence[Optional[int]]):

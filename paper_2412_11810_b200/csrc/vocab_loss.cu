@@ -1,0 +1,772 @@
+// Soft-max cross entropy over a large vocabulary with the readout product inside, and its gradients (include/snn.h,
+// "sequence-model operators").  The logits never reach memory: the forward pass reduces every 256 x 256 tile of them to a
+// maximum and a sum per row while it leaves tensor memory, the backward pass recomputes the tiles, turns them into
+// derivatives dz on the way out and multiplies those, one piece of the vocabulary at a time, by w and by x.
+//
+// Everything heavy is one persistent kernel on pairs of SMs (umma.cuh) with four epilogues:
+//   STATS   z tile -> per row (maximum, sum of exponentials), the target's logit
+//   GRAD    z tile -> dz tile, to memory through shared memory and TMA
+//   DX      dz w^T, fp32, added to what earlier pieces left (the contraction may be split; parts are joined at the end)
+//   DW      x^T dz, scaled and rounded
+// Work per pass: 2 rows dim classes for STATS, three times that for the backward pass (one of them the recomputation).
+#include <algorithm>
+#include <cmath>
+#include <mutex>
+
+#include "seq_common.cuh"
+#include "umma.cuh"
+
+using namespace snnk;
+
+namespace {
+
+constexpr uint32_t VL_TIMEOUT = 1u;               // status bit: a bounded wait ran out
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int VL_EPILOGUE_WARPS = 4;
+constexpr int VL_THREADS = 32 * (2 + VL_EPILOGUE_WARPS);
+constexpr uint32_t VL_STORE_BYTES = UM_HALF * 128;           // one staged block of dz: 128 rows x 64 values
+constexpr size_t VL_SMEM = 1024 + (size_t)UM_STAGES * UM_STAGE_BYTES + 2 * VL_STORE_BYTES + 256;
+constexpr float FP16_DZ_SCALE = 16384.f;   // dz / (gradient of the row loss) lies in [-1, 1]; fp16 keeps small values better after this
+constexpr size_t PIECE_BYTES = (size_t)256 << 20;            // dz held at a time
+constexpr int MAX_SPLITS = 32;
+
+enum Epilogue { STATS, GRAD, DX, DW };
+
+struct ProductParams {
+  CUtensorMap a, b, out;      // out: GRAD only
+  int tiles_m, tiles_n;       // 256 x 256 tiles; m is the fastest in the order of work for STATS, GRAD and DX, n for DW
+  int kblocks, splits;        // 64-deep blocks of the contraction; DX: parts of it
+  int n_pairs;                // products of operand planes: 1, or 6 for fp32 operands in three bf16 planes
+  uint32_t pair_a, pair_b;    // their planes, four bits each, the smallest products first
+  int a0, b0, bk0;            // first row of A and of B, first k of B (A's k starts at 0)
+  int m, n;                   // rows of A and of B that exist from there on
+  bool bf16;
+  // STATS and GRAD
+  const void* targets;
+  int target_bits;
+  int64_t ignore_index;
+  int classes;
+  float z_scale;              // times log2 e: exponents of 2
+  float2* partial;            // [tile_n][rows]
+  float* target_z;            // [rows], in units of log 2
+  const float* lse;
+  float dz_scale;
+  int planes;
+  // DX and DW
+  float* acc;                 // DX: [splits][m][n_pitch]
+  int64_t acc_split;
+  int acc_pitch;
+  bool accumulate;
+  void* dw;
+  int64_t dw_stride;
+  int dw_dtype;
+  const float* alpha;         // DW: factor, from the device
+  uint32_t* status;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// The target of a row, or -1 if it does not count, -2 if it is not a class.
+__device__ __forceinline__ int target_of(const void* targets, int bits, int64_t ignore, int classes, int row) {
+  const int64_t t = bits == 64 ? reinterpret_cast<const int64_t*>(targets)[row] : (int64_t) reinterpret_cast<const int32_t*>(targets)[row];
+  if (t == ignore) return -1;
+  return t >= 0 && t < classes ? (int)t : -2;
+}
+
+struct Barriers {
+  uint64_t full[UM_STAGES], empty[UM_STAGES];   // full: used in the even block only
+  uint64_t acc_full[2], acc_empty[2];           // acc_empty: used in the even block only
+  uint32_t tmem;
+  uint32_t gave_up;
+};
+
+// A bounded wait that also ends when another role of this block gave up.
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Barriers& s, uint32_t* status) {
+  for (uint32_t i = 0; i < MBAR_WAIT_LIMIT; ++i) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((i & 63u) == 63u && *reinterpret_cast<volatile uint32_t*>(&s.gave_up)) return false;
+  }
+  *reinterpret_cast<volatile uint32_t*>(&s.gave_up) = 1u;
+  atomicOr(status, VL_TIMEOUT);
+  return false;
+}
+
+template <bool MN_MAJOR>
+__device__ __forceinline__ void load_operand(unsigned char* smem, const CUtensorMap* map, int row, int k, int plane, uint32_t bar) {
+  if (MN_MAJOR) {
+    tma_pair_load_3d(smem, map, row, k, plane, bar);
+    tma_pair_load_3d(smem + UM_KB * 128, map, row + 64, k, plane, bar);
+  } else {
+    tma_pair_load_3d(smem, map, k, row, plane, bar);
+  }
+}
+
+// the i-th unit of work of a pair: its tile and its part of the contraction
+struct Unit {
+  int m, n, split, kb0, kbs;
+};
+template <int EPI> __device__ __forceinline__ Unit unit_of(const ProductParams& p, int u) {
+  Unit w;
+  if (EPI == DW) {
+    w.n = u % p.tiles_n; w.m = u / p.tiles_n; w.split = 0;
+  } else {
+    w.m = u % p.tiles_m;
+    const int v = u / p.tiles_m;
+    w.n = v % p.tiles_n; w.split = v / p.tiles_n;
+  }
+  w.kb0 = (int)((int64_t)p.kblocks * w.split / p.splits);
+  w.kbs = (int)((int64_t)p.kblocks * (w.split + 1) / p.splits) - w.kb0;
+  return w;
+}
+
+template <int EPI, bool A_MN, bool B_MN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) product_kernel(const __grid_constant__ ProductParams p) {
+  extern __shared__ unsigned char s_raw[];
+  unsigned char* const s_base = s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u);
+  unsigned char* const s_store = s_base + (size_t)UM_STAGES * UM_STAGE_BYTES;
+  Barriers& s = *reinterpret_cast<Barriers*>(s_store + 2 * VL_STORE_BYTES);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t rank = cluster_rank();
+  const int pair = blockIdx.x >> 1, n_pairs_sm = gridDim.x >> 1;
+  const int units = p.tiles_m * p.tiles_n * p.splits;
+
+  if (tid == 0) {
+    for (int i = 0; i < UM_STAGES; ++i) {
+      mbar_init(&s.full[i], 1);
+      mbar_init(&s.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s.acc_full[i], 1);
+      mbar_init(&s.acc_empty[i], 2 * VL_EPILOGUE_WARPS);
+    }
+    s.gave_up = 0;
+    mbar_fence_init();
+  }
+  if (warp == 1) pair_tmem_alloc(&s.tmem, UM_TMEM_COLS);
+  tcgen05_before_sync();
+  cluster_sync_all();
+  tcgen05_after_sync();
+  const uint32_t tmem = s.tmem;
+
+  if (warp == 0) {
+    if (lane == 0) {   // loads: this block's halves of A and B, announced to the even block's barrier
+      int it = 0;
+      bool ok = true;
+      for (int u = pair; u < units && ok; u += n_pairs_sm) {
+        const Unit w = unit_of<EPI>(p, u);
+        const int row_a = p.a0 + w.m * UM_TILE + (int)rank * UM_HALF, row_b = p.b0 + w.n * UM_TILE + (int)rank * UM_HALF;
+        for (int q = 0; q < p.n_pairs && ok; ++q) {
+          const int plane_a = (p.pair_a >> (4 * q)) & 15, plane_b = (p.pair_b >> (4 * q)) & 15;
+          for (int kb = 0; kb < w.kbs; ++kb, ++it) {
+            const int st = it % UM_STAGES;
+            if (it >= UM_STAGES && !(ok = wait_for(&s.empty[st], (uint32_t)(it / UM_STAGES - 1) & 1u, s, p.status))) break;
+            unsigned char* const at = s_base + (size_t)st * UM_STAGE_BYTES;
+            if (rank == 0) mbar_arrive_expect_tx(&s.full[st], 2 * UM_STAGE_BYTES);
+            const uint32_t bar = peer_address(smem_u32(&s.full[st]), 0);
+            const int k = (w.kb0 + kb) * UM_KB;
+            load_operand<A_MN>(at, &p.a, row_a, k, plane_a, bar);
+            load_operand<B_MN>(at + UM_OPERAND_BYTES, &p.b, row_b, p.bk0 + k, plane_b, bar);
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {   // products, of both blocks
+      const uint32_t idesc = f16_instruction(p.bf16, A_MN, B_MN);
+      int it = 0, tile = 0;
+      bool ok = true;
+      for (int u = pair; u < units && ok; u += n_pairs_sm, ++tile) {
+        const Unit w = unit_of<EPI>(p, u);
+        const int buf = tile & 1;
+        if (tile >= 2 && !(ok = wait_for(&s.acc_empty[buf], (uint32_t)(tile / 2 - 1) & 1u, s, p.status))) break;
+        tcgen05_after_sync();
+        const uint32_t acc = tmem + (uint32_t)buf * UM_TILE;
+        const int n_it = p.n_pairs * w.kbs;
+        for (int i = 0; i < n_it; ++i, ++it) {
+          const int st = it % UM_STAGES;
+          if (!(ok = wait_for(&s.full[st], (uint32_t)(it / UM_STAGES) & 1u, s, p.status))) break;
+          tcgen05_after_sync();
+          const uint32_t at = smem_u32(s_base + (size_t)st * UM_STAGE_BYTES);
+#pragma unroll
+          for (int j = 0; j < UM_KB / 16; ++j)
+            pair_mma_f16(acc, operand_descriptor<A_MN>(at + j * kstep_bytes<A_MN>()),
+                         operand_descriptor<B_MN>(at + UM_OPERAND_BYTES + j * kstep_bytes<B_MN>()), idesc, i > 0 || j > 0);
+          pair_commit(&s.empty[st]);
+        }
+        if (ok) pair_commit(&s.acc_full[buf]);
+      }
+    }
+  } else {
+    // ---- epilogue: a thread has one row of this block's half of the tile
+    const int quarter = warp & 3, row_in_block = quarter * 32 + lane;
+    const float alpha = EPI == DW ? *p.alpha : 0.f;
+    int tile = 0;
+    bool ok = true;
+    int store_buf = 0;
+    for (int u = pair; u < units && ok; u += n_pairs_sm, ++tile) {
+      const Unit w = unit_of<EPI>(p, u);
+      const int buf = tile & 1;
+      ok = __all_sync(0xffffffffu, wait_for(&s.acc_full[buf], (uint32_t)(tile / 2) & 1u, s, p.status));
+      if (!ok) break;
+      tcgen05_after_sync();
+      const uint32_t acc = tmem + (uint32_t)buf * UM_TILE + ((uint32_t)(32 * quarter) << 16);
+      const int block_row0 = w.m * UM_TILE + (int)rank * UM_HALF;
+      const int row = block_row0 + row_in_block;          // within A's rows
+      const int col0 = w.n * UM_TILE, cols = min(p.n - col0, UM_TILE);
+      const bool row_on = row < p.m;
+      if constexpr (EPI == STATS) {
+        const int target = row_on ? target_of(p.targets, p.target_bits, p.ignore_index, p.classes, row) - (p.b0 + col0) : -1;
+        float top = -INFINITY, sum = 0.f;
+        for (int c = 0; c < cols; c += 32) {
+          float v[32];
+          tmem_load_32(acc + c, v);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = v[j] * p.z_scale;
+          if (target >= c && target < c + 32) {
+            float z = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) z = c + j == target ? v[j] : z;
+            p.target_z[row] = z;
+          }
+          if (cols - c < 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = c + j < cols ? v[j] : -INFINITY;
+          }
+          float m = top;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) m = fmaxf(m, v[j]);
+          const float at = m == -INFINITY ? 0.f : m;
+          float part = 0.f;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) part += exp2_fast(v[j] - at);
+          sum = sum * exp2_fast(top - at) + part;
+          top = m;
+        }
+        if (row_on) p.partial[(int64_t)w.n * p.m + row] = make_float2(top, sum);
+      }
+      if constexpr (EPI == GRAD) {
+        const int target = row_on ? target_of(p.targets, p.target_bits, p.ignore_index, p.classes, row) : -1;
+        const bool counts = target >= 0;
+        const int target_col = target - (p.b0 + col0);
+        const float lse2 = counts ? p.lse[row] * LOG2E : 0.f;
+        for (int c = 0; c < cols; c += 64) {
+          float v[64];
+          tmem_load_32(acc + c, *reinterpret_cast<float(*)[32]>(&v[0]));
+          tmem_load_32(acc + c + 32, *reinterpret_cast<float(*)[32]>(&v[32]));
+#pragma unroll
+          for (int j = 0; j < 64; ++j) v[j] = counts ? exp2_fast(fmaf(v[j], p.z_scale, -lse2)) : 0.f;
+          if (counts && target_col >= c && target_col < c + 64) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j) v[j] = c + j == target_col ? v[j] - 1.f : v[j];
+          }
+          for (int plane = 0; plane < p.planes; ++plane) {
+            // the buffer's previous store has to have read it
+            if (tid == 64) bulk_read_done<1>();
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * VL_EPILOGUE_WARPS) : "memory");
+            unsigned char* const out = s_store + store_buf * VL_STORE_BYTES + row_in_block * 128;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {   // 16-byte pieces, swizzled as the tensor map says
+              uint32_t q[4];
+#pragma unroll
+              for (int h = 0; h < 4; ++h) {
+                float &lo = v[8 * g + 2 * h], &hi = v[8 * g + 2 * h + 1];
+                if (p.bf16) {
+                  const __nv_bfloat162 r = __float22bfloat162_rn(make_float2(lo, hi));
+                  q[h] = *reinterpret_cast<const uint32_t*>(&r);
+                  if (p.planes > 1) {   // what is left for the next plane
+                    const float2 f = __bfloat1622float2(r);
+                    lo -= f.x;
+                    hi -= f.y;
+                  }
+                } else {
+                  const __half2 r = __float22half2_rn(make_float2(lo * p.dz_scale, hi * p.dz_scale));
+                  q[h] = *reinterpret_cast<const uint32_t*>(&r);
+                }
+              }
+              *reinterpret_cast<uint4*>(out + ((g ^ (row_in_block & 7)) << 4)) = make_uint4(q[0], q[1], q[2], q[3]);
+            }
+            fence_proxy_async_smem();
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * VL_EPILOGUE_WARPS) : "memory");
+            if (tid == 64 && block_row0 < p.m) tma_store_3d(&p.out, col0 + c, block_row0, plane, s_store + store_buf * VL_STORE_BYTES);
+            if (tid == 64) bulk_commit();
+            store_buf ^= 1;
+          }
+        }
+      }
+      if constexpr (EPI == DX) {
+        for (int c = 0; c < cols; c += 32) {
+          float v[32];
+          tmem_load_32(acc + c, v);
+          if (row_on) {
+            float* const out = p.acc + w.split * p.acc_split + (int64_t)row * p.acc_pitch + col0 + c;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {   // acc_pitch is a multiple of 4: whole groups
+              if (c + j < cols) {
+                float4 f = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                if (p.accumulate) {
+                  const float4 o = *reinterpret_cast<const float4*>(out + j);
+                  f = make_float4(f.x + o.x, f.y + o.y, f.z + o.z, f.w + o.w);
+                }
+                *reinterpret_cast<float4*>(out + j) = f;
+              }
+            }
+          }
+        }
+      }
+      if constexpr (EPI == DW) {
+        for (int c = 0; c < cols; c += 32) {
+          float v[32];
+          tmem_load_32(acc + c, v);
+          if (!row_on) continue;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] *= alpha;
+          const int64_t at = (int64_t)row * p.dw_stride + col0 + c;
+          if (p.dw_dtype == SNN_DTYPE_FP32) {
+            float* const out = (float*)p.dw + at;
+            if (cols - c >= 32 && ((uintptr_t)out & 15) == 0) {
+#pragma unroll
+              for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(out + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (c + j < cols) out[j] = v[j];
+            }
+          } else {
+            uint16_t* const out = (uint16_t*)p.dw + at;
+            uint32_t q[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              if (p.dw_dtype == SNN_DTYPE_BF16) {
+                const __nv_bfloat162 r = __float22bfloat162_rn(make_float2(v[2 * j], v[2 * j + 1]));
+                q[j] = *reinterpret_cast<const uint32_t*>(&r);
+              } else {
+                const __half2 r = __float22half2_rn(make_float2(v[2 * j], v[2 * j + 1]));
+                q[j] = *reinterpret_cast<const uint32_t*>(&r);
+              }
+            }
+            if (cols - c >= 32 && ((uintptr_t)out & 15) == 0) {
+#pragma unroll
+              for (int j = 0; j < 16; j += 4) *reinterpret_cast<uint4*>(out + 2 * j) = make_uint4(q[j], q[j + 1], q[j + 2], q[j + 3]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 32; ++j)
+                if (c + j < cols) out[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+            }
+          }
+        }
+      }
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_at(peer_address(smem_u32(&s.acc_empty[buf]), 0));
+    }
+    if (EPI == GRAD && tid == 64) bulk_done();
+  }
+  // After a wait that ran out, copies and products may still be under way: give them time to land.
+  __syncwarp();
+  if (*reinterpret_cast<volatile uint32_t*>(&s.gave_up))
+    for (int i = 0; i < 100; ++i) __nanosleep(20000);
+  tcgen05_before_sync();
+  cluster_sync_all();
+  if (warp == 1) pair_tmem_dealloc(tmem, UM_TMEM_COLS);
+}
+
+// ---- around the products ---------------------------------------------------------------------------------------
+
+// Operand rows to 16-bit planes: a copy with an aligned pitch, or fp32 values in three bf16 parts.  With targets: rows that
+// do not count become zeros (what they hold must not reach the sums over rows).
+template <typename IO>
+__global__ void __launch_bounds__(256) stage_operand_kernel(const IO* src, int64_t stride, int rows, int cols, uint16_t* dst, int pitch,
+                                                            int64_t plane, const void* targets, int bits, int64_t ignore, int classes) {
+  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+    const bool on = !targets || target_of(targets, bits, ignore, classes, (int)row) >= 0;
+    for (int c = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 2; c < pitch; c += (int)(gridDim.x * blockDim.x) * 2) {
+      IO v[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) v[j] = on && c + j < cols ? src[row * stride + c + j] : from_f32<IO>(0.f);
+      uint16_t* const out = dst + row * pitch + c;
+      if constexpr (sizeof(IO) == 4) {
+        float2 f = make_float2(v[0], v[1]);
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          const __nv_bfloat162 r = __float22bfloat162_rn(f);
+          *reinterpret_cast<__nv_bfloat162*>(out + part * plane) = r;
+          const float2 g = __bfloat1622float2(r);
+          f = make_float2(f.x - g.x, f.y - g.y);
+        }
+      } else {
+        *reinterpret_cast<IO*>(out) = v[0];
+        *reinterpret_cast<IO*>(out + 1) = v[1];
+      }
+    }
+  }
+}
+
+// Sums of a block's values, the same in every thread; `warp_sums` has 32 entries.
+__device__ __forceinline__ double block_sum(double v, double* warp_sums) {
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double t = 0;
+  for (int w = 0; w < (int)blockDim.x / 32; ++w) t += warp_sums[w];
+  return t;
+}
+
+// The tiles' (maximum, sum) of a row joined: log-sum-exp and loss of the row.  32 rows per block, 8 threads per row.
+__global__ void __launch_bounds__(256) row_loss_kernel(const float2* partial, int tiles, const float* target_z, int rows, const void* targets,
+                                                       int bits, int64_t ignore, int classes, float* lse, float* row_loss, float* row_out,
+                                                       const uint32_t* status) {
+  __shared__ float2 s_part[8][32];
+  const int row = blockIdx.x * 32 + threadIdx.x % 32, part = threadIdx.x / 32;
+  float top = -INFINITY, sum = 0.f;
+  if (row < rows) {
+    for (int t = part; t < tiles; t += 8) {
+      const float2 v = partial[(int64_t)t * rows + row];
+      const float m = fmaxf(top, v.x), at = m == -INFINITY ? 0.f : m;
+      sum = sum * exp2f(top - at) + v.y * exp2f(v.x - at);
+      top = m;
+    }
+  }
+  s_part[part][threadIdx.x % 32] = make_float2(top, sum);
+  __syncthreads();
+  if (part == 0 && row < rows) {
+    for (int q = 1; q < 8; ++q) {
+      const float2 v = s_part[q][threadIdx.x];
+      const float m = fmaxf(top, v.x), at = m == -INFINITY ? 0.f : m;
+      sum = sum * exp2f(top - at) + v.y * exp2f(v.x - at);
+      top = m;
+    }
+    const int target = target_of(targets, bits, ignore, classes, row);
+    float l = (top + log2f(sum)) * LN2, loss = l - (target >= 0 ? target_z[row] * LN2 : 0.f);
+    if (target < 0) l = 0.f, loss = target == -1 ? 0.f : __uint_as_float(0x7fc00000u);
+    if (*status & VL_TIMEOUT) loss = l = __uint_as_float(0x7fc00000u);
+    lse[row] = l;
+    row_loss[row] = loss;
+    if (row_out) row_out[row] = loss;
+  }
+}
+
+// One block.  The mean of row_loss over the rows that count (loss != NULL), and the factor of the gradients (alpha != NULL).
+__global__ void __launch_bounds__(1024) mean_kernel(const float* row_loss, int rows, const void* targets, int bits, int64_t ignore, int classes,
+                                                    float* loss, float* alpha, float factor, const float* dloss) {
+  __shared__ double warp_sums[32];
+  double sum = 0, count = 0;
+  for (int r = threadIdx.x; r < rows; r += blockDim.x) {
+    if (loss) sum += (double)row_loss[r];
+    count += target_of(targets, bits, ignore, classes, r) >= 0;
+  }
+  if (loss) sum = block_sum(sum, warp_sums);
+  count = block_sum(count, warp_sums);
+  if (threadIdx.x == 0) {
+    if (loss) *loss = (float)(sum / fmax(count, 1.));
+    if (alpha) *alpha = count > 0 ? (float)((double)factor * (dloss ? (double)*dloss : 1.) / count) : 0.f;
+  }
+}
+
+// The parts of dx joined, scaled and rounded; rows that do not count are zero.
+template <typename IO>
+__global__ void __launch_bounds__(256) join_dx_kernel(const float* acc, int splits, int64_t split_stride, int pitch, int rows, int cols,
+                                                      const float* alpha, const void* targets, int bits, int64_t ignore, int classes, IO* dx,
+                                                      int64_t stride, const uint32_t* status) {
+  const float a = (*status & VL_TIMEOUT) ? __uint_as_float(0x7fc00000u) : *alpha;
+  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+    const bool on = target_of(targets, bits, ignore, classes, (int)row) >= 0;
+    for (int c = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 4; c < cols; c += (int)(gridDim.x * blockDim.x) * 4) {
+      float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s = 0; s < splits; ++s) {
+        const float4 o = *reinterpret_cast<const float4*>(acc + s * split_stride + row * pitch + c);
+        f = make_float4(f.x + o.x, f.y + o.y, f.z + o.z, f.w + o.w);
+      }
+      const float v[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + j < cols) dx[row * stride + c + j] = from_f32<IO>(on ? v[j] * a : 0.f);
+    }
+  }
+}
+
+// ---- host --------------------------------------------------------------------------------------------------------
+size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
+int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+
+// Pairs of SMs of the current device.
+int sm_pairs() {
+  static std::mutex mutex;
+  static int known[64] = {};
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return 0; }
+  std::lock_guard<std::mutex> lock(mutex);
+  if (dev < 64 && known[dev]) return known[dev];
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return 0; }
+  if (dev < 64) known[dev] = sms / 2;
+  return sms / 2;
+}
+
+struct Operand {           // how a matrix of rows x cols is handed to the products
+  bool staged;             // copied to the workspace first
+  int planes;
+  int64_t pitch, plane;    // in values
+  size_t offset, bytes;    // in the workspace, if staged
+};
+struct Layout {
+  Operand x, w;
+  size_t status, alpha, partial, target_z, row_loss, dz, acc, total;
+  int piece;               // classes per piece of the backward pass
+  int64_t dz_pitch, dz_plane;
+  int splits, acc_pitch;
+  int64_t acc_split;
+};
+
+bool usable_directly(const void* p, int64_t stride, int dtype) {
+  return dtype != SNN_DTYPE_FP32 && (uintptr_t)p % 16 == 0 && stride % 8 == 0;
+}
+// Parts of the contraction of dx: as many as fill the device best, in whole waves, each at least 8 k-blocks deep.
+int dx_splits(int tiles, int kblocks, int pairs) {
+  int best = 1;
+  double best_cost = 1e30;
+  for (int s = 1; s <= MAX_SPLITS && (s == 1 || kblocks / s >= 8); ++s) {
+    const double cost = ceil_div((int64_t)tiles * s, pairs) / (double)s + 0.02 * s;   // waves of full depth, and the cost of joining
+    if (cost < best_cost) best_cost = cost, best = s;
+  }
+  return best;
+}
+Layout layout_of(const snn_vocab_loss_args* a, bool backward, int pairs) {
+  Layout l{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes); return o; };
+  const int planes = a->dtype == SNN_DTYPE_FP32 ? 3 : 1;
+  auto operand = [&](const void* p, int64_t stride, int rows, int cols, bool always) {
+    Operand o{};
+    o.planes = planes;
+    o.staged = always || !usable_directly(p, rows == 1 ? 0 : stride, a->dtype);
+    o.pitch = o.staged || rows == 1 ? round_up(cols, 8) : stride;   // (the stride of a single row means nothing)
+    o.plane = o.pitch * rows;
+    if (o.staged) {
+      o.bytes = (size_t)planes * o.plane * 2;
+      o.offset = take(o.bytes);
+    }
+    return o;
+  };
+  l.status = take(256);
+  l.alpha = l.status + 128;
+  l.x = operand(a->x, a->x_stride, a->rows, a->dim, backward);
+  const bool by_class = a->w_layout == SNN_W_BY_CLASS;
+  l.w = operand(a->w, a->w_stride, by_class ? a->classes : a->dim, by_class ? a->dim : a->classes, false);
+  if (!backward) {
+    l.partial = take(sizeof(float2) * (size_t)a->rows * ceil_div(a->classes, UM_TILE));
+    l.target_z = take(sizeof(float) * (size_t)a->rows);
+    l.row_loss = take(sizeof(float) * (size_t)a->rows);
+  } else {
+    const int64_t fit = (int64_t)(PIECE_BYTES / (2 * (size_t)planes * std::max(a->rows, 1))) / UM_TILE * UM_TILE;
+    l.piece = (int)std::min<int64_t>(std::max<int64_t>(fit, UM_TILE), round_up(a->classes, UM_TILE));
+    // pieces of equal width
+    l.piece = (int)round_up(ceil_div(a->classes, ceil_div(a->classes, l.piece)), UM_TILE);
+    l.dz_pitch = l.piece;
+    l.dz_plane = l.dz_pitch * a->rows;
+    l.dz = take((size_t)planes * l.dz_plane * 2);
+    l.splits = dx_splits(ceil_div(a->rows, UM_TILE) * ceil_div(a->dim, UM_TILE), l.piece / UM_KB, std::max(pairs, 1));
+    l.acc_pitch = (int)round_up(a->dim, 4);
+    l.acc_split = (int64_t)l.acc_pitch * a->rows;
+    l.acc = take(sizeof(float) * (size_t)l.acc_split * l.splits);
+  }
+  l.total = at;
+  return l;
+}
+
+snn_status check(const snn_vocab_loss_args* a) {
+  constexpr int LIMIT = 1 << 30;
+  if (!a || a->rows < 0 || a->dim < 1 || a->classes < 1 || a->rows >= LIMIT || a->dim >= LIMIT || a->classes >= LIMIT) return SNN_ERR_INVALID_ARG;
+  if (a->dtype < SNN_DTYPE_FP32 || a->dtype > SNN_DTYPE_FP16) return SNN_ERR_INVALID_ARG;
+  if (a->w_layout != SNN_W_BY_FEATURE && a->w_layout != SNN_W_BY_CLASS) return SNN_ERR_INVALID_ARG;
+  if (a->target_bits != 32 && a->target_bits != 64) return SNN_ERR_INVALID_ARG;
+  if (!(std::fabs(a->scale) < INFINITY)) return SNN_ERR_INVALID_ARG;
+  const int64_t w_cols = a->w_layout == SNN_W_BY_CLASS ? a->dim : a->classes, w_rows = a->w_layout == SNN_W_BY_CLASS ? a->classes : a->dim;
+  if ((a->rows > 1 && a->x_stride < a->dim) || (w_rows > 1 && a->w_stride < w_cols)) return SNN_ERR_INVALID_ARG;
+  if (!a->w || (a->rows > 0 && (!a->x || !a->targets))) return SNN_ERR_INVALID_ARG;
+  return SNN_OK;
+}
+bool is_bf16(int dtype) { return dtype != SNN_DTYPE_FP16; }   // fp32: bf16 planes
+
+template <int EPI, bool A_MN, bool B_MN> snn_status launch_product(const ProductParams& p, int pairs, cudaStream_t stream) {
+  const auto kernel = product_kernel<EPI, A_MN, B_MN>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)VL_SMEM) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
+  const int64_t units = (int64_t)p.tiles_m * p.tiles_n * p.splits;
+  if (units > INT32_MAX / 2) return SNN_ERR_UNSUPPORTED;
+  kernel<<<2 * (unsigned)std::min<int64_t>(units, pairs), VL_THREADS, VL_SMEM, stream>>>(p);
+  return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+}
+
+struct Call {
+  const snn_vocab_loss_args* a;
+  Layout l;
+  char* ws;
+  cudaStream_t stream;
+  int pairs;
+  uint32_t* status() const { return (uint32_t*)(ws + l.status); }
+  float* alpha() const { return (float*)(ws + l.alpha); }
+
+  snn_status begin(bool backward, void* s) {
+    stream = (cudaStream_t)s;
+    pairs = sm_pairs();
+    if (pairs < 1) return SNN_ERR_CUDA;
+    l = layout_of(a, backward, pairs);
+    if (!a->workspace || (uintptr_t)a->workspace % 256 != 0) return SNN_ERR_INVALID_ARG;
+    if (a->workspace_bytes < l.total) return SNN_ERR_WORKSPACE_TOO_SMALL;
+    ws = (char*)a->workspace;
+    return cudaMemsetAsync(ws + l.status, 0, 4, stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+  }
+  snn_status stage(const Operand& o, const void* src, int64_t stride, int rows, int cols, bool mask) const {
+    if (!o.staged) return SNN_OK;
+    uint16_t* const dst = (uint16_t*)(ws + o.offset);
+    const void* const targets = mask ? a->targets : nullptr;
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(o.pitch, 512), 1024), (unsigned)std::min(rows, 16384));
+    auto go = [&](auto io) {
+      using IO = decltype(io);
+      stage_operand_kernel<IO><<<grid, 256, 0, stream>>>((const IO*)src, stride, rows, cols, dst, (int)o.pitch, o.plane, targets, a->target_bits,
+                                                         a->ignore_index, a->classes);
+    };
+    if (a->dtype == SNN_DTYPE_FP32) go(float());
+    else go(__half());   // 16 bits are copied, whatever they mean
+    return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+  }
+  const void* data(const Operand& o, const void* direct) const { return o.staged ? ws + o.offset : direct; }
+  bool map(CUtensorMap* m, const Operand& o, const void* direct, int rows, int cols, bool mn_major) const {
+    return make_tensor_map_16bit(m, data(o, direct), is_bf16(a->dtype), cols, rows, o.planes, o.pitch, o.plane, mn_major ? UM_KB : UM_HALF);
+  }
+  ProductParams base() const {
+    ProductParams p{};
+    p.bf16 = is_bf16(a->dtype);
+    p.splits = 1;
+    p.planes = l.x.planes;
+    p.n_pairs = p.planes == 3 ? 6 : 1;
+    p.targets = a->targets; p.target_bits = a->target_bits; p.ignore_index = a->ignore_index; p.classes = a->classes;
+    p.z_scale = a->scale * LOG2E;
+    p.status = status();
+    p.dz_scale = a->dtype == SNN_DTYPE_FP16 ? FP16_DZ_SCALE : 1.f;
+    if (p.planes == 3) {
+      // (plane of a, plane of b), 0 the leading part: 2 0, 0 2, 1 1, 1 0, 0 1, 0 0
+      const int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
+      p.pair_a = p.pair_b = 0;
+      for (int i = 0; i < 6; ++i) p.pair_a |= (uint32_t)pa[i] << (4 * i), p.pair_b |= (uint32_t)pb[i] << (4 * i);
+    }
+    return p;
+  }
+};
+
+#define VL_TRY(expr)                            \
+  do {                                          \
+    const snn_status st_ = (expr);              \
+    if (st_ != SNN_OK) return st_;              \
+  } while (0)
+
+}  // namespace
+
+extern "C" snn_status snn_vocab_loss_workspace(const snn_vocab_loss_args* a, int32_t backward, size_t* bytes) {
+  VL_TRY(check(a));
+  if (!bytes) return SNN_ERR_INVALID_ARG;
+  int pairs = sm_pairs();
+  *bytes = layout_of(a, backward != 0, pairs < 1 ? 74 : pairs).total;
+  return SNN_OK;
+}
+
+extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void* stream) {
+  VL_TRY(check(a));
+  if (!a->loss || (a->rows > 0 && !a->lse)) return SNN_ERR_INVALID_ARG;
+  Call c{a};
+  VL_TRY(c.begin(false, stream));
+  if (a->rows == 0) return cudaMemsetAsync(a->loss, 0, 4, c.stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+  const bool by_class = a->w_layout == SNN_W_BY_CLASS;
+  const int w_rows = by_class ? a->classes : a->dim, w_cols = by_class ? a->dim : a->classes;
+  VL_TRY(c.stage(c.l.x, a->x, a->x_stride, a->rows, a->dim, false));
+  VL_TRY(c.stage(c.l.w, a->w, a->w_stride, w_rows, w_cols, false));
+  ProductParams p = c.base();
+  if (!c.map(&p.a, c.l.x, a->x, a->rows, a->dim, false) || !c.map(&p.b, c.l.w, a->w, w_rows, w_cols, !by_class)) return SNN_ERR_CUDA;
+  p.tiles_m = ceil_div(a->rows, UM_TILE);
+  p.tiles_n = ceil_div(a->classes, UM_TILE);
+  p.kblocks = ceil_div(a->dim, UM_KB);
+  p.m = a->rows;
+  p.n = a->classes;
+  p.partial = (float2*)(c.ws + c.l.partial);
+  p.target_z = (float*)(c.ws + c.l.target_z);
+  VL_TRY((by_class ? launch_product<STATS, false, false>(p, c.pairs, c.stream) : launch_product<STATS, false, true>(p, c.pairs, c.stream)));
+  float* const row_loss = (float*)(c.ws + c.l.row_loss);
+  row_loss_kernel<<<ceil_div(a->rows, 32), 256, 0, c.stream>>>(p.partial, p.tiles_n, p.target_z, a->rows, a->targets, a->target_bits,
+                                                               a->ignore_index, a->classes, a->lse, row_loss, a->row_loss, c.status());
+  mean_kernel<<<1, 1024, 0, c.stream>>>(row_loss, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, a->loss, nullptr, 0.f, nullptr);
+  return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+}
+
+extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void* stream) {
+  VL_TRY(check(a));
+  const bool by_class = a->w_layout == SNN_W_BY_CLASS;
+  const int w_rows = by_class ? a->classes : a->dim, w_cols = by_class ? a->dim : a->classes;
+  if (!a->dw || (a->rows > 0 && (!a->dx || !a->lse))) return SNN_ERR_INVALID_ARG;
+  if ((a->rows > 1 && a->dx_stride < a->dim) || (w_rows > 1 && a->dw_stride < w_cols)) return SNN_ERR_INVALID_ARG;
+  Call c{a};
+  VL_TRY(c.begin(true, stream));
+  const size_t size = a->dtype == SNN_DTYPE_FP32 ? 4 : 2;
+  if (a->rows == 0)
+    return cudaMemset2DAsync(a->dw, a->dw_stride * size, 0, w_cols * size, w_rows, c.stream) == cudaSuccess ? SNN_OK
+                                                                                                         : (cudaGetLastError(), SNN_ERR_CUDA);
+  const Layout& l = c.l;
+  VL_TRY(c.stage(l.x, a->x, a->x_stride, a->rows, a->dim, true));
+  VL_TRY(c.stage(l.w, a->w, a->w_stride, w_rows, w_cols, false));
+  const ProductParams base = c.base();
+  mean_kernel<<<1, 1024, 0, c.stream>>>(nullptr, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, nullptr, c.alpha(),
+                                        a->dloss * a->scale / base.dz_scale, a->dloss_device);
+  CUtensorMap x_k, x_mn, w_z, w_dx, dz_k, dz_mn;   // as operands that are contiguous along the contraction, and across it
+  bool ok = c.map(&x_k, l.x, a->x, a->rows, a->dim, false) && c.map(&x_mn, l.x, a->x, a->rows, a->dim, true);
+  ok = ok && c.map(&w_z, l.w, a->w, w_rows, w_cols, !by_class) && c.map(&w_dx, l.w, a->w, w_rows, w_cols, by_class);
+  for (int v0 = 0; v0 < a->classes; v0 += l.piece) {
+    const int width = std::min(l.piece, a->classes - v0);
+    // (the maps end at the piece's width: columns beyond it arrive as zeros and are not stored)
+    ok = ok && make_tensor_map_16bit(&dz_k, c.ws + l.dz, base.bf16, width, a->rows, base.planes, l.dz_pitch, l.dz_plane, UM_HALF) &&
+         make_tensor_map_16bit(&dz_mn, c.ws + l.dz, base.bf16, width, a->rows, base.planes, l.dz_pitch, l.dz_plane, UM_KB);
+    if (!ok) return SNN_ERR_CUDA;
+    ProductParams p = base;   // dz of the piece
+    p.a = x_k; p.b = w_z; p.out = dz_k;
+    p.tiles_m = ceil_div(a->rows, UM_TILE); p.tiles_n = ceil_div(width, UM_TILE); p.kblocks = ceil_div(a->dim, UM_KB);
+    p.m = a->rows; p.n = width; p.b0 = v0;
+    p.lse = a->lse;
+    VL_TRY((by_class ? launch_product<GRAD, false, false>(p, c.pairs, c.stream) : launch_product<GRAD, false, true>(p, c.pairs, c.stream)));
+    p = base;                 // dx += dz w^T
+    p.a = dz_k; p.b = w_dx;
+    p.tiles_m = ceil_div(a->rows, UM_TILE); p.tiles_n = ceil_div(a->dim, UM_TILE); p.kblocks = ceil_div(width, UM_KB);
+    p.splits = std::min(l.splits, p.kblocks);
+    p.bk0 = v0;
+    p.m = a->rows; p.n = a->dim;
+    p.acc = (float*)(c.ws + l.acc); p.acc_pitch = l.acc_pitch; p.acc_split = l.acc_split; p.accumulate = v0 > 0;
+    VL_TRY((by_class ? launch_product<DX, false, true>(p, c.pairs, c.stream) : launch_product<DX, false, false>(p, c.pairs, c.stream)));
+    p = base;                 // the piece's part of dw
+    p.kblocks = ceil_div(a->rows, UM_KB);
+    p.alpha = c.alpha();
+    p.dw_stride = a->dw_stride; p.dw_dtype = a->dtype;
+    if (by_class) {           // rows are classes
+      p.a = dz_mn; p.b = x_mn;
+      p.m = width; p.n = a->dim;
+      p.dw = (char*)a->dw + (size_t)v0 * a->dw_stride * size;
+    } else {
+      p.a = x_mn; p.b = dz_mn;
+      p.m = a->dim; p.n = width;
+      p.dw = (char*)a->dw + (size_t)v0 * size;
+    }
+    p.tiles_m = ceil_div(p.m, UM_TILE); p.tiles_n = ceil_div(p.n, UM_TILE);
+    VL_TRY((launch_product<DW, true, true>(p, c.pairs, c.stream)));
+  }
+  const int splits = std::min(l.splits, ceil_div(std::min(l.piece, a->classes), UM_KB));
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a->dim, 1024), 64), (unsigned)std::min(a->rows, 16384));
+  auto join = [&](auto io) {
+    using IO = decltype(io);
+    join_dx_kernel<IO><<<grid, 256, 0, c.stream>>>((const float*)(c.ws + l.acc), splits, l.acc_split, l.acc_pitch, a->rows, a->dim, c.alpha(),
+                                                   a->targets, a->target_bits, a->ignore_index, a->classes, (IO*)a->dx, a->dx_stride, c.status());
+  };
+  if (a->dtype == SNN_DTYPE_FP32) join(float());
+  else if (a->dtype == SNN_DTYPE_BF16) join(__nv_bfloat16());
+  else join(__half());
+  return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+}

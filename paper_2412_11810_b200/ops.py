@@ -4,6 +4,8 @@
     dx, dgate, dstate = gated_scan_backward(kept, dh, dlast)
     h, state = gated_scan_step(x, gate, state)                  # one token
     packed = pack_activation(x, "int8"); x = unpack_activation(packed)
+    loss, row_loss, lse = vocab_loss(x, w_out, targets)         # soft-max cross entropy of x w_out, logits never stored
+    dx, dw = vocab_loss_backward(x, w_out, targets, lse)
 
 Gradients are explicit, as in the training step: nothing is recorded for autograd.  Work is launched on the current torch
 stream of the tensors' device and the calls return without waiting; they can be captured into a CUDA graph.  Arguments
@@ -253,3 +255,76 @@ def gated_scan_backward(kept: ScanKept, dh: torch.Tensor, dlast: Optional[torch.
         a.states, a.dlast, a.dstate = kept.states.data_ptr(), _ptr(dlast), dstate.data_ptr()
         sb.snn_scan_backward(a, _stream(like.device))
     return dx, dgate, dstate
+
+
+# ---- soft-max cross entropy over a vocabulary ------------------------------------------------------------------
+def _vocab_args(x, w_out, targets, scale: float, ignore_index: int):
+    _need_values(x, "x", 2)
+    _need(isinstance(w_out, torch.Tensor) and w_out.device == x.device, f"w_out: a tensor on {x.device} is required")
+    _need(w_out.dtype == x.dtype, f"w_out: dtype {w_out.dtype} instead of {x.dtype}")
+    rows, dim = x.shape
+    _need(w_out.dim() == 2 and w_out.shape[0] == dim, f"w_out: shape {tuple(w_out.shape)} instead of ({dim}, classes)")
+    classes = w_out.shape[1]
+    _need(dim >= 1 and classes >= 1, "w_out: at least one feature and one class are required")
+    _need(max(rows, dim, classes) < 2 ** 30, "x, w_out: too large")
+    _need(rows <= 1 or x.stride(0) >= dim, "x: rows overlap")
+    by_feature = (classes == 1 or w_out.stride(1) == 1) and (dim == 1 or w_out.stride(0) >= classes)
+    by_class = (dim == 1 or w_out.stride(0) == 1) and (classes == 1 or w_out.stride(1) >= dim)
+    _need(by_feature or by_class, "w_out: its features or its classes have to be contiguous, without overlap")
+    _need(isinstance(targets, torch.Tensor) and targets.device == x.device, f"targets: a tensor on {x.device} is required")
+    _need(targets.dtype in (torch.int32, torch.int64), f"targets: dtype {targets.dtype} is not int32 or int64")
+    _need(tuple(targets.shape) == (rows,), f"targets: shape {tuple(targets.shape)} instead of ({rows},)")
+    _need(targets.is_contiguous(), "targets: has to be contiguous")
+    _need(-2 ** 63 <= ignore_index < 2 ** 63, "ignore_index: does not fit 64 bits")
+    _need(abs(scale) <= 3.4e38, "scale: has to be finite")
+    a = sb.snn_vocab_loss_args()
+    a.rows, a.dim, a.classes, a.dtype = rows, dim, classes, _DTYPES[x.dtype]
+    a.x, a.x_stride, a.w = x.data_ptr(), x.stride(0), w_out.data_ptr()
+    a.w_layout, a.w_stride = (sb.SNN_W_BY_FEATURE, w_out.stride(0)) if by_feature else (sb.SNN_W_BY_CLASS, w_out.stride(1))
+    a.targets, a.target_bits, a.ignore_index, a.scale = targets.data_ptr(), targets.element_size() * 8, ignore_index, scale
+    return a
+
+
+def vocab_loss(x: torch.Tensor, w_out: torch.Tensor, targets: torch.Tensor, *, scale: float = 1.0, ignore_index: int = -100):
+    """Mean soft-max cross entropy of the logits scale * x w_out, which are never stored.
+
+    x: [rows][dim], w_out: [dim][classes] of the same type (fp32, bf16 or fp16), stored by feature (contiguous) or by class
+    (`table.t()` of a [classes][dim] table).  targets: int32 or int64 [rows]; rows with ignore_index do not count, any other
+    target outside [0, classes) makes its row's loss and the mean NaN.
+    Returns (loss, a 0-d tensor; row_loss [rows]; lse [rows], the log-sum-exp that `vocab_loss_backward` needs), all fp32,
+    with zeros for rows that do not count."""
+    a = _vocab_args(x, w_out, targets, scale, ignore_index)
+    with _on(x.device):
+        out = torch.empty((2, a.rows), dtype=torch.float32, device=x.device)
+        loss = torch.empty((), dtype=torch.float32, device=x.device)
+        a.row_loss, a.lse, a.loss = out[0].data_ptr(), out[1].data_ptr(), loss.data_ptr()
+        ws = torch.empty(sb.snn_vocab_loss_workspace(a, False), dtype=torch.uint8, device=x.device)
+        a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+        sb.snn_vocab_loss_forward(a, _stream(x.device))
+    return loss, out[0], out[1]
+
+
+def vocab_loss_backward(x: torch.Tensor, w_out: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, *, scale: float = 1.0,
+                        ignore_index: int = -100, dloss=1.0):
+    """Gradients of `vocab_loss` by x and w_out: (dx [rows][dim], dw [dim][classes], stored as w_out is), in their type.
+    dloss: the gradient of the loss, a number or an fp32 0-d tensor on the device."""
+    a = _vocab_args(x, w_out, targets, scale, ignore_index)
+    _need_like(lse, "lse", x, (a.rows,), torch.float32)
+    if isinstance(dloss, torch.Tensor):
+        _need_like(dloss, "dloss", x, (), torch.float32)
+        a.dloss, a.dloss_device = 1.0, dloss.data_ptr()
+    else:
+        a.dloss = dloss
+    with _on(x.device):
+        dx = torch.empty((a.rows, a.dim), dtype=x.dtype, device=x.device)
+        if a.w_layout == sb.SNN_W_BY_FEATURE:
+            dw = torch.empty((a.dim, a.classes), dtype=x.dtype, device=x.device)
+            a.dw_stride = a.classes
+        else:
+            dw = torch.empty((a.classes, a.dim), dtype=x.dtype, device=x.device).t()
+            a.dw_stride = a.dim
+        a.lse, a.dx, a.dx_stride, a.dw = lse.data_ptr(), dx.data_ptr(), a.dim, dw.data_ptr()
+        ws = torch.empty(sb.snn_vocab_loss_workspace(a, True), dtype=torch.uint8, device=x.device)
+        a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+        sb.snn_vocab_loss_backward(a, _stream(x.device))
+    return dx, dw

@@ -121,3 +121,57 @@ def scan_backward(x, gate, state, lengths, mode, dh, dlast, keep=None, keep_gate
     z = lambda v: np.where(on, v, 0.0)  # noqa: E731
     return {"dx": z(dx), "dx_tol": z(dx_tol), "dgate": z(dg), "dgate_tol": z(dg_tol), "dstate": e, "dstate_tol": ee,
             "states": f["states"], "states_tol": f["E"][0:T:CHUNK]}
+
+
+# ---- vocabulary loss (torch, float64, on the tensors' device) ----------------------------------------------------
+def vocab_loss(x, w, targets, scale, ignore, dtype, dloss=1.0):
+    """loss, row_loss, lse, dx, dw and their bounds, for float64 x [n][D], w [D][V].
+
+    Bounds.  A tensor-core instruction adds 16 products to a fp32 accumulator; it cuts or rounds, and two units of 2^-23 of
+    the sum of magnitudes cover it.  fp32 operands take six instructions where 16-bit ones take one, and the products left
+    out (mid x lo, lo x mid, lo x lo) are below 2^-23 of the magnitudes.  So a sum of K products is off by
+    (2 ceil(K / 16) P + 4) 2^-23 of the sum of magnitudes, P = 1 or 6.  exp2 is off by 2^-22, its argument by a rounding of
+    2^-24 of each of its two parts, and what is below 2^-126, the smallest normal number, counts as zero; a row's sum of exponentials has 32 + 8 + V / 2048 + 8 roundings.  dz is rounded to its
+    type (fp32: three parts, 2^-24) before it is multiplied.
+    """
+    import torch
+    P = 6 if dtype == "fp32" else 1
+    unit, half = 2.0 ** -23, HALF_STEP[dtype]
+
+    def steps(K):
+        return (2 * -(-K // 16) * P + 4) * unit
+
+    n, D = x.shape
+    V = w.shape[1]
+    valid = (targets >= 0) & (targets < V) & (targets != ignore)
+    bad = ~valid & (targets != ignore)
+    on = valid[:, None]
+    x = torch.where(on, x, 0.0)
+    count = max(1, int(valid.sum()))
+    z = scale * (x @ w)
+    ez = steps(D) * abs(scale) * (x.abs() @ w.abs())
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None])
+    # the error of lse: that of the logits weighted by p, and of the sum
+    lse_tol = (p * ez).sum(1) + (60 + V / 2048) * unit + 4 * unit * lse.abs() + 2 * unit * z.abs().amax(1)
+    at = torch.where(valid, targets, 0).long()[:, None]
+    zt, ezt = z.gather(1, at).squeeze(1), ez.gather(1, at).squeeze(1)
+    row = lse - zt
+    row_tol = lse_tol + ezt + 4 * unit * (zt.abs() + row.abs())
+    zero = torch.zeros_like(lse)
+    out = {"row": torch.where(valid, row, zero), "row_tol": torch.where(valid, row_tol, zero),
+           "lse": torch.where(valid, lse, zero), "lse_tol": torch.where(valid, lse_tol, zero)}
+    out["row"] = torch.where(bad, torch.full_like(row, float("nan")), out["row"])
+    out["loss"], out["loss_tol"] = out["row"].sum() / count, out["row_tol"].sum() / count + unit * out["row"].abs().sum() / count
+    dz = p.clone()
+    dz.scatter_add_(1, at, torch.full_like(at, -1.0, dtype=dz.dtype))
+    ep = p * (ez + lse_tol[:, None] + 4 * unit * (1 + z.abs() + lse.abs()[:, None]))
+    ep.scatter_add_(1, at, torch.full_like(at, unit, dtype=dz.dtype))
+    ep = ep + 2.0 ** -126 + half * dz.abs() + (2.0 ** -25 / 16384 if dtype == "fp16" else 0.0)
+    dz, ep = torch.where(on, dz, 0.0), torch.where(on, ep, 0.0)
+    k = abs(scale * dloss) / count
+    out["dx"] = scale * dloss / count * (dz @ w.t())
+    out["dx_tol"] = k * ((ep + (steps(V) + 8 * unit) * dz.abs()) @ w.abs().t())
+    out["dw"] = scale * dloss / count * (x.t() @ dz)
+    out["dw_tol"] = k * (x.abs().t() @ (ep + (steps(n) + 8 * unit) * dz.abs()))
+    return out

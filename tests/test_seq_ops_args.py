@@ -47,10 +47,50 @@ def test_pack_refuses_invalid_arguments(rows, cols, dtype, fmt):
     assert sb.lib.snn_activation_unpack(None, None, fmt, rows, cols, None, dtype, 4, None) == sb.SNN_ERR_INVALID_ARG
 
 
+def _loss_args(**kw):
+    a = sb.snn_vocab_loss_args()
+    a.rows, a.dim, a.classes, a.x_stride, a.w_stride, a.target_bits, a.scale = 4, 8, 16, 8, 16, 64, 1.0
+    a.dx_stride, a.dw_stride = 8, 16
+    for name in ("x", "w", "targets", "lse", "loss", "dx", "dw"):
+        setattr(a, name, 1 << 20)   # never read: every call below is refused first
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+@pytest.mark.parametrize("change", [{"rows": -1}, {"dim": 0}, {"classes": 0}, {"rows": 1 << 30}, {"dtype": 3}, {"w_layout": 2},
+                                    {"target_bits": 16}, {"scale": float("nan")}, {"scale": float("inf")}, {"x_stride": 7},
+                                    {"w_stride": 15}, {"x": None}, {"w": None}, {"targets": None}])
+def test_loss_refuses_invalid_arguments(change):
+    n = C.c_size_t()
+    for call in (lambda a: sb.lib.snn_vocab_loss_forward(C.byref(a), None), lambda a: sb.lib.snn_vocab_loss_backward(C.byref(a), None),
+                 lambda a: sb.lib.snn_vocab_loss_workspace(C.byref(a), 0, C.byref(n))):
+        assert call(_loss_args(**change)) == sb.SNN_ERR_INVALID_ARG
+
+
+def test_loss_refuses_missing_buffers():
+    for name in ("lse", "loss"):
+        assert sb.lib.snn_vocab_loss_forward(C.byref(_loss_args(**{name: None})), None) == sb.SNN_ERR_INVALID_ARG
+    for change in ({"dx": None}, {"dw": None}, {"lse": None}, {"dx_stride": 7}, {"dw_stride": 15}):
+        assert sb.lib.snn_vocab_loss_backward(C.byref(_loss_args(**change)), None) == sb.SNN_ERR_INVALID_ARG
+    assert sb.lib.snn_vocab_loss_forward(None, None) == sb.SNN_ERR_INVALID_ARG
+    assert sb.lib.snn_vocab_loss_workspace(C.byref(_loss_args()), 0, None) == sb.SNN_ERR_INVALID_ARG
+
+
+def test_loss_workspace_does_not_grow_with_the_logits():
+    """The forward pass holds a pair of numbers per row and 256 classes, the backward pass a bounded piece of dz."""
+    a = _loss_args(rows=8192, dim=1024, classes=131072, x_stride=1024, w_stride=131072, dtype=sb.SNN_DTYPE_BF16)
+    logits = 4 * 8192 * 131072
+    assert 0 < sb.snn_vocab_loss_workspace(a, False) < logits / 64
+    assert 0 < sb.snn_vocab_loss_workspace(a, True) < logits / 8
+
+
 def test_sequence_operators_need_cuda_tensors():
     x = torch.zeros(4, 2, 8)
     for call in (lambda: ops.gated_scan(x, x), lambda: ops.gated_scan_step(x[0], x[0]), lambda: ops.pack_activation(x),
                  lambda: ops.gated_scan_backward(None, x),
+                 lambda: ops.vocab_loss(x[0], x[0].t(), torch.zeros(2, dtype=torch.int64)),
+                 lambda: ops.vocab_loss_backward(x[0], x[0].t(), torch.zeros(2, dtype=torch.int64), x[0, :, 0]),
                  lambda: ops.unpack_activation(ops.PackedActivation(x, x, "int8", torch.float32))):
         with pytest.raises(ValueError):
             call()
@@ -64,10 +104,12 @@ def test_struct_sizes_match_the_header(tmp_path):
     src = tmp_path / "s.c"
     src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "%s/include/snn.h"\nint main(void) {\n'
                    'printf("%%zu %%zu\\n", sizeof(snn_scan_args), offsetof(snn_scan_args, dstate));\n'
+                   'printf("%%zu %%zu\\n", sizeof(snn_vocab_loss_args), offsetof(snn_vocab_loss_args, workspace_bytes));\n'
                    'printf("%%d %%d\\n", SNN_KEEP_GROUP, SNN_SCAN_CHUNK); return 0; }\n' % root)
     subprocess.run(["gcc", str(src), "-o", str(tmp_path / "s")], check=True)
     out = subprocess.run([str(tmp_path / "s")], check=True, capture_output=True, text=True).stdout.split()
-    assert [int(v) for v in out] == [C.sizeof(sb.snn_scan_args), sb.snn_scan_args.dstate.offset, ops.KEEP_GROUP, ops.SCAN_CHUNK]
+    assert [int(v) for v in out] == [C.sizeof(sb.snn_scan_args), sb.snn_scan_args.dstate.offset, C.sizeof(sb.snn_vocab_loss_args),
+                                     sb.snn_vocab_loss_args.workspace_bytes.offset, ops.KEEP_GROUP, ops.SCAN_CHUNK]
 
 
 # ---- the 64-bit reference itself ---------------------------------------------------------------------------------

@@ -5,7 +5,7 @@ import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
-SOURCES = [os.path.join(CSRC, f) for f in ("snn_api.cu", "schedule.cpp", "scan.cu", "vocab_loss.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("snn_api.cu", "schedule.cpp", "scan.cu", "activation.cu", "vocab_loss.cu")]
 HEADERS = [os.path.join(CSRC, f) for f in ("kernels.cuh", "tma.cuh", "tc_gemm.cuh", "seq_common.cuh", "umma.cuh")] + [os.path.join(HERE, "..", "include", "snn.h")]
 LIB = os.path.join(HERE, "libsnnckpt.so")
 LIB_DEBUG = os.path.join(HERE, "libsnnckpt_debug.so")   # the same sources with -DSNN_DEBUG_CHECKS=1 (bounds-checked)

@@ -1,14 +1,16 @@
-// The gated linear recurrence with its backward pass, and activations in 8 bits (include/snn.h, "sequence-model
-// operators").
+// The gated linear recurrence with its backward pass (include/snn.h, "sequence-model operators").
 //
 // A step is an affine map of the state, h -> a h + b, and maps compose: (a2, b2) o (a1, b1) = (a2 a1, a2 b1 + b2).  So a
 // run of steps can be summarised before its start is known, and time is split three ways: a thread takes 8 steps of two
 // neighbouring channels in registers, the 8 warps of a thread block a chunk of 64 steps, the blocks of a cluster (1..8)
-// neighbouring chunks.  Warps exchange their summaries through shared memory, blocks through distributed shared memory
-// behind one hardware cluster barrier per turn; the state at the end of a turn is carried to the next one in registers.
-// Every input is read once, every output written once, nothing waits on a flag in memory, and the order of the
-// arithmetic is fixed by the sizes alone.  The kernels are bound by HBM; the cluster size only has to supply enough
-// blocks for it when there are few channels.
+// neighbouring chunks; together they take a turn, and the state at its end is carried to the next one.  One warp chains the
+// summaries of the block's warps, those of the cluster's blocks come to it through distributed shared memory.  Every input
+// is read once, every output written once, and the order of the arithmetic is fixed by the sizes alone.
+//
+// The kernels are bound by HBM as long as a step costs few instructions: channels are handled in pairs (f32x2 arithmetic),
+// tiles of 64 steps x 64 channels arrive by TMA a turn or two ahead and leave by TMA, so that the threads compute no
+// addresses.  Data that TMA cannot describe (rows that are not multiples of 16 bytes) takes one of two other paths: pairs
+// copied by cp.async, or plain loads of single values.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -28,11 +30,19 @@ constexpr int SCAN_THREADS = 32 * SCAN_WARPS;
 constexpr int SCAN_COLS = 64;                   // channels per thread block, two per lane: one group of the 8-bit format
 constexpr int SCAN_MAX_CLUSTER = 8;
 constexpr int SCAN_SHORT = 16;                  // up to so many steps a thread simply walks through them
+constexpr int SCAN_DEPTH = 2;                   // turns whose inputs are in shared memory or on their way
+constexpr int PIECE = SNN_SCAN_CHUNK * SCAN_COLS;   // values of one tensor that a block needs for a turn
+constexpr int WARP_PIECE = SCAN_K * SCAN_COLS;      // ... that a warp does
 static_assert(SCAN_K * SCAN_WARPS == SNN_SCAN_CHUNK, "a thread block's run of steps is a chunk");
 static_assert(SCAN_COLS == KEEP_GROUP, "a warp encodes one group at a time");
 
+// How data comes and goes: TILES by TMA (rows of the tensors are multiples of 16 bytes), PAIRS two values at a time,
+// SCALAR one at a time.
+enum Path { SCALAR, PAIRS, TILES };
+
 struct ScanParams {
-  int T, B, N, n_tiles;      // n_tiles: column tiles per sample
+  CUtensorMap in[3], out[4];   // TILES.  forward: x, gate -> h, -, codes of x, codes of gate; backward: dh, x, gate -> dx, dgate
+  int T, B, N, n_tiles;        // n_tiles: column tiles per sample
   int mode, x_format, gate_format;
   const void *x, *gate, *dh;
   void *h, *dx, *dgate;
@@ -43,39 +53,57 @@ struct ScanParams {
   uint8_t *x_codes, *x_scales, *gate_codes, *gate_scales;
 };
 
+// ---- pairs of channels ---------------------------------------------------------------------------------------
+__device__ __forceinline__ uint64_t bits2(float2 v) { return (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x); }
+__device__ __forceinline__ float2 from_bits2(uint64_t u) { return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32))); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+struct Map2 {   // the affine maps of two channels
+  float2 a, b;
+};
+__device__ __forceinline__ float2 apply(const Map2& m, float2 h) { return fma2(m.a, h, m.b); }
+__device__ __forceinline__ float4 as4(const Map2& m) { return make_float4(m.a.x, m.a.y, m.b.x, m.b.y); }
+__device__ __forceinline__ Map2 as_map(float4 v) { return {make_float2(v.x, v.y), make_float2(v.z, v.w)}; }
+__device__ __forceinline__ Map2 then(const Map2& first, const Map2& second) { return {mul2(first.a, second.a), fma2(second.a, first.b, second.b)}; }
+
 // a and the factor i of x.  sigmoid(g) and 1 - sigmoid(g) both without cancellation: with e = exp(-|g|), the larger of
 // the two is 1 / (1 + e) and the smaller e / (1 + e).  (1 + e lies in [1, 2]: the hardware's reciprocal needs no care for
 // the ends of the range; an e below 2^-126 counts as zero.)
-__device__ __forceinline__ void sigmoids(float g, float& a, float& i) {
-  float e, large;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(fabsf(g) * -1.44269504f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large) : "f"(1.f + e));
-  const float small = e * large;
-  a = g >= 0.f ? large : small;
-  i = g >= 0.f ? small : large;
+__device__ __forceinline__ void sigmoids(float2 g, float2& a, float2& i) {
+  float2 e, large;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(fabsf(g.x) * -1.44269504f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(fabsf(g.y) * -1.44269504f));
+  const float2 d = add2(e, both(1.f));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.x) : "f"(d.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.y) : "f"(d.y));
+  const float2 small = mul2(e, large);
+  a = make_float2(g.x >= 0.f ? large.x : small.x, g.y >= 0.f ? large.y : small.y);
+  i = make_float2(g.x >= 0.f ? small.x : large.x, g.y >= 0.f ? small.y : large.y);
 }
 // gv becomes a, in becomes i, for all steps of a thread
 __device__ __forceinline__ void coefficients(float2 (&gv)[SCAN_K], float2 (&in)[SCAN_K], int mode) {
   if (mode == SNN_SCAN_DIRECT) {
 #pragma unroll
-    for (int k = 0; k < SCAN_K; ++k) in[k] = make_float2(1.f, 1.f);
+    for (int k = 0; k < SCAN_K; ++k) in[k] = both(1.f);
   } else {
 #pragma unroll
-    for (int k = 0; k < SCAN_K; ++k) {
-      sigmoids(gv[k].x, gv[k].x, in[k].x);
-      sigmoids(gv[k].y, gv[k].y, in[k].y);
-    }
+    for (int k = 0; k < SCAN_K; ++k) sigmoids(gv[k], gv[k], in[k]);
   }
-}
-
-struct Map2 {   // the affine maps of two channels
-  float a0, b0, a1, b1;
-};
-__device__ __forceinline__ float2 apply(const Map2& m, float2 h) { return make_float2(fmaf(m.a0, h.x, m.b0), fmaf(m.a1, h.y, m.b1)); }
-__device__ __forceinline__ float4 as4(const Map2& m) { return make_float4(m.a0, m.b0, m.a1, m.b1); }
-__device__ __forceinline__ Map2 as_map(float4 v) { return {v.x, v.y, v.z, v.w}; }
-__device__ __forceinline__ Map2 then(const Map2& first, const Map2& second) {
-  return {first.a0 * second.a0, fmaf(second.a0, first.b0, second.b0), first.a1 * second.a1, fmaf(second.a1, first.b1, second.b1)};
 }
 
 __device__ __forceinline__ float2 load_state(const float* p, int64_t row, int N, int c, int n_ok) {
@@ -88,110 +116,128 @@ __device__ __forceinline__ void store_state(float* p, int64_t row, int N, int c,
   if (p && n_ok > 0) p[row * N + c] = v.x;
   if (p && n_ok > 1) p[row * N + c + 1] = v.y;
 }
-
-// ---- kept rows in 8 bits ------------------------------------------------------------------------------------
-// The scale and this lane's two codes of a row of 64 values, two per lane.  Called by whole warps.
-template <int FORMAT> __device__ __forceinline__ uint32_t encode_row(float2 v, int n_ok, uint32_t& byte) {
-  const float m = larger_magnitude(n_ok > 0 ? v.x : 0.f, n_ok > 1 ? v.y : 0.f);
-  const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(m));   // bit patterns of magnitudes sort as they do
-  byte = keep_scale_byte<FORMAT>(top);
-  return byte == 255u ? 0u : keep_encode2<FORMAT>(v, keep_scale_inverse(byte), top);
-}
-// Encodes the warp's steps t0.. (those before `len`) and stores codes and scales.  FAST: rows of codes are multiples of 16
-// bytes and aligned to them; they go through the warp's 512 bytes of shared memory, to be stored 16 bytes at a time.
-template <int FORMAT, bool FAST>
-__device__ __forceinline__ void keep_steps(const float2 (&v)[SCAN_K], const ScanParams& p, int b, int c, int n_ok, int t0, int len,
-                                           uint8_t* codes, uint8_t* scales, unsigned char* s_codes) {
-  const int lane = threadIdx.x & 31, groups = (p.N + KEEP_GROUP - 1) / KEEP_GROUP;
-  uint32_t mine = 0;
-#pragma unroll
-  for (int k = 0; k < SCAN_K; ++k) {
-    uint32_t byte;
-    const uint32_t pair = encode_row<FORMAT>(v[k], n_ok, byte);
-    if (lane == k) mine = byte;
-    if (FAST) {
-      *reinterpret_cast<uint16_t*>(s_codes + k * SCAN_COLS + 2 * lane) = (uint16_t)pair;
-    } else if (t0 + k < len) {
-      uint8_t* const at = codes + ((int64_t)(t0 + k) * p.B + b) * p.N + c;
-      if (n_ok > 0) at[0] = (uint8_t)(pair & 255u);
-      if (n_ok > 1) at[1] = (uint8_t)(pair >> 8);
-    }
-  }
-  if (lane < SCAN_K && t0 + lane < len) scales[((int64_t)(t0 + lane) * p.B + b) * groups + c / KEEP_GROUP] = (uint8_t)mine;
-  if (FAST) {
-    __syncwarp();
-    const int k = lane >> 2, col = c / SCAN_COLS * SCAN_COLS + (lane & 3) * 16;
-    const uint4 row = *reinterpret_cast<const uint4*>(s_codes + lane * 16);
-    if (t0 + k < len && col < p.N) *reinterpret_cast<uint4*>(codes + ((int64_t)(t0 + k) * p.B + b) * p.N + col) = row;
-    __syncwarp();
-  }
-}
-
 __device__ __forceinline__ int length_of(const ScanParams& p, int b) {
   return p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
 }
 
-// Zeros at the steps [t0, T) of two channels, one step per warp of the cluster.
-template <bool PAIRS, typename IO>
-__device__ __forceinline__ void zero_steps(const ScanParams& p, IO* out, const int64_t* stride, int b, int c, int n_ok, int t0, int first,
-                                           int step) {
-  for (int64_t t = (int64_t)t0 + first; t < p.T; t += step)
-    store_pair<PAIRS>(out + t * stride[0] + b * stride[1], c, n_ok, make_float2(0.f, 0.f));
+// Where a thread stands: its block's chunk within the turn, its warp's steps within the chunk, its two channels.
+struct Place {
+  int S, rank, lane, warp, b, col0, c, n_ok, len, per_turn, ahead;
+};
+__device__ __forceinline__ Place place_of(const ScanParams& p, const cg::cluster_group& cluster) {
+  Place w;
+  w.S = (int)cluster.num_blocks();
+  w.rank = (int)cluster.block_rank();
+  w.lane = threadIdx.x & 31;
+  w.warp = threadIdx.x >> 5;
+  const int tile = (int)blockIdx.x / w.S;
+  w.b = tile / p.n_tiles;
+  w.col0 = (tile % p.n_tiles) * SCAN_COLS;
+  w.c = w.col0 + 2 * w.lane;
+  w.n_ok = min(max(p.N - w.c, 0), 2);
+  w.len = length_of(p, w.b);
+  w.per_turn = w.S * SNN_SCAN_CHUNK;
+  w.ahead = w.rank * SNN_SCAN_CHUNK + w.warp * SCAN_K;
+  return w;
 }
 
-// ---- staging ------------------------------------------------------------------------------------------------
-// Pairs on their way from HBM: every thread copies its own pairs of the coming turns to shared memory (cp.async, 4 or 8
-// bytes), as many turns ahead as the ring is deep, and reads back only what it copied itself: no barrier, and the loads of
-// a turn are in flight while the ones before it are computed and handed on.
-template <typename IO> struct Ring { static constexpr int DEPTH = sizeof(IO) == 4 ? 2 : 3; };
+// Zeros at the steps [from, T) of two channels, one step per warp of the cluster.
+template <bool IN_PAIRS, typename IO>
+__device__ __forceinline__ void zero_steps(const ScanParams& p, const Place& w, IO* out, const int64_t* stride, int from) {
+  for (int64_t t = (int64_t)from + w.rank * SCAN_WARPS + w.warp; t < p.T; t += w.S * SCAN_WARPS)
+    store_pair<IN_PAIRS>(out + t * stride[0] + w.b * stride[1], w.c, w.n_ok, make_float2(0.f, 0.f));
+}
+
+// ---- inputs and outputs of a turn -----------------------------------------------------------------------------
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int y, int z, const void* smem_src) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z),
+               "r"(smem_u32(smem_src)) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int PENDING> __device__ __forceinline__ void bulk_read_done() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory"); }
+
 template <int BYTES> __device__ __forceinline__ void copy_async(void* smem, const void* gmem) {
-  if (BYTES == 16)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem) : "memory");
-  else
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem), "n"(BYTES)
-                 : "memory");
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem), "n"(BYTES) : "memory");
 }
 __device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
-constexpr int PIECE = SCAN_K * SCAN_THREADS;          // pairs of one tensor that a block needs for a turn
-constexpr int CODE_PIECE = SCAN_K * SCAN_WARPS * SCAN_COLS;   // bytes, if they are 8-bit codes
-
-// Copies this thread's SCAN_K steps from t0 on to smem[k * SCAN_THREADS]; behind the sequence's end the last step again.
+// PAIRS: this thread's pairs of SCAN_K steps from t0 on, to where a tile by TMA would have them; behind the sequence's end
+// the last step again.
 template <typename IO>
-__device__ __forceinline__ void stage(typename Pair<IO>::raw* smem, const IO* column, int64_t stride, int t0, int len) {
-  if (t0 + SCAN_K <= len) {
-    const IO* at = column + t0 * stride;
+__device__ __forceinline__ void stage_pairs(IO* tile, const IO* sample, int64_t stride, const Place& w, int t0) {
+  IO* const to = tile + w.warp * WARP_PIECE + 2 * w.lane;
+  const IO* const column = sample + (w.n_ok ? w.c : 0);
 #pragma unroll
-    for (int k = 0; k < SCAN_K; ++k, at += stride) copy_async<2 * sizeof(IO)>(smem + k * SCAN_THREADS, at);
-  } else {
-#pragma unroll
-    for (int k = 0; k < SCAN_K; ++k) copy_async<2 * sizeof(IO)>(smem + k * SCAN_THREADS, column + min(t0 + k, len - 1) * stride);
-  }
+  for (int k = 0; k < SCAN_K; ++k) copy_async<2 * sizeof(IO)>(to + k * SCAN_COLS, column + min(t0 + k, w.len - 1) * stride);
 }
-// The codes of the warp's steps, 16 bytes per lane, to the warp's 512 bytes at smem.
-__device__ __forceinline__ void stage_codes(unsigned char* smem, const uint8_t* codes, const ScanParams& p, int b, int col0, int t0, int len) {
-  const int lane = threadIdx.x & 31, col = col0 + (lane & 3) * 16;
-  const int64_t row = (int64_t)min(t0 + (lane >> 2), len - 1) * p.B + b;
-  if (col < p.N) copy_async<16>(smem + lane * 16, codes + row * p.N + col);
+// This thread's pairs out of a staged tile.
+template <typename IO>
+__device__ __forceinline__ void read_pairs(float2 (&v)[SCAN_K], const void* tile, const Place& w) {
+  using raw = typename Pair<IO>::raw;
+  const raw* const at = reinterpret_cast<const raw*>(reinterpret_cast<const IO*>(tile) + w.warp * WARP_PIECE) + w.lane;
+#pragma unroll
+  for (int k = 0; k < SCAN_K; ++k) v[k] = to_f32(at[k * (SCAN_COLS / 2)]);
+}
+// This thread's values straight from memory.
+template <typename IO>
+__device__ __forceinline__ void load_values(float2 (&v)[SCAN_K], const IO* sample, int64_t stride, const Place& w, int t0) {
+#pragma unroll
+  for (int k = 0; k < SCAN_K; ++k) v[k] = load_pair<false>(sample + min(t0 + k, w.len - 1) * stride, w.c, w.n_ok);
+}
+
+// ---- kept rows in 8 bits ------------------------------------------------------------------------------------
+// Encodes the warp's steps t0.. (those before the sequence's end); codes to s_codes (TILES: they leave by TMA) or to memory.
+template <int FORMAT, bool TO_SMEM>
+__device__ __forceinline__ void keep_steps(const float2 (&v)[SCAN_K], const ScanParams& p, const Place& w, int t0, uint8_t* codes,
+                                           uint8_t* scales, unsigned char* s_codes) {
+  uint32_t mine = 0;
+#pragma unroll
+  for (int k = 0; k < SCAN_K; ++k) {
+    uint32_t byte;
+    const uint32_t pair = encode_row<FORMAT>(v[k], w.n_ok, byte);
+    if (w.lane == k) mine = byte;
+    if (TO_SMEM) {
+      *reinterpret_cast<uint16_t*>(s_codes + k * SCAN_COLS + 2 * w.lane) = (uint16_t)pair;
+    } else if (t0 + k < w.len) {
+      uint8_t* const at = codes + ((int64_t)(t0 + k) * p.B + w.b) * p.N + w.c;
+      if (w.n_ok > 0) at[0] = (uint8_t)(pair & 255u);
+      if (w.n_ok > 1) at[1] = (uint8_t)(pair >> 8);
+    }
+  }
+  if (w.lane < SCAN_K && t0 + w.lane < w.len) scales[((int64_t)(t0 + w.lane) * p.B + w.b) * p.n_tiles + w.col0 / KEEP_GROUP] = (uint8_t)mine;
+}
+template <bool TO_SMEM>
+__device__ __forceinline__ void keep_steps(int format, const float2 (&v)[SCAN_K], const ScanParams& p, const Place& w, int t0, uint8_t* codes,
+                                           uint8_t* scales, unsigned char* s_codes) {
+  if (format == SNN_KEEP_INT8) keep_steps<SNN_KEEP_INT8, TO_SMEM>(v, p, w, t0, codes, scales, s_codes);
+  if (format == SNN_KEEP_E4M3) keep_steps<SNN_KEEP_E4M3, TO_SMEM>(v, p, w, t0, codes, scales, s_codes);
+}
+// The kept values of this thread's steps; the scales' bytes lie in lanes from, from + 1, ...
+template <int FORMAT, typename IO>
+__device__ __forceinline__ void decode_steps(float2 (&v)[SCAN_K], const void* tile, const Place& w, uint32_t bytes, int from) {
+  const uint16_t* const at = reinterpret_cast<const uint16_t*>(reinterpret_cast<const unsigned char*>(tile) + w.warp * WARP_PIECE) + w.lane;
+  const float scale = keep_scale_value(bytes);
+#pragma unroll
+  for (int k = 0; k < SCAN_K; ++k) v[k] = keep_decode2<IO, FORMAT>(at[k * (SCAN_COLS / 2)], __shfl_sync(0xffffffffu, scale, from + k));
+}
+template <typename IO>
+__device__ __forceinline__ void decode_from_memory(float2 (&v)[SCAN_K], const uint8_t* codes, const ScanParams& p, const Place& w, int t0,
+                                                   uint32_t bytes, int from, int format) {
+#pragma unroll
+  for (int k = 0; k < SCAN_K; ++k)
+    v[k] = decode_pair<IO>(codes + ((int64_t)min(t0 + k, w.len - 1) * p.B + w.b) * p.N, __shfl_sync(0xffffffffu, bytes, from + k), w.c, w.n_ok,
+                           format);
 }
 
 // ---- between the blocks of a cluster --------------------------------------------------------------------------
 // Every turn each block sends the summary of its chunk to all blocks: asynchronous stores to their shared memory that
 // count towards an mbarrier there.  Two buffers are enough: a block sends the summary of turn i + 2 only after it has all of
-// turn i + 1, and a block sends that one only after its warps have read those of turn i.
+// turn i + 1, and a block sends that one only after it has read those of turn i.
 struct ClusterExchange {
   float4 slot[2][SCAN_MAX_CLUSTER][32];
   uint64_t full[2];
 };
-__device__ __forceinline__ void exchange_init(ClusterExchange& x, cg::cluster_group& cluster) {
-  if (threadIdx.x == 0) {
-    mbar_init(&x.full[0], 1);
-    mbar_init(&x.full[1], 1);
-    mbar_fence_init();
-  }
-  cluster.sync();
-}
 // by one whole warp
 __device__ __forceinline__ void exchange_send(ClusterExchange& x, int i, int S, int rank, float4 v) {
   const int lane = threadIdx.x & 31;
@@ -206,124 +252,168 @@ __device__ __forceinline__ void exchange_send(ClusterExchange& x, int i, int S, 
                  : "memory");
   }
 }
-// by all threads; false if the summaries did not come (then the caller makes its results NaN)
+// by the same warp; false if the summaries did not come (then the caller makes its results NaN)
 __device__ __forceinline__ bool exchange_wait(ClusterExchange& x, int i) { return mbar_wait(&x.full[i & 1], (uint32_t)(i >> 1) & 1u); }
 
+struct Shared {
+  ClusterExchange exchange;
+  uint64_t landed[SCAN_DEPTH];   // TILES: the bytes of a slot of the ring
+};
+__device__ __forceinline__ void shared_init(Shared& s, cg::cluster_group& cluster, int S) {
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) mbar_init(&s.exchange.full[i], 1);
+    for (int i = 0; i < SCAN_DEPTH; ++i) mbar_init(&s.landed[i], 1);
+    mbar_fence_init();
+  }
+  if (S > 1) cluster.sync();
+  else __syncthreads();
+}
+__device__ __forceinline__ float2 nan2() { return both(__uint_as_float(0x7fc00000u)); }
+
 // ---- forward -----------------------------------------------------------------------------------------------
-template <typename IO, bool KEEP, bool FAST>
-__global__ void __launch_bounds__(SCAN_THREADS, 3) scan_forward_kernel(const ScanParams p) {
-  using raw = typename Pair<IO>::raw;
-  constexpr int DEPTH = Ring<IO>::DEPTH;
-  extern __shared__ __align__(16) unsigned char s_ring[];   // FAST: [DEPTH][x, gate][SCAN_K][SCAN_THREADS] pairs
-  __shared__ float4 s_warp[2][SCAN_WARPS][32];
-  __shared__ ClusterExchange s_exchange;
-  __shared__ __align__(16) unsigned char s_codes[KEEP ? SCAN_WARPS : 1][SCAN_K * SCAN_COLS];
+template <typename IO> __host__ __device__ constexpr int forward_slot() { return 2 * PIECE * (int)sizeof(IO); }
+template <typename IO, bool KEEP> __host__ __device__ constexpr int forward_out() { return WARP_PIECE * ((int)sizeof(IO) + (KEEP ? 2 : 0)); }   // per warp and buffer
+
+template <typename IO, bool KEEP, int PATH>
+__global__ void __launch_bounds__(SCAN_THREADS, 3) scan_forward_kernel(const __grid_constant__ ScanParams p) {
+  constexpr int SLOT = forward_slot<IO>(), OUT = forward_out<IO, KEEP>();
+  extern __shared__ __align__(128) unsigned char s_dyn[];   // ring [SCAN_DEPTH][x, gate]; TILES: then out [SCAN_WARPS][2][h, codes]
+  __shared__ float4 s_sum[SCAN_WARPS][32];
+  __shared__ float2 s_start[SCAN_WARPS][32];
+  __shared__ Shared s;
   cg::cluster_group cluster = cg::this_cluster();
-  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int tile = (int)blockIdx.x / S, b = tile / p.n_tiles, c = (tile % p.n_tiles) * SCAN_COLS + 2 * lane;
-  const int n_ok = min(max(p.N - c, 0), 2);
-  const int len = length_of(p, b);
-  const IO* const x = (const IO*)p.x + b * p.xs[1];
-  const IO* const gate = (const IO*)p.gate + b * p.gs[1];
-  IO* const h_out = (IO*)p.h + b * p.hs[1] + c;
-  const int per_turn = S * SNN_SCAN_CHUNK, ahead = rank * SNN_SCAN_CHUNK + warp * SCAN_K;
-  raw* const ring = reinterpret_cast<raw*>(s_ring) + threadIdx.x;
-  auto issue = [&](int turn, int slot) {
-    if (FAST && turn < len) {
-      stage<IO>(ring + slot * (2 * PIECE), x + (n_ok ? c : 0), p.xs[0], turn + ahead, len);
-      stage<IO>(ring + slot * (2 * PIECE) + PIECE, gate + (n_ok ? c : 0), p.gs[0], turn + ahead, len);
+  const Place w = place_of(p, cluster);
+  const IO* const x = (const IO*)p.x + w.b * p.xs[1];
+  const IO* const gate = (const IO*)p.gate + w.b * p.gs[1];
+  IO* const h_out = (IO*)p.h + w.b * p.hs[1];
+  auto issue = [&](int turn, int slot) {   // TILES: one thread; PAIRS: all
+    unsigned char* const at = s_dyn + slot * SLOT;
+    if constexpr (PATH == TILES) {
+      if (turn < w.len) {
+        mbar_arrive_expect_tx(&s.landed[slot], SLOT);
+        tma_load_3d(at, &p.in[0], w.col0, w.b, turn + w.rank * SNN_SCAN_CHUNK, &s.landed[slot]);
+        tma_load_3d(at + SLOT / 2, &p.in[1], w.col0, w.b, turn + w.rank * SNN_SCAN_CHUNK, &s.landed[slot]);
+      }
     }
-    if (FAST) copies_issued();
+    if constexpr (PATH == PAIRS) {
+      if (turn < w.len) {
+        stage_pairs<IO>(reinterpret_cast<IO*>(at), x, p.xs[0], w, turn + w.ahead);
+        stage_pairs<IO>(reinterpret_cast<IO*>(at + SLOT / 2), gate, p.gs[0], w, turn + w.ahead);
+      }
+      copies_issued();
+    }
   };
-  float2 carry = load_state(p.state, b, p.N, c, n_ok);
-  int slot = 0;
-  for (int d = 0; d < DEPTH - 1; ++d) issue(d * per_turn, d);
-  if (S > 1) exchange_init(s_exchange, cluster);
-  for (int turn = 0, i = 0; turn < len; turn += per_turn, ++i) {
-    const int buf = i & 1, chunk0 = turn + rank * SNN_SCAN_CHUNK, t0 = turn + ahead;
-    const bool full = t0 + SCAN_K <= len;
+  shared_init(s, cluster, w.S);
+  const bool loader = PATH == PAIRS || (PATH == TILES && threadIdx.x == SCAN_THREADS - 32);
+  if (loader)
+    for (int d = 0; d < SCAN_DEPTH; ++d) issue(d * w.per_turn, d);
+  float2 carry = w.warp == 0 ? load_state(p.state, w.b, p.N, w.c, w.n_ok) : both(0.f);   // warp 0 chains the summaries
+  bool alive = true;
+  int turn = 0;
+  for (int i = 0; turn < w.len; turn += w.per_turn, ++i) {
+    const int slot = i % SCAN_DEPTH, chunk0 = turn + w.rank * SNN_SCAN_CHUNK, t0 = turn + w.ahead;
+    const bool full = t0 + SCAN_K <= w.len;
+    unsigned char* const out = s_dyn + SCAN_DEPTH * SLOT + (w.warp * 2 + (i & 1)) * OUT;
     float2 xv[SCAN_K], gv[SCAN_K];
-    if (FAST) {
-      issue(turn + (DEPTH - 1) * per_turn, slot == 0 ? DEPTH - 1 : slot - 1);
-      copies_landed<DEPTH - 1>();
-      const raw* const at = ring + slot * (2 * PIECE);
-      slot = slot == DEPTH - 1 ? 0 : slot + 1;
-#pragma unroll
-      for (int k = 0; k < SCAN_K; ++k) {
-        xv[k] = to_f32(at[k * SCAN_THREADS]);
-        gv[k] = to_f32(at[PIECE + k * SCAN_THREADS]);
-      }
+    if constexpr (PATH == SCALAR) {
+      load_values<IO>(xv, x, p.xs[0], w, t0);
+      load_values<IO>(gv, gate, p.gs[0], w, t0);
     } else {
-#pragma unroll
-      for (int k = 0; k < SCAN_K; ++k) {
-        xv[k] = load_pair<FAST>(x + min(t0 + k, len - 1) * p.xs[0], c, n_ok);
-        gv[k] = load_pair<FAST>(gate + min(t0 + k, len - 1) * p.gs[0], c, n_ok);
+      if (PATH == TILES) {
+        if (alive) alive = mbar_wait(&s.landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
+        if (w.lane == 0) bulk_read_done<1>();   // the out buffer used two turns ago has been read
+        __syncwarp();
+      } else {
+        copies_landed<SCAN_DEPTH - 1>();
       }
+      read_pairs<IO>(xv, s_dyn + slot * SLOT, w);
+      read_pairs<IO>(gv, s_dyn + slot * SLOT + SLOT / 2, w);
+      if (!alive) gv[0] = nan2();
+      if (PATH == PAIRS) issue(turn + SCAN_DEPTH * w.per_turn, slot);
     }
-    if (KEEP) {
-      if (p.x_format == SNN_KEEP_INT8) keep_steps<SNN_KEEP_INT8, FAST>(xv, p, b, c, n_ok, t0, len, p.x_codes, p.x_scales, s_codes[warp]);
-      if (p.x_format == SNN_KEEP_E4M3) keep_steps<SNN_KEEP_E4M3, FAST>(xv, p, b, c, n_ok, t0, len, p.x_codes, p.x_scales, s_codes[warp]);
-      if (p.gate_format == SNN_KEEP_INT8)
-        keep_steps<SNN_KEEP_INT8, FAST>(gv, p, b, c, n_ok, t0, len, p.gate_codes, p.gate_scales, s_codes[warp]);
-      if (p.gate_format == SNN_KEEP_E4M3)
-        keep_steps<SNN_KEEP_E4M3, FAST>(gv, p, b, c, n_ok, t0, len, p.gate_codes, p.gate_scales, s_codes[warp]);
+    if constexpr (KEEP) {
+      unsigned char* const codes = out + WARP_PIECE * sizeof(IO);
+      keep_steps<PATH == TILES>(p.x_format, xv, p, w, t0, p.x_codes, p.x_scales, codes);
+      keep_steps<PATH == TILES>(p.gate_format, gv, p, w, t0, p.gate_codes, p.gate_scales, codes + WARP_PIECE);
     }
     float2 in[SCAN_K];
     coefficients(gv, in, p.mode);   // gv becomes a, and xv b
 #pragma unroll
-    for (int k = 0; k < SCAN_K; ++k) xv[k] = make_float2(in[k].x * xv[k].x, in[k].y * xv[k].y);
+    for (int k = 0; k < SCAN_K; ++k) xv[k] = mul2(in[k], xv[k]);
     if (!full) {
 #pragma unroll
       for (int k = 0; k < SCAN_K; ++k)
-        if (t0 + k >= len) gv[k] = make_float2(1.f, 1.f), xv[k] = make_float2(0.f, 0.f);
+        if (t0 + k >= w.len) gv[k] = both(1.f), xv[k] = both(0.f);
     }
-    Map2 mine{gv[0].x, xv[0].x, gv[0].y, xv[0].y};
+    Map2 mine{gv[0], xv[0]};
 #pragma unroll
-    for (int k = 1; k < SCAN_K; ++k) mine = then(mine, Map2{gv[k].x, xv[k].x, gv[k].y, xv[k].y});
-    s_warp[buf][warp][lane] = as4(mine);
+    for (int k = 1; k < SCAN_K; ++k) mine = then(mine, Map2{gv[k], xv[k]});
+    s_sum[w.warp][w.lane] = as4(mine);
     __syncthreads();
-    float2 h;                // the state before this warp's steps
-    float2 start = carry;    // ... before this block's chunk
-    if (S > 1) {
-      if (warp == 0) {
+    if (PATH == TILES && loader) issue(turn + SCAN_DEPTH * w.per_turn, slot);   // all warps have read the slot
+    if (w.warp == 0) {
+      float2 h = carry;
+      if (w.S > 1) {
         Map2 all = mine;
-        for (int w = 1; w < SCAN_WARPS; ++w) all = then(all, as_map(s_warp[buf][w][lane]));
-        exchange_send(s_exchange, i, S, rank, as4(all));
-      }
-      const bool came = exchange_wait(s_exchange, i);
-      for (int r = 0; r < S; ++r) {
-        if (r == rank) start = carry;
-        carry = apply(as_map(s_exchange.slot[buf][r][lane]), carry);
-      }
-      if (!came) carry.x = carry.y = start.x = start.y = __uint_as_float(0x7fc00000u);
-      h = start;
-      for (int w = 0; w < warp; ++w) h = apply(as_map(s_warp[buf][w][lane]), h);
-    } else {
 #pragma unroll
-      for (int w = 0; w < SCAN_WARPS; ++w) {
-        if (w == warp) h = carry;
-        carry = apply(as_map(s_warp[buf][w][lane]), carry);
+        for (int v = 1; v < SCAN_WARPS; ++v) all = then(all, as_map(s_sum[v][w.lane]));
+        exchange_send(s.exchange, i, w.S, w.rank, as4(all));
+        const bool came = exchange_wait(s.exchange, i);
+        for (int r = 0; r < w.S; ++r) {
+          if (r == w.rank) h = carry;
+          carry = apply(as_map(s.exchange.slot[i & 1][r][w.lane]), carry);
+        }
+        if (!came) h = carry = nan2();
       }
+      if (!alive) h = carry = nan2();
+      if (KEEP && chunk0 < w.len) store_state(p.states, (int64_t)(chunk0 / SNN_SCAN_CHUNK) * p.B + w.b, p.N, w.c, w.n_ok, h);
+#pragma unroll
+      for (int v = 0; v < SCAN_WARPS; ++v) {
+        s_start[v][w.lane] = h;
+        h = apply(as_map(s_sum[v][w.lane]), h);
+      }
+      if (w.S == 1) carry = h;
     }
-    if (KEEP && warp == 0 && chunk0 < len)
-      store_state(p.states, (int64_t)(chunk0 / SNN_SCAN_CHUNK) * p.B + b, p.N, c, n_ok, start);
-    IO* at = h_out + t0 * p.hs[0];
+    __syncthreads();
+    float2 h = s_start[w.warp][w.lane];
+    if constexpr (PATH == TILES) {
+      IO* const to = reinterpret_cast<IO*>(out) + 2 * w.lane;
 #pragma unroll
-    for (int k = 0; k < SCAN_K; ++k, at += p.hs[0]) {
-      h.x = fmaf(gv[k].x, h.x, xv[k].x);
-      h.y = fmaf(gv[k].y, h.y, xv[k].y);
-      if (full || t0 + k < len) store_pair<FAST>(at, 0, n_ok, h);
+      for (int k = 0; k < SCAN_K; ++k) {
+        h = fma2(gv[k], h, xv[k]);
+        const float2 shown = full || t0 + k < w.len ? h : both(0.f);
+        store_pair<true>(to + k * SCAN_COLS, 0, 2, shown);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (w.lane == 0) {
+        if (t0 < p.T) {
+          tma_store_3d(&p.out[0], w.col0, w.b, t0, out);
+          if (KEEP && p.x_format != SNN_KEEP_RAW) tma_store_3d(&p.out[2], w.col0, w.b, t0, out + WARP_PIECE * sizeof(IO));
+          if (KEEP && p.gate_format != SNN_KEEP_RAW) tma_store_3d(&p.out[3], w.col0, w.b, t0, out + WARP_PIECE * (sizeof(IO) + 1));
+        }
+        bulk_commit();
+      }
+    } else {
+      IO* at = h_out + t0 * p.hs[0];
+#pragma unroll
+      for (int k = 0; k < SCAN_K; ++k, at += p.hs[0]) {
+        h = fma2(gv[k], h, xv[k]);
+        if (full || t0 + k < w.len) store_pair<PATH == PAIRS>(at, w.c, w.n_ok, h);
+      }
     }
   }
-  if (rank == 0 && warp == 0) store_state(p.last, b, p.N, c, n_ok, carry);
-  zero_steps<FAST>(p, (IO*)p.h, p.hs, b, c, n_ok, len, rank * SCAN_WARPS + warp, S * SCAN_WARPS);
-  if (S > 1) cluster.sync();   // no block leaves while another may still write to its shared memory
+  if (w.rank == 0 && w.warp == 0) store_state(p.last, w.b, p.N, w.c, w.n_ok, carry);
+  zero_steps<PATH != SCALAR>(p, w, (IO*)p.h, p.hs, PATH == TILES ? turn : w.len);
+  if (PATH == TILES && w.lane == 0) bulk_read_done<0>();
+  if (!alive)
+    for (int i = 0; i < 100; ++i) __nanosleep(20000);   // copies that did not come in time may still be under way
+  if (w.S > 1) cluster.sync();   // no block leaves while another may still write to its shared memory
 }
 
 // Few steps (the token of a serving loop): a thread takes two channels of one sample through all of them.
-template <typename IO, bool PAIRS>
-__global__ void __launch_bounds__(128) scan_short_kernel(const ScanParams p) {
+template <typename IO, bool IN_PAIRS>
+__global__ void __launch_bounds__(128) scan_short_kernel(const __grid_constant__ ScanParams p) {
   const int pairs = (p.N + 1) / 2;
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= (int64_t)p.B * pairs) return;
@@ -337,15 +427,15 @@ __global__ void __launch_bounds__(128) scan_short_kernel(const ScanParams p) {
   for (int64_t t = 0; t < p.T; ++t) {
     float2 shown = make_float2(0.f, 0.f);
     if (t < len) {
-      const float2 xv = load_pair<PAIRS>(x + t * p.xs[0], c, n_ok), gv = load_pair<PAIRS>(gate + t * p.gs[0], c, n_ok);
-      float a0 = gv.x, a1 = gv.y, i0 = 1.f, i1 = 1.f;
+      float2 xv = load_pair<IN_PAIRS>(x + t * p.xs[0], c, n_ok), a = load_pair<IN_PAIRS>(gate + t * p.gs[0], c, n_ok);
       if (p.mode != SNN_SCAN_DIRECT) {
-        sigmoids(gv.x, a0, i0);
-        sigmoids(gv.y, a1, i1);
+        float2 in;
+        sigmoids(a, a, in);
+        xv = mul2(in, xv);
       }
-      h = shown = make_float2(fmaf(a0, h.x, i0 * xv.x), fmaf(a1, h.y, i1 * xv.y));
+      h = shown = fma2(a, h, xv);
     }
-    store_pair<PAIRS>(h_out + t * p.hs[0], c, n_ok, shown);
+    store_pair<IN_PAIRS>(h_out + t * p.hs[0], c, n_ok, shown);
   }
   store_state(p.last, b, p.N, c, n_ok, h);
 }
@@ -353,307 +443,247 @@ __global__ void __launch_bounds__(128) scan_short_kernel(const ScanParams p) {
 // ---- backward ----------------------------------------------------------------------------------------------
 // The quantity handed from step to step is e_t = a_t D_t = a_t (dh_t + e_{t+1}), again an affine map, composed from the
 // last step to the first; the states of the chunk are recomputed from its checkpoint by the forward maps.  A block's
-// chunk starts at a checkpoint, so only e crosses blocks.
-template <typename IO>
-__device__ __forceinline__ float2 decode_pair(const uint8_t* row, uint32_t scale, int c, int n_ok, int format) {
-  const uint32_t pair = (uint32_t)row[n_ok ? c : 0] | (uint32_t)row[n_ok == 2 ? c + 1 : 0] << 8;
-  return format == SNN_KEEP_INT8 ? keep_decode2<IO, SNN_KEEP_INT8>(pair, keep_scale_value(scale))
-                                 : keep_decode2<IO, SNN_KEEP_E4M3>(pair, keep_scale_value(scale));
-}
-template <int FORMAT, typename IO>
-__device__ __forceinline__ void decode_steps(float2 (&v)[SCAN_K], const unsigned char* s_codes, uint32_t scales, int from) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int k = 0; k < SCAN_K; ++k) {
-    const float scale = keep_scale_value(__shfl_sync(0xffffffffu, scales, from + k));
-    v[k] = keep_decode2<IO, FORMAT>(*reinterpret_cast<const uint16_t*>(s_codes + k * SCAN_COLS + 2 * lane), scale);
-  }
-}
-
-template <typename IO, bool FAST>
-__global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const ScanParams p) {
-  using raw = typename Pair<IO>::raw;
-  constexpr int DEPTH = Ring<IO>::DEPTH;
-  extern __shared__ __align__(16) unsigned char s_ring[];   // FAST: [DEPTH] of dh pairs, x and gate (pairs or codes)
-  __shared__ float4 s_fwd[2][SCAN_WARPS][32];
-  __shared__ float4 s_bwd[2][SCAN_WARPS][32];
-  __shared__ ClusterExchange s_exchange;
+// chunk starts at a checkpoint, so only e crosses blocks.  Warp 0 chains the states, warp 1 the e.
+template <typename IO, int PATH>
+__global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const __grid_constant__ ScanParams p) {
+  constexpr int VALUES = PIECE * (int)sizeof(IO), OUT = 2 * WARP_PIECE * (int)sizeof(IO);
+  extern __shared__ __align__(128) unsigned char s_dyn[];   // ring [SCAN_DEPTH] of dh, x, gate (values or codes); TILES: out
+  __shared__ float4 s_forth[SCAN_WARPS][32];
+  __shared__ float2 s_back[SCAN_WARPS][32];
+  __shared__ float2 s_h[SCAN_WARPS][32], s_e[SCAN_WARPS][32];
+  __shared__ Shared s;
   cg::cluster_group cluster = cg::this_cluster();
-  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int tile = (int)blockIdx.x / S, b = tile / p.n_tiles, col0 = (tile % p.n_tiles) * SCAN_COLS, c = col0 + 2 * lane;
-  const int n_ok = min(max(p.N - c, 0), 2), groups = p.n_tiles;
-  const int len = length_of(p, b);
-  const IO* const x = (const IO*)p.x + b * p.xs[1];
-  const IO* const gate = (const IO*)p.gate + b * p.gs[1];
-  const IO* const dh = (const IO*)p.dh + b * p.dhs[1];
-  IO* const dx = (IO*)p.dx + b * p.dxs[1] + c;
-  IO* const dgate = (IO*)p.dgate + b * p.dgs[1] + c;
+  const Place w = place_of(p, cluster);
+  const IO* const x = (const IO*)p.x + w.b * p.xs[1];
+  const IO* const gate = (const IO*)p.gate + w.b * p.gs[1];
+  const IO* const dh = (const IO*)p.dh + w.b * p.dhs[1];
   const bool raw_x = p.x_format == SNN_KEEP_RAW, raw_gate = p.gate_format == SNN_KEEP_RAW;
-  const int per_turn = S * SNN_SCAN_CHUNK, ahead = rank * SNN_SCAN_CHUNK + warp * SCAN_K;
-  const int x_at = PIECE * (int)sizeof(raw), gate_at = x_at + (raw_x ? PIECE * (int)sizeof(raw) : CODE_PIECE);
-  const int slot_bytes = gate_at + (raw_gate ? PIECE * (int)sizeof(raw) : CODE_PIECE);
-  const int code_off = warp * SCAN_K * SCAN_COLS;
-  auto pairs_of = [&](int at) { return reinterpret_cast<raw*>(s_ring + at) + threadIdx.x; };
+  const int x_at = VALUES, gate_at = x_at + (raw_x ? VALUES : PIECE), slot_bytes = gate_at + (raw_gate ? VALUES : PIECE);
   auto issue = [&](int turn, int slot) {
-    if (FAST && turn >= 0) {
-      const int at = slot * slot_bytes, t0 = turn + ahead;
-      stage<IO>(pairs_of(at), dh + (n_ok ? c : 0), p.dhs[0], t0, len);
-      if (raw_x) stage<IO>(pairs_of(at + x_at), x + (n_ok ? c : 0), p.xs[0], t0, len);
-      else stage_codes(s_ring + at + x_at + code_off, p.x_codes, p, b, col0, t0, len);
-      if (raw_gate) stage<IO>(pairs_of(at + gate_at), gate + (n_ok ? c : 0), p.gs[0], t0, len);
-      else stage_codes(s_ring + at + gate_at + code_off, p.gate_codes, p, b, col0, t0, len);
+    unsigned char* const at = s_dyn + slot * slot_bytes;
+    if constexpr (PATH == TILES) {
+      if (turn >= 0) {
+        const int t = turn + w.rank * SNN_SCAN_CHUNK;
+        mbar_arrive_expect_tx(&s.landed[slot], slot_bytes);
+        tma_load_3d(at, &p.in[0], w.col0, w.b, t, &s.landed[slot]);
+        tma_load_3d(at + x_at, &p.in[1], w.col0, w.b, t, &s.landed[slot]);
+        tma_load_3d(at + gate_at, &p.in[2], w.col0, w.b, t, &s.landed[slot]);
+      }
     }
-    if (FAST) copies_issued();
+    if constexpr (PATH == PAIRS) {   // (8-bit codes are read from memory on this path)
+      if (turn >= 0) {
+        stage_pairs<IO>(reinterpret_cast<IO*>(at), dh, p.dhs[0], w, turn + w.ahead);
+        if (raw_x) stage_pairs<IO>(reinterpret_cast<IO*>(at + x_at), x, p.xs[0], w, turn + w.ahead);
+        if (raw_gate) stage_pairs<IO>(reinterpret_cast<IO*>(at + gate_at), gate, p.gs[0], w, turn + w.ahead);
+      }
+      copies_issued();
+    }
   };
   // scale bytes: of x in lanes 0..7 (one per step), of the gate in lanes 8..15, read one turn ahead
   auto load_scales = [&](int turn) -> uint32_t {
-    const int64_t row = (int64_t)max(min(turn + ahead + (lane & 7), len - 1), 0) * p.B + b;
-    if (turn < 0) return 0;
-    if (lane < 8) return raw_x ? 0 : p.x_scales[row * groups + col0 / KEEP_GROUP];
-    if (lane < 16) return raw_gate ? 0 : p.gate_scales[row * groups + col0 / KEEP_GROUP];
-    return 0;
+    if (turn < 0 || w.lane >= 16 || (w.lane < 8 ? raw_x : raw_gate)) return 0u;
+    const int64_t row = (int64_t)min(turn + w.ahead + (w.lane & 7), w.len - 1) * p.B + w.b;
+    return (w.lane < 8 ? p.x_scales : p.gate_scales)[row * p.n_tiles + w.col0 / KEEP_GROUP];
   };
   auto load_start = [&](int turn) {   // the kept state of this block's chunk
-    if (turn < 0) return make_float2(0.f, 0.f);
-    return load_state(p.states, (int64_t)(min(turn + rank * SNN_SCAN_CHUNK, len - 1) / SNN_SCAN_CHUNK) * p.B + b, p.N, c, n_ok);
+    if (turn < 0 || w.warp != 0) return both(0.f);
+    return load_state(p.states, (int64_t)(min(turn + w.rank * SNN_SCAN_CHUNK, w.len - 1) / SNN_SCAN_CHUNK) * p.B + w.b, p.N, w.c, w.n_ok);
   };
-  float2 carry = load_state(p.dlast, b, p.N, c, n_ok);   // e behind the turn's last step
-  int slot = 0;
-  const int last_turn = (len + per_turn - 1) / per_turn * per_turn - per_turn;
-  for (int d = 0; d < DEPTH - 1; ++d) issue(last_turn - d * per_turn, d);
+  shared_init(s, cluster, w.S);
+  const bool loader = PATH == PAIRS || (PATH == TILES && threadIdx.x == SCAN_THREADS - 32);
+  const int turns = (w.len + w.per_turn - 1) / w.per_turn, last_turn = (turns - 1) * w.per_turn;
+  if (loader)
+    for (int d = 0; d < SCAN_DEPTH; ++d) issue(last_turn - d * w.per_turn, d);
+  float2 carry = w.warp == 1 ? load_state(p.dlast, w.b, p.N, w.c, w.n_ok) : both(0.f);   // e behind the turn's last step
   uint32_t next_scales = load_scales(last_turn);
   float2 next_start = load_start(last_turn);
-  if (S > 1) exchange_init(s_exchange, cluster);
-  for (int turn = last_turn, i = 0; turn >= 0; turn -= per_turn, ++i) {
-    const int buf = i & 1, t0 = turn + ahead;
-    const bool full = t0 + SCAN_K <= len;
+  bool alive = true;
+  for (int turn = last_turn, i = 0; turn >= 0; turn -= w.per_turn, ++i) {
+    const int slot = i % SCAN_DEPTH, t0 = turn + w.ahead;
+    const bool full = t0 + SCAN_K <= w.len;
+    unsigned char* const out = s_dyn + SCAN_DEPTH * slot_bytes + (w.warp * 2 + (i & 1)) * OUT;
     float2 xv[SCAN_K], a[SCAN_K], in[SCAN_K], d[SCAN_K];
     const uint32_t scales = next_scales;
-    float2 h = next_start;
-    next_scales = load_scales(turn - per_turn);
-    next_start = load_start(turn - per_turn);
-    if (FAST) {
-      issue(turn - (DEPTH - 1) * per_turn, slot == 0 ? DEPTH - 1 : slot - 1);
-      copies_landed<DEPTH - 1>();
-      __syncwarp();   // codes were copied by other lanes
-      const int at = slot * slot_bytes;
-      slot = slot == DEPTH - 1 ? 0 : slot + 1;
-#pragma unroll
-      for (int k = 0; k < SCAN_K; ++k) d[k] = to_f32(pairs_of(at)[k * SCAN_THREADS]);
-      if (raw_x) {
-#pragma unroll
-        for (int k = 0; k < SCAN_K; ++k) xv[k] = to_f32(pairs_of(at + x_at)[k * SCAN_THREADS]);
-      } else if (p.x_format == SNN_KEEP_INT8) {
-        decode_steps<SNN_KEEP_INT8, IO>(xv, s_ring + at + x_at + code_off, scales, 0);
-      } else {
-        decode_steps<SNN_KEEP_E4M3, IO>(xv, s_ring + at + x_at + code_off, scales, 0);
-      }
-      if (raw_gate) {
-#pragma unroll
-        for (int k = 0; k < SCAN_K; ++k) a[k] = to_f32(pairs_of(at + gate_at)[k * SCAN_THREADS]);
-      } else if (p.gate_format == SNN_KEEP_INT8) {
-        decode_steps<SNN_KEEP_INT8, IO>(a, s_ring + at + gate_at + code_off, scales, 8);
-      } else {
-        decode_steps<SNN_KEEP_E4M3, IO>(a, s_ring + at + gate_at + code_off, scales, 8);
-      }
-      __syncwarp();   // all lanes have read their codes before the slot is filled again
-    } else {
-#pragma unroll
-      for (int k = 0; k < SCAN_K; ++k) {
-        const int64_t t = min(t0 + k, len - 1);
-        d[k] = load_pair<FAST>(dh + t * p.dhs[0], c, n_ok);
-        xv[k] = raw_x ? load_pair<FAST>(x + t * p.xs[0], c, n_ok)
-                      : decode_pair<IO>(p.x_codes + (t * p.B + b) * p.N, __shfl_sync(0xffffffffu, scales, k), c, n_ok, p.x_format);
-        a[k] = raw_gate ? load_pair<FAST>(gate + t * p.gs[0], c, n_ok)
-                        : decode_pair<IO>(p.gate_codes + (t * p.B + b) * p.N, __shfl_sync(0xffffffffu, scales, 8 + k), c, n_ok, p.gate_format);
-      }
+    const float2 start = next_start;
+    next_scales = load_scales(turn - w.per_turn);
+    next_start = load_start(turn - w.per_turn);
+    unsigned char* const at = s_dyn + slot * slot_bytes;
+    if (PATH == TILES) {
+      if (alive) alive = mbar_wait(&s.landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
+      if (w.lane == 0) bulk_read_done<1>();
+      __syncwarp();
     }
+    if (PATH == PAIRS) copies_landed<SCAN_DEPTH - 1>();
+    if constexpr (PATH == SCALAR) load_values<IO>(d, dh, p.dhs[0], w, t0);
+    else read_pairs<IO>(d, at, w);
+    if (raw_x) {
+      if constexpr (PATH == SCALAR) load_values<IO>(xv, x, p.xs[0], w, t0);
+      else read_pairs<IO>(xv, at + x_at, w);
+    } else if constexpr (PATH == TILES) {
+      if (p.x_format == SNN_KEEP_INT8) decode_steps<SNN_KEEP_INT8, IO>(xv, at + x_at, w, scales, 0);
+      else decode_steps<SNN_KEEP_E4M3, IO>(xv, at + x_at, w, scales, 0);
+    } else {
+      decode_from_memory<IO>(xv, p.x_codes, p, w, t0, scales, 0, p.x_format);
+    }
+    if (raw_gate) {
+      if constexpr (PATH == SCALAR) load_values<IO>(a, gate, p.gs[0], w, t0);
+      else read_pairs<IO>(a, at + gate_at, w);
+    } else if constexpr (PATH == TILES) {
+      if (p.gate_format == SNN_KEEP_INT8) decode_steps<SNN_KEEP_INT8, IO>(a, at + gate_at, w, scales, 8);
+      else decode_steps<SNN_KEEP_E4M3, IO>(a, at + gate_at, w, scales, 8);
+    } else {
+      decode_from_memory<IO>(a, p.gate_codes, p, w, t0, scales, 8, p.gate_format);
+    }
+    if (PATH == PAIRS) issue(turn - SCAN_DEPTH * w.per_turn, slot);
+    if (!alive) a[0] = nan2();
     coefficients(a, in, p.mode);
     if (!full) {
 #pragma unroll
       for (int k = 0; k < SCAN_K; ++k)
-        if (t0 + k >= len) a[k] = make_float2(1.f, 1.f), xv[k] = d[k] = in[k] = make_float2(0.f, 0.f);
+        if (t0 + k >= w.len) a[k] = both(1.f), xv[k] = d[k] = in[k] = both(0.f);
     }
-    Map2 forth{a[0].x, in[0].x * xv[0].x, a[0].y, in[0].y * xv[0].y};
+    Map2 forth{a[0], mul2(in[0], xv[0])};
 #pragma unroll
-    for (int k = 1; k < SCAN_K; ++k) forth = then(forth, Map2{a[k].x, in[k].x * xv[k].x, a[k].y, in[k].y * xv[k].y});
+    for (int k = 1; k < SCAN_K; ++k) forth = then(forth, Map2{a[k], mul2(in[k], xv[k])});
     // the way back has the same product of decays; its other part is e before the warp's steps if none came in
-    float2 e0 = make_float2(0.f, 0.f);
+    float2 e0 = mul2(a[SCAN_K - 1], d[SCAN_K - 1]);
 #pragma unroll
-    for (int k = SCAN_K - 1; k >= 0; --k) e0 = make_float2(a[k].x * (d[k].x + e0.x), a[k].y * (d[k].y + e0.y));
-    const Map2 back{forth.a0, e0.x, forth.a1, e0.y};
-    s_fwd[buf][warp][lane] = as4(forth);
-    s_bwd[buf][warp][lane] = as4(back);
+    for (int k = SCAN_K - 2; k >= 0; --k) e0 = mul2(a[k], add2(d[k], e0));
+    s_forth[w.warp][w.lane] = as4(forth);
+    s_back[w.warp][w.lane] = e0;
     __syncthreads();
-    for (int w = 0; w < warp; ++w) h = apply(as_map(s_fwd[buf][w][lane]), h);
-    float2 e;   // behind this warp's steps
-    if (S > 1) {
-      if (warp == 0) {
-        Map2 all = as_map(s_bwd[buf][SCAN_WARPS - 1][lane]);
-        for (int w = SCAN_WARPS - 2; w >= 0; --w) all = then(all, as_map(s_bwd[buf][w][lane]));
-        exchange_send(s_exchange, i, S, rank, as4(all));
-      }
-      const bool came = exchange_wait(s_exchange, i);
-      e = carry;
-      for (int r = S - 1; r >= 0; --r) {
-        if (r == rank) e = carry;
-        carry = apply(as_map(s_exchange.slot[buf][r][lane]), carry);
-      }
-      if (!came) carry.x = carry.y = e.x = e.y = __uint_as_float(0x7fc00000u);
-      for (int w = SCAN_WARPS - 1; w > warp; --w) e = apply(as_map(s_bwd[buf][w][lane]), e);
-    } else {
+    if (PATH == TILES && loader) issue(turn - SCAN_DEPTH * w.per_turn, slot);
+    if (w.warp == 0) {
+      float2 h = alive ? start : nan2();
 #pragma unroll
-      for (int w = SCAN_WARPS - 1; w >= 0; --w) {
-        if (w == warp) e = carry;
-        carry = apply(as_map(s_bwd[buf][w][lane]), carry);
+      for (int v = 0; v < SCAN_WARPS; ++v) {
+        s_h[v][w.lane] = h;
+        h = apply(as_map(s_forth[v][w.lane]), h);
       }
+    } else if (w.warp == 1) {
+      auto back = [&](int v) { return Map2{as_map(s_forth[v][w.lane]).a, s_back[v][w.lane]}; };
+      float2 e = carry;
+      if (w.S > 1) {
+        Map2 all = back(SCAN_WARPS - 1);
+#pragma unroll
+        for (int v = SCAN_WARPS - 2; v >= 0; --v) all = then(all, back(v));
+        exchange_send(s.exchange, i, w.S, w.rank, as4(all));
+        const bool came = exchange_wait(s.exchange, i);
+        for (int r = w.S - 1; r >= 0; --r) {
+          if (r == w.rank) e = carry;
+          carry = apply(as_map(s.exchange.slot[i & 1][r][w.lane]), carry);
+        }
+        if (!came) e = carry = nan2();
+      }
+      if (!alive) e = carry = nan2();
+#pragma unroll
+      for (int v = SCAN_WARPS - 1; v >= 0; --v) {
+        s_e[v][w.lane] = e;
+        e = apply(back(v), e);
+      }
+      if (w.S == 1) carry = e;
     }
+    __syncthreads();
+    float2 h = s_h[w.warp][w.lane], e = s_e[w.warp][w.lane];
 #pragma unroll
     for (int k = SCAN_K - 1; k >= 0; --k) {   // d becomes D
-      d[k] = make_float2(d[k].x + e.x, d[k].y + e.y);
-      e = make_float2(a[k].x * d[k].x, a[k].y * d[k].y);
+      d[k] = add2(d[k], e);
+      e = mul2(a[k], d[k]);
     }
-    IO *dx_at = dx + t0 * p.dxs[0], *dg_at = dgate + t0 * p.dgs[0];
     const bool direct = p.mode == SNN_SCAN_DIRECT;
-#pragma unroll
-    for (int k = 0; k < SCAN_K; ++k, dx_at += p.dxs[0], dg_at += p.dgs[0]) {
-      // DIRECT: dx = D, dgate = D h; SIGMOID: dx = D i, dgate = D i a (h - x)
-      const float2 gx = make_float2(d[k].x * in[k].x, d[k].y * in[k].y);
-      const float2 gg = direct ? make_float2(d[k].x * h.x, d[k].y * h.y)
-                               : make_float2(gx.x * a[k].x * (h.x - xv[k].x), gx.y * a[k].y * (h.y - xv[k].y));
-      if (full || t0 + k < len) {
-        store_pair<FAST>(dx_at, 0, n_ok, gx);
-        store_pair<FAST>(dg_at, 0, n_ok, gg);
-      }
-      h = make_float2(fmaf(a[k].x, h.x, in[k].x * xv[k].x), fmaf(a[k].y, h.y, in[k].y * xv[k].y));
+    IO *dx_to, *dg_to;
+    int64_t dx_step, dg_step;
+    if (PATH == TILES) {
+      dx_to = reinterpret_cast<IO*>(out) + 2 * w.lane;
+      dg_to = dx_to + WARP_PIECE;
+      dx_step = dg_step = SCAN_COLS;
+    } else {
+      dx_to = (IO*)p.dx + w.b * p.dxs[1] + t0 * p.dxs[0];
+      dg_to = (IO*)p.dgate + w.b * p.dgs[1] + t0 * p.dgs[0];
+      dx_step = p.dxs[0];
+      dg_step = p.dgs[0];
     }
-  }
-  if (rank == 0 && warp == 0) store_state(p.dstate, b, p.N, c, n_ok, carry);
-  zero_steps<FAST>(p, (IO*)p.dx, p.dxs, b, c, n_ok, len, rank * SCAN_WARPS + warp, S * SCAN_WARPS);
-  zero_steps<FAST>(p, (IO*)p.dgate, p.dgs, b, c, n_ok, len, rank * SCAN_WARPS + warp, S * SCAN_WARPS);
-  if (S > 1) cluster.sync();
-}
-
-// ---- 8-bit activations on their own --------------------------------------------------------------------------
-// Bound by HBM (bytes of a value + 1 each way).  FAST: eight lanes share a group, eight neighbouring values each, so that
-// loads and stores are 8 to 32 bytes per lane, and a warp has PACK_UNROLL x 4 groups in flight; it needs rows that are
-// multiples of 8 values and aligned to them.  Otherwise a warp takes one group at a time, two values per lane.
-constexpr int PACK_WARPS = 8, PACK_UNROLL = 4;
-template <typename IO> struct Eight;   // eight neighbouring values, in 16-byte accesses
-template <> struct Eight<float> {
-  float4 a, b;
-  __device__ float2 pair(int j) const { return j == 0 ? make_float2(a.x, a.y) : j == 1 ? make_float2(a.z, a.w) : j == 2 ? make_float2(b.x, b.y) : make_float2(b.z, b.w); }
-  __device__ void set(int j, float2 v) { if (j == 0) a.x = v.x, a.y = v.y; else if (j == 1) a.z = v.x, a.w = v.y; else if (j == 2) b.x = v.x, b.y = v.y; else b.z = v.x, b.w = v.y; }
-};
-template <typename IO> struct alignas(16) EightHalves {
-  typename Pair<IO>::raw v[4];
-  __device__ float2 pair(int j) const { return to_f32(v[j]); }
-  __device__ void set(int j, float2 x) { set_raw(v[j], x); }
-};
-template <> struct Eight<__nv_bfloat16> : EightHalves<__nv_bfloat16> {};
-template <> struct Eight<__half> : EightHalves<__half> {};
-
-template <typename IO, int FORMAT, bool FAST>
-__global__ void __launch_bounds__(32 * PACK_WARPS) activation_pack_kernel(const IO* values, int64_t n_rows, int n_cols, int64_t stride,
-                                                                          uint8_t* codes, uint8_t* scales) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int groups = (n_cols + KEEP_GROUP - 1) / KEEP_GROUP;
-  const int64_t n = n_rows * groups;
-  if constexpr (FAST) {
-    const int64_t step = (int64_t)gridDim.x * PACK_WARPS * 4 * PACK_UNROLL;
-    for (int64_t g0 = ((int64_t)blockIdx.x * PACK_WARPS + warp) * 4 * PACK_UNROLL + (lane >> 3); g0 - (lane >> 3) < n; g0 += step) {
-      Eight<IO> v[PACK_UNROLL];
 #pragma unroll
-      for (int u = 0; u < PACK_UNROLL; ++u) {   // (groups that do not exist: another one, not stored)
-        const int64_t g = min(g0 + 4 * u, n - 1), row = g / groups;
-        const int c = (int)(g - row * groups) * KEEP_GROUP + (lane & 7) * 8;
-        v[u] = *reinterpret_cast<const Eight<IO>*>(values + row * stride + (c < n_cols ? c : 0));
-      }
-#pragma unroll
-      for (int u = 0; u < PACK_UNROLL; ++u) {
-        const int64_t g = min(g0 + 4 * u, n - 1), row = g / groups;
-        const int group = (int)(g - row * groups), c = group * KEEP_GROUP + (lane & 7) * 8;
-        const bool on = c < n_cols;
-        float m = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) m = larger_magnitude(m, larger_magnitude(v[u].pair(j).x, v[u].pair(j).y));
-        uint32_t top = on ? __float_as_uint(m) : 0u;
-#pragma unroll
-        for (int o = 1; o < 8; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const uint32_t byte = keep_scale_byte<FORMAT>(top);
-        const float inverse = keep_scale_inverse(byte);
-        uint2 q = make_uint2(0u, 0u);
-        if (byte != 255u) {
-          q.x = keep_encode2<FORMAT>(v[u].pair(0), inverse, top) | keep_encode2<FORMAT>(v[u].pair(1), inverse, top) << 16;
-          q.y = keep_encode2<FORMAT>(v[u].pair(2), inverse, top) | keep_encode2<FORMAT>(v[u].pair(3), inverse, top) << 16;
+    for (int k = 0; k < SCAN_K; ++k) {
+      // DIRECT: dx = D, dgate = D h; SIGMOID: dx = D i, dgate = D i a (h - x).  Behind the end i is 0, and so are both but
+      // for the direct mode's dgate and dx, whose D is not: they are cleared below.
+      float2 gx = mul2(d[k], in[k]);
+      float2 gg = direct ? mul2(d[k], h) : mul2(mul2(gx, a[k]), fma2(xv[k], both(-1.f), h));
+      h = fma2(a[k], h, mul2(in[k], xv[k]));
+      if (PATH == TILES) {
+        if (!full && t0 + k >= w.len) gx = gg = both(0.f);
+        store_pair<true>(dx_to + k * SCAN_COLS, 0, 2, gx);
+        store_pair<true>(dg_to + k * SCAN_COLS, 0, 2, gg);
+      } else {
+        if (full || t0 + k < w.len) {
+          store_pair<PATH == PAIRS>(dx_to, w.c, w.n_ok, gx);
+          store_pair<PATH == PAIRS>(dg_to, w.c, w.n_ok, gg);
         }
-        if (g0 + 4 * u < n) {
-          if (on) *reinterpret_cast<uint2*>(codes + row * n_cols + c) = q;
-          if ((lane & 7) == 0) scales[g] = (uint8_t)byte;
+        dx_to += dx_step;
+        dg_to += dg_step;
+      }
+    }
+    if (PATH == TILES) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (w.lane == 0) {
+        if (t0 < p.T) {
+          tma_store_3d(&p.out[0], w.col0, w.b, t0, out);
+          tma_store_3d(&p.out[1], w.col0, w.b, t0, out + OUT / 2);
         }
+        bulk_commit();
       }
     }
-  } else for (int64_t i = (int64_t)blockIdx.x * PACK_WARPS + warp; i < n; i += (int64_t)gridDim.x * PACK_WARPS) {
-    const int64_t row = i / groups;
-    const int c = (int)(i % groups) * KEEP_GROUP + 2 * lane, n_ok = min(max(n_cols - c, 0), 2);
-    uint32_t byte;
-    const uint32_t pair = encode_row<FORMAT>(load_pair<false>(values + row * stride, c, n_ok), n_ok, byte);
-    if (n_ok > 0) codes[row * n_cols + c] = (uint8_t)(pair & 255u);
-    if (n_ok > 1) codes[row * n_cols + c + 1] = (uint8_t)(pair >> 8);
-    if (lane == 0) scales[i] = (uint8_t)byte;
   }
-}
-template <typename IO, int FORMAT, bool FAST>
-__global__ void __launch_bounds__(32 * PACK_WARPS) activation_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int64_t n_rows,
-                                                                            int n_cols, IO* values, int64_t stride) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int groups = (n_cols + KEEP_GROUP - 1) / KEEP_GROUP;
-  const int64_t n = n_rows * groups;
-  if constexpr (FAST) {
-    const int64_t step = (int64_t)gridDim.x * PACK_WARPS * 4 * PACK_UNROLL;
-    for (int64_t g0 = ((int64_t)blockIdx.x * PACK_WARPS + warp) * 4 * PACK_UNROLL + (lane >> 3); g0 - (lane >> 3) < n; g0 += step) {
-      uint2 q[PACK_UNROLL];
-      uint32_t byte[PACK_UNROLL];
-#pragma unroll
-      for (int u = 0; u < PACK_UNROLL; ++u) {
-        const int64_t g = min(g0 + 4 * u, n - 1), row = g / groups;
-        const int c = (int)(g - row * groups) * KEEP_GROUP + (lane & 7) * 8;
-        q[u] = *reinterpret_cast<const uint2*>(codes + row * n_cols + (c < n_cols ? c : 0));
-        byte[u] = scales[g];
-      }
-#pragma unroll
-      for (int u = 0; u < PACK_UNROLL; ++u) {
-        const int64_t g = min(g0 + 4 * u, n - 1), row = g / groups;
-        const int c = (int)(g - row * groups) * KEEP_GROUP + (lane & 7) * 8;
-        const float scale = keep_scale_value(byte[u]);
-        Eight<IO> v;
-        v.set(0, keep_decode2<IO, FORMAT>(q[u].x & 0xffffu, scale));
-        v.set(1, keep_decode2<IO, FORMAT>(q[u].x >> 16, scale));
-        v.set(2, keep_decode2<IO, FORMAT>(q[u].y & 0xffffu, scale));
-        v.set(3, keep_decode2<IO, FORMAT>(q[u].y >> 16, scale));
-        if (g0 + 4 * u < n && c < n_cols) *reinterpret_cast<Eight<IO>*>(values + row * stride + c) = v;
-      }
-    }
-  } else for (int64_t i = (int64_t)blockIdx.x * PACK_WARPS + warp; i < n; i += (int64_t)gridDim.x * PACK_WARPS) {
-    const int64_t row = i / groups;
-    const int c = (int)(i % groups) * KEEP_GROUP + 2 * lane, n_ok = min(max(n_cols - c, 0), 2);
-    store_pair<false>(values + row * stride, c, n_ok, decode_pair<IO>(codes + row * n_cols, scales[i], c, n_ok, FORMAT));
-  }
+  if (w.rank == 0 && w.warp == 1) store_state(p.dstate, w.b, p.N, w.c, w.n_ok, carry);
+  const int from = PATH == TILES ? turns * w.per_turn : w.len;
+  zero_steps<PATH != SCALAR>(p, w, (IO*)p.dx, p.dxs, from);
+  zero_steps<PATH != SCALAR>(p, w, (IO*)p.dgate, p.dgs, from);
+  if (PATH == TILES && w.lane == 0) bulk_read_done<0>();
+  if (!alive)
+    for (int i = 0; i < 100; ++i) __nanosleep(20000);
+  if (w.S > 1) cluster.sync();
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------
-size_t dtype_size(int dtype) { return dtype == SNN_DTYPE_FP32 ? 4 : 2; }
-bool dtype_known(int dtype) { return dtype >= SNN_DTYPE_FP32 && dtype <= SNN_DTYPE_FP16; }
 // whether pairs of values can be accessed at once: even offsets everywhere
-bool pairs_aligned(const void* p, size_t size, int64_t s0, int64_t s1 = 0) {
-  return (uintptr_t)p % (2 * size) == 0 && s0 % 2 == 0 && s1 % 2 == 0;
+bool pairs_aligned(const void* p, size_t size, const int64_t* s) {
+  return (uintptr_t)p % (2 * size) == 0 && s[0] % 2 == 0 && s[1] % 2 == 0;
 }
-// the kernels' template arguments: the value type, and whether the fast path's alignment holds
-template <typename F> snn_status by_dtype(int dtype, bool pairs, F&& f) {
-  if (dtype == SNN_DTYPE_FP32) return pairs ? f(float(), std::true_type()) : f(float(), std::false_type());
-  if (dtype == SNN_DTYPE_BF16) return pairs ? f(__nv_bfloat16(), std::true_type()) : f(__nv_bfloat16(), std::false_type());
-  return pairs ? f(__half(), std::true_type()) : f(__half(), std::false_type());
+// A tensor map over [T][B][N] with boxes of `steps` x 64 channels of one sample; false if TMA cannot describe it.
+bool tile_map(CUtensorMap* out, const void* base, int dtype_bytes, int dtype, int T, int B, int N, int64_t st, int64_t sb, int steps) {
+  tensor_map_encode_fn encode = tensor_map_encoder();
+  if (!encode || (uintptr_t)base % 16 != 0) return false;
+  // (a stride that is never used may be anything: take one that fits)
+  const int64_t row = ((int64_t)N * dtype_bytes + 15) / 16 * 16;
+  const int64_t b_bytes = B > 1 ? sb * dtype_bytes : row, t_bytes = T > 1 ? st * dtype_bytes : row * B;
+  if (b_bytes % 16 != 0 || t_bytes % 16 != 0 || b_bytes <= 0 || t_bytes <= 0 || b_bytes >= ((int64_t)1 << 40) || t_bytes >= ((int64_t)1 << 40))
+    return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)N, (cuuint64_t)B, (cuuint64_t)T}, strides[2] = {(cuuint64_t)b_bytes, (cuuint64_t)t_bytes};
+  const cuuint32_t box[3] = {SCAN_COLS, 1, (cuuint32_t)steps}, elem[3] = {1, 1, 1};
+  const CUtensorMapDataType type = dtype < 0                     ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                   : dtype == SNN_DTYPE_FP32     ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == SNN_DTYPE_BF16     ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                                 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return encode(out, type, 3, const_cast<void*>(base), dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool value_map(CUtensorMap* out, const void* base, const snn_scan_args* a, const int64_t* s, int steps) {
+  return tile_map(out, base, (int)dtype_size(a->dtype), a->dtype, a->T, a->B, a->N, s[0], s[1], steps);
+}
+bool code_map(CUtensorMap* out, const uint8_t* base, const snn_scan_args* a, int steps) {
+  return tile_map(out, base, 1, -1, a->T, a->B, a->N, (int64_t)a->B * a->N, a->N, steps);
+}
+// the kernels' template arguments: the value type and the path
+template <typename F> snn_status by_path(int path, F&& f) {
+  if (path == TILES) return f(std::integral_constant<int, TILES>());
+  return path == PAIRS ? f(std::integral_constant<int, PAIRS>()) : f(std::integral_constant<int, SCALAR>());
+}
+template <typename F> snn_status by_type(int dtype, int path, F&& f) {
+  return by_path(path, [&](auto is_path) {
+    if (dtype == SNN_DTYPE_FP32) return f(float(), is_path);
+    return dtype == SNN_DTYPE_BF16 ? f(__nv_bfloat16(), is_path) : f(__half(), is_path);
+  });
 }
 
 snn_status check_common(const snn_scan_args* a) {
@@ -678,20 +708,13 @@ ScanParams params_of(const snn_scan_args* a) {
   p.x_codes = a->x_codes; p.x_scales = a->x_scales; p.gate_codes = a->gate_codes; p.gate_scales = a->gate_scales;
   return p;
 }
-// rows of 8-bit codes that can be accessed 16 bytes at a time
-bool codes_aligned(const ScanParams& p) {
-  bool ok = true;
-  if (p.x_format != SNN_KEEP_RAW) ok = ok && p.N % 16 == 0 && (uintptr_t)p.x_codes % 16 == 0;
-  if (p.gate_format != SNN_KEEP_RAW) ok = ok && p.N % 16 == 0 && (uintptr_t)p.gate_codes % 16 == 0;
-  return ok;
-}
 // Blocks per column tile: enough for four blocks on each of 148 SMs, no more than there are chunks.
 int cluster_of(int64_t tiles, int T) {
   int S = 1;
   while (S < SCAN_MAX_CLUSTER && tiles * S < 4 * 148 && (int64_t)S * SNN_SCAN_CHUNK < T) S *= 2;
   return S;
 }
-template <typename K> snn_status launch_clusters(K kernel, size_t ring_bytes, const ScanParams& p, cudaStream_t stream) {
+template <typename K> snn_status launch_clusters(K kernel, size_t smem, const ScanParams& p, cudaStream_t stream) {
   const int64_t tiles = (int64_t)p.B * p.n_tiles;
   const int S = cluster_of(tiles, p.T);
   if (tiles * S > INT32_MAX) return SNN_ERR_UNSUPPORTED;
@@ -699,8 +722,8 @@ template <typename K> snn_status launch_clusters(K kernel, size_t ring_bytes, co
   cfg.gridDim = dim3((unsigned)(tiles * S));
   cfg.blockDim = dim3(SCAN_THREADS);
   cfg.stream = stream;
-  cfg.dynamicSmemBytes = ring_bytes;
-  if (ring_bytes && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring_bytes) != cudaSuccess)
+  cfg.dynamicSmemBytes = smem;
+  if (smem && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return cudaGetLastError(), SNN_ERR_CUDA;
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeClusterDimension;
@@ -710,15 +733,6 @@ template <typename K> snn_status launch_clusters(K kernel, size_t ring_bytes, co
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
 }
-// whether rows can be accessed eight values at a time
-bool rows_of_eight(const void* values, int n_cols, int64_t row_stride, const uint8_t* codes) {
-  return n_cols % 8 == 0 && row_stride % 8 == 0 && (uintptr_t)values % 16 == 0 && (uintptr_t)codes % 8 == 0;
-}
-unsigned pack_blocks(int64_t n_rows, int n_cols, bool fast) {
-  const int64_t groups = n_rows * ((n_cols + KEEP_GROUP - 1) / KEEP_GROUP), per_block = PACK_WARPS * (fast ? 4 * PACK_UNROLL : 1);
-  return (unsigned)std::min<int64_t>((groups + per_block - 1) / per_block, 148 * 8);
-}
-snn_status launched() { return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA; }
 
 }  // namespace
 
@@ -735,21 +749,28 @@ extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
   }
   ScanParams p = params_of(a);
   const size_t size = dtype_size(a->dtype);
-  const bool fast = p.N % 2 == 0 && pairs_aligned(p.x, size, p.xs[0], p.xs[1]) && pairs_aligned(p.gate, size, p.gs[0], p.gs[1]) &&
-                    pairs_aligned(p.h, size, p.hs[0], p.hs[1]) && codes_aligned(p);
+  const bool pairs = a->N % 2 == 0 && pairs_aligned(p.x, size, p.xs) && pairs_aligned(p.gate, size, p.gs) && pairs_aligned(p.h, size, p.hs);
   const cudaStream_t s = (cudaStream_t)stream;
-  return by_dtype(a->dtype, fast, [&](auto io, auto is_fast) {
-    using IO = decltype(io);
-    constexpr bool FAST = decltype(is_fast)::value;
-    if (!keep && p.T <= SCAN_SHORT) {
-      const int64_t blocks = ((int64_t)p.B * ((p.N + 1) / 2) + 127) / 128;
-      if (blocks > INT32_MAX) return SNN_ERR_UNSUPPORTED;
-      scan_short_kernel<IO, FAST><<<(unsigned)blocks, 128, 0, s>>>(p);
+  if (!keep && a->T <= SCAN_SHORT) {
+    const int64_t blocks = ((int64_t)p.B * ((p.N + 1) / 2) + 127) / 128;
+    if (blocks > INT32_MAX) return SNN_ERR_UNSUPPORTED;
+    return by_type(a->dtype, pairs ? PAIRS : SCALAR, [&](auto io, auto path) {
+      scan_short_kernel<decltype(io), decltype(path)::value == PAIRS><<<(unsigned)blocks, 128, 0, s>>>(p);
       return launched();
-    }
-    const size_t ring = FAST ? Ring<IO>::DEPTH * 2 * PIECE * 2 * sizeof(IO) : 0;
-    return keep ? launch_clusters(scan_forward_kernel<IO, true, FAST>, ring, p, s)
-                : launch_clusters(scan_forward_kernel<IO, false, FAST>, ring, p, s);
+    });
+  }
+  const bool tiles = pairs && value_map(&p.in[0], p.x, a, p.xs, SNN_SCAN_CHUNK) && value_map(&p.in[1], p.gate, a, p.gs, SNN_SCAN_CHUNK) &&
+                     value_map(&p.out[0], p.h, a, p.hs, SCAN_K) && (p.x_format == SNN_KEEP_RAW || code_map(&p.out[2], p.x_codes, a, SCAN_K)) &&
+                     (p.gate_format == SNN_KEEP_RAW || code_map(&p.out[3], p.gate_codes, a, SCAN_K));
+  return by_type(a->dtype, tiles ? TILES : pairs ? PAIRS : SCALAR, [&](auto io, auto path) {
+    using IO = decltype(io);
+    constexpr int PATH = decltype(path)::value;
+    auto go = [&](auto is_keep) {
+      constexpr bool KEEP = decltype(is_keep)::value;
+      const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * forward_slot<IO>(), out = PATH == TILES ? 2 * SCAN_WARPS * forward_out<IO, KEEP>() : 0;
+      return launch_clusters(scan_forward_kernel<IO, KEEP, PATH>, ring + out, p, s);
+    };
+    return keep ? go(std::true_type()) : go(std::false_type());
   });
 }
 
@@ -757,50 +778,25 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
   const snn_status st = check_common(a);
   if (st != SNN_OK) return st;
   if (a->B == 0 || a->N == 0) return SNN_OK;
+  const bool raw_x = a->x_format == SNN_KEEP_RAW, raw_gate = a->gate_format == SNN_KEEP_RAW;
   if (a->T > 0) {
     if (!a->dh || !a->dx || !a->dgate || !a->states) return SNN_ERR_INVALID_ARG;
-    if (a->x_format == SNN_KEEP_RAW ? !a->x : !a->x_codes || !a->x_scales) return SNN_ERR_INVALID_ARG;
-    if (a->gate_format == SNN_KEEP_RAW ? !a->gate : !a->gate_codes || !a->gate_scales) return SNN_ERR_INVALID_ARG;
+    if (raw_x ? !a->x : !a->x_codes || !a->x_scales) return SNN_ERR_INVALID_ARG;
+    if (raw_gate ? !a->gate : !a->gate_codes || !a->gate_scales) return SNN_ERR_INVALID_ARG;
   }
   ScanParams p = params_of(a);
   const size_t size = dtype_size(a->dtype);
-  const bool fast = p.N % 2 == 0 && pairs_aligned(p.dh, size, p.dhs[0], p.dhs[1]) && pairs_aligned(p.dx, size, p.dxs[0], p.dxs[1]) &&
-                    pairs_aligned(p.dgate, size, p.dgs[0], p.dgs[1]) && codes_aligned(p) &&
-                    (p.x_format != SNN_KEEP_RAW || pairs_aligned(p.x, size, p.xs[0], p.xs[1])) &&
-                    (p.gate_format != SNN_KEEP_RAW || pairs_aligned(p.gate, size, p.gs[0], p.gs[1]));
-  return by_dtype(a->dtype, fast, [&](auto io, auto is_fast) {
+  const bool pairs = a->N % 2 == 0 && pairs_aligned(p.dh, size, p.dhs) && pairs_aligned(p.dx, size, p.dxs) && pairs_aligned(p.dgate, size, p.dgs) &&
+                     (!raw_x || pairs_aligned(p.x, size, p.xs)) && (!raw_gate || pairs_aligned(p.gate, size, p.gs));
+  const bool tiles = pairs && a->T > 0 && value_map(&p.in[0], p.dh, a, p.dhs, SNN_SCAN_CHUNK) &&
+                     (raw_x ? value_map(&p.in[1], p.x, a, p.xs, SNN_SCAN_CHUNK) : code_map(&p.in[1], p.x_codes, a, SNN_SCAN_CHUNK)) &&
+                     (raw_gate ? value_map(&p.in[2], p.gate, a, p.gs, SNN_SCAN_CHUNK) : code_map(&p.in[2], p.gate_codes, a, SNN_SCAN_CHUNK)) &&
+                     value_map(&p.out[0], p.dx, a, p.dxs, SCAN_K) && value_map(&p.out[1], p.dgate, a, p.dgs, SCAN_K);
+  return by_type(a->dtype, tiles ? TILES : pairs ? PAIRS : SCALAR, [&](auto io, auto path) {
     using IO = decltype(io);
-    constexpr bool FAST = decltype(is_fast)::value;
-    const size_t piece = PIECE * 2 * sizeof(IO);
-    const size_t slot = piece + (p.x_format == SNN_KEEP_RAW ? piece : CODE_PIECE) + (p.gate_format == SNN_KEEP_RAW ? piece : CODE_PIECE);
-    return launch_clusters(scan_backward_kernel<IO, FAST>, FAST ? Ring<IO>::DEPTH * slot : 0, p, (cudaStream_t)stream);
-  });
-}
-
-extern "C" snn_status snn_activation_pack(const void* values, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t row_stride,
-                                          int32_t format, uint8_t* codes, uint8_t* scales, void* stream) {
-  if (n_rows < 0 || n_cols < 0 || !dtype_known(dtype) || (format != SNN_KEEP_INT8 && format != SNN_KEEP_E4M3)) return SNN_ERR_INVALID_ARG;
-  if (n_rows == 0 || n_cols == 0) return SNN_OK;
-  if (!values || !codes || !scales) return SNN_ERR_INVALID_ARG;
-  return by_dtype(dtype, rows_of_eight(values, n_cols, row_stride, codes), [&](auto io, auto is_fast) {
-    using IO = decltype(io);
-    constexpr bool FAST = decltype(is_fast)::value;
-    const auto kernel = format == SNN_KEEP_INT8 ? activation_pack_kernel<IO, SNN_KEEP_INT8, FAST> : activation_pack_kernel<IO, SNN_KEEP_E4M3, FAST>;
-    kernel<<<pack_blocks(n_rows, n_cols, FAST), 32 * PACK_WARPS, 0, (cudaStream_t)stream>>>((const IO*)values, n_rows, n_cols, row_stride, codes, scales);
-    return launched();
-  });
-}
-
-extern "C" snn_status snn_activation_unpack(const uint8_t* codes, const uint8_t* scales, int32_t format, int64_t n_rows, int32_t n_cols,
-                                            void* values, int32_t dtype, int64_t row_stride, void* stream) {
-  if (n_rows < 0 || n_cols < 0 || !dtype_known(dtype) || (format != SNN_KEEP_INT8 && format != SNN_KEEP_E4M3)) return SNN_ERR_INVALID_ARG;
-  if (n_rows == 0 || n_cols == 0) return SNN_OK;
-  if (!values || !codes || !scales) return SNN_ERR_INVALID_ARG;
-  return by_dtype(dtype, rows_of_eight(values, n_cols, row_stride, codes), [&](auto io, auto is_fast) {
-    using IO = decltype(io);
-    constexpr bool FAST = decltype(is_fast)::value;
-    const auto kernel = format == SNN_KEEP_INT8 ? activation_unpack_kernel<IO, SNN_KEEP_INT8, FAST> : activation_unpack_kernel<IO, SNN_KEEP_E4M3, FAST>;
-    kernel<<<pack_blocks(n_rows, n_cols, FAST), 32 * PACK_WARPS, 0, (cudaStream_t)stream>>>(codes, scales, n_rows, n_cols, (IO*)values, row_stride);
-    return launched();
+    constexpr int PATH = decltype(path)::value;
+    const size_t values = PIECE * sizeof(IO), slot = values + (raw_x ? values : PIECE) + (raw_gate ? values : PIECE);
+    const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * slot, out = PATH == TILES ? 2 * SCAN_WARPS * 2 * WARP_PIECE * sizeof(IO) : 0;
+    return launch_clusters(scan_backward_kernel<IO, PATH>, ring + out, p, (cudaStream_t)stream);
   });
 }

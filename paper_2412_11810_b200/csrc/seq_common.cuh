@@ -113,4 +113,23 @@ __device__ __forceinline__ float larger_magnitude(float a, float b) {
   return m;
 }
 
+// The scale and this lane's two codes of a row of 64 values, two per lane.  Called by whole warps.
+template <int FORMAT> __device__ __forceinline__ uint32_t encode_row(float2 v, int n_ok, uint32_t& byte) {
+  const float m = larger_magnitude(n_ok > 0 ? v.x : 0.f, n_ok > 1 ? v.y : 0.f);
+  const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(m));   // bit patterns of magnitudes sort as they do
+  byte = keep_scale_byte<FORMAT>(top);
+  return byte == 255u ? 0u : keep_encode2<FORMAT>(v, keep_scale_inverse(byte), top);
+}
+template <typename IO>
+__device__ __forceinline__ float2 decode_pair(const uint8_t* row, uint32_t scale, int c, int n_ok, int format) {
+  const uint32_t pair = (uint32_t)row[n_ok ? c : 0] | (uint32_t)row[n_ok == 2 ? c + 1 : 0] << 8;
+  return format == SNN_KEEP_INT8 ? keep_decode2<IO, SNN_KEEP_INT8>(pair, keep_scale_value(scale))
+                                 : keep_decode2<IO, SNN_KEEP_E4M3>(pair, keep_scale_value(scale));
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------
+inline size_t dtype_size(int dtype) { return dtype == SNN_DTYPE_FP32 ? 4 : 2; }
+inline bool dtype_known(int dtype) { return dtype >= SNN_DTYPE_FP32 && dtype <= SNN_DTYPE_FP16; }
+inline snn_status launched() { return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA; }
+
 }  // namespace snnk

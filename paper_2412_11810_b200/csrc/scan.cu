@@ -14,6 +14,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "seq_common.cuh"
@@ -81,25 +82,45 @@ __device__ __forceinline__ float4 as4(const Map2& m) { return make_float4(m.a.x,
 __device__ __forceinline__ Map2 as_map(float4 v) { return {make_float2(v.x, v.y), make_float2(v.z, v.w)}; }
 __device__ __forceinline__ Map2 then(const Map2& first, const Map2& second) { return {mul2(first.a, second.a), fma2(second.a, first.b, second.b)}; }
 
-// a and the factor i of x.  sigmoid(g) and 1 - sigmoid(g) both without cancellation: with e = exp(-|g|), the larger of
-// the two is 1 / (1 + e) and the smaller e / (1 + e).  (1 + e lies in [1, 2]: the hardware's reciprocal needs no care for
-// the ends of the range; an e below 2^-126 counts as zero.)
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float reciprocal(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// a and the factor i of x: sigmoid(g) and 1 - sigmoid(g), both without cancellation.
+// For any g: with e = exp(-|g|), the larger of the two is 1 / (1 + e) and the smaller e / (1 + e).  (1 + e lies in [1, 2]; an
+// e below 2^-126 counts as zero.)
 __device__ __forceinline__ void sigmoids(float2 g, float2& a, float2& i) {
-  float2 e, large;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(fabsf(g.x) * -1.44269504f));
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(fabsf(g.y) * -1.44269504f));
-  const float2 d = add2(e, both(1.f));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.x) : "f"(d.x));
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(large.y) : "f"(d.y));
-  const float2 small = mul2(e, large);
+  const float2 e = make_float2(exp2_fast(fabsf(g.x) * -1.44269504f), exp2_fast(fabsf(g.y) * -1.44269504f));
+  const float2 d = add2(e, both(1.f)), large = make_float2(reciprocal(d.x), reciprocal(d.y)), small = mul2(e, large);
   a = make_float2(g.x >= 0.f ? large.x : small.x, g.y >= 0.f ? large.y : small.y);
   i = make_float2(g.x >= 0.f ? small.x : large.x, g.y >= 0.f ? small.y : large.y);
+}
+// For g >= LOWEST_GATE: with e = exp(-g), a = 1 / (1 + e) and i = e a; nothing leaves the range of fp32.
+constexpr float LOWEST_GATE = -80.f;
+__device__ __forceinline__ void ordinary_sigmoids(float2 g, float2& a, float2& i) {
+  const float2 t = mul2(g, both(-1.44269504f)), e = make_float2(exp2_fast(t.x), exp2_fast(t.y)), d = add2(e, both(1.f));
+  a = make_float2(reciprocal(d.x), reciprocal(d.y));
+  i = mul2(e, a);
 }
 // gv becomes a, in becomes i, for all steps of a thread
 __device__ __forceinline__ void coefficients(float2 (&gv)[SCAN_K], float2 (&in)[SCAN_K], int mode) {
   if (mode == SNN_SCAN_DIRECT) {
 #pragma unroll
     for (int k = 0; k < SCAN_K; ++k) in[k] = both(1.f);
+    return;
+  }
+  float lowest = 0.f;
+#pragma unroll
+  for (int k = 0; k < SCAN_K; ++k) lowest = fminf(lowest, fminf(gv[k].x, gv[k].y));
+  if (lowest >= LOWEST_GATE) {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) ordinary_sigmoids(gv[k], gv[k], in[k]);
   } else {
 #pragma unroll
     for (int k = 0; k < SCAN_K; ++k) sigmoids(gv[k], gv[k], in[k]);
@@ -187,25 +208,56 @@ __device__ __forceinline__ void load_values(float2 (&v)[SCAN_K], const IO* sampl
 }
 
 // ---- kept rows in 8 bits ------------------------------------------------------------------------------------
-// Encodes the warp's steps t0.. (those before the sequence's end); codes to s_codes (TILES: they leave by TMA) or to memory.
+// Encodes the warp's steps t0.. (those before the sequence's end); codes to s_codes (TILES: they leave by TMA, and channels
+// that do not exist are zeros) or to memory.
 template <int FORMAT, bool TO_SMEM>
 __device__ __forceinline__ void keep_steps(const float2 (&v)[SCAN_K], const ScanParams& p, const Place& w, int t0, uint8_t* codes,
                                            uint8_t* scales, unsigned char* s_codes) {
-  uint32_t mine = 0;
+  uint32_t top[SCAN_K], worst = 0, fraction = 0;   // magnitudes' bit patterns sort as they do
 #pragma unroll
   for (int k = 0; k < SCAN_K; ++k) {
-    uint32_t byte;
-    const uint32_t pair = encode_row<FORMAT>(v[k], w.n_ok, byte);
-    if (w.lane == k) mine = byte;
-    if (TO_SMEM) {
-      *reinterpret_cast<uint16_t*>(s_codes + k * SCAN_COLS + 2 * w.lane) = (uint16_t)pair;
-    } else if (t0 + k < w.len) {
-      uint8_t* const at = codes + ((int64_t)(t0 + k) * p.B + w.b) * p.N + w.c;
-      if (w.n_ok > 0) at[0] = (uint8_t)(pair & 255u);
-      if (w.n_ok > 1) at[1] = (uint8_t)(pair >> 8);
+    const float m = TO_SMEM ? larger_magnitude(v[k].x, v[k].y) : larger_magnitude(w.n_ok > 0 ? v[k].x : 0.f, w.n_ok > 1 ? v[k].y : 0.f);
+    top[k] = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+    worst = max(worst, top[k]);
+    fraction = max(fraction, top[k] & 0x7fffffu);
+  }
+  uint32_t pair[SCAN_K];
+  if (worst < 0x7f800000u && (FORMAT == SNN_KEEP_E4M3 || fraction < 0x7f0000u)) {
+    // all finite, and no int8 code beyond 127: 1 / scale from the exponent alone (see keep_scale_byte)
+    constexpr uint32_t add = FORMAT == SNN_KEEP_INT8 ? 0u : 0x1fffffu, from = (FORMAT == SNN_KEEP_INT8 ? 260u : 262u) << 23;
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) {
+      const float2 u = mul2(v[k], both(__uint_as_float(min(from - ((top[k] + add) & 0x7f800000u), 254u << 23))));
+      if (FORMAT == SNN_KEEP_INT8) {
+        const float2 r = add2(u, both(12582912.f));
+        pair[k] = __byte_perm(__float_as_uint(r.x), __float_as_uint(r.y), 0x0040);
+      } else {
+        pair[k] = (uint32_t)__nv_cvt_float2_to_fp8x2(u, __NV_SATFINITE, __NV_E4M3);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) {
+      const uint32_t byte = keep_scale_byte<FORMAT>(top[k]);
+      pair[k] = byte == 255u ? 0u : keep_encode2<FORMAT>(v[k], keep_scale_inverse(byte), top[k]);
     }
   }
-  if (w.lane < SCAN_K && t0 + w.lane < w.len) scales[((int64_t)(t0 + w.lane) * p.B + w.b) * p.n_tiles + w.col0 / KEEP_GROUP] = (uint8_t)mine;
+#pragma unroll
+  for (int k = 0; k < SCAN_K; ++k) {
+    if (TO_SMEM) {
+      *reinterpret_cast<uint16_t*>(s_codes + k * SCAN_COLS + 2 * w.lane) = (uint16_t)pair[k];
+    } else if (t0 + k < w.len) {
+      uint8_t* const at = codes + ((int64_t)(t0 + k) * p.B + w.b) * p.N + w.c;
+      if (w.n_ok > 0) at[0] = (uint8_t)(pair[k] & 255u);
+      if (w.n_ok > 1) at[1] = (uint8_t)(pair[k] >> 8);
+    }
+  }
+  // lane k writes the scale of step k
+  static_assert(SCAN_K == 8, "three bits select a step");
+  const bool b0 = w.lane & 1, b1 = w.lane & 2, b2 = w.lane & 4;
+  const uint32_t lo = b1 ? (b0 ? top[3] : top[2]) : (b0 ? top[1] : top[0]), hi = b1 ? (b0 ? top[7] : top[6]) : (b0 ? top[5] : top[4]);
+  if (w.lane < SCAN_K && t0 + w.lane < w.len)
+    scales[((int64_t)(t0 + w.lane) * p.B + w.b) * p.n_tiles + w.col0 / KEEP_GROUP] = (uint8_t)keep_scale_byte<FORMAT>(b2 ? hi : lo);
 }
 template <bool TO_SMEM>
 __device__ __forceinline__ void keep_steps(int format, const float2 (&v)[SCAN_K], const ScanParams& p, const Place& w, int t0, uint8_t* codes,
@@ -218,8 +270,22 @@ template <int FORMAT, typename IO>
 __device__ __forceinline__ void decode_steps(float2 (&v)[SCAN_K], const void* tile, const Place& w, uint32_t bytes, int from) {
   const uint16_t* const at = reinterpret_cast<const uint16_t*>(reinterpret_cast<const unsigned char*>(tile) + w.warp * WARP_PIECE) + w.lane;
   const float scale = keep_scale_value(bytes);
+  if (FORMAT == SNN_KEEP_INT8) {
 #pragma unroll
-  for (int k = 0; k < SCAN_K; ++k) v[k] = keep_decode2<IO, FORMAT>(at[k * (SCAN_COLS / 2)], __shfl_sync(0xffffffffu, scale, from + k));
+    for (int k = 0; k < SCAN_K; ++k) v[k] = keep_decode2<IO, FORMAT>(at[k * (SCAN_COLS / 2)], __shfl_sync(0xffffffffu, scale, from + k));
+    return;
+  }
+  // no e4m3 value beyond the type's range at these scales: nothing to cut
+  const bool within = __all_sync(0xffffffffu, !(448.f * scale > largest_finite<IO>()));
+  if (within) {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k)
+      v[k] = mul2(__half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)at[k * (SCAN_COLS / 2)], __NV_E4M3))),
+                  both(__shfl_sync(0xffffffffu, scale, from + k)));
+  } else {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) v[k] = keep_decode2<IO, FORMAT>(at[k * (SCAN_COLS / 2)], __shfl_sync(0xffffffffu, scale, from + k));
+  }
 }
 template <typename IO>
 __device__ __forceinline__ void decode_from_memory(float2 (&v)[SCAN_K], const uint8_t* codes, const ScanParams& p, const Place& w, int t0,
@@ -378,11 +444,15 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) scan_forward_kernel(const __g
     float2 h = s_start[w.warp][w.lane];
     if constexpr (PATH == TILES) {
       IO* const to = reinterpret_cast<IO*>(out) + 2 * w.lane;
+      if (full) {
 #pragma unroll
-      for (int k = 0; k < SCAN_K; ++k) {
-        h = fma2(gv[k], h, xv[k]);
-        const float2 shown = full || t0 + k < w.len ? h : both(0.f);
-        store_pair<true>(to + k * SCAN_COLS, 0, 2, shown);
+        for (int k = 0; k < SCAN_K; ++k) store_pair<true>(to + k * SCAN_COLS, 0, 2, h = fma2(gv[k], h, xv[k]));
+      } else {
+#pragma unroll
+        for (int k = 0; k < SCAN_K; ++k) {
+          h = fma2(gv[k], h, xv[k]);
+          store_pair<true>(to + k * SCAN_COLS, 0, 2, t0 + k < w.len ? h : both(0.f));
+        }
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -590,39 +660,36 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const __
       d[k] = add2(d[k], e);
       e = mul2(a[k], d[k]);
     }
-    const bool direct = p.mode == SNN_SCAN_DIRECT;
-    IO *dx_to, *dg_to;
-    int64_t dx_step, dg_step;
-    if (PATH == TILES) {
-      dx_to = reinterpret_cast<IO*>(out) + 2 * w.lane;
-      dg_to = dx_to + WARP_PIECE;
-      dx_step = dg_step = SCAN_COLS;
-    } else {
-      dx_to = (IO*)p.dx + w.b * p.dxs[1] + t0 * p.dxs[0];
-      dg_to = (IO*)p.dgate + w.b * p.dgs[1] + t0 * p.dgs[0];
-      dx_step = p.dxs[0];
-      dg_step = p.dgs[0];
-    }
-#pragma unroll
-    for (int k = 0; k < SCAN_K; ++k) {
-      // DIRECT: dx = D, dgate = D h; SIGMOID: dx = D i, dgate = D i a (h - x).  Behind the end i is 0, and so are both but
-      // for the direct mode's dgate and dx, whose D is not: they are cleared below.
-      float2 gx = mul2(d[k], in[k]);
-      float2 gg = direct ? mul2(d[k], h) : mul2(mul2(gx, a[k]), fma2(xv[k], both(-1.f), h));
-      h = fma2(a[k], h, mul2(in[k], xv[k]));
+    // DIRECT: dx = D, dgate = D h; SIGMOID: dx = D i, dgate = D i a (h - x)
+    auto outputs = [&](auto is_direct, auto is_full) {
+      constexpr bool DIRECT = decltype(is_direct)::value, FULL = decltype(is_full)::value;
+      IO *dx_to, *dg_to;
       if (PATH == TILES) {
-        if (!full && t0 + k >= w.len) gx = gg = both(0.f);
-        store_pair<true>(dx_to + k * SCAN_COLS, 0, 2, gx);
-        store_pair<true>(dg_to + k * SCAN_COLS, 0, 2, gg);
+        dx_to = reinterpret_cast<IO*>(out) + 2 * w.lane;
+        dg_to = dx_to + WARP_PIECE;
       } else {
-        if (full || t0 + k < w.len) {
-          store_pair<PATH == PAIRS>(dx_to, w.c, w.n_ok, gx);
-          store_pair<PATH == PAIRS>(dg_to, w.c, w.n_ok, gg);
-        }
-        dx_to += dx_step;
-        dg_to += dg_step;
+        dx_to = (IO*)p.dx + w.b * p.dxs[1] + t0 * p.dxs[0];
+        dg_to = (IO*)p.dgate + w.b * p.dgs[1] + t0 * p.dgs[0];
       }
-    }
+#pragma unroll
+      for (int k = 0; k < SCAN_K; ++k) {
+        const float2 gx = DIRECT ? d[k] : mul2(d[k], in[k]);
+        const float2 gg = DIRECT ? mul2(d[k], h) : mul2(mul2(gx, a[k]), fma2(xv[k], both(-1.f), h));
+        h = fma2(a[k], h, DIRECT ? xv[k] : mul2(in[k], xv[k]));
+        const bool on = FULL || t0 + k < w.len;
+        if (PATH == TILES) {
+          store_pair<true>(dx_to + k * SCAN_COLS, 0, 2, on ? gx : both(0.f));
+          store_pair<true>(dg_to + k * SCAN_COLS, 0, 2, on ? gg : both(0.f));
+        } else {
+          if (on) store_pair<PATH == PAIRS>(dx_to, w.c, w.n_ok, gx);
+          if (on) store_pair<PATH == PAIRS>(dg_to, w.c, w.n_ok, gg);
+          dx_to += p.dxs[0];
+          dg_to += p.dgs[0];
+        }
+      }
+    };
+    if (p.mode == SNN_SCAN_DIRECT) full ? outputs(std::true_type(), std::true_type()) : outputs(std::true_type(), std::false_type());
+    else full ? outputs(std::false_type(), std::true_type()) : outputs(std::false_type(), std::false_type());
     if (PATH == TILES) {
       fence_proxy_async_smem();
       __syncwarp();
@@ -708,15 +775,22 @@ ScanParams params_of(const snn_scan_args* a) {
   p.x_codes = a->x_codes; p.x_scales = a->x_scales; p.gate_codes = a->gate_codes; p.gate_scales = a->gate_scales;
   return p;
 }
-// Blocks per column tile: enough for four blocks on each of 148 SMs, no more than there are chunks.
-int cluster_of(int64_t tiles, int T) {
-  int S = 1;
-  while (S < SCAN_MAX_CLUSTER && tiles * S < 4 * 148 && (int64_t)S * SNN_SCAN_CHUNK < T) S *= 2;
-  return S;
+// Blocks per column tile.  All blocks take equally long, so what counts is how full the device is over the waves that they
+// need, at `resident` blocks per SM; among clusters that fill it about as well the smallest (a larger one waits longer for
+// its summaries).  No more blocks than there are chunks.
+int cluster_of(int64_t tiles, int T, int resident) {
+  const double slots = 148.0 * resident;
+  int best = 1;
+  double best_fill = 0;
+  for (int S = 1; S <= SCAN_MAX_CLUSTER && (S == 1 || (int64_t)(S / 2) * SNN_SCAN_CHUNK < T); S *= 2) {
+    const double waves = (double)tiles * S / slots, fill = waves / std::ceil(waves);
+    if (fill > 1.08 * best_fill) best = S, best_fill = fill;
+  }
+  return best;
 }
-template <typename K> snn_status launch_clusters(K kernel, size_t smem, const ScanParams& p, cudaStream_t stream) {
+template <typename K> snn_status launch_clusters(K kernel, size_t smem, int resident, const ScanParams& p, cudaStream_t stream) {
   const int64_t tiles = (int64_t)p.B * p.n_tiles;
-  const int S = cluster_of(tiles, p.T);
+  const int S = cluster_of(tiles, p.T, resident);
   if (tiles * S > INT32_MAX) return SNN_ERR_UNSUPPORTED;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(tiles * S));
@@ -768,7 +842,7 @@ extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
     auto go = [&](auto is_keep) {
       constexpr bool KEEP = decltype(is_keep)::value;
       const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * forward_slot<IO>(), out = PATH == TILES ? 2 * SCAN_WARPS * forward_out<IO, KEEP>() : 0;
-      return launch_clusters(scan_forward_kernel<IO, KEEP, PATH>, ring + out, p, s);
+      return launch_clusters(scan_forward_kernel<IO, KEEP, PATH>, ring + out, ring + out > 90000 ? 2 : 3, p, s);
     };
     return keep ? go(std::true_type()) : go(std::false_type());
   });
@@ -797,6 +871,6 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
     constexpr int PATH = decltype(path)::value;
     const size_t values = PIECE * sizeof(IO), slot = values + (raw_x ? values : PIECE) + (raw_gate ? values : PIECE);
     const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * slot, out = PATH == TILES ? 2 * SCAN_WARPS * 2 * WARP_PIECE * sizeof(IO) : 0;
-    return launch_clusters(scan_backward_kernel<IO, PATH>, ring + out, p, (cudaStream_t)stream);
+    return launch_clusters(scan_backward_kernel<IO, PATH>, ring + out, ring + out > 90000 ? 1 : 2, p, (cudaStream_t)stream);
   });
 }

@@ -381,7 +381,7 @@ snn_status snn_activation_unpack(const uint8_t* codes, const uint8_t* scales, in
  * written) or in 8 bits, encoded by the forward pass while it reads them.  The backward pass recomputes the states of
  * a chunk from its checkpoint and the kept inputs.  The gate of SNN_SCAN_DIRECT is a decay close to one, which 8 bits
  * do not resolve: its gate_format must be SNN_KEEP_RAW (SNN_ERR_UNSUPPORTED otherwise).
- * Runs of steps are combined before the state they start from is known: the decays are meant to be at most one in
+ * Runs of steps are combined before the state that they start from is known: the decays are meant to be at most one in
  * magnitude, and where a product of consecutive decays leaves the range of fp32 the result may not be finite.
  * lengths (optional, device int32 [B], clamped to [0, T]): sample b ends after lengths[b] steps.  What x, gate and dh
  * hold behind that is not read; h, dx and dgate are set to zero there; `last` is the state at the end. */
@@ -407,7 +407,12 @@ typedef struct {
   void *dx, *dgate;              /* [T][B][N], backward                                                         */
   int64_t dx_stride[2], dgate_stride[2];
   float* dstate;                 /* [B][N] or NULL, backward                                                    */
+  void* workspace; size_t workspace_bytes;   /* device, 256-byte aligned, as snn_scan_workspace says (it may be
+                                    0 bytes); calls that may overlap in time need workspaces of their own       */
 } snn_scan_args;
+/* Bytes of workspace that the forward (backward = 0) or backward pass (1) needs; it depends on T, B, N and dtype alone
+ * and is a few per cent of the inputs at most: few channels and many steps need the summaries of parts of the time axis. */
+snn_status snn_scan_workspace(const snn_scan_args* args, int32_t backward, size_t* bytes);
 snn_status snn_scan_forward(const snn_scan_args* args, void* stream);
 snn_status snn_scan_backward(const snn_scan_args* args, void* stream);
 

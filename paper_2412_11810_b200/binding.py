@@ -45,7 +45,7 @@ EXPORTS = ["snn_create", "snn_destroy", "snn_alpha", "snn_workspace_query", "snn
            "snn_memory_stats_get", "snn_last_error", "snn_plan", "snn_compact_spikes", "snn_get_event_layout",
            "snn_phase_times_get", "snn_train_step_static", "snn_suggest_ckpt", "snn_selftest_wait_timeout",
            "snn_debug_checks_enabled", "snn_activation_pack", "snn_activation_unpack", "snn_scan_forward",
-           "snn_scan_backward", "snn_vocab_loss_workspace", "snn_vocab_loss_forward", "snn_vocab_loss_backward"]
+           "snn_scan_backward", "snn_scan_workspace", "snn_vocab_loss_workspace", "snn_vocab_loss_forward", "snn_vocab_loss_backward"]
 SNN_STATIC_WORKSPACE_BYTES = 32 << 20
 
 
@@ -98,7 +98,8 @@ class snn_scan_args(C.Structure):
                 ("x_codes", C.c_void_p), ("x_scales", C.c_void_p), ("gate_codes", C.c_void_p),
                 ("gate_scales", C.c_void_p), ("dh", C.c_void_p), ("dh_stride", C.c_int64 * 2), ("dlast", C.c_void_p),
                 ("dx", C.c_void_p), ("dgate", C.c_void_p), ("dx_stride", C.c_int64 * 2),
-                ("dgate_stride", C.c_int64 * 2), ("dstate", C.c_void_p)]
+                ("dgate_stride", C.c_int64 * 2), ("dstate", C.c_void_p), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
 
 
 class snn_vocab_loss_args(C.Structure):
@@ -145,6 +146,7 @@ def _load() -> C.CDLL:
                                         C.c_void_p, C.c_void_p]
     lib.snn_activation_unpack.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_void_p,
                                           C.c_int32, C.c_int64, C.c_void_p]
+    lib.snn_scan_workspace.argtypes = [C.POINTER(snn_scan_args), C.c_int32, C.POINTER(C.c_size_t)]
     lib.snn_scan_forward.argtypes = [C.POINTER(snn_scan_args), C.c_void_p]
     lib.snn_scan_backward.argtypes = [C.POINTER(snn_scan_args), C.c_void_p]
     lib.snn_vocab_loss_workspace.argtypes = [C.POINTER(snn_vocab_loss_args), C.c_int32, C.POINTER(C.c_size_t)]
@@ -270,6 +272,12 @@ def snn_activation_pack(values_ptr: int, dtype: int, n_rows: int, n_cols: int, r
 def snn_activation_unpack(codes_ptr: int, scales_ptr: int, fmt: int, n_rows: int, n_cols: int, values_ptr: int,
                           dtype: int, row_stride: int, stream: int = 0) -> None:
     _check(lib.snn_activation_unpack(codes_ptr, scales_ptr, fmt, n_rows, n_cols, values_ptr, dtype, row_stride, stream))
+
+
+def snn_scan_workspace(args: snn_scan_args, backward: bool) -> int:
+    n = C.c_size_t()
+    _check(lib.snn_scan_workspace(C.byref(args), int(backward), C.byref(n)))
+    return n.value
 
 
 def snn_scan_forward(args: snn_scan_args, stream: int = 0) -> None:

@@ -1,18 +1,19 @@
 // The gated linear recurrence with its backward pass (include/snn.h, "sequence-model operators").
 //
 // A step is an affine map of the state, h -> a h + b, and maps compose: (a2, b2) o (a1, b1) = (a2 a1, a2 b1 + b2).  So a
-// run of steps can be summarised before its start is known, and time is split three ways: a thread takes 8 steps of two
-// neighbouring channels in registers, the 8 warps of a thread block a chunk of 64 steps, the blocks of a cluster (1..8)
-// neighbouring chunks; together they take a turn, and the state at its end is carried to the next one.  One warp chains the
-// summaries of the block's warps, those of the cluster's blocks come to it through distributed shared memory.  Every input
-// is read once, every output written once, and the order of the arithmetic is fixed by the sizes alone.
+// run of steps can be summarised before its start is known.  A thread takes 8 steps of two neighbouring channels in
+// registers, the 8 warps of a thread block a chunk of 64 steps, and the block walks through the chunks of its 64 channels;
+// each turn one warp chains the summaries of the others.  Every input is read once, every output written once.
+// Where there are fewer tiles of channels than SMs the time axis is cut into segments as well: a first kernel summarises
+// every segment (it reads the inputs once more, without a barrier in its loop), and the blocks of the second one chain the
+// summaries of the segments before their own.  (Blocks in a cluster that hand summaries on every turn read the inputs only
+// once, but wait for one another: 65536 x 1024 bf16 forward took 235 us that way.)  The order of the arithmetic is fixed
+// by the sizes alone.
 //
 // The kernels are bound by HBM as long as a step costs few instructions: channels are handled in pairs (f32x2 arithmetic),
 // tiles of 64 steps x 64 channels arrive by TMA a turn or two ahead and leave by TMA, so that the threads compute no
 // addresses.  Data that TMA cannot describe (rows that are not multiples of 16 bytes) takes one of two other paths: pairs
 // copied by cp.async, or plain loads of single values.
-#include <cooperative_groups.h>
-
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -20,21 +21,17 @@
 #include "seq_common.cuh"
 #include "tma.cuh"
 
-namespace cg = cooperative_groups;
 using namespace snnk;
 
 namespace {
 
 constexpr int SCAN_K = 8;                       // steps per thread
-constexpr int SCAN_WARPS = 8;
-constexpr int SCAN_THREADS = 32 * SCAN_WARPS;
+constexpr int WARPS = SNN_SCAN_CHUNK / SCAN_K;  // a thread block's turn is a chunk
 constexpr int SCAN_COLS = 64;                   // channels per thread block, two per lane: one group of the 8-bit format
-constexpr int SCAN_MAX_CLUSTER = 8;
 constexpr int SCAN_SHORT = 16;                  // up to so many steps a thread simply walks through them
 constexpr int SCAN_DEPTH = 2;                   // turns whose inputs are in shared memory or on their way
 constexpr int PIECE = SNN_SCAN_CHUNK * SCAN_COLS;   // values of one tensor that a block needs for a turn
 constexpr int WARP_PIECE = SCAN_K * SCAN_COLS;      // ... that a warp does
-static_assert(SCAN_K * SCAN_WARPS == SNN_SCAN_CHUNK, "a thread block's run of steps is a chunk");
 static_assert(SCAN_COLS == KEEP_GROUP, "a warp encodes one group at a time");
 
 // How data comes and goes: TILES by TMA (rows of the tensors are multiples of 16 bytes), PAIRS two values at a time,
@@ -44,6 +41,8 @@ enum Path { SCALAR, PAIRS, TILES };
 struct ScanParams {
   CUtensorMap in[3], out[4];   // TILES.  forward: x, gate -> h, -, codes of x, codes of gate; backward: dh, x, gate -> dx, dgate
   int T, B, N, n_tiles;        // n_tiles: column tiles per sample
+  int segments, segment_steps; // of the time axis; a multiple of a chunk each
+  float4* summaries;           // [segments][B][n_tiles][32] maps of pairs of channels, if there are several segments
   int mode, x_format, gate_format;
   const void *x, *gate, *dh;
   void *h, *dx, *dgate;
@@ -141,31 +140,45 @@ __device__ __forceinline__ int length_of(const ScanParams& p, int b) {
   return p.lengths ? min(max(p.lengths[b], 0), p.T) : p.T;
 }
 
-// Where a thread stands: its block's chunk within the turn, its warp's steps within the chunk, its two channels.
+// Where a thread stands: its block's segment [from, to) of one sample's steps, of which those before `end` exist, its
+// warp's steps within a turn, its two channels.
 struct Place {
-  int S, rank, lane, warp, b, col0, c, n_ok, len, per_turn, ahead;
+  int lane, warp, b, col0, c, n_ok, len, segment, from, to, end, ahead;
+  int64_t map;   // of its pair of channels in a segment's summaries
 };
-__device__ __forceinline__ Place place_of(const ScanParams& p, const cg::cluster_group& cluster) {
+__device__ __forceinline__ Place place_of(const ScanParams& p) {
   Place w;
-  w.S = (int)cluster.num_blocks();
-  w.rank = (int)cluster.block_rank();
   w.lane = threadIdx.x & 31;
   w.warp = threadIdx.x >> 5;
-  const int tile = (int)blockIdx.x / w.S;
+  w.segment = (int)blockIdx.x % p.segments;
+  const int tile = (int)blockIdx.x / p.segments;
   w.b = tile / p.n_tiles;
   w.col0 = (tile % p.n_tiles) * SCAN_COLS;
   w.c = w.col0 + 2 * w.lane;
   w.n_ok = min(max(p.N - w.c, 0), 2);
   w.len = length_of(p, w.b);
-  w.per_turn = w.S * SNN_SCAN_CHUNK;
-  w.ahead = w.rank * SNN_SCAN_CHUNK + w.warp * SCAN_K;
+  w.from = w.segment * p.segment_steps;
+  w.to = w.segment == p.segments - 1 ? p.T : w.from + p.segment_steps;
+  w.end = min(w.to, w.len);
+  w.ahead = w.warp * SCAN_K;
+  w.map = (int64_t)tile * 32 + w.lane;
   return w;
 }
+__device__ __forceinline__ int64_t maps_per_segment(const ScanParams& p) { return (int64_t)p.B * p.n_tiles * 32; }
+// The state before a segment (REVERSE: e behind it), from that before the first (behind the last).
+template <bool REVERSE> __device__ __forceinline__ float2 enter_segment(const ScanParams& p, const Place& w, float2 h) {
+  const int n = REVERSE ? p.segments - 1 - w.segment : w.segment;
+  const float4* at = p.summaries + (REVERSE ? p.segments - 1 : 0) * maps_per_segment(p) + w.map;
+  const int64_t step = REVERSE ? -maps_per_segment(p) : maps_per_segment(p);
+#pragma unroll 8
+  for (int q = 0; q < n; ++q, at += step) h = apply(as_map(*at), h);
+  return h;
+}
 
-// Zeros at the steps [from, T) of two channels, one step per warp of the cluster.
+// Zeros at the steps of the segment from `first` on, two channels, one step per warp.
 template <bool IN_PAIRS, typename IO>
-__device__ __forceinline__ void zero_steps(const ScanParams& p, const Place& w, IO* out, const int64_t* stride, int from) {
-  for (int64_t t = (int64_t)from + w.rank * SCAN_WARPS + w.warp; t < p.T; t += w.S * SCAN_WARPS)
+__device__ __forceinline__ void zero_steps(const Place& w, IO* out, const int64_t* stride, int first) {
+  for (int64_t t = (int64_t)first + w.warp; t < w.to; t += WARPS)
     store_pair<IN_PAIRS>(out + t * stride[0] + w.b * stride[1], w.c, w.n_ok, make_float2(0.f, 0.f));
 }
 
@@ -296,43 +309,13 @@ __device__ __forceinline__ void decode_from_memory(float2 (&v)[SCAN_K], const ui
                            format);
 }
 
-// ---- between the blocks of a cluster --------------------------------------------------------------------------
-// Every turn each block sends the summary of its chunk to all blocks: asynchronous stores to their shared memory that
-// count towards an mbarrier there.  Two buffers are enough: a block sends the summary of turn i + 2 only after it has all of
-// turn i + 1, and a block sends that one only after it has read those of turn i.
-struct ClusterExchange {
-  float4 slot[2][SCAN_MAX_CLUSTER][32];
-  uint64_t full[2];
-};
-// by one whole warp
-__device__ __forceinline__ void exchange_send(ClusterExchange& x, int i, int S, int rank, float4 v) {
-  const int lane = threadIdx.x & 31;
-  const uint32_t slot = smem_u32(&x.slot[i & 1][rank][lane]), bar = smem_u32(&x.full[i & 1]);
-  if (lane == 0) mbar_arrive_expect_tx(&x.full[i & 1], (uint32_t)S * 32u * sizeof(float4));
-  for (int r = 0; r < S; ++r) {
-    uint32_t to, signal;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(slot), "r"(r));
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(signal) : "r"(bar), "r"(r));
-    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(to),
-                 "r"(__float_as_uint(v.x)), "r"(__float_as_uint(v.y)), "r"(__float_as_uint(v.z)), "r"(__float_as_uint(v.w)), "r"(signal)
-                 : "memory");
-  }
-}
-// by the same warp; false if the summaries did not come (then the caller makes its results NaN)
-__device__ __forceinline__ bool exchange_wait(ClusterExchange& x, int i) { return mbar_wait(&x.full[i & 1], (uint32_t)(i >> 1) & 1u); }
-
-struct Shared {
-  ClusterExchange exchange;
-  uint64_t landed[SCAN_DEPTH];   // TILES: the bytes of a slot of the ring
-};
-__device__ __forceinline__ void shared_init(Shared& s, cg::cluster_group& cluster, int S) {
+// The barriers that count the bytes of the ring's slots (TILES).
+__device__ __forceinline__ void barriers_init(uint64_t* landed) {
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2; ++i) mbar_init(&s.exchange.full[i], 1);
-    for (int i = 0; i < SCAN_DEPTH; ++i) mbar_init(&s.landed[i], 1);
+    for (int i = 0; i < SCAN_DEPTH; ++i) mbar_init(&landed[i], 1);
     mbar_fence_init();
   }
-  if (S > 1) cluster.sync();
-  else __syncthreads();
+  __syncthreads();
 }
 __device__ __forceinline__ float2 nan2() { return both(__uint_as_float(0x7fc00000u)); }
 
@@ -341,43 +324,43 @@ template <typename IO> __host__ __device__ constexpr int forward_slot() { return
 template <typename IO, bool KEEP> __host__ __device__ constexpr int forward_out() { return WARP_PIECE * ((int)sizeof(IO) + (KEEP ? 2 : 0)); }   // per warp and buffer
 
 template <typename IO, bool KEEP, int PATH>
-__global__ void __launch_bounds__(SCAN_THREADS, 3) scan_forward_kernel(const __grid_constant__ ScanParams p) {
+__global__ void __launch_bounds__(32 * WARPS, 3) scan_forward_kernel(const __grid_constant__ ScanParams p) {
   constexpr int SLOT = forward_slot<IO>(), OUT = forward_out<IO, KEEP>();
-  extern __shared__ __align__(128) unsigned char s_dyn[];   // ring [SCAN_DEPTH][x, gate]; TILES: then out [SCAN_WARPS][2][h, codes]
-  __shared__ float4 s_sum[SCAN_WARPS][32];
-  __shared__ float2 s_start[SCAN_WARPS][32];
-  __shared__ Shared s;
-  cg::cluster_group cluster = cg::this_cluster();
-  const Place w = place_of(p, cluster);
+  extern __shared__ __align__(128) unsigned char s_dyn[];   // ring [SCAN_DEPTH][x, gate]; TILES: then out [WARPS][2][h, codes]
+  __shared__ float4 s_sum[WARPS][32];
+  __shared__ float2 s_start[WARPS][32];
+  __shared__ uint64_t s_landed[SCAN_DEPTH];
+  const Place w = place_of(p);
   const IO* const x = (const IO*)p.x + w.b * p.xs[1];
   const IO* const gate = (const IO*)p.gate + w.b * p.gs[1];
   IO* const h_out = (IO*)p.h + w.b * p.hs[1];
   auto issue = [&](int turn, int slot) {   // TILES: one thread; PAIRS: all
     unsigned char* const at = s_dyn + slot * SLOT;
     if constexpr (PATH == TILES) {
-      if (turn < w.len) {
-        mbar_arrive_expect_tx(&s.landed[slot], SLOT);
-        tma_load_3d(at, &p.in[0], w.col0, w.b, turn + w.rank * SNN_SCAN_CHUNK, &s.landed[slot]);
-        tma_load_3d(at + SLOT / 2, &p.in[1], w.col0, w.b, turn + w.rank * SNN_SCAN_CHUNK, &s.landed[slot]);
+      if (turn < w.end) {
+        mbar_arrive_expect_tx(&s_landed[slot], SLOT);
+        tma_load_3d(at, &p.in[0], w.col0, w.b, turn, &s_landed[slot]);
+        tma_load_3d(at + SLOT / 2, &p.in[1], w.col0, w.b, turn, &s_landed[slot]);
       }
     }
     if constexpr (PATH == PAIRS) {
-      if (turn < w.len) {
+      if (turn < w.end) {
         stage_pairs<IO>(reinterpret_cast<IO*>(at), x, p.xs[0], w, turn + w.ahead);
         stage_pairs<IO>(reinterpret_cast<IO*>(at + SLOT / 2), gate, p.gs[0], w, turn + w.ahead);
       }
       copies_issued();
     }
   };
-  shared_init(s, cluster, w.S);
-  const bool loader = PATH == PAIRS || (PATH == TILES && threadIdx.x == SCAN_THREADS - 32);
+  barriers_init(s_landed);
+  const bool loader = PATH == PAIRS || (PATH == TILES && threadIdx.x == 32 * (WARPS - 1));
   if (loader)
-    for (int d = 0; d < SCAN_DEPTH; ++d) issue(d * w.per_turn, d);
-  float2 carry = w.warp == 0 ? load_state(p.state, w.b, p.N, w.c, w.n_ok) : both(0.f);   // warp 0 chains the summaries
+    for (int d = 0; d < SCAN_DEPTH; ++d) issue(w.from + d * SNN_SCAN_CHUNK, d);
+  float2 carry = both(0.f);   // warp 0 chains the summaries
+  if (w.warp == 0) carry = enter_segment<false>(p, w, load_state(p.state, w.b, p.N, w.c, w.n_ok));
   bool alive = true;
-  int turn = 0;
-  for (int i = 0; turn < w.len; turn += w.per_turn, ++i) {
-    const int slot = i % SCAN_DEPTH, chunk0 = turn + w.rank * SNN_SCAN_CHUNK, t0 = turn + w.ahead;
+  int turn = w.from;
+  for (int i = 0; turn < w.end; turn += SNN_SCAN_CHUNK, ++i) {
+    const int slot = i % SCAN_DEPTH, t0 = turn + w.ahead;
     const bool full = t0 + SCAN_K <= w.len;
     unsigned char* const out = s_dyn + SCAN_DEPTH * SLOT + (w.warp * 2 + (i & 1)) * OUT;
     float2 xv[SCAN_K], gv[SCAN_K];
@@ -386,7 +369,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) scan_forward_kernel(const __g
       load_values<IO>(gv, gate, p.gs[0], w, t0);
     } else {
       if (PATH == TILES) {
-        if (alive) alive = mbar_wait(&s.landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
+        if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
         if (w.lane == 0) bulk_read_done<1>();   // the out buffer used two turns ago has been read
         __syncwarp();
       } else {
@@ -395,7 +378,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) scan_forward_kernel(const __g
       read_pairs<IO>(xv, s_dyn + slot * SLOT, w);
       read_pairs<IO>(gv, s_dyn + slot * SLOT + SLOT / 2, w);
       if (!alive) gv[0] = nan2();
-      if (PATH == PAIRS) issue(turn + SCAN_DEPTH * w.per_turn, slot);
+      if (PATH == PAIRS) issue(turn + SCAN_DEPTH * SNN_SCAN_CHUNK, slot);
     }
     if constexpr (KEEP) {
       unsigned char* const codes = out + WARP_PIECE * sizeof(IO);
@@ -416,29 +399,17 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) scan_forward_kernel(const __g
     for (int k = 1; k < SCAN_K; ++k) mine = then(mine, Map2{gv[k], xv[k]});
     s_sum[w.warp][w.lane] = as4(mine);
     __syncthreads();
-    if (PATH == TILES && loader) issue(turn + SCAN_DEPTH * w.per_turn, slot);   // all warps have read the slot
+    if (PATH == TILES && loader) issue(turn + SCAN_DEPTH * SNN_SCAN_CHUNK, slot);   // all warps have read the slot
     if (w.warp == 0) {
       float2 h = carry;
-      if (w.S > 1) {
-        Map2 all = mine;
+      if (!alive) h = nan2();
+      if (KEEP) store_state(p.states, (int64_t)(turn / SNN_SCAN_CHUNK) * p.B + w.b, p.N, w.c, w.n_ok, h);
 #pragma unroll
-        for (int v = 1; v < SCAN_WARPS; ++v) all = then(all, as_map(s_sum[v][w.lane]));
-        exchange_send(s.exchange, i, w.S, w.rank, as4(all));
-        const bool came = exchange_wait(s.exchange, i);
-        for (int r = 0; r < w.S; ++r) {
-          if (r == w.rank) h = carry;
-          carry = apply(as_map(s.exchange.slot[i & 1][r][w.lane]), carry);
-        }
-        if (!came) h = carry = nan2();
-      }
-      if (!alive) h = carry = nan2();
-      if (KEEP && chunk0 < w.len) store_state(p.states, (int64_t)(chunk0 / SNN_SCAN_CHUNK) * p.B + w.b, p.N, w.c, w.n_ok, h);
-#pragma unroll
-      for (int v = 0; v < SCAN_WARPS; ++v) {
+      for (int v = 0; v < WARPS; ++v) {
         s_start[v][w.lane] = h;
         h = apply(as_map(s_sum[v][w.lane]), h);
       }
-      if (w.S == 1) carry = h;
+      carry = h;
     }
     __syncthreads();
     float2 h = s_start[w.warp][w.lane];
@@ -457,7 +428,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) scan_forward_kernel(const __g
       fence_proxy_async_smem();
       __syncwarp();
       if (w.lane == 0) {
-        if (t0 < p.T) {
+        if (t0 < w.to) {
           tma_store_3d(&p.out[0], w.col0, w.b, t0, out);
           if (KEEP && p.x_format != SNN_KEEP_RAW) tma_store_3d(&p.out[2], w.col0, w.b, t0, out + WARP_PIECE * sizeof(IO));
           if (KEEP && p.gate_format != SNN_KEEP_RAW) tma_store_3d(&p.out[3], w.col0, w.b, t0, out + WARP_PIECE * (sizeof(IO) + 1));
@@ -473,12 +444,11 @@ __global__ void __launch_bounds__(SCAN_THREADS, 3) scan_forward_kernel(const __g
       }
     }
   }
-  if (w.rank == 0 && w.warp == 0) store_state(p.last, w.b, p.N, w.c, w.n_ok, carry);
-  zero_steps<PATH != SCALAR>(p, w, (IO*)p.h, p.hs, PATH == TILES ? turn : w.len);
+  if (w.segment == p.segments - 1 && w.warp == 0) store_state(p.last, w.b, p.N, w.c, w.n_ok, carry);
+  zero_steps<PATH != SCALAR>(w, (IO*)p.h, p.hs, PATH == TILES ? turn : max(w.end, w.from));
   if (PATH == TILES && w.lane == 0) bulk_read_done<0>();
   if (!alive)
     for (int i = 0; i < 100; ++i) __nanosleep(20000);   // copies that did not come in time may still be under way
-  if (w.S > 1) cluster.sync();   // no block leaves while another may still write to its shared memory
 }
 
 // Few steps (the token of a serving loop): a thread takes two channels of one sample through all of them.
@@ -515,15 +485,14 @@ __global__ void __launch_bounds__(128) scan_short_kernel(const __grid_constant__
 // last step to the first; the states of the chunk are recomputed from its checkpoint by the forward maps.  A block's
 // chunk starts at a checkpoint, so only e crosses blocks.  Warp 0 chains the states, warp 1 the e.
 template <typename IO, int PATH>
-__global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const __grid_constant__ ScanParams p) {
+__global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __grid_constant__ ScanParams p) {
   constexpr int VALUES = PIECE * (int)sizeof(IO), OUT = 2 * WARP_PIECE * (int)sizeof(IO);
   extern __shared__ __align__(128) unsigned char s_dyn[];   // ring [SCAN_DEPTH] of dh, x, gate (values or codes); TILES: out
-  __shared__ float4 s_forth[SCAN_WARPS][32];
-  __shared__ float2 s_back[SCAN_WARPS][32];
-  __shared__ float2 s_h[SCAN_WARPS][32], s_e[SCAN_WARPS][32];
-  __shared__ Shared s;
-  cg::cluster_group cluster = cg::this_cluster();
-  const Place w = place_of(p, cluster);
+  __shared__ float4 s_forth[WARPS][32];
+  __shared__ float2 s_back[WARPS][32];
+  __shared__ float2 s_h[WARPS][32], s_e[WARPS][32];
+  __shared__ uint64_t s_landed[SCAN_DEPTH];
+  const Place w = place_of(p);
   const IO* const x = (const IO*)p.x + w.b * p.xs[1];
   const IO* const gate = (const IO*)p.gate + w.b * p.gs[1];
   const IO* const dh = (const IO*)p.dh + w.b * p.dhs[1];
@@ -532,16 +501,15 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const __
   auto issue = [&](int turn, int slot) {
     unsigned char* const at = s_dyn + slot * slot_bytes;
     if constexpr (PATH == TILES) {
-      if (turn >= 0) {
-        const int t = turn + w.rank * SNN_SCAN_CHUNK;
-        mbar_arrive_expect_tx(&s.landed[slot], slot_bytes);
-        tma_load_3d(at, &p.in[0], w.col0, w.b, t, &s.landed[slot]);
-        tma_load_3d(at + x_at, &p.in[1], w.col0, w.b, t, &s.landed[slot]);
-        tma_load_3d(at + gate_at, &p.in[2], w.col0, w.b, t, &s.landed[slot]);
+      if (turn >= w.from) {
+        mbar_arrive_expect_tx(&s_landed[slot], slot_bytes);
+        tma_load_3d(at, &p.in[0], w.col0, w.b, turn, &s_landed[slot]);
+        tma_load_3d(at + x_at, &p.in[1], w.col0, w.b, turn, &s_landed[slot]);
+        tma_load_3d(at + gate_at, &p.in[2], w.col0, w.b, turn, &s_landed[slot]);
       }
     }
     if constexpr (PATH == PAIRS) {   // (8-bit codes are read from memory on this path)
-      if (turn >= 0) {
+      if (turn >= w.from) {
         stage_pairs<IO>(reinterpret_cast<IO*>(at), dh, p.dhs[0], w, turn + w.ahead);
         if (raw_x) stage_pairs<IO>(reinterpret_cast<IO*>(at + x_at), x, p.xs[0], w, turn + w.ahead);
         if (raw_gate) stage_pairs<IO>(reinterpret_cast<IO*>(at + gate_at), gate, p.gs[0], w, turn + w.ahead);
@@ -551,35 +519,36 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const __
   };
   // scale bytes: of x in lanes 0..7 (one per step), of the gate in lanes 8..15, read one turn ahead
   auto load_scales = [&](int turn) -> uint32_t {
-    if (turn < 0 || w.lane >= 16 || (w.lane < 8 ? raw_x : raw_gate)) return 0u;
+    if (turn < w.from || w.lane >= 16 || (w.lane < 8 ? raw_x : raw_gate)) return 0u;
     const int64_t row = (int64_t)min(turn + w.ahead + (w.lane & 7), w.len - 1) * p.B + w.b;
     return (w.lane < 8 ? p.x_scales : p.gate_scales)[row * p.n_tiles + w.col0 / KEEP_GROUP];
   };
-  auto load_start = [&](int turn) {   // the kept state of this block's chunk
-    if (turn < 0 || w.warp != 0) return both(0.f);
-    return load_state(p.states, (int64_t)(min(turn + w.rank * SNN_SCAN_CHUNK, w.len - 1) / SNN_SCAN_CHUNK) * p.B + w.b, p.N, w.c, w.n_ok);
+  auto load_start = [&](int turn) {   // the kept state of the turn's chunk
+    if (turn < w.from || w.warp != 0) return both(0.f);
+    return load_state(p.states, (int64_t)(turn / SNN_SCAN_CHUNK) * p.B + w.b, p.N, w.c, w.n_ok);
   };
-  shared_init(s, cluster, w.S);
-  const bool loader = PATH == PAIRS || (PATH == TILES && threadIdx.x == SCAN_THREADS - 32);
-  const int turns = (w.len + w.per_turn - 1) / w.per_turn, last_turn = (turns - 1) * w.per_turn;
+  barriers_init(s_landed);
+  const bool loader = PATH == PAIRS || (PATH == TILES && threadIdx.x == 32 * (WARPS - 1));
+  const int turns = (max(w.end - w.from, 0) + SNN_SCAN_CHUNK - 1) / SNN_SCAN_CHUNK, last_turn = w.from + (turns - 1) * SNN_SCAN_CHUNK;
   if (loader)
-    for (int d = 0; d < SCAN_DEPTH; ++d) issue(last_turn - d * w.per_turn, d);
-  float2 carry = w.warp == 1 ? load_state(p.dlast, w.b, p.N, w.c, w.n_ok) : both(0.f);   // e behind the turn's last step
+    for (int d = 0; d < SCAN_DEPTH; ++d) issue(last_turn - d * SNN_SCAN_CHUNK, d);
+  float2 carry = both(0.f);   // e behind the turn's last step, chained by warp 1
+  if (w.warp == 1) carry = enter_segment<true>(p, w, load_state(p.dlast, w.b, p.N, w.c, w.n_ok));
   uint32_t next_scales = load_scales(last_turn);
   float2 next_start = load_start(last_turn);
   bool alive = true;
-  for (int turn = last_turn, i = 0; turn >= 0; turn -= w.per_turn, ++i) {
+  for (int turn = last_turn, i = 0; turn >= w.from; turn -= SNN_SCAN_CHUNK, ++i) {
     const int slot = i % SCAN_DEPTH, t0 = turn + w.ahead;
     const bool full = t0 + SCAN_K <= w.len;
     unsigned char* const out = s_dyn + SCAN_DEPTH * slot_bytes + (w.warp * 2 + (i & 1)) * OUT;
     float2 xv[SCAN_K], a[SCAN_K], in[SCAN_K], d[SCAN_K];
     const uint32_t scales = next_scales;
     const float2 start = next_start;
-    next_scales = load_scales(turn - w.per_turn);
-    next_start = load_start(turn - w.per_turn);
+    next_scales = load_scales(turn - SNN_SCAN_CHUNK);
+    next_start = load_start(turn - SNN_SCAN_CHUNK);
     unsigned char* const at = s_dyn + slot * slot_bytes;
     if (PATH == TILES) {
-      if (alive) alive = mbar_wait(&s.landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
+      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
       if (w.lane == 0) bulk_read_done<1>();
       __syncwarp();
     }
@@ -604,7 +573,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const __
     } else {
       decode_from_memory<IO>(a, p.gate_codes, p, w, t0, scales, 8, p.gate_format);
     }
-    if (PATH == PAIRS) issue(turn - SCAN_DEPTH * w.per_turn, slot);
+    if (PATH == PAIRS) issue(turn - SCAN_DEPTH * SNN_SCAN_CHUNK, slot);
     if (!alive) a[0] = nan2();
     coefficients(a, in, p.mode);
     if (!full) {
@@ -622,36 +591,24 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const __
     s_forth[w.warp][w.lane] = as4(forth);
     s_back[w.warp][w.lane] = e0;
     __syncthreads();
-    if (PATH == TILES && loader) issue(turn - SCAN_DEPTH * w.per_turn, slot);
+    if (PATH == TILES && loader) issue(turn - SCAN_DEPTH * SNN_SCAN_CHUNK, slot);
     if (w.warp == 0) {
       float2 h = alive ? start : nan2();
 #pragma unroll
-      for (int v = 0; v < SCAN_WARPS; ++v) {
+      for (int v = 0; v < WARPS; ++v) {
         s_h[v][w.lane] = h;
         h = apply(as_map(s_forth[v][w.lane]), h);
       }
     } else if (w.warp == 1) {
       auto back = [&](int v) { return Map2{as_map(s_forth[v][w.lane]).a, s_back[v][w.lane]}; };
       float2 e = carry;
-      if (w.S > 1) {
-        Map2 all = back(SCAN_WARPS - 1);
+      if (!alive) e = nan2();
 #pragma unroll
-        for (int v = SCAN_WARPS - 2; v >= 0; --v) all = then(all, back(v));
-        exchange_send(s.exchange, i, w.S, w.rank, as4(all));
-        const bool came = exchange_wait(s.exchange, i);
-        for (int r = w.S - 1; r >= 0; --r) {
-          if (r == w.rank) e = carry;
-          carry = apply(as_map(s.exchange.slot[i & 1][r][w.lane]), carry);
-        }
-        if (!came) e = carry = nan2();
-      }
-      if (!alive) e = carry = nan2();
-#pragma unroll
-      for (int v = SCAN_WARPS - 1; v >= 0; --v) {
+      for (int v = WARPS - 1; v >= 0; --v) {
         s_e[v][w.lane] = e;
         e = apply(back(v), e);
       }
-      if (w.S == 1) carry = e;
+      carry = e;
     }
     __syncthreads();
     float2 h = s_h[w.warp][w.lane], e = s_e[w.warp][w.lane];
@@ -694,7 +651,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const __
       fence_proxy_async_smem();
       __syncwarp();
       if (w.lane == 0) {
-        if (t0 < p.T) {
+        if (t0 < w.to) {
           tma_store_3d(&p.out[0], w.col0, w.b, t0, out);
           tma_store_3d(&p.out[1], w.col0, w.b, t0, out + OUT / 2);
         }
@@ -702,14 +659,75 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(const __
       }
     }
   }
-  if (w.rank == 0 && w.warp == 1) store_state(p.dstate, w.b, p.N, w.c, w.n_ok, carry);
-  const int from = PATH == TILES ? turns * w.per_turn : w.len;
-  zero_steps<PATH != SCALAR>(p, w, (IO*)p.dx, p.dxs, from);
-  zero_steps<PATH != SCALAR>(p, w, (IO*)p.dgate, p.dgs, from);
+  if (w.segment == 0 && w.warp == 1) store_state(p.dstate, w.b, p.N, w.c, w.n_ok, carry);
+  const int first = PATH == TILES ? w.from + turns * SNN_SCAN_CHUNK : max(w.end, w.from);
+  zero_steps<PATH != SCALAR>(w, (IO*)p.dx, p.dxs, first);
+  zero_steps<PATH != SCALAR>(w, (IO*)p.dgate, p.dgs, first);
   if (PATH == TILES && w.lane == 0) bulk_read_done<0>();
   if (!alive)
     for (int i = 0; i < 100; ++i) __nanosleep(20000);
-  if (w.S > 1) cluster.sync();
+}
+
+// ---- segments ------------------------------------------------------------------------------------------------
+// The map of every segment but the last (REVERSE, the backward pass: but the first).  A warp takes an eighth of the
+// segment's steps on its own, so nothing waits inside the loop; plain loads, 8 steps at a time.
+template <typename IO, bool IN_PAIRS, bool REVERSE>
+__global__ void __launch_bounds__(32 * WARPS, 3) scan_summary_kernel(const __grid_constant__ ScanParams p) {
+  __shared__ float4 s_sum[WARPS][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int tile = (int)blockIdx.x / (p.segments - 1), segment = (int)blockIdx.x % (p.segments - 1) + (REVERSE ? 1 : 0);
+  const int b = tile / p.n_tiles, c = (tile % p.n_tiles) * SCAN_COLS + 2 * lane, n_ok = min(max(p.N - c, 0), 2);
+  const int len = length_of(p, b), share = p.segment_steps / WARPS, first = segment * p.segment_steps + warp * share;
+  const int end = min(first + share, len);
+  const IO* const from = REVERSE ? (const IO*)p.dh + b * p.dhs[1] : (const IO*)p.x + b * p.xs[1];
+  const int64_t from_stride = REVERSE ? p.dhs[0] : p.xs[0];
+  const IO* const gate = (const IO*)p.gate + b * p.gs[1];
+  const bool raw_gate = !REVERSE || p.gate_format == SNN_KEEP_RAW;
+  Map2 m{both(1.f), both(0.f)};
+  const int turns = (max(end - first, 0) + SCAN_K - 1) / SCAN_K;
+  for (int i = 0; i < turns; ++i) {
+    const int t0 = first + (REVERSE ? turns - 1 - i : i) * SCAN_K;
+    float2 v[SCAN_K], a[SCAN_K], in[SCAN_K];
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) v[k] = load_pair<IN_PAIRS>(from + min(t0 + k, end - 1) * from_stride, c, n_ok);
+    if (raw_gate) {
+#pragma unroll
+      for (int k = 0; k < SCAN_K; ++k) a[k] = load_pair<IN_PAIRS>(gate + min(t0 + k, end - 1) * p.gs[0], c, n_ok);
+    } else {
+      uint32_t codes[SCAN_K], bytes[SCAN_K];
+#pragma unroll
+      for (int k = 0; k < SCAN_K; ++k) {
+        const int64_t row = (int64_t)min(t0 + k, end - 1) * p.B + b;
+        const uint8_t* const at = p.gate_codes + row * p.N;
+        if (IN_PAIRS) codes[k] = *reinterpret_cast<const uint16_t*>(at + (n_ok ? c : 0));
+        else codes[k] = (uint32_t)at[n_ok ? c : 0] | (uint32_t)at[n_ok == 2 ? c + 1 : 0] << 8;
+        bytes[k] = p.gate_scales[row * p.n_tiles + (c - 2 * lane) / KEEP_GROUP];
+      }
+#pragma unroll
+      for (int k = 0; k < SCAN_K; ++k)
+        a[k] = p.gate_format == SNN_KEEP_INT8 ? keep_decode2<IO, SNN_KEEP_INT8>(codes[k], keep_scale_value(bytes[k]))
+                                              : keep_decode2<IO, SNN_KEEP_E4M3>(codes[k], keep_scale_value(bytes[k]));
+    }
+    coefficients(a, in, p.mode);
+    if (t0 + SCAN_K > end) {
+#pragma unroll
+      for (int k = 0; k < SCAN_K; ++k)
+        if (t0 + k >= end) a[k] = both(1.f), v[k] = both(0.f);
+    }
+#pragma unroll
+    for (int j = 0; j < SCAN_K; ++j) {
+      const int k = REVERSE ? SCAN_K - 1 - j : j;
+      m = then(m, Map2{a[k], mul2(REVERSE ? a[k] : in[k], v[k])});
+    }
+  }
+  s_sum[warp][lane] = as4(m);
+  __syncthreads();
+  if (warp == 0) {
+    m = as_map(s_sum[REVERSE ? WARPS - 1 : 0][lane]);
+#pragma unroll
+    for (int v = 1; v < WARPS; ++v) m = then(m, as_map(s_sum[REVERSE ? WARPS - 1 - v : v][lane]));
+    p.summaries[segment * maps_per_segment(p) + (int64_t)tile * 32 + lane] = as4(m);
+  }
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------
@@ -775,40 +793,47 @@ ScanParams params_of(const snn_scan_args* a) {
   p.x_codes = a->x_codes; p.x_scales = a->x_scales; p.gate_codes = a->gate_codes; p.gate_scales = a->gate_scales;
   return p;
 }
-// Blocks per column tile.  All blocks take equally long, so what counts is how full the device is over the waves that they
-// need, at `resident` blocks per SM; among clusters that fill it about as well the smallest (a larger one waits longer for
-// its summaries).  No more blocks than there are chunks.
-int cluster_of(int64_t tiles, int T, int resident) {
-  const double slots = 148.0 * resident;
-  int best = 1;
-  double best_fill = 0;
-  for (int S = 1; S <= SCAN_MAX_CLUSTER && (S == 1 || (int64_t)(S / 2) * SNN_SCAN_CHUNK < T); S *= 2) {
-    const double waves = (double)tiles * S / slots, fill = waves / std::ceil(waves);
-    if (fill > 1.08 * best_fill) best = S, best_fill = fill;
-  }
-  return best;
-}
-template <typename K> snn_status launch_clusters(K kernel, size_t smem, int resident, const ScanParams& p, cudaStream_t stream) {
+// Segments of the time axis.  One while there are about as many column tiles as SMs.  Below that the device is filled once
+// (`resident` blocks fit an SM), as long as a segment has a few turns: reading the inputs twice costs less than the SMs
+// left idle.
+void cut_time(ScanParams& p, int resident) {
   const int64_t tiles = (int64_t)p.B * p.n_tiles;
-  const int S = cluster_of(tiles, p.T, resident);
-  if (tiles * S > INT32_MAX) return SNN_ERR_UNSUPPORTED;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(tiles * S));
-  cfg.blockDim = dim3(SCAN_THREADS);
-  cfg.stream = stream;
-  cfg.dynamicSmemBytes = smem;
+  int64_t n = 1;
+  if (tiles > 0 && tiles < 148) n = std::min<int64_t>(148 * resident / tiles, p.T / (4 * SNN_SCAN_CHUNK));
+  n = std::max<int64_t>(n, 1);
+  p.segment_steps = (int)((((int64_t)p.T + n - 1) / n + SNN_SCAN_CHUNK - 1) / SNN_SCAN_CHUNK * SNN_SCAN_CHUNK);
+  p.segments = p.segment_steps ? (p.T + p.segment_steps - 1) / p.segment_steps : 1;
+}
+int resident_blocks(const snn_scan_args* a, bool backward) { return (backward ? 2 : 3) - (a->dtype == SNN_DTYPE_FP32); }
+size_t summary_bytes(const ScanParams& p) { return p.segments > 1 ? sizeof(float4) * 32 * (size_t)p.segments * p.B * p.n_tiles : 0; }
+
+snn_status set_segments(ScanParams& p, const snn_scan_args* a, bool backward) {
+  cut_time(p, resident_blocks(a, backward));
+  if (p.segments == 1) return SNN_OK;
+  if (a->workspace_bytes < summary_bytes(p)) return SNN_ERR_WORKSPACE_TOO_SMALL;
+  if (!a->workspace || (uintptr_t)a->workspace % 256 != 0) return SNN_ERR_INVALID_ARG;
+  p.summaries = (float4*)a->workspace;
+  return SNN_OK;
+}
+template <typename K> snn_status launch(K kernel, size_t smem, int64_t blocks, const ScanParams& p, cudaStream_t stream) {
+  if (blocks > INT32_MAX) return SNN_ERR_UNSUPPORTED;
   if (smem && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return cudaGetLastError(), SNN_ERR_CUDA;
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeClusterDimension;
-  at.val.clusterDim.x = (unsigned)S;
-  at.val.clusterDim.y = at.val.clusterDim.z = 1;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+  kernel<<<(unsigned)blocks, 32 * WARPS, smem, stream>>>(p);
+  return launched();
 }
 
 }  // namespace
+
+extern "C" snn_status snn_scan_workspace(const snn_scan_args* a, int32_t backward, size_t* bytes) {
+  const snn_status st = check_common(a);
+  if (st != SNN_OK) return st;
+  if (!bytes) return SNN_ERR_INVALID_ARG;
+  ScanParams p = params_of(a);
+  cut_time(p, resident_blocks(a, backward != 0));
+  *bytes = summary_bytes(p);
+  return SNN_OK;
+}
 
 extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
   const snn_status st = check_common(a);
@@ -833,17 +858,24 @@ extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
       return launched();
     });
   }
+  const snn_status cut = set_segments(p, a, false);
+  if (cut != SNN_OK) return cut;
   const bool tiles = pairs && value_map(&p.in[0], p.x, a, p.xs, SNN_SCAN_CHUNK) && value_map(&p.in[1], p.gate, a, p.gs, SNN_SCAN_CHUNK) &&
                      value_map(&p.out[0], p.h, a, p.hs, SCAN_K) && (p.x_format == SNN_KEEP_RAW || code_map(&p.out[2], p.x_codes, a, SCAN_K)) &&
                      (p.gate_format == SNN_KEEP_RAW || code_map(&p.out[3], p.gate_codes, a, SCAN_K));
   return by_type(a->dtype, tiles ? TILES : pairs ? PAIRS : SCALAR, [&](auto io, auto path) {
     using IO = decltype(io);
     constexpr int PATH = decltype(path)::value;
+    const int64_t blocks = (int64_t)p.B * p.n_tiles;
     auto go = [&](auto is_keep) {
       constexpr bool KEEP = decltype(is_keep)::value;
-      const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * forward_slot<IO>(), out = PATH == TILES ? 2 * SCAN_WARPS * forward_out<IO, KEEP>() : 0;
-      return launch_clusters(scan_forward_kernel<IO, KEEP, PATH>, ring + out, ring + out > 90000 ? 2 : 3, p, s);
+      const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * forward_slot<IO>(), out = PATH == TILES ? 2 * WARPS * forward_out<IO, KEEP>() : 0;
+      return launch(scan_forward_kernel<IO, KEEP, PATH>, ring + out, blocks * p.segments, p, s);
     };
+    if (p.segments > 1) {
+      const snn_status st = launch(scan_summary_kernel<IO, PATH != SCALAR, false>, 0, blocks * (p.segments - 1), p, s);
+      if (st != SNN_OK) return st;
+    }
     return keep ? go(std::true_type()) : go(std::false_type());
   });
 }
@@ -862,6 +894,8 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
   const size_t size = dtype_size(a->dtype);
   const bool pairs = a->N % 2 == 0 && pairs_aligned(p.dh, size, p.dhs) && pairs_aligned(p.dx, size, p.dxs) && pairs_aligned(p.dgate, size, p.dgs) &&
                      (!raw_x || pairs_aligned(p.x, size, p.xs)) && (!raw_gate || pairs_aligned(p.gate, size, p.gs));
+  const snn_status cut = set_segments(p, a, true);
+  if (cut != SNN_OK) return cut;
   const bool tiles = pairs && a->T > 0 && value_map(&p.in[0], p.dh, a, p.dhs, SNN_SCAN_CHUNK) &&
                      (raw_x ? value_map(&p.in[1], p.x, a, p.xs, SNN_SCAN_CHUNK) : code_map(&p.in[1], p.x_codes, a, SNN_SCAN_CHUNK)) &&
                      (raw_gate ? value_map(&p.in[2], p.gate, a, p.gs, SNN_SCAN_CHUNK) : code_map(&p.in[2], p.gate_codes, a, SNN_SCAN_CHUNK)) &&
@@ -870,7 +904,12 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
     using IO = decltype(io);
     constexpr int PATH = decltype(path)::value;
     const size_t values = PIECE * sizeof(IO), slot = values + (raw_x ? values : PIECE) + (raw_gate ? values : PIECE);
-    const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * slot, out = PATH == TILES ? 2 * SCAN_WARPS * 2 * WARP_PIECE * sizeof(IO) : 0;
-    return launch_clusters(scan_backward_kernel<IO, PATH>, ring + out, ring + out > 90000 ? 1 : 2, p, (cudaStream_t)stream);
+    const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * slot, out = PATH == TILES ? 2 * WARPS * 2 * WARP_PIECE * sizeof(IO) : 0;
+    const int64_t blocks = (int64_t)p.B * p.n_tiles;
+    if (p.segments > 1) {
+      const snn_status st = launch(scan_summary_kernel<IO, PATH != SCALAR, true>, 0, blocks * (p.segments - 1), p, (cudaStream_t)stream);
+      if (st != SNN_OK) return st;
+    }
+    return launch(scan_backward_kernel<IO, PATH>, ring + out, blocks * p.segments, p, (cudaStream_t)stream);
   });
 }

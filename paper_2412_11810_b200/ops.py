@@ -141,6 +141,15 @@ def _scan_args(shape, dtype: torch.dtype, mode: str, lengths: Optional[torch.Ten
     return a
 
 
+def _scan_workspace(a: sb.snn_scan_args, backward: bool, device: torch.device) -> Optional[torch.Tensor]:
+    n = sb.snn_scan_workspace(a, backward)
+    if n == 0:
+        return None
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    a.workspace, a.workspace_bytes = ws.data_ptr(), n
+    return ws
+
+
 def _set_strided(a, name: str, t: torch.Tensor) -> None:
     setattr(a, name, t.data_ptr())
     s = getattr(a, name + "_stride")
@@ -199,6 +208,7 @@ def gated_scan(x: torch.Tensor, gate: torch.Tensor, state: Optional[torch.Tensor
                 setattr(a, name + "_codes", codes.data_ptr())
                 setattr(a, name + "_scales", scales.data_ptr())
             kept = ScanKept((T, B, N), x.dtype, mode, states, lengths, held["x"], held["gate"])
+        ws = _scan_workspace(a, False, x.device)  # noqa: F841  (held until the launch)
         sb.snn_scan_forward(a, _stream(x.device))
     return h, last, kept
 
@@ -253,6 +263,7 @@ def gated_scan_backward(kept: ScanKept, dh: torch.Tensor, dlast: Optional[torch.
         _set_strided(a, "dx", dx)
         _set_strided(a, "dgate", dgate)
         a.states, a.dlast, a.dstate = kept.states.data_ptr(), _ptr(dlast), dstate.data_ptr()
+        ws = _scan_workspace(a, True, like.device)  # noqa: F841
         sb.snn_scan_backward(a, _stream(like.device))
     return dx, dgate, dstate
 

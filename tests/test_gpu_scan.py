@@ -83,7 +83,7 @@ def test_scan_with_gradients(T, B, N, mode, dtype):
 @pytest.mark.parametrize("dtype,keep", [("fp32", "raw"), ("bf16", "raw"), ("fp32", "int8"), ("bf16", "int8"), ("fp16", "e4m3")])
 @pytest.mark.parametrize("T,B,N,lengths", [(70, 4, 130, (0, 70, 33, 1)), (600, 3, 67, (64, 599, 777)), (150, 2, 64, (-3, 128)),
                                            (5, 3, 9, (5, 0, 2)), (9, 2, 128, (0, 0)), (700, 3, 80, (700, 65, 129)),
-                                           (2000, 1, 16, (1999,)), (300, 200, 48, tuple((i * 37) % 301 for i in range(200)))])
+                                           (2000, 1, 16, (1999,)), (2000, 2, 16, (700, 3)), (3000, 1, 33, (2561,)), (300, 200, 48, tuple((i * 37) % 301 for i in range(200)))])
 def test_scan_layouts_lengths_and_kept_formats(T, B, N, lengths, dtype, keep, layout):
     x, gate, dh, state, dlast, n = inputs(T, B, N, dtype, "sigmoid", 2, lengths, layout)
     eight = None if keep == "raw" else keep

@@ -41,6 +41,22 @@ def test_scan_refuses_missing_buffers():
     assert sb.lib.snn_scan_backward(C.byref(direct), None) == sb.SNN_ERR_UNSUPPORTED
 
 
+def test_scan_workspace():
+    """Needed where there are few channels and many steps; small, and refused when it is missing."""
+    for backward in (False, True):
+        assert sb.snn_scan_workspace(_scan_args(T=64), backward) == 0
+        assert sb.snn_scan_workspace(_scan_args(T=4096, B=64, N=1024), backward) == 0
+        a = _scan_args(T=65536, B=1, N=1024, dtype=sb.SNN_DTYPE_BF16)
+        n = sb.snn_scan_workspace(a, backward)
+        assert 0 < n < 65536 * 1024 * 2 // 50
+        a.workspace, a.workspace_bytes = 1 << 20, n - 1
+        call = sb.lib.snn_scan_backward if backward else sb.lib.snn_scan_forward
+        assert call(C.byref(a), None) == sb.SNN_ERR_WORKSPACE_TOO_SMALL
+        a.workspace, a.workspace_bytes = (1 << 20) + 16, n
+        assert call(C.byref(a), None) == sb.SNN_ERR_INVALID_ARG
+    assert sb.lib.snn_scan_workspace(C.byref(_scan_args()), 0, None) == sb.SNN_ERR_INVALID_ARG
+
+
 @pytest.mark.parametrize("rows,cols,dtype,fmt", [(-1, 4, 0, 1), (4, -1, 0, 1), (4, 4, 3, 1), (4, 4, 0, 0), (4, 4, 0, 3), (4, 4, 0, 1)])
 def test_pack_refuses_invalid_arguments(rows, cols, dtype, fmt):
     assert sb.lib.snn_activation_pack(None, dtype, rows, cols, 4, fmt, None, None, None) == sb.SNN_ERR_INVALID_ARG
@@ -103,12 +119,12 @@ def test_struct_sizes_match_the_header(tmp_path):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     src = tmp_path / "s.c"
     src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "%s/include/snn.h"\nint main(void) {\n'
-                   'printf("%%zu %%zu\\n", sizeof(snn_scan_args), offsetof(snn_scan_args, dstate));\n'
+                   'printf("%%zu %%zu\\n", sizeof(snn_scan_args), offsetof(snn_scan_args, workspace_bytes));\n'
                    'printf("%%zu %%zu\\n", sizeof(snn_vocab_loss_args), offsetof(snn_vocab_loss_args, workspace_bytes));\n'
                    'printf("%%d %%d\\n", SNN_KEEP_GROUP, SNN_SCAN_CHUNK); return 0; }\n' % root)
     subprocess.run(["gcc", str(src), "-o", str(tmp_path / "s")], check=True)
     out = subprocess.run([str(tmp_path / "s")], check=True, capture_output=True, text=True).stdout.split()
-    assert [int(v) for v in out] == [C.sizeof(sb.snn_scan_args), sb.snn_scan_args.dstate.offset, C.sizeof(sb.snn_vocab_loss_args),
+    assert [int(v) for v in out] == [C.sizeof(sb.snn_scan_args), sb.snn_scan_args.workspace_bytes.offset, C.sizeof(sb.snn_vocab_loss_args),
                                      sb.snn_vocab_loss_args.workspace_bytes.offset, ops.KEEP_GROUP, ops.SCAN_CHUNK]
 
 

@@ -324,7 +324,7 @@ template <typename IO> __host__ __device__ constexpr int forward_slot() { return
 template <typename IO, bool KEEP> __host__ __device__ constexpr int forward_out() { return WARP_PIECE * ((int)sizeof(IO) + (KEEP ? 2 : 0)); }   // per warp and buffer
 
 template <typename IO, bool KEEP, int PATH>
-__global__ void __launch_bounds__(32 * WARPS, 3) scan_forward_kernel(const __grid_constant__ ScanParams p) {
+__global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) scan_forward_kernel(const __grid_constant__ ScanParams p) {
   constexpr int SLOT = forward_slot<IO>(), OUT = forward_out<IO, KEEP>();
   extern __shared__ __align__(128) unsigned char s_dyn[];   // ring [SCAN_DEPTH][x, gate]; TILES: then out [WARPS][2][h, codes]
   __shared__ float4 s_sum[WARPS][32];

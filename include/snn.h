@@ -423,10 +423,10 @@ snn_status snn_scan_backward(const snn_scan_args* args, void* stream);
  * A row with target = ignore_index does not count: its row_loss and lse are 0, its dx is 0, whatever x holds there.  Any
  * other target outside [0, classes) makes that row_loss and the loss NaN and counts like an ignored row in the gradients;
  * it is never used as an index.  If no row counts, loss and gradients are 0.
- * The products run on the tensor cores.  bf16 and fp16 operands are used as they are; fp32 ones are split into three bf16
- * parts (24 bits in all) of which the six products that matter are summed.  Sums are fp32.  In the backward pass the
- * derivatives by the logits exist one piece of the vocabulary at a time, rounded to the operands' type (fp32: in three
- * parts), in the workspace.
+ * The products run on the tensor cores.  bf16 and fp16 operands are used as they are; fp32 ones are scaled by a power of
+ * two and split into two fp16 parts: 22 bits of a value, down to 2^-40 of the largest magnitude in its tensor (rows that
+ * do not count left out).  Sums are fp32.  In the backward pass the derivatives by the logits exist one piece of the
+ * vocabulary at a time, rounded to the operands' type (fp32: to 22 bits), in the workspace.
  * W_out is stored by feature (SNN_W_BY_FEATURE: [dim][classes] as everywhere in this library) or by class
  * (SNN_W_BY_CLASS: [classes][dim], the transpose, as in an embedding table); w_stride is the distance of its rows. dw has
  * the same layout with its own stride. */

@@ -9,6 +9,12 @@
 //   DX      dz w^T, fp32, added to what earlier pieces left (the contraction may be split; parts are joined at the end)
 //   DW      x^T dz, scaled and rounded
 // Work per pass: 2 rows dim classes for STATS, three times that for the backward pass (one of them the recomputation).
+//
+// fp32 operands are scaled by a power of two, so that the largest magnitude of a tensor lies in [2^14, 2^15), and split
+// into two fp16 parts: 22 bits of a value, down to 2^-40 of the largest one.  Three products of parts instead of one (the
+// product of the two small parts, below 2^-22 of the whole, is left out).  Three bf16 parts keep all 24 bits at any
+// magnitude, but need six products: twice the time for errors that the sums' own fp32 rounding hides (measured against
+// 64 bits at 500 x 1000 x 5003).
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -26,7 +32,7 @@ constexpr int VL_EPILOGUE_WARPS = 4;
 constexpr int VL_THREADS = 32 * (2 + VL_EPILOGUE_WARPS);
 constexpr uint32_t VL_STORE_BYTES = UM_HALF * 128;           // one staged block of dz: 128 rows x 64 values
 constexpr size_t VL_SMEM = 1024 + (size_t)UM_STAGES * UM_STAGE_BYTES + 2 * VL_STORE_BYTES + 256;
-constexpr float FP16_DZ_SCALE = 16384.f;   // dz / (gradient of the row loss) lies in [-1, 1]; fp16 keeps small values better after this
+constexpr float FP16_DZ_SCALE = 16384.f;   // dz / (gradient of the row loss) lies in [-1, 1]; as fp16 it keeps small values better after this
 constexpr size_t PIECE_BYTES = (size_t)256 << 20;            // dz held at a time
 constexpr int MAX_SPLITS = 32;
 
@@ -36,7 +42,7 @@ struct ProductParams {
   CUtensorMap a, b, out;      // out: GRAD only
   int tiles_m, tiles_n;       // 256 x 256 tiles; m is the fastest in the order of work for STATS, GRAD and DX, n for DW
   int kblocks, splits;        // 64-deep blocks of the contraction; DX: parts of it
-  int n_pairs;                // products of operand planes: 1, or 6 for fp32 operands in three bf16 planes
+  int n_pairs;                // products of operand planes: 1, or 3 for fp32 operands in two fp16 planes
   uint32_t pair_a, pair_b;    // their planes, four bits each, the smallest products first
   int a0, b0, bk0;            // first row of A and of B, first k of B (A's k starts at 0)
   int m, n;                   // rows of A and of B that exist from there on
@@ -50,7 +56,6 @@ struct ProductParams {
   float2* partial;            // [tile_n][rows]
   float* target_z;            // [rows], in units of log 2
   const float* lse;
-  float dz_scale;
   int planes;
   // DX and DW
   float* acc;                 // DX: [splits][m][n_pitch]
@@ -61,6 +66,7 @@ struct ProductParams {
   int64_t dw_stride;
   int dw_dtype;
   const float* alpha;         // DW: factor, from the device
+  const uint32_t* tops;       // fp32 operands: bit patterns of the largest magnitudes of x and w
   uint32_t* status;
 };
 
@@ -69,6 +75,12 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The scale of an fp32 operand whose largest magnitude has the bit pattern `top`, and its inverse.
+__device__ __forceinline__ uint32_t operand_exponent(uint32_t top) {
+  return top == 0u || top >= 0x7f800000u ? 127u : min(268u - (top >> 23), 253u);
+}
+__device__ __forceinline__ float operand_scale(uint32_t top) { return __uint_as_float(operand_exponent(top) << 23); }
+__device__ __forceinline__ float operand_unscale(uint32_t top) { return __uint_as_float((254u - operand_exponent(top)) << 23); }
 // The target of a row, or -1 if it does not count, -2 if it is not a class.
 __device__ __forceinline__ int target_of(const void* targets, int bits, int64_t ignore, int classes, int row) {
   const int64_t t = bits == 64 ? reinterpret_cast<const int64_t*>(targets)[row] : (int64_t) reinterpret_cast<const int32_t*>(targets)[row];
@@ -202,7 +214,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
   } else {
     // ---- epilogue: a thread has one row of this block's half of the tile
     const int quarter = warp & 3, row_in_block = quarter * 32 + lane;
-    const float alpha = EPI == DW ? *p.alpha : 0.f;
+    const float alpha = EPI == DW ? *p.alpha * (p.tops ? operand_unscale(p.tops[0]) : 1.f) : 0.f;
+    const float z_scale = p.tops ? p.z_scale * operand_unscale(p.tops[0]) * operand_unscale(p.tops[1]) : p.z_scale;
     int tile = 0;
     bool ok = true;
     int store_buf = 0;
@@ -224,7 +237,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
           float v[32];
           tmem_load_32(acc + c, v);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = v[j] * p.z_scale;
+          for (int j = 0; j < 32; ++j) v[j] = v[j] * z_scale;
           if (target >= c && target < c + 32) {
             float z = 0.f;
 #pragma unroll
@@ -257,10 +270,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
           tmem_load_32(acc + c, *reinterpret_cast<float(*)[32]>(&v[0]));
           tmem_load_32(acc + c + 32, *reinterpret_cast<float(*)[32]>(&v[32]));
 #pragma unroll
-          for (int j = 0; j < 64; ++j) v[j] = counts ? exp2_fast(fmaf(v[j], p.z_scale, -lse2)) : 0.f;
+          for (int j = 0; j < 64; ++j) v[j] = counts ? exp2_fast(fmaf(v[j], z_scale, -lse2)) : 0.f;
           if (counts && target_col >= c && target_col < c + 64) {
 #pragma unroll
             for (int j = 0; j < 64; ++j) v[j] = c + j == target_col ? v[j] - 1.f : v[j];
+          }
+          if (!p.bf16) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j) v[j] *= FP16_DZ_SCALE;
           }
           for (int plane = 0; plane < p.planes; ++plane) {
             // the buffer's previous store has to have read it
@@ -276,14 +293,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
                 if (p.bf16) {
                   const __nv_bfloat162 r = __float22bfloat162_rn(make_float2(lo, hi));
                   q[h] = *reinterpret_cast<const uint32_t*>(&r);
+                } else {
+                  const __half2 r = __float22half2_rn(make_float2(lo, hi));
+                  q[h] = *reinterpret_cast<const uint32_t*>(&r);
                   if (p.planes > 1) {   // what is left for the next plane
-                    const float2 f = __bfloat1622float2(r);
+                    const float2 f = __half22float2(r);
                     lo -= f.x;
                     hi -= f.y;
                   }
-                } else {
-                  const __half2 r = __float22half2_rn(make_float2(lo * p.dz_scale, hi * p.dz_scale));
-                  q[h] = *reinterpret_cast<const uint32_t*>(&r);
                 }
               }
               *reinterpret_cast<uint4*>(out + ((g ^ (row_in_block & 7)) << 4)) = make_uint4(q[0], q[1], q[2], q[3]);
@@ -375,11 +392,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
 
 // ---- around the products ---------------------------------------------------------------------------------------
 
-// Operand rows to 16-bit planes: a copy with an aligned pitch, or fp32 values in three bf16 parts.  With targets: rows that
-// do not count become zeros (what they hold must not reach the sums over rows).
+// The largest magnitude of an fp32 operand; rows that do not count (if targets are given) are left out.
+__global__ void __launch_bounds__(256) largest_kernel(const float* src, int64_t stride, int rows, int cols, const void* targets, int bits,
+                                                      int64_t ignore, int classes, uint32_t* top) {
+  uint32_t m = 0;
+  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
+    if (targets && target_of(targets, bits, ignore, classes, (int)row) < 0) continue;
+    for (int c = blockIdx.x * blockDim.x + threadIdx.x; c < cols; c += gridDim.x * blockDim.x)
+      m = max(m, __float_as_uint(src[row * stride + c]) & 0x7fffffffu);
+  }
+  m = __reduce_max_sync(0xffffffffu, m);
+  if ((threadIdx.x & 31) == 0 && m) atomicMax(top, m);   // (the maximum does not depend on the order)
+}
+// Operand rows to 16-bit planes: a copy with an aligned pitch, or scaled fp32 values in two fp16 parts.  With targets: rows
+// that do not count become zeros (what they hold must not reach the sums over rows).
 template <typename IO>
 __global__ void __launch_bounds__(256) stage_operand_kernel(const IO* src, int64_t stride, int rows, int cols, uint16_t* dst, int pitch,
-                                                            int64_t plane, const void* targets, int bits, int64_t ignore, int classes) {
+                                                            int64_t plane, const void* targets, int bits, int64_t ignore, int classes,
+                                                            const uint32_t* top) {
+  const float scale = sizeof(IO) == 4 ? operand_scale(*top) : 1.f;
   for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
     const bool on = !targets || target_of(targets, bits, ignore, classes, (int)row) >= 0;
     for (int c = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 2; c < pitch; c += (int)(gridDim.x * blockDim.x) * 2) {
@@ -388,14 +419,11 @@ __global__ void __launch_bounds__(256) stage_operand_kernel(const IO* src, int64
       for (int j = 0; j < 2; ++j) v[j] = on && c + j < cols ? src[row * stride + c + j] : from_f32<IO>(0.f);
       uint16_t* const out = dst + row * pitch + c;
       if constexpr (sizeof(IO) == 4) {
-        float2 f = make_float2(v[0], v[1]);
-#pragma unroll
-        for (int part = 0; part < 3; ++part) {
-          const __nv_bfloat162 r = __float22bfloat162_rn(f);
-          *reinterpret_cast<__nv_bfloat162*>(out + part * plane) = r;
-          const float2 g = __bfloat1622float2(r);
-          f = make_float2(f.x - g.x, f.y - g.y);
-        }
+        const float2 f = make_float2(v[0] * scale, v[1] * scale);
+        const __half2 hi = __float22half2_rn(f);
+        const float2 g = __half22float2(hi);
+        *reinterpret_cast<__half2*>(out) = hi;
+        *reinterpret_cast<__half2*>(out + plane) = __float22half2_rn(make_float2(f.x - g.x, f.y - g.y));
       } else {
         *reinterpret_cast<IO*>(out) = v[0];
         *reinterpret_cast<IO*>(out + 1) = v[1];
@@ -471,8 +499,8 @@ __global__ void __launch_bounds__(1024) mean_kernel(const float* row_loss, int r
 template <typename IO>
 __global__ void __launch_bounds__(256) join_dx_kernel(const float* acc, int splits, int64_t split_stride, int pitch, int rows, int cols,
                                                       const float* alpha, const void* targets, int bits, int64_t ignore, int classes, IO* dx,
-                                                      int64_t stride, const uint32_t* status) {
-  const float a = (*status & VL_TIMEOUT) ? __uint_as_float(0x7fc00000u) : *alpha;
+                                                      int64_t stride, const uint32_t* status, const uint32_t* tops) {
+  const float a = (*status & VL_TIMEOUT) ? __uint_as_float(0x7fc00000u) : *alpha * (tops ? operand_unscale(tops[1]) : 1.f);
   for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
     const bool on = target_of(targets, bits, ignore, classes, (int)row) >= 0;
     for (int c = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 4; c < cols; c += (int)(gridDim.x * blockDim.x) * 4) {
@@ -539,7 +567,7 @@ Layout layout_of(const snn_vocab_loss_args* a, bool backward, int pairs) {
   Layout l{};
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes); return o; };
-  const int planes = a->dtype == SNN_DTYPE_FP32 ? 3 : 1;
+  const int planes = a->dtype == SNN_DTYPE_FP32 ? 2 : 1;
   auto operand = [&](const void* p, int64_t stride, int rows, int cols, bool always) {
     Operand o{};
     o.planes = planes;
@@ -590,7 +618,7 @@ snn_status check(const snn_vocab_loss_args* a) {
   if (!a->w || (a->rows > 0 && (!a->x || !a->targets))) return SNN_ERR_INVALID_ARG;
   return SNN_OK;
 }
-bool is_bf16(int dtype) { return dtype != SNN_DTYPE_FP16; }   // fp32: bf16 planes
+bool is_bf16(int dtype) { return dtype == SNN_DTYPE_BF16; }   // (fp32: fp16 planes)
 
 template <int EPI, bool A_MN, bool B_MN> snn_status launch_product(const ProductParams& p, int pairs, cudaStream_t stream) {
   const auto kernel = product_kernel<EPI, A_MN, B_MN>;
@@ -609,6 +637,7 @@ struct Call {
   int pairs;
   uint32_t* status() const { return (uint32_t*)(ws + l.status); }
   float* alpha() const { return (float*)(ws + l.alpha); }
+  uint32_t* tops() const { return a->dtype == SNN_DTYPE_FP32 ? (uint32_t*)(ws + l.status + 64) : nullptr; }
 
   snn_status begin(bool backward, void* s) {
     stream = (cudaStream_t)s;
@@ -618,17 +647,24 @@ struct Call {
     if (!a->workspace || (uintptr_t)a->workspace % 256 != 0) return SNN_ERR_INVALID_ARG;
     if (a->workspace_bytes < l.total) return SNN_ERR_WORKSPACE_TOO_SMALL;
     ws = (char*)a->workspace;
-    return cudaMemsetAsync(ws + l.status, 0, 4, stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+    return cudaMemsetAsync(ws + l.status, 0, 128, stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
   }
-  snn_status stage(const Operand& o, const void* src, int64_t stride, int rows, int cols, bool mask) const {
+  // which: 0 for x, 1 for w
+  snn_status stage(int which, const Operand& o, const void* src, int64_t stride, int rows, int cols) const {
     if (!o.staged) return SNN_OK;
+    const bool mask = which == 0;
+    uint32_t* const top = tops() ? tops() + which : nullptr;
     uint16_t* const dst = (uint16_t*)(ws + o.offset);
     const void* const targets = mask ? a->targets : nullptr;
     const dim3 grid((unsigned)std::min<int64_t>(ceil_div(o.pitch, 512), 1024), (unsigned)std::min(rows, 16384));
+    if (top) {   // a few thousand blocks at most: each ends with an atomic per warp
+      const unsigned gx = (unsigned)std::min<int64_t>(ceil_div(cols, 256), 32), gy = (unsigned)std::min<int64_t>(rows, std::max(1u, 2048u / gx));
+      largest_kernel<<<dim3(gx, gy), 256, 0, stream>>>((const float*)src, stride, rows, cols, targets, a->target_bits, a->ignore_index, a->classes, top);
+    }
     auto go = [&](auto io) {
       using IO = decltype(io);
       stage_operand_kernel<IO><<<grid, 256, 0, stream>>>((const IO*)src, stride, rows, cols, dst, (int)o.pitch, o.plane, targets, a->target_bits,
-                                                         a->ignore_index, a->classes);
+                                                         a->ignore_index, a->classes, top);
     };
     if (a->dtype == SNN_DTYPE_FP32) go(float());
     else go(__half());   // 16 bits are copied, whatever they mean
@@ -643,17 +679,14 @@ struct Call {
     p.bf16 = is_bf16(a->dtype);
     p.splits = 1;
     p.planes = l.x.planes;
-    p.n_pairs = p.planes == 3 ? 6 : 1;
+    // fp32: (plane of a, plane of b) = (1, 0), (0, 1), (0, 0), plane 0 the leading part: the small products first
+    p.n_pairs = p.planes == 2 ? 3 : 1;
+    p.pair_a = p.planes == 2 ? 0x001u : 0u;
+    p.pair_b = p.planes == 2 ? 0x010u : 0u;
+    p.tops = tops();
     p.targets = a->targets; p.target_bits = a->target_bits; p.ignore_index = a->ignore_index; p.classes = a->classes;
     p.z_scale = a->scale * LOG2E;
     p.status = status();
-    p.dz_scale = a->dtype == SNN_DTYPE_FP16 ? FP16_DZ_SCALE : 1.f;
-    if (p.planes == 3) {
-      // (plane of a, plane of b), 0 the leading part: 2 0, 0 2, 1 1, 1 0, 0 1, 0 0
-      const int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
-      p.pair_a = p.pair_b = 0;
-      for (int i = 0; i < 6; ++i) p.pair_a |= (uint32_t)pa[i] << (4 * i), p.pair_b |= (uint32_t)pb[i] << (4 * i);
-    }
     return p;
   }
 };
@@ -682,8 +715,8 @@ extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void*
   if (a->rows == 0) return cudaMemsetAsync(a->loss, 0, 4, c.stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
   const bool by_class = a->w_layout == SNN_W_BY_CLASS;
   const int w_rows = by_class ? a->classes : a->dim, w_cols = by_class ? a->dim : a->classes;
-  VL_TRY(c.stage(c.l.x, a->x, a->x_stride, a->rows, a->dim, false));
-  VL_TRY(c.stage(c.l.w, a->w, a->w_stride, w_rows, w_cols, false));
+  VL_TRY(c.stage(0, c.l.x, a->x, a->x_stride, a->rows, a->dim));
+  VL_TRY(c.stage(1, c.l.w, a->w, a->w_stride, w_rows, w_cols));
   ProductParams p = c.base();
   if (!c.map(&p.a, c.l.x, a->x, a->rows, a->dim, false) || !c.map(&p.b, c.l.w, a->w, w_rows, w_cols, !by_class)) return SNN_ERR_CUDA;
   p.tiles_m = ceil_div(a->rows, UM_TILE);
@@ -714,11 +747,11 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     return cudaMemset2DAsync(a->dw, a->dw_stride * size, 0, w_cols * size, w_rows, c.stream) == cudaSuccess ? SNN_OK
                                                                                                          : (cudaGetLastError(), SNN_ERR_CUDA);
   const Layout& l = c.l;
-  VL_TRY(c.stage(l.x, a->x, a->x_stride, a->rows, a->dim, true));
-  VL_TRY(c.stage(l.w, a->w, a->w_stride, w_rows, w_cols, false));
+  VL_TRY(c.stage(0, l.x, a->x, a->x_stride, a->rows, a->dim));
+  VL_TRY(c.stage(1, l.w, a->w, a->w_stride, w_rows, w_cols));
   const ProductParams base = c.base();
   mean_kernel<<<1, 1024, 0, c.stream>>>(nullptr, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, nullptr, c.alpha(),
-                                        a->dloss * a->scale / base.dz_scale, a->dloss_device);
+                                        a->dloss * a->scale / (base.bf16 ? 1.f : FP16_DZ_SCALE), a->dloss_device);
   CUtensorMap x_k, x_mn, w_z, w_dx, dz_k, dz_mn;   // as operands that are contiguous along the contraction, and across it
   bool ok = c.map(&x_k, l.x, a->x, a->rows, a->dim, false) && c.map(&x_mn, l.x, a->x, a->rows, a->dim, true);
   ok = ok && c.map(&w_z, l.w, a->w, w_rows, w_cols, !by_class) && c.map(&w_dx, l.w, a->w, w_rows, w_cols, by_class);
@@ -763,7 +796,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
   auto join = [&](auto io) {
     using IO = decltype(io);
     join_dx_kernel<IO><<<grid, 256, 0, c.stream>>>((const float*)(c.ws + l.acc), splits, l.acc_split, l.acc_pitch, a->rows, a->dim, c.alpha(),
-                                                   a->targets, a->target_bits, a->ignore_index, a->classes, (IO*)a->dx, a->dx_stride, c.status());
+                                                   a->targets, a->target_bits, a->ignore_index, a->classes, (IO*)a->dx, a->dx_stride, c.status(), c.tops());
   };
   if (a->dtype == SNN_DTYPE_FP32) join(float());
   else if (a->dtype == SNN_DTYPE_BF16) join(__nv_bfloat16());

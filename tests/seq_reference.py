@@ -128,18 +128,19 @@ def vocab_loss(x, w, targets, scale, ignore, dtype, dloss=1.0):
     """loss, row_loss, lse, dx, dw and their bounds, for float64 x [n][D], w [D][V].
 
     Bounds.  A tensor-core instruction adds 16 products to a fp32 accumulator; it cuts or rounds, and two units of 2^-23 of
-    the sum of magnitudes cover it.  fp32 operands take six instructions where 16-bit ones take one, and the products left
-    out (mid x lo, lo x mid, lo x lo) are below 2^-23 of the magnitudes.  So a sum of K products is off by
-    (2 ceil(K / 16) P + 4) 2^-23 of the sum of magnitudes, P = 1 or 6.  exp2 is off by 2^-22, its argument by a rounding of
+    the sum of magnitudes cover it.  fp32 operands, in two fp16 parts, take three instructions where 16-bit ones take one;
+    each operand is off by 2^-22 of its value (2^-11 of what the first part, off by 2^-11, leaves) and the product left out
+    is below 2^-22: six units of 2^-23 in all.  So a sum of K products is off by (2 ceil(K / 16) P + 4) 2^-23 of the sum of
+    magnitudes, P = 1, or (2 ceil(K / 16) P + 10) 2^-23, P = 3.  exp2 is off by 2^-22, its argument by a rounding of
     2^-24 of each of its two parts, and what is below 2^-126, the smallest normal number, counts as zero; a row's sum of exponentials has 32 + 8 + V / 2048 + 8 roundings.  dz is rounded to its
-    type (fp32: three parts, 2^-24) before it is multiplied.
+    type (fp32: two fp16 parts, 2^-22) before it is multiplied.
     """
     import torch
-    P = 6 if dtype == "fp32" else 1
-    unit, half = 2.0 ** -23, HALF_STEP[dtype]
+    P, more = (3, 10) if dtype == "fp32" else (1, 4)
+    unit, half = 2.0 ** -23, 2.0 ** -22 if dtype == "fp32" else HALF_STEP[dtype]
 
     def steps(K):
-        return (2 * -(-K // 16) * P + 4) * unit
+        return (2 * -(-K // 16) * P + more) * unit
 
     n, D = x.shape
     V = w.shape[1]
@@ -167,7 +168,7 @@ def vocab_loss(x, w, targets, scale, ignore, dtype, dloss=1.0):
     dz.scatter_add_(1, at, torch.full_like(at, -1.0, dtype=dz.dtype))
     ep = p * (ez + lse_tol[:, None] + 4 * unit * (1 + z.abs() + lse.abs()[:, None]))
     ep.scatter_add_(1, at, torch.full_like(at, unit, dtype=dz.dtype))
-    ep = ep + 2.0 ** -126 + half * dz.abs() + (2.0 ** -25 / 16384 if dtype == "fp16" else 0.0)
+    ep = ep + 2.0 ** -126 + half * dz.abs() + (0.0 if dtype == "bf16" else 2.0 ** -25 / 16384)
     dz, ep = torch.where(on, dz, 0.0), torch.where(on, ep, 0.0)
     k = abs(scale * dloss) / count
     out["dx"] = scale * dloss / count * (dz @ w.t())

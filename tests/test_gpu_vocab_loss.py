@@ -95,6 +95,17 @@ def test_loss_long_contraction_in_fp32():
     check(*inputs(40, 2000, 3001, "fp32", 6), "fp32")
 
 
+def test_loss_fp32_of_any_magnitude():
+    """fp32 operands are scaled as a whole: large ones, small ones, zeros, and padding that is no number."""
+    x, w, t = inputs(40, 64, 300, "fp32", 12)
+    check(x * 1e12, w * 1e-12, t, "fp32")
+    check(x * 1e-30, w * 1e30, t, "fp32")
+    check(torch.zeros_like(x), w, t, "fp32")
+    check(x, torch.zeros_like(w), t, "fp32")
+    x[t < 0] = float("inf")
+    check(x, w, t, "fp32")
+
+
 def test_loss_rows_that_do_not_count():
     o = ops()
     x, w, t = inputs(50, 64, 300, "bf16", 7, ignored=0.0)

@@ -65,6 +65,7 @@ struct ProductParams {
   void* dw;
   int64_t dw_stride;
   int dw_dtype;
+  bool dw_vector;             // rows of dw are aligned to 16 bytes
   const float* alpha;         // DW: factor, from the device
   const uint32_t* tops;       // fp32 operands: bit patterns of the largest magnitudes of x and w
   uint32_t* status;
@@ -102,7 +103,7 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Barrier
     if ((i & 63u) == 63u && *reinterpret_cast<volatile uint32_t*>(&s.gave_up)) return false;
   }
   *reinterpret_cast<volatile uint32_t*>(&s.gave_up) = 1u;
-  atomicOr(status, VL_TIMEOUT);
+  if (status) atomicOr(status, VL_TIMEOUT);
   return false;
 }
 
@@ -223,7 +224,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
       const Unit w = unit_of<EPI>(p, u);
       const int buf = tile & 1;
       ok = __all_sync(0xffffffffu, wait_for(&s.acc_full[buf], (uint32_t)(tile / 2) & 1u, s, p.status));
-      if (!ok) break;
+      if (!ok) {
+        if (EPI == STATS) {   // the rows' losses become NaN
+          const float nan = __uint_as_float(0x7fc00000u);
+          for (; u < units; u += n_pairs_sm) {
+            const Unit left = unit_of<EPI>(p, u);
+            const int row = left.m * UM_TILE + (int)rank * UM_HALF + row_in_block;
+            if (row < p.m) p.partial[(int64_t)left.n * p.m + row] = make_float2(nan, nan);
+          }
+        }
+        break;
+      }
       tcgen05_after_sync();
       const uint32_t acc = tmem + (uint32_t)buf * UM_TILE + ((uint32_t)(32 * quarter) << 16);
       const int block_row0 = w.m * UM_TILE + (int)rank * UM_HALF;
@@ -337,40 +348,51 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
         for (int c = 0; c < cols; c += 32) {
           float v[32];
           tmem_load_32(acc + c, v);
-          if (!row_on) continue;
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] *= alpha;
+          if (!p.dw_vector || cols - c < 32) {
+            // odd strides, the last columns: through shared memory, so that a warp stores along a row
+            float* const mine = reinterpret_cast<float*>(s_store) + quarter * (32 * 33);
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < 32; ++j) mine[lane * 33 + j] = v[j];
+            __syncwarp();
+            const int first = block_row0 + quarter * 32, n_rows = min(p.m - first, 32);
+            if (c + lane < cols) {
+              const int64_t at = (int64_t)first * p.dw_stride + col0 + c + lane;
+#pragma unroll 4
+              for (int r = 0; r < n_rows; ++r) {
+                const float f = mine[r * 33 + lane];
+                const int64_t to = at + r * p.dw_stride;
+                if (p.dw_dtype == SNN_DTYPE_FP32) ((float*)p.dw)[to] = f;
+                else if (p.dw_dtype == SNN_DTYPE_BF16) ((__nv_bfloat16*)p.dw)[to] = __float2bfloat16_rn(f);
+                else ((__half*)p.dw)[to] = __float2half_rn(f);
+              }
+            }
+            continue;
+          }
+          if (!row_on) continue;
           const int64_t at = (int64_t)row * p.dw_stride + col0 + c;
           if (p.dw_dtype == SNN_DTYPE_FP32) {
             float* const out = (float*)p.dw + at;
-            if (cols - c >= 32 && ((uintptr_t)out & 15) == 0) {
 #pragma unroll
-              for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(out + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (c + j < cols) out[j] = v[j];
-            }
+            for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(out + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
           } else {
             uint16_t* const out = (uint16_t*)p.dw + at;
-            uint32_t q[16];
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              if (p.dw_dtype == SNN_DTYPE_BF16) {
-                const __nv_bfloat162 r = __float22bfloat162_rn(make_float2(v[2 * j], v[2 * j + 1]));
-                q[j] = *reinterpret_cast<const uint32_t*>(&r);
-              } else {
-                const __half2 r = __float22half2_rn(make_float2(v[2 * j], v[2 * j + 1]));
-                q[j] = *reinterpret_cast<const uint32_t*>(&r);
+            for (int j = 0; j < 32; j += 8) {
+              uint32_t q[4];
+#pragma unroll
+              for (int h = 0; h < 4; ++h) {
+                if (p.dw_dtype == SNN_DTYPE_BF16) {
+                  const __nv_bfloat162 r = __float22bfloat162_rn(make_float2(v[j + 2 * h], v[j + 2 * h + 1]));
+                  q[h] = *reinterpret_cast<const uint32_t*>(&r);
+                } else {
+                  const __half2 r = __float22half2_rn(make_float2(v[j + 2 * h], v[j + 2 * h + 1]));
+                  q[h] = *reinterpret_cast<const uint32_t*>(&r);
+                }
               }
-            }
-            if (cols - c >= 32 && ((uintptr_t)out & 15) == 0) {
-#pragma unroll
-              for (int j = 0; j < 16; j += 4) *reinterpret_cast<uint4*>(out + 2 * j) = make_uint4(q[j], q[j + 1], q[j + 2], q[j + 3]);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 32; ++j)
-                if (c + j < cols) out[j] = (uint16_t)(q[j / 2] >> (16 * (j & 1)));
+              *reinterpret_cast<uint4*>(out + j) = make_uint4(q[0], q[1], q[2], q[3]);
             }
           }
         }
@@ -392,41 +414,77 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
 
 // ---- around the products ---------------------------------------------------------------------------------------
 
-// The largest magnitude of an fp32 operand; rows that do not count (if targets are given) are left out.
-__global__ void __launch_bounds__(256) largest_kernel(const float* src, int64_t stride, int rows, int cols, const void* targets, int bits,
-                                                      int64_t ignore, int classes, uint32_t* top) {
+// An operand on its way to 16-bit planes: a copy with an aligned pitch, or scaled fp32 values in two fp16 parts.  With
+// `mask`, rows that do not count become zeros (what they hold must not reach the sums over rows).
+struct StageJob {
+  const void* src;
+  int64_t stride;
+  int rows, cols;
+  uint16_t* dst;
+  int64_t pitch, plane;
+  bool mask;
+};
+struct StageParams {
+  StageJob job[2];      // x and w; rows = 0 if there is nothing to do.  blockIdx.y selects one
+  const void* targets;
+  int bits;
+  int64_t ignore;
+  int classes;
+  uint32_t* tops;       // fp32: bit patterns of the largest magnitudes
+};
+constexpr int STAGE_COLS = 1024;   // columns of a row that a block takes at a time, four per thread
+
+// The largest magnitudes of fp32 operands.  (The maximum does not depend on the order of the atomics.)
+__global__ void __launch_bounds__(256) largest_kernel(const __grid_constant__ StageParams p) {
+  __shared__ uint32_t s_top;
+  const StageJob& j = p.job[blockIdx.y];
+  const int parts = (j.cols + STAGE_COLS - 1) / STAGE_COLS;
+  if (threadIdx.x == 0) s_top = 0;
+  __syncthreads();
   uint32_t m = 0;
-  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-    if (targets && target_of(targets, bits, ignore, classes, (int)row) < 0) continue;
-    for (int c = blockIdx.x * blockDim.x + threadIdx.x; c < cols; c += gridDim.x * blockDim.x)
-      m = max(m, __float_as_uint(src[row * stride + c]) & 0x7fffffffu);
+  for (int64_t i = blockIdx.x; i < (int64_t)j.rows * parts; i += gridDim.x) {
+    const int row = (int)(i / parts), c = (int)(i % parts) * STAGE_COLS + threadIdx.x;
+    if (j.mask && target_of(p.targets, p.bits, p.ignore, p.classes, row) < 0) continue;
+    const float* const src = (const float*)j.src + row * j.stride;
+    float v[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = src[min(c + 256 * q, j.cols - 1)];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) m = max(m, __float_as_uint(v[q]) & 0x7fffffffu);
   }
   m = __reduce_max_sync(0xffffffffu, m);
-  if ((threadIdx.x & 31) == 0 && m) atomicMax(top, m);   // (the maximum does not depend on the order)
+  if ((threadIdx.x & 31) == 0 && m) atomicMax(&s_top, m);
+  __syncthreads();
+  if (threadIdx.x == 0 && s_top) atomicMax(p.tops + blockIdx.y, s_top);
 }
-// Operand rows to 16-bit planes: a copy with an aligned pitch, or scaled fp32 values in two fp16 parts.  With targets: rows
-// that do not count become zeros (what they hold must not reach the sums over rows).
-template <typename IO>
-__global__ void __launch_bounds__(256) stage_operand_kernel(const IO* src, int64_t stride, int rows, int cols, uint16_t* dst, int pitch,
-                                                            int64_t plane, const void* targets, int bits, int64_t ignore, int classes,
-                                                            const uint32_t* top) {
-  const float scale = sizeof(IO) == 4 ? operand_scale(*top) : 1.f;
-  for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
-    const bool on = !targets || target_of(targets, bits, ignore, classes, (int)row) >= 0;
-    for (int c = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 2; c < pitch; c += (int)(gridDim.x * blockDim.x) * 2) {
-      IO v[2];
+template <typename IO> __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ StageParams p) {
+  const StageJob& j = p.job[blockIdx.y];
+  const int parts = (int)((j.pitch + STAGE_COLS - 1) / STAGE_COLS);
+  const float scale = sizeof(IO) == 4 && j.rows ? operand_scale(p.tops[blockIdx.y]) : 1.f;
+  for (int64_t i = blockIdx.x; i < (int64_t)j.rows * parts; i += gridDim.x) {
+    const int row = (int)(i / parts), c0 = (int)(i % parts) * STAGE_COLS + 2 * threadIdx.x;
+    const bool on = !j.mask || target_of(p.targets, p.bits, p.ignore, p.classes, row) >= 0;
+    const IO* const src = (const IO*)j.src + row * j.stride;
+    uint16_t* const dst = j.dst + row * j.pitch;
+    IO v[2][2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) v[j] = on && c + j < cols ? src[row * stride + c + j] : from_f32<IO>(0.f);
-      uint16_t* const out = dst + row * pitch + c;
+    for (int q = 0; q < 4; ++q) v[q / 2][q % 2] = src[min(c0 + 512 * (q / 2) + q % 2, j.cols - 1)];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int c = c0 + 512 * q;
+      if (c >= j.pitch) continue;
       if constexpr (sizeof(IO) == 4) {
-        const float2 f = make_float2(v[0] * scale, v[1] * scale);
+        const float2 f = make_float2(on && c < j.cols ? v[q][0] * scale : 0.f, on && c + 1 < j.cols ? v[q][1] * scale : 0.f);
         const __half2 hi = __float22half2_rn(f);
         const float2 g = __half22float2(hi);
-        *reinterpret_cast<__half2*>(out) = hi;
-        *reinterpret_cast<__half2*>(out + plane) = __float22half2_rn(make_float2(f.x - g.x, f.y - g.y));
+        *reinterpret_cast<__half2*>(dst + c) = hi;
+        *reinterpret_cast<__half2*>(dst + j.plane + c) = __float22half2_rn(make_float2(f.x - g.x, f.y - g.y));
       } else {
-        *reinterpret_cast<IO*>(out) = v[0];
-        *reinterpret_cast<IO*>(out + 1) = v[1];
+        const IO zero = from_f32<IO>(0.f);
+        __half2 r;
+        r.x = on && c < j.cols ? v[q][0] : zero;
+        r.y = on && c + 1 < j.cols ? v[q][1] : zero;
+        *reinterpret_cast<__half2*>(dst + c) = r;
       }
     }
   }
@@ -444,37 +502,51 @@ __device__ __forceinline__ double block_sum(double v, double* warp_sums) {
   return t;
 }
 
-// The tiles' (maximum, sum) of a row joined: log-sum-exp and loss of the row.  32 rows per block, 8 threads per row.
-__global__ void __launch_bounds__(256) row_loss_kernel(const float2* partial, int tiles, const float* target_z, int rows, const void* targets,
-                                                       int bits, int64_t ignore, int classes, float* lse, float* row_loss, float* row_out,
-                                                       const uint32_t* status) {
-  __shared__ float2 s_part[8][32];
-  const int row = blockIdx.x * 32 + threadIdx.x % 32, part = threadIdx.x / 32;
-  float top = -INFINITY, sum = 0.f;
-  if (row < rows) {
-    for (int t = part; t < tiles; t += 8) {
-      const float2 v = partial[(int64_t)t * rows + row];
-      const float m = fmaxf(top, v.x), at = m == -INFINITY ? 0.f : m;
-      sum = sum * exp2f(top - at) + v.y * exp2f(v.x - at);
-      top = m;
-    }
-  }
-  s_part[part][threadIdx.x % 32] = make_float2(top, sum);
+__device__ __forceinline__ float2 join_sums(float2 a, float2 b) {   // (maximum, sum of exponentials)
+  const float m = a.x != a.x || b.x != b.x ? __uint_as_float(0x7fc00000u) : fmaxf(a.x, b.x), at = m == -INFINITY ? 0.f : m;
+  return make_float2(m, a.y * exp2f(a.x - at) + b.y * exp2f(b.x - at));
+}
+// The tiles' (maximum, sum) of a row joined: log-sum-exp and loss of the row.  32 rows per block, 32 threads per row.  If
+// one block has all rows it takes the mean as well (loss != NULL).
+__global__ void __launch_bounds__(1024) row_loss_kernel(const float2* partial, int tiles, const float* target_z, int rows, const void* targets,
+                                                        int bits, int64_t ignore, int classes, float* lse, float* row_loss, float* row_out,
+                                                        float* loss) {
+  __shared__ float2 s_part[32][33];
+  const int in_block = threadIdx.x % 32, part = threadIdx.x / 32, row = blockIdx.x * 32 + in_block;
+  float2 v = make_float2(-INFINITY, 0.f);
+  if (row < rows)
+    for (int t = part; t < tiles; t += 32) v = join_sums(v, partial[(int64_t)t * rows + row]);
+  s_part[part][in_block] = v;
   __syncthreads();
-  if (part == 0 && row < rows) {
-    for (int q = 1; q < 8; ++q) {
-      const float2 v = s_part[q][threadIdx.x];
-      const float m = fmaxf(top, v.x), at = m == -INFINITY ? 0.f : m;
-      sum = sum * exp2f(top - at) + v.y * exp2f(v.x - at);
-      top = m;
-    }
+  // warp `part` joins the 32 parts of row `part` of the block
+  v = s_part[in_block][part];
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2)
+    v = join_sums(v, make_float2(__shfl_down_sync(0xffffffffu, v.x, o), __shfl_down_sync(0xffffffffu, v.y, o)));
+  __syncthreads();
+  if (in_block == 0) s_part[0][part] = v;
+  __syncthreads();
+  if (part != 0) return;
+  float out = 0.f, count = 0.f;
+  if (row < rows) {
+    v = s_part[0][in_block];
     const int target = target_of(targets, bits, ignore, classes, row);
-    float l = (top + log2f(sum)) * LN2, loss = l - (target >= 0 ? target_z[row] * LN2 : 0.f);
-    if (target < 0) l = 0.f, loss = target == -1 ? 0.f : __uint_as_float(0x7fc00000u);
-    if (*status & VL_TIMEOUT) loss = l = __uint_as_float(0x7fc00000u);
+    float l = (v.x + log2f(v.y)) * LN2;
+    out = l - (target >= 0 ? target_z[row] * LN2 : 0.f);
+    if (target < 0) l = 0.f, out = target == -1 ? 0.f : __uint_as_float(0x7fc00000u);
+    count = target >= 0;
     lse[row] = l;
-    row_loss[row] = loss;
-    if (row_out) row_out[row] = loss;
+    row_loss[row] = out;
+    if (row_out) row_out[row] = out;
+  }
+  if (loss) {
+    double sum = out;
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) {
+      sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      count += __shfl_xor_sync(0xffffffffu, count, o);
+    }
+    if (in_block == 0) *loss = (float)(sum / fmax((double)count, 1.));
   }
 }
 
@@ -515,6 +587,175 @@ __global__ void __launch_bounds__(256) join_dx_kernel(const float* acc, int spli
         if (c + j < cols) dx[row * stride + c + j] = from_f32<IO>(on ? v[j] * a : 0.f);
     }
   }
+}
+
+// ---- a few rows (scoring the last position of a sequence) ----------------------------------------------------------
+// Up to FEW_ROWS rows the forward pass is one pass over w at HBM speed: plain fp32 arithmetic on what is loaded, every
+// block a share of the classes.  (256 x 256 tiles would be nearly empty, and a wave and a half of them leaves SMs idle: 1 x
+// 1024 x 32000 bf16 took 33 us with both kernels behind it.)
+constexpr int FEW_ROWS = 4, FEW_BLOCKS = 148 * 4, FEW_WARPS = 8;
+constexpr int FEW_VALUES = 7168;      // rows (as many as a kernel takes) x dim, as fp32 in shared memory
+
+struct FewParams {
+  const void *x, *w, *targets;
+  int64_t x_stride, w_stride, ignore;
+  int rows, dim, classes, bits;
+  float z_scale;
+  float2* partial;      // [gridDim.x][rows]
+  float* target_z;
+};
+template <typename IO, int R> __device__ __forceinline__ void few_targets(const FewParams& p, int (&target)[R]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r) target[r] = r < p.rows ? target_of(p.targets, p.bits, p.ignore, p.classes, r) : -1;
+}
+// The block's partial sums: those of its warps joined.
+template <int R> __device__ __forceinline__ void few_finish(const FewParams& p, const float2 (&v)[R], float2 (*s_part)[R]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  __syncthreads();
+  if (lane == 0)
+#pragma unroll
+    for (int r = 0; r < R; ++r) s_part[warp][r] = v[r];
+  __syncthreads();
+  if (threadIdx.x < p.rows) {
+    float2 t = s_part[0][threadIdx.x];
+    for (int q = 1; q < FEW_WARPS; ++q) t = join_sums(t, s_part[q][threadIdx.x]);
+    p.partial[(int64_t)blockIdx.x * p.rows + threadIdx.x] = t;
+  }
+}
+template <typename IO> struct EightValues;
+template <> struct EightValues<float> {
+  float4 a, b;
+  __device__ void get(float (&v)[8]) const { v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w; }
+};
+template <typename IO> struct alignas(16) EightHalfValues {
+  typename Pair<IO>::raw q[4];
+  __device__ void get(float (&v)[8]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = to_f32(q[i]);
+      v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    }
+  }
+};
+template <> struct EightValues<__nv_bfloat16> : EightHalfValues<__nv_bfloat16> {};
+template <> struct EightValues<__half> : EightHalfValues<__half> {};
+
+// w by class: a warp takes a run of classes, four at a time; its lanes share the features.  VEC: eight features per load
+// (dim a multiple of 8, rows aligned to 16 bytes).
+template <typename IO, int R, bool VEC> __global__ void __launch_bounds__(32 * FEW_WARPS) few_rows_by_class_kernel(const FewParams p) {
+  extern __shared__ __align__(16) float s_x[];   // VEC: [R][2][dim / 8] float4, the halves of eight features apart; else [R][dim]
+  __shared__ float2 s_part[FEW_WARPS][R];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int i = threadIdx.x; i < R * p.dim; i += blockDim.x) {
+    const int r = i / p.dim, d = i % p.dim;
+    const float v = r < p.rows ? to_f32(((const IO*)p.x)[r * p.x_stride + d]) : 0.f;
+    s_x[VEC ? r * p.dim + (d / 4 % 2) * (p.dim / 2) + d / 8 * 4 + d % 4 : i] = v;
+  }
+  __syncthreads();
+  int target[R];
+  few_targets<IO, R>(p, target);
+  float2 sum[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) sum[r] = make_float2(-INFINITY, 0.f);
+  const int64_t n = (int64_t)gridDim.x * FEW_WARPS, id = (int64_t)blockIdx.x * FEW_WARPS + warp;
+  const int last = (int)(p.classes * (id + 1) / n);
+  for (int v0 = (int)(p.classes * id / n); v0 < last; v0 += 4) {
+    const IO* row[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) row[j] = (const IO*)p.w + min(v0 + j, last - 1) * p.w_stride;
+    float acc[4][R] = {};
+    if (VEC) {
+#pragma unroll 2
+      for (int d = lane * 8; d < p.dim; d += 256) {
+        EightValues<IO> q[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = *reinterpret_cast<const EightValues<IO>*>(row[j] + d);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float4 xa = *reinterpret_cast<const float4*>(s_x + r * p.dim + d / 2);
+          const float4 xb = *reinterpret_cast<const float4*>(s_x + r * p.dim + p.dim / 2 + d / 2);
+          const float xs[8] = {xa.x, xa.y, xa.z, xa.w, xb.x, xb.y, xb.z, xb.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            float f[8];
+            q[j].get(f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) acc[j][r] = fmaf(f[k], xs[k], acc[j][r]);
+          }
+        }
+      }
+    } else {
+#pragma unroll 4
+      for (int d = lane; d < p.dim; d += 32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float f = to_f32(row[j][d]);
+#pragma unroll
+          for (int r = 0; r < R; ++r) acc[j][r] = fmaf(f, s_x[r * p.dim + d], acc[j][r]);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (v0 + j >= last) break;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float z = acc[j][r];
+#pragma unroll
+        for (int o = 16; o > 0; o /= 2) z += __shfl_xor_sync(0xffffffffu, z, o);
+        z *= p.z_scale;
+        if (lane == 0 && target[r] == v0 + j) p.target_z[r] = z;
+        sum[r] = join_sums(sum[r], make_float2(z, z == -INFINITY ? 0.f : 1.f));
+      }
+    }
+  }
+  few_finish<R>(p, sum, s_part);
+}
+// w by feature: a block takes 128 classes, four per lane; its warps share the features.
+template <typename IO, int R> __global__ void __launch_bounds__(32 * FEW_WARPS) few_rows_by_feature_kernel(const FewParams p) {
+  extern __shared__ __align__(16) float s_x[];   // [R][dim]
+  __shared__ float s_acc[FEW_WARPS][R][128];
+  __shared__ float2 s_part[FEW_WARPS][R];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  for (int i = threadIdx.x; i < R * p.dim; i += blockDim.x) s_x[i] = i / p.dim < p.rows ? to_f32(((const IO*)p.x)[i / p.dim * p.x_stride + i % p.dim]) : 0.f;
+  __syncthreads();
+  int target[R];
+  few_targets<IO, R>(p, target);
+  const int v0 = blockIdx.x * 128;
+  float acc[4][R] = {};
+#pragma unroll 8
+  for (int d = warp; d < p.dim; d += FEW_WARPS) {
+    const IO* const row = (const IO*)p.w + d * p.w_stride;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float f = to_f32(row[min(v0 + 32 * j + lane, p.classes - 1)]);
+#pragma unroll
+      for (int r = 0; r < R; ++r) acc[j][r] = fmaf(f, s_x[r * p.dim + d], acc[j][r]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int r = 0; r < R; ++r) s_acc[warp][r][32 * j + lane] = acc[j][r];
+  __syncthreads();
+  float2 sum[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    sum[r] = make_float2(-INFINITY, 0.f);
+    const int c = warp * 16 + lane % 16, v = v0 + c;   // 16 classes per warp
+    if (lane < 16 && v < p.classes) {
+      float z = 0.f;
+#pragma unroll
+      for (int q = 0; q < FEW_WARPS; ++q) z += s_acc[q][r][c];
+      z *= p.z_scale;
+      if (target[r] == v) p.target_z[r] = z;
+      sum[r] = make_float2(z, z == -INFINITY ? 0.f : 1.f);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2)
+      sum[r] = join_sums(sum[r], make_float2(__shfl_xor_sync(0xffffffffu, sum[r].x, o), __shfl_xor_sync(0xffffffffu, sum[r].y, o)));
+  }
+  few_finish<R>(p, sum, s_part);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
@@ -563,6 +804,11 @@ int dx_splits(int tiles, int kblocks, int pairs) {
   }
   return best;
 }
+int few_kernel_rows(int rows) { return rows <= 2 ? rows : 4; }
+bool few_rows(const snn_vocab_loss_args* a) { return a->rows > 0 && a->rows <= FEW_ROWS && (int64_t)few_kernel_rows(a->rows) * a->dim <= FEW_VALUES; }
+int few_blocks(const snn_vocab_loss_args* a) {
+  return a->w_layout == SNN_W_BY_CLASS ? std::min(FEW_BLOCKS, ceil_div(a->classes, 4 * FEW_WARPS)) : ceil_div(a->classes, 128);
+}
 Layout layout_of(const snn_vocab_loss_args* a, bool backward, int pairs) {
   Layout l{};
   size_t at = 0;
@@ -582,11 +828,11 @@ Layout layout_of(const snn_vocab_loss_args* a, bool backward, int pairs) {
   };
   l.status = take(256);
   l.alpha = l.status + 128;
-  l.x = operand(a->x, a->x_stride, a->rows, a->dim, backward);
   const bool by_class = a->w_layout == SNN_W_BY_CLASS;
-  l.w = operand(a->w, a->w_stride, by_class ? a->classes : a->dim, by_class ? a->dim : a->classes, false);
+  if (backward || !few_rows(a)) l.x = operand(a->x, a->x_stride, a->rows, a->dim, backward);
+  if (backward || !few_rows(a)) l.w = operand(a->w, a->w_stride, by_class ? a->classes : a->dim, by_class ? a->dim : a->classes, false);
   if (!backward) {
-    l.partial = take(sizeof(float2) * (size_t)a->rows * ceil_div(a->classes, UM_TILE));
+    l.partial = take(sizeof(float2) * (size_t)a->rows * (few_rows(a) ? few_blocks(a) : ceil_div(a->classes, UM_TILE)));
     l.target_z = take(sizeof(float) * (size_t)a->rows);
     l.row_loss = take(sizeof(float) * (size_t)a->rows);
   } else {
@@ -647,32 +893,42 @@ struct Call {
     if (!a->workspace || (uintptr_t)a->workspace % 256 != 0) return SNN_ERR_INVALID_ARG;
     if (a->workspace_bytes < l.total) return SNN_ERR_WORKSPACE_TOO_SMALL;
     ws = (char*)a->workspace;
+    if (!backward && a->dtype != SNN_DTYPE_FP32) return SNN_OK;   // neither a status nor magnitudes
     return cudaMemsetAsync(ws + l.status, 0, 128, stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
   }
-  // which: 0 for x, 1 for w
-  snn_status stage(int which, const Operand& o, const void* src, int64_t stride, int rows, int cols) const {
-    if (!o.staged) return SNN_OK;
-    const bool mask = which == 0;
-    uint32_t* const top = tops() ? tops() + which : nullptr;
-    uint16_t* const dst = (uint16_t*)(ws + o.offset);
-    const void* const targets = mask ? a->targets : nullptr;
-    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(o.pitch, 512), 1024), (unsigned)std::min(rows, 16384));
-    if (top) {   // a few thousand blocks at most: each ends with an atomic per warp
-      const unsigned gx = (unsigned)std::min<int64_t>(ceil_div(cols, 256), 32), gy = (unsigned)std::min<int64_t>(rows, std::max(1u, 2048u / gx));
-      largest_kernel<<<dim3(gx, gy), 256, 0, stream>>>((const float*)src, stride, rows, cols, targets, a->target_bits, a->ignore_index, a->classes, top);
+  snn_status stage_operands() const {
+    const bool by_class = a->w_layout == SNN_W_BY_CLASS;
+    StageParams p{};
+    p.targets = a->targets; p.bits = a->target_bits; p.ignore = a->ignore_index; p.classes = a->classes;
+    p.tops = tops();
+    if (l.x.staged) p.job[0] = {a->x, a->x_stride, a->rows, a->dim, (uint16_t*)(ws + l.x.offset), l.x.pitch, l.x.plane, true};
+    if (l.w.staged)
+      p.job[1] = {a->w, a->w_stride, by_class ? a->classes : a->dim, by_class ? a->dim : a->classes, (uint16_t*)(ws + l.w.offset), l.w.pitch, l.w.plane, false};
+    int64_t work = 0;
+    for (const StageJob& j : p.job) work = std::max(work, j.rows * (j.pitch / STAGE_COLS + 1));
+    if (work == 0) return SNN_OK;
+    const dim3 grid((unsigned)std::min<int64_t>(work, 148 * 8), 2);
+    if (p.tops) {
+      largest_kernel<<<grid, 256, 0, stream>>>(p);
+      stage_kernel<float><<<grid, 256, 0, stream>>>(p);
+    } else {
+      stage_kernel<__half><<<grid, 256, 0, stream>>>(p);   // 16 bits are copied, whatever they mean
     }
-    auto go = [&](auto io) {
-      using IO = decltype(io);
-      stage_operand_kernel<IO><<<grid, 256, 0, stream>>>((const IO*)src, stride, rows, cols, dst, (int)o.pitch, o.plane, targets, a->target_bits,
-                                                         a->ignore_index, a->classes, top);
-    };
-    if (a->dtype == SNN_DTYPE_FP32) go(float());
-    else go(__half());   // 16 bits are copied, whatever they mean
     return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
   }
   const void* data(const Operand& o, const void* direct) const { return o.staged ? ws + o.offset : direct; }
   bool map(CUtensorMap* m, const Operand& o, const void* direct, int rows, int cols, bool mn_major) const {
     return make_tensor_map_16bit(m, data(o, direct), is_bf16(a->dtype), cols, rows, o.planes, o.pitch, o.plane, mn_major ? UM_KB : UM_HALF);
+  }
+  // partial sums of `tiles` parts of the vocabulary to the losses
+  snn_status row_losses(const float2* partial, int tiles, const float* target_z) const {
+    float* const row_loss = (float*)(ws + l.row_loss);
+    const bool one = a->rows <= 32;
+    row_loss_kernel<<<ceil_div(a->rows, 32), 1024, 0, stream>>>(partial, tiles, target_z, a->rows, a->targets, a->target_bits, a->ignore_index,
+                                                                a->classes, a->lse, row_loss, a->row_loss, one ? a->loss : nullptr);
+    if (!one)
+      mean_kernel<<<1, 1024, 0, stream>>>(row_loss, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, a->loss, nullptr, 0.f, nullptr);
+    return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
   }
   ProductParams base() const {
     ProductParams p{};
@@ -690,6 +946,26 @@ struct Call {
     return p;
   }
 };
+
+// The forward pass of a few rows.
+template <typename IO, int R> void launch_few(const Call& c, const FewParams& p) {
+  const snn_vocab_loss_args* a = c.a;
+  const unsigned blocks = (unsigned)few_blocks(a);
+  const size_t smem = sizeof(float) * R * a->dim;   // at most 28 KB
+  if (a->w_layout != SNN_W_BY_CLASS) few_rows_by_feature_kernel<IO, R><<<blocks, 32 * FEW_WARPS, smem, c.stream>>>(p);
+  else if (a->dim % 8 == 0 && (uintptr_t)a->w % 16 == 0 && a->w_stride % 8 == 0) few_rows_by_class_kernel<IO, R, true><<<blocks, 32 * FEW_WARPS, smem, c.stream>>>(p);
+  else few_rows_by_class_kernel<IO, R, false><<<blocks, 32 * FEW_WARPS, smem, c.stream>>>(p);
+}
+template <typename IO> snn_status forward_few(const Call& c) {
+  const snn_vocab_loss_args* a = c.a;
+  FewParams p{a->x, a->w, a->targets, a->x_stride, a->w_stride, a->ignore_index, a->rows, a->dim, a->classes, a->target_bits, a->scale * LOG2E,
+              (float2*)(c.ws + c.l.partial), (float*)(c.ws + c.l.target_z)};
+  if (a->rows == 1) launch_few<IO, 1>(c, p);
+  else if (a->rows == 2) launch_few<IO, 2>(c, p);
+  else launch_few<IO, 4>(c, p);
+  if (cudaGetLastError() != cudaSuccess) return SNN_ERR_CUDA;
+  return c.row_losses(p.partial, few_blocks(a), p.target_z);
+}
 
 #define VL_TRY(expr)                            \
   do {                                          \
@@ -713,11 +989,15 @@ extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void*
   Call c{a};
   VL_TRY(c.begin(false, stream));
   if (a->rows == 0) return cudaMemsetAsync(a->loss, 0, 4, c.stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+  if (few_rows(a))
+    return a->dtype == SNN_DTYPE_FP32   ? forward_few<float>(c)
+           : a->dtype == SNN_DTYPE_BF16 ? forward_few<__nv_bfloat16>(c)
+                                        : forward_few<__half>(c);
   const bool by_class = a->w_layout == SNN_W_BY_CLASS;
   const int w_rows = by_class ? a->classes : a->dim, w_cols = by_class ? a->dim : a->classes;
-  VL_TRY(c.stage(0, c.l.x, a->x, a->x_stride, a->rows, a->dim));
-  VL_TRY(c.stage(1, c.l.w, a->w, a->w_stride, w_rows, w_cols));
+  VL_TRY(c.stage_operands());
   ProductParams p = c.base();
+  p.status = nullptr;   // (a wait that ran out shows in the losses)
   if (!c.map(&p.a, c.l.x, a->x, a->rows, a->dim, false) || !c.map(&p.b, c.l.w, a->w, w_rows, w_cols, !by_class)) return SNN_ERR_CUDA;
   p.tiles_m = ceil_div(a->rows, UM_TILE);
   p.tiles_n = ceil_div(a->classes, UM_TILE);
@@ -727,11 +1007,7 @@ extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void*
   p.partial = (float2*)(c.ws + c.l.partial);
   p.target_z = (float*)(c.ws + c.l.target_z);
   VL_TRY((by_class ? launch_product<STATS, false, false>(p, c.pairs, c.stream) : launch_product<STATS, false, true>(p, c.pairs, c.stream)));
-  float* const row_loss = (float*)(c.ws + c.l.row_loss);
-  row_loss_kernel<<<ceil_div(a->rows, 32), 256, 0, c.stream>>>(p.partial, p.tiles_n, p.target_z, a->rows, a->targets, a->target_bits,
-                                                               a->ignore_index, a->classes, a->lse, row_loss, a->row_loss, c.status());
-  mean_kernel<<<1, 1024, 0, c.stream>>>(row_loss, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, a->loss, nullptr, 0.f, nullptr);
-  return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+  return c.row_losses(p.partial, p.tiles_n, p.target_z);
 }
 
 extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void* stream) {
@@ -747,8 +1023,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     return cudaMemset2DAsync(a->dw, a->dw_stride * size, 0, w_cols * size, w_rows, c.stream) == cudaSuccess ? SNN_OK
                                                                                                          : (cudaGetLastError(), SNN_ERR_CUDA);
   const Layout& l = c.l;
-  VL_TRY(c.stage(0, l.x, a->x, a->x_stride, a->rows, a->dim));
-  VL_TRY(c.stage(1, l.w, a->w, a->w_stride, w_rows, w_cols));
+  VL_TRY(c.stage_operands());
   const ProductParams base = c.base();
   mean_kernel<<<1, 1024, 0, c.stream>>>(nullptr, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, nullptr, c.alpha(),
                                         a->dloss * a->scale / (base.bf16 ? 1.f : FP16_DZ_SCALE), a->dloss_device);
@@ -788,6 +1063,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
       p.m = a->dim; p.n = width;
       p.dw = (char*)a->dw + (size_t)v0 * size;
     }
+    p.dw_vector = (uintptr_t)p.dw % 16 == 0 && p.dw_stride * (int64_t)size % 16 == 0;
     p.tiles_m = ceil_div(p.m, UM_TILE); p.tiles_n = ceil_div(p.n, UM_TILE);
     VL_TRY((launch_product<DW, true, true>(p, c.pairs, c.stream)));
   }

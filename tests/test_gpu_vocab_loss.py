@@ -70,6 +70,13 @@ def test_loss_and_gradients(n, D, V, dtype, layout):
     check(*inputs(n, D, V, dtype, 1, layout), dtype)
 
 
+@pytest.mark.parametrize("layout", ["feature", "class", "wide", "wide_class"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("n,D,V", [(1, 1024, 5000), (2, 72, 20001), (3, 2048, 127), (4, 33, 129), (1, 8192, 40), (4, 2056, 50), (1, 4, 70000), (5, 64, 300)])
+def test_loss_of_a_few_rows(n, D, V, dtype, layout):
+    check(*inputs(n, D, V, dtype, 13, layout), dtype, scale=0.7, backward=False)
+
+
 @pytest.mark.parametrize("layout", ["wide", "wide_class"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("bits", [32, 64])

@@ -646,11 +646,10 @@ template <typename IO, int R, bool VEC> __global__ void __launch_bounds__(32 * F
   extern __shared__ __align__(16) float s_x[];   // VEC: [R][2][dim / 8] float4, the halves of eight features apart; else [R][dim]
   __shared__ float2 s_part[FEW_WARPS][R];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int i = threadIdx.x; i < R * p.dim; i += blockDim.x) {
-    const int r = i / p.dim, d = i % p.dim;
-    const float v = r < p.rows ? to_f32(((const IO*)p.x)[r * p.x_stride + d]) : 0.f;
-    s_x[VEC ? r * p.dim + (d / 4 % 2) * (p.dim / 2) + d / 8 * 4 + d % 4 : i] = v;
-  }
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    for (int d = threadIdx.x; d < p.dim; d += blockDim.x)
+      s_x[r * p.dim + (VEC ? (d / 4 % 2) * (p.dim / 2) + d / 8 * 4 + d % 4 : d)] = r < p.rows ? to_f32(((const IO*)p.x)[r * p.x_stride + d]) : 0.f;
   __syncthreads();
   int target[R];
   few_targets<IO, R>(p, target);
@@ -665,11 +664,7 @@ template <typename IO, int R, bool VEC> __global__ void __launch_bounds__(32 * F
     for (int j = 0; j < 4; ++j) row[j] = (const IO*)p.w + min(v0 + j, last - 1) * p.w_stride;
     float acc[4][R] = {};
     if (VEC) {
-#pragma unroll 2
-      for (int d = lane * 8; d < p.dim; d += 256) {
-        EightValues<IO> q[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) q[j] = *reinterpret_cast<const EightValues<IO>*>(row[j] + d);
+      auto add = [&](const EightValues<IO> (&q)[4], int d) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           const float4 xa = *reinterpret_cast<const float4*>(s_x + r * p.dim + d / 2);
@@ -683,6 +678,16 @@ template <typename IO, int R, bool VEC> __global__ void __launch_bounds__(32 * F
             for (int k = 0; k < 8; ++k) acc[j][r] = fmaf(f[k], xs[k], acc[j][r]);
           }
         }
+      };
+      for (int d = lane * 8; d < p.dim; d += 512) {   // eight loads in flight per lane
+        const bool two = d + 256 < p.dim;
+        EightValues<IO> q[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) q[h][j] = *reinterpret_cast<const EightValues<IO>*>(row[j] + (h && two ? d + 256 : d));
+        add(q[0], d);
+        if (two) add(q[1], d + 256);
       }
     } else {
 #pragma unroll 4
@@ -717,7 +722,9 @@ template <typename IO, int R> __global__ void __launch_bounds__(32 * FEW_WARPS) 
   __shared__ float s_acc[FEW_WARPS][R][128];
   __shared__ float2 s_part[FEW_WARPS][R];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int i = threadIdx.x; i < R * p.dim; i += blockDim.x) s_x[i] = i / p.dim < p.rows ? to_f32(((const IO*)p.x)[i / p.dim * p.x_stride + i % p.dim]) : 0.f;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    for (int d = threadIdx.x; d < p.dim; d += blockDim.x) s_x[r * p.dim + d] = r < p.rows ? to_f32(((const IO*)p.x)[r * p.x_stride + d]) : 0.f;
   __syncthreads();
   int target[R];
   few_targets<IO, R>(p, target);
@@ -756,6 +763,39 @@ template <typename IO, int R> __global__ void __launch_bounds__(32 * FEW_WARPS) 
       sum[r] = join_sums(sum[r], make_float2(__shfl_xor_sync(0xffffffffu, sum[r].x, o), __shfl_xor_sync(0xffffffffu, sum[r].y, o)));
   }
   few_finish<R>(p, sum, s_part);
+}
+
+// One block: the blocks' partial sums of a few rows to the rows' losses and their mean; lanes across the parts.
+__global__ void __launch_bounds__(1024) few_loss_kernel(const float2* partial, int parts, const float* target_z, int rows, const void* targets,
+                                                        int bits, int64_t ignore, int classes, float* lse, float* row_out, float* loss) {
+  __shared__ float2 s_part[32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  double sum = 0.;
+  int count = 0;
+  for (int row = 0; row < rows; ++row) {
+    float2 v = make_float2(-INFINITY, 0.f);
+    for (int t = threadIdx.x; t < parts; t += blockDim.x) v = join_sums(v, partial[(int64_t)t * rows + row]);
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) v = join_sums(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+    if (lane == 0) s_part[warp] = v;
+    __syncthreads();
+    if (warp == 0) {
+      v = s_part[lane];
+#pragma unroll
+      for (int o = 16; o > 0; o /= 2) v = join_sums(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+      const int target = target_of(targets, bits, ignore, classes, row);
+      float l = (v.x + log2f(v.y)) * LN2, out = l - (target >= 0 ? target_z[row] * LN2 : 0.f);
+      if (target < 0) l = 0.f, out = target == -1 ? 0.f : __uint_as_float(0x7fc00000u);
+      sum += out;
+      count += target >= 0;
+      if (lane == 0) {
+        lse[row] = l;
+        if (row_out) row_out[row] = out;
+      }
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *loss = (float)(sum / (double)max(count, 1));
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------
@@ -964,7 +1004,9 @@ template <typename IO> snn_status forward_few(const Call& c) {
   else if (a->rows == 2) launch_few<IO, 2>(c, p);
   else launch_few<IO, 4>(c, p);
   if (cudaGetLastError() != cudaSuccess) return SNN_ERR_CUDA;
-  return c.row_losses(p.partial, few_blocks(a), p.target_z);
+  few_loss_kernel<<<1, 1024, 0, c.stream>>>(p.partial, few_blocks(a), p.target_z, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes,
+                                            a->lse, a->row_loss, a->loss);
+  return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
 }
 
 #define VL_TRY(expr)                            \

@@ -213,6 +213,18 @@ __device__ __forceinline__ void read_pairs(float2 (&v)[SCAN_K], const void* tile
 #pragma unroll
   for (int k = 0; k < SCAN_K; ++k) v[k] = to_f32(at[k * (SCAN_COLS / 2)]);
 }
+// The same as they are.
+template <typename IO>
+__device__ __forceinline__ void read_raw(typename Pair<IO>::raw (&v)[SCAN_K], const void* tile, const Place& w) {
+  using raw = typename Pair<IO>::raw;
+  const raw* const at = reinterpret_cast<const raw*>(reinterpret_cast<const IO*>(tile) + w.warp * WARP_PIECE) + w.lane;
+#pragma unroll
+  for (int k = 0; k < SCAN_K; ++k) v[k] = at[k * (SCAN_COLS / 2)];
+}
+template <typename IO> __device__ __forceinline__ void to_raw(typename Pair<IO>::raw (&r)[SCAN_K], const float2 (&v)[SCAN_K]) {
+#pragma unroll
+  for (int k = 0; k < SCAN_K; ++k) set_raw(r[k], v[k]);
+}
 // This thread's values straight from memory.
 template <typename IO>
 __device__ __forceinline__ void load_values(float2 (&v)[SCAN_K], const IO* sample, int64_t stride, const Place& w, int t0) {
@@ -486,6 +498,7 @@ __global__ void __launch_bounds__(128) scan_short_kernel(const __grid_constant__
 // chunk starts at a checkpoint, so only e crosses blocks.  Warp 0 chains the states, warp 1 the e.
 template <typename IO, int PATH>
 __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __grid_constant__ ScanParams p) {
+  using raw = typename Pair<IO>::raw;
   constexpr int VALUES = PIECE * (int)sizeof(IO), OUT = 2 * WARP_PIECE * (int)sizeof(IO);
   extern __shared__ __align__(128) unsigned char s_dyn[];   // ring [SCAN_DEPTH] of dh, x, gate (values or codes); TILES: out
   __shared__ float4 s_forth[WARPS][32];
@@ -541,7 +554,9 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     const int slot = i % SCAN_DEPTH, t0 = turn + w.ahead;
     const bool full = t0 + SCAN_K <= w.len;
     unsigned char* const out = s_dyn + SCAN_DEPTH * slot_bytes + (w.warp * 2 + (i & 1)) * OUT;
-    float2 xv[SCAN_K], a[SCAN_K], in[SCAN_K], d[SCAN_K];
+    // x and dh stay in their own type (a register per pair if it has 16 bits); kept values fit it (see keep_decode2)
+    raw xr[SCAN_K], dr[SCAN_K];
+    float2 a[SCAN_K], in[SCAN_K];
     const uint32_t scales = next_scales;
     const float2 start = next_start;
     next_scales = load_scales(turn - SNN_SCAN_CHUNK);
@@ -553,16 +568,22 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
       __syncwarp();
     }
     if (PATH == PAIRS) copies_landed<SCAN_DEPTH - 1>();
-    if constexpr (PATH == SCALAR) load_values<IO>(d, dh, p.dhs[0], w, t0);
-    else read_pairs<IO>(d, at, w);
-    if (raw_x) {
-      if constexpr (PATH == SCALAR) load_values<IO>(xv, x, p.xs[0], w, t0);
-      else read_pairs<IO>(xv, at + x_at, w);
-    } else if constexpr (PATH == TILES) {
-      if (p.x_format == SNN_KEEP_INT8) decode_steps<SNN_KEEP_INT8, IO>(xv, at + x_at, w, scales, 0);
-      else decode_steps<SNN_KEEP_E4M3, IO>(xv, at + x_at, w, scales, 0);
+    if constexpr (PATH == SCALAR) {
+      float2 v[SCAN_K];
+      load_values<IO>(v, dh, p.dhs[0], w, t0);
+      to_raw<IO>(dr, v);
     } else {
-      decode_from_memory<IO>(xv, p.x_codes, p, w, t0, scales, 0, p.x_format);
+      read_raw<IO>(dr, at, w);
+    }
+    if (raw_x && PATH != SCALAR) {
+      read_raw<IO>(xr, at + x_at, w);
+    } else {
+      float2 v[SCAN_K];
+      if (raw_x) load_values<IO>(v, x, p.xs[0], w, t0);
+      else if (PATH != TILES) decode_from_memory<IO>(v, p.x_codes, p, w, t0, scales, 0, p.x_format);
+      else if (p.x_format == SNN_KEEP_INT8) decode_steps<SNN_KEEP_INT8, IO>(v, at + x_at, w, scales, 0);
+      else decode_steps<SNN_KEEP_E4M3, IO>(v, at + x_at, w, scales, 0);
+      to_raw<IO>(xr, v);
     }
     if (raw_gate) {
       if constexpr (PATH == SCALAR) load_values<IO>(a, gate, p.gs[0], w, t0);
@@ -579,15 +600,20 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     if (!full) {
 #pragma unroll
       for (int k = 0; k < SCAN_K; ++k)
-        if (t0 + k >= w.len) a[k] = both(1.f), xv[k] = d[k] = in[k] = both(0.f);
+        if (t0 + k >= w.len) {
+          a[k] = both(1.f);
+          in[k] = both(0.f);
+          set_raw(xr[k], both(0.f));
+          set_raw(dr[k], both(0.f));
+        }
     }
-    Map2 forth{a[0], mul2(in[0], xv[0])};
+    Map2 forth{a[0], mul2(in[0], to_f32(xr[0]))};
 #pragma unroll
-    for (int k = 1; k < SCAN_K; ++k) forth = then(forth, Map2{a[k], mul2(in[k], xv[k])});
+    for (int k = 1; k < SCAN_K; ++k) forth = then(forth, Map2{a[k], mul2(in[k], to_f32(xr[k]))});
     // the way back has the same product of decays; its other part is e before the warp's steps if none came in
-    float2 e0 = mul2(a[SCAN_K - 1], d[SCAN_K - 1]);
+    float2 e0 = mul2(a[SCAN_K - 1], to_f32(dr[SCAN_K - 1]));
 #pragma unroll
-    for (int k = SCAN_K - 2; k >= 0; --k) e0 = mul2(a[k], add2(d[k], e0));
+    for (int k = SCAN_K - 2; k >= 0; --k) e0 = mul2(a[k], add2(to_f32(dr[k]), e0));
     s_forth[w.warp][w.lane] = as4(forth);
     s_back[w.warp][w.lane] = e0;
     __syncthreads();
@@ -612,36 +638,40 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     }
     __syncthreads();
     float2 h = s_h[w.warp][w.lane], e = s_e[w.warp][w.lane];
-#pragma unroll
-    for (int k = SCAN_K - 1; k >= 0; --k) {   // d becomes D
-      d[k] = add2(d[k], e);
-      e = mul2(a[k], d[k]);
-    }
-    // DIRECT: dx = D, dgate = D h; SIGMOID: dx = D i, dgate = D i a (h - x)
+    // u_k = dgate_k / D_k from the first step to the last, then D and the results from the last to the first.
+    // DIRECT: u = h, dx = D; SIGMOID: u = i a (h - x), dx = D i
     auto outputs = [&](auto is_direct, auto is_full) {
       constexpr bool DIRECT = decltype(is_direct)::value, FULL = decltype(is_full)::value;
-      IO *dx_to, *dg_to;
-      if (PATH == TILES) {
-        dx_to = reinterpret_cast<IO*>(out) + 2 * w.lane;
-        dg_to = dx_to + WARP_PIECE;
-      } else {
-        dx_to = (IO*)p.dx + w.b * p.dxs[1] + t0 * p.dxs[0];
-        dg_to = (IO*)p.dgate + w.b * p.dgs[1] + t0 * p.dgs[0];
-      }
+      float2 u[SCAN_K];
 #pragma unroll
       for (int k = 0; k < SCAN_K; ++k) {
-        const float2 gx = DIRECT ? d[k] : mul2(d[k], in[k]);
-        const float2 gg = DIRECT ? mul2(d[k], h) : mul2(mul2(gx, a[k]), fma2(xv[k], both(-1.f), h));
-        h = fma2(a[k], h, DIRECT ? xv[k] : mul2(in[k], xv[k]));
+        const float2 xv = to_f32(xr[k]);
+        u[k] = DIRECT ? h : mul2(mul2(in[k], a[k]), fma2(xv, both(-1.f), h));
+        h = fma2(a[k], h, DIRECT ? xv : mul2(in[k], xv));
+      }
+      IO *dx_to, *dg_to;
+      if (PATH == TILES) {
+        dx_to = reinterpret_cast<IO*>(out) + (SCAN_K - 1) * SCAN_COLS + 2 * w.lane;
+        dg_to = dx_to + WARP_PIECE;
+      } else {
+        dx_to = (IO*)p.dx + w.b * p.dxs[1] + (t0 + SCAN_K - 1) * p.dxs[0];
+        dg_to = (IO*)p.dgate + w.b * p.dgs[1] + (t0 + SCAN_K - 1) * p.dgs[0];
+      }
+#pragma unroll
+      for (int k = SCAN_K - 1; k >= 0; --k) {
+        const float2 D = add2(to_f32(dr[k]), e), gx = DIRECT ? D : mul2(D, in[k]), gg = mul2(D, u[k]);
+        e = mul2(a[k], D);
         const bool on = FULL || t0 + k < w.len;
         if (PATH == TILES) {
-          store_pair<true>(dx_to + k * SCAN_COLS, 0, 2, on ? gx : both(0.f));
-          store_pair<true>(dg_to + k * SCAN_COLS, 0, 2, on ? gg : both(0.f));
+          store_pair<true>(dx_to, 0, 2, on ? gx : both(0.f));
+          store_pair<true>(dg_to, 0, 2, on ? gg : both(0.f));
+          dx_to -= SCAN_COLS;
+          dg_to -= SCAN_COLS;
         } else {
           if (on) store_pair<PATH == PAIRS>(dx_to, w.c, w.n_ok, gx);
           if (on) store_pair<PATH == PAIRS>(dg_to, w.c, w.n_ok, gg);
-          dx_to += p.dxs[0];
-          dg_to += p.dgs[0];
+          dx_to -= p.dxs[0];
+          dg_to -= p.dgs[0];
         }
       }
     };

@@ -202,8 +202,14 @@ template <typename IO>
 __device__ __forceinline__ void stage_pairs(IO* tile, const IO* sample, int64_t stride, const Place& w, int t0) {
   IO* const to = tile + w.warp * WARP_PIECE + 2 * w.lane;
   const IO* const column = sample + (w.n_ok ? w.c : 0);
+  if (t0 + SCAN_K <= w.len) {
+    const IO* at = column + t0 * stride;
 #pragma unroll
-  for (int k = 0; k < SCAN_K; ++k) copy_async<2 * sizeof(IO)>(to + k * SCAN_COLS, column + min(t0 + k, w.len - 1) * stride);
+    for (int k = 0; k < SCAN_K; ++k, at += stride) copy_async<2 * sizeof(IO)>(to + k * SCAN_COLS, at);
+  } else {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) copy_async<2 * sizeof(IO)>(to + k * SCAN_COLS, column + min(t0 + k, w.len - 1) * stride);
+  }
 }
 // This thread's pairs out of a staged tile.
 template <typename IO>
@@ -228,8 +234,14 @@ template <typename IO> __device__ __forceinline__ void to_raw(typename Pair<IO>:
 // This thread's values straight from memory.
 template <typename IO>
 __device__ __forceinline__ void load_values(float2 (&v)[SCAN_K], const IO* sample, int64_t stride, const Place& w, int t0) {
+  if (t0 + SCAN_K <= w.len) {
+    const IO* at = sample + t0 * stride;
 #pragma unroll
-  for (int k = 0; k < SCAN_K; ++k) v[k] = load_pair<false>(sample + min(t0 + k, w.len - 1) * stride, w.c, w.n_ok);
+    for (int k = 0; k < SCAN_K; ++k, at += stride) v[k] = load_pair<false>(at, w.c, w.n_ok);
+  } else {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) v[k] = load_pair<false>(sample + min(t0 + k, w.len - 1) * stride, w.c, w.n_ok);
+  }
 }
 
 // ---- kept rows in 8 bits ------------------------------------------------------------------------------------
@@ -823,14 +835,13 @@ ScanParams params_of(const snn_scan_args* a) {
   p.x_codes = a->x_codes; p.x_scales = a->x_scales; p.gate_codes = a->gate_codes; p.gate_scales = a->gate_scales;
   return p;
 }
-// Segments of the time axis.  One while there are about as many column tiles as SMs.  Below that the device is filled once
-// (`resident` blocks fit an SM), as long as a segment has a few turns: reading the inputs twice costs less than the SMs
-// left idle.
+// Segments of the time axis: as many as fill the device once (`resident` blocks fit an SM), each with two turns at least.
+// Below four segments one is as fast: what the SMs left idle would win goes into reading the inputs twice and into a second
+// launch (2048 x 2 x 4096 bf16, 128 tiles: 43 us with one segment, 42 with three; 4096 x 2 x 512, 16 tiles: 80 and 18).
 void cut_time(ScanParams& p, int resident) {
-  const int64_t tiles = (int64_t)p.B * p.n_tiles;
-  int64_t n = 1;
-  if (tiles > 0 && tiles < 148) n = std::min<int64_t>(148 * resident / tiles, p.T / (4 * SNN_SCAN_CHUNK));
-  n = std::max<int64_t>(n, 1);
+  const int64_t tiles = std::max<int64_t>((int64_t)p.B * p.n_tiles, 1);
+  int64_t n = std::min<int64_t>(148 * resident / tiles, p.T / (2 * SNN_SCAN_CHUNK));
+  if (n < 4) n = 1;
   p.segment_steps = (int)((((int64_t)p.T + n - 1) / n + SNN_SCAN_CHUNK - 1) / SNN_SCAN_CHUNK * SNN_SCAN_CHUNK);
   p.segments = p.segment_steps ? (p.T + p.segment_steps - 1) / p.segment_steps : 1;
 }

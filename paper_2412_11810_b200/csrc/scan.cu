@@ -190,27 +190,6 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, int x, int 
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 template <int PENDING> __device__ __forceinline__ void bulk_read_done() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory"); }
 
-template <int BYTES> __device__ __forceinline__ void copy_async(void* smem, const void* gmem) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(gmem), "n"(BYTES) : "memory");
-}
-__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int PENDING> __device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
-
-// PAIRS: this thread's pairs of SCAN_K steps from t0 on, to where a tile by TMA would have them; behind the sequence's end
-// the last step again.
-template <typename IO>
-__device__ __forceinline__ void stage_pairs(IO* tile, const IO* sample, int64_t stride, const Place& w, int t0) {
-  IO* const to = tile + w.warp * WARP_PIECE + 2 * w.lane;
-  const IO* const column = sample + (w.n_ok ? w.c : 0);
-  if (t0 + SCAN_K <= w.len) {
-    const IO* at = column + t0 * stride;
-#pragma unroll
-    for (int k = 0; k < SCAN_K; ++k, at += stride) copy_async<2 * sizeof(IO)>(to + k * SCAN_COLS, at);
-  } else {
-#pragma unroll
-    for (int k = 0; k < SCAN_K; ++k) copy_async<2 * sizeof(IO)>(to + k * SCAN_COLS, column + min(t0 + k, w.len - 1) * stride);
-  }
-}
 // This thread's pairs out of a staged tile.
 template <typename IO>
 __device__ __forceinline__ void read_pairs(float2 (&v)[SCAN_K], const void* tile, const Place& w) {
@@ -232,15 +211,15 @@ template <typename IO> __device__ __forceinline__ void to_raw(typename Pair<IO>:
   for (int k = 0; k < SCAN_K; ++k) set_raw(r[k], v[k]);
 }
 // This thread's values straight from memory.
-template <typename IO>
+template <bool IN_PAIRS, typename IO>
 __device__ __forceinline__ void load_values(float2 (&v)[SCAN_K], const IO* sample, int64_t stride, const Place& w, int t0) {
   if (t0 + SCAN_K <= w.len) {
     const IO* at = sample + t0 * stride;
 #pragma unroll
-    for (int k = 0; k < SCAN_K; ++k, at += stride) v[k] = load_pair<false>(at, w.c, w.n_ok);
+    for (int k = 0; k < SCAN_K; ++k, at += stride) v[k] = load_pair<IN_PAIRS>(at, w.c, w.n_ok);
   } else {
 #pragma unroll
-    for (int k = 0; k < SCAN_K; ++k) v[k] = load_pair<false>(sample + min(t0 + k, w.len - 1) * stride, w.c, w.n_ok);
+    for (int k = 0; k < SCAN_K; ++k) v[k] = load_pair<IN_PAIRS>(sample + min(t0 + k, w.len - 1) * stride, w.c, w.n_ok);
   }
 }
 
@@ -358,7 +337,7 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
   const IO* const x = (const IO*)p.x + w.b * p.xs[1];
   const IO* const gate = (const IO*)p.gate + w.b * p.gs[1];
   IO* const h_out = (IO*)p.h + w.b * p.hs[1];
-  auto issue = [&](int turn, int slot) {   // TILES: one thread; PAIRS: all
+  auto issue = [&](int turn, int slot) {   // by one thread
     unsigned char* const at = s_dyn + slot * SLOT;
     if constexpr (PATH == TILES) {
       if (turn < w.end) {
@@ -367,16 +346,9 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
         tma_load_3d(at + SLOT / 2, &p.in[1], w.col0, w.b, turn, &s_landed[slot]);
       }
     }
-    if constexpr (PATH == PAIRS) {
-      if (turn < w.end) {
-        stage_pairs<IO>(reinterpret_cast<IO*>(at), x, p.xs[0], w, turn + w.ahead);
-        stage_pairs<IO>(reinterpret_cast<IO*>(at + SLOT / 2), gate, p.gs[0], w, turn + w.ahead);
-      }
-      copies_issued();
-    }
   };
   barriers_init(s_landed);
-  const bool loader = PATH == PAIRS || (PATH == TILES && threadIdx.x == 32 * (WARPS - 1));
+  const bool loader = PATH == TILES && threadIdx.x == 32 * (WARPS - 1);
   if (loader)
     for (int d = 0; d < SCAN_DEPTH; ++d) issue(w.from + d * SNN_SCAN_CHUNK, d);
   float2 carry = both(0.f);   // warp 0 chains the summaries
@@ -388,21 +360,16 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
     const bool full = t0 + SCAN_K <= w.len;
     unsigned char* const out = s_dyn + SCAN_DEPTH * SLOT + (w.warp * 2 + (i & 1)) * OUT;
     float2 xv[SCAN_K], gv[SCAN_K];
-    if constexpr (PATH == SCALAR) {
-      load_values<IO>(xv, x, p.xs[0], w, t0);
-      load_values<IO>(gv, gate, p.gs[0], w, t0);
+    if constexpr (PATH != TILES) {
+      load_values<PATH == PAIRS>(xv, x, p.xs[0], w, t0);
+      load_values<PATH == PAIRS>(gv, gate, p.gs[0], w, t0);
     } else {
-      if (PATH == TILES) {
-        if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
-        if (w.lane == 0) bulk_read_done<1>();   // the out buffer used two turns ago has been read
-        __syncwarp();
-      } else {
-        copies_landed<SCAN_DEPTH - 1>();
-      }
+      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
+      if (w.lane == 0) bulk_read_done<1>();   // the out buffer used two turns ago has been read
+      __syncwarp();
       read_pairs<IO>(xv, s_dyn + slot * SLOT, w);
       read_pairs<IO>(gv, s_dyn + slot * SLOT + SLOT / 2, w);
       if (!alive) gv[0] = nan2();
-      if (PATH == PAIRS) issue(turn + SCAN_DEPTH * SNN_SCAN_CHUNK, slot);
     }
     if constexpr (KEEP) {
       unsigned char* const codes = out + WARP_PIECE * sizeof(IO);
@@ -423,7 +390,7 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
     for (int k = 1; k < SCAN_K; ++k) mine = then(mine, Map2{gv[k], xv[k]});
     s_sum[w.warp][w.lane] = as4(mine);
     __syncthreads();
-    if (PATH == TILES && loader) issue(turn + SCAN_DEPTH * SNN_SCAN_CHUNK, slot);   // all warps have read the slot
+    if (loader) issue(turn + SCAN_DEPTH * SNN_SCAN_CHUNK, slot);   // all warps have read the slot
     if (w.warp == 0) {
       float2 h = carry;
       if (!alive) h = nan2();
@@ -533,14 +500,6 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
         tma_load_3d(at + gate_at, &p.in[2], w.col0, w.b, turn, &s_landed[slot]);
       }
     }
-    if constexpr (PATH == PAIRS) {   // (8-bit codes are read from memory on this path)
-      if (turn >= w.from) {
-        stage_pairs<IO>(reinterpret_cast<IO*>(at), dh, p.dhs[0], w, turn + w.ahead);
-        if (raw_x) stage_pairs<IO>(reinterpret_cast<IO*>(at + x_at), x, p.xs[0], w, turn + w.ahead);
-        if (raw_gate) stage_pairs<IO>(reinterpret_cast<IO*>(at + gate_at), gate, p.gs[0], w, turn + w.ahead);
-      }
-      copies_issued();
-    }
   };
   // scale bytes: of x in lanes 0..7 (one per step), of the gate in lanes 8..15, read one turn ahead
   auto load_scales = [&](int turn) -> uint32_t {
@@ -553,7 +512,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     return load_state(p.states, (int64_t)(turn / SNN_SCAN_CHUNK) * p.B + w.b, p.N, w.c, w.n_ok);
   };
   barriers_init(s_landed);
-  const bool loader = PATH == PAIRS || (PATH == TILES && threadIdx.x == 32 * (WARPS - 1));
+  const bool loader = PATH == TILES && threadIdx.x == 32 * (WARPS - 1);
   const int turns = (max(w.end - w.from, 0) + SNN_SCAN_CHUNK - 1) / SNN_SCAN_CHUNK, last_turn = w.from + (turns - 1) * SNN_SCAN_CHUNK;
   if (loader)
     for (int d = 0; d < SCAN_DEPTH; ++d) issue(last_turn - d * SNN_SCAN_CHUNK, d);
@@ -579,26 +538,25 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
       if (w.lane == 0) bulk_read_done<1>();
       __syncwarp();
     }
-    if (PATH == PAIRS) copies_landed<SCAN_DEPTH - 1>();
-    if constexpr (PATH == SCALAR) {
+    if constexpr (PATH != TILES) {
       float2 v[SCAN_K];
-      load_values<IO>(v, dh, p.dhs[0], w, t0);
+      load_values<PATH == PAIRS>(v, dh, p.dhs[0], w, t0);
       to_raw<IO>(dr, v);
     } else {
       read_raw<IO>(dr, at, w);
     }
-    if (raw_x && PATH != SCALAR) {
+    if (raw_x && PATH == TILES) {
       read_raw<IO>(xr, at + x_at, w);
     } else {
       float2 v[SCAN_K];
-      if (raw_x) load_values<IO>(v, x, p.xs[0], w, t0);
+      if (raw_x) load_values<PATH == PAIRS>(v, x, p.xs[0], w, t0);
       else if (PATH != TILES) decode_from_memory<IO>(v, p.x_codes, p, w, t0, scales, 0, p.x_format);
       else if (p.x_format == SNN_KEEP_INT8) decode_steps<SNN_KEEP_INT8, IO>(v, at + x_at, w, scales, 0);
       else decode_steps<SNN_KEEP_E4M3, IO>(v, at + x_at, w, scales, 0);
       to_raw<IO>(xr, v);
     }
     if (raw_gate) {
-      if constexpr (PATH == SCALAR) load_values<IO>(a, gate, p.gs[0], w, t0);
+      if constexpr (PATH != TILES) load_values<PATH == PAIRS>(a, gate, p.gs[0], w, t0);
       else read_pairs<IO>(a, at + gate_at, w);
     } else if constexpr (PATH == TILES) {
       if (p.gate_format == SNN_KEEP_INT8) decode_steps<SNN_KEEP_INT8, IO>(a, at + gate_at, w, scales, 8);
@@ -606,7 +564,6 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     } else {
       decode_from_memory<IO>(a, p.gate_codes, p, w, t0, scales, 8, p.gate_format);
     }
-    if (PATH == PAIRS) issue(turn - SCAN_DEPTH * SNN_SCAN_CHUNK, slot);
     if (!alive) a[0] = nan2();
     coefficients(a, in, p.mode);
     if (!full) {
@@ -629,7 +586,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     s_forth[w.warp][w.lane] = as4(forth);
     s_back[w.warp][w.lane] = e0;
     __syncthreads();
-    if (PATH == TILES && loader) issue(turn - SCAN_DEPTH * SNN_SCAN_CHUNK, slot);
+    if (loader) issue(turn - SCAN_DEPTH * SNN_SCAN_CHUNK, slot);
     if (w.warp == 0) {
       float2 h = alive ? start : nan2();
 #pragma unroll
@@ -910,7 +867,7 @@ extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
     const int64_t blocks = (int64_t)p.B * p.n_tiles;
     auto go = [&](auto is_keep) {
       constexpr bool KEEP = decltype(is_keep)::value;
-      const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * forward_slot<IO>(), out = PATH == TILES ? 2 * WARPS * forward_out<IO, KEEP>() : 0;
+      const size_t ring = PATH != TILES ? 0 : SCAN_DEPTH * forward_slot<IO>(), out = PATH == TILES ? 2 * WARPS * forward_out<IO, KEEP>() : 0;
       return launch(scan_forward_kernel<IO, KEEP, PATH>, ring + out, blocks * p.segments, p, s);
     };
     if (p.segments > 1) {
@@ -945,7 +902,7 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
     using IO = decltype(io);
     constexpr int PATH = decltype(path)::value;
     const size_t values = PIECE * sizeof(IO), slot = values + (raw_x ? values : PIECE) + (raw_gate ? values : PIECE);
-    const size_t ring = PATH == SCALAR ? 0 : SCAN_DEPTH * slot, out = PATH == TILES ? 2 * WARPS * 2 * WARP_PIECE * sizeof(IO) : 0;
+    const size_t ring = PATH != TILES ? 0 : SCAN_DEPTH * slot, out = PATH == TILES ? 2 * WARPS * 2 * WARP_PIECE * sizeof(IO) : 0;
     const int64_t blocks = (int64_t)p.B * p.n_tiles;
     if (p.segments > 1) {
       const snn_status st = launch(scan_summary_kernel<IO, PATH != SCALAR, true>, 0, blocks * (p.segments - 1), p, (cudaStream_t)stream);

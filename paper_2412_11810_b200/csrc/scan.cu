@@ -226,13 +226,13 @@ __device__ __forceinline__ void load_values(float2 (&v)[SCAN_K], const IO* sampl
 // ---- kept rows in 8 bits ------------------------------------------------------------------------------------
 // Encodes the warp's steps t0.. (those before the sequence's end); codes to s_codes (TILES: they leave by TMA, and channels
 // that do not exist are zeros) or to memory.
-template <int FORMAT, bool TO_SMEM>
+template <int FORMAT, int PATH>
 __device__ __forceinline__ void keep_steps(const float2 (&v)[SCAN_K], const ScanParams& p, const Place& w, int t0, uint8_t* codes,
                                            uint8_t* scales, unsigned char* s_codes) {
   uint32_t top[SCAN_K], worst = 0, fraction = 0;   // magnitudes' bit patterns sort as they do
 #pragma unroll
   for (int k = 0; k < SCAN_K; ++k) {
-    const float m = TO_SMEM ? larger_magnitude(v[k].x, v[k].y) : larger_magnitude(w.n_ok > 0 ? v[k].x : 0.f, w.n_ok > 1 ? v[k].y : 0.f);
+    const float m = PATH == TILES ? larger_magnitude(v[k].x, v[k].y) : larger_magnitude(w.n_ok > 0 ? v[k].x : 0.f, w.n_ok > 1 ? v[k].y : 0.f);
     top[k] = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
     worst = max(worst, top[k]);
     fraction = max(fraction, top[k] & 0x7fffffu);
@@ -260,12 +260,16 @@ __device__ __forceinline__ void keep_steps(const float2 (&v)[SCAN_K], const Scan
   }
 #pragma unroll
   for (int k = 0; k < SCAN_K; ++k) {
-    if (TO_SMEM) {
+    if (PATH == TILES) {
       *reinterpret_cast<uint16_t*>(s_codes + k * SCAN_COLS + 2 * w.lane) = (uint16_t)pair[k];
     } else if (t0 + k < w.len) {
       uint8_t* const at = codes + ((int64_t)(t0 + k) * p.B + w.b) * p.N + w.c;
-      if (w.n_ok > 0) at[0] = (uint8_t)(pair[k] & 255u);
-      if (w.n_ok > 1) at[1] = (uint8_t)(pair[k] >> 8);
+      if (PATH == PAIRS) {
+        if (w.n_ok) *reinterpret_cast<uint16_t*>(at) = (uint16_t)pair[k];
+      } else {
+        if (w.n_ok > 0) at[0] = (uint8_t)(pair[k] & 255u);
+        if (w.n_ok > 1) at[1] = (uint8_t)(pair[k] >> 8);
+      }
     }
   }
   // lane k writes the scale of step k
@@ -275,11 +279,11 @@ __device__ __forceinline__ void keep_steps(const float2 (&v)[SCAN_K], const Scan
   if (w.lane < SCAN_K && t0 + w.lane < w.len)
     scales[((int64_t)(t0 + w.lane) * p.B + w.b) * p.n_tiles + w.col0 / KEEP_GROUP] = (uint8_t)keep_scale_byte<FORMAT>(b2 ? hi : lo);
 }
-template <bool TO_SMEM>
+template <int PATH>
 __device__ __forceinline__ void keep_steps(int format, const float2 (&v)[SCAN_K], const ScanParams& p, const Place& w, int t0, uint8_t* codes,
                                            uint8_t* scales, unsigned char* s_codes) {
-  if (format == SNN_KEEP_INT8) keep_steps<SNN_KEEP_INT8, TO_SMEM>(v, p, w, t0, codes, scales, s_codes);
-  if (format == SNN_KEEP_E4M3) keep_steps<SNN_KEEP_E4M3, TO_SMEM>(v, p, w, t0, codes, scales, s_codes);
+  if (format == SNN_KEEP_INT8) keep_steps<SNN_KEEP_INT8, PATH>(v, p, w, t0, codes, scales, s_codes);
+  if (format == SNN_KEEP_E4M3) keep_steps<SNN_KEEP_E4M3, PATH>(v, p, w, t0, codes, scales, s_codes);
 }
 // The kept values of this thread's steps; the scales' bytes lie in lanes from, from + 1, ...
 template <int FORMAT, typename IO>
@@ -303,15 +307,27 @@ __device__ __forceinline__ void decode_steps(float2 (&v)[SCAN_K], const void* ti
     for (int k = 0; k < SCAN_K; ++k) v[k] = keep_decode2<IO, FORMAT>(at[k * (SCAN_COLS / 2)], __shfl_sync(0xffffffffu, scale, from + k));
   }
 }
-template <typename IO>
-__device__ __forceinline__ void decode_from_memory(float2 (&v)[SCAN_K], const uint8_t* codes, const ScanParams& p, const Place& w, int t0,
-                                                   uint32_t bytes, int from, int format) {
+// The same straight from memory, all loads before the first use.
+template <bool IN_PAIRS>
+__device__ __forceinline__ void load_codes(uint32_t (&q)[SCAN_K], const uint8_t* codes, const ScanParams& p, const Place& w, int t0) {
 #pragma unroll
-  for (int k = 0; k < SCAN_K; ++k)
-    v[k] = decode_pair<IO>(codes + ((int64_t)min(t0 + k, w.len - 1) * p.B + w.b) * p.N, __shfl_sync(0xffffffffu, bytes, from + k), w.c, w.n_ok,
-                           format);
+  for (int k = 0; k < SCAN_K; ++k) {
+    const uint8_t* const row = codes + ((int64_t)min(t0 + k, w.len - 1) * p.B + w.b) * p.N;
+    if (IN_PAIRS) q[k] = *reinterpret_cast<const uint16_t*>(row + (w.n_ok ? w.c : 0));
+    else q[k] = (uint32_t)row[w.n_ok ? w.c : 0] | (uint32_t)row[w.n_ok == 2 ? w.c + 1 : 0] << 8;
+  }
 }
-
+template <typename IO>
+__device__ __forceinline__ void decode_loaded(float2 (&v)[SCAN_K], const uint32_t (&q)[SCAN_K], uint32_t bytes, int from, int format) {
+  const float scale = keep_scale_value(bytes);
+  if (format == SNN_KEEP_INT8) {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) v[k] = keep_decode2<IO, SNN_KEEP_INT8>(q[k], __shfl_sync(0xffffffffu, scale, from + k));
+  } else {
+#pragma unroll
+    for (int k = 0; k < SCAN_K; ++k) v[k] = keep_decode2<IO, SNN_KEEP_E4M3>(q[k], __shfl_sync(0xffffffffu, scale, from + k));
+  }
+}
 // The barriers that count the bytes of the ring's slots (TILES).
 __device__ __forceinline__ void barriers_init(uint64_t* landed) {
   if (threadIdx.x == 0) {
@@ -373,8 +389,8 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
     }
     if constexpr (KEEP) {
       unsigned char* const codes = out + WARP_PIECE * sizeof(IO);
-      keep_steps<PATH == TILES>(p.x_format, xv, p, w, t0, p.x_codes, p.x_scales, codes);
-      keep_steps<PATH == TILES>(p.gate_format, gv, p, w, t0, p.gate_codes, p.gate_scales, codes + WARP_PIECE);
+      keep_steps<PATH>(p.x_format, xv, p, w, t0, p.x_codes, p.x_scales, codes);
+      keep_steps<PATH>(p.gate_format, gv, p, w, t0, p.gate_codes, p.gate_scales, codes + WARP_PIECE);
     }
     float2 in[SCAN_K];
     coefficients(gv, in, p.mode);   // gv becomes a, and xv b
@@ -538,7 +554,10 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
       if (w.lane == 0) bulk_read_done<1>();
       __syncwarp();
     }
+    uint32_t xq[SCAN_K], gq[SCAN_K];   // codes, where they do not come by TMA
     if constexpr (PATH != TILES) {
+      if (!raw_x) load_codes<PATH == PAIRS>(xq, p.x_codes, p, w, t0);
+      if (!raw_gate) load_codes<PATH == PAIRS>(gq, p.gate_codes, p, w, t0);
       float2 v[SCAN_K];
       load_values<PATH == PAIRS>(v, dh, p.dhs[0], w, t0);
       to_raw<IO>(dr, v);
@@ -550,7 +569,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     } else {
       float2 v[SCAN_K];
       if (raw_x) load_values<PATH == PAIRS>(v, x, p.xs[0], w, t0);
-      else if (PATH != TILES) decode_from_memory<IO>(v, p.x_codes, p, w, t0, scales, 0, p.x_format);
+      else if (PATH != TILES) decode_loaded<IO>(v, xq, scales, 0, p.x_format);
       else if (p.x_format == SNN_KEEP_INT8) decode_steps<SNN_KEEP_INT8, IO>(v, at + x_at, w, scales, 0);
       else decode_steps<SNN_KEEP_E4M3, IO>(v, at + x_at, w, scales, 0);
       to_raw<IO>(xr, v);
@@ -562,7 +581,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
       if (p.gate_format == SNN_KEEP_INT8) decode_steps<SNN_KEEP_INT8, IO>(a, at + gate_at, w, scales, 8);
       else decode_steps<SNN_KEEP_E4M3, IO>(a, at + gate_at, w, scales, 8);
     } else {
-      decode_from_memory<IO>(a, p.gate_codes, p, w, t0, scales, 8, p.gate_format);
+      decode_loaded<IO>(a, gq, scales, 8, p.gate_format);
     }
     if (!alive) a[0] = nan2();
     coefficients(a, in, p.mode);
@@ -846,7 +865,8 @@ extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
   }
   ScanParams p = params_of(a);
   const size_t size = dtype_size(a->dtype);
-  const bool pairs = a->N % 2 == 0 && pairs_aligned(p.x, size, p.xs) && pairs_aligned(p.gate, size, p.gs) && pairs_aligned(p.h, size, p.hs);
+  const bool pairs = a->N % 2 == 0 && pairs_aligned(p.x, size, p.xs) && pairs_aligned(p.gate, size, p.gs) && pairs_aligned(p.h, size, p.hs) &&
+                     (uintptr_t)p.x_codes % 2 == 0 && (uintptr_t)p.gate_codes % 2 == 0;
   const cudaStream_t s = (cudaStream_t)stream;
   if (!keep && a->T <= SCAN_SHORT) {
     const int64_t blocks = ((int64_t)p.B * ((p.N + 1) / 2) + 127) / 128;
@@ -891,7 +911,8 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
   ScanParams p = params_of(a);
   const size_t size = dtype_size(a->dtype);
   const bool pairs = a->N % 2 == 0 && pairs_aligned(p.dh, size, p.dhs) && pairs_aligned(p.dx, size, p.dxs) && pairs_aligned(p.dgate, size, p.dgs) &&
-                     (!raw_x || pairs_aligned(p.x, size, p.xs)) && (!raw_gate || pairs_aligned(p.gate, size, p.gs));
+                     (!raw_x || pairs_aligned(p.x, size, p.xs)) && (!raw_gate || pairs_aligned(p.gate, size, p.gs)) &&
+                     (uintptr_t)p.x_codes % 2 == 0 && (uintptr_t)p.gate_codes % 2 == 0;
   const snn_status cut = set_segments(p, a, true);
   if (cut != SNN_OK) return cut;
   const bool tiles = pairs && a->T > 0 && value_map(&p.in[0], p.dh, a, p.dhs, SNN_SCAN_CHUNK) &&

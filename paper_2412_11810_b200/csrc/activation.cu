@@ -1,8 +1,9 @@
 // Activations in 8 bits (include/snn.h, "sequence-model operators"; the format stands in seq_common.cuh).
 //
-// Bound by HBM (bytes of a value + 1 each way).  FAST: eight lanes share a group, eight neighbouring values each, so that
-// loads and stores are 8 to 32 bytes per lane, and a warp has PACK_UNROLL x 4 groups in flight; it needs rows that are
-// multiples of 8 values and aligned to them.  Otherwise a warp takes one group at a time, two values per lane.
+// Bound by HBM (bytes of a value + 1 each way) as long as a value costs few instructions: eight lanes share a group, eight
+// values each, and a warp has PACK_UNROLL x 4 groups in flight.  FAST: 16 bytes of values per access, neighbouring lanes at
+// neighbouring addresses; it needs rows that are multiples of 8 values and aligned.  Otherwise value by value, eight
+// neighbouring ones per group and access.
 #include <algorithm>
 #include <type_traits>
 
@@ -13,105 +14,141 @@ using namespace snnk;
 namespace {
 
 constexpr int PACK_WARPS = 8, PACK_UNROLL = 4;
-template <typename IO> struct Eight;   // eight neighbouring values, in 16-byte accesses
-template <> struct Eight<float> {
-  float4 a, b;
-  __device__ float2 pair(int j) const { return j == 0 ? make_float2(a.x, a.y) : j == 1 ? make_float2(a.z, a.w) : j == 2 ? make_float2(b.x, b.y) : make_float2(b.z, b.w); }
-  __device__ void set(int j, float2 v) { if (j == 0) a.x = v.x, a.y = v.y; else if (j == 1) a.z = v.x, a.w = v.y; else if (j == 2) b.x = v.x, b.y = v.y; else b.z = v.x, b.w = v.y; }
+// Quotients by the groups of a row: a multiplication with ceil(2^64 / d) is exact while the dividend times d is below 2^64.
+struct Divisor {
+  uint64_t inverse;   // 0: the divisor is 1
+  int d;
+  __device__ __forceinline__ int64_t quotient(int64_t n) const { return inverse ? (int64_t)__umul64hi((uint64_t)n, inverse) : n; }
 };
-template <typename IO> struct alignas(16) EightHalves {
-  typename Pair<IO>::raw v[4];
-  __device__ float2 pair(int j) const { return to_f32(v[j]); }
-  __device__ void set(int j, float2 x) { set_raw(v[j], x); }
+// Place in its group of the j-th value of lane s (of eight).
+template <typename IO, bool FAST> __device__ __forceinline__ constexpr int place(int s, int j) {
+  constexpr int V = 16 / sizeof(IO);   // values per access
+  return FAST ? j / V * (8 * V) + s * V + j % V : s + 8 * j;
+}
+template <typename IO> struct alignas(16) Sixteen {
+  typename Pair<IO>::raw v[8 / sizeof(IO)];
 };
-template <> struct Eight<__nv_bfloat16> : EightHalves<__nv_bfloat16> {};
-template <> struct Eight<__half> : EightHalves<__half> {};
+// The eight values of a lane as fp32 pairs, and back; `row`: the group's first value, of which n exist.
+template <typename IO, bool FAST> struct Values {
+  Sixteen<IO> q[sizeof(IO) / 2];
+  __device__ __forceinline__ void load(const IO* row, int s, int n) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(IO) / 2; ++i) {
+      const int at = place<IO, true>(s, i * (16 / (int)sizeof(IO)));
+      q[i] = *reinterpret_cast<const Sixteen<IO>*>(row + (at < n ? at : 0));
+    }
+  }
+  __device__ __forceinline__ float2 pair(int j) const { return to_f32(q[2 * j / (16 / (int)sizeof(IO))].v[j % (8 / (int)sizeof(IO))]); }
+};
+template <typename IO> struct Values<IO, false> {
+  IO v[8];
+  __device__ __forceinline__ void load(const IO* row, int s, int n) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = row[min(s + 8 * j, n - 1)];
+  }
+  __device__ __forceinline__ float2 pair(int j) const { return make_float2(to_f32(v[2 * j]), to_f32(v[2 * j + 1])); }
+};
 
 template <typename IO, int FORMAT, bool FAST>
-__global__ void __launch_bounds__(32 * PACK_WARPS) activation_pack_kernel(const IO* values, int64_t n_rows, int n_cols, int64_t stride,
-                                                                          uint8_t* codes, uint8_t* scales) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int groups = (n_cols + KEEP_GROUP - 1) / KEEP_GROUP;
-  const int64_t n = n_rows * groups;
-  if constexpr (FAST) {
-    const int64_t step = (int64_t)gridDim.x * PACK_WARPS * 4 * PACK_UNROLL;
-    for (int64_t g0 = ((int64_t)blockIdx.x * PACK_WARPS + warp) * 4 * PACK_UNROLL + (lane >> 3); g0 - (lane >> 3) < n; g0 += step) {
-      Eight<IO> v[PACK_UNROLL];
+__global__ void __launch_bounds__(32 * PACK_WARPS, 4) activation_pack_kernel(const IO* values, int64_t n_rows, int n_cols, int64_t stride,
+                                                                             Divisor by, uint8_t* codes, uint8_t* scales) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = lane % 8;
+  const int64_t n = n_rows * by.d, step = (int64_t)gridDim.x * PACK_WARPS * 4 * PACK_UNROLL;
+  for (int64_t first = ((int64_t)blockIdx.x * PACK_WARPS + warp) * 4 * PACK_UNROLL; first < n; first += step) {
+    Values<IO, FAST> v[PACK_UNROLL];
 #pragma unroll
-      for (int u = 0; u < PACK_UNROLL; ++u) {   // (groups that do not exist: another one, not stored)
-        const int64_t g = min(g0 + 4 * u, n - 1), row = g / groups;
-        const int c = (int)(g - row * groups) * KEEP_GROUP + (lane & 7) * 8;
-        v[u] = *reinterpret_cast<const Eight<IO>*>(values + row * stride + (c < n_cols ? c : 0));
-      }
-#pragma unroll
-      for (int u = 0; u < PACK_UNROLL; ++u) {
-        const int64_t g = min(g0 + 4 * u, n - 1), row = g / groups;
-        const int group = (int)(g - row * groups), c = group * KEEP_GROUP + (lane & 7) * 8;
-        const bool on = c < n_cols;
-        float m = 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) m = larger_magnitude(m, larger_magnitude(v[u].pair(j).x, v[u].pair(j).y));
-        uint32_t top = on ? __float_as_uint(m) : 0u;
-#pragma unroll
-        for (int o = 1; o < 8; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const uint32_t byte = keep_scale_byte<FORMAT>(top);
-        const float inverse = keep_scale_inverse(byte);
-        uint2 q = make_uint2(0u, 0u);
-        if (byte != 255u) {
-          q.x = keep_encode2<FORMAT>(v[u].pair(0), inverse, top) | keep_encode2<FORMAT>(v[u].pair(1), inverse, top) << 16;
-          q.y = keep_encode2<FORMAT>(v[u].pair(2), inverse, top) | keep_encode2<FORMAT>(v[u].pair(3), inverse, top) << 16;
-        }
-        if (g0 + 4 * u < n) {
-          if (on) *reinterpret_cast<uint2*>(codes + row * n_cols + c) = q;
-          if ((lane & 7) == 0) scales[g] = (uint8_t)byte;
-        }
-      }
+    for (int u = 0; u < PACK_UNROLL; ++u) {   // (groups that do not exist: the last one again, not stored)
+      const int64_t g = min(first + 4 * u + lane / 8, n - 1), row = by.quotient(g);
+      const int c0 = (int)(g - row * by.d) * KEEP_GROUP;
+      v[u].load(values + row * stride + c0, s, n_cols - c0);
     }
-  } else for (int64_t i = (int64_t)blockIdx.x * PACK_WARPS + warp; i < n; i += (int64_t)gridDim.x * PACK_WARPS) {
-    const int64_t row = i / groups;
-    const int c = (int)(i % groups) * KEEP_GROUP + 2 * lane, n_ok = min(max(n_cols - c, 0), 2);
-    uint32_t byte;
-    const uint32_t pair = encode_row<FORMAT>(load_pair<false>(values + row * stride, c, n_ok), n_ok, byte);
-    if (n_ok > 0) codes[row * n_cols + c] = (uint8_t)(pair & 255u);
-    if (n_ok > 1) codes[row * n_cols + c + 1] = (uint8_t)(pair >> 8);
-    if (lane == 0) scales[i] = (uint8_t)byte;
+#pragma unroll
+    for (int u = 0; u < PACK_UNROLL; ++u) {
+      const int64_t wanted = first + 4 * u + lane / 8, g = min(wanted, n - 1), row = by.quotient(g);
+      const int c0 = (int)(g - row * by.d) * KEEP_GROUP, here = min(n_cols - c0, KEEP_GROUP);
+      float m = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {   // (values that do not exist are copies of others of the group)
+        const float2 f = v[u].pair(j);
+        m = larger_magnitude(m, larger_magnitude(f.x, f.y));
+      }
+      uint32_t top = __float_as_uint(m);
+#pragma unroll
+      for (int o = 1; o < 8; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const uint32_t byte = keep_scale_byte<FORMAT>(top);
+      const float inverse = keep_scale_inverse(byte);
+      const bool cut = __any_sync(0xffffffffu, keep_needs_cut<FORMAT>(top));
+      uint32_t q[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) q[j] = byte == 255u ? 0u : keep_encode2<FORMAT>(v[u].pair(j), inverse, cut);
+      if (wanted >= n) continue;
+      uint8_t* const out = codes + row * n_cols + c0;
+      if constexpr (!FAST) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (s + 8 * j < here) out[s + 8 * j] = (uint8_t)(q[j / 2] >> (8 * (j % 2)));
+      } else if constexpr (sizeof(IO) == 2) {
+        if (8 * s < here) *reinterpret_cast<uint2*>(out + 8 * s) = make_uint2(q[0] | q[1] << 16, q[2] | q[3] << 16);
+      } else {
+        if (4 * s < here) *reinterpret_cast<uint32_t*>(out + 4 * s) = q[0] | q[1] << 16;
+        if (32 + 4 * s < here) *reinterpret_cast<uint32_t*>(out + 32 + 4 * s) = q[2] | q[3] << 16;
+      }
+      if (s == 0) scales[g] = (uint8_t)byte;
+    }
   }
 }
 template <typename IO, int FORMAT, bool FAST>
-__global__ void __launch_bounds__(32 * PACK_WARPS) activation_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int64_t n_rows,
-                                                                            int n_cols, IO* values, int64_t stride) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int groups = (n_cols + KEEP_GROUP - 1) / KEEP_GROUP;
-  const int64_t n = n_rows * groups;
-  if constexpr (FAST) {
-    const int64_t step = (int64_t)gridDim.x * PACK_WARPS * 4 * PACK_UNROLL;
-    for (int64_t g0 = ((int64_t)blockIdx.x * PACK_WARPS + warp) * 4 * PACK_UNROLL + (lane >> 3); g0 - (lane >> 3) < n; g0 += step) {
-      uint2 q[PACK_UNROLL];
-      uint32_t byte[PACK_UNROLL];
+__global__ void __launch_bounds__(32 * PACK_WARPS, 4) activation_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int64_t n_rows,
+                                                                               int n_cols, Divisor by, IO* values, int64_t stride) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = lane % 8;
+  const int64_t n = n_rows * by.d, step = (int64_t)gridDim.x * PACK_WARPS * 4 * PACK_UNROLL;
+  for (int64_t first = ((int64_t)blockIdx.x * PACK_WARPS + warp) * 4 * PACK_UNROLL; first < n; first += step) {
+    uint32_t q[PACK_UNROLL][4], byte[PACK_UNROLL];
 #pragma unroll
-      for (int u = 0; u < PACK_UNROLL; ++u) {
-        const int64_t g = min(g0 + 4 * u, n - 1), row = g / groups;
-        const int c = (int)(g - row * groups) * KEEP_GROUP + (lane & 7) * 8;
-        q[u] = *reinterpret_cast<const uint2*>(codes + row * n_cols + (c < n_cols ? c : 0));
-        byte[u] = scales[g];
+    for (int u = 0; u < PACK_UNROLL; ++u) {
+      const int64_t g = min(first + 4 * u + lane / 8, n - 1), row = by.quotient(g);
+      const int c0 = (int)(g - row * by.d) * KEEP_GROUP, here = min(n_cols - c0, KEEP_GROUP);
+      const uint8_t* const in = codes + row * n_cols + c0;
+      if constexpr (!FAST) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[u][j] = (uint32_t)in[min(s + 16 * j, here - 1)] | (uint32_t)in[min(s + 16 * j + 8, here - 1)] << 8;
+      } else {
+        uint2 w;
+        if constexpr (sizeof(IO) == 2) {
+          w = *reinterpret_cast<const uint2*>(in + (8 * s < here ? 8 * s : 0));
+        } else {
+          w.x = *reinterpret_cast<const uint32_t*>(in + (4 * s < here ? 4 * s : 0));
+          w.y = *reinterpret_cast<const uint32_t*>(in + (32 + 4 * s < here ? 32 + 4 * s : 0));
+        }
+        q[u][0] = w.x & 0xffffu, q[u][1] = w.x >> 16, q[u][2] = w.y & 0xffffu, q[u][3] = w.y >> 16;
       }
+      byte[u] = scales[g];
+    }
 #pragma unroll
-      for (int u = 0; u < PACK_UNROLL; ++u) {
-        const int64_t g = min(g0 + 4 * u, n - 1), row = g / groups;
-        const int c = (int)(g - row * groups) * KEEP_GROUP + (lane & 7) * 8;
-        const float scale = keep_scale_value(byte[u]);
-        Eight<IO> v;
-        v.set(0, keep_decode2<IO, FORMAT>(q[u].x & 0xffffu, scale));
-        v.set(1, keep_decode2<IO, FORMAT>(q[u].x >> 16, scale));
-        v.set(2, keep_decode2<IO, FORMAT>(q[u].y & 0xffffu, scale));
-        v.set(3, keep_decode2<IO, FORMAT>(q[u].y >> 16, scale));
-        if (g0 + 4 * u < n && c < n_cols) *reinterpret_cast<Eight<IO>*>(values + row * stride + c) = v;
+    for (int u = 0; u < PACK_UNROLL; ++u) {
+      const int64_t wanted = first + 4 * u + lane / 8, g = min(wanted, n - 1), row = by.quotient(g);
+      const int c0 = (int)(g - row * by.d) * KEEP_GROUP, here = min(n_cols - c0, KEEP_GROUP);
+      const float scale = keep_scale_value(byte[u]);
+      if (wanted >= n) continue;
+      IO* const out = values + row * stride + c0;
+      float2 f[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[j] = keep_decode2<IO, FORMAT>(q[u][j], scale);
+      if constexpr (!FAST) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (s + 8 * j < here) out[s + 8 * j] = from_f32<IO>(j % 2 ? f[j / 2].y : f[j / 2].x);
+      } else {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(IO) / 2; ++i) {
+          Sixteen<IO> r;
+#pragma unroll
+          for (int h = 0; h < 8 / (int)sizeof(IO); ++h) set_raw(r.v[h], f[i * (8 / (int)sizeof(IO)) + h]);
+          const int at = place<IO, true>(s, i * (16 / (int)sizeof(IO)));
+          if (at < here) *reinterpret_cast<Sixteen<IO>*>(out + at) = r;
+        }
       }
     }
-  } else for (int64_t i = (int64_t)blockIdx.x * PACK_WARPS + warp; i < n; i += (int64_t)gridDim.x * PACK_WARPS) {
-    const int64_t row = i / groups;
-    const int c = (int)(i % groups) * KEEP_GROUP + 2 * lane, n_ok = min(max(n_cols - c, 0), 2);
-    store_pair<false>(values + row * stride, c, n_ok, decode_pair<IO>(codes + row * n_cols, scales[i], c, n_ok, FORMAT));
   }
 }
 
@@ -123,13 +160,18 @@ template <typename F> snn_status by_dtype(int dtype, bool pairs, F&& f) {
   return pairs ? f(__half(), std::true_type()) : f(__half(), std::false_type());
 }
 
-// whether rows can be accessed eight values at a time
-bool rows_of_eight(const void* values, int n_cols, int64_t row_stride, const uint8_t* codes) {
+// whether rows can be accessed 16 bytes of values, or eight codes, at a time
+bool rows_of_sixteen(const void* values, int n_cols, int64_t row_stride, const uint8_t* codes) {
   return n_cols % 8 == 0 && row_stride % 8 == 0 && (uintptr_t)values % 16 == 0 && (uintptr_t)codes % 8 == 0;
 }
-unsigned pack_blocks(int64_t n_rows, int n_cols, bool fast) {
-  const int64_t groups = n_rows * ((n_cols + KEEP_GROUP - 1) / KEEP_GROUP), per_block = PACK_WARPS * (fast ? 4 * PACK_UNROLL : 1);
-  return (unsigned)std::min<int64_t>((groups + per_block - 1) / per_block, 148 * 8);
+Divisor divisor_of(int n_cols) {
+  const int d = (n_cols + KEEP_GROUP - 1) / KEEP_GROUP;
+  return {d == 1 ? 0 : ~(uint64_t)0 / d + 1, d};
+}
+// four blocks fit an SM
+unsigned pack_blocks(int64_t n_rows, int n_cols) {
+  const int64_t groups = n_rows * ((n_cols + KEEP_GROUP - 1) / KEEP_GROUP), per_block = PACK_WARPS * PACK_UNROLL * 4;
+  return (unsigned)std::min<int64_t>((groups + per_block - 1) / per_block, 148 * 4);
 }
 }  // namespace
 
@@ -138,11 +180,11 @@ extern "C" snn_status snn_activation_pack(const void* values, int32_t dtype, int
   if (n_rows < 0 || n_cols < 0 || !dtype_known(dtype) || (format != SNN_KEEP_INT8 && format != SNN_KEEP_E4M3)) return SNN_ERR_INVALID_ARG;
   if (n_rows == 0 || n_cols == 0) return SNN_OK;
   if (!values || !codes || !scales) return SNN_ERR_INVALID_ARG;
-  return by_dtype(dtype, rows_of_eight(values, n_cols, row_stride, codes), [&](auto io, auto is_fast) {
+  return by_dtype(dtype, rows_of_sixteen(values, n_cols, row_stride, codes), [&](auto io, auto is_fast) {
     using IO = decltype(io);
     constexpr bool FAST = decltype(is_fast)::value;
     const auto kernel = format == SNN_KEEP_INT8 ? activation_pack_kernel<IO, SNN_KEEP_INT8, FAST> : activation_pack_kernel<IO, SNN_KEEP_E4M3, FAST>;
-    kernel<<<pack_blocks(n_rows, n_cols, FAST), 32 * PACK_WARPS, 0, (cudaStream_t)stream>>>((const IO*)values, n_rows, n_cols, row_stride, codes, scales);
+    kernel<<<pack_blocks(n_rows, n_cols), 32 * PACK_WARPS, 0, (cudaStream_t)stream>>>((const IO*)values, n_rows, n_cols, row_stride, divisor_of(n_cols), codes, scales);
     return launched();
   });
 }
@@ -152,11 +194,11 @@ extern "C" snn_status snn_activation_unpack(const uint8_t* codes, const uint8_t*
   if (n_rows < 0 || n_cols < 0 || !dtype_known(dtype) || (format != SNN_KEEP_INT8 && format != SNN_KEEP_E4M3)) return SNN_ERR_INVALID_ARG;
   if (n_rows == 0 || n_cols == 0) return SNN_OK;
   if (!values || !codes || !scales) return SNN_ERR_INVALID_ARG;
-  return by_dtype(dtype, rows_of_eight(values, n_cols, row_stride, codes), [&](auto io, auto is_fast) {
+  return by_dtype(dtype, rows_of_sixteen(values, n_cols, row_stride, codes), [&](auto io, auto is_fast) {
     using IO = decltype(io);
     constexpr bool FAST = decltype(is_fast)::value;
     const auto kernel = format == SNN_KEEP_INT8 ? activation_unpack_kernel<IO, SNN_KEEP_INT8, FAST> : activation_unpack_kernel<IO, SNN_KEEP_E4M3, FAST>;
-    kernel<<<pack_blocks(n_rows, n_cols, FAST), 32 * PACK_WARPS, 0, (cudaStream_t)stream>>>(codes, scales, n_rows, n_cols, (IO*)values, row_stride);
+    kernel<<<pack_blocks(n_rows, n_cols), 32 * PACK_WARPS, 0, (cudaStream_t)stream>>>(codes, scales, n_rows, n_cols, divisor_of(n_cols), (IO*)values, row_stride);
     return launched();
   });
 }

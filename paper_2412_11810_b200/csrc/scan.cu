@@ -53,26 +53,6 @@ struct ScanParams {
   uint8_t *x_codes, *x_scales, *gate_codes, *gate_scales;
 };
 
-// ---- pairs of channels ---------------------------------------------------------------------------------------
-__device__ __forceinline__ uint64_t bits2(float2 v) { return (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x); }
-__device__ __forceinline__ float2 from_bits2(uint64_t u) { return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32))); }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  uint64_t d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
-  return from_bits2(d);
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
-  return from_bits2(d);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
-  return from_bits2(d);
-}
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-
 struct Map2 {   // the affine maps of two channels
   float2 a, b;
 };
@@ -255,7 +235,7 @@ __device__ __forceinline__ void keep_steps(const float2 (&v)[SCAN_K], const Scan
 #pragma unroll
     for (int k = 0; k < SCAN_K; ++k) {
       const uint32_t byte = keep_scale_byte<FORMAT>(top[k]);
-      pair[k] = byte == 255u ? 0u : keep_encode2<FORMAT>(v[k], keep_scale_inverse(byte), top[k]);
+      pair[k] = byte == 255u ? 0u : keep_encode2<FORMAT>(v[k], keep_scale_inverse(byte), keep_needs_cut<FORMAT>(top[k]));
     }
   }
 #pragma unroll

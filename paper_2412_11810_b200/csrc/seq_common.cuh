@@ -59,6 +59,26 @@ __device__ __forceinline__ void store_pair(IO* row, int c, int n_ok, float2 v) {
   if (n_ok > 1) row[c + 1] = from_f32<IO>(v.y);
 }
 
+// ---- pairs of fp32 values --------------------------------------------------------------------------------
+__device__ __forceinline__ uint64_t bits2(float2 v) { return (uint64_t)__float_as_uint(v.y) << 32 | __float_as_uint(v.x); }
+__device__ __forceinline__ float2 from_bits2(uint64_t u) { return make_float2(__uint_as_float((uint32_t)u), __uint_as_float((uint32_t)(u >> 32))); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits2(a)), "l"(bits2(b)));
+  return from_bits2(d);
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
 // ---- 8-bit codes -------------------------------------------------------------------------------------------
 // Scale byte of a group whose largest magnitude has the bit pattern `top` (NaN sorts above infinity above the rest).
 template <int FORMAT> __device__ __forceinline__ uint32_t keep_scale_byte(uint32_t top) {
@@ -74,21 +94,22 @@ __device__ __forceinline__ float keep_scale_inverse(uint32_t c) { return __uint_
 __device__ __forceinline__ float keep_scale_value(uint32_t c) {
   return __uint_as_float(c == 0u ? 0x00400000u : c == 255u ? 0x7fc00000u : c << 23);
 }
-// Two code bytes, low first.  `top` is the group's largest magnitude, as in keep_scale_byte.
-template <int FORMAT> __device__ __forceinline__ uint32_t keep_encode2(float2 v, float inverse, uint32_t top) {
-  const float a = __fmul_rn(v.x, inverse), b = __fmul_rn(v.y, inverse);
+// Whether an int8 code of a group could round to 128 and has to be cut.
+template <int FORMAT> __device__ __forceinline__ bool keep_needs_cut(uint32_t top) {
+  return FORMAT == SNN_KEEP_INT8 && (top & 0x7fffffu) >= 0x7f0000u;
+}
+// Two code bytes, low first.
+template <int FORMAT> __device__ __forceinline__ uint32_t keep_encode2(float2 v, float inverse, bool cut) {
+  const float2 u = mul2(v, both(inverse));
   if (FORMAT == SNN_KEEP_INT8) {
     // adding 1.5 x 2^23 rounds to an integer (nearest even) and leaves it in the low bits: no conversion instructions,
     // which run at a quarter of the rate
     const float magic = 12582912.f;
-    float i = __fadd_rn(a, magic), j = __fadd_rn(b, magic);
-    if ((top & 0x7fffffu) >= 0x7f0000u) {   // only then can a value round to 128
-      i = fminf(fmaxf(i, magic - 127.f), magic + 127.f);
-      j = fminf(fmaxf(j, magic - 127.f), magic + 127.f);
-    }
-    return __byte_perm(__float_as_uint(i), __float_as_uint(j), 0x0040) & 0xffffu;
+    float2 r = add2(u, both(magic));
+    if (cut) r = make_float2(fminf(fmaxf(r.x, magic - 127.f), magic + 127.f), fminf(fmaxf(r.y, magic - 127.f), magic + 127.f));
+    return __byte_perm(__float_as_uint(r.x), __float_as_uint(r.y), 0x0040) & 0xffffu;
   }
-  return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(u, __NV_SATFINITE, __NV_E4M3);
 }
 template <typename IO> __device__ __forceinline__ float largest_finite();
 template <> __device__ __forceinline__ float largest_finite<float>() { return __uint_as_float(0x7f7fffffu); }
@@ -111,20 +132,6 @@ __device__ __forceinline__ float larger_magnitude(float a, float b) {
   float m;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(fabsf(a)), "f"(fabsf(b)));
   return m;
-}
-
-// The scale and this lane's two codes of a row of 64 values, two per lane.  Called by whole warps.
-template <int FORMAT> __device__ __forceinline__ uint32_t encode_row(float2 v, int n_ok, uint32_t& byte) {
-  const float m = larger_magnitude(n_ok > 0 ? v.x : 0.f, n_ok > 1 ? v.y : 0.f);
-  const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(m));   // bit patterns of magnitudes sort as they do
-  byte = keep_scale_byte<FORMAT>(top);
-  return byte == 255u ? 0u : keep_encode2<FORMAT>(v, keep_scale_inverse(byte), top);
-}
-template <typename IO>
-__device__ __forceinline__ float2 decode_pair(const uint8_t* row, uint32_t scale, int c, int n_ok, int format) {
-  const uint32_t pair = (uint32_t)row[n_ok ? c : 0] | (uint32_t)row[n_ok == 2 ? c + 1 : 0] << 8;
-  return format == SNN_KEEP_INT8 ? keep_decode2<IO, SNN_KEEP_INT8>(pair, keep_scale_value(scale))
-                                 : keep_decode2<IO, SNN_KEEP_E4M3>(pair, keep_scale_value(scale));
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------

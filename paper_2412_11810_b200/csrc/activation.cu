@@ -50,7 +50,7 @@ template <typename IO> struct Values<IO, false> {
 };
 
 template <typename IO, int FORMAT, bool FAST>
-__global__ void __launch_bounds__(32 * PACK_WARPS, 4) activation_pack_kernel(const IO* values, int64_t n_rows, int n_cols, int64_t stride,
+__global__ void __launch_bounds__(32 * PACK_WARPS, 3) activation_pack_kernel(const IO* values, int64_t n_rows, int n_cols, int64_t stride,
                                                                              Divisor by, uint8_t* codes, uint8_t* scales) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = lane % 8;
   const int64_t n = n_rows * by.d, step = (int64_t)gridDim.x * PACK_WARPS * 4 * PACK_UNROLL;
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(32 * PACK_WARPS, 4) activation_pack_kernel(con
   }
 }
 template <typename IO, int FORMAT, bool FAST>
-__global__ void __launch_bounds__(32 * PACK_WARPS, 4) activation_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int64_t n_rows,
+__global__ void __launch_bounds__(32 * PACK_WARPS, 3) activation_unpack_kernel(const uint8_t* codes, const uint8_t* scales, int64_t n_rows,
                                                                                int n_cols, Divisor by, IO* values, int64_t stride) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, s = lane % 8;
   const int64_t n = n_rows * by.d, step = (int64_t)gridDim.x * PACK_WARPS * 4 * PACK_UNROLL;
@@ -168,10 +168,10 @@ Divisor divisor_of(int n_cols) {
   const int d = (n_cols + KEEP_GROUP - 1) / KEEP_GROUP;
   return {d == 1 ? 0 : ~(uint64_t)0 / d + 1, d};
 }
-// four blocks fit an SM
+// three blocks fit an SM
 unsigned pack_blocks(int64_t n_rows, int n_cols) {
   const int64_t groups = n_rows * ((n_cols + KEEP_GROUP - 1) / KEEP_GROUP), per_block = PACK_WARPS * PACK_UNROLL * 4;
-  return (unsigned)std::min<int64_t>((groups + per_block - 1) / per_block, 148 * 4);
+  return (unsigned)std::min<int64_t>((groups + per_block - 1) / per_block, 148 * 3);
 }
 }  // namespace
 

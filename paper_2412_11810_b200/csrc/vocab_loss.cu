@@ -28,12 +28,15 @@ namespace {
 
 constexpr uint32_t VL_TIMEOUT = 1u;               // status bit: a bounded wait ran out
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int VL_EPILOGUE_WARPS = 4;
-constexpr int VL_THREADS = 32 * (2 + VL_EPILOGUE_WARPS);
-constexpr uint32_t VL_STORE_BYTES = UM_HALF * 128;           // one staged block of dz: 128 rows x 64 values
+// Warps of the epilogue: one per quarter of tensor memory's lanes, or two with half of the tile's columns each.  Two hide
+// the epilogue's latency where the contraction is short and the epilogue sets the pace (8192 x 64 x 65536 bf16 forward: 403
+// us with four warps, 336 with eight); where it is long four leave more of the SM to the products (8192 x 2048 x 131072
+// backward: 9.3 ms against 9.8).
+constexpr int VL_SHORT = 16;                                 // k-blocks x products of parts: eight warps below
+constexpr uint32_t VL_STORE_BYTES = UM_HALF * 128;           // one staged block of dz per half: 128 rows x 64 values
 constexpr size_t VL_SMEM = 1024 + (size_t)UM_STAGES * UM_STAGE_BYTES + 2 * VL_STORE_BYTES + 256;
 constexpr float FP16_DZ_SCALE = 16384.f;   // dz / (gradient of the row loss) lies in [-1, 1]; as fp16 it keeps small values better after this
-constexpr size_t PIECE_BYTES = (size_t)256 << 20;            // dz held at a time
+constexpr size_t PIECE_BYTES = (size_t)512 << 20;            // dz held at a time
 constexpr int MAX_SPLITS = 32;
 
 enum Epilogue { STATS, GRAD, DX, DW };
@@ -53,7 +56,7 @@ struct ProductParams {
   int64_t ignore_index;
   int classes;
   float z_scale;              // times log2 e: exponents of 2
-  float2* partial;            // [tile_n][rows]
+  float2* partial;            // [tile_n][halves][rows]
   float* target_z;            // [rows], in units of log 2
   const float* lse;
   int planes;
@@ -135,8 +138,9 @@ template <int EPI> __device__ __forceinline__ Unit unit_of(const ProductParams& 
   return w;
 }
 
-template <int EPI, bool A_MN, bool B_MN>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) product_kernel(const __grid_constant__ ProductParams p) {
+template <int EPI, bool A_MN, bool B_MN, int WARPS>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1) product_kernel(const __grid_constant__ ProductParams p) {
+  constexpr int HALVES = WARPS / 4, WIDTH = UM_TILE / HALVES;   // columns per warp of the epilogue
   extern __shared__ unsigned char s_raw[];
   unsigned char* const s_base = s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u);
   unsigned char* const s_store = s_base + (size_t)UM_STAGES * UM_STAGE_BYTES;
@@ -153,7 +157,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.acc_full[i], 1);
-      mbar_init(&s.acc_empty[i], 2 * VL_EPILOGUE_WARPS);
+      mbar_init(&s.acc_empty[i], 2 * WARPS);
     }
     s.gave_up = 0;
     mbar_fence_init();
@@ -214,12 +218,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
     }
   } else {
     // ---- epilogue: a thread has one row of this block's half of the tile
-    const int quarter = warp & 3, row_in_block = quarter * 32 + lane;
+    const int quarter = warp & 3, row_in_block = quarter * 32 + lane, half = (warp - 2) / 4, half_col0 = half * WIDTH;
+    const bool storer = threadIdx.x == 64 + 128 * half;   // of the half's dz blocks
+    int store_buf = half;
     const float alpha = EPI == DW ? *p.alpha * (p.tops ? operand_unscale(p.tops[0]) : 1.f) : 0.f;
     const float z_scale = p.tops ? p.z_scale * operand_unscale(p.tops[0]) * operand_unscale(p.tops[1]) : p.z_scale;
     int tile = 0;
     bool ok = true;
-    int store_buf = 0;
     for (int u = pair; u < units && ok; u += n_pairs_sm, ++tile) {
       const Unit w = unit_of<EPI>(p, u);
       const int buf = tile & 1;
@@ -230,16 +235,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
           for (; u < units; u += n_pairs_sm) {
             const Unit left = unit_of<EPI>(p, u);
             const int row = left.m * UM_TILE + (int)rank * UM_HALF + row_in_block;
-            if (row < p.m) p.partial[(int64_t)left.n * p.m + row] = make_float2(nan, nan);
+            if (row < p.m) p.partial[((int64_t)left.n * HALVES + half) * p.m + row] = make_float2(nan, nan);
           }
         }
         break;
       }
       tcgen05_after_sync();
-      const uint32_t acc = tmem + (uint32_t)buf * UM_TILE + ((uint32_t)(32 * quarter) << 16);
+      const uint32_t acc = tmem + (uint32_t)(buf * UM_TILE + half_col0) + ((uint32_t)(32 * quarter) << 16);
       const int block_row0 = w.m * UM_TILE + (int)rank * UM_HALF;
       const int row = block_row0 + row_in_block;          // within A's rows
-      const int col0 = w.n * UM_TILE, cols = min(p.n - col0, UM_TILE);
+      const int col0 = w.n * UM_TILE + half_col0, cols = max(min(p.n - col0, WIDTH), 0);   // of this warp's half
       const bool row_on = row < p.m;
       if constexpr (EPI == STATS) {
         const int target = row_on ? target_of(p.targets, p.target_bits, p.ignore_index, p.classes, row) - (p.b0 + col0) : -1;
@@ -269,7 +274,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
           sum = sum * exp2_fast(top - at) + part;
           top = m;
         }
-        if (row_on) p.partial[(int64_t)w.n * p.m + row] = make_float2(top, sum);
+        if (row_on) p.partial[((int64_t)w.n * HALVES + half) * p.m + row] = make_float2(top, sum);
       }
       if constexpr (EPI == GRAD) {
         const int target = row_on ? target_of(p.targets, p.target_bits, p.ignore_index, p.classes, row) : -1;
@@ -291,9 +296,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
             for (int j = 0; j < 64; ++j) v[j] *= FP16_DZ_SCALE;
           }
           for (int plane = 0; plane < p.planes; ++plane) {
-            // the buffer's previous store has to have read it
-            if (tid == 64) bulk_read_done<1>();
-            asm volatile("bar.sync 1, %0;" ::"n"(32 * VL_EPILOGUE_WARPS) : "memory");
+            // the buffer's previous store has to have read it (there are two buffers: one per half, or both for all)
+            if (storer) bulk_read_done<HALVES == 1 ? 1 : 0>();
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
             unsigned char* const out = s_store + store_buf * VL_STORE_BYTES + row_in_block * 128;
 #pragma unroll
             for (int g = 0; g < 8; ++g) {   // 16-byte pieces, swizzled as the tensor map says
@@ -317,10 +322,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
               *reinterpret_cast<uint4*>(out + ((g ^ (row_in_block & 7)) << 4)) = make_uint4(q[0], q[1], q[2], q[3]);
             }
             fence_proxy_async_smem();
-            asm volatile("bar.sync 1, %0;" ::"n"(32 * VL_EPILOGUE_WARPS) : "memory");
-            if (tid == 64 && block_row0 < p.m) tma_store_3d(&p.out, col0 + c, block_row0, plane, s_store + store_buf * VL_STORE_BYTES);
-            if (tid == 64) bulk_commit();
-            store_buf ^= 1;
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+            if (storer && block_row0 < p.m) tma_store_3d(&p.out, col0 + c, block_row0, plane, s_store + store_buf * VL_STORE_BYTES);
+            if (storer) bulk_commit();
+            if (HALVES == 1) store_buf ^= 1;
           }
         }
       }
@@ -352,17 +357,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
           for (int j = 0; j < 32; ++j) v[j] *= alpha;
           if (!p.dw_vector || cols - c < 32) {
             // odd strides, the last columns: through shared memory, so that a warp stores along a row
-            float* const mine = reinterpret_cast<float*>(s_store) + quarter * (32 * 33);
+            // (places exchanged within a row, so that both ways use all banks)
+            float* const mine = reinterpret_cast<float*>(s_store) + (warp - 2) * (32 * 32);
             __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) mine[lane * 33 + j] = v[j];
+            for (int j = 0; j < 32; ++j) mine[lane * 32 + (j ^ lane)] = v[j];
             __syncwarp();
             const int first = block_row0 + quarter * 32, n_rows = min(p.m - first, 32);
             if (c + lane < cols) {
               const int64_t at = (int64_t)first * p.dw_stride + col0 + c + lane;
 #pragma unroll 4
               for (int r = 0; r < n_rows; ++r) {
-                const float f = mine[r * 33 + lane];
+                const float f = mine[r * 32 + (lane ^ r)];
                 const int64_t to = at + r * p.dw_stride;
                 if (p.dw_dtype == SNN_DTYPE_FP32) ((float*)p.dw)[to] = f;
                 else if (p.dw_dtype == SNN_DTYPE_BF16) ((__nv_bfloat16*)p.dw)[to] = __float2bfloat16_rn(f);
@@ -401,7 +407,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VL_THREADS, 1) produ
       __syncwarp();
       if (lane == 0) mbar_arrive_at(peer_address(smem_u32(&s.acc_empty[buf]), 0));
     }
-    if (EPI == GRAD && tid == 64) bulk_done();
+    if (EPI == GRAD && storer) bulk_done();
   }
   // After a wait that ran out, copies and products may still be under way: give them time to land.
   __syncwarp();
@@ -872,7 +878,7 @@ Layout layout_of(const snn_vocab_loss_args* a, bool backward, int pairs) {
   if (backward || !few_rows(a)) l.x = operand(a->x, a->x_stride, a->rows, a->dim, backward);
   if (backward || !few_rows(a)) l.w = operand(a->w, a->w_stride, by_class ? a->classes : a->dim, by_class ? a->dim : a->classes, false);
   if (!backward) {
-    l.partial = take(sizeof(float2) * (size_t)a->rows * (few_rows(a) ? few_blocks(a) : ceil_div(a->classes, UM_TILE)));
+    l.partial = take(sizeof(float2) * (size_t)a->rows * (few_rows(a) ? few_blocks(a) : 2 * ceil_div(a->classes, UM_TILE)));
     l.target_z = take(sizeof(float) * (size_t)a->rows);
     l.row_loss = take(sizeof(float) * (size_t)a->rows);
   } else {
@@ -906,13 +912,19 @@ snn_status check(const snn_vocab_loss_args* a) {
 }
 bool is_bf16(int dtype) { return dtype == SNN_DTYPE_BF16; }   // (fp32: fp16 planes)
 
-template <int EPI, bool A_MN, bool B_MN> snn_status launch_product(const ProductParams& p, int pairs, cudaStream_t stream) {
-  const auto kernel = product_kernel<EPI, A_MN, B_MN>;
+template <int EPI, bool A_MN, bool B_MN, int WARPS> snn_status launch_product(const ProductParams& p, int pairs, cudaStream_t stream) {
+  const auto kernel = product_kernel<EPI, A_MN, B_MN, WARPS>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)VL_SMEM) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
   const int64_t units = (int64_t)p.tiles_m * p.tiles_n * p.splits;
   if (units > INT32_MAX / 2) return SNN_ERR_UNSUPPORTED;
-  kernel<<<2 * (unsigned)std::min<int64_t>(units, pairs), VL_THREADS, VL_SMEM, stream>>>(p);
+  kernel<<<2 * (unsigned)std::min<int64_t>(units, pairs), 32 * (2 + WARPS), VL_SMEM, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+}
+bool short_contraction(const ProductParams& p) { return p.kblocks * p.n_pairs < VL_SHORT; }
+// z products: B is w, by class (K-major) or by feature
+template <int EPI> snn_status launch_z(const ProductParams& p, bool by_class, int pairs, cudaStream_t stream) {
+  if (short_contraction(p)) return by_class ? launch_product<EPI, false, false, 8>(p, pairs, stream) : launch_product<EPI, false, true, 8>(p, pairs, stream);
+  return by_class ? launch_product<EPI, false, false, 4>(p, pairs, stream) : launch_product<EPI, false, true, 4>(p, pairs, stream);
 }
 
 struct Call {
@@ -1048,8 +1060,8 @@ extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void*
   p.n = a->classes;
   p.partial = (float2*)(c.ws + c.l.partial);
   p.target_z = (float*)(c.ws + c.l.target_z);
-  VL_TRY((by_class ? launch_product<STATS, false, false>(p, c.pairs, c.stream) : launch_product<STATS, false, true>(p, c.pairs, c.stream)));
-  return c.row_losses(p.partial, p.tiles_n, p.target_z);
+  VL_TRY(launch_z<STATS>(p, by_class, c.pairs, c.stream));
+  return c.row_losses(p.partial, (short_contraction(p) ? 2 : 1) * p.tiles_n, p.target_z);
 }
 
 extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void* stream) {
@@ -1083,7 +1095,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     p.tiles_m = ceil_div(a->rows, UM_TILE); p.tiles_n = ceil_div(width, UM_TILE); p.kblocks = ceil_div(a->dim, UM_KB);
     p.m = a->rows; p.n = width; p.b0 = v0;
     p.lse = a->lse;
-    VL_TRY((by_class ? launch_product<GRAD, false, false>(p, c.pairs, c.stream) : launch_product<GRAD, false, true>(p, c.pairs, c.stream)));
+    VL_TRY(launch_z<GRAD>(p, by_class, c.pairs, c.stream));
     p = base;                 // dx += dz w^T
     p.a = dz_k; p.b = w_dx;
     p.tiles_m = ceil_div(a->rows, UM_TILE); p.tiles_n = ceil_div(a->dim, UM_TILE); p.kblocks = ceil_div(width, UM_KB);
@@ -1091,7 +1103,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     p.bk0 = v0;
     p.m = a->rows; p.n = a->dim;
     p.acc = (float*)(c.ws + l.acc); p.acc_pitch = l.acc_pitch; p.acc_split = l.acc_split; p.accumulate = v0 > 0;
-    VL_TRY((by_class ? launch_product<DX, false, true>(p, c.pairs, c.stream) : launch_product<DX, false, false>(p, c.pairs, c.stream)));
+    VL_TRY((by_class ? launch_product<DX, false, true, 4>(p, c.pairs, c.stream) : launch_product<DX, false, false, 4>(p, c.pairs, c.stream)));
     p = base;                 // the piece's part of dw
     p.kblocks = ceil_div(a->rows, UM_KB);
     p.alpha = c.alpha();
@@ -1107,7 +1119,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     }
     p.dw_vector = (uintptr_t)p.dw % 16 == 0 && p.dw_stride * (int64_t)size % 16 == 0;
     p.tiles_m = ceil_div(p.m, UM_TILE); p.tiles_n = ceil_div(p.n, UM_TILE);
-    VL_TRY((launch_product<DW, true, true>(p, c.pairs, c.stream)));
+    VL_TRY((launch_product<DW, true, true, 4>(p, c.pairs, c.stream)));
   }
   const int splits = std::min(l.splits, ceil_div(std::min(l.piece, a->classes), UM_KB));
   const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a->dim, 1024), 64), (unsigned)std::min(a->rows, 16384));

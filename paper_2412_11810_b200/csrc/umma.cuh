@@ -110,6 +110,18 @@ __device__ __forceinline__ void tmem_load_32(uint32_t taddr, float (&v)[32]) {
       : "r"(taddr) : "memory");
 }
 
+// The same for 16 columns.
+__device__ __forceinline__ void tmem_load_16(uint32_t taddr, float (&v)[16]) {
+  __syncwarp();
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]),
+        "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(taddr) : "memory");
+}
+
 // Host side: a 3-D tensor map [planes][rows][cols] of 16-bit values, rows `pitch` values apart (a multiple of 8), box of
 // 64 columns (128 bytes, 128-byte swizzle) x box_rows.
 inline bool make_tensor_map_16bit(CUtensorMap* out, const void* base, bool bf16, uint64_t cols, uint64_t rows, uint64_t planes,

@@ -32,7 +32,8 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // the epilogue's latency where the contraction is short and the epilogue sets the pace (8192 x 64 x 65536 bf16 forward: 403
 // us with four warps, 336 with eight); where it is long four leave more of the SM to the products (8192 x 2048 x 131072
 // backward: 9.3 ms against 9.8).
-constexpr int VL_SHORT = 16;                                 // k-blocks x products of parts: eight warps below
+constexpr int VL_RUN = 8;                                    // k-blocks per run (fp32 operands)
+constexpr int VL_SHORT = 16;                                 // k-blocks: eight warps below
 constexpr uint32_t VL_STORE_BYTES = UM_HALF * 128;           // one staged block of dz per half: 128 rows x 64 values
 constexpr size_t VL_SMEM = 1024 + (size_t)UM_STAGES * UM_STAGE_BYTES + 2 * VL_STORE_BYTES + 256;
 constexpr float FP16_DZ_SCALE = 16384.f;   // dz / (gradient of the row loss) lies in [-1, 1]; as fp16 it keeps small values better after this
@@ -40,6 +41,9 @@ constexpr size_t PIECE_BYTES = (size_t)512 << 20;            // dz held at a tim
 constexpr int MAX_SPLITS = 32;
 
 enum Epilogue { STATS, GRAD, DX, DW };
+// The tensor cores do not round a sum to nearest, and what they cut adds up over a long contraction: 5e-6 of the result
+// after 8000 terms, where fp32 should have a tenth of that.  So for fp32 operands (RUNS) the epilogue takes over the
+// accumulator after every VL_RUN k-blocks and adds it to sums in its registers; the other accumulator fills meanwhile.
 
 struct ProductParams {
   CUtensorMap a, b, out;      // out: GRAD only
@@ -138,9 +142,10 @@ template <int EPI> __device__ __forceinline__ Unit unit_of(const ProductParams& 
   return w;
 }
 
-template <int EPI, bool A_MN, bool B_MN, int WARPS>
+template <int EPI, bool A_MN, bool B_MN, int WARPS, bool RUNS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1) product_kernel(const __grid_constant__ ProductParams p) {
   constexpr int HALVES = WARPS / 4, WIDTH = UM_TILE / HALVES;   // columns per warp of the epilogue
+  static_assert(!RUNS || HALVES == 2, "a thread's sums fit its registers");
   extern __shared__ unsigned char s_raw[];
   unsigned char* const s_base = s_raw + ((1024u - (smem_u32(s_raw) & 1023u)) & 1023u);
   unsigned char* const s_store = s_base + (size_t)UM_STAGES * UM_STAGE_BYTES;
@@ -193,27 +198,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {   // products, of both blocks
       const uint32_t idesc = f16_instruction(p.bf16, A_MN, B_MN);
-      int it = 0, tile = 0;
+      int it = 0, run = 0;
       bool ok = true;
-      for (int u = pair; u < units && ok; u += n_pairs_sm, ++tile) {
+      for (int u = pair; u < units && ok; u += n_pairs_sm) {
         const Unit w = unit_of<EPI>(p, u);
-        const int buf = tile & 1;
-        if (tile >= 2 && !(ok = wait_for(&s.acc_empty[buf], (uint32_t)(tile / 2 - 1) & 1u, s, p.status))) break;
-        tcgen05_after_sync();
-        const uint32_t acc = tmem + (uint32_t)buf * UM_TILE;
         const int n_it = p.n_pairs * w.kbs;
-        for (int i = 0; i < n_it; ++i, ++it) {
-          const int st = it % UM_STAGES;
-          if (!(ok = wait_for(&s.full[st], (uint32_t)(it / UM_STAGES) & 1u, s, p.status))) break;
+        for (int i0 = 0; i0 < n_it && ok; i0 += RUNS ? VL_RUN : n_it, ++run) {   // a run of k-blocks into one accumulator
+          const int buf = run & 1, end = RUNS ? min(i0 + VL_RUN, n_it) : n_it;
+          if (run >= 2 && !(ok = wait_for(&s.acc_empty[buf], (uint32_t)(run / 2 - 1) & 1u, s, p.status))) break;
           tcgen05_after_sync();
-          const uint32_t at = smem_u32(s_base + (size_t)st * UM_STAGE_BYTES);
+          const uint32_t acc = tmem + (uint32_t)buf * UM_TILE;
+          for (int i = i0; i < end; ++i, ++it) {
+            const int st = it % UM_STAGES;
+            if (!(ok = wait_for(&s.full[st], (uint32_t)(it / UM_STAGES) & 1u, s, p.status))) break;
+            tcgen05_after_sync();
+            const uint32_t at = smem_u32(s_base + (size_t)st * UM_STAGE_BYTES);
 #pragma unroll
-          for (int j = 0; j < UM_KB / 16; ++j)
-            pair_mma_f16(acc, operand_descriptor<A_MN>(at + j * kstep_bytes<A_MN>()),
-                         operand_descriptor<B_MN>(at + UM_OPERAND_BYTES + j * kstep_bytes<B_MN>()), idesc, i > 0 || j > 0);
-          pair_commit(&s.empty[st]);
+            for (int j = 0; j < UM_KB / 16; ++j)
+              pair_mma_f16(acc, operand_descriptor<A_MN>(at + j * kstep_bytes<A_MN>()),
+                           operand_descriptor<B_MN>(at + UM_OPERAND_BYTES + j * kstep_bytes<B_MN>()), idesc, i > i0 || j > 0);
+            pair_commit(&s.empty[st]);
+          }
+          if (ok) pair_commit(&s.acc_full[buf]);
         }
-        if (ok) pair_commit(&s.acc_full[buf]);
       }
     }
   } else {
@@ -223,12 +230,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
     int store_buf = half;
     const float alpha = EPI == DW ? *p.alpha * (p.tops ? operand_unscale(p.tops[0]) : 1.f) : 0.f;
     const float z_scale = p.tops ? p.z_scale * operand_unscale(p.tops[0]) * operand_unscale(p.tops[1]) : p.z_scale;
-    int tile = 0;
+    int run = 0;
     bool ok = true;
-    for (int u = pair; u < units && ok; u += n_pairs_sm, ++tile) {
+    float sums[RUNS ? WIDTH : 1];
+    // the run's accumulator is complete / may be filled again
+    auto run_full = [&]() { return __all_sync(0xffffffffu, wait_for(&s.acc_full[run & 1], (uint32_t)(run / 2) & 1u, s, p.status)); };
+    auto run_read = [&]() {
+      tcgen05_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_at(peer_address(smem_u32(&s.acc_empty[run & 1]), 0));
+      ++run;
+    };
+    auto accumulator = [&]() { return tmem + (uint32_t)((run & 1) * UM_TILE + half_col0) + ((uint32_t)(32 * quarter) << 16); };
+    for (int u = pair; u < units && ok; u += n_pairs_sm) {
       const Unit w = unit_of<EPI>(p, u);
-      const int buf = tile & 1;
-      ok = __all_sync(0xffffffffu, wait_for(&s.acc_full[buf], (uint32_t)(tile / 2) & 1u, s, p.status));
+      if constexpr (RUNS) {
+        const int n_runs = (p.n_pairs * w.kbs + VL_RUN - 1) / VL_RUN;
+#pragma unroll
+        for (int j = 0; j < WIDTH; ++j) sums[j] = 0.f;
+#pragma unroll 1
+        for (int r = 0; r < n_runs && (ok = run_full()); ++r) {
+          tcgen05_after_sync();
+#pragma unroll
+          for (int c = 0; c < WIDTH; c += 16) {
+            float v[16];
+            tmem_load_16(accumulator() + c, v);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sums[c + j] += v[j];
+          }
+          run_read();
+        }
+      } else {
+        ok = run_full();
+      }
       if (!ok) {
         if (EPI == STATS) {   // the rows' losses become NaN
           const float nan = __uint_as_float(0x7fc00000u);
@@ -241,36 +275,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
         break;
       }
       tcgen05_after_sync();
-      const uint32_t acc = tmem + (uint32_t)(buf * UM_TILE + half_col0) + ((uint32_t)(32 * quarter) << 16);
+      const uint32_t acc = accumulator();
       const int block_row0 = w.m * UM_TILE + (int)rank * UM_HALF;
       const int row = block_row0 + row_in_block;          // within A's rows
       const int col0 = w.n * UM_TILE + half_col0, cols = max(min(p.n - col0, WIDTH), 0);   // of this warp's half
       const bool row_on = row < p.m;
+      // the j-th column from c on: in registers already, or loaded from tensor memory
+#define V(j) (RUNS ? sums[RUNS ? c + (j) : 0] : loaded[RUNS ? 0 : (j)])
       if constexpr (EPI == STATS) {
         const int target = row_on ? target_of(p.targets, p.target_bits, p.ignore_index, p.classes, row) - (p.b0 + col0) : -1;
         float top = -INFINITY, sum = 0.f;
-        for (int c = 0; c < cols; c += 32) {
-          float v[32];
-          tmem_load_32(acc + c, v);
+#pragma unroll(RUNS ? WIDTH / 32 : 1)
+        for (int c = 0; c < WIDTH; c += 32) {
+          if (c >= cols) continue;
+          float loaded[RUNS ? 1 : 32];
+          if constexpr (!RUNS) tmem_load_32(acc + c, loaded);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = v[j] * z_scale;
+          for (int j = 0; j < 32; ++j) V(j) = V(j) * z_scale;
           if (target >= c && target < c + 32) {
             float z = 0.f;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) z = c + j == target ? v[j] : z;
+            for (int j = 0; j < 32; ++j) z = c + j == target ? V(j) : z;
             p.target_z[row] = z;
           }
           if (cols - c < 32) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = c + j < cols ? v[j] : -INFINITY;
+            for (int j = 0; j < 32; ++j) V(j) = c + j < cols ? V(j) : -INFINITY;
           }
           float m = top;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) m = fmaxf(m, v[j]);
+          for (int j = 0; j < 32; ++j) m = fmaxf(m, V(j));
           const float at = m == -INFINITY ? 0.f : m;
           float part = 0.f;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) part += exp2_fast(v[j] - at);
+          for (int j = 0; j < 32; ++j) part += exp2_fast(V(j) - at);
           sum = sum * exp2_fast(top - at) + part;
           top = m;
         }
@@ -280,20 +318,26 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
         const int target = row_on ? target_of(p.targets, p.target_bits, p.ignore_index, p.classes, row) : -1;
         const bool counts = target >= 0;
         const int target_col = target - (p.b0 + col0);
-        const float lse2 = counts ? p.lse[row] * LOG2E : 0.f;
-        for (int c = 0; c < cols; c += 64) {
-          float v[64];
-          tmem_load_32(acc + c, *reinterpret_cast<float(*)[32]>(&v[0]));
-          tmem_load_32(acc + c + 32, *reinterpret_cast<float(*)[32]>(&v[32]));
+        // lse log2 e in two parts: the second, what rounding the first leaves, as a factor
+        const double lse2_exact = counts ? (double)p.lse[row] * 1.4426950408889634074 : 0.;
+        const float lse2 = (float)lse2_exact, rest = 1.f - (float)(lse2_exact - (double)lse2) * LN2;
+#pragma unroll(RUNS ? WIDTH / 64 : 1)
+        for (int c = 0; c < WIDTH; c += 64) {
+          if (c >= cols) continue;
+          float loaded[RUNS ? 1 : 64];
+          if constexpr (!RUNS) {
+            tmem_load_32(acc + c, *reinterpret_cast<float(*)[32]>(&loaded[0]));
+            tmem_load_32(acc + c + 32, *reinterpret_cast<float(*)[32]>(&loaded[32]));
+          }
 #pragma unroll
-          for (int j = 0; j < 64; ++j) v[j] = counts ? exp2_fast(fmaf(v[j], z_scale, -lse2)) : 0.f;
+          for (int j = 0; j < 64; ++j) V(j) = counts ? exp2_fast(fmaf(V(j), z_scale, -lse2)) * rest : 0.f;
           if (counts && target_col >= c && target_col < c + 64) {
 #pragma unroll
-            for (int j = 0; j < 64; ++j) v[j] = c + j == target_col ? v[j] - 1.f : v[j];
+            for (int j = 0; j < 64; ++j) V(j) = c + j == target_col ? V(j) - 1.f : V(j);
           }
           if (!p.bf16) {
 #pragma unroll
-            for (int j = 0; j < 64; ++j) v[j] *= FP16_DZ_SCALE;
+            for (int j = 0; j < 64; ++j) V(j) *= FP16_DZ_SCALE;
           }
           for (int plane = 0; plane < p.planes; ++plane) {
             // the buffer's previous store has to have read it (there are two buffers: one per half, or both for all)
@@ -305,7 +349,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
               uint32_t q[4];
 #pragma unroll
               for (int h = 0; h < 4; ++h) {
-                float &lo = v[8 * g + 2 * h], &hi = v[8 * g + 2 * h + 1];
+                float &lo = V(8 * g + 2 * h), &hi = V(8 * g + 2 * h + 1);
                 if (p.bf16) {
                   const __nv_bfloat162 r = __float22bfloat162_rn(make_float2(lo, hi));
                   q[h] = *reinterpret_cast<const uint32_t*>(&r);
@@ -330,15 +374,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
         }
       }
       if constexpr (EPI == DX) {
-        for (int c = 0; c < cols; c += 32) {
-          float v[32];
-          tmem_load_32(acc + c, v);
+#pragma unroll(RUNS ? WIDTH / 32 : 1)
+        for (int c = 0; c < WIDTH; c += 32) {
+          if (c >= cols) continue;
+          float loaded[RUNS ? 1 : 32];
+          if constexpr (!RUNS) tmem_load_32(acc + c, loaded);
           if (row_on) {
             float* const out = p.acc + w.split * p.acc_split + (int64_t)row * p.acc_pitch + col0 + c;
 #pragma unroll
             for (int j = 0; j < 32; j += 4) {   // acc_pitch is a multiple of 4: whole groups
               if (c + j < cols) {
-                float4 f = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                float4 f = make_float4(V(j), V(j + 1), V(j + 2), V(j + 3));
                 if (p.accumulate) {
                   const float4 o = *reinterpret_cast<const float4*>(out + j);
                   f = make_float4(f.x + o.x, f.y + o.y, f.z + o.z, f.w + o.w);
@@ -350,18 +396,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
         }
       }
       if constexpr (EPI == DW) {
-        for (int c = 0; c < cols; c += 32) {
-          float v[32];
-          tmem_load_32(acc + c, v);
+#pragma unroll(RUNS ? WIDTH / 32 : 1)
+        for (int c = 0; c < WIDTH; c += 32) {
+          if (c >= cols) continue;
+          float loaded[RUNS ? 1 : 32];
+          if constexpr (!RUNS) tmem_load_32(acc + c, loaded);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] *= alpha;
+          for (int j = 0; j < 32; ++j) V(j) *= alpha;
           if (!p.dw_vector || cols - c < 32) {
             // odd strides, the last columns: through shared memory, so that a warp stores along a row
             // (places exchanged within a row, so that both ways use all banks)
             float* const mine = reinterpret_cast<float*>(s_store) + (warp - 2) * (32 * 32);
             __syncwarp();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) mine[lane * 32 + (j ^ lane)] = v[j];
+            for (int j = 0; j < 32; ++j) mine[lane * 32 + (j ^ lane)] = V(j);
             __syncwarp();
             const int first = block_row0 + quarter * 32, n_rows = min(p.m - first, 32);
             if (c + lane < cols) {
@@ -382,7 +430,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
           if (p.dw_dtype == SNN_DTYPE_FP32) {
             float* const out = (float*)p.dw + at;
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(out + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            for (int j = 0; j < 32; j += 4) *reinterpret_cast<float4*>(out + j) = make_float4(V(j), V(j + 1), V(j + 2), V(j + 3));
           } else {
             uint16_t* const out = (uint16_t*)p.dw + at;
 #pragma unroll
@@ -391,10 +439,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
 #pragma unroll
               for (int h = 0; h < 4; ++h) {
                 if (p.dw_dtype == SNN_DTYPE_BF16) {
-                  const __nv_bfloat162 r = __float22bfloat162_rn(make_float2(v[j + 2 * h], v[j + 2 * h + 1]));
+                  const __nv_bfloat162 r = __float22bfloat162_rn(make_float2(V(j + 2 * h), V(j + 2 * h + 1)));
                   q[h] = *reinterpret_cast<const uint32_t*>(&r);
                 } else {
-                  const __half2 r = __float22half2_rn(make_float2(v[j + 2 * h], v[j + 2 * h + 1]));
+                  const __half2 r = __float22half2_rn(make_float2(V(j + 2 * h), V(j + 2 * h + 1)));
                   q[h] = *reinterpret_cast<const uint32_t*>(&r);
                 }
               }
@@ -403,9 +451,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
           }
         }
       }
-      tcgen05_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_at(peer_address(smem_u32(&s.acc_empty[buf]), 0));
+#undef V
+      if constexpr (!RUNS) run_read();
     }
     if (EPI == GRAD && storer) bulk_done();
   }
@@ -512,6 +559,8 @@ __device__ __forceinline__ float2 join_sums(float2 a, float2 b) {   // (maximum,
   const float m = a.x != a.x || b.x != b.x ? __uint_as_float(0x7fc00000u) : fmaxf(a.x, b.x), at = m == -INFINITY ? 0.f : m;
   return make_float2(m, a.y * exp2f(a.x - at) + b.y * exp2f(b.x - at));
 }
+// log-sum-exp of a row from its joined (maximum, sum), in units of 1
+__device__ __forceinline__ double log_sum(float2 v) { return ((double)v.x + (double)log2f(v.y)) * 0.69314718055994530942; }
 // The tiles' (maximum, sum) of a row joined: log-sum-exp and loss of the row.  32 rows per block, 32 threads per row.  If
 // one block has all rows it takes the mean as well (loss != NULL).
 __global__ void __launch_bounds__(1024) row_loss_kernel(const float2* partial, int tiles, const float* target_z, int rows, const void* targets,
@@ -537,8 +586,9 @@ __global__ void __launch_bounds__(1024) row_loss_kernel(const float2* partial, i
   if (row < rows) {
     v = s_part[0][in_block];
     const int target = target_of(targets, bits, ignore, classes, row);
-    float l = (v.x + log2f(v.y)) * LN2;
-    out = l - (target >= 0 ? target_z[row] * LN2 : 0.f);
+    const double exact = log_sum(v);
+    float l = (float)exact;
+    out = (float)(exact - (target >= 0 ? (double)target_z[row] * 0.69314718055994530942 : 0.));
     if (target < 0) l = 0.f, out = target == -1 ? 0.f : __uint_as_float(0x7fc00000u);
     count = target >= 0;
     lse[row] = l;
@@ -790,7 +840,8 @@ __global__ void __launch_bounds__(1024) few_loss_kernel(const float2* partial, i
 #pragma unroll
       for (int o = 16; o > 0; o /= 2) v = join_sums(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
       const int target = target_of(targets, bits, ignore, classes, row);
-      float l = (v.x + log2f(v.y)) * LN2, out = l - (target >= 0 ? target_z[row] * LN2 : 0.f);
+      const double exact = log_sum(v);
+      float l = (float)exact, out = (float)(exact - (target >= 0 ? (double)target_z[row] * 0.69314718055994530942 : 0.));
       if (target < 0) l = 0.f, out = target == -1 ? 0.f : __uint_as_float(0x7fc00000u);
       sum += out;
       count += target >= 0;
@@ -912,19 +963,24 @@ snn_status check(const snn_vocab_loss_args* a) {
 }
 bool is_bf16(int dtype) { return dtype == SNN_DTYPE_BF16; }   // (fp32: fp16 planes)
 
-template <int EPI, bool A_MN, bool B_MN, int WARPS> snn_status launch_product(const ProductParams& p, int pairs, cudaStream_t stream) {
-  const auto kernel = product_kernel<EPI, A_MN, B_MN, WARPS>;
+template <int EPI, bool A_MN, bool B_MN, int WARPS, bool RUNS> snn_status launch_one(const ProductParams& p, int pairs, cudaStream_t stream) {
+  const auto kernel = product_kernel<EPI, A_MN, B_MN, WARPS, RUNS>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)VL_SMEM) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
   const int64_t units = (int64_t)p.tiles_m * p.tiles_n * p.splits;
   if (units > INT32_MAX / 2) return SNN_ERR_UNSUPPORTED;
   kernel<<<2 * (unsigned)std::min<int64_t>(units, pairs), 32 * (2 + WARPS), VL_SMEM, stream>>>(p);
   return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
 }
-bool short_contraction(const ProductParams& p) { return p.kblocks * p.n_pairs < VL_SHORT; }
+bool eight_warps(const ProductParams& p) { return p.planes == 2 || p.kblocks < VL_SHORT; }
+template <int EPI, bool A_MN, bool B_MN> snn_status launch_product(const ProductParams& p, int pairs, cudaStream_t stream) {
+  if (p.planes == 2) return launch_one<EPI, A_MN, B_MN, 8, true>(p, pairs, stream);
+  if constexpr (EPI == STATS || EPI == GRAD)
+    if (eight_warps(p)) return launch_one<EPI, A_MN, B_MN, 8, false>(p, pairs, stream);
+  return launch_one<EPI, A_MN, B_MN, 4, false>(p, pairs, stream);
+}
 // z products: B is w, by class (K-major) or by feature
 template <int EPI> snn_status launch_z(const ProductParams& p, bool by_class, int pairs, cudaStream_t stream) {
-  if (short_contraction(p)) return by_class ? launch_product<EPI, false, false, 8>(p, pairs, stream) : launch_product<EPI, false, true, 8>(p, pairs, stream);
-  return by_class ? launch_product<EPI, false, false, 4>(p, pairs, stream) : launch_product<EPI, false, true, 4>(p, pairs, stream);
+  return by_class ? launch_product<EPI, false, false>(p, pairs, stream) : launch_product<EPI, false, true>(p, pairs, stream);
 }
 
 struct Call {
@@ -1061,7 +1117,7 @@ extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void*
   p.partial = (float2*)(c.ws + c.l.partial);
   p.target_z = (float*)(c.ws + c.l.target_z);
   VL_TRY(launch_z<STATS>(p, by_class, c.pairs, c.stream));
-  return c.row_losses(p.partial, (short_contraction(p) ? 2 : 1) * p.tiles_n, p.target_z);
+  return c.row_losses(p.partial, (eight_warps(p) ? 2 : 1) * p.tiles_n, p.target_z);
 }
 
 extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void* stream) {
@@ -1103,7 +1159,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     p.bk0 = v0;
     p.m = a->rows; p.n = a->dim;
     p.acc = (float*)(c.ws + l.acc); p.acc_pitch = l.acc_pitch; p.acc_split = l.acc_split; p.accumulate = v0 > 0;
-    VL_TRY((by_class ? launch_product<DX, false, true, 4>(p, c.pairs, c.stream) : launch_product<DX, false, false, 4>(p, c.pairs, c.stream)));
+    VL_TRY((by_class ? launch_product<DX, false, true>(p, c.pairs, c.stream) : launch_product<DX, false, false>(p, c.pairs, c.stream)));
     p = base;                 // the piece's part of dw
     p.kblocks = ceil_div(a->rows, UM_KB);
     p.alpha = c.alpha();
@@ -1119,7 +1175,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     }
     p.dw_vector = (uintptr_t)p.dw % 16 == 0 && p.dw_stride * (int64_t)size % 16 == 0;
     p.tiles_m = ceil_div(p.m, UM_TILE); p.tiles_n = ceil_div(p.n, UM_TILE);
-    VL_TRY((launch_product<DW, true, true, 4>(p, c.pairs, c.stream)));
+    VL_TRY((launch_product<DW, true, true>(p, c.pairs, c.stream)));
   }
   const int splits = std::min(l.splits, ceil_div(std::min(l.piece, a->classes), UM_KB));
   const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a->dim, 1024), 64), (unsigned)std::min(a->rows, 16384));

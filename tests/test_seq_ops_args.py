@@ -112,6 +112,17 @@ def test_sequence_operators_need_cuda_tensors():
             call()
 
 
+def test_enumerators_match_the_header():
+    import os
+    import re
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "snn.h")).read()
+    found = re.findall(r"\b(SNN_(?:DTYPE|KEEP|SCAN|W)_[A-Z0-9_]+)\s*=\s*(\d+)", header)
+    found += re.findall(r"#define\s+(SNN_(?:KEEP|SCAN)_[A-Z]+)\s+(\d+)", header)
+    assert len(found) == 12
+    for name, value in found:
+        assert getattr(sb, name) == int(value), name
+
+
 def test_struct_sizes_match_the_header(tmp_path):
     """The argument structs are spelled twice (include/snn.h and binding.py): same sizes and last offsets."""
     import os

@@ -357,8 +357,8 @@ typedef enum { SNN_DTYPE_FP32 = 0, SNN_DTYPE_BF16 = 1, SNN_DTYPE_FP16 = 2 } snn_
  * (SNN_KEEP_INT8, rounded to nearest even, at most 127 in magnitude) or a 4-bit-exponent, 3-bit-fraction float
  * (SNN_KEEP_E4M3, rounded to nearest even).  The scale is the smallest power of two, not below 2^-127, at which the
  * largest magnitude of the group is below 128 resp. no more than 448.  c = 255: the group held an infinity or a NaN, and
- * all of it decodes to NaN.  A finite value stays finite: what rounding takes beyond the type's range decodes to its
- * largest finite value. */
+ * all of it decodes to NaN.  A finite value stays finite: what lies beyond the range of the type it is
+ * decoded to becomes that type's largest finite value. */
 typedef enum { SNN_KEEP_RAW = 0, SNN_KEEP_INT8 = 1, SNN_KEEP_E4M3 = 2 } snn_keep_format;
 #define SNN_KEEP_GROUP 64
 

@@ -116,16 +116,24 @@ template <> __device__ __forceinline__ float largest_finite<float>() { return __
 template <> __device__ __forceinline__ float largest_finite<__nv_bfloat16>() { return __uint_as_float(0x7f7f0000u); }
 template <> __device__ __forceinline__ float largest_finite<__half>() { return 65504.f; }
 // The values of two codes, within the range of type IO.
+template <typename IO> __device__ __forceinline__ float within(float v) {   // NaN stays
+  const float top = largest_finite<IO>();
+  return fabsf(v) > top ? copysignf(top, v) : v;
+}
 template <typename IO, int FORMAT> __device__ __forceinline__ float2 keep_decode2(uint32_t codes, float scale) {
+  float a, b;
   if (FORMAT == SNN_KEEP_INT8) {   // code + 128 in the low bits of 2^23: again no conversion instructions
     const uint32_t u = codes ^ 0x8080u;
-    const float i = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650));
-    const float j = __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7651));
-    return make_float2(__fmul_rn(i - 8388736.f, scale), __fmul_rn(j - 8388736.f, scale));
+    a = __fmul_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7650)) - 8388736.f, scale);
+    b = __fmul_rn(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7651)) - 8388736.f, scale);
+    // (an int8 code stays below the largest value of the type that was packed: only fp16 can be too narrow for it)
+    if (largest_finite<IO>() > 65504.f) return make_float2(a, b);
+  } else {
+    const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3)));
+    a = __fmul_rn(v.x, scale);
+    b = __fmul_rn(v.y, scale);
   }
-  const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3)));
-  const float a = __fmul_rn(v.x, scale), b = __fmul_rn(v.y, scale), top = largest_finite<IO>();
-  return make_float2(fabsf(a) > top ? copysignf(top, a) : a, fabsf(b) > top ? copysignf(top, b) : b);   // NaN stays
+  return make_float2(within<IO>(a), within<IO>(b));
 }
 // The larger magnitude of two values; NaN if one of them is.
 __device__ __forceinline__ float larger_magnitude(float a, float b) {

@@ -148,7 +148,8 @@ def unpack_activation(packed: PackedActivation, dtype: Optional[torch.dtype] = N
 @dataclass(frozen=True)
 class ScanKept:
     """What a forward pass of `gated_scan` kept for the backward pass: the state before every 64th step and the inputs,
-    each as the caller's own tensor (do not change it before the backward pass) or in 8 bits."""
+    each as the caller's own tensor (do not change it before the backward pass, nor `lengths`) or in 8 bits.  What lies
+    behind a sequence's end is not kept."""
     shape: Tuple[int, int, int]
     dtype: torch.dtype
     mode: str
@@ -327,7 +328,7 @@ def vocab_loss(x: torch.Tensor, w_out: torch.Tensor, targets: torch.Tensor, *, s
     """Mean soft-max cross entropy of the logits scale * x w_out, which are never stored.
 
     x: [rows][dim], w_out: [dim][classes] of the same type (fp32, bf16 or fp16), stored by feature (contiguous) or by class
-    (`table.t()` of a [classes][dim] table).  targets: int32 or int64 [rows]; rows with ignore_index do not count, any other
+    (`table.t()` of a [classes][dim] table); 16-bit operands whose rows are not multiples of 16 bytes are copied first.  targets: int32 or int64 [rows]; rows with ignore_index do not count, any other
     target outside [0, classes) makes its row's loss and the mean NaN.
     Returns (loss, a 0-d tensor; row_loss [rows]; lse [rows], the log-sum-exp that `vocab_loss_backward` needs), all fp32,
     with zeros for rows that do not count."""

@@ -186,6 +186,26 @@ def test_scan_steps_follow_the_scan():
         close(h, f["h"][t], f["h_tol"][t], "fp32", f"token {t}")
 
 
+def test_scan_offsets_beyond_32_bits():
+    """2.4e9 values per tensor: the last group of channels against the reference."""
+    T, N = 40000, 60000
+    g = torch.Generator(device="cuda").manual_seed(14)
+    x, dh = (torch.empty(T, 1, N, dtype=torch.bfloat16, device="cuda").normal_(generator=g) for _ in range(2))
+    gate = torch.empty(T, 1, N, dtype=torch.bfloat16, device="cuda").normal_(1.0, 2.0, generator=g)
+    h, last, kept = ops().gated_scan(x, gate, keep="int8")
+    part = slice(N - N % 64, N)
+    small = [f64(v[:, :, part]) for v in (x, gate, dh)]
+    r = ref.scan_backward(small[0], small[1], None, None, "sigmoid", small[2], None, "int8", "int8")
+    f = ref.scan_forward(small[0], small[1], None, None, "sigmoid")
+    close(h[:, :, part], f["h"], f["h_tol"], "bf16", "h")
+    close(last[:, part], f["last"], f["last_tol"], "fp32", "last")
+    dx, dgate, _ = ops().gated_scan_backward(kept, dh)
+    close(dx[:, :, part], r["dx"], r["dx_tol"], "bf16", "dx")
+    close(dgate[:, :, part], r["dgate"], r["dgate_tol"], "bf16", "dgate")
+    back = ops().unpack_activation(kept.x)
+    assert np.array_equal(f64(back[-5:, :, part]), ref.eight_bits(small[0][-5:], "int8")[0])
+
+
 def test_scan_nothing_to_do():
     o = ops()
     for T, B, N in ((0, 2, 5), (3, 0, 5), (3, 2, 0)):
@@ -276,6 +296,14 @@ def test_pack_keeps_the_largest_values_finite(dtype, fmt):
     x[0, 1::2] *= -1
     back = ops().unpack_activation(ops().pack_activation(x, fmt))
     assert torch.isfinite(back).all() and np.array_equal(f64(back), ref.eight_bits(f64(x), fmt, dtype)[0])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_unpack_to_a_narrower_type(fmt):
+    x = torch.tensor([[1e6, -3e5, 100.0, 7.0]], device="cuda")
+    p = ops().pack_activation(x, fmt)
+    want = np.clip(ref.eight_bits(f64(x), fmt)[0], -65504, 65504)
+    assert np.array_equal(f64(ops().unpack_activation(p, torch.float16)), want.astype(np.float16).astype(np.float64))
 
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])

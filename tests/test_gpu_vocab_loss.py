@@ -98,6 +98,33 @@ def test_loss_more_than_one_piece_of_the_vocabulary(layout):
     check(*inputs(5000, 40, 60001, "bf16", 5, layout), "bf16")
 
 
+def test_loss_of_more_than_32_bits_of_logits():
+    """70000 x 40000 logits, never stored: the last rows and the last classes against the definition."""
+    o = ops()
+    n, D, V = 70000, 16, 40000
+    x, w, t = inputs(n, D, V, "bf16", 15, "class")
+    _, row, lse = o.vocab_loss(x, w, t)
+    dx, dw = o.vocab_loss_backward(x, w, t, lse)
+    rows = slice(n - 64, n)
+    r = ref.vocab_loss(x[rows].double(), w.double(), t[rows], 1.0, -100, "bf16")
+    close(row[rows], r["row"], r["row_tol"], "fp32", "row_loss")
+    part, count = int((t[rows] >= 0).sum()), int((t >= 0).sum())
+    close(dx[rows], r["dx"] * part / count, r["dx_tol"] * part / count, "bf16", "dx")
+    # the gradient of the last 32 classes, from all rows
+    z = torch.empty(n, 32, dtype=torch.float64, device="cuda")
+    for a in range(0, n, 10000):
+        b = slice(a, a + 10000)
+        full = x[b].double() @ w.double()
+        z[b] = torch.softmax(full, 1)[:, -32:]
+    at = t - (V - 32)
+    on = (t >= 0).double()[:, None]
+    z = (z - torch.nn.functional.one_hot(at.clamp(min=-1) + 1, 33)[:, 1:].double()) * on
+    want = x.double().t() @ z / count
+    # dz is rounded to bf16 (2^-8 of each) and computed to 2^-16; the sum over the rows is cut 2 n / 16 times by 2^-23
+    tol = x.double().abs().t() @ z.abs() / count * (2.0 ** -8 + 2.0 ** -16 + 2 * n / 16 * 2.0 ** -23)
+    close(dw[:, -32:], want, tol, "bf16", "dw")
+
+
 def test_loss_long_contraction_in_fp32():
     check(*inputs(40, 2000, 3001, "fp32", 6), "fp32")
 

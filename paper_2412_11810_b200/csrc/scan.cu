@@ -42,7 +42,8 @@ struct ScanParams {
   CUtensorMap in[3], out[4];   // TILES.  forward: x, gate -> h, -, codes of x, codes of gate; backward: dh, x, gate -> dx, dgate
   int T, B, N, n_tiles;        // n_tiles: column tiles per sample
   int segments, segment_steps; // of the time axis; a multiple of a chunk each
-  float4* summaries;           // [segments][B][n_tiles][32] maps of pairs of channels, if there are several segments
+  int parts;                   // of a segment, summarised by a block each
+  float4* summaries;           // [segments][parts][B][n_tiles][32] maps of pairs of channels, if there are several segments
   int mode, x_format, gate_format;
   const void *x, *gate, *dh;
   void *h, *dx, *dgate;
@@ -130,8 +131,9 @@ __device__ __forceinline__ Place place_of(const ScanParams& p) {
   Place w;
   w.lane = threadIdx.x & 31;
   w.warp = threadIdx.x >> 5;
-  w.segment = (int)blockIdx.x % p.segments;
-  const int tile = (int)blockIdx.x / p.segments;
+  // neighbouring blocks: neighbouring channels of the same steps, which lie in the same DRAM pages
+  const int tiles = p.B * p.n_tiles, tile = (int)(blockIdx.x % (unsigned)tiles);
+  w.segment = (int)(blockIdx.x / (unsigned)tiles);
   w.b = tile / p.n_tiles;
   w.col0 = (tile % p.n_tiles) * SCAN_COLS;
   w.c = w.col0 + 2 * w.lane;
@@ -144,13 +146,13 @@ __device__ __forceinline__ Place place_of(const ScanParams& p) {
   w.map = (int64_t)tile * 32 + w.lane;
   return w;
 }
-__device__ __forceinline__ int64_t maps_per_segment(const ScanParams& p) { return (int64_t)p.B * p.n_tiles * 32; }
+__device__ __forceinline__ int64_t maps_per_part(const ScanParams& p) { return (int64_t)p.B * p.n_tiles * 32; }
 // The state before a segment (REVERSE: e behind it), from that before the first (behind the last).
 template <bool REVERSE> __device__ __forceinline__ float2 enter_segment(const ScanParams& p, const Place& w, float2 h) {
-  const int n = REVERSE ? p.segments - 1 - w.segment : w.segment;
-  const float4* at = p.summaries + (REVERSE ? p.segments - 1 : 0) * maps_per_segment(p) + w.map;
-  const int64_t step = REVERSE ? -maps_per_segment(p) : maps_per_segment(p);
-#pragma unroll 8
+  const int n = (REVERSE ? p.segments - 1 - w.segment : w.segment) * p.parts;
+  const float4* at = p.summaries + (REVERSE ? p.segments * p.parts - 1 : 0) * maps_per_part(p) + w.map;
+  const int64_t step = REVERSE ? -maps_per_part(p) : maps_per_part(p);
+#pragma unroll 16
   for (int q = 0; q < n; ++q, at += step) h = apply(as_map(*at), h);
   return h;
 }
@@ -667,30 +669,34 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
 }
 
 // ---- segments ------------------------------------------------------------------------------------------------
-// The map of every segment but the last (REVERSE, the backward pass: but the first).  A warp takes an eighth of the
-// segment's steps on its own, so nothing waits inside the loop; plain loads, 8 steps at a time.
+// The maps of the parts of every segment but the last (REVERSE, the backward pass: but the first).  A warp takes an eighth of
+// a part's steps on its own, so nothing waits inside the loop; plain loads, 8 steps at a time.
 template <typename IO, bool IN_PAIRS, bool REVERSE>
-__global__ void __launch_bounds__(32 * WARPS, 3) scan_summary_kernel(const __grid_constant__ ScanParams p) {
+__global__ void __launch_bounds__(32 * WARPS, sizeof(IO) == 2 ? 4 : 3) scan_summary_kernel(const __grid_constant__ ScanParams p) {
   __shared__ float4 s_sum[WARPS][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int tile = (int)blockIdx.x / (p.segments - 1), segment = (int)blockIdx.x % (p.segments - 1) + (REVERSE ? 1 : 0);
+  const unsigned tiles = (unsigned)(p.B * p.n_tiles);
+  const int tile = (int)(blockIdx.x % tiles), part = (int)(blockIdx.x / tiles) + (REVERSE ? p.parts : 0);   // counted from the first segment's first
   const int b = tile / p.n_tiles, c = (tile % p.n_tiles) * SCAN_COLS + 2 * lane, n_ok = min(max(p.N - c, 0), 2);
-  const int len = length_of(p, b), share = p.segment_steps / WARPS, first = segment * p.segment_steps + warp * share;
+  const int len = length_of(p, b), steps = p.segment_steps / p.parts, share = steps / WARPS, first = part * steps + warp * share;
   const int end = min(first + share, len);
   const IO* const from = REVERSE ? (const IO*)p.dh + b * p.dhs[1] : (const IO*)p.x + b * p.xs[1];
   const int64_t from_stride = REVERSE ? p.dhs[0] : p.xs[0];
   const IO* const gate = (const IO*)p.gate + b * p.gs[1];
   const bool raw_gate = !REVERSE || p.gate_format == SNN_KEEP_RAW;
+  using raw = typename Pair<IO>::raw;
   Map2 m{both(1.f), both(0.f)};
   const int turns = (max(end - first, 0) + SCAN_K - 1) / SCAN_K;
   for (int i = 0; i < turns; ++i) {
     const int t0 = first + (REVERSE ? turns - 1 - i : i) * SCAN_K;
-    float2 v[SCAN_K], a[SCAN_K], in[SCAN_K];
+    const bool full = t0 + SCAN_K <= end;
+    // values stay in their own type until their step: registers for a fourth block per SM
+    raw v[SCAN_K], g[SCAN_K];
 #pragma unroll
-    for (int k = 0; k < SCAN_K; ++k) v[k] = load_pair<IN_PAIRS>(from + min(t0 + k, end - 1) * from_stride, c, n_ok);
+    for (int k = 0; k < SCAN_K; ++k) v[k] = load_raw<IN_PAIRS>(from + min(t0 + k, end - 1) * from_stride, c, n_ok);
     if (raw_gate) {
 #pragma unroll
-      for (int k = 0; k < SCAN_K; ++k) a[k] = load_pair<IN_PAIRS>(gate + min(t0 + k, end - 1) * p.gs[0], c, n_ok);
+      for (int k = 0; k < SCAN_K; ++k) g[k] = load_raw<IN_PAIRS>(gate + min(t0 + k, end - 1) * p.gs[0], c, n_ok);
     } else {
       uint32_t codes[SCAN_K], bytes[SCAN_K];
 #pragma unroll
@@ -703,20 +709,29 @@ __global__ void __launch_bounds__(32 * WARPS, 3) scan_summary_kernel(const __gri
       }
 #pragma unroll
       for (int k = 0; k < SCAN_K; ++k)
-        a[k] = p.gate_format == SNN_KEEP_INT8 ? keep_decode2<IO, SNN_KEEP_INT8>(codes[k], keep_scale_value(bytes[k]))
-                                              : keep_decode2<IO, SNN_KEEP_E4M3>(codes[k], keep_scale_value(bytes[k]));
+        set_raw(g[k], p.gate_format == SNN_KEEP_INT8 ? keep_decode2<IO, SNN_KEEP_INT8>(codes[k], keep_scale_value(bytes[k]))
+                                                     : keep_decode2<IO, SNN_KEEP_E4M3>(codes[k], keep_scale_value(bytes[k])));
     }
-    coefficients(a, in, p.mode);
-    if (t0 + SCAN_K > end) {
+    float lowest = 0.f;
+    if (p.mode != SNN_SCAN_DIRECT) {
 #pragma unroll
-      for (int k = 0; k < SCAN_K; ++k)
-        if (t0 + k >= end) a[k] = both(1.f), v[k] = both(0.f);
+      for (int k = 0; k < SCAN_K; ++k) lowest = fminf(lowest, fminf(to_f32(g[k]).x, to_f32(g[k]).y));
     }
+    auto compose = [&](auto kind) {   // 0: direct, 1: ordinary gates, 2: any
 #pragma unroll
-    for (int j = 0; j < SCAN_K; ++j) {
-      const int k = REVERSE ? SCAN_K - 1 - j : j;
-      m = then(m, Map2{a[k], mul2(REVERSE ? a[k] : in[k], v[k])});
-    }
+      for (int j = 0; j < SCAN_K; ++j) {
+        const int k = REVERSE ? SCAN_K - 1 - j : j;
+        float2 a = to_f32(g[k]), in = both(1.f), x = to_f32(v[k]);
+        if constexpr (decltype(kind)::value == 1) ordinary_sigmoids(a, a, in);
+        if constexpr (decltype(kind)::value == 2) sigmoids(a, a, in);
+        float2 added = mul2(REVERSE ? a : in, x);
+        if (!full && t0 + k >= end) a = both(1.f), added = both(0.f);
+        m = then(m, Map2{a, added});
+      }
+    };
+    if (p.mode == SNN_SCAN_DIRECT) compose(std::integral_constant<int, 0>());
+    else if (lowest >= LOWEST_GATE) compose(std::integral_constant<int, 1>());
+    else compose(std::integral_constant<int, 2>());
   }
   s_sum[warp][lane] = as4(m);
   __syncthreads();
@@ -724,7 +739,7 @@ __global__ void __launch_bounds__(32 * WARPS, 3) scan_summary_kernel(const __gri
     m = as_map(s_sum[REVERSE ? WARPS - 1 : 0][lane]);
 #pragma unroll
     for (int v = 1; v < WARPS; ++v) m = then(m, as_map(s_sum[REVERSE ? WARPS - 1 - v : v][lane]));
-    p.summaries[segment * maps_per_segment(p) + (int64_t)tile * 32 + lane] = as4(m);
+    p.summaries[part * maps_per_part(p) + (int64_t)tile * 32 + lane] = as4(m);
   }
 }
 
@@ -800,9 +815,11 @@ void cut_time(ScanParams& p, int resident) {
   if (n < 4) n = 1;
   p.segment_steps = (int)((((int64_t)p.T + n - 1) / n + SNN_SCAN_CHUNK - 1) / SNN_SCAN_CHUNK * SNN_SCAN_CHUNK);
   p.segments = p.segment_steps ? (p.T + p.segment_steps - 1) / p.segment_steps : 1;
+  // the summary's blocks are small and wait for their loads: twice as many of them, as long as a warp has 32 steps
+  p.parts = p.segment_steps >= 2 * WARPS * 32 ? 2 : 1;
 }
 int resident_blocks(const snn_scan_args* a, bool backward) { return (backward ? 2 : 3) - (a->dtype == SNN_DTYPE_FP32); }
-size_t summary_bytes(const ScanParams& p) { return p.segments > 1 ? sizeof(float4) * 32 * (size_t)p.segments * p.B * p.n_tiles : 0; }
+size_t summary_bytes(const ScanParams& p) { return p.segments > 1 ? sizeof(float4) * 32 * (size_t)p.segments * p.parts * p.B * p.n_tiles : 0; }
 
 snn_status set_segments(ScanParams& p, const snn_scan_args* a, bool backward) {
   cut_time(p, resident_blocks(a, backward));
@@ -871,7 +888,7 @@ extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
       return launch(scan_forward_kernel<IO, KEEP, PATH>, ring + out, blocks * p.segments, p, s);
     };
     if (p.segments > 1) {
-      const snn_status st = launch(scan_summary_kernel<IO, PATH != SCALAR, false>, 0, blocks * (p.segments - 1), p, s);
+      const snn_status st = launch(scan_summary_kernel<IO, PATH != SCALAR, false>, 0, blocks * (p.segments - 1) * p.parts, p, s);
       if (st != SNN_OK) return st;
     }
     return keep ? go(std::true_type()) : go(std::false_type());
@@ -906,7 +923,7 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
     const size_t ring = PATH != TILES ? 0 : SCAN_DEPTH * slot, out = PATH == TILES ? 2 * WARPS * 2 * WARP_PIECE * sizeof(IO) : 0;
     const int64_t blocks = (int64_t)p.B * p.n_tiles;
     if (p.segments > 1) {
-      const snn_status st = launch(scan_summary_kernel<IO, PATH != SCALAR, true>, 0, blocks * (p.segments - 1), p, (cudaStream_t)stream);
+      const snn_status st = launch(scan_summary_kernel<IO, PATH != SCALAR, true>, 0, blocks * (p.segments - 1) * p.parts, p, (cudaStream_t)stream);
       if (st != SNN_OK) return st;
     }
     return launch(scan_backward_kernel<IO, PATH>, ring + out, blocks * p.segments, p, (cudaStream_t)stream);

@@ -47,6 +47,15 @@ __device__ __forceinline__ float2 load_pair(const IO* row, int c, int n_ok) {
   if (PAIRS) return to_f32(*reinterpret_cast<const typename Pair<IO>::raw*>(row + (n_ok ? c : 0)));
   return make_float2(to_f32(row[n_ok ? c : 0]), to_f32(row[n_ok == 2 ? c + 1 : 0]));
 }
+// The same in the values' own type.
+template <bool PAIRS, typename IO>
+__device__ __forceinline__ typename Pair<IO>::raw load_raw(const IO* row, int c, int n_ok) {
+  if (PAIRS) return *reinterpret_cast<const typename Pair<IO>::raw*>(row + (n_ok ? c : 0));
+  typename Pair<IO>::raw r;
+  r.x = row[n_ok ? c : 0];
+  r.y = row[n_ok == 2 ? c + 1 : 0];
+  return r;
+}
 template <bool PAIRS, typename IO>
 __device__ __forceinline__ void store_pair(IO* row, int c, int n_ok, float2 v) {
   if (PAIRS) {

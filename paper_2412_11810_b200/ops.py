@@ -76,6 +76,11 @@ def _stream(t: torch.Tensor) -> int:
     return _raw_stream(t.get_device()) if _raw_stream else torch.cuda.current_stream(t.device).cuda_stream
 
 
+def _dense(t: torch.Tensor) -> torch.Tensor:
+    """A new contiguous tensor of the same shape and type (empty_like is the cheaper call where it can be used)."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
@@ -205,8 +210,8 @@ def gated_scan(x: torch.Tensor, gate: torch.Tensor, state: Optional[torch.Tensor
     if lengths is not None:
         _like(lengths, "lengths", x, (B,), torch.int32)
     with _on(x):
-        h = x.new_empty(shape)
-        last = x.new_empty((B, N), dtype=torch.float32)
+        h = _dense(x)
+        last = x.new_empty((B, N), dtype=torch.float32) if state is None else torch.empty_like(state)
         a = sb.snn_scan_args(T, B, N, _DTYPES[dtype], _MODES[mode], x.data_ptr(), gate.data_ptr(), x.stride()[:2], gate.stride()[:2],
                              _ptr(lengths), _ptr(state), h.data_ptr(), (B * N, N), last.data_ptr())
         kept = None
@@ -245,8 +250,8 @@ def gated_scan_step(x: torch.Tensor, gate: torch.Tensor, state: Optional[torch.T
     if B > _INT32_MAX or N > _INT32_MAX:
         raise ValueError("x: too large")
     with _on(x):
-        h = x.new_empty(shape)
-        last = state if inplace else x.new_empty(shape, dtype=torch.float32)
+        h = _dense(x)
+        last = state if inplace else x.new_empty(shape, dtype=torch.float32) if state is None else torch.empty_like(state)
         sb.snn_scan_forward(sb.snn_scan_args(1, B, N, _DTYPES[dtype], _MODES[mode], x.data_ptr(), gate.data_ptr(), (0, x.stride(0)),
                                              (0, gate.stride(0)), None, _ptr(state), h.data_ptr(), (0, N), last.data_ptr()), _stream(x))
     return h, last
@@ -265,7 +270,7 @@ def gated_scan_backward(kept: ScanKept, dh: torch.Tensor, dlast: Optional[torch.
     if dlast is not None:
         _like(dlast, "dlast", like, (B, N), torch.float32)
     with _on(like):
-        dx, dgate = dh.new_empty(shape), dh.new_empty(shape)
+        dx, dgate = _dense(dh), _dense(dh)
         dstate = like.new_empty((B, N))
         a = sb.snn_scan_args(T, B, N, _DTYPES[kept.dtype], _MODES[kept.mode])
         a.lengths, a.states, a.dlast, a.dstate = _ptr(kept.lengths), like.data_ptr(), _ptr(dlast), dstate.data_ptr()
@@ -354,7 +359,7 @@ def vocab_loss_backward(x: torch.Tensor, w_out: torch.Tensor, targets: torch.Ten
     else:
         a.dloss = dloss
     with _on(x):
-        dx = x.new_empty(x.shape)
+        dx = _dense(x)
         if a.w_layout == sb.SNN_W_BY_FEATURE:
             dw = x.new_empty((a.dim, a.classes))
             a.dw_stride = a.classes

@@ -484,6 +484,12 @@ struct StageParams {
   int64_t ignore;
   int classes;
   uint32_t* tops;       // fp32: bit patterns of the largest magnitudes
+  // the backward pass has blocks with blockIdx.y = 2: the first counts the rows and writes the gradients' factor
+  float* alpha;
+  float factor;
+  const float* dloss;
+  uint32_t* status;
+  int rows;
 };
 constexpr int STAGE_COLS = 1024;   // columns of a row that a block takes at a time, four per thread
 
@@ -510,7 +516,31 @@ __global__ void __launch_bounds__(256) largest_kernel(const __grid_constant__ St
   __syncthreads();
   if (threadIdx.x == 0 && s_top) atomicMax(p.tops + blockIdx.y, s_top);
 }
+// Sums of a block's values, the same in every thread; `warp_sums` has 32 entries.
+__device__ __forceinline__ double block_sum(double v, double* warp_sums) {
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5] = v;
+  __syncthreads();
+  double t = 0;
+  for (int w = 0; w < (int)blockDim.x / 32; ++w) t += warp_sums[w];
+  return t;
+}
 template <typename IO> __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ StageParams p) {
+  if (blockIdx.y == 2) {
+    __shared__ double warp_sums[32];
+    if (blockIdx.x != 0) return;
+    int n = 0;
+#pragma unroll 8
+    for (int r = threadIdx.x; r < p.rows; r += 256) n += target_of(p.targets, p.bits, p.ignore, p.classes, r) >= 0;
+    const double count = block_sum((double)n, warp_sums);
+    if (threadIdx.x == 0) {
+      *p.alpha = count > 0 ? (float)((double)p.factor * (p.dloss ? (double)*p.dloss : 1.) / count) : 0.f;
+      *p.status = 0u;
+    }
+    return;
+  }
   const StageJob& j = p.job[blockIdx.y];
   const int parts = (int)((j.pitch + STAGE_COLS - 1) / STAGE_COLS);
   const float scale = sizeof(IO) == 4 && j.rows ? operand_scale(p.tops[blockIdx.y]) : 1.f;
@@ -541,18 +571,6 @@ template <typename IO> __global__ void __launch_bounds__(256) stage_kernel(const
       }
     }
   }
-}
-
-// Sums of a block's values, the same in every thread; `warp_sums` has 32 entries.
-__device__ __forceinline__ double block_sum(double v, double* warp_sums) {
-#pragma unroll
-  for (int o = 16; o > 0; o /= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) warp_sums[threadIdx.x >> 5] = v;
-  __syncthreads();
-  double t = 0;
-  for (int w = 0; w < (int)blockDim.x / 32; ++w) t += warp_sums[w];
-  return t;
 }
 
 __device__ __forceinline__ float2 join_sums(float2 a, float2 b) {   // (maximum, sum of exponentials)
@@ -606,21 +624,18 @@ __global__ void __launch_bounds__(1024) row_loss_kernel(const float2* partial, i
   }
 }
 
-// One block.  The mean of row_loss over the rows that count (loss != NULL), and the factor of the gradients (alpha != NULL).
+// One block.  The mean of row_loss over the rows that count.
 __global__ void __launch_bounds__(1024) mean_kernel(const float* row_loss, int rows, const void* targets, int bits, int64_t ignore, int classes,
-                                                    float* loss, float* alpha, float factor, const float* dloss) {
+                                                    float* loss) {
   __shared__ double warp_sums[32];
   double sum = 0, count = 0;
   for (int r = threadIdx.x; r < rows; r += blockDim.x) {
-    if (loss) sum += (double)row_loss[r];
+    sum += (double)row_loss[r];
     count += target_of(targets, bits, ignore, classes, r) >= 0;
   }
-  if (loss) sum = block_sum(sum, warp_sums);
+  sum = block_sum(sum, warp_sums);
   count = block_sum(count, warp_sums);
-  if (threadIdx.x == 0) {
-    if (loss) *loss = (float)(sum / fmax(count, 1.));
-    if (alpha) *alpha = count > 0 ? (float)((double)factor * (dloss ? (double)*dloss : 1.) / count) : 0.f;
-  }
+  if (threadIdx.x == 0) *loss = (float)(sum / fmax(count, 1.));
 }
 
 // The parts of dx joined, scaled and rounded; rows that do not count are zero.
@@ -1001,10 +1016,11 @@ struct Call {
     if (!a->workspace || (uintptr_t)a->workspace % 256 != 0) return SNN_ERR_INVALID_ARG;
     if (a->workspace_bytes < l.total) return SNN_ERR_WORKSPACE_TOO_SMALL;
     ws = (char*)a->workspace;
-    if (!backward && a->dtype != SNN_DTYPE_FP32) return SNN_OK;   // neither a status nor magnitudes
-    return cudaMemsetAsync(ws + l.status, 0, 128, stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+    if (a->dtype != SNN_DTYPE_FP32) return SNN_OK;   // (the status is cleared by the staging kernel)
+    return cudaMemsetAsync(tops(), 0, 2 * sizeof(uint32_t), stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
   }
-  snn_status stage_operands() const {
+  // with `factor`, for the backward pass: alpha and the status as well
+  snn_status stage_operands(const float* factor) const {
     const bool by_class = a->w_layout == SNN_W_BY_CLASS;
     StageParams p{};
     p.targets = a->targets; p.bits = a->target_bits; p.ignore = a->ignore_index; p.classes = a->classes;
@@ -1014,10 +1030,14 @@ struct Call {
       p.job[1] = {a->w, a->w_stride, by_class ? a->classes : a->dim, by_class ? a->dim : a->classes, (uint16_t*)(ws + l.w.offset), l.w.pitch, l.w.plane, false};
     int64_t work = 0;
     for (const StageJob& j : p.job) work = std::max(work, j.rows * (j.pitch / STAGE_COLS + 1));
+    if (factor) {
+      p.alpha = alpha(); p.factor = *factor; p.dloss = a->dloss_device; p.status = status(); p.rows = a->rows;
+      work = std::max<int64_t>(work, 1);
+    }
     if (work == 0) return SNN_OK;
-    const dim3 grid((unsigned)std::min<int64_t>(work, 148 * 8), 2);
+    const dim3 grid((unsigned)std::min<int64_t>(work, 148 * 8), factor ? 3 : 2);
     if (p.tops) {
-      largest_kernel<<<grid, 256, 0, stream>>>(p);
+      largest_kernel<<<dim3(grid.x, 2), 256, 0, stream>>>(p);
       stage_kernel<float><<<grid, 256, 0, stream>>>(p);
     } else {
       stage_kernel<__half><<<grid, 256, 0, stream>>>(p);   // 16 bits are copied, whatever they mean
@@ -1035,7 +1055,7 @@ struct Call {
     row_loss_kernel<<<ceil_div(a->rows, 32), 1024, 0, stream>>>(partial, tiles, target_z, a->rows, a->targets, a->target_bits, a->ignore_index,
                                                                 a->classes, a->lse, row_loss, a->row_loss, one ? a->loss : nullptr);
     if (!one)
-      mean_kernel<<<1, 1024, 0, stream>>>(row_loss, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, a->loss, nullptr, 0.f, nullptr);
+      mean_kernel<<<1, 1024, 0, stream>>>(row_loss, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, a->loss);
     return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
   }
   ProductParams base() const {
@@ -1105,7 +1125,7 @@ extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void*
                                         : forward_few<__half>(c);
   const bool by_class = a->w_layout == SNN_W_BY_CLASS;
   const int w_rows = by_class ? a->classes : a->dim, w_cols = by_class ? a->dim : a->classes;
-  VL_TRY(c.stage_operands());
+  VL_TRY(c.stage_operands(nullptr));
   ProductParams p = c.base();
   p.status = nullptr;   // (a wait that ran out shows in the losses)
   if (!c.map(&p.a, c.l.x, a->x, a->rows, a->dim, false) || !c.map(&p.b, c.l.w, a->w, w_rows, w_cols, !by_class)) return SNN_ERR_CUDA;
@@ -1133,10 +1153,9 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     return cudaMemset2DAsync(a->dw, a->dw_stride * size, 0, w_cols * size, w_rows, c.stream) == cudaSuccess ? SNN_OK
                                                                                                          : (cudaGetLastError(), SNN_ERR_CUDA);
   const Layout& l = c.l;
-  VL_TRY(c.stage_operands());
   const ProductParams base = c.base();
-  mean_kernel<<<1, 1024, 0, c.stream>>>(nullptr, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, nullptr, c.alpha(),
-                                        a->dloss * a->scale / (base.bf16 ? 1.f : FP16_DZ_SCALE), a->dloss_device);
+  const float factor = a->dloss * a->scale / (base.bf16 ? 1.f : FP16_DZ_SCALE);
+  VL_TRY(c.stage_operands(&factor));
   CUtensorMap x_k, x_mn, w_z, w_dx, dz_k, dz_mn;   // as operands that are contiguous along the contraction, and across it
   bool ok = c.map(&x_k, l.x, a->x, a->rows, a->dim, false) && c.map(&x_mn, l.x, a->x, a->rows, a->dim, true);
   ok = ok && c.map(&w_z, l.w, a->w, w_rows, w_cols, !by_class) && c.map(&w_dx, l.w, a->w, w_rows, w_cols, by_class);

@@ -37,6 +37,10 @@ constexpr int VL_SHORT = 16;                                 // k-blocks: eight 
 constexpr uint32_t VL_STORE_BYTES = UM_HALF * 128;           // one staged block of dz per half: 128 rows x 64 values
 constexpr size_t VL_SMEM = 1024 + (size_t)UM_STAGES * UM_STAGE_BYTES + 2 * VL_STORE_BYTES + 256;
 constexpr float FP16_DZ_SCALE = 16384.f;   // dz / (gradient of the row loss) lies in [-1, 1]; as fp16 it keeps small values better after this
+// The kernels of a call follow one another closely: each is launched while the one before still runs, sets itself up, and
+// waits here before it touches memory.  (Every kernel behind another one waits, so that their bodies never overlap.)
+__device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;"); }
 constexpr size_t PIECE_BYTES = (size_t)512 << 20;            // dz held at a time
 constexpr int MAX_SPLITS = 32;
 
@@ -54,6 +58,7 @@ struct ProductParams {
   int a0, b0, bk0;            // first row of A and of B, first k of B (A's k starts at 0)
   int m, n;                   // rows of A and of B that exist from there on
   bool bf16;
+  bool behind;                // (host) another kernel of the call
   // STATS and GRAD
   const void* targets;
   int target_bits;
@@ -154,6 +159,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1, n_pairs_sm = gridDim.x >> 1;
   const int units = p.tiles_m * p.tiles_n * p.splits;
+  let_next_kernel_start();
 
   if (tid == 0) {
     for (int i = 0; i < UM_STAGES; ++i) {
@@ -172,6 +178,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
   cluster_sync_all();
   tcgen05_after_sync();
   const uint32_t tmem = s.tmem;
+  wait_for_kernel_before();
 
   if (warp == 0) {
     if (lane == 0) {   // loads: this block's halves of A and B, announced to the even block's barrier
@@ -496,6 +503,7 @@ constexpr int STAGE_COLS = 1024;   // columns of a row that a block takes at a t
 // The largest magnitudes of fp32 operands.  (The maximum does not depend on the order of the atomics.)
 __global__ void __launch_bounds__(256) largest_kernel(const __grid_constant__ StageParams p) {
   __shared__ uint32_t s_top;
+  let_next_kernel_start();
   const StageJob& j = p.job[blockIdx.y];
   const int parts = (j.cols + STAGE_COLS - 1) / STAGE_COLS;
   if (threadIdx.x == 0) s_top = 0;
@@ -528,6 +536,8 @@ __device__ __forceinline__ double block_sum(double v, double* warp_sums) {
   return t;
 }
 template <typename IO> __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ StageParams p) {
+  let_next_kernel_start();
+  wait_for_kernel_before();
   if (blockIdx.y == 2) {
     __shared__ double warp_sums[32];
     if (blockIdx.x != 0) return;
@@ -585,6 +595,8 @@ __global__ void __launch_bounds__(1024) row_loss_kernel(const float2* partial, i
                                                         int bits, int64_t ignore, int classes, float* lse, float* row_loss, float* row_out,
                                                         float* loss) {
   __shared__ float2 s_part[32][33];
+  let_next_kernel_start();
+  wait_for_kernel_before();
   const int in_block = threadIdx.x % 32, part = threadIdx.x / 32, row = blockIdx.x * 32 + in_block;
   float2 v = make_float2(-INFINITY, 0.f);
   if (row < rows)
@@ -628,6 +640,7 @@ __global__ void __launch_bounds__(1024) row_loss_kernel(const float2* partial, i
 __global__ void __launch_bounds__(1024) mean_kernel(const float* row_loss, int rows, const void* targets, int bits, int64_t ignore, int classes,
                                                     float* loss) {
   __shared__ double warp_sums[32];
+  wait_for_kernel_before();
   double sum = 0, count = 0;
   for (int r = threadIdx.x; r < rows; r += blockDim.x) {
     sum += (double)row_loss[r];
@@ -643,6 +656,7 @@ template <typename IO>
 __global__ void __launch_bounds__(256) join_dx_kernel(const float* acc, int splits, int64_t split_stride, int pitch, int rows, int cols,
                                                       const float* alpha, const void* targets, int bits, int64_t ignore, int classes, IO* dx,
                                                       int64_t stride, const uint32_t* status, const uint32_t* tops) {
+  wait_for_kernel_before();
   const float a = (*status & VL_TIMEOUT) ? __uint_as_float(0x7fc00000u) : *alpha * (tops ? operand_unscale(tops[1]) : 1.f);
   for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
     const bool on = target_of(targets, bits, ignore, classes, (int)row) >= 0;
@@ -714,6 +728,7 @@ template <> struct EightValues<__half> : EightHalfValues<__half> {};
 // w by class: a warp takes a run of classes, four at a time; its lanes share the features.  VEC: eight features per load
 // (dim a multiple of 8, rows aligned to 16 bytes).
 template <typename IO, int R, bool VEC> __global__ void __launch_bounds__(32 * FEW_WARPS) few_rows_by_class_kernel(const FewParams p) {
+  let_next_kernel_start();
   extern __shared__ __align__(16) float s_x[];   // VEC: [R][2][dim / 8] float4, the halves of eight features apart; else [R][dim]
   __shared__ float2 s_part[FEW_WARPS][R];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -789,6 +804,7 @@ template <typename IO, int R, bool VEC> __global__ void __launch_bounds__(32 * F
 }
 // w by feature: a block takes 128 classes, four per lane; its warps share the features.
 template <typename IO, int R> __global__ void __launch_bounds__(32 * FEW_WARPS) few_rows_by_feature_kernel(const FewParams p) {
+  let_next_kernel_start();
   extern __shared__ __align__(16) float s_x[];   // [R][dim]
   __shared__ float s_acc[FEW_WARPS][R][128];
   __shared__ float2 s_part[FEW_WARPS][R];
@@ -840,6 +856,7 @@ template <typename IO, int R> __global__ void __launch_bounds__(32 * FEW_WARPS) 
 __global__ void __launch_bounds__(1024) few_loss_kernel(const float2* partial, int parts, const float* target_z, int rows, const void* targets,
                                                         int bits, int64_t ignore, int classes, float* lse, float* row_out, float* loss) {
   __shared__ float2 s_part[32];
+  wait_for_kernel_before();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   double sum = 0.;
   int count = 0;
@@ -978,13 +995,27 @@ snn_status check(const snn_vocab_loss_args* a) {
 }
 bool is_bf16(int dtype) { return dtype == SNN_DTYPE_BF16; }   // (fp32: fp16 planes)
 
+// Launches a kernel; `behind` another one of the same call.
+template <typename... P, typename... A>
+snn_status launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, bool behind, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = &at;
+  cfg.numAttrs = behind ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+}
 template <int EPI, bool A_MN, bool B_MN, int WARPS, bool RUNS> snn_status launch_one(const ProductParams& p, int pairs, cudaStream_t stream) {
   const auto kernel = product_kernel<EPI, A_MN, B_MN, WARPS, RUNS>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)VL_SMEM) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
   const int64_t units = (int64_t)p.tiles_m * p.tiles_n * p.splits;
   if (units > INT32_MAX / 2) return SNN_ERR_UNSUPPORTED;
-  kernel<<<2 * (unsigned)std::min<int64_t>(units, pairs), 32 * (2 + WARPS), VL_SMEM, stream>>>(p);
-  return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+  return launch(kernel, dim3(2 * (unsigned)std::min<int64_t>(units, pairs)), 32 * (2 + WARPS), VL_SMEM, stream, p.behind, p);
 }
 bool eight_warps(const ProductParams& p) { return p.planes == 2 || p.kblocks < VL_SHORT; }
 template <int EPI, bool A_MN, bool B_MN> snn_status launch_product(const ProductParams& p, int pairs, cudaStream_t stream) {
@@ -1037,12 +1068,10 @@ struct Call {
     if (work == 0) return SNN_OK;
     const dim3 grid((unsigned)std::min<int64_t>(work, 148 * 8), factor ? 3 : 2);
     if (p.tops) {
-      largest_kernel<<<dim3(grid.x, 2), 256, 0, stream>>>(p);
-      stage_kernel<float><<<grid, 256, 0, stream>>>(p);
-    } else {
-      stage_kernel<__half><<<grid, 256, 0, stream>>>(p);   // 16 bits are copied, whatever they mean
+      const snn_status st = launch(largest_kernel, dim3(grid.x, 2), 256, 0, stream, false, p);   // (behind a memset)
+      return st != SNN_OK ? st : launch(stage_kernel<float>, grid, 256, 0, stream, true, p);
     }
-    return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+    return launch(stage_kernel<__half>, grid, 256, 0, stream, false, p);   // 16 bits are copied, whatever they mean
   }
   const void* data(const Operand& o, const void* direct) const { return o.staged ? ws + o.offset : direct; }
   bool map(CUtensorMap* m, const Operand& o, const void* direct, int rows, int cols, bool mn_major) const {
@@ -1052,11 +1081,10 @@ struct Call {
   snn_status row_losses(const float2* partial, int tiles, const float* target_z) const {
     float* const row_loss = (float*)(ws + l.row_loss);
     const bool one = a->rows <= 32;
-    row_loss_kernel<<<ceil_div(a->rows, 32), 1024, 0, stream>>>(partial, tiles, target_z, a->rows, a->targets, a->target_bits, a->ignore_index,
-                                                                a->classes, a->lse, row_loss, a->row_loss, one ? a->loss : nullptr);
-    if (!one)
-      mean_kernel<<<1, 1024, 0, stream>>>(row_loss, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, a->loss);
-    return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+    const snn_status st = launch(row_loss_kernel, dim3(ceil_div(a->rows, 32)), 1024, 0, stream, true, partial, tiles, target_z, a->rows, a->targets,
+                                 a->target_bits, a->ignore_index, a->classes, a->lse, row_loss, a->row_loss, one ? a->loss : nullptr);
+    if (st != SNN_OK || one) return st;
+    return launch(mean_kernel, dim3(1), 1024, 0, stream, true, row_loss, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes, a->loss);
   }
   ProductParams base() const {
     ProductParams p{};
@@ -1071,6 +1099,7 @@ struct Call {
     p.targets = a->targets; p.target_bits = a->target_bits; p.ignore_index = a->ignore_index; p.classes = a->classes;
     p.z_scale = a->scale * LOG2E;
     p.status = status();
+    p.behind = true;
     return p;
   }
 };
@@ -1092,9 +1121,8 @@ template <typename IO> snn_status forward_few(const Call& c) {
   else if (a->rows == 2) launch_few<IO, 2>(c, p);
   else launch_few<IO, 4>(c, p);
   if (cudaGetLastError() != cudaSuccess) return SNN_ERR_CUDA;
-  few_loss_kernel<<<1, 1024, 0, c.stream>>>(p.partial, few_blocks(a), p.target_z, a->rows, a->targets, a->target_bits, a->ignore_index, a->classes,
-                                            a->lse, a->row_loss, a->loss);
-  return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+  return launch(few_loss_kernel, dim3(1), 1024, 0, c.stream, true, p.partial, few_blocks(a), p.target_z, a->rows, a->targets, a->target_bits,
+                a->ignore_index, a->classes, a->lse, a->row_loss, a->loss);
 }
 
 #define VL_TRY(expr)                            \
@@ -1127,6 +1155,7 @@ extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void*
   const int w_rows = by_class ? a->classes : a->dim, w_cols = by_class ? a->dim : a->classes;
   VL_TRY(c.stage_operands(nullptr));
   ProductParams p = c.base();
+  p.behind = c.l.x.staged || c.l.w.staged;
   p.status = nullptr;   // (a wait that ran out shows in the losses)
   if (!c.map(&p.a, c.l.x, a->x, a->rows, a->dim, false) || !c.map(&p.b, c.l.w, a->w, w_rows, w_cols, !by_class)) return SNN_ERR_CUDA;
   p.tiles_m = ceil_div(a->rows, UM_TILE);
@@ -1200,11 +1229,8 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
   const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a->dim, 1024), 64), (unsigned)std::min(a->rows, 16384));
   auto join = [&](auto io) {
     using IO = decltype(io);
-    join_dx_kernel<IO><<<grid, 256, 0, c.stream>>>((const float*)(c.ws + l.acc), splits, l.acc_split, l.acc_pitch, a->rows, a->dim, c.alpha(),
-                                                   a->targets, a->target_bits, a->ignore_index, a->classes, (IO*)a->dx, a->dx_stride, c.status(), c.tops());
+    return launch(join_dx_kernel<IO>, grid, 256, 0, c.stream, true, (const float*)(c.ws + l.acc), splits, l.acc_split, l.acc_pitch, a->rows, a->dim,
+                  c.alpha(), a->targets, a->target_bits, a->ignore_index, a->classes, (IO*)a->dx, a->dx_stride, c.status(), c.tops());
   };
-  if (a->dtype == SNN_DTYPE_FP32) join(float());
-  else if (a->dtype == SNN_DTYPE_BF16) join(__nv_bfloat16());
-  else join(__half());
-  return cudaGetLastError() == cudaSuccess ? SNN_OK : SNN_ERR_CUDA;
+  return a->dtype == SNN_DTYPE_FP32 ? join(float()) : a->dtype == SNN_DTYPE_BF16 ? join(__nv_bfloat16()) : join(__half());
 }

@@ -12,8 +12,8 @@
 //
 // The kernels are bound by HBM as long as a step costs few instructions: channels are handled in pairs (f32x2 arithmetic),
 // tiles of 64 steps x 64 channels arrive by TMA a turn or two ahead and leave by TMA, so that the threads compute no
-// addresses.  Data that TMA cannot describe (rows that are not multiples of 16 bytes) takes one of two other paths: pairs
-// copied by cp.async, or plain loads of single values.
+// addresses.  Data that TMA cannot describe (rows that are not multiples of 16 bytes) takes one of two other paths: plain
+// loads of pairs, or of single values.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

@@ -28,11 +28,11 @@ namespace {
 
 constexpr uint32_t VL_TIMEOUT = 1u;               // status bit: a bounded wait ran out
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int VL_RUN = 8;                                    // k-blocks per run (fp32 operands)
 // Warps of the epilogue: one per quarter of tensor memory's lanes, or two with half of the tile's columns each.  Two hide
 // the epilogue's latency where the contraction is short and the epilogue sets the pace (8192 x 64 x 65536 bf16 forward: 403
 // us with four warps, 336 with eight); where it is long four leave more of the SM to the products (8192 x 2048 x 131072
 // backward: 9.3 ms against 9.8).
-constexpr int VL_RUN = 8;                                    // k-blocks per run (fp32 operands)
 constexpr int VL_SHORT = 16;                                 // k-blocks: eight warps below
 constexpr uint32_t VL_STORE_BYTES = UM_HALF * 128;           // one staged block of dz per half: 128 rows x 64 values
 constexpr size_t VL_SMEM = 1024 + (size_t)UM_STAGES * UM_STAGE_BYTES + 2 * VL_STORE_BYTES + 256;

@@ -333,8 +333,9 @@ def vocab_loss(x: torch.Tensor, w_out: torch.Tensor, targets: torch.Tensor, *, s
     """Mean soft-max cross entropy of the logits scale * x w_out, which are never stored.
 
     x: [rows][dim], w_out: [dim][classes] of the same type (fp32, bf16 or fp16), stored by feature (contiguous) or by class
-    (`table.t()` of a [classes][dim] table); 16-bit operands whose rows are not multiples of 16 bytes are copied first.  targets: int32 or int64 [rows]; rows with ignore_index do not count, any other
-    target outside [0, classes) makes its row's loss and the mean NaN.
+    (`table.t()` of a [classes][dim] table); 16-bit operands whose rows are not multiples of 16 bytes are copied first.
+    targets: int32 or int64 [rows]; rows with ignore_index do not count, any other target outside [0, classes) makes its
+    row's loss and the mean NaN.
     Returns (loss, a 0-d tensor; row_loss [rows]; lse [rows], the log-sum-exp that `vocab_loss_backward` needs), all fp32,
     with zeros for rows that do not count."""
     a = _vocab_args(x, w_out, targets, scale, ignore_index)

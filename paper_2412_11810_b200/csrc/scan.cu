@@ -8,7 +8,7 @@
 // every segment (it reads the inputs once more, without a barrier in its loop), and the blocks of the second one chain the
 // summaries of the segments before their own.  (Blocks in a cluster that hand summaries on every turn read the inputs only
 // once, but wait for one another: 65536 x 1024 bf16 forward took 235 us that way.)  The order of the arithmetic is fixed
-// by the sizes alone.
+// by the sizes and by what is kept.
 //
 // The kernels are bound by HBM as long as a step costs few instructions: channels are handled in pairs (f32x2 arithmetic),
 // tiles of 64 steps x 64 channels arrive by TMA a turn or two ahead and leave by TMA, so that the threads compute no
@@ -808,21 +808,29 @@ ScanParams params_of(const snn_scan_args* a) {
 }
 // Segments of the time axis: as many as fill the device once (`resident` blocks fit an SM), each with two turns at least.
 // Below four segments one is as fast: what the SMs left idle would win goes into reading the inputs twice and into a second
-// launch (2048 x 2 x 4096 bf16, 128 tiles: 43 us with one segment, 42 with three; 4096 x 2 x 512, 16 tiles: 80 and 18).
+// launch (2048 x 2 x 4096 bf16, 128 tiles: 43 us with one segment, 42 with three, 41 with four; 4096 x 2 x 512, 16 tiles: 80 and 18).
 void cut_time(ScanParams& p, int resident) {
   const int64_t tiles = std::max<int64_t>((int64_t)p.B * p.n_tiles, 1);
   int64_t n = std::min<int64_t>(148 * resident / tiles, p.T / (2 * SNN_SCAN_CHUNK));
   if (n < 4) n = 1;
   p.segment_steps = (int)((((int64_t)p.T + n - 1) / n + SNN_SCAN_CHUNK - 1) / SNN_SCAN_CHUNK * SNN_SCAN_CHUNK);
   p.segments = p.segment_steps ? (p.T + p.segment_steps - 1) / p.segment_steps : 1;
-  // the summary's blocks are small and wait for their loads: twice as many of them, as long as a warp has 32 steps
-  p.parts = p.segment_steps >= 2 * WARPS * 32 ? 2 : 1;
+  // the summary's blocks wait for their loads, and more than fit at once share the work more evenly: parts as long as a
+  // warp has 128 steps (65536 x 1 x 2048 bf16 backward, 912 steps per warp with one part: 516, 493, 469, 470 us with 1, 2,
+  // 4, 8; 65536 x 1 x 1024, 456 steps: 211, 195, 196, 196; forward, 304 steps: 144, 142, 145, 150)
+  p.parts = 1;
+  while (p.parts < 4 && p.segment_steps >= 2 * p.parts * WARPS * 128) p.parts *= 2;
 }
-int resident_blocks(const snn_scan_args* a, bool backward) { return (backward ? 2 : 3) - (a->dtype == SNN_DTYPE_FP32); }
+// Blocks per SM: a forward pass that keeps nothing fits a fourth one of 16-bit values (65536 x 1 x 1024 bf16: 142 us with
+// segments for three, 133 for four).
+int resident_blocks(int dtype, bool backward, bool keep) {
+  if (dtype == SNN_DTYPE_FP32) return backward ? 1 : 2;
+  return backward ? 2 : keep ? 3 : 4;
+}
 size_t summary_bytes(const ScanParams& p) { return p.segments > 1 ? sizeof(float4) * 32 * (size_t)p.segments * p.parts * p.B * p.n_tiles : 0; }
 
 snn_status set_segments(ScanParams& p, const snn_scan_args* a, bool backward) {
-  cut_time(p, resident_blocks(a, backward));
+  cut_time(p, resident_blocks(a->dtype, backward, a->states != nullptr));
   if (p.segments == 1) return SNN_OK;
   if (a->workspace_bytes < summary_bytes(p)) return SNN_ERR_WORKSPACE_TOO_SMALL;
   if (!a->workspace || (uintptr_t)a->workspace % 256 != 0) return SNN_ERR_INVALID_ARG;
@@ -844,8 +852,11 @@ extern "C" snn_status snn_scan_workspace(const snn_scan_args* a, int32_t backwar
   if (st != SNN_OK) return st;
   if (!bytes) return SNN_ERR_INVALID_ARG;
   ScanParams p = params_of(a);
-  cut_time(p, resident_blocks(a, backward != 0));
-  *bytes = summary_bytes(p);
+  *bytes = 0;
+  for (bool keep : {false, true}) {   // enough for either forward pass
+    cut_time(p, resident_blocks(a->dtype, backward != 0, keep));
+    *bytes = std::max(*bytes, summary_bytes(p));
+  }
   return SNN_OK;
 }
 

@@ -165,7 +165,7 @@ class ScanKept:
 
 
 def _scan_workspace(a: sb.snn_scan_args, backward: bool, like: torch.Tensor) -> Optional[torch.Tensor]:
-    if a.B * a.N >= 128 * 64 or a.T < 512:   # only few channels and many steps need one
+    if a.B * a.N >= 149 * 64 or a.T < 512:   # only few channels and many steps need one
         return None
     n = sb.snn_scan_workspace(a, backward)
     if n == 0:

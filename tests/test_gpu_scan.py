@@ -324,3 +324,27 @@ def test_pack_strided_rows_and_long_tensors():
     assert np.array_equal(f64(ops().unpack_activation(p)), ref.eight_bits(f64(view), "int8")[0])
     assert ops().unpack_activation(ops().pack_activation(torch.zeros(0, 5, device="cuda"))).shape == (0, 5)
     assert ops().unpack_activation(ops().pack_activation(torch.zeros(5, 0, device="cuda"))).shape == (5, 0)
+
+
+@pytest.mark.parametrize("T,B,N,length", [(40007, 1, 2048, None), (40007, 1, 2048, 37003), (3001, 2, 70, 1500), (70001, 3, 33, None)])
+def test_segments_of_the_time_axis_lose_nothing(T, B, N, length):
+    """With gates of one and small whole numbers the states are running sums that fp32 holds exactly, in any order: every
+    part of a segment has to arrive, whether or not the pass keeps states (which cuts the time axis differently)."""
+    g = torch.Generator(device="cuda").manual_seed(T + N)
+    whole = lambda *shape: torch.randint(-1, 2, shape, generator=g, device="cuda").float()  # noqa: E731
+    x, dh, state, dlast, gate = whole(T, B, N), whole(T, B, N), whole(B, N), whole(B, N), torch.ones(T, B, N, device="cuda")
+    lengths, end = None, T
+    if length is not None:
+        lengths, end = torch.full((B,), length, dtype=torch.int32, device="cuda"), length
+    want = torch.zeros(T, B, N, device="cuda")
+    want[:end] = state + x[:end].cumsum(0)
+    d = torch.zeros_like(want)
+    d[:end] = dlast + dh[:end].flip(0).cumsum(0).flip(0)
+    before = torch.cat([state[None], want[:-1]])
+    for keep in (None, "raw"):
+        h, last, kept = ops().gated_scan(x, gate, state, lengths=lengths, mode="direct", keep=keep)
+        assert torch.equal(h, want) and torch.equal(last, want[end - 1])
+    dx, dgate, dstate = ops().gated_scan_backward(kept, dh, dlast)
+    assert torch.equal(dx, d) and torch.equal(dstate, d[0])
+    assert float((d * before).abs().max()) < 2 ** 24   # so the products are exact too
+    assert torch.equal(dgate, d * before)

@@ -455,6 +455,12 @@ typedef struct {
 snn_status snn_vocab_loss_workspace(const snn_vocab_loss_args* args, int32_t backward, size_t* bytes);
 snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* args, void* stream);
 snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* args, void* stream);
+/* A self-test of the bounded waits: the same pass, in which waits of one of its product kernels run out (kernel 0 of the
+ * forward pass: the logits' sums; 0, 1, 2 of the backward pass: the derivatives by the logits, dx, dw) after poll_limit polls,
+ * since from the unit-th tile of work on nothing is loaded (quits = 0) or one warp does not wait (quits = 1).  The call ends
+ * all the same and the results that need those tiles are NaN.  It does not apply to forward passes of four rows or fewer. */
+snn_status snn_selftest_vocab_loss_wait(const snn_vocab_loss_args* args, int32_t backward, int32_t kernel, int32_t unit, int32_t quits,
+                                        uint32_t poll_limit, void* stream);
 
 #ifdef __cplusplus
 }

@@ -81,6 +81,10 @@ struct ProductParams {
   const float* alpha;         // DW: factor, from the device
   const uint32_t* tops;       // fp32 operands: bit patterns of the largest magnitudes of x and w
   uint32_t* status;
+  // limits of the waits; the self-test lets them run out: no loads from a unit of work on, or one warp of the epilogue that
+  // does not wait for it
+  uint32_t polls;
+  int loads_end, quits_at;
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -109,14 +113,26 @@ struct Barriers {
 };
 
 // A bounded wait that also ends when another role of this block gave up.
-__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Barriers& s, uint32_t* status) {
-  for (uint32_t i = 0; i < MBAR_WAIT_LIMIT; ++i) {
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, Barriers& s, uint32_t* status, uint32_t limit) {
+  for (uint32_t i = 0; i < limit; ++i) {
     if (mbar_try_wait(bar, parity)) return true;
     if ((i & 63u) == 63u && *reinterpret_cast<volatile uint32_t*>(&s.gave_up)) return false;
   }
   *reinterpret_cast<volatile uint32_t*>(&s.gave_up) = 1u;
   if (status) atomicOr(status, VL_TIMEOUT);
   return false;
+}
+
+// Whether all 128 threads at a named barrier say so.
+__device__ __forceinline__ bool together(bool ok, int barrier) {
+  uint32_t all;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 p, %2, 0;\n\t"
+      "barrier.cta.red.and.pred q, %1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(all) : "r"(barrier), "r"((uint32_t)ok) : "memory");
+  return all != 0;
 }
 
 template <bool MN_MAJOR>
@@ -184,14 +200,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
     if (lane == 0) {   // loads: this block's halves of A and B, announced to the even block's barrier
       int it = 0;
       bool ok = true;
-      for (int u = pair; u < units && ok; u += n_pairs_sm) {
+      for (int u = pair; u < units && u < p.loads_end && ok; u += n_pairs_sm) {
         const Unit w = unit_of<EPI>(p, u);
         const int row_a = p.a0 + w.m * UM_TILE + (int)rank * UM_HALF, row_b = p.b0 + w.n * UM_TILE + (int)rank * UM_HALF;
         for (int q = 0; q < p.n_pairs && ok; ++q) {
           const int plane_a = (p.pair_a >> (4 * q)) & 15, plane_b = (p.pair_b >> (4 * q)) & 15;
           for (int kb = 0; kb < w.kbs; ++kb, ++it) {
             const int st = it % UM_STAGES;
-            if (it >= UM_STAGES && !(ok = wait_for(&s.empty[st], (uint32_t)(it / UM_STAGES - 1) & 1u, s, p.status))) break;
+            if (it >= UM_STAGES && !(ok = wait_for(&s.empty[st], (uint32_t)(it / UM_STAGES - 1) & 1u, s, p.status, p.polls))) break;
             unsigned char* const at = s_base + (size_t)st * UM_STAGE_BYTES;
             if (rank == 0) mbar_arrive_expect_tx(&s.full[st], 2 * UM_STAGE_BYTES);
             const uint32_t bar = peer_address(smem_u32(&s.full[st]), 0);
@@ -212,12 +228,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
         const int n_it = p.n_pairs * w.kbs;
         for (int i0 = 0; i0 < n_it && ok; i0 += RUNS ? VL_RUN : n_it, ++run) {   // a run of k-blocks into one accumulator
           const int buf = run & 1, end = RUNS ? min(i0 + VL_RUN, n_it) : n_it;
-          if (run >= 2 && !(ok = wait_for(&s.acc_empty[buf], (uint32_t)(run / 2 - 1) & 1u, s, p.status))) break;
+          if (run >= 2 && !(ok = wait_for(&s.acc_empty[buf], (uint32_t)(run / 2 - 1) & 1u, s, p.status, p.polls))) break;
           tcgen05_after_sync();
           const uint32_t acc = tmem + (uint32_t)buf * UM_TILE;
           for (int i = i0; i < end; ++i, ++it) {
             const int st = it % UM_STAGES;
-            if (!(ok = wait_for(&s.full[st], (uint32_t)(it / UM_STAGES) & 1u, s, p.status))) break;
+            if (!(ok = wait_for(&s.full[st], (uint32_t)(it / UM_STAGES) & 1u, s, p.status, p.polls))) break;
             tcgen05_after_sync();
             const uint32_t at = smem_u32(s_base + (size_t)st * UM_STAGE_BYTES);
 #pragma unroll
@@ -241,7 +257,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
     bool ok = true;
     float sums[RUNS ? WIDTH : 1];
     // the run's accumulator is complete / may be filled again
-    auto run_full = [&]() { return __all_sync(0xffffffffu, wait_for(&s.acc_full[run & 1], (uint32_t)(run / 2) & 1u, s, p.status)); };
+    auto run_full = [&](int u) {
+      const uint32_t polls = warp == 2 && u >= p.quits_at ? 0u : p.polls;
+      return (bool)__all_sync(0xffffffffu, wait_for(&s.acc_full[run & 1], (uint32_t)(run / 2) & 1u, s, p.status, polls));
+    };
     auto run_read = [&]() {
       tcgen05_before_sync();
       __syncwarp();
@@ -256,7 +275,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
 #pragma unroll
         for (int j = 0; j < WIDTH; ++j) sums[j] = 0.f;
 #pragma unroll 1
-        for (int r = 0; r < n_runs && (ok = run_full()); ++r) {
+        for (int r = 0; r < n_runs && (ok = run_full(u)); ++r) {
           tcgen05_after_sync();
 #pragma unroll
           for (int c = 0; c < WIDTH; c += 16) {
@@ -268,8 +287,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
           run_read();
         }
       } else {
-        ok = run_full();
+        ok = run_full(u);
       }
+      // Every warp decides for itself whether a wait ran out.  Those that share the buffers of dz meet at a barrier, where one
+      // that left would be waited for without end: they go on together or not at all.
+      if constexpr (EPI == GRAD) ok = together(ok, 1 + half);
       if (!ok) {
         if (EPI == STATS) {   // the rows' losses become NaN
           const float nan = __uint_as_float(0x7fc00000u);
@@ -1029,8 +1051,14 @@ template <int EPI> snn_status launch_z(const ProductParams& p, bool by_class, in
   return by_class ? launch_product<EPI, false, false>(p, pairs, stream) : launch_product<EPI, false, true>(p, pairs, stream);
 }
 
+struct WaitTest {   // of snn_selftest_vocab_loss_wait
+  int kernel, unit;
+  bool quits;
+  uint32_t polls;
+};
 struct Call {
   const snn_vocab_loss_args* a;
+  const WaitTest* test;
   Layout l;
   char* ws;
   cudaStream_t stream;
@@ -1100,7 +1128,15 @@ struct Call {
     p.z_scale = a->scale * LOG2E;
     p.status = status();
     p.behind = true;
+    p.polls = MBAR_WAIT_LIMIT;
+    p.loads_end = p.quits_at = INT32_MAX;
     return p;
+  }
+  // the self-test's limits for the call's kernel of this number
+  void limit(ProductParams& p, int kernel) const {
+    if (!test || test->kernel != kernel) return;
+    p.polls = test->polls;
+    (test->quits ? p.quits_at : p.loads_end) = test->unit;
   }
 };
 
@@ -1141,10 +1177,11 @@ extern "C" snn_status snn_vocab_loss_workspace(const snn_vocab_loss_args* a, int
   return SNN_OK;
 }
 
-extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void* stream) {
+namespace {
+snn_status forward(const snn_vocab_loss_args* a, const WaitTest* test, void* stream) {
   VL_TRY(check(a));
   if (!a->loss || (a->rows > 0 && !a->lse)) return SNN_ERR_INVALID_ARG;
-  Call c{a};
+  Call c{a, test};
   VL_TRY(c.begin(false, stream));
   if (a->rows == 0) return cudaMemsetAsync(a->loss, 0, 4, c.stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
   if (few_rows(a))
@@ -1165,17 +1202,18 @@ extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void*
   p.n = a->classes;
   p.partial = (float2*)(c.ws + c.l.partial);
   p.target_z = (float*)(c.ws + c.l.target_z);
+  c.limit(p, 0);
   VL_TRY(launch_z<STATS>(p, by_class, c.pairs, c.stream));
   return c.row_losses(p.partial, (eight_warps(p) ? 2 : 1) * p.tiles_n, p.target_z);
 }
 
-extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void* stream) {
+snn_status backward(const snn_vocab_loss_args* a, const WaitTest* test, void* stream) {
   VL_TRY(check(a));
   const bool by_class = a->w_layout == SNN_W_BY_CLASS;
   const int w_rows = by_class ? a->classes : a->dim, w_cols = by_class ? a->dim : a->classes;
   if (!a->dw || (a->rows > 0 && (!a->dx || !a->lse))) return SNN_ERR_INVALID_ARG;
   if ((a->rows > 1 && a->dx_stride < a->dim) || (w_rows > 1 && a->dw_stride < w_cols)) return SNN_ERR_INVALID_ARG;
-  Call c{a};
+  Call c{a, test};
   VL_TRY(c.begin(true, stream));
   const size_t size = a->dtype == SNN_DTYPE_FP32 ? 4 : 2;
   if (a->rows == 0)
@@ -1199,6 +1237,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     p.tiles_m = ceil_div(a->rows, UM_TILE); p.tiles_n = ceil_div(width, UM_TILE); p.kblocks = ceil_div(a->dim, UM_KB);
     p.m = a->rows; p.n = width; p.b0 = v0;
     p.lse = a->lse;
+    c.limit(p, 0);
     VL_TRY(launch_z<GRAD>(p, by_class, c.pairs, c.stream));
     p = base;                 // dx += dz w^T
     p.a = dz_k; p.b = w_dx;
@@ -1207,6 +1246,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     p.bk0 = v0;
     p.m = a->rows; p.n = a->dim;
     p.acc = (float*)(c.ws + l.acc); p.acc_pitch = l.acc_pitch; p.acc_split = l.acc_split; p.accumulate = v0 > 0;
+    c.limit(p, 1);
     VL_TRY((by_class ? launch_product<DX, false, true>(p, c.pairs, c.stream) : launch_product<DX, false, false>(p, c.pairs, c.stream)));
     p = base;                 // the piece's part of dw
     p.kblocks = ceil_div(a->rows, UM_KB);
@@ -1223,6 +1263,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
     }
     p.dw_vector = (uintptr_t)p.dw % 16 == 0 && p.dw_stride * (int64_t)size % 16 == 0;
     p.tiles_m = ceil_div(p.m, UM_TILE); p.tiles_n = ceil_div(p.n, UM_TILE);
+    c.limit(p, 2);
     VL_TRY((launch_product<DW, true, true>(p, c.pairs, c.stream)));
   }
   const int splits = std::min(l.splits, ceil_div(std::min(l.piece, a->classes), UM_KB));
@@ -1233,4 +1274,15 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
                   c.alpha(), a->targets, a->target_bits, a->ignore_index, a->classes, (IO*)a->dx, a->dx_stride, c.status(), c.tops());
   };
   return a->dtype == SNN_DTYPE_FP32 ? join(float()) : a->dtype == SNN_DTYPE_BF16 ? join(__nv_bfloat16()) : join(__half());
+}
+}  // namespace
+
+extern "C" snn_status snn_vocab_loss_forward(const snn_vocab_loss_args* a, void* stream) { return forward(a, nullptr, stream); }
+extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void* stream) { return backward(a, nullptr, stream); }
+
+extern "C" snn_status snn_selftest_vocab_loss_wait(const snn_vocab_loss_args* a, int32_t is_backward, int32_t kernel, int32_t unit, int32_t quits,
+                                                   uint32_t poll_limit, void* stream) {
+  if (kernel < 0 || kernel > (is_backward ? 2 : 0) || unit < 0 || poll_limit == 0 || poll_limit > MBAR_WAIT_LIMIT) return SNN_ERR_INVALID_ARG;
+  const WaitTest test{kernel, unit, quits != 0, poll_limit};
+  return is_backward ? backward(a, &test, stream) : forward(a, &test, stream);
 }

@@ -168,3 +168,10 @@ def test_reference_eight_bits():
     assert np.array_equal(q[0], [127, 2, 0, 64]) and s[0, 0] == 127 and s[1, 0] == 129
     q, s = ref.eight_bits(v, "e4m3")
     assert np.array_equal(q, [[128, 2.5, -0.5, 64], [448, 448, 16, 0]]) and s[0, 0] == 126 and s[1, 0] == 128
+
+
+def test_loss_wait_selftest_refuses_invalid_arguments():
+    call = lambda a, *v: sb.lib.snn_selftest_vocab_loss_wait(C.byref(a), *v, None)  # noqa: E731
+    for v in ((0, 1, 0, 0, 10), (1, 3, 0, 0, 10), (1, -1, 0, 0, 10), (1, 0, -1, 0, 10), (1, 0, 0, 0, 0), (1, 0, 0, 0, 1 << 23)):
+        assert call(_loss_args(), *v) == sb.SNN_ERR_INVALID_ARG
+    assert call(_loss_args(rows=-1), 1, 0, 0, 0, 10) == sb.SNN_ERR_INVALID_ARG

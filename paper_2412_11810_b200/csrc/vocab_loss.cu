@@ -163,6 +163,12 @@ template <int EPI> __device__ __forceinline__ Unit unit_of(const ProductParams& 
   return w;
 }
 
+__device__ __forceinline__ void store_dw(const ProductParams& p, int64_t at, float f) {
+  if (p.dw_dtype == SNN_DTYPE_FP32) ((float*)p.dw)[at] = f;
+  else if (p.dw_dtype == SNN_DTYPE_BF16) ((__nv_bfloat16*)p.dw)[at] = __float2bfloat16_rn(f);
+  else ((__half*)p.dw)[at] = __float2half_rn(f);
+}
+
 template <int EPI, bool A_MN, bool B_MN, int WARPS, bool RUNS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1) product_kernel(const __grid_constant__ ProductParams p) {
   constexpr int HALVES = WARPS / 4, WIDTH = UM_TILE / HALVES;   // columns per warp of the epilogue
@@ -251,7 +257,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
     const int quarter = warp & 3, row_in_block = quarter * 32 + lane, half = (warp - 2) / 4, half_col0 = half * WIDTH;
     const bool storer = threadIdx.x == 64 + 128 * half;   // of the half's dz blocks
     int store_buf = half;
-    const float alpha = EPI == DW ? *p.alpha * (p.tops ? operand_unscale(p.tops[0]) : 1.f) : 0.f;
+    const float nan = __uint_as_float(0x7fc00000u);
+    // (a wait that ran out in a kernel before: dz is not what it should be)
+    const float alpha = EPI != DW ? 0.f : *p.status & VL_TIMEOUT ? nan : *p.alpha * (p.tops ? operand_unscale(p.tops[0]) : 1.f);
     const float z_scale = p.tops ? p.z_scale * operand_unscale(p.tops[0]) * operand_unscale(p.tops[1]) : p.z_scale;
     int run = 0;
     bool ok = true;
@@ -294,11 +302,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
       if constexpr (EPI == GRAD) ok = together(ok, 1 + half);
       if (!ok) {
         if (EPI == STATS) {   // the rows' losses become NaN
-          const float nan = __uint_as_float(0x7fc00000u);
           for (; u < units; u += n_pairs_sm) {
             const Unit left = unit_of<EPI>(p, u);
             const int row = left.m * UM_TILE + (int)rank * UM_HALF + row_in_block;
             if (row < p.m) p.partial[((int64_t)left.n * HALVES + half) * p.m + row] = make_float2(nan, nan);
+          }
+        }
+        if (EPI == DW) {      // and the gradients of the tiles that are left
+          for (; u < units; u += n_pairs_sm) {
+            const Unit left = unit_of<EPI>(p, u);
+            const int row = left.m * UM_TILE + (int)rank * UM_HALF + row_in_block, col0 = left.n * UM_TILE + half_col0;
+            for (int c = 0; c < WIDTH && row < p.m && col0 + c < p.n; ++c) store_dw(p, (int64_t)row * p.dw_stride + col0 + c, nan);
           }
         }
         break;
@@ -446,10 +460,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
 #pragma unroll 4
               for (int r = 0; r < n_rows; ++r) {
                 const float f = mine[r * 32 + (lane ^ r)];
-                const int64_t to = at + r * p.dw_stride;
-                if (p.dw_dtype == SNN_DTYPE_FP32) ((float*)p.dw)[to] = f;
-                else if (p.dw_dtype == SNN_DTYPE_BF16) ((__nv_bfloat16*)p.dw)[to] = __float2bfloat16_rn(f);
-                else ((__half*)p.dw)[to] = __float2half_rn(f);
+                store_dw(p, at + r * p.dw_stride, f);
               }
             }
             continue;

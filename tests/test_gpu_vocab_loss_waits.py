@@ -66,3 +66,27 @@ def test_losses_are_nan_when_a_wait_runs_out(dtype, D, quits):
     on = t >= 0
     lost = on if not quits else on & (torch.arange(2600, device="cuda") % 128 // 32 == 2)
     assert torch.isnan(row[lost]).all() and torch.isnan(lse[lost]).all() and (row[~on] == 0).all()
+
+
+@pytest.mark.parametrize("quits", [False, True])
+@pytest.mark.parametrize("kernel", [GRAD, DX, DW])
+@pytest.mark.parametrize("dtype,D", CASES + [("fp16", 72), ("bf16", 1001)])
+def test_gradients_are_nan_when_a_wait_runs_out(dtype, D, kernel, quits):
+    """No gradient is finite that rests on a tile that never came: all of dx, and of dw all if its derivatives are in doubt,
+    the tiles left out if it is its own product."""
+    from paper_2412_11810_b200 import ops
+    x, w, t = problem(2600, D, 5000, dtype)
+    _, _, lse = ops.vocab_loss(x, w, t)
+    dx, dw = backward_with_a_lost_wait(x, w, t, lse, kernel, 0, quits)
+    assert torch.isnan(dx[t >= 0]).all()
+    if kernel != DW or not quits:
+        assert torch.isnan(dw).all()
+    else:   # the warp that left had 32 of every 128 classes
+        assert torch.isnan(dw[:, torch.arange(5000, device="cuda") % 128 // 32 == 2][: 128 if dtype == "fp32" else 256]).all()
+    if kernel == DW and not quits and D == 1024:   # 20 x 4 tiles, classes by features; those before the 7th are whole
+        want = ops.vocab_loss_backward(x, w, t, lse)[1]
+        _, dw = backward_with_a_lost_wait(x, w, t, lse, kernel, 7, quits)
+        rows = torch.arange(5000, device="cuda") // 256
+        cols = torch.arange(D, device="cuda") // 256
+        unit = cols[:, None] + 4 * rows[None, :]
+        assert torch.isnan(dw[unit >= 7]).all() and torch.equal(dw[unit < 7], want[unit < 7])

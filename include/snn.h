@@ -393,7 +393,7 @@ typedef struct {
   const void *x, *gate;          /* [T][B][N]; the backward pass reads them only where the format is RAW        */
   int64_t x_stride[2], gate_stride[2];   /* of T and of B                                                       */
   const int32_t* lengths;        /* [B] or NULL                                                                 */
-  const float* state;            /* [B][N] or NULL; may be the same buffer as `last`                            */
+  const float* state;            /* [B][N] or NULL; may be the same buffer as `last` (no other buffers overlap) */
   void* h;                       /* [T][B][N], forward                                                          */
   int64_t h_stride[2];
   float* last;                   /* [B][N] or NULL, forward                                                     */

@@ -44,6 +44,8 @@ struct ScanParams {
   int segments, segment_steps; // of the time axis; a multiple of a chunk each
   int parts;                   // of a segment, summarised by a block each
   float4* summaries;           // [segments][parts][B][n_tiles][32] maps of pairs of channels, if there are several segments
+  float2* start;               // forward, several segments: the summary kernel's copy of `state`, [B][n_tiles][32].  The blocks of
+                               // the last segment write `last`, which may be the same buffer, while others still start
   int mode, x_format, gate_format;
   const void *x, *gate, *dh;
   void *h, *dx, *dgate;
@@ -350,7 +352,7 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
   if (loader)
     for (int d = 0; d < SCAN_DEPTH; ++d) issue(w.from + d * SNN_SCAN_CHUNK, d);
   float2 carry = both(0.f);   // warp 0 chains the summaries
-  if (w.warp == 0) carry = enter_segment<false>(p, w, load_state(p.state, w.b, p.N, w.c, w.n_ok));
+  if (w.warp == 0) carry = enter_segment<false>(p, w, p.segments > 1 ? p.start[w.map] : load_state(p.state, w.b, p.N, w.c, w.n_ok));
   bool alive = true;
   int turn = w.from;
   for (int i = 0; turn < w.end; turn += SNN_SCAN_CHUNK, ++i) {
@@ -740,6 +742,7 @@ __global__ void __launch_bounds__(32 * WARPS, sizeof(IO) == 2 ? 4 : 3) scan_summ
 #pragma unroll
     for (int v = 1; v < WARPS; ++v) m = then(m, as_map(s_sum[REVERSE ? WARPS - 1 - v : v][lane]));
     p.summaries[part * maps_per_part(p) + (int64_t)tile * 32 + lane] = as4(m);
+    if (!REVERSE && part == 0) p.start[(int64_t)tile * 32 + lane] = load_state(p.state, b, p.N, c, n_ok);
   }
 }
 
@@ -827,7 +830,8 @@ int resident_blocks(int dtype, bool backward, bool keep) {
   if (dtype == SNN_DTYPE_FP32) return backward ? 1 : 2;
   return backward ? 2 : keep ? 3 : 4;
 }
-size_t summary_bytes(const ScanParams& p) { return p.segments > 1 ? sizeof(float4) * 32 * (size_t)p.segments * p.parts * p.B * p.n_tiles : 0; }
+size_t map_bytes(const ScanParams& p) { return sizeof(float4) * 32 * (size_t)p.segments * p.parts * p.B * p.n_tiles; }
+size_t summary_bytes(const ScanParams& p) { return p.segments > 1 ? map_bytes(p) + sizeof(float2) * 32 * (size_t)p.B * p.n_tiles : 0; }
 
 snn_status set_segments(ScanParams& p, const snn_scan_args* a, bool backward) {
   cut_time(p, resident_blocks(a->dtype, backward, a->states != nullptr));
@@ -835,6 +839,7 @@ snn_status set_segments(ScanParams& p, const snn_scan_args* a, bool backward) {
   if (a->workspace_bytes < summary_bytes(p)) return SNN_ERR_WORKSPACE_TOO_SMALL;
   if (!a->workspace || (uintptr_t)a->workspace % 256 != 0) return SNN_ERR_INVALID_ARG;
   p.summaries = (float4*)a->workspace;
+  p.start = (float2*)((char*)a->workspace + map_bytes(p));
   return SNN_OK;
 }
 template <typename K> snn_status launch(K kernel, size_t smem, int64_t blocks, const ScanParams& p, cudaStream_t stream) {

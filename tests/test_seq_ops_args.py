@@ -175,3 +175,13 @@ def test_loss_wait_selftest_refuses_invalid_arguments():
     for v in ((0, 1, 0, 0, 10), (1, 3, 0, 0, 10), (1, -1, 0, 0, 10), (1, 0, -1, 0, 10), (1, 0, 0, 0, 0), (1, 0, 0, 0, 1 << 23)):
         assert call(_loss_args(), *v) == sb.SNN_ERR_INVALID_ARG
     assert call(_loss_args(rows=-1), 1, 0, 0, 0, 10) == sb.SNN_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("dtype", [sb.SNN_DTYPE_FP32, sb.SNN_DTYPE_BF16])
+def test_scan_workspace_has_room_for_the_first_state(dtype):
+    """Where the time axis is cut, the blocks of the last part write `last` while others still start: they take `state`, which
+    may be the same buffer, from a copy beside the summaries (16 bytes per pair of channels and part)."""
+    for T, B, N in ((4096, 1, 64), (65536, 1, 1024), (5000, 3, 100)):
+        tiles = B * -(-N // 64)
+        n = sb.snn_scan_workspace(_scan_args(T=T, B=B, N=N, dtype=dtype), False)
+        assert n > 0 and n % (tiles * 32 * 16) == tiles * 32 * 8

@@ -415,6 +415,11 @@ typedef struct {
 snn_status snn_scan_workspace(const snn_scan_args* args, int32_t backward, size_t* bytes);
 snn_status snn_scan_forward(const snn_scan_args* args, void* stream);
 snn_status snn_scan_backward(const snn_scan_args* args, void* stream);
+/* A self-test of the bounded waits: the same pass, in which the waits for tiles from step `step` on (in the order in which
+ * the pass goes through them) run out after poll_limit polls, since nothing is loaded (quits = 0) or one warp does not wait
+ * (quits = 1).  The call ends all the same; what rests on those steps is NaN.  It applies to data that TMA can describe
+ * (rows of multiples of 16 bytes), more than 16 steps or with states kept. */
+snn_status snn_selftest_scan_wait(const snn_scan_args* args, int32_t backward, int32_t step, int32_t quits, uint32_t poll_limit, void* stream);
 
 /* Soft-max cross entropy over a large vocabulary, with the readout product inside (the readout and loss of snn_train_step
  * for many classes: z = scale * x W_out, x [rows][dim], W_out [dim][classes]) and without storing z:

@@ -46,7 +46,7 @@ EXPORTS = ["snn_create", "snn_destroy", "snn_alpha", "snn_workspace_query", "snn
            "snn_phase_times_get", "snn_train_step_static", "snn_suggest_ckpt", "snn_selftest_wait_timeout",
            "snn_debug_checks_enabled", "snn_activation_pack", "snn_activation_unpack", "snn_scan_forward",
            "snn_scan_backward", "snn_scan_workspace", "snn_vocab_loss_workspace", "snn_vocab_loss_forward", "snn_vocab_loss_backward",
-           "snn_selftest_vocab_loss_wait"]
+           "snn_selftest_scan_wait", "snn_selftest_vocab_loss_wait"]
 SNN_STATIC_WORKSPACE_BYTES = 32 << 20
 
 
@@ -150,6 +150,7 @@ def _load() -> C.CDLL:
     lib.snn_scan_workspace.argtypes = [C.POINTER(snn_scan_args), C.c_int32, C.POINTER(C.c_size_t)]
     lib.snn_scan_forward.argtypes = [C.POINTER(snn_scan_args), C.c_void_p]
     lib.snn_scan_backward.argtypes = [C.POINTER(snn_scan_args), C.c_void_p]
+    lib.snn_selftest_scan_wait.argtypes = [C.POINTER(snn_scan_args), C.c_int32, C.c_int32, C.c_int32, C.c_uint32, C.c_void_p]
     lib.snn_vocab_loss_workspace.argtypes = [C.POINTER(snn_vocab_loss_args), C.c_int32, C.POINTER(C.c_size_t)]
     lib.snn_vocab_loss_forward.argtypes = [C.POINTER(snn_vocab_loss_args), C.c_void_p]
     lib.snn_vocab_loss_backward.argtypes = [C.POINTER(snn_vocab_loss_args), C.c_void_p]
@@ -289,6 +290,10 @@ def snn_scan_forward(args: snn_scan_args, stream: int = 0) -> None:
 
 def snn_scan_backward(args: snn_scan_args, stream: int = 0) -> None:
     _check(lib.snn_scan_backward(C.byref(args), stream))
+
+
+def snn_selftest_scan_wait(args: snn_scan_args, backward: bool, step: int, quits: bool, poll_limit: int, stream: int = 0) -> None:
+    _check(lib.snn_selftest_scan_wait(C.byref(args), int(backward), step, int(quits), poll_limit, stream))
 
 
 def snn_vocab_loss_workspace(args: snn_vocab_loss_args, backward: bool) -> int:

@@ -54,6 +54,10 @@ struct ScanParams {
   const float *state, *dlast;
   float *last, *states, *dstate;
   uint8_t *x_codes, *x_scales, *gate_codes, *gate_scales;
+  // TILES: limits of the waits.  The self-test lets them run out: no loads of the turns from this step on (in the order in
+  // which the pass goes), or a warp that does not wait for them
+  uint32_t polls;
+  int loads_end, quits_at;
 };
 
 struct Map2 {   // the affine maps of two channels
@@ -340,7 +344,7 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
   auto issue = [&](int turn, int slot) {   // by one thread
     unsigned char* const at = s_dyn + slot * SLOT;
     if constexpr (PATH == TILES) {
-      if (turn < w.end) {
+      if (turn < w.end && turn < p.loads_end) {
         mbar_arrive_expect_tx(&s_landed[slot], SLOT);
         tma_load_3d(at, &p.in[0], w.col0, w.b, turn, &s_landed[slot]);
         tma_load_3d(at + SLOT / 2, &p.in[1], w.col0, w.b, turn, &s_landed[slot]);
@@ -364,12 +368,15 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
       load_values<PATH == PAIRS>(xv, x, p.xs[0], w, t0);
       load_values<PATH == PAIRS>(gv, gate, p.gs[0], w, t0);
     } else {
-      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
+      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u, w.warp == 5 && turn >= p.quits_at ? 0u : p.polls);
       if (w.lane == 0) bulk_read_done<1>();   // the out buffer used two turns ago has been read
       __syncwarp();
       read_pairs<IO>(xv, s_dyn + slot * SLOT, w);
       read_pairs<IO>(gv, s_dyn + slot * SLOT + SLOT / 2, w);
-      if (!alive) gv[0] = nan2();
+      if (!alive) {   // what is kept has to show it too
+#pragma unroll
+        for (int k = 0; k < SCAN_K; ++k) xv[k] = gv[k] = nan2();
+      }
     }
     if constexpr (KEEP) {
       unsigned char* const codes = out + WARP_PIECE * sizeof(IO);
@@ -493,7 +500,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
   auto issue = [&](int turn, int slot) {
     unsigned char* const at = s_dyn + slot * slot_bytes;
     if constexpr (PATH == TILES) {
-      if (turn >= w.from) {
+      if (turn >= w.from && turn > p.loads_end) {
         mbar_arrive_expect_tx(&s_landed[slot], slot_bytes);
         tma_load_3d(at, &p.in[0], w.col0, w.b, turn, &s_landed[slot]);
         tma_load_3d(at + x_at, &p.in[1], w.col0, w.b, turn, &s_landed[slot]);
@@ -534,7 +541,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     next_start = load_start(turn - SNN_SCAN_CHUNK);
     unsigned char* const at = s_dyn + slot * slot_bytes;
     if (PATH == TILES) {
-      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u);
+      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u, w.warp == 5 && turn <= p.quits_at ? 0u : p.polls);
       if (w.lane == 0) bulk_read_done<1>();
       __syncwarp();
     }
@@ -610,6 +617,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     }
     __syncthreads();
     float2 h = s_h[w.warp][w.lane], e = s_e[w.warp][w.lane];
+    if (!alive) h = e = nan2();   // (a has a NaN at the first of the warp's steps, e goes through them from the last one)
     // u_k = dgate_k / D_k from the first step to the last, then D and the results from the last to the first.
     // DIRECT: u = h, dx = D; SIGMOID: u = i a (h - x), dx = D i
     auto outputs = [&](auto is_direct, auto is_full) {
@@ -807,6 +815,7 @@ ScanParams params_of(const snn_scan_args* a) {
   }
   p.lengths = a->lengths; p.state = a->state; p.dlast = a->dlast; p.last = a->last; p.states = a->states; p.dstate = a->dstate;
   p.x_codes = a->x_codes; p.x_scales = a->x_scales; p.gate_codes = a->gate_codes; p.gate_scales = a->gate_scales;
+  p.polls = MBAR_WAIT_LIMIT;
   return p;
 }
 // Segments of the time axis: as many as fill the device once (`resident` blocks fit an SM), each with two turns at least.
@@ -850,6 +859,18 @@ template <typename K> snn_status launch(K kernel, size_t smem, int64_t blocks, c
   return launched();
 }
 
+struct WaitTest {   // of snn_selftest_scan_wait
+  int step;
+  bool quits;
+  uint32_t polls;
+};
+void set_limits(ScanParams& p, const WaitTest* test, int never) {
+  p.loads_end = p.quits_at = never;
+  if (!test) return;
+  p.polls = test->polls;
+  (test->quits ? p.quits_at : p.loads_end) = test->step;
+}
+
 }  // namespace
 
 extern "C" snn_status snn_scan_workspace(const snn_scan_args* a, int32_t backward, size_t* bytes) {
@@ -865,7 +886,8 @@ extern "C" snn_status snn_scan_workspace(const snn_scan_args* a, int32_t backwar
   return SNN_OK;
 }
 
-extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
+namespace {
+snn_status forward(const snn_scan_args* a, const WaitTest* test, void* stream) {
   const snn_status st = check_common(a);
   if (st != SNN_OK) return st;
   const bool keep = a->states != nullptr && a->T > 0;
@@ -889,6 +911,7 @@ extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
       return launched();
     });
   }
+  set_limits(p, test, INT32_MAX);
   const snn_status cut = set_segments(p, a, false);
   if (cut != SNN_OK) return cut;
   const bool tiles = pairs && value_map(&p.in[0], p.x, a, p.xs, SNN_SCAN_CHUNK) && value_map(&p.in[1], p.gate, a, p.gs, SNN_SCAN_CHUNK) &&
@@ -911,7 +934,7 @@ extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) {
   });
 }
 
-extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
+snn_status backward(const snn_scan_args* a, const WaitTest* test, void* stream) {
   const snn_status st = check_common(a);
   if (st != SNN_OK) return st;
   if (a->B == 0 || a->N == 0) return SNN_OK;
@@ -926,6 +949,7 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
   const bool pairs = a->N % 2 == 0 && pairs_aligned(p.dh, size, p.dhs) && pairs_aligned(p.dx, size, p.dxs) && pairs_aligned(p.dgate, size, p.dgs) &&
                      (!raw_x || pairs_aligned(p.x, size, p.xs)) && (!raw_gate || pairs_aligned(p.gate, size, p.gs)) &&
                      (uintptr_t)p.x_codes % 2 == 0 && (uintptr_t)p.gate_codes % 2 == 0;
+  set_limits(p, test, -1);
   const snn_status cut = set_segments(p, a, true);
   if (cut != SNN_OK) return cut;
   const bool tiles = pairs && a->T > 0 && value_map(&p.in[0], p.dh, a, p.dhs, SNN_SCAN_CHUNK) &&
@@ -944,4 +968,15 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) {
     }
     return launch(scan_backward_kernel<IO, PATH>, ring + out, blocks * p.segments, p, (cudaStream_t)stream);
   });
+}
+}  // namespace
+
+extern "C" snn_status snn_scan_forward(const snn_scan_args* a, void* stream) { return forward(a, nullptr, stream); }
+extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) { return backward(a, nullptr, stream); }
+
+extern "C" snn_status snn_selftest_scan_wait(const snn_scan_args* a, int32_t is_backward, int32_t step, int32_t quits, uint32_t poll_limit,
+                                             void* stream) {
+  if (step < 0 || poll_limit == 0 || poll_limit > MBAR_WAIT_LIMIT) return SNN_ERR_INVALID_ARG;
+  const WaitTest test{step, quits != 0, poll_limit};
+  return is_backward ? backward(a, &test, stream) : forward(a, &test, stream);
 }

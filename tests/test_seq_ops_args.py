@@ -185,3 +185,9 @@ def test_scan_workspace_has_room_for_the_first_state(dtype):
         tiles = B * -(-N // 64)
         n = sb.snn_scan_workspace(_scan_args(T=T, B=B, N=N, dtype=dtype), False)
         assert n > 0 and n % (tiles * 32 * 16) == tiles * 32 * 8
+
+
+def test_scan_wait_selftest_refuses_invalid_arguments():
+    for v in ((0, -1, 0, 10), (1, -1, 0, 10), (0, 0, 0, 0), (1, 0, 0, 1 << 23)):
+        assert sb.lib.snn_selftest_scan_wait(C.byref(_scan_args()), *v, None) == sb.SNN_ERR_INVALID_ARG
+    assert sb.lib.snn_selftest_scan_wait(C.byref(_scan_args(N=-1)), 1, 0, 0, 10, None) == sb.SNN_ERR_INVALID_ARG

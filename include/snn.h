@@ -428,10 +428,12 @@ snn_status snn_selftest_scan_wait(const snn_scan_args* args, int32_t backward, i
  * A row with target = ignore_index does not count: its row_loss and lse are 0, its dx is 0, whatever x holds there.  Any
  * other target outside [0, classes) makes that row_loss and the loss NaN and counts like an ignored row in the gradients;
  * it is never used as an index.  If no row counts, loss and gradients are 0.
- * The products run on the tensor cores.  bf16 and fp16 operands are used as they are; fp32 ones are scaled by a power of
- * two and split into two fp16 parts: 22 bits of a value, down to 2^-40 of the largest magnitude in its tensor (rows that
- * do not count left out).  Sums are fp32.  In the backward pass the derivatives by the logits exist one piece of the
- * vocabulary at a time, rounded to the operands' type (fp32: to 22 bits), in the workspace.
+ * The products run on the tensor cores.  bf16 and fp16 operands are used as they are; fp32 ones are split into three bf16
+ * parts, 24 bits of a value of any magnitude above 2^-109, and six products of parts are summed: errors are those of fp32
+ * arithmetic.  Sums are fp32; those of 16-bit products stay in the tensor cores' accumulators, which cut what does not fit
+ * instead of rounding it (about 2^-24 of the sum per 16 terms).  In the backward pass the derivatives by the logits exist one
+ * piece of the vocabulary at a time in the workspace, rounded to the operands' type: 8 bits in bf16; 11 bits in fp16, where
+ * the derivative of a row's own loss is above 2^-28, and a step of 2^-38 below; all 24 in fp32.
  * W_out is stored by feature (SNN_W_BY_FEATURE: [dim][classes] as everywhere in this library) or by class
  * (SNN_W_BY_CLASS: [classes][dim], the transpose, as in an embedding table); w_stride is the distance of its rows. dw has
  * the same layout with its own stride. */

@@ -10,11 +10,10 @@
 //   DW      x^T dz, scaled and rounded
 // Work per pass: 2 rows dim classes for STATS, three times that for the backward pass (one of them the recomputation).
 //
-// fp32 operands are scaled by a power of two, so that the largest magnitude of a tensor lies in [2^14, 2^15), and split
-// into two fp16 parts: 22 bits of a value, down to 2^-40 of the largest one.  Three products of parts instead of one (the
-// product of the two small parts, below 2^-22 of the whole, is left out).  Three bf16 parts keep all 24 bits at any
-// magnitude, but need six products: twice the time for errors that the sums' own fp32 rounding hides (measured against
-// 64 bits at 500 x 1000 x 5003).
+// fp32 operands are split into three bf16 parts of 8 bits: all 24 bits of a value, whatever its magnitude beside the others'
+// (bf16 has the exponents of fp32).  Six products of parts instead of one: those left out are below 2^-24 of the whole.  Two
+// scaled fp16 parts need half of them, but what is 2^18 times smaller than the largest value of its tensor loses bits to the
+// common scale: with one feature of x 10^9 times the others the others' rows of dw were off by 2e-3 of their norm.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -36,7 +35,11 @@ constexpr int VL_RUN = 8;                                    // k-blocks per run
 constexpr int VL_SHORT = 16;                                 // k-blocks: eight warps below
 constexpr uint32_t VL_STORE_BYTES = UM_HALF * 128;           // one staged block of dz per half: 128 rows x 64 values
 constexpr size_t VL_SMEM = 1024 + (size_t)UM_STAGES * UM_STAGE_BYTES + 2 * VL_STORE_BYTES + 256;
-constexpr float FP16_DZ_SCALE = 16384.f;   // dz / (gradient of the row loss) lies in [-1, 1]; as fp16 it keeps small values better after this
+// dz / (gradient of the row loss) lies in [-1, 1].  As an operand of the next two products it has the operands' type: of fp32
+// three bf16 parts (nothing is lost), bf16 8 bits, fp16 11 bits down to 2^-28, after this scale, and steps of 2^-38 below.
+// (The rounding adds 6e-4 to the 1.7e-3 that rounding the gradients themselves to bf16 costs: 4096 x 1024 x 50257, norms;
+// two parts would double the time of two of the three products.)
+constexpr float FP16_DZ_SCALE = 16384.f;
 // The kernels of a call follow one another closely: each is launched while the one before still runs, sets itself up, and
 // waits here before it touches memory.  (Every kernel behind another one waits, so that their bodies never overlap.)
 __device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -53,7 +56,7 @@ struct ProductParams {
   CUtensorMap a, b, out;      // out: GRAD only
   int tiles_m, tiles_n;       // 256 x 256 tiles; m is the fastest in the order of work for STATS, GRAD and DX, n for DW
   int kblocks, splits;        // 64-deep blocks of the contraction; DX: parts of it
-  int n_pairs;                // products of operand planes: 1, or 3 for fp32 operands in two fp16 planes
+  int n_pairs;                // products of operand planes: 1, or 6 for fp32 operands in three bf16 planes
   uint32_t pair_a, pair_b;    // their planes, four bits each, the smallest products first
   int a0, b0, bk0;            // first row of A and of B, first k of B (A's k starts at 0)
   int m, n;                   // rows of A and of B that exist from there on
@@ -79,7 +82,6 @@ struct ProductParams {
   int dw_dtype;
   bool dw_vector;             // rows of dw are aligned to 16 bytes
   const float* alpha;         // DW: factor, from the device
-  const uint32_t* tops;       // fp32 operands: bit patterns of the largest magnitudes of x and w
   uint32_t* status;
   // limits of the waits; the self-test lets them run out: no loads from a unit of work on, or one warp of the epilogue that
   // does not wait for it
@@ -92,12 +94,6 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// The scale of an fp32 operand whose largest magnitude has the bit pattern `top`, and its inverse.
-__device__ __forceinline__ uint32_t operand_exponent(uint32_t top) {
-  return top == 0u || top >= 0x7f800000u ? 127u : min(268u - (top >> 23), 253u);
-}
-__device__ __forceinline__ float operand_scale(uint32_t top) { return __uint_as_float(operand_exponent(top) << 23); }
-__device__ __forceinline__ float operand_unscale(uint32_t top) { return __uint_as_float((254u - operand_exponent(top)) << 23); }
 // The target of a row, or -1 if it does not count, -2 if it is not a class.
 __device__ __forceinline__ int target_of(const void* targets, int bits, int64_t ignore, int classes, int row) {
   const int64_t t = bits == 64 ? reinterpret_cast<const int64_t*>(targets)[row] : (int64_t) reinterpret_cast<const int32_t*>(targets)[row];
@@ -259,8 +255,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
     int store_buf = half;
     const float nan = __uint_as_float(0x7fc00000u);
     // (a wait that ran out in a kernel before: dz is not what it should be)
-    const float alpha = EPI != DW ? 0.f : *p.status & VL_TIMEOUT ? nan : *p.alpha * (p.tops ? operand_unscale(p.tops[0]) : 1.f);
-    const float z_scale = p.tops ? p.z_scale * operand_unscale(p.tops[0]) * operand_unscale(p.tops[1]) : p.z_scale;
+    const float alpha = EPI != DW ? 0.f : *p.status & VL_TIMEOUT ? nan : *p.alpha;
     int run = 0;
     bool ok = true;
     float sums[RUNS ? WIDTH : 1];
@@ -334,7 +329,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
           float loaded[RUNS ? 1 : 32];
           if constexpr (!RUNS) tmem_load_32(acc + c, loaded);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) V(j) = V(j) * z_scale;
+          for (int j = 0; j < 32; ++j) V(j) = V(j) * p.z_scale;
           if (target >= c && target < c + 32) {
             float z = 0.f;
 #pragma unroll
@@ -373,7 +368,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
             tmem_load_32(acc + c + 32, *reinterpret_cast<float(*)[32]>(&loaded[32]));
           }
 #pragma unroll
-          for (int j = 0; j < 64; ++j) V(j) = counts ? exp2_fast(fmaf(V(j), z_scale, -lse2)) * rest : 0.f;
+          for (int j = 0; j < 64; ++j) V(j) = counts ? exp2_fast(fmaf(V(j), p.z_scale, -lse2)) * rest : 0.f;
           if (counts && target_col >= c && target_col < c + 64) {
 #pragma unroll
             for (int j = 0; j < 64; ++j) V(j) = c + j == target_col ? V(j) - 1.f : V(j);
@@ -396,14 +391,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
                 if (p.bf16) {
                   const __nv_bfloat162 r = __float22bfloat162_rn(make_float2(lo, hi));
                   q[h] = *reinterpret_cast<const uint32_t*>(&r);
-                } else {
-                  const __half2 r = __float22half2_rn(make_float2(lo, hi));
-                  q[h] = *reinterpret_cast<const uint32_t*>(&r);
                   if (p.planes > 1) {   // what is left for the next plane
-                    const float2 f = __half22float2(r);
+                    const float2 f = __bfloat1622float2(r);
                     lo -= f.x;
                     hi -= f.y;
                   }
+                } else {
+                  const __half2 r = __float22half2_rn(make_float2(lo, hi));
+                  q[h] = *reinterpret_cast<const uint32_t*>(&r);
                 }
               }
               *reinterpret_cast<uint4*>(out + ((g ^ (row_in_block & 7)) << 4)) = make_uint4(q[0], q[1], q[2], q[3]);
@@ -507,8 +502,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
 
 // ---- around the products ---------------------------------------------------------------------------------------
 
-// An operand on its way to 16-bit planes: a copy with an aligned pitch, or scaled fp32 values in two fp16 parts.  With
-// `mask`, rows that do not count become zeros (what they hold must not reach the sums over rows).
+// An operand on its way to 16-bit planes: a copy with an aligned pitch, or fp32 values in three bf16 parts.  With `mask`, rows
+// that do not count become zeros (what they hold must not reach the sums over rows).
 struct StageJob {
   const void* src;
   int64_t stride;
@@ -523,7 +518,6 @@ struct StageParams {
   int bits;
   int64_t ignore;
   int classes;
-  uint32_t* tops;       // fp32: bit patterns of the largest magnitudes
   // the backward pass has blocks with blockIdx.y = 2: the first counts the rows and writes the gradients' factor
   float* alpha;
   float factor;
@@ -533,29 +527,10 @@ struct StageParams {
 };
 constexpr int STAGE_COLS = 1024;   // columns of a row that a block takes at a time, four per thread
 
-// The largest magnitudes of fp32 operands.  (The maximum does not depend on the order of the atomics.)
-__global__ void __launch_bounds__(256) largest_kernel(const __grid_constant__ StageParams p) {
-  __shared__ uint32_t s_top;
-  let_next_kernel_start();
-  const StageJob& j = p.job[blockIdx.y];
-  const int parts = (j.cols + STAGE_COLS - 1) / STAGE_COLS;
-  if (threadIdx.x == 0) s_top = 0;
-  __syncthreads();
-  uint32_t m = 0;
-  for (int64_t i = blockIdx.x; i < (int64_t)j.rows * parts; i += gridDim.x) {
-    const int row = (int)(i / parts), c = (int)(i % parts) * STAGE_COLS + threadIdx.x;
-    if (j.mask && target_of(p.targets, p.bits, p.ignore, p.classes, row) < 0) continue;
-    const float* const src = (const float*)j.src + row * j.stride;
-    float v[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = src[min(c + 256 * q, j.cols - 1)];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) m = max(m, __float_as_uint(v[q]) & 0x7fffffffu);
-  }
-  m = __reduce_max_sync(0xffffffffu, m);
-  if ((threadIdx.x & 31) == 0 && m) atomicMax(&s_top, m);
-  __syncthreads();
-  if (threadIdx.x == 0 && s_top) atomicMax(p.tops + blockIdx.y, s_top);
+// To the nearest bf16 value; what is finite stays finite (fp32's largest values round to infinity).
+__device__ __forceinline__ __nv_bfloat16 to_bf16_finite(float f) {
+  const float top = largest_finite<__nv_bfloat16>();
+  return __float2bfloat16_rn(fabsf(f) > top && isfinite(f) ? copysignf(top, f) : f);
 }
 // Sums of a block's values, the same in every thread; `warp_sums` has 32 entries.
 __device__ __forceinline__ double block_sum(double v, double* warp_sums) {
@@ -570,7 +545,6 @@ __device__ __forceinline__ double block_sum(double v, double* warp_sums) {
 }
 template <typename IO> __global__ void __launch_bounds__(256) stage_kernel(const __grid_constant__ StageParams p) {
   let_next_kernel_start();
-  wait_for_kernel_before();
   if (blockIdx.y == 2) {
     __shared__ double warp_sums[32];
     if (blockIdx.x != 0) return;
@@ -586,7 +560,6 @@ template <typename IO> __global__ void __launch_bounds__(256) stage_kernel(const
   }
   const StageJob& j = p.job[blockIdx.y];
   const int parts = (int)((j.pitch + STAGE_COLS - 1) / STAGE_COLS);
-  const float scale = sizeof(IO) == 4 && j.rows ? operand_scale(p.tops[blockIdx.y]) : 1.f;
   for (int64_t i = blockIdx.x; i < (int64_t)j.rows * parts; i += gridDim.x) {
     const int row = (int)(i / parts), c0 = (int)(i % parts) * STAGE_COLS + 2 * threadIdx.x;
     const bool on = !j.mask || target_of(p.targets, p.bits, p.ignore, p.classes, row) >= 0;
@@ -600,11 +573,14 @@ template <typename IO> __global__ void __launch_bounds__(256) stage_kernel(const
       const int c = c0 + 512 * q;
       if (c >= j.pitch) continue;
       if constexpr (sizeof(IO) == 4) {
-        const float2 f = make_float2(on && c < j.cols ? v[q][0] * scale : 0.f, on && c + 1 < j.cols ? v[q][1] * scale : 0.f);
-        const __half2 hi = __float22half2_rn(f);
-        const float2 g = __half22float2(hi);
-        *reinterpret_cast<__half2*>(dst + c) = hi;
-        *reinterpret_cast<__half2*>(dst + j.plane + c) = __float22half2_rn(make_float2(f.x - g.x, f.y - g.y));
+        float2 f = make_float2(on && c < j.cols ? v[q][0] : 0.f, on && c + 1 < j.cols ? v[q][1] : 0.f);
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+          const __nv_bfloat162 r = __halves2bfloat162(to_bf16_finite(f.x), to_bf16_finite(f.y));
+          *reinterpret_cast<__nv_bfloat162*>(dst + part * j.plane + c) = r;
+          const float2 g = __bfloat1622float2(r);
+          f = make_float2(f.x - g.x, f.y - g.y);   // exact
+        }
       } else {
         const IO zero = from_f32<IO>(0.f);
         __half2 r;
@@ -688,9 +664,9 @@ __global__ void __launch_bounds__(1024) mean_kernel(const float* row_loss, int r
 template <typename IO>
 __global__ void __launch_bounds__(256) join_dx_kernel(const float* acc, int splits, int64_t split_stride, int pitch, int rows, int cols,
                                                       const float* alpha, const void* targets, int bits, int64_t ignore, int classes, IO* dx,
-                                                      int64_t stride, const uint32_t* status, const uint32_t* tops) {
+                                                      int64_t stride, const uint32_t* status) {
   wait_for_kernel_before();
-  const float a = (*status & VL_TIMEOUT) ? __uint_as_float(0x7fc00000u) : *alpha * (tops ? operand_unscale(tops[1]) : 1.f);
+  const float a = (*status & VL_TIMEOUT) ? __uint_as_float(0x7fc00000u) : *alpha;
   for (int64_t row = blockIdx.y; row < rows; row += gridDim.y) {
     const bool on = target_of(targets, bits, ignore, classes, (int)row) >= 0;
     for (int c = (int)(blockIdx.x * blockDim.x + threadIdx.x) * 4; c < cols; c += (int)(gridDim.x * blockDim.x) * 4) {
@@ -975,7 +951,7 @@ Layout layout_of(const snn_vocab_loss_args* a, bool backward, int pairs) {
   Layout l{};
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes); return o; };
-  const int planes = a->dtype == SNN_DTYPE_FP32 ? 2 : 1;
+  const int planes = a->dtype == SNN_DTYPE_FP32 ? 3 : 1;
   auto operand = [&](const void* p, int64_t stride, int rows, int cols, bool always) {
     Operand o{};
     o.planes = planes;
@@ -1026,7 +1002,7 @@ snn_status check(const snn_vocab_loss_args* a) {
   if (!a->w || (a->rows > 0 && (!a->x || !a->targets))) return SNN_ERR_INVALID_ARG;
   return SNN_OK;
 }
-bool is_bf16(int dtype) { return dtype == SNN_DTYPE_BF16; }   // (fp32: fp16 planes)
+bool is_bf16(int dtype) { return dtype != SNN_DTYPE_FP16; }   // (fp32: bf16 planes)
 
 // Launches a kernel; `behind` another one of the same call.
 template <typename... P, typename... A>
@@ -1050,9 +1026,9 @@ template <int EPI, bool A_MN, bool B_MN, int WARPS, bool RUNS> snn_status launch
   if (units > INT32_MAX / 2) return SNN_ERR_UNSUPPORTED;
   return launch(kernel, dim3(2 * (unsigned)std::min<int64_t>(units, pairs)), 32 * (2 + WARPS), VL_SMEM, stream, p.behind, p);
 }
-bool eight_warps(const ProductParams& p) { return p.planes == 2 || p.kblocks < VL_SHORT; }
+bool eight_warps(const ProductParams& p) { return p.planes > 1 || p.kblocks < VL_SHORT; }
 template <int EPI, bool A_MN, bool B_MN> snn_status launch_product(const ProductParams& p, int pairs, cudaStream_t stream) {
-  if (p.planes == 2) return launch_one<EPI, A_MN, B_MN, 8, true>(p, pairs, stream);
+  if (p.planes > 1) return launch_one<EPI, A_MN, B_MN, 8, true>(p, pairs, stream);
   if constexpr (EPI == STATS || EPI == GRAD)
     if (eight_warps(p)) return launch_one<EPI, A_MN, B_MN, 8, false>(p, pairs, stream);
   return launch_one<EPI, A_MN, B_MN, 4, false>(p, pairs, stream);
@@ -1076,7 +1052,6 @@ struct Call {
   int pairs;
   uint32_t* status() const { return (uint32_t*)(ws + l.status); }
   float* alpha() const { return (float*)(ws + l.alpha); }
-  uint32_t* tops() const { return a->dtype == SNN_DTYPE_FP32 ? (uint32_t*)(ws + l.status + 64) : nullptr; }
 
   snn_status begin(bool backward, void* s) {
     stream = (cudaStream_t)s;
@@ -1086,15 +1061,13 @@ struct Call {
     if (!a->workspace || (uintptr_t)a->workspace % 256 != 0) return SNN_ERR_INVALID_ARG;
     if (a->workspace_bytes < l.total) return SNN_ERR_WORKSPACE_TOO_SMALL;
     ws = (char*)a->workspace;
-    if (a->dtype != SNN_DTYPE_FP32) return SNN_OK;   // (the status is cleared by the staging kernel)
-    return cudaMemsetAsync(tops(), 0, 2 * sizeof(uint32_t), stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+    return SNN_OK;   // (the status is cleared by the staging kernel)
   }
   // with `factor`, for the backward pass: alpha and the status as well
   snn_status stage_operands(const float* factor) const {
     const bool by_class = a->w_layout == SNN_W_BY_CLASS;
     StageParams p{};
     p.targets = a->targets; p.bits = a->target_bits; p.ignore = a->ignore_index; p.classes = a->classes;
-    p.tops = tops();
     if (l.x.staged) p.job[0] = {a->x, a->x_stride, a->rows, a->dim, (uint16_t*)(ws + l.x.offset), l.x.pitch, l.x.plane, true};
     if (l.w.staged)
       p.job[1] = {a->w, a->w_stride, by_class ? a->classes : a->dim, by_class ? a->dim : a->classes, (uint16_t*)(ws + l.w.offset), l.w.pitch, l.w.plane, false};
@@ -1106,10 +1079,7 @@ struct Call {
     }
     if (work == 0) return SNN_OK;
     const dim3 grid((unsigned)std::min<int64_t>(work, 148 * 8), factor ? 3 : 2);
-    if (p.tops) {
-      const snn_status st = launch(largest_kernel, dim3(grid.x, 2), 256, 0, stream, false, p);   // (behind a memset)
-      return st != SNN_OK ? st : launch(stage_kernel<float>, grid, 256, 0, stream, true, p);
-    }
+    if (a->dtype == SNN_DTYPE_FP32) return launch(stage_kernel<float>, grid, 256, 0, stream, false, p);
     return launch(stage_kernel<__half>, grid, 256, 0, stream, false, p);   // 16 bits are copied, whatever they mean
   }
   const void* data(const Operand& o, const void* direct) const { return o.staged ? ws + o.offset : direct; }
@@ -1130,11 +1100,10 @@ struct Call {
     p.bf16 = is_bf16(a->dtype);
     p.splits = 1;
     p.planes = l.x.planes;
-    // fp32: (plane of a, plane of b) = (1, 0), (0, 1), (0, 0), plane 0 the leading part: the small products first
-    p.n_pairs = p.planes == 2 ? 3 : 1;
-    p.pair_a = p.planes == 2 ? 0x001u : 0u;
-    p.pair_b = p.planes == 2 ? 0x010u : 0u;
-    p.tops = tops();
+    // fp32: (plane of a, plane of b) = (2, 0), (0, 2), (1, 1), (1, 0), (0, 1), (0, 0), plane 0 the leading part: the small products first
+    p.n_pairs = p.planes == 3 ? 6 : 1;
+    p.pair_a = p.planes == 3 ? 0x001102u : 0u;
+    p.pair_b = p.planes == 3 ? 0x010120u : 0u;
     p.targets = a->targets; p.target_bits = a->target_bits; p.ignore_index = a->ignore_index; p.classes = a->classes;
     p.z_scale = a->scale * LOG2E;
     p.status = status();
@@ -1282,7 +1251,7 @@ snn_status backward(const snn_vocab_loss_args* a, const WaitTest* test, void* st
   auto join = [&](auto io) {
     using IO = decltype(io);
     return launch(join_dx_kernel<IO>, grid, 256, 0, c.stream, true, (const float*)(c.ws + l.acc), splits, l.acc_split, l.acc_pitch, a->rows, a->dim,
-                  c.alpha(), a->targets, a->target_bits, a->ignore_index, a->classes, (IO*)a->dx, a->dx_stride, c.status(), c.tops());
+                  c.alpha(), a->targets, a->target_bits, a->ignore_index, a->classes, (IO*)a->dx, a->dx_stride, c.status());
   };
   return a->dtype == SNN_DTYPE_FP32 ? join(float()) : a->dtype == SNN_DTYPE_BF16 ? join(__nv_bfloat16()) : join(__half());
 }

@@ -40,6 +40,14 @@ constexpr size_t VL_SMEM = 1024 + (size_t)UM_STAGES * UM_STAGE_BYTES + 2 * VL_ST
 // (The rounding adds 6e-4 to the 1.7e-3 that rounding the gradients themselves to bf16 costs: 4096 x 1024 x 50257, norms;
 // two parts would double the time of two of the three products.)
 constexpr float FP16_DZ_SCALE = 16384.f;
+// The others have the range for the mean's factor, as a power of two, before the products, so that sums over the rows stay
+// within fp32 wherever their mean does.
+float dz_unit_of(int dtype, int rows) {
+  float unit = 1.f;
+  if (dtype == SNN_DTYPE_FP16) return FP16_DZ_SCALE;
+  for (int64_t n = 1; n < rows; n *= 2) unit *= 0.5f;
+  return unit;
+}
 // The kernels of a call follow one another closely: each is launched while the one before still runs, sets itself up, and
 // waits here before it touches memory.  (Every kernel behind another one waits, so that their bodies never overlap.)
 __device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
@@ -71,6 +79,7 @@ struct ProductParams {
   float2* partial;            // [tile_n][halves][rows]
   float* target_z;            // [rows], in units of log 2
   const float* lse;
+  float dz_unit;              // GRAD: what stands for a derivative of one, a power of two
   int planes;
   // DX and DW
   float* acc;                 // DX: [splits][m][n_pitch]
@@ -358,7 +367,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
         const int target_col = target - (p.b0 + col0);
         // lse log2 e in two parts: the second, what rounding the first leaves, as a factor
         const double lse2_exact = counts ? (double)p.lse[row] * 1.4426950408889634074 : 0.;
-        const float lse2 = (float)lse2_exact, rest = 1.f - (float)(lse2_exact - (double)lse2) * LN2;
+        const float lse2 = (float)lse2_exact, rest = p.dz_unit * (1.f - (float)(lse2_exact - (double)lse2) * LN2);
 #pragma unroll(RUNS ? WIDTH / 64 : 1)
         for (int c = 0; c < WIDTH; c += 64) {
           if (c >= cols) continue;
@@ -371,11 +380,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
           for (int j = 0; j < 64; ++j) V(j) = counts ? exp2_fast(fmaf(V(j), p.z_scale, -lse2)) * rest : 0.f;
           if (counts && target_col >= c && target_col < c + 64) {
 #pragma unroll
-            for (int j = 0; j < 64; ++j) V(j) = c + j == target_col ? V(j) - 1.f : V(j);
-          }
-          if (!p.bf16) {
-#pragma unroll
-            for (int j = 0; j < 64; ++j) V(j) *= FP16_DZ_SCALE;
+            for (int j = 0; j < 64; ++j) V(j) = c + j == target_col ? V(j) - p.dz_unit : V(j);
           }
           for (int plane = 0; plane < p.planes; ++plane) {
             // the buffer's previous store has to have read it (there are two buffers: one per half, or both for all)
@@ -1201,7 +1206,7 @@ snn_status backward(const snn_vocab_loss_args* a, const WaitTest* test, void* st
                                                                                                          : (cudaGetLastError(), SNN_ERR_CUDA);
   const Layout& l = c.l;
   const ProductParams base = c.base();
-  const float factor = a->dloss * a->scale / (base.bf16 ? 1.f : FP16_DZ_SCALE);
+  const float dz_unit = dz_unit_of(a->dtype, a->rows), factor = a->dloss * a->scale / dz_unit;
   VL_TRY(c.stage_operands(&factor));
   CUtensorMap x_k, x_mn, w_z, w_dx, dz_k, dz_mn;   // as operands that are contiguous along the contraction, and across it
   bool ok = c.map(&x_k, l.x, a->x, a->rows, a->dim, false) && c.map(&x_mn, l.x, a->x, a->rows, a->dim, true);
@@ -1217,6 +1222,7 @@ snn_status backward(const snn_vocab_loss_args* a, const WaitTest* test, void* st
     p.tiles_m = ceil_div(a->rows, UM_TILE); p.tiles_n = ceil_div(width, UM_TILE); p.kblocks = ceil_div(a->dim, UM_KB);
     p.m = a->rows; p.n = width; p.b0 = v0;
     p.lse = a->lse;
+    p.dz_unit = dz_unit;
     c.limit(p, 0);
     VL_TRY(launch_z<GRAD>(p, by_class, c.pairs, c.stream));
     p = base;                 // dx += dz w^T

@@ -135,6 +135,15 @@ def test_operands_near_the_ends_of_the_range(n, D, V, layout, size):
     check(x * size, w / size, t)
 
 
+def test_the_largest_values_of_the_type():
+    """Those that round to infinity in 8 bits."""
+    x, w, t = inputs(70, 40, 300, "feature", 6)
+    top = torch.finfo(torch.float32).max
+    x[:, 2], w[2] = top, w[2] / top
+    x[5:20, 2] *= -1
+    check(x, w, t)
+
+
 @LAYOUT
 def test_classes_of_small_probability(layout):
     """Logits from 0 down to -60: the gradients of rare classes keep their bits too."""
@@ -143,3 +152,17 @@ def test_classes_of_small_probability(layout):
     w[1:] *= 0.1
     t = torch.where(t >= 0, t % 20, t)
     check(x, w, t)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sums_over_many_rows_stay_within_the_range_of_their_mean(dtype):
+    """The gradient by w is a mean over the rows: finite for values whose sum over the rows is not."""
+    n, D, V = 3000, 8, 4
+    x = torch.full((n, D), 2.0 ** 127, dtype=dtype, device="cuda")
+    w = torch.zeros(D, V, dtype=dtype, device="cuda")
+    t = torch.zeros(n, dtype=torch.int64, device="cuda")
+    _, _, lse = ops().vocab_loss(x, w, t)
+    dx, dw = ops().vocab_loss_backward(x, w, t, lse)
+    # four classes of the same logit: the derivatives are -3/4 and 1/4, exact but for the roundings of lse and exp2 (below 2^-20)
+    want = torch.tensor([-0.75, 0.25, 0.25, 0.25], dtype=torch.float64, device="cuda").expand(D, V) * 2.0 ** 127
+    assert ((dw.double() - want).abs() <= want.abs() * (2.0 ** -20 + torch.finfo(dtype).eps / 2)).all() and (dx == 0).all()

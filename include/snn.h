@@ -363,7 +363,7 @@ typedef enum { SNN_KEEP_RAW = 0, SNN_KEEP_INT8 = 1, SNN_KEEP_E4M3 = 2 } snn_keep
 #define SNN_KEEP_GROUP 64
 
 /* Encodes n_rows rows of n_cols values (device; rows `row_stride` elements apart) to codes [n_rows][n_cols] and scales
- * [n_rows][ceil(n_cols / 64)] (device). */
+ * [n_rows][ceil(n_cols / 64)] (device).  SNN_ERR_UNSUPPORTED: n_cols above 2^31 - 64. */
 snn_status snn_activation_pack(const void* values, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t row_stride,
                                int32_t format, uint8_t* codes, uint8_t* scales, void* stream);
 /* Decodes them to n_rows rows of n_cols values of the given type. */
@@ -388,7 +388,7 @@ snn_status snn_activation_unpack(const uint8_t* codes, const uint8_t* scales, in
 typedef enum { SNN_SCAN_SIGMOID = 0, SNN_SCAN_DIRECT = 1 } snn_scan_mode;
 #define SNN_SCAN_CHUNK 64
 typedef struct {
-  int32_t T, B, N;               /* steps, samples, channels: each >= 0; T < 2^30                               */
+  int32_t T, B, N;               /* steps, samples, channels: each >= 0; T < 2^30, N <= 2^31 - 64 (SNN_ERR_UNSUPPORTED) */
   int32_t dtype, mode;           /* snn_dtype of x, gate, h, dh, dx, dgate; snn_scan_mode                       */
   const void *x, *gate;          /* [T][B][N]; the backward pass reads them only where the format is RAW        */
   int64_t x_stride[2], gate_stride[2];   /* of T and of B                                                       */

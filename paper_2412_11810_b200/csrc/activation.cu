@@ -160,6 +160,7 @@ template <typename F> snn_status by_dtype(int dtype, bool pairs, F&& f) {
   return pairs ? f(__half(), std::true_type()) : f(__half(), std::false_type());
 }
 
+constexpr int32_t WIDEST = INT32_MAX - (KEEP_GROUP - 1);   // a row's last group ends within 32 bits
 // whether rows can be accessed 16 bytes of values, or eight codes, at a time
 bool rows_of_sixteen(const void* values, int n_cols, int64_t row_stride, const uint8_t* codes) {
   return n_cols % 8 == 0 && row_stride % 8 == 0 && (uintptr_t)values % 16 == 0 && (uintptr_t)codes % 8 == 0;
@@ -178,6 +179,7 @@ unsigned pack_blocks(int64_t n_rows, int n_cols) {
 extern "C" snn_status snn_activation_pack(const void* values, int32_t dtype, int64_t n_rows, int32_t n_cols, int64_t row_stride,
                                           int32_t format, uint8_t* codes, uint8_t* scales, void* stream) {
   if (n_rows < 0 || n_cols < 0 || !dtype_known(dtype) || (format != SNN_KEEP_INT8 && format != SNN_KEEP_E4M3)) return SNN_ERR_INVALID_ARG;
+  if (n_cols > WIDEST) return SNN_ERR_UNSUPPORTED;
   if (n_rows == 0 || n_cols == 0) return SNN_OK;
   if (!values || !codes || !scales) return SNN_ERR_INVALID_ARG;
   return by_dtype(dtype, rows_of_sixteen(values, n_cols, row_stride, codes), [&](auto io, auto is_fast) {
@@ -192,6 +194,7 @@ extern "C" snn_status snn_activation_pack(const void* values, int32_t dtype, int
 extern "C" snn_status snn_activation_unpack(const uint8_t* codes, const uint8_t* scales, int32_t format, int64_t n_rows, int32_t n_cols,
                                             void* values, int32_t dtype, int64_t row_stride, void* stream) {
   if (n_rows < 0 || n_cols < 0 || !dtype_known(dtype) || (format != SNN_KEEP_INT8 && format != SNN_KEEP_E4M3)) return SNN_ERR_INVALID_ARG;
+  if (n_cols > WIDEST) return SNN_ERR_UNSUPPORTED;
   if (n_rows == 0 || n_cols == 0) return SNN_OK;
   if (!values || !codes || !scales) return SNN_ERR_INVALID_ARG;
   return by_dtype(dtype, rows_of_sixteen(values, n_cols, row_stride, codes), [&](auto io, auto is_fast) {

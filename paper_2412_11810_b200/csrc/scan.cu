@@ -801,6 +801,7 @@ snn_status check_common(const snn_scan_args* a) {
   for (int f : {a->x_format, a->gate_format})
     if (f < SNN_KEEP_RAW || f > SNN_KEEP_E4M3) return SNN_ERR_INVALID_ARG;
   if (a->mode == SNN_SCAN_DIRECT && a->gate_format != SNN_KEEP_RAW) return SNN_ERR_UNSUPPORTED;
+  if (a->N > INT32_MAX - (SCAN_COLS - 1)) return SNN_ERR_UNSUPPORTED;   // (the last tile of channels ends within 32 bits)
   return SNN_OK;
 }
 ScanParams params_of(const snn_scan_args* a) {

@@ -28,6 +28,7 @@ _MODES = {"sigmoid": sb.SNN_SCAN_SIGMOID, "direct": sb.SNN_SCAN_DIRECT}
 _FORMATS = {"int8": sb.SNN_KEEP_INT8, "e4m3": sb.SNN_KEEP_E4M3}
 _KEEPS = {"raw": sb.SNN_KEEP_RAW, **_FORMATS}
 _INT32_MAX = 2 ** 31 - 1
+_WIDEST = 2 ** 31 - 64           # channels: the last group of 64 ends within 32 bits
 
 
 # The checks below run before every launch, and small calls take microseconds: conditions are tested in place, and messages
@@ -108,8 +109,8 @@ def pack_activation(x: torch.Tensor, format: str = "int8") -> PackedActivation:
         raise ValueError("x: a CUDA tensor is required")
     if x.dtype not in _DTYPES:
         raise ValueError(f"x: dtype {x.dtype} is not fp32, bf16 or fp16")
-    if x.dim() < 1 or x.shape[-1] > _INT32_MAX:
-        raise ValueError("x: at least one dimension is required, the last one below 2^31")
+    if x.dim() < 1 or x.shape[-1] > _WIDEST:
+        raise ValueError("x: at least one dimension is required, the last one at most 2^31 - 64")
     _choice(format, "format", _FORMATS)
     n, count = x.shape[-1], x.numel()
     stride = n
@@ -138,6 +139,8 @@ def unpack_activation(packed: PackedActivation, dtype: Optional[torch.dtype] = N
     codes = packed.codes
     if not (isinstance(codes, torch.Tensor) and codes.is_cuda):
         raise ValueError("codes: a CUDA tensor is required")
+    if codes.dim() < 1 or codes.shape[-1] > _WIDEST:
+        raise ValueError("codes: at least one dimension is required, the last one at most 2^31 - 64")
     n, count = codes.shape[-1], codes.numel()
     _like(codes, "codes", codes, codes.shape, torch.uint8)
     _like(packed.scales, "scales", codes, (*codes.shape[:-1], -(-n // KEEP_GROUP)), torch.uint8)
@@ -193,7 +196,7 @@ def gated_scan(x: torch.Tensor, gate: torch.Tensor, state: Optional[torch.Tensor
     _like(gate, "gate", x, shape, dtype, dense=False)
     _choice(mode, "mode", _MODES)
     T, B, N = shape
-    if T >= 2 ** 30 or B > _INT32_MAX or N > _INT32_MAX:
+    if T >= 2 ** 30 or B > _INT32_MAX or N > _WIDEST:
         raise ValueError("x: too large")
     if keep is None:
         if keep_gate is not None:
@@ -247,7 +250,7 @@ def gated_scan_step(x: torch.Tensor, gate: torch.Tensor, state: Optional[torch.T
     elif inplace:
         raise ValueError("inplace: needs a state")
     B, N = shape
-    if B > _INT32_MAX or N > _INT32_MAX:
+    if B > _INT32_MAX or N > _WIDEST:
         raise ValueError("x: too large")
     with _on(x):
         h = _dense(x)

@@ -191,3 +191,16 @@ def test_scan_wait_selftest_refuses_invalid_arguments():
     for v in ((0, -1, 0, 10), (1, -1, 0, 10), (0, 0, 0, 0), (1, 0, 0, 1 << 23)):
         assert sb.lib.snn_selftest_scan_wait(C.byref(_scan_args()), *v, None) == sb.SNN_ERR_INVALID_ARG
     assert sb.lib.snn_selftest_scan_wait(C.byref(_scan_args(N=-1)), 1, 0, 0, 10, None) == sb.SNN_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("width", [2 ** 31 - 1, 2 ** 31 - 63])
+def test_widths_whose_last_group_passes_32_bits_are_refused(width):
+    p = 1 << 20   # never read
+    assert sb.lib.snn_activation_pack(p, 0, 1, width, width, 1, p, p, None) == sb.SNN_ERR_UNSUPPORTED
+    assert sb.lib.snn_activation_unpack(p, p, 1, 1, width, p, 0, width, None) == sb.SNN_ERR_UNSUPPORTED
+    for T in (1, 100):
+        a = _scan_args(T=T, B=1, N=width)
+        assert sb.lib.snn_scan_forward(C.byref(a), None) == sb.SNN_ERR_UNSUPPORTED
+        assert sb.lib.snn_scan_backward(C.byref(a), None) == sb.SNN_ERR_UNSUPPORTED
+        n = C.c_size_t()
+        assert sb.lib.snn_scan_workspace(C.byref(a), 0, C.byref(n)) == sb.SNN_ERR_UNSUPPORTED

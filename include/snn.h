@@ -447,7 +447,7 @@ typedef struct {
   int32_t target_bits;         /* 32 or 64: targets are int32 or int64                                  */
   const void* targets;         /* [rows], device                                                        */
   int64_t ignore_index;
-  float scale;
+  float scale;                 /* finite, also times log2 e: below 2.35e38 in magnitude                 */
   float* row_loss;             /* [rows], forward; may be NULL                                          */
   float* lse;                  /* [rows]; written by the forward pass, read by the backward pass        */
   float* loss;                 /* one value, forward                                                    */

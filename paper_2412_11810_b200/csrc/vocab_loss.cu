@@ -1001,7 +1001,7 @@ snn_status check(const snn_vocab_loss_args* a) {
   if (a->dtype < SNN_DTYPE_FP32 || a->dtype > SNN_DTYPE_FP16) return SNN_ERR_INVALID_ARG;
   if (a->w_layout != SNN_W_BY_FEATURE && a->w_layout != SNN_W_BY_CLASS) return SNN_ERR_INVALID_ARG;
   if (a->target_bits != 32 && a->target_bits != 64) return SNN_ERR_INVALID_ARG;
-  if (!(std::fabs(a->scale) < INFINITY)) return SNN_ERR_INVALID_ARG;
+  if (!(std::fabs(a->scale * LOG2E) < INFINITY)) return SNN_ERR_INVALID_ARG;   // (as it multiplies the logits)
   const int64_t w_cols = a->w_layout == SNN_W_BY_CLASS ? a->dim : a->classes, w_rows = a->w_layout == SNN_W_BY_CLASS ? a->classes : a->dim;
   if ((a->rows > 1 && a->x_stride < a->dim) || (w_rows > 1 && a->w_stride < w_cols)) return SNN_ERR_INVALID_ARG;
   if (!a->w || (a->rows > 0 && (!a->x || !a->targets))) return SNN_ERR_INVALID_ARG;

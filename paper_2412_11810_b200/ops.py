@@ -319,8 +319,8 @@ def _vocab_args(x, w_out, targets, scale: float, ignore_index: int):
     _like(targets, "targets", x, (rows,), targets.dtype)
     if not -2 ** 63 <= ignore_index < 2 ** 63:
         raise ValueError("ignore_index: does not fit 64 bits")
-    if not abs(scale) <= 3.4e38:
-        raise ValueError("scale: has to be finite")
+    if not abs(scale) <= 2.35e38:
+        raise ValueError("scale: has to be at most 2.35e38 in magnitude")
     return sb.snn_vocab_loss_args(rows, dim, classes, _DTYPES[x.dtype], x.data_ptr(), x.stride(0), w_out.data_ptr(), s0 if by_feature else s1,
                                   sb.SNN_W_BY_FEATURE if by_feature else sb.SNN_W_BY_CLASS, targets.element_size() * 8, targets.data_ptr(),
                                   ignore_index, scale)

@@ -204,3 +204,11 @@ def test_widths_whose_last_group_passes_32_bits_are_refused(width):
         assert sb.lib.snn_scan_backward(C.byref(a), None) == sb.SNN_ERR_UNSUPPORTED
         n = C.c_size_t()
         assert sb.lib.snn_scan_workspace(C.byref(a), 0, C.byref(n)) == sb.SNN_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("scale", [2.4e38, -3.4e38])
+def test_loss_refuses_a_scale_that_leaves_fp32_times_log2_e(scale):
+    n = C.c_size_t()
+    for call in (lambda a: sb.lib.snn_vocab_loss_forward(C.byref(a), None), lambda a: sb.lib.snn_vocab_loss_backward(C.byref(a), None),
+                 lambda a: sb.lib.snn_vocab_loss_workspace(C.byref(a), 0, C.byref(n))):
+        assert call(_loss_args(scale=scale)) == sb.SNN_ERR_INVALID_ARG

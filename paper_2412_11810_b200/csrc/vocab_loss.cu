@@ -1201,9 +1201,10 @@ snn_status backward(const snn_vocab_loss_args* a, const WaitTest* test, void* st
   Call c{a, test};
   VL_TRY(c.begin(true, stream));
   const size_t size = a->dtype == SNN_DTYPE_FP32 ? 4 : 2;
-  if (a->rows == 0)
-    return cudaMemset2DAsync(a->dw, a->dw_stride * size, 0, w_cols * size, w_rows, c.stream) == cudaSuccess ? SNN_OK
-                                                                                                         : (cudaGetLastError(), SNN_ERR_CUDA);
+  if (a->rows == 0) {   // (the stride of a single row means nothing)
+    const size_t width = w_cols * size, pitch = w_rows > 1 ? a->dw_stride * size : width;
+    return cudaMemset2DAsync(a->dw, pitch, 0, width, w_rows, c.stream) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+  }
   const Layout& l = c.l;
   const ProductParams base = c.base();
   const float dz_unit = dz_unit_of(a->dtype, a->rows), factor = a->dloss * a->scale / dz_unit;

@@ -418,7 +418,8 @@ snn_status snn_scan_backward(const snn_scan_args* args, void* stream);
 /* A self-test of the bounded waits: the same pass, in which the waits for tiles from step `step` on (in the order in which
  * the pass goes through them) run out after poll_limit polls, since nothing is loaded (quits = 0) or one warp does not wait
  * (quits = 1).  The call ends all the same; what rests on those steps is NaN.  It applies to data that TMA can describe
- * (rows of multiples of 16 bytes), more than 16 steps or with states kept. */
+ * (rows of multiples of 16 bytes), more than 16 steps or with states kept.  In the bounds-checked build only
+ * (SNN_ERR_UNSUPPORTED). */
 snn_status snn_selftest_scan_wait(const snn_scan_args* args, int32_t backward, int32_t step, int32_t quits, uint32_t poll_limit, void* stream);
 
 /* Soft-max cross entropy over a large vocabulary, with the readout product inside (the readout and loss of snn_train_step
@@ -465,7 +466,8 @@ snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* args, void* stream
 /* A self-test of the bounded waits: the same pass, in which waits of one of its product kernels run out (kernel 0 of the
  * forward pass: the logits' sums; 0, 1, 2 of the backward pass: the derivatives by the logits, dx, dw) after poll_limit polls,
  * since from the unit-th tile of work on nothing is loaded (quits = 0) or one warp does not wait (quits = 1).  The call ends
- * all the same and the results that need those tiles are NaN.  It does not apply to forward passes of four rows or fewer. */
+ * all the same and the results that need those tiles are NaN.  It does not apply to forward passes of four rows or fewer.
+ * In the bounds-checked build only (SNN_ERR_UNSUPPORTED). */
 snn_status snn_selftest_vocab_loss_wait(const snn_vocab_loss_args* args, int32_t backward, int32_t kernel, int32_t unit, int32_t quits,
                                         uint32_t poll_limit, void* stream);
 

@@ -54,8 +54,8 @@ struct ScanParams {
   const float *state, *dlast;
   float *last, *states, *dstate;
   uint8_t *x_codes, *x_scales, *gate_codes, *gate_scales;
-  // TILES: limits of the waits.  The self-test lets them run out: no loads of the turns from this step on (in the order in
-  // which the pass goes), or a warp that does not wait for them
+  // TILES, WAIT_TESTS: limits of the waits.  The self-test lets them run out: no loads of the turns from this step on (in the
+  // order in which the pass goes), or a warp that does not wait for them
   uint32_t polls;
   int loads_end, quits_at;
 };
@@ -273,6 +273,13 @@ __device__ __forceinline__ void keep_steps(int format, const float2 (&v)[SCAN_K]
   if (format == SNN_KEEP_INT8) keep_steps<SNN_KEEP_INT8, PATH>(v, p, w, t0, codes, scales, s_codes);
   if (format == SNN_KEEP_E4M3) keep_steps<SNN_KEEP_E4M3, PATH>(v, p, w, t0, codes, scales, s_codes);
 }
+// The warp's steps kept as no numbers (by the lanes that wrote the scales).
+__device__ __forceinline__ void void_kept(const ScanParams& p, const Place& w, int t0) {
+  if (w.lane >= SCAN_K || t0 + w.lane >= w.len) return;
+  const int64_t at = ((int64_t)(t0 + w.lane) * p.B + w.b) * p.n_tiles + w.col0 / KEEP_GROUP;
+  if (p.x_format != SNN_KEEP_RAW) p.x_scales[at] = 255;
+  if (p.gate_format != SNN_KEEP_RAW) p.gate_scales[at] = 255;
+}
 // The kept values of this thread's steps; the scales' bytes lie in lanes from, from + 1, ...
 template <int FORMAT, typename IO>
 __device__ __forceinline__ void decode_steps(float2 (&v)[SCAN_K], const void* tile, const Place& w, uint32_t bytes, int from) {
@@ -324,6 +331,9 @@ __device__ __forceinline__ void barriers_init(uint64_t* landed) {
   }
   __syncthreads();
 }
+__device__ __forceinline__ uint32_t polls_of(const ScanParams& p, const Place& w, bool quits) {
+  return !WAIT_TESTS ? MBAR_WAIT_LIMIT : quits && w.warp == 5 ? 0u : p.polls;
+}
 __device__ __forceinline__ float2 nan2() { return both(__uint_as_float(0x7fc00000u)); }
 
 // ---- forward -----------------------------------------------------------------------------------------------
@@ -344,7 +354,7 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
   auto issue = [&](int turn, int slot) {   // by one thread
     unsigned char* const at = s_dyn + slot * SLOT;
     if constexpr (PATH == TILES) {
-      if (turn < w.end && turn < p.loads_end) {
+      if (turn < w.end && !(WAIT_TESTS && turn >= p.loads_end)) {
         mbar_arrive_expect_tx(&s_landed[slot], SLOT);
         tma_load_3d(at, &p.in[0], w.col0, w.b, turn, &s_landed[slot]);
         tma_load_3d(at + SLOT / 2, &p.in[1], w.col0, w.b, turn, &s_landed[slot]);
@@ -368,20 +378,18 @@ __global__ void __launch_bounds__(32 * WARPS, KEEP || sizeof(IO) == 4 ? 3 : 4) s
       load_values<PATH == PAIRS>(xv, x, p.xs[0], w, t0);
       load_values<PATH == PAIRS>(gv, gate, p.gs[0], w, t0);
     } else {
-      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u, w.warp == 5 && turn >= p.quits_at ? 0u : p.polls);
+      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u, polls_of(p, w, turn >= p.quits_at));
       if (w.lane == 0) bulk_read_done<1>();   // the out buffer used two turns ago has been read
       __syncwarp();
       read_pairs<IO>(xv, s_dyn + slot * SLOT, w);
       read_pairs<IO>(gv, s_dyn + slot * SLOT + SLOT / 2, w);
-      if (!alive) {   // what is kept has to show it too
-#pragma unroll
-        for (int k = 0; k < SCAN_K; ++k) xv[k] = gv[k] = nan2();
-      }
+      if (!alive) gv[0] = nan2();
     }
     if constexpr (KEEP) {
       unsigned char* const codes = out + WARP_PIECE * sizeof(IO);
       keep_steps<PATH>(p.x_format, xv, p, w, t0, p.x_codes, p.x_scales, codes);
       keep_steps<PATH>(p.gate_format, gv, p, w, t0, p.gate_codes, p.gate_scales, codes + WARP_PIECE);
+      if (!alive) void_kept(p, w, t0);
     }
     float2 in[SCAN_K];
     coefficients(gv, in, p.mode);   // gv becomes a, and xv b
@@ -482,6 +490,12 @@ __global__ void __launch_bounds__(128) scan_short_kernel(const __grid_constant__
 // The quantity handed from step to step is e_t = a_t D_t = a_t (dh_t + e_{t+1}), again an affine map, composed from the
 // last step to the first; the states of the chunk are recomputed from its checkpoint by the forward maps.  A block's
 // chunk starts at a checkpoint, so only e crosses blocks.  Warp 0 chains the states, warp 1 the e.
+// NaN in place of the gradients of a warp's steps.
+template <typename IO> __device__ __forceinline__ void void_steps(unsigned char* out, const Place& w, int t0) {
+  IO* const to = reinterpret_cast<IO*>(out) + 2 * w.lane;
+  for (int k = 0; k < 2 * SCAN_K; ++k) store_pair<true>(to + k * SCAN_COLS, 0, 2, t0 + k % SCAN_K < w.len ? nan2() : both(0.f));
+}
+
 template <typename IO, int PATH>
 __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __grid_constant__ ScanParams p) {
   using raw = typename Pair<IO>::raw;
@@ -500,7 +514,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
   auto issue = [&](int turn, int slot) {
     unsigned char* const at = s_dyn + slot * slot_bytes;
     if constexpr (PATH == TILES) {
-      if (turn >= w.from && turn > p.loads_end) {
+      if (turn >= w.from && !(WAIT_TESTS && turn <= p.loads_end)) {
         mbar_arrive_expect_tx(&s_landed[slot], slot_bytes);
         tma_load_3d(at, &p.in[0], w.col0, w.b, turn, &s_landed[slot]);
         tma_load_3d(at + x_at, &p.in[1], w.col0, w.b, turn, &s_landed[slot]);
@@ -541,7 +555,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     next_start = load_start(turn - SNN_SCAN_CHUNK);
     unsigned char* const at = s_dyn + slot * slot_bytes;
     if (PATH == TILES) {
-      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u, w.warp == 5 && turn <= p.quits_at ? 0u : p.polls);
+      if (alive) alive = mbar_wait(&s_landed[slot], (uint32_t)(i / SCAN_DEPTH) & 1u, polls_of(p, w, turn <= p.quits_at));
       if (w.lane == 0) bulk_read_done<1>();
       __syncwarp();
     }
@@ -617,7 +631,6 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     }
     __syncthreads();
     float2 h = s_h[w.warp][w.lane], e = s_e[w.warp][w.lane];
-    if (!alive) h = e = nan2();   // (a has a NaN at the first of the warp's steps, e goes through them from the last one)
     // u_k = dgate_k / D_k from the first step to the last, then D and the results from the last to the first.
     // DIRECT: u = h, dx = D; SIGMOID: u = i a (h - x), dx = D i
     auto outputs = [&](auto is_direct, auto is_full) {
@@ -658,6 +671,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) scan_backward_kernel(const __gr
     if (p.mode == SNN_SCAN_DIRECT) full ? outputs(std::true_type(), std::true_type()) : outputs(std::true_type(), std::false_type());
     else full ? outputs(std::false_type(), std::true_type()) : outputs(std::false_type(), std::false_type());
     if (PATH == TILES) {
+      if (!alive) void_steps<IO>(out, w, t0);
       fence_proxy_async_smem();
       __syncwarp();
       if (w.lane == 0) {
@@ -835,7 +849,8 @@ void cut_time(ScanParams& p, int resident) {
   while (p.parts < 4 && p.segment_steps >= 2 * p.parts * WARPS * 128) p.parts *= 2;
 }
 // Blocks per SM: a forward pass that keeps nothing fits a fourth one of 16-bit values (65536 x 1 x 1024 bf16: 142 us with
-// segments for three, 133 for four).
+// segments for three, 133 for four).  fp32: two, but one where states are kept (the tiles and the room for two copies in 8 bits
+// take 119 KB); it is cut as for two all the same, and its segments take two turns on the device.
 int resident_blocks(int dtype, bool backward, bool keep) {
   if (dtype == SNN_DTYPE_FP32) return backward ? 1 : 2;
   return backward ? 2 : keep ? 3 : 4;
@@ -978,6 +993,7 @@ extern "C" snn_status snn_scan_backward(const snn_scan_args* a, void* stream) { 
 extern "C" snn_status snn_selftest_scan_wait(const snn_scan_args* a, int32_t is_backward, int32_t step, int32_t quits, uint32_t poll_limit,
                                              void* stream) {
   if (step < 0 || poll_limit == 0 || poll_limit > MBAR_WAIT_LIMIT) return SNN_ERR_INVALID_ARG;
+  if (!WAIT_TESTS) return SNN_ERR_UNSUPPORTED;
   const WaitTest test{step, quits != 0, poll_limit};
   return is_backward ? backward(a, &test, stream) : forward(a, &test, stream);
 }

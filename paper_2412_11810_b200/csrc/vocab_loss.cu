@@ -92,8 +92,8 @@ struct ProductParams {
   bool dw_vector;             // rows of dw are aligned to 16 bytes
   const float* alpha;         // DW: factor, from the device
   uint32_t* status;
-  // limits of the waits; the self-test lets them run out: no loads from a unit of work on, or one warp of the epilogue that
-  // does not wait for it
+  // WAIT_TESTS: limits of the waits.  The self-test lets them run out: no loads from a unit of work on, or one warp of the
+  // epilogue that does not wait for it
   uint32_t polls;
   int loads_end, quits_at;
 };
@@ -186,6 +186,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
   const uint32_t rank = cluster_rank();
   const int pair = blockIdx.x >> 1, n_pairs_sm = gridDim.x >> 1;
   const int units = p.tiles_m * p.tiles_n * p.splits;
+  const uint32_t polls = WAIT_TESTS ? p.polls : MBAR_WAIT_LIMIT;
   let_next_kernel_start();
 
   if (tid == 0) {
@@ -211,14 +212,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
     if (lane == 0) {   // loads: this block's halves of A and B, announced to the even block's barrier
       int it = 0;
       bool ok = true;
-      for (int u = pair; u < units && u < p.loads_end && ok; u += n_pairs_sm) {
+      for (int u = pair; u < units && !(WAIT_TESTS && u >= p.loads_end) && ok; u += n_pairs_sm) {
         const Unit w = unit_of<EPI>(p, u);
         const int row_a = p.a0 + w.m * UM_TILE + (int)rank * UM_HALF, row_b = p.b0 + w.n * UM_TILE + (int)rank * UM_HALF;
         for (int q = 0; q < p.n_pairs && ok; ++q) {
           const int plane_a = (p.pair_a >> (4 * q)) & 15, plane_b = (p.pair_b >> (4 * q)) & 15;
           for (int kb = 0; kb < w.kbs; ++kb, ++it) {
             const int st = it % UM_STAGES;
-            if (it >= UM_STAGES && !(ok = wait_for(&s.empty[st], (uint32_t)(it / UM_STAGES - 1) & 1u, s, p.status, p.polls))) break;
+            if (it >= UM_STAGES && !(ok = wait_for(&s.empty[st], (uint32_t)(it / UM_STAGES - 1) & 1u, s, p.status, polls))) break;
             unsigned char* const at = s_base + (size_t)st * UM_STAGE_BYTES;
             if (rank == 0) mbar_arrive_expect_tx(&s.full[st], 2 * UM_STAGE_BYTES);
             const uint32_t bar = peer_address(smem_u32(&s.full[st]), 0);
@@ -239,12 +240,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
         const int n_it = p.n_pairs * w.kbs;
         for (int i0 = 0; i0 < n_it && ok; i0 += RUNS ? VL_RUN : n_it, ++run) {   // a run of k-blocks into one accumulator
           const int buf = run & 1, end = RUNS ? min(i0 + VL_RUN, n_it) : n_it;
-          if (run >= 2 && !(ok = wait_for(&s.acc_empty[buf], (uint32_t)(run / 2 - 1) & 1u, s, p.status, p.polls))) break;
+          if (run >= 2 && !(ok = wait_for(&s.acc_empty[buf], (uint32_t)(run / 2 - 1) & 1u, s, p.status, polls))) break;
           tcgen05_after_sync();
           const uint32_t acc = tmem + (uint32_t)buf * UM_TILE;
           for (int i = i0; i < end; ++i, ++it) {
             const int st = it % UM_STAGES;
-            if (!(ok = wait_for(&s.full[st], (uint32_t)(it / UM_STAGES) & 1u, s, p.status, p.polls))) break;
+            if (!(ok = wait_for(&s.full[st], (uint32_t)(it / UM_STAGES) & 1u, s, p.status, polls))) break;
             tcgen05_after_sync();
             const uint32_t at = smem_u32(s_base + (size_t)st * UM_STAGE_BYTES);
 #pragma unroll
@@ -270,8 +271,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32 * (2 + WARPS), 1)
     float sums[RUNS ? WIDTH : 1];
     // the run's accumulator is complete / may be filled again
     auto run_full = [&](int u) {
-      const uint32_t polls = warp == 2 && u >= p.quits_at ? 0u : p.polls;
-      return (bool)__all_sync(0xffffffffu, wait_for(&s.acc_full[run & 1], (uint32_t)(run / 2) & 1u, s, p.status, polls));
+      const bool quits = WAIT_TESTS && warp == 2 && u >= p.quits_at;
+      return (bool)__all_sync(0xffffffffu, wait_for(&s.acc_full[run & 1], (uint32_t)(run / 2) & 1u, s, p.status, quits ? 0u : polls));
     };
     auto run_read = [&]() {
       tcgen05_before_sync();
@@ -1270,6 +1271,7 @@ extern "C" snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* a, void
 extern "C" snn_status snn_selftest_vocab_loss_wait(const snn_vocab_loss_args* a, int32_t is_backward, int32_t kernel, int32_t unit, int32_t quits,
                                                    uint32_t poll_limit, void* stream) {
   if (kernel < 0 || kernel > (is_backward ? 2 : 0) || unit < 0 || poll_limit == 0 || poll_limit > MBAR_WAIT_LIMIT) return SNN_ERR_INVALID_ARG;
+  if (!WAIT_TESTS) return SNN_ERR_UNSUPPORTED;
   const WaitTest test{kernel, unit, quits != 0, poll_limit};
   return is_backward ? backward(a, &test, stream) : forward(a, &test, stream);
 }

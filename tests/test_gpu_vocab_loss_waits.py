@@ -4,6 +4,17 @@ import pytest
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
+
+@pytest.fixture(autouse=True)
+def checked_build(monkeypatch):
+    """The self-tests of waits are in the bounds-checked build of the same sources."""
+    import os
+    from paper_2412_11810_b200 import binding as sb
+    monkeypatch.setattr(sb, "LIB_PATH", os.path.join(sb.HERE, "libsnnckpt_debug.so"))
+    monkeypatch.setattr(sb, "lib", sb._load())
+    assert sb.lib.snn_debug_checks_enabled() == 1
+
+
 DT = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
 POLLS = 1 << 14   # a tile takes microseconds, so many polls some milliseconds
 GRAD, DX, DW = 0, 1, 2

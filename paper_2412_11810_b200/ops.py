@@ -184,12 +184,19 @@ def gated_scan(x: torch.Tensor, gate: torch.Tensor, state: Optional[torch.Tensor
     """The gated linear recurrence over x, gate [T][B][N] (fp32, bf16 or fp16; any strides with contiguous channels):
 
         mode "sigmoid":  h_t = a_t h_{t-1} + (1 - a_t) x_t,  a_t = sigmoid(gate_t)
-        mode "direct":   h_t = gate_t h_{t-1} + x_t
+        mode "direct":   h_t = gate_t h_{t-1} + x_t; the gate is a decay, at most one in magnitude: steps are combined
+                         before the state they start from is known, and where a product of consecutive gates leaves
+                         the range of fp32 the result may not be finite, even if that of step after step is
 
     state: fp32 [B][N], the state before the first step (zero if None).  lengths: int32 [B], sample b ends after
     lengths[b] steps (clamped to [0, T]); h is zero behind that and nothing there is read.
     keep: None keeps nothing; "raw" keeps references to x and gate, "int8" and "e4m3" an 8-bit copy of each, made in the
     same pass; keep_gate overrides the format of the gate.  In mode "direct" the gate, a decay close to one, is kept raw.
+    What 8 bits cost the gradients, as norms of their distance to those from raw inputs over 2048 steps of normal x and
+    gates with a standard deviation of 1.5 (states held for about ten steps, gates of mean 2, and a hundred, mean 5):
+    int8 dx 1.1 and 2.7 %, dgate 1.4 and 2.7 %, dstate 0.5 %; e4m3 dx 1.8 and 4.8 %, dgate 3.6 and 5.9 %, dstate 1.1 %.
+    dx owes it to the gate alone (keep_gate="raw": none).  Groups of 64 channels share a scale: a few large ones cost the
+    others bits in int8 (every 50th value of x 20 times the others: dgate 2.6 instead of 1.4 %).
     Returns (h [T][B][N], last state fp32 [B][N], what was kept for `gated_scan_backward` or None)."""
     _values(x, "x", 3)
     shape, dtype = x.shape, x.dtype
@@ -340,7 +347,11 @@ def vocab_loss(x: torch.Tensor, w_out: torch.Tensor, targets: torch.Tensor, *, s
     targets: int32 or int64 [rows]; rows with ignore_index do not count, any other target outside [0, classes) makes its
     row's loss and the mean NaN.
     Returns (loss, a 0-d tensor; row_loss [rows]; lse [rows], the log-sum-exp that `vocab_loss_backward` needs), all fp32,
-    with zeros for rows that do not count."""
+    with zeros for rows that do not count.
+
+    Products of fp32 operands are those of fp32 arithmetic (three 16-bit parts of every value, on the tensor cores), of 16-bit
+    ones exact; sums are fp32 (of 16-bit products: in the tensor cores' accumulators, which cut what does not fit).
+    Workspace: 8 bytes per row and 128 classes (up to four rows: per block), and in fp32 6 bytes per value of x and w."""
     a = _vocab_args(x, w_out, targets, scale, ignore_index)
     with _on(x):
         row_loss = x.new_empty(a.rows, dtype=torch.float32)
@@ -354,7 +365,13 @@ def vocab_loss(x: torch.Tensor, w_out: torch.Tensor, targets: torch.Tensor, *, s
 def vocab_loss_backward(x: torch.Tensor, w_out: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, *, scale: float = 1.0,
                         ignore_index: int = -100, dloss=1.0):
     """Gradients of `vocab_loss` by x and w_out: (dx [rows][dim], dw [dim][classes], stored as w_out is), in their type.
-    dloss: the gradient of the loss, a number or an fp32 0-d tensor on the device."""
+    dloss: the gradient of the loss, a number or an fp32 0-d tensor on the device.
+
+    The logits are computed again; their derivatives are rounded to the operands' type before they are multiplied by w and x
+    (bf16: to 8 bits, which adds 4e-4 to 6e-4 of their norm to gradients that are themselves rounded to 1.7e-3; fp16: to 11
+    bits; fp32: not at all).  Workspace: 512 MB of them at a time at most (less if rows x classes are fewer; at least 256
+    classes), a copy of x, in fp32 also one of w of 6 bytes per value, and fp32 sums for dx, several of them where rows x
+    dim are few."""
     a = _vocab_args(x, w_out, targets, scale, ignore_index)
     _like(lse, "lse", x, (a.rows,), torch.float32)
     if isinstance(dloss, torch.Tensor):

@@ -434,7 +434,7 @@ snn_status snn_selftest_scan_wait(const snn_scan_args* args, int32_t backward, i
  * arithmetic.  Sums are fp32; those of 16-bit products stay in the tensor cores' accumulators, which cut what does not fit
  * instead of rounding it (about 2^-24 of the sum per 16 terms).  In the backward pass the derivatives by the logits exist one
  * piece of the vocabulary at a time in the workspace, rounded to the operands' type: 8 bits in bf16; 11 bits in fp16, where
- * the derivative of a row's own loss is above 2^-28, and a step of 2^-38 below; all 24 in fp32.
+ * the derivative of a row's own loss is above 2^-28, and a step of 2^-38 below; all 24 in fp32 (above 2^-109 times the rows).
  * W_out is stored by feature (SNN_W_BY_FEATURE: [dim][classes] as everywhere in this library) or by class
  * (SNN_W_BY_CLASS: [classes][dim], the transpose, as in an embedding table); w_stride is the distance of its rows. dw has
  * the same layout with its own stride. */

@@ -471,6 +471,114 @@ snn_status snn_vocab_loss_backward(const snn_vocab_loss_args* args, void* stream
 snn_status snn_selftest_vocab_loss_wait(const snn_vocab_loss_args* args, int32_t backward, int32_t kernel, int32_t unit, int32_t quits,
                                         uint32_t poll_limit, void* stream);
 
+/* Root-mean-square norm of the rows of x [rows][n], with the residual's addition in front of it:
+ *   h = x + residual, rounded to the type (h = x without one);  rstd = 1 / sqrt(mean(h^2) + eps);  y = h rstd weight
+ * and its backward pass, for the gradients dy of y and dh of h (what the residual stream hands back; NULL: zero):
+ *   g = dy weight,  c = mean(g h rstd):   dx = rstd (g - h rstd c) + dh,   dweight = sum over the rows of dy h rstd
+ * dx is the gradient by x and by the residual alike.  y is written as values, in 8 bits (keep_format; of the values before
+ * they are rounded to the type), or both.  Squares that leave the range of fp32 are summed scaled, so that rows of any finite
+ * values are normed; a row with an infinity has rstd = 0. */
+typedef struct {
+  int64_t rows;                /* >= 0                                                                  */
+  int32_t n;                   /* 1 <= n <= 2^31 - 64 (SNN_ERR_UNSUPPORTED)                             */
+  int32_t dtype;               /* snn_dtype of x, residual, h, y, dy, dh, dx                            */
+  int32_t weight_dtype;        /* that of weight and dweight: dtype, or fp32                            */
+  float eps;                   /* from 1e-30 to 1                                                       */
+  const void* x; int64_t x_stride;              /* forward                                              */
+  const void* residual; int64_t residual_stride;/* forward, or NULL; strides are those of rows          */
+  const void* weight;          /* [n], or NULL: ones                                                    */
+  void* h; int64_t h_stride;   /* written by the forward pass where there is a residual (it may be that
+                                  of x or of the residual); read by the backward pass                   */
+  void* y; int64_t y_stride;   /* forward; may be NULL where codes are written                          */
+  int32_t keep_format;         /* snn_keep_format: RAW for no 8-bit copy                                */
+  uint8_t *codes, *scales;     /* [rows][n] and [rows][ceil(n / 64)]                                    */
+  float* rstd;                 /* [rows]; written by the forward pass (may be NULL), read by the backward pass */
+  const void* dy; int64_t dy_stride;            /* backward                                             */
+  const void* dh; int64_t dh_stride;            /* backward, or NULL                                    */
+  void* dx; int64_t dx_stride; /* backward; may be dy or dh                                             */
+  void* dweight;               /* [n], backward, or NULL                                                */
+  void* workspace; size_t workspace_bytes;      /* device, 256-byte aligned: backward pass with dweight only; calls
+                                  that may overlap in time need workspaces of their own                 */
+} snn_rms_norm_args;
+/* Bytes of workspace that the backward pass needs: it depends on rows and n alone, 4 n bytes per thread block. */
+snn_status snn_rms_norm_workspace(const snn_rms_norm_args* args, size_t* bytes);
+snn_status snn_rms_norm_forward(const snn_rms_norm_args* args, void* stream);
+snn_status snn_rms_norm_backward(const snn_rms_norm_args* args, void* stream);
+
+/* One AdamW step over any number of tensors at once, with t the number of this step:
+ *   g = scale grad (times max_norm / norm, where the 2-norm of all g is above max_norm)
+ *   m' = beta1 m + (1 - beta1) g,   v' = beta2 v + (1 - beta2) g^2
+ *   p' = p (1 - lr weight_decay) - lr m' / (1 - beta1^t) / (sqrt(v' / (1 - beta2^t)) + eps)
+ * in fp32, p' rounded to the parameters' type once (16-bit parameters whose change is below half a step stay as they are: keep
+ * them in fp32 then, and let `copy` hold the 16-bit copies that the products read).
+ * The moments of all tensors lie one behind the other, each tensor's from a multiple of 64 values on: tensor k from the sum of
+ * 64 ceil(n_j / 64) over j < k on.  Places behind a tensor's end are padding.
+ *   SNN_KEEP_RAW: fp32 m and v.   SNN_KEEP_E4M3: m and sqrt(v) in e4m3 groups of 64 (codes and scale bytes as
+ * snn_activation_unpack reads them), since in sqrt(v) e4m3 holds a range of 2^36 of v.  A moment moves by a small part of its
+ * codes' steps, so codes are rounded up or down at random: magnitude u in steps becomes floor(u + r / 2^16); m takes the lower
+ * and sqrt(v) the upper 16 bits of hash(seed, t, place) (adamw.cu), and a sqrt(v) above zero at least the smallest code.  A group
+ * with an infinity or a NaN decodes to NaN from then on.
+ * With max_norm > 0 a step whose norm is not finite is left out: nothing changes, and *step does not count it.
+ * v is fp32: gradients beyond 1.8e19 in magnitude make it infinite, and stop that parameter. */
+typedef struct {
+  void* param; const void* grad;   /* device, contiguous; no two tensors overlap                        */
+  void* copy;                      /* device, or NULL: p' rounded to copy_dtype                          */
+  int64_t n;                       /* values, >= 0                                                       */
+  int32_t param_dtype, grad_dtype, copy_dtype;   /* snn_dtype                                            */
+} snn_adamw_tensor;
+typedef struct {
+  int32_t count;
+  int32_t moment_format;           /* SNN_KEEP_RAW or SNN_KEEP_E4M3                                      */
+  const snn_adamw_tensor* tensors; /* [count], host; read before the call returns                        */
+  float *m, *v;                    /* SNN_KEEP_RAW; 32-byte aligned                                      */
+  uint8_t *m_codes, *m_scales, *v_codes, *v_scales;   /* SNN_KEEP_E4M3; codes 8-byte aligned             */
+  int64_t* step;                   /* device: steps done so far; the call adds one                       */
+  double lr, beta1, beta2, eps, weight_decay;   /* lr, weight_decay >= 0; 0 <= beta < 1; 1e-30 <= eps <= 1 */
+  const float* lr_device;          /* or NULL: used in place of lr                                       */
+  float scale;                     /* of the gradients                                                   */
+  const float* scale_device;       /* or NULL: a factor beside scale                                     */
+  double max_norm;                 /* 0: no clip, and no norm is computed                                */
+  float* norm;                     /* device, or NULL: the norm before the clip (max_norm > 0)           */
+  uint64_t seed;
+  void* workspace; size_t workspace_bytes;      /* device, 256-byte aligned; calls that may overlap in time need
+                                      workspaces of their own                                            */
+} snn_adamw_args;
+/* (SNN_ADAMW_WORKSPACE bytes, whatever the tensors.) */
+#define SNN_ADAMW_WORKSPACE 5120
+snn_status snn_adamw_workspace(const snn_adamw_args* args, size_t* bytes);
+snn_status snn_adamw_step(const snn_adamw_args* args, void* stream);
+
+/* One step of beam search: of the K V continuations of a sample's beams the best W,
+ *   score(k, c) = scores[k] + log softmax(logits[k])[c],
+ * ranked in 64 bits, classes of one beam by their logits; ties go to the lower beam, then to the lower class.  An ended beam
+ * goes on with `end` alone, at its own score.  Continuations at -infinity come last, in the order of k V + c: all others of an
+ * ended beam, masked classes (logits of -infinity), and every one of a beam that is dead, whose score is not finite or
+ * whose logits are all masked or hold a NaN or +infinity.
+ * Limits (SNN_ERR_UNSUPPORTED): K and W up to 32, V up to 2^22. */
+typedef struct {
+  const void* from; void* to;      /* device: rows one behind the other; the same pointer, where W = K: in place; no other overlap */
+  int64_t row_bytes;
+} snn_state_rows;
+typedef struct {
+  int32_t B, K, W, V;              /* samples, beams of each, survivors of each, classes; B >= 0, W <= K V */
+  int32_t dtype;                   /* snn_dtype of the logits                                            */
+  const void* logits; int64_t sample_stride, beam_stride;   /* [B][K][V]                                 */
+  const float* scores;             /* [B][K]                                                             */
+  const uint8_t* ended;            /* [B][K], or NULL: none has                                          */
+  int64_t end;                     /* the class that ends a beam; -1: none does (ended, new_ended are NULL then) */
+  int64_t *tokens, *parents;       /* [B][W]: class and beam of each survivor, the best first            */
+  float* new_scores;               /* [B][W]                                                             */
+  uint8_t* new_ended;              /* [B][W], or NULL                                                    */
+  const snn_state_rows* states; int32_t n_states;   /* host; read before the call returns: moved as snn_reorder_rows does */
+  void* workspace; size_t workspace_bytes;      /* device, 256-byte aligned; calls that may overlap in time need
+                                      workspaces of their own                                            */
+} snn_beam_args;
+snn_status snn_beam_workspace(const snn_beam_args* args, size_t* bytes);
+snn_status snn_beam_step(const snn_beam_args* args, void* stream);
+/* to[b][w] = from[b][parents[b][w]] for rows [B][K] -> [B][W] of any number of arrays; a parent outside [0, K) leaves a row
+ * of zeros and is never an index.  parents: device, [B][W]. */
+snn_status snn_reorder_rows(const snn_state_rows* states, int32_t count, const int64_t* parents, int32_t B, int32_t K, int32_t W, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

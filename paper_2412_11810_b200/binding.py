@@ -46,8 +46,10 @@ EXPORTS = ["snn_create", "snn_destroy", "snn_alpha", "snn_workspace_query", "snn
            "snn_phase_times_get", "snn_train_step_static", "snn_suggest_ckpt", "snn_selftest_wait_timeout",
            "snn_debug_checks_enabled", "snn_activation_pack", "snn_activation_unpack", "snn_scan_forward",
            "snn_scan_backward", "snn_scan_workspace", "snn_vocab_loss_workspace", "snn_vocab_loss_forward", "snn_vocab_loss_backward",
-           "snn_selftest_scan_wait", "snn_selftest_vocab_loss_wait"]
+           "snn_selftest_scan_wait", "snn_selftest_vocab_loss_wait", "snn_rms_norm_workspace", "snn_rms_norm_forward",
+           "snn_rms_norm_backward", "snn_adamw_workspace", "snn_adamw_step", "snn_beam_workspace", "snn_beam_step", "snn_reorder_rows"]
 SNN_STATIC_WORKSPACE_BYTES = 32 << 20
+SNN_ADAMW_WORKSPACE = 5120
 
 
 class snn_config(C.Structure):
@@ -112,6 +114,41 @@ class snn_vocab_loss_args(C.Structure):
                 ("dw_stride", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class snn_rms_norm_args(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("n", C.c_int32), ("dtype", C.c_int32), ("weight_dtype", C.c_int32), ("eps", C.c_float),
+                ("x", C.c_void_p), ("x_stride", C.c_int64), ("residual", C.c_void_p), ("residual_stride", C.c_int64),
+                ("weight", C.c_void_p), ("h", C.c_void_p), ("h_stride", C.c_int64), ("y", C.c_void_p), ("y_stride", C.c_int64),
+                ("keep_format", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p), ("rstd", C.c_void_p),
+                ("dy", C.c_void_p), ("dy_stride", C.c_int64), ("dh", C.c_void_p), ("dh_stride", C.c_int64), ("dx", C.c_void_p),
+                ("dx_stride", C.c_int64), ("dweight", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class snn_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("n", C.c_int64), ("param_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("copy_dtype", C.c_int32)]
+
+
+class snn_adamw_args(C.Structure):
+    _fields_ = [("count", C.c_int32), ("moment_format", C.c_int32), ("tensors", C.POINTER(snn_adamw_tensor)), ("m", C.c_void_p),
+                ("v", C.c_void_p), ("m_codes", C.c_void_p), ("m_scales", C.c_void_p), ("v_codes", C.c_void_p),
+                ("v_scales", C.c_void_p), ("step", C.c_void_p), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
+                ("eps", C.c_double), ("weight_decay", C.c_double), ("lr_device", C.c_void_p), ("scale", C.c_float),
+                ("scale_device", C.c_void_p), ("max_norm", C.c_double), ("norm", C.c_void_p), ("seed", C.c_uint64),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class snn_state_rows(C.Structure):
+    _fields_ = [("source", C.c_void_p), ("to", C.c_void_p), ("row_bytes", C.c_int64)]   # ("from" is a word of Python)
+
+
+class snn_beam_args(C.Structure):
+    _fields_ = [("B", C.c_int32), ("K", C.c_int32), ("W", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32), ("logits", C.c_void_p),
+                ("sample_stride", C.c_int64), ("beam_stride", C.c_int64), ("scores", C.c_void_p), ("ended", C.c_void_p),
+                ("end", C.c_int64), ("tokens", C.c_void_p), ("parents", C.c_void_p), ("new_scores", C.c_void_p),
+                ("new_ended", C.c_void_p), ("states", C.POINTER(snn_state_rows)), ("n_states", C.c_int32),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python paper_2412_11810_b200/build.py` "
@@ -156,6 +193,14 @@ def _load() -> C.CDLL:
     lib.snn_vocab_loss_backward.argtypes = [C.POINTER(snn_vocab_loss_args), C.c_void_p]
     lib.snn_selftest_vocab_loss_wait.argtypes = [C.POINTER(snn_vocab_loss_args), C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                                  C.c_uint32, C.c_void_p]
+    lib.snn_rms_norm_workspace.argtypes = [C.POINTER(snn_rms_norm_args), C.POINTER(C.c_size_t)]
+    lib.snn_rms_norm_forward.argtypes = [C.POINTER(snn_rms_norm_args), C.c_void_p]
+    lib.snn_rms_norm_backward.argtypes = [C.POINTER(snn_rms_norm_args), C.c_void_p]
+    lib.snn_adamw_workspace.argtypes = [C.POINTER(snn_adamw_args), C.POINTER(C.c_size_t)]
+    lib.snn_adamw_step.argtypes = [C.POINTER(snn_adamw_args), C.c_void_p]
+    lib.snn_beam_workspace.argtypes = [C.POINTER(snn_beam_args), C.POINTER(C.c_size_t)]
+    lib.snn_beam_step.argtypes = [C.POINTER(snn_beam_args), C.c_void_p]
+    lib.snn_reorder_rows.argtypes = [C.POINTER(snn_state_rows), C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p]
     return lib
 
 
@@ -313,6 +358,44 @@ def snn_vocab_loss_backward(args: snn_vocab_loss_args, stream: int = 0) -> None:
 def snn_selftest_vocab_loss_wait(args: snn_vocab_loss_args, backward: bool, kernel: int, unit: int, quits: bool, poll_limit: int,
                                  stream: int = 0) -> None:
     _check(lib.snn_selftest_vocab_loss_wait(C.byref(args), int(backward), kernel, unit, int(quits), poll_limit, stream))
+
+
+def snn_rms_norm_workspace(args: snn_rms_norm_args) -> int:
+    n = C.c_size_t()
+    _check(lib.snn_rms_norm_workspace(C.byref(args), C.byref(n)))
+    return n.value
+
+
+def snn_rms_norm_forward(args: snn_rms_norm_args, stream: int = 0) -> None:
+    _check(lib.snn_rms_norm_forward(C.byref(args), stream))
+
+
+def snn_rms_norm_backward(args: snn_rms_norm_args, stream: int = 0) -> None:
+    _check(lib.snn_rms_norm_backward(C.byref(args), stream))
+
+
+def snn_adamw_workspace(args: snn_adamw_args) -> int:
+    n = C.c_size_t()
+    _check(lib.snn_adamw_workspace(C.byref(args), C.byref(n)))
+    return n.value
+
+
+def snn_adamw_step(args: snn_adamw_args, stream: int = 0) -> None:
+    _check(lib.snn_adamw_step(C.byref(args), stream))
+
+
+def snn_beam_workspace(args: snn_beam_args) -> int:
+    n = C.c_size_t()
+    _check(lib.snn_beam_workspace(C.byref(args), C.byref(n)))
+    return n.value
+
+
+def snn_beam_step(args: snn_beam_args, stream: int = 0) -> None:
+    _check(lib.snn_beam_step(C.byref(args), stream))
+
+
+def snn_reorder_rows(states, count: int, parents_ptr: int, B: int, K: int, W: int, stream: int = 0) -> None:
+    _check(lib.snn_reorder_rows(states, count, parents_ptr, B, K, W, stream))
 
 
 def ptr_array(ptrs: Sequence[Optional[int]]):

@@ -1,0 +1,562 @@
+// One step of beam search over a vocabulary, and the beams' states in their new order (include/snn.h, "sequence-model operators").
+//
+//   score(k, v) = s_k + (z_kv - m_k) - log sum_v exp(z_kv - m_k),  m_k = max_v z_kv;  the best `width` of a sample, lower k V + v first
+//
+// Bound by HBM: the logits are read once.  A thread block walks through a part of a beam's row, segment by segment, and leaves
+// behind its maximum, its sum of exponentials and its `width` best classes; a second kernel, a block per sample, joins the parts
+// of each row and the rows of the sample; a third moves the states.  Each is set up while the one before it runs.
+//
+// The best of a part: 64 groups of four lanes have a maximum each in the first segment, and the width-th largest of them is a
+// bound that at least `width` values reach: few more do (a dozen for eight), and those are ranked by comparing each with all.
+// From then on the width-th best so far is the bound, which few values of a later segment pass.
+// Keys hold the value above the complement of the class, so that no two are the same and ties go to the lower class.
+#include <algorithm>
+
+#include "octet.cuh"
+
+using namespace snnk;
+
+namespace {
+
+constexpr int BM_THREADS = 256, BM_GROUPS = BM_THREADS / 4, BM_CANDIDATES = 1024, BM_STAGES = 3;
+constexpr int BM_MOST = 32;          // beams of a sample, and survivors
+constexpr int BM_JOIN_WARPS = 8;
+constexpr int BM_TABLE = 64;         // states of one launch
+constexpr int BM_COPY_THREADS = 256;
+constexpr int BM_PIECE = 16 * 1024, BM_PIECE_IN_PLACE = 1024;   // bytes of a row at a time
+
+struct BeamParams {
+  int64_t rows;
+  int K, W, V, splits, length;        // a row is cut into `splits` parts of `length` segments
+  int64_t sample_stride, beam_stride, end;
+  const void* logits;
+  const float* scores;
+  const uint8_t* ended;
+  uint64_t* keys;                    // [rows][splits][W], falling; 0: none
+  float2* stats;                     // [rows][splits]: maximum, sum of exp(z - maximum)
+  int64_t *tokens, *parents;         // [B][W]
+  float* new_scores;
+  uint8_t* new_ended;
+};
+
+__device__ __forceinline__ uint32_t rising(float v) {   // unsigned numbers that order as finite values do; -0 is 0
+  const uint32_t u = __float_as_uint(v + 0.f);
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float from_rising(uint32_t r) { return __uint_as_float(r & 0x80000000u ? r ^ 0x80000000u : ~r); }
+__device__ __forceinline__ uint64_t key_of(float v, uint32_t c) { return (uint64_t)rising(v) << 32 | (0xffffffffu - c); }
+__device__ __forceinline__ uint32_t class_of(uint64_t key) { return 0xffffffffu - (uint32_t)key; }
+__device__ __forceinline__ uint64_t warp_max(uint64_t v) {
+  const uint32_t high = __reduce_max_sync(0xffffffffu, (uint32_t)(v >> 32));
+  const uint32_t low = __reduce_max_sync(0xffffffffu, (uint32_t)(v >> 32) == high ? (uint32_t)v : 0u);
+  return (uint64_t)high << 32 | low;
+}
+// Whether a beam goes on to other classes than the end's: it has not ended, and its score is a number.
+__device__ __forceinline__ bool goes_on(const BeamParams& p, int64_t row) {
+  return !(p.ended && p.ended[row]) && fabsf(p.scores[row]) <= largest_finite<float>();
+}
+
+// Copies of 16 bytes from global to shared memory that the thread does not wait for.
+__device__ __forceinline__ void copy_16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void close_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int OPEN> __device__ __forceinline__ void wait_groups() { asm volatile("cp.async.wait_group %0;" ::"n"(OPEN) : "memory"); }
+
+// A segment's place in shared memory, and the values of a thread: fp32 classes tid + 256 j, 16-bit ones 2 tid + 512 j and the
+// next, whatever the address of the row (so that equal rows have equal sums).  The bytes lie as in the row, 16 by 16: class 0
+// of the segment stands `lead` values behind the start.
+template <typename IO, int VALUES> struct Segment {
+  static constexpr int CLASSES = BM_THREADS * VALUES, PER_COPY = 16 / sizeof(IO), BYTES = CLASSES * sizeof(IO) + 32;
+  // Starts the copies of classes c0 .. of a row of V; 16 bytes that reach beyond the row's ends are read value by value.
+  static __device__ __forceinline__ void fetch(uint8_t* to, const IO* z, int64_t c0, int V) {
+    const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO)), here = (int)min((int64_t)CLASSES, V - c0);
+    const int copies = (lead + here + PER_COPY - 1) / PER_COPY;
+    for (int i = threadIdx.x; i < copies; i += BM_THREADS) {
+      const int64_t c = c0 + i * PER_COPY - lead;
+      if (c >= 0 && c + PER_COPY <= V) {
+        copy_16((uint32_t)__cvta_generic_to_shared(to + 16 * i), z + c);
+      } else {
+        for (int j = 0; j < PER_COPY; ++j)
+          if (c + j >= 0 && c + j < V) reinterpret_cast<IO*>(to)[i * PER_COPY + j] = z[c + j];
+      }
+    }
+  }
+  using Raw = typename Pair<IO>::raw;
+  Raw raw[VALUES / 2];    // what does not exist is -infinity: never a candidate, as what is masked
+  __device__ __forceinline__ void read(const uint8_t* from, const IO* z, int64_t c0, int V) {
+    const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO)), here = (int)min((int64_t)CLASSES, V - c0);
+    const IO none = from_f32<IO>(__uint_as_float(0xff800000u));
+    const IO* const at = reinterpret_cast<const IO*>(from) + lead;
+    if (sizeof(IO) == 2 && lead % 2 == 0 && here == CLASSES) {
+#pragma unroll
+      for (int i = 0; i < VALUES / 2; ++i) raw[i] = *reinterpret_cast<const Raw*>(at + place(2 * i));
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < VALUES / 2; ++i) {
+      const int a = place(2 * i), b = place(2 * i + 1);
+      raw[i].x = a < here ? at[a] : none;
+      raw[i].y = b < here ? at[b] : none;
+    }
+  }
+  static __device__ __forceinline__ int place(int j) {
+    return sizeof(IO) == 2 ? 2 * (int)threadIdx.x + j / 2 * (2 * BM_THREADS) + j % 2 : (int)threadIdx.x + j * BM_THREADS;
+  }
+  __device__ __forceinline__ float2 pair(int i) const { return to_f32(raw[i]); }
+  __device__ __forceinline__ float value(int j) const { return j % 2 ? pair(j / 2).y : pair(j / 2).x; }
+};
+__device__ __forceinline__ float exp2_of(float v) {
+  float e;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v));
+  return e;
+}
+constexpr float LOG2_E = 1.4426950408889634f;
+
+// A block: `length` segments of a row, one behind the other through a ring of BM_STAGES places in shared memory.
+template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS, 4) beam_rows_kernel(const BeamParams p) {
+  using Seg = Segment<IO, VALUES>;
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ float group_max[BM_GROUPS], warp_part[2][BM_THREADS / 32];
+  __shared__ uint32_t need;            // candidates are values v with rising(v) at or above it
+  __shared__ int count;                // candidates so far, the best `kept` of earlier segments first
+  __shared__ uint64_t candidates[BM_CANDIDATES];
+  let_next_kernel_start();
+  const int64_t row = blockIdx.x / p.splits;
+  const int split = blockIdx.x % p.splits, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (!goes_on(p, row)) return;
+  const IO* const z = (const IO*)p.logits + row / p.K * p.sample_stride + row % p.K * p.beam_stride;
+  const int64_t first = (int64_t)split * p.length * Seg::CLASSES;
+  const int segments = (int)min((int64_t)p.length, (p.V - first + Seg::CLASSES - 1) / Seg::CLASSES);
+  auto fetch = [&](int s) {
+    if (s < segments) Seg::fetch(ring + s % BM_STAGES * Seg::BYTES, z, first + (int64_t)s * Seg::CLASSES, p.V);
+    close_group();
+  };
+#pragma unroll
+  for (int s = 0; s < BM_STAGES - 1; ++s) fetch(s);
+  if (tid == 0) count = 0;
+  const float none = __uint_as_float(0xff800000u);
+  float most = none, sum = 0.f;        // of this thread's values: the maximum, and the sum of exp(v - maximum)
+  int kept = 0;
+  for (int s = 0; s < segments; ++s) {
+    wait_groups<BM_STAGES - 2>();
+    __syncthreads();                   // the segment is there for all, and the one before it has been read by all
+    fetch(s + BM_STAGES - 1);
+    const int64_t c0 = first + (int64_t)s * Seg::CLASSES;
+    Seg g;
+    g.read(ring + s % BM_STAGES * Seg::BYTES, z, c0, p.V);
+    float here = none;
+#pragma unroll
+    for (int i = 0; i < VALUES / 2; ++i) here = fmaxf(here, fmaxf(g.pair(i).x, g.pair(i).y));
+    if (here > most) {
+      sum *= exp2_of((most - here) * LOG2_E);   // (0 of a sum that is 0)
+      most = here;
+    }
+    if (most > none) {
+      // (the difference first: it is exact where the values are near one another, which is where it counts)
+      float2 more = both(0.f);
+#pragma unroll
+      for (int i = 0; i < VALUES / 2; ++i) {
+        const float2 d = mul2(add2(g.pair(i), both(-most)), both(LOG2_E));
+        more = add2(more, make_float2(exp2_of(d.x), exp2_of(d.y)));
+      }
+      sum += more.x + more.y;
+    } else {   // masked places alone, or NaN, of which fmaxf takes no notice
+#pragma unroll
+      for (int i = 0; i < VALUES / 2; ++i)
+        if (g.pair(i).x != g.pair(i).x || g.pair(i).y != g.pair(i).y) sum = __uint_as_float(0x7fc00000u);
+    }
+    // the first segment: the width-th largest of its groups' maxima is a bound that at least `width` values reach
+    if (s == 0) {
+      float m = fmaxf(here, __shfl_xor_sync(0xffffffffu, here, 1));
+      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
+      if (lane % 4 == 0) group_max[tid / 4] = m;
+      __syncthreads();
+      if (tid < BM_GROUPS) {
+        const float mine = group_max[tid];
+        int before = 0;
+#pragma unroll 8
+        for (int j = 0; j < BM_GROUPS; ++j) before += group_max[j] > mine || (group_max[j] == mine && j < tid);
+        if (before == p.W - 1) need = rising(mine);
+      }
+      __syncthreads();
+    }
+    const uint32_t bound = need;
+    bool pushed = false;
+    if (here > none && rising(here) >= bound) {
+      pushed = true;
+#pragma unroll
+      for (int j = 0; j < VALUES; ++j) {
+        const float v = g.value(j);
+        if (v > none && rising(v) >= bound) {
+          const int at = atomicAdd(&count, 1);
+          if (at < BM_CANDIDATES) candidates[at] = key_of(v, (uint32_t)(c0 + Seg::place(j)));
+        }
+      }
+    }
+    if (!__syncthreads_or(pushed)) continue;
+    const int n = count;
+    if (n <= BM_CANDIDATES) {
+      // each of them goes to the place that the number of larger ones gives it
+      uint64_t mine[BM_CANDIDATES / BM_THREADS];
+      int to[BM_CANDIDATES / BM_THREADS];
+#pragma unroll
+      for (int k = 0; k < BM_CANDIDATES / BM_THREADS; ++k) {
+        const int i = tid + k * BM_THREADS;
+        to[k] = p.W;
+        if (i >= n) continue;
+        mine[k] = candidates[i];
+        to[k] = 0;
+        for (int j = 0; j < n; ++j) to[k] += candidates[j] > mine[k];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < BM_CANDIDATES / BM_THREADS; ++k)
+        if (to[k] < p.W) candidates[to[k]] = mine[k];
+      kept = min(n, p.W);
+    } else {
+      // too many at or above the bound (equal values, or rising ones): the next best of all, one after the other
+      const uint64_t held = tid < kept ? candidates[tid] : 0;
+      uint64_t last = ~(uint64_t)0;
+      int found = 0;
+      for (; found < p.W; ++found) {
+        uint64_t best = held < last ? held : 0;
+#pragma unroll
+        for (int j = 0; j < VALUES; ++j) {
+          const float v = g.value(j);
+          const uint64_t key = v > none ? key_of(v, (uint32_t)(c0 + Seg::place(j))) : 0;
+          if (key < last && key > best) best = key;
+        }
+        best = warp_max(best);
+        __syncthreads();
+        if (lane == 0) candidates[BM_MOST + warp] = best;
+        __syncthreads();
+        for (int k = 0; k < BM_THREADS / 32; ++k) best = max(best, candidates[BM_MOST + k]);
+        if (!best) break;
+        if (tid == 0) candidates[found] = best;   // (what stood there is held by its thread)
+        last = best;
+      }
+      kept = found;
+    }
+    __syncthreads();
+    if (tid == 0) {
+      count = kept;
+      if (kept == p.W) need = (uint32_t)(candidates[p.W - 1] >> 32) + 1;   // a later class has to be larger, not equal
+    }
+    __syncthreads();
+  }
+  uint64_t* const out = p.keys + (row * p.splits + split) * p.W;
+  if (tid < p.W) out[tid] = tid < kept ? candidates[tid] : 0;
+  float m = most;
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (lane == 0) warp_part[0][warp] = m;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < BM_THREADS / 32; ++k) m = fmaxf(m, warp_part[0][k]);
+  float total = most > none ? sum * exp2_of((most - m) * LOG2_E) : sum;
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
+  if (lane == 0) warp_part[1][warp] = total;
+  __syncthreads();
+  if (tid > 0) return;
+  for (int k = 1; k < BM_THREADS / 32; ++k) total += warp_part[1][k];
+  p.stats[row * p.splits + split] = make_float2(m, total);
+}
+
+// A block per sample: the rows of its beams from their segments, a warp each, then the sample from its rows.
+__global__ void __launch_bounds__(32 * BM_JOIN_WARPS) beam_join_kernel(const BeamParams p) {
+  __shared__ uint64_t rows[BM_MOST][BM_MOST];   // the best of each beam
+  __shared__ float row_max[BM_MOST];
+  __shared__ double row_base[BM_MOST];          // score less log sum
+  __shared__ int64_t found[BM_MOST];
+  extern __shared__ uint8_t heads_of_all[];
+  let_next_kernel_start();
+  wait_for_kernel_before();
+  const int64_t b = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  uint8_t* const heads = heads_of_all + warp * p.splits;
+  for (int k = warp; k < p.K; k += warps) {
+    const int64_t row = b * p.K + k;
+    if (!goes_on(p, row)) {
+      // an ended beam goes on with the end alone, at its own score
+      const bool stays = p.ended && p.ended[row] && fabsf(p.scores[row]) <= largest_finite<float>();
+      for (int r = lane; r < p.W; r += 32) rows[k][r] = r == 0 && stays ? key_of(0.f, (uint32_t)p.end) : 0;
+      if (lane == 0) row_max[k] = 0.f, row_base[k] = (double)p.scores[row];
+      continue;
+    }
+    float m = __uint_as_float(0xff800000u);
+    for (int l = lane; l < p.splits; l += 32) m = fmaxf(m, p.stats[row * p.splits + l].x);
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    double total = 0.0;
+    for (int l = lane; l < p.splits; l += 32) {
+      const float2 s = p.stats[row * p.splits + l];
+      if (s.y != 0.f) total += (double)s.y * exp((double)s.x - (double)m);   // (a segment without a value has a sum of zero)
+      heads[l] = 0;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
+    const bool alive = total > 0.0 && total < INFINITY;   // (not where it is NaN)
+    if (lane == 0) row_max[k] = m, row_base[k] = (double)p.scores[row] - log(total);
+    __syncwarp();
+    const uint64_t* const keys = p.keys + row * p.splits * p.W;
+    // a lane looks after the lists lane, lane + 32, ..; the largest of their first keys is taken, `width` times.  Where it has
+    // one list, the key behind the first one is already here when that is taken.
+    uint64_t here = 0, behind = 0;
+    int from = 0;
+    const bool one = p.splits <= 32;
+    auto key_at = [&](int l, int at) { return at < p.W ? keys[(int64_t)l * p.W + at] : 0; };
+    auto look = [&]() {
+      here = 0;
+      for (int l = lane; l < p.splits; l += 32) {
+        const uint64_t key = key_at(l, heads[l]);
+        if (key > here) here = key, from = l;
+      }
+    };
+    if (one) {
+      if (lane < p.splits) here = key_at(lane, 0), behind = key_at(lane, 1);
+      from = 1;
+    } else {
+      look();
+    }
+    for (int r = 0; r < p.W; ++r) {
+      const uint64_t best = alive ? warp_max(here) : 0;
+      if (lane == 0) rows[k][r] = best;
+      if (best && best == here) {
+        if (one) {
+          here = behind;
+          behind = key_at(lane, ++from);
+        } else {
+          ++heads[from];
+          look();
+        }
+      }
+      __syncwarp();
+    }
+  }
+  __syncthreads();
+  if (warp > 0) return;
+  // lane k looks after beam k; the lower beam first among equal scores
+  int next = 0, n = 0;
+  uint64_t here = 0, key = 0;
+  auto look = [&]() {
+    here = 0;
+    if (lane >= p.K || next >= p.W) return;
+    key = rows[lane][next];
+    if (!key) return;
+    const double score = row_base[lane] + ((double)from_rising((uint32_t)(key >> 32)) - (double)row_max[lane]);
+    const uint64_t u = (uint64_t)__double_as_longlong(score + 0.0);
+    here = u ^ ((uint64_t)((int64_t)u >> 63) | (uint64_t)1 << 63);
+  };
+  auto write = [&](int at, int64_t flat, float score) {
+    const int64_t k = flat / p.V, c = flat % p.V, to = b * p.W + at;
+    p.tokens[to] = c;
+    p.parents[to] = k;
+    p.new_scores[to] = score;
+    if (p.new_ended) p.new_ended[to] = (p.ended && p.ended[b * p.K + k]) || c == p.end;
+    found[at] = flat;
+  };
+  look();
+  for (; n < p.W; ++n) {
+    const uint64_t best = warp_max(here);
+    if (!best) break;
+    if (lane == __ffs(__ballot_sync(0xffffffffu, here == best)) - 1) {
+      const uint64_t u = here & (uint64_t)1 << 63 ? here ^ (uint64_t)1 << 63 : ~here;
+      write(n, (int64_t)lane * p.V + class_of(key), (float)__longlong_as_double((int64_t)u));
+      ++next;
+      look();
+    }
+    __syncwarp();
+  }
+  if (n == p.W || lane > 0) return;
+  // fewer continuations than survivors: all of them are here, and the others, at -infinity, follow in their order
+  for (int64_t flat = 0; n < p.W; ++flat) {
+    bool taken = false;
+    for (int i = 0; i < n; ++i) taken = taken || found[i] == flat;
+    if (!taken) write(n++, flat, __uint_as_float(0xff800000u));
+  }
+}
+
+// ---- rows in the order of their parents ------------------------------------------------------------------------
+struct RowsOf {
+  const uint8_t* from;
+  uint8_t* to;
+  int64_t bytes;                // of a row
+  int64_t tile;                 // number of its first tile
+  int64_t pieces;               // of a row
+  int32_t unit, in_place;       // bytes of an access; from == to
+};
+struct ReorderParams {
+  int count, K, W;
+  int64_t tiles;
+  const int64_t* parents;       // [B][W]
+  RowsOf t[BM_TABLE];
+};
+// A piece of one row.
+template <typename U> __device__ __forceinline__ void copy_piece(const RowsOf& t, const ReorderParams& p, int64_t row, int64_t begin) {
+  const int64_t sample = row / p.W, parent = p.parents[row];
+  const int units = (int)(min((int64_t)BM_PIECE, t.bytes - begin) / sizeof(U));
+  const bool exists = parent >= 0 && parent < p.K;
+  const U* const from = reinterpret_cast<const U*>(t.from + (sample * p.K + (exists ? parent : 0)) * t.bytes + begin);
+  U* const to = reinterpret_cast<U*>(t.to + row * t.bytes + begin);
+#pragma unroll 4
+  for (int i = threadIdx.x; i < units; i += BM_COPY_THREADS) to[i] = exists ? from[i] : U{};
+}
+// A piece of all rows of a sample, through shared memory: all of them are read before one is written.
+template <typename U> __device__ __forceinline__ void exchange_piece(const RowsOf& t, const ReorderParams& p, int64_t sample, int64_t begin, U* held) {
+  const int units = (int)(min((int64_t)BM_PIECE_IN_PLACE, t.bytes - begin) / sizeof(U));
+  uint8_t* const rows = t.to + sample * p.K * t.bytes + begin;
+  for (int k = 0; k < p.K; ++k)
+    for (int i = threadIdx.x; i < units; i += BM_COPY_THREADS) held[k * units + i] = reinterpret_cast<const U*>(rows + k * t.bytes)[i];
+  __syncthreads();
+  for (int w = 0; w < p.W; ++w) {
+    const int64_t k = p.parents[sample * p.W + w];
+    if (k == w) continue;
+    for (int i = threadIdx.x; i < units; i += BM_COPY_THREADS) reinterpret_cast<U*>(rows + w * t.bytes)[i] = k >= 0 && k < p.K ? held[k * units + i] : U{};
+  }
+  __syncthreads();
+}
+template <typename U> __device__ __forceinline__ void reorder_piece(const RowsOf& t, const ReorderParams& p, int64_t tile, void* stage) {
+  if (t.in_place)
+    exchange_piece<U>(t, p, tile / t.pieces, tile % t.pieces * BM_PIECE_IN_PLACE, (U*)stage);
+  else
+    copy_piece<U>(t, p, tile / t.pieces, tile % t.pieces * BM_PIECE);
+}
+__global__ void __launch_bounds__(BM_COPY_THREADS) reorder_rows_kernel(const __grid_constant__ ReorderParams p) {
+  extern __shared__ uint4 stage[];
+  wait_for_kernel_before();
+  for (int64_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+    int low = 0, high = p.count;
+    while (high - low > 1) {
+      const int mid = (low + high) / 2;
+      if (p.t[mid].tile <= tile)
+        low = mid;
+      else
+        high = mid;
+    }
+    const RowsOf& t = p.t[low];
+    if (t.unit == 16)
+      reorder_piece<uint4>(t, p, tile - t.tile, stage);
+    else if (t.unit == 4)
+      reorder_piece<uint32_t>(t, p, tile - t.tile, stage);
+    else
+      reorder_piece<uint8_t>(t, p, tile - t.tile, stage);
+  }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------
+struct Split {
+  bool wide;                   // segments of 16 KB, otherwise 2048 classes
+  int length, splits;
+};
+constexpr int WIDE = 16384 / BM_THREADS, NARROW = 8;   // bytes, values of a thread
+// Parts of four segments of 16 KB where there are rows enough to give every SM several of them, shorter ones for fewer rows: down
+// to one segment of 2048 classes, which are on their way at once in a block of their own.
+Split split_of(int64_t rows, int V, int dtype) {
+  const int64_t classes = (int64_t)BM_THREADS * WIDE / (int)dtype_size(dtype);
+  const int64_t segments = (V + classes - 1) / classes;
+  for (int64_t length = 4; length >= 1; length /= 2)
+    if (rows * ((segments + length - 1) / length) >= 148 * 4) return {true, (int)length, (int)((segments + length - 1) / length)};
+  const int64_t small = BM_THREADS * NARROW;
+  // (no more than 1024 parts, whose lists the joining kernel looks after)
+  const int64_t count = (V + small - 1) / small, length = (count + 1023) / 1024;
+  return {false, (int)length, (int)((count + length - 1) / length)};
+}
+snn_status check(const snn_beam_args* a) {
+  if (!a || a->B < 0 || a->K < 1 || a->W < 1 || a->V < 1 || !dtype_known(a->dtype)) return SNN_ERR_INVALID_ARG;
+  if ((int64_t)a->K * a->V < a->W || a->end < -1 || a->end >= a->V || (a->end < 0 && (a->ended || a->new_ended))) return SNN_ERR_INVALID_ARG;
+  if (a->K > BM_MOST || a->W > BM_MOST || a->V > 1 << 22) return SNN_ERR_UNSUPPORTED;
+  const int64_t rows = (int64_t)a->B * a->K;
+  if (rows * split_of(rows, a->V, a->dtype).splits > INT32_MAX) return SNN_ERR_UNSUPPORTED;
+  return SNN_OK;
+}
+struct Layout {
+  size_t stats, total;
+};
+Layout layout_of(const snn_beam_args* a) {
+  const int64_t rows = (int64_t)a->B * a->K;
+  const size_t lists = (size_t)rows * split_of(rows, a->V, a->dtype).splits;
+  const size_t keys = (lists * a->W * 8 + 255) / 256 * 256;
+  return {keys, keys + (lists * 8 + 255) / 256 * 256};
+}
+snn_status check_rows(const snn_state_rows* t, int32_t count, int32_t K, int32_t W) {
+  if (count < 0 || (count > 0 && !t)) return SNN_ERR_INVALID_ARG;
+  for (int k = 0; k < count; ++k) {
+    if (t[k].row_bytes < 0 || t[k].row_bytes > (int64_t)1 << 50) return SNN_ERR_INVALID_ARG;
+    if (t[k].row_bytes > 0 && (!t[k].from || !t[k].to || (t[k].from == t[k].to && K != W))) return SNN_ERR_INVALID_ARG;
+  }
+  return SNN_OK;
+}
+snn_status reorder(const snn_state_rows* t, int32_t count, const int64_t* parents, int64_t B, int K, int W, cudaStream_t stream, bool behind) {
+  ReorderParams p{};
+  p.K = K, p.W = W, p.parents = parents;
+  for (int k = 0; k < count;) {
+    p.count = 0, p.tiles = 0;
+    bool staged = false;
+    for (; k < count && p.count < BM_TABLE; ++k) {
+      if (t[k].row_bytes == 0) continue;
+      const uintptr_t all = (uintptr_t)t[k].from | (uintptr_t)t[k].to | (uintptr_t)t[k].row_bytes;
+      const bool in_place = t[k].from == t[k].to;
+      staged = staged || in_place;
+      const int64_t piece = in_place ? BM_PIECE_IN_PLACE : BM_PIECE, pieces = (t[k].row_bytes + piece - 1) / piece;
+      p.t[p.count++] = {(const uint8_t*)t[k].from, (uint8_t*)t[k].to, t[k].row_bytes, p.tiles, pieces, all % 16 == 0 ? 16 : all % 4 == 0 ? 4 : 1, in_place};
+      p.tiles += pieces * B * (in_place ? 1 : W);
+    }
+    if (p.tiles == 0) continue;
+    const snn_status st = launch_behind(reorder_rows_kernel, (unsigned)std::min<int64_t>(p.tiles, 148 * 8), BM_COPY_THREADS, staged ? (size_t)K * BM_PIECE_IN_PLACE : 0, stream, behind, p);
+    if (st != SNN_OK) return st;
+    behind = false;
+  }
+  return SNN_OK;
+}
+template <typename IO, int VALUES> snn_status launch_segments(const BeamParams& p, cudaStream_t stream) {
+  constexpr int SMEM = BM_STAGES * Segment<IO, VALUES>::BYTES;
+  if (cudaFuncSetAttribute(beam_rows_kernel<IO, VALUES>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
+  return launch_behind(beam_rows_kernel<IO, VALUES>, (unsigned)(p.rows * p.splits), BM_THREADS, SMEM, stream, false, p);
+}
+template <typename IO> snn_status launch_rows(const BeamParams& p, bool wide, cudaStream_t stream) {
+  return wide ? launch_segments<IO, WIDE / (int)sizeof(IO)>(p, stream) : launch_segments<IO, NARROW>(p, stream);
+}
+}  // namespace
+
+extern "C" snn_status snn_beam_workspace(const snn_beam_args* a, size_t* bytes) {
+  const snn_status st = check(a);
+  if (st != SNN_OK) return st;
+  if (!bytes) return SNN_ERR_INVALID_ARG;
+  *bytes = layout_of(a).total;
+  return SNN_OK;
+}
+
+extern "C" snn_status snn_beam_step(const snn_beam_args* a, void* stream) {
+  snn_status st = check(a);
+  if (st == SNN_OK) st = check_rows(a->states, a->n_states, a->K, a->W);
+  if (st != SNN_OK) return st;
+  if (a->B == 0) return SNN_OK;
+  if (!a->logits || !a->scores || !a->tokens || !a->parents || !a->new_scores || !aligned_to(a->logits, dtype_size(a->dtype))) return SNN_ERR_INVALID_ARG;
+  if (!a->workspace || !aligned_to(a->workspace, 256)) return SNN_ERR_INVALID_ARG;
+  const Layout l = layout_of(a);
+  if (a->workspace_bytes < l.total) return SNN_ERR_WORKSPACE_TOO_SMALL;
+  BeamParams p{};
+  p.rows = (int64_t)a->B * a->K;
+  const Split s = split_of(p.rows, a->V, a->dtype);
+  p.K = a->K, p.W = a->W, p.V = a->V, p.splits = s.splits, p.length = s.length, p.sample_stride = a->sample_stride, p.beam_stride = a->beam_stride, p.end = a->end;
+  p.logits = a->logits, p.scores = a->scores, p.ended = a->ended;
+  p.keys = (uint64_t*)a->workspace, p.stats = (float2*)((char*)a->workspace + l.stats);
+  p.tokens = a->tokens, p.parents = a->parents, p.new_scores = a->new_scores, p.new_ended = a->new_ended;
+  const cudaStream_t on = (cudaStream_t)stream;
+  st = a->dtype == SNN_DTYPE_FP32   ? launch_rows<float>(p, s.wide, on)
+       : a->dtype == SNN_DTYPE_BF16 ? launch_rows<__nv_bfloat16>(p, s.wide, on)
+                                    : launch_rows<__half>(p, s.wide, on);
+  if (st != SNN_OK) return st;
+  const int warps = std::min(a->K, BM_JOIN_WARPS);
+  st = launch_behind(beam_join_kernel, (unsigned)a->B, 32 * warps, (size_t)warps * s.splits, on, true, p);
+  if (st != SNN_OK) return st;
+  return reorder(a->states, a->n_states, a->parents, a->B, a->K, a->W, on, true);
+}
+
+extern "C" snn_status snn_reorder_rows(const snn_state_rows* states, int32_t count, const int64_t* parents, int32_t B, int32_t K, int32_t W, void* stream) {
+  const snn_status st = check_rows(states, count, K, W);
+  if (st != SNN_OK) return st;
+  if (B < 0 || K < 1 || W < 1 || (B > 0 && count > 0 && !parents)) return SNN_ERR_INVALID_ARG;
+  if (K > BM_MOST || W > BM_MOST) return SNN_ERR_UNSUPPORTED;
+  return B == 0 ? SNN_OK : reorder(states, count, parents, B, K, W, (cudaStream_t)stream, false);
+}

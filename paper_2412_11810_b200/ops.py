@@ -6,6 +6,11 @@
     packed = pack_activation(x, "int8"); x = unpack_activation(packed)
     loss, row_loss, lse = vocab_loss(x, w_out, targets)         # soft-max cross entropy of x w_out, logits never stored
     dx, dw = vocab_loss_backward(x, w_out, targets, lse)
+    y, h, rstd, kept = rms_norm(x, weight, residual, keep="int8")   # the norm in front of a layer, with the residual's addition
+    dx, dweight = rms_norm_backward(h, rstd, dy, weight, dh)
+    state = adamw_state(params, bits=8); norm = adamw_step(params, grads, state, lr=1e-3, max_norm=1.0)
+    tokens, parents, scores, ended, states = beam_step(logits, scores, states=states)   # beam search, [B][K][V]
+    states = reorder_states(states, parents)
 
 Gradients are explicit, as in the training step: nothing is recorded for autograd.  Work is launched on the current torch
 stream of the tensors' device and the calls return without waiting; they can be captured into a CUDA graph.  Arguments
@@ -15,7 +20,7 @@ from __future__ import annotations
 
 import contextlib
 from dataclasses import dataclass
-from typing import Optional, Tuple
+from typing import List, Optional, Sequence, Tuple
 
 import torch
 
@@ -102,6 +107,21 @@ def _empty_codes(like: torch.Tensor, shape) -> Tuple[torch.Tensor, torch.Tensor]
             like.new_empty((*shape[:-1], -(-shape[-1] // KEEP_GROUP)), dtype=torch.uint8))
 
 
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """The distance of the rows of a tensor [..., N] whose leading dimensions are taken as one."""
+    n = t.shape[-1]
+    if t.is_contiguous():
+        return n
+    count = t.numel()
+    try:
+        rows = t.view(-1, n) if count else t
+    except RuntimeError:
+        raise ValueError(f"{name}: the leading dimensions have to collapse into one without a copy") from None
+    if count and n > 1 and rows.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension has to be contiguous")
+    return rows.stride(0)
+
+
 def pack_activation(x: torch.Tensor, format: str = "int8") -> PackedActivation:
     """Encodes a tensor [..., N] to 8 bits ("int8" or "e4m3").  The leading dimensions have to collapse into one without a
     copy, the last one has to be contiguous."""
@@ -113,15 +133,7 @@ def pack_activation(x: torch.Tensor, format: str = "int8") -> PackedActivation:
         raise ValueError("x: at least one dimension is required, the last one at most 2^31 - 64")
     _choice(format, "format", _FORMATS)
     n, count = x.shape[-1], x.numel()
-    stride = n
-    if not x.is_contiguous():
-        try:
-            rows = x.view(-1, n) if count else x
-        except RuntimeError:
-            raise ValueError("x: the leading dimensions have to collapse into one without a copy") from None
-        if count and n > 1 and rows.stride(-1) != 1:
-            raise ValueError("x: the last dimension has to be contiguous")
-        stride = rows.stride(0)
+    stride = _row_stride(x, "x")
     with _on(x):
         codes, scales = _empty_codes(x, x.shape)
         if count:
@@ -391,3 +403,357 @@ def vocab_loss_backward(x: torch.Tensor, w_out: torch.Tensor, targets: torch.Ten
         ws = _loss_workspace(a, True, x)  # noqa: F841
         sb.snn_vocab_loss_backward(a, _stream(x))
     return dx, dw
+
+
+# ---- root-mean-square norm with the residual's addition --------------------------------------------------------
+def _rows(t: torch.Tensor, name: str) -> None:
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise ValueError(f"{name}: a CUDA tensor is required")
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"{name}: dtype {t.dtype} is not fp32, bf16 or fp16")
+    if t.dim() < 1 or not 1 <= t.shape[-1] <= _WIDEST:
+        raise ValueError(f"{name}: at least one dimension is required, the last one from 1 to 2^31 - 64")
+
+
+def _rows_like(t: torch.Tensor, name: str, like: torch.Tensor) -> int:
+    """Checks a tensor of the shape and type of another, and returns the distance of its rows."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != like.get_device():
+        raise ValueError(f"{name}: a tensor on {like.device} is required")
+    if t.dtype is not like.dtype:
+        raise ValueError(f"{name}: dtype {t.dtype} instead of {like.dtype}")
+    if t.shape != like.shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} instead of {tuple(like.shape)}")
+    return _row_stride(t, name)
+
+
+def _norm_weight(weight: Optional[torch.Tensor], like: torch.Tensor) -> int:
+    """Checks a norm's weight and returns its type's number."""
+    if weight is None:
+        return _DTYPES[like.dtype]
+    if not isinstance(weight, torch.Tensor) or weight.get_device() != like.get_device():
+        raise ValueError(f"weight: a tensor on {like.device} is required")
+    if weight.dtype is not like.dtype and weight.dtype is not torch.float32:
+        raise ValueError(f"weight: dtype {weight.dtype} is neither {like.dtype} nor fp32")
+    if weight.shape != like.shape[-1:]:
+        raise ValueError(f"weight: shape {tuple(weight.shape)} instead of {tuple(like.shape[-1:])}")
+    if not weight.is_contiguous():
+        raise ValueError("weight: has to be contiguous")
+    return _DTYPES[weight.dtype]
+
+
+def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
+             keep: Optional[str] = None, values: bool = True, inplace: bool = False):
+    """Root-mean-square norm of the rows of a tensor [..., N], after the residual has been added to it:
+
+        h = x + residual (in their type),  rstd = 1 / sqrt(mean(h^2) + eps),  y = h rstd weight
+
+    x, residual: fp32, bf16 or fp16, leading dimensions that collapse into one without a copy; weight: [N], of their type or
+    fp32 (ones if None).  keep: "int8" or "e4m3" for a copy of y in 8 bits, made in the same pass from the values before they
+    are rounded to the type; values=False leaves y itself out.  inplace: h replaces the residual in its memory.
+    eps: from 1e-30 to 1.  Rows of any finite values are normed, also where their squares leave fp32.
+    Returns (y or None, h, rstd fp32 [...], PackedActivation or None); h is x itself where there is no residual."""
+    _rows(x, "x")
+    shape, n = x.shape, x.shape[-1]
+    weight_dtype = _norm_weight(weight, x)
+    if keep is not None:
+        _choice(keep, "keep", _FORMATS)
+    elif not values:
+        raise ValueError("values: without them, keep is required")
+    if not 1e-30 <= eps <= 1.0:
+        raise ValueError("eps: has to be from 1e-30 to 1")
+    count = x.numel()
+    a = sb.snn_rms_norm_args(count // n, n, _DTYPES[x.dtype], weight_dtype, eps, x.data_ptr(), _row_stride(x, "x"))
+    if residual is not None:
+        a.residual, a.residual_stride = residual.data_ptr() if isinstance(residual, torch.Tensor) else None, _rows_like(residual, "residual", x)
+    elif inplace:
+        raise ValueError("inplace: needs a residual")
+    a.weight = _ptr(weight)
+    with _on(x):
+        h = x
+        if residual is not None:
+            if inplace:
+                h, a.h_stride = residual, a.residual_stride
+                if a.rows > 1 and a.h_stride < n:
+                    raise ValueError("residual: rows overlap")
+            else:
+                h, a.h_stride = _dense(x), n
+            a.h = h.data_ptr()
+        rstd = x.new_empty(shape[:-1], dtype=torch.float32)
+        a.rstd = rstd.data_ptr()
+        y = kept = None
+        if values:
+            y = _dense(x)
+            a.y, a.y_stride = y.data_ptr(), n
+        if keep is not None:
+            codes, scales = _empty_codes(x, shape)
+            kept = PackedActivation(codes, scales, keep, x.dtype)
+            a.keep_format, a.codes, a.scales = _FORMATS[keep], codes.data_ptr(), scales.data_ptr()
+        if count:
+            sb.snn_rms_norm_forward(a, _stream(x))
+    return y, h, rstd, kept
+
+
+def rms_norm_backward(h: torch.Tensor, rstd: torch.Tensor, dy: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                      dh: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Gradients of a loss from those by y (dy) and by h (dh, what the residual stream hands back; zero if None), with h and
+    rstd as `rms_norm` returned them.  Where y was kept in 8 bits, they are those of the values before.
+    Returns (dx, the gradient by x and by the residual alike, of their type; dweight, of weight's type, None without one).
+    Workspace: 4 N bytes per thread block, of which there are at most 592, and no more than rows."""
+    _rows(h, "h")
+    n = h.shape[-1]
+    weight_dtype = _norm_weight(weight, h)
+    _like(rstd, "rstd", h, h.shape[:-1], torch.float32)
+    a = sb.snn_rms_norm_args(h.numel() // n, n, _DTYPES[h.dtype], weight_dtype)
+    a.h, a.h_stride, a.weight, a.rstd = h.data_ptr(), _row_stride(h, "h"), _ptr(weight), rstd.data_ptr()
+    a.dy_stride, a.dy = _rows_like(dy, "dy", h), dy.data_ptr()
+    if dh is not None:
+        a.dh_stride, a.dh = _rows_like(dh, "dh", h), dh.data_ptr()
+    with _on(h):
+        dx = _dense(h)
+        a.dx, a.dx_stride = dx.data_ptr(), n
+        dweight = None
+        if weight is not None:
+            dweight = torch.empty_like(weight)
+            a.dweight = dweight.data_ptr()
+            ws = h.new_empty(sb.snn_rms_norm_workspace(a), dtype=torch.uint8)
+            a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+        sb.snn_rms_norm_backward(a, _stream(h))
+    return dx, dweight
+
+
+# ---- AdamW over many tensors -----------------------------------------------------------------------------------
+@dataclass(frozen=True)
+class AdamWState:
+    """The moments of a list of tensors, one behind the other, each tensor's from a multiple of 64 values on, and the number of
+    steps done: m and v fp32, or in 8 bits (e4m3), where v holds square roots."""
+    m: object                      # torch.Tensor or PackedActivation
+    v: object
+    step: torch.Tensor             # int64, 0-d, on the device
+
+
+def _moments(sizes) -> int:
+    return sum(-(-n // KEEP_GROUP) * KEEP_GROUP for n in sizes)
+
+
+def adamw_state(params: Sequence[torch.Tensor], bits: int = 32) -> AdamWState:
+    """The state that `adamw_step` starts from: moments of zero in 32 or 8 bits (8 or 2 1/32 bytes per parameter)."""
+    if bits not in (32, 8):
+        raise ValueError(f"bits: {bits!r} is neither 32 nor 8")
+    if len(params) == 0:
+        raise ValueError("params: at least one tensor is required")
+    for k, p in enumerate(params):
+        if not (isinstance(p, torch.Tensor) and p.is_cuda):
+            raise ValueError(f"params[{k}]: a CUDA tensor is required")
+    n, like = _moments(p.numel() for p in params), params[0]
+    step = like.new_zeros((), dtype=torch.int64)
+    if bits == 32:
+        return AdamWState(like.new_zeros(n, dtype=torch.float32), like.new_zeros(n, dtype=torch.float32), step)
+    m, v = (PackedActivation(like.new_zeros(n, dtype=torch.uint8), like.new_zeros(n // KEEP_GROUP, dtype=torch.uint8), "e4m3", torch.float32)
+            for _ in range(2))
+    return AdamWState(m, v, step)
+
+
+def _scalar_on(t: torch.Tensor, name: str, like: torch.Tensor, dtype) -> None:
+    _like(t, name, like, (), dtype)
+
+
+def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], state: AdamWState, *, lr, betas: Tuple[float, float] = (0.9, 0.999),
+               eps: float = 1e-8, weight_decay: float = 0.01, max_norm: Optional[float] = None, scale=1.0, seed: int = 0,
+               copies: Optional[Sequence[Optional[torch.Tensor]]] = None) -> Optional[torch.Tensor]:
+    """One AdamW step over all tensors in `params`, in place, with the step's number t counted in `state`:
+
+        g = scale grad, times max_norm / norm where the norm of all gradients together is above max_norm
+        m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
+        p = p (1 - lr weight_decay) - lr m / (1 - b1^t) / (sqrt(v / (1 - b2^t)) + eps)
+
+    params, grads: contiguous tensors of fp32, bf16 or fp16, in any mixture; no two of them may overlap.  copies: tensors of
+    the parameters' shapes (or None) that receive the new parameters in their own type, as 16-bit copies of fp32 ones; a 16-bit
+    parameter whose change is less than half a step stays as it is.
+    lr and scale: numbers, or fp32 0-d tensors on the device, so that a captured step follows a schedule.
+    max_norm: None computes no norm; otherwise a step whose norm is not finite is left out and not counted.
+    Moments in 8 bits are rounded at random, by a hash of seed, t and place: give every list of tensors a seed of its own.
+    eps: from 1e-30 to 1.  Returns the norm before the clip (fp32, 0-d), or None without max_norm."""
+    if not isinstance(state, AdamWState):
+        raise ValueError("state: what adamw_state returned is required")
+    count = len(params)
+    if len(grads) != count or (copies is not None and len(copies) != count):
+        raise ValueError("grads, copies: as many as params are required")
+    like = state.step
+    device = like.get_device() if isinstance(like, torch.Tensor) else -1
+    if device < 0:
+        raise ValueError("state.step: a CUDA tensor is required")
+    table, dtypes, room = (sb.snn_adamw_tensor * count)(), _DTYPES, 0
+    written = set()
+    for k in range(count):
+        p, g = params[k], grads[k]
+        n = p.numel() if isinstance(p, torch.Tensor) else 0
+        if not isinstance(p, torch.Tensor) or p.get_device() != device or p.dtype not in dtypes or not p.is_contiguous():
+            raise ValueError(f"params[{k}]: a contiguous tensor of fp32, bf16 or fp16 on {like.device} is required")
+        if not isinstance(g, torch.Tensor) or g.get_device() != device or g.dtype not in dtypes or not g.is_contiguous():
+            raise ValueError(f"grads[{k}]: a contiguous tensor of fp32, bf16 or fp16 on {like.device} is required")
+        if g.shape != p.shape:
+            raise ValueError(f"grads[{k}]: shape {tuple(g.shape)} instead of {tuple(p.shape)}")
+        room += n + -n % KEEP_GROUP
+        if n == 0:
+            continue
+        e = table[k]
+        at = p.data_ptr()
+        e.param, e.grad, e.n, e.param_dtype, e.grad_dtype = at, g.data_ptr(), n, dtypes[p.dtype], dtypes[g.dtype]
+        if at in written:
+            raise ValueError(f"params[{k}]: given twice")
+        written.add(at)
+        c = None if copies is None else copies[k]
+        if c is not None:
+            if not isinstance(c, torch.Tensor) or c.get_device() != device or c.dtype not in dtypes or not c.is_contiguous() or c.shape != p.shape:
+                raise ValueError(f"copies[{k}]: a contiguous tensor of fp32, bf16 or fp16 and of the parameter's shape is required")
+            at = c.data_ptr()
+            if at in written:
+                raise ValueError(f"copies[{k}]: given twice")
+            written.add(at)
+            e.copy, e.copy_dtype = at, dtypes[c.dtype]
+    if like.dtype is not torch.int64 or like.dim() != 0:
+        raise ValueError("state.step: an int64 0-d tensor is required")
+    a = sb.snn_adamw_args()
+    a.count, a.tensors, a.step = count, table, like.data_ptr()
+    if isinstance(state.m, PackedActivation):
+        a.moment_format = sb.SNN_KEEP_E4M3
+        for name in ("m", "v"):
+            t = getattr(state, name)
+            if not isinstance(t, PackedActivation) or t.format != "e4m3":
+                raise ValueError(f"state.{name}: not in e4m3, as the other moment is")
+            _like(t.codes, f"state.{name}", like, (room,), torch.uint8)
+            _like(t.scales, f"state.{name}", like, (room // KEEP_GROUP,), torch.uint8)
+            setattr(a, name + "_codes", t.codes.data_ptr())
+            setattr(a, name + "_scales", t.scales.data_ptr())
+    else:
+        for name in ("m", "v"):
+            t = getattr(state, name)
+            _like(t, f"state.{name}", like, (room,), torch.float32)
+            setattr(a, name, t.data_ptr())
+    for name, value in (("lr", lr), ("scale", scale)):
+        if isinstance(value, torch.Tensor):
+            _scalar_on(value, name, like, torch.float32)
+            setattr(a, name + "_device", value.data_ptr())
+            value = 1.0
+        elif not abs(value) <= 3e38 or (name == "lr" and value < 0):
+            raise ValueError(f"{name}: has to be finite" + (" and at least zero" if name == "lr" else ""))
+        setattr(a, name, value)
+    if not (0 <= betas[0] < 1 and 0 <= betas[1] < 1):
+        raise ValueError("betas: have to be from 0 to less than 1")
+    if not 1e-30 <= eps <= 1.0:
+        raise ValueError("eps: has to be from 1e-30 to 1")
+    if not 0 <= weight_decay <= 3e38:
+        raise ValueError("weight_decay: has to be finite and at least zero")
+    if max_norm is not None and not max_norm > 0:
+        raise ValueError("max_norm: has to be above zero")
+    if not 0 <= seed < 2 ** 64:
+        raise ValueError("seed: has to fit 64 bits")
+    a.beta1, a.beta2, a.eps, a.weight_decay, a.max_norm, a.seed = *betas, eps, weight_decay, max_norm or 0.0, seed
+    with _on(like):
+        norm = None
+        if max_norm is not None:
+            norm = like.new_empty((), dtype=torch.float32)
+            a.norm = norm.data_ptr()
+        ws = like.new_empty(sb.SNN_ADAMW_WORKSPACE, dtype=torch.uint8)
+        a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+        sb.snn_adamw_step(a, _stream(like))
+    return norm
+
+
+# ---- beam search -----------------------------------------------------------------------------------------------
+MOST_BEAMS = 32
+
+
+def _state_table(states, rows: int, out_rows: int, inplace: bool, device: int):
+    """(table for the library, tensors that receive the rows)."""
+    if isinstance(states, torch.Tensor):
+        raise ValueError("states: a sequence of tensors is required")
+    table, out, seen = (sb.snn_state_rows * len(states))(), [], set()
+    for k, t in enumerate(states):
+        if not isinstance(t, torch.Tensor) or t.get_device() != device or not t.is_contiguous():
+            raise ValueError(f"states[{k}]: a contiguous tensor on the device of the beams is required")
+        if t.dim() < 1 or t.shape[0] != rows:
+            raise ValueError(f"states[{k}]: {rows} rows are required, one for each beam")
+        at, size = t.data_ptr(), t.numel() * t.element_size()
+        if inplace:
+            if size and at in seen:
+                raise ValueError(f"states[{k}]: given twice")
+            seen.add(at)
+            new = t
+        else:
+            new = torch.empty_like(t) if rows == out_rows else t.new_empty((out_rows, *t.shape[1:]))
+        out.append(new)
+        e = table[k]
+        e.source, e.to, e.row_bytes = at, new.data_ptr(), size // rows if rows else 0
+    return table, out
+
+
+def beam_step(logits: torch.Tensor, scores: torch.Tensor, *, width: Optional[int] = None, ended: Optional[torch.Tensor] = None,
+              end: Optional[int] = None, states: Sequence[torch.Tensor] = (), inplace: bool = False):
+    """One step of beam search: the best `width` (K if None) continuations of the K beams of each sample, by
+
+        score(k, c) = scores[b, k] + log_softmax(logits[b, k])[c]
+
+    logits: [B][K][V], fp32, bf16 or fp16, with contiguous classes; scores: fp32 [B][K] (a first step from one beam has K = 1).
+    Scores are ranked in 64 bits, classes of one beam by their logits; ties go to the lower beam, then to the lower class.
+    end: the class that ends a beam; ended: bool [B][K], the beams that have: they go on with `end` alone, at their score.
+    Continuations at -infinity come last, in the order of k V + c: classes masked by logits of -infinity, and all of a
+    beam whose score is not finite, or whose logits are all masked or hold a NaN or +infinity.
+    states: tensors whose rows [B K, ...] belong to the beams (what gated_scan_step carries, tokens so far): they come back
+    as rows [B width, ...] of the beams' parents, with inplace in their own memory (width = K).
+    K and width are at most 32, V at most 2^22.  Returns (tokens int64 [B][width], parents int64 [B][width], the beam of each,
+    scores fp32 [B][width], ended bool [B][width] or None without end, list of states)."""
+    _values(logits, "logits", 3)
+    B, K, V = logits.shape
+    width = K if width is None else width
+    if not (1 <= K <= MOST_BEAMS and 1 <= width <= MOST_BEAMS):
+        raise ValueError(f"logits, width: from 1 to {MOST_BEAMS} beams are required")
+    if not 1 <= V <= 1 << 22 or B * K > 1 << 24:
+        raise ValueError("logits: from 1 to 2^22 classes and at most 2^24 beams are required")
+    if width > K * V:
+        raise ValueError("width: more than there are continuations")
+    _like(scores, "scores", logits, (B, K), torch.float32)
+    if end is None:
+        if ended is not None:
+            raise ValueError("ended: needs end")
+    elif not 0 <= end < V:
+        raise ValueError("end: is not a class")
+    if ended is not None:
+        _like(ended, "ended", logits, (B, K), torch.bool)
+    if inplace and width != K:
+        raise ValueError("inplace: needs as many survivors as beams")
+    with _on(logits):
+        table, out = _state_table(states, B * K, B * width, inplace, logits.get_device())
+        tokens = logits.new_empty((2, B, width), dtype=torch.int64)
+        tokens, parents = tokens[0], tokens[1]
+        new_scores = logits.new_empty((B, width), dtype=torch.float32)
+        new_ended = None if end is None else logits.new_empty((B, width), dtype=torch.bool)
+        a = sb.snn_beam_args(B, K, width, V, _DTYPES[logits.dtype], logits.data_ptr(), logits.stride(0), logits.stride(1), scores.data_ptr(),
+                             _ptr(ended), -1 if end is None else end, tokens.data_ptr(), parents.data_ptr(), new_scores.data_ptr(),
+                             _ptr(new_ended), table, len(out))
+        if B:
+            ws = logits.new_empty(sb.snn_beam_workspace(a), dtype=torch.uint8)
+            a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+            sb.snn_beam_step(a, _stream(logits))
+    return tokens, parents, new_scores, new_ended, out
+
+
+def reorder_states(states: Sequence[torch.Tensor], parents: torch.Tensor, *, beams: Optional[int] = None, inplace: bool = False) -> List[torch.Tensor]:
+    """Rows [B K, ...] of tensors of any type in the order of their parents, int64 [B][W]: row b W + w of a result is row
+    b K + parents[b, w]; a parent outside [0, K) leaves zeros.  beams: K, where it is not W.  inplace: in the tensors' own
+    memory (K = W); rows that stay where they are are not written.  K and W are at most 32."""
+    if not (isinstance(parents, torch.Tensor) and parents.is_cuda and parents.dtype is torch.int64 and parents.dim() == 2 and parents.is_contiguous()):
+        raise ValueError("parents: a contiguous int64 CUDA tensor of two dimensions is required")
+    B, W = parents.shape
+    K = W if beams is None else beams
+    if not (1 <= K <= MOST_BEAMS and 1 <= W <= MOST_BEAMS):
+        raise ValueError(f"parents, beams: from 1 to {MOST_BEAMS} beams are required")
+    if B > 1 << 24:
+        raise ValueError("parents: too many samples")
+    if inplace and K != W:
+        raise ValueError("inplace: needs as many survivors as beams")
+    with _on(parents):
+        table, out = _state_table(states, B * K, B * W, inplace, parents.get_device())
+        if B and out:
+            sb.snn_reorder_rows(table, len(out), parents.data_ptr(), B, K, W, _stream(parents))
+    return out

@@ -12,6 +12,7 @@ import numpy as np
 import torch
 
 from . import binding as sb
+from . import ops
 
 
 class Session:
@@ -36,6 +37,7 @@ class Session:
         self.dW_out: Optional[torch.Tensor] = None
         self.device_ws: Optional[torch.Tensor] = None
         self.pinned_ws: Optional[torch.Tensor] = None
+        self.adamw: Optional[ops.AdamWState] = None
         self.debug_V: Optional[List[torch.Tensor]] = None
         self._last = None
 
@@ -64,6 +66,7 @@ class Session:
         self.dW_ff = [torch.empty_like(w) for w in self.W_ff]
         self.dW_rec = [torch.empty_like(w) for w in self.W_rec]
         self.dW_out = torch.empty_like(self.W_out)
+        self.adamw = None
 
     def ckpt(self, strategy: int, chunk_size: int = 0, remote_chunk_size: int = 0, nb_local: int = 0) -> sb.snn_ckpt:
         return sb.snn_ckpt(strategy, chunk_size, remote_chunk_size, nb_local)
@@ -122,6 +125,20 @@ class Session:
         self._last = (T, B, input_bits, targets)   # keep inputs alive until the call returns
         torch.cuda.current_stream(self.device).synchronize()
         return sb.snn_train_step(self.net, a)
+
+    # ---- the update --------------------------------------------------------------------------
+    def parameters(self) -> List[torch.Tensor]:
+        return [*self.W_ff, *self.W_rec, self.W_out]
+
+    def parameter_gradients(self) -> List[torch.Tensor]:
+        return [*self.dW_ff, *self.dW_rec, self.dW_out]
+
+    def adamw_step(self, lr, bits: int = 32, **kw) -> Optional[torch.Tensor]:
+        """One AdamW step on all weights with the gradients of the last train step, on the current stream; `bits` (32 or 8)
+        are those of the moments, chosen by the first step, and the other arguments those of `ops.adamw_step`."""
+        if self.adamw is None:
+            self.adamw = ops.adamw_state(self.parameters(), bits)
+        return ops.adamw_step(self.parameters(), self.parameter_gradients(), self.adamw, lr=lr, **kw)
 
     # ---- inspection ------------------------------------------------------------------------
     def gradients(self):

@@ -6,7 +6,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = [os.path.join(CSRC, f) for f in ("snn_api.cu", "schedule.cpp", "scan.cu", "activation.cu", "vocab_loss.cu", "rms_norm.cu", "adamw.cu", "beam.cu")]
-HEADERS = [os.path.join(CSRC, f) for f in ("kernels.cuh", "tma.cuh", "tc_gemm.cuh", "seq_common.cuh", "umma.cuh", "octet.cuh")] + [os.path.join(HERE, "..", "include", "snn.h")]
+HEADERS = [os.path.join(CSRC, f) for f in ("kernels.cuh", "tma.cuh", "tc_gemm.cuh", "seq_common.cuh", "umma.cuh", "unit.cuh")] + [os.path.join(HERE, "..", "include", "snn.h")]
 LIB = os.path.join(HERE, "libsnnckpt.so")
 LIB_DEBUG = os.path.join(HERE, "libsnnckpt_debug.so")   # the same sources with -DSNN_DEBUG_CHECKS=1 (bounds-checked)
 # -fmad=false: nothing is fused unless the source says fmaf; the forward arithmetic that decides

@@ -12,7 +12,7 @@
 // Keys hold the value above the complement of the class, so that no two are the same and ties go to the lower class.
 #include <algorithm>
 
-#include "octet.cuh"
+#include "unit.cuh"
 
 using namespace snnk;
 

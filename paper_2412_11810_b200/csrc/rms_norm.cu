@@ -3,25 +3,24 @@
 //   h = x + residual, rounded to the type;  s = 1 / sqrt(mean(h^2) + eps);  y = h s w
 //   with g = dy w, c = mean(g h s):  dx = s (g - h s c) + dh,  dw = sum over the rows of dy h s
 //
-// Bound by HBM: every value is read and written once.  A row belongs to `lanes` threads (8, 16, 32, or whole warps) that hold
-// one or two octets each in registers, so that the second use of h costs no second read.  Up to 32 lanes a warp handles whole
-// rows and nothing waits for a block.  Rows that do not fit (16384 columns forward, 8192 backward, where dy, dh and the sums
-// for dw are held as well) are read a second time, from L2.
+// Bound by HBM: every value is read and written once.  A row belongs to `lanes` threads (part of a warp, or whole warps) that
+// hold one or two units each (unit.cuh) in registers, so that the second use of h costs no second read.  Within a warp nothing
+// waits for a block.  Rows that do not fit are read a second time, from L2.
 #include <algorithm>
 #include <type_traits>
 
-#include "octet.cuh"
+#include "unit.cuh"
 
 using namespace snnk;
 
 namespace {
 
 constexpr int RMS_THREADS = 256;      // of a block whose rows need no more than a warp
-constexpr int RMS_MOST_LANES = 1024, RMS_MOST_LANES_BACK = 512;
+constexpr int RMS_MOST_LANES = 512, RMS_WIDE = 1024;   // threads of a row; of one that does not fit registers
 
 struct RmsParams {
   int64_t rows;
-  int n, lanes, keep_format;
+  int n, groups, lanes, keep_format;
   float eps, inverse_n;
   const void *x, *residual, *weight, *dy, *dh;
   int64_t x_stride, residual_stride, h_stride, y_stride, dy_stride, dh_stride, dx_stride;
@@ -33,15 +32,17 @@ struct RmsParams {
 
 // The sum over the lanes of a row, the same bits for all of them.  `turn` counts the calls: two buffers take turns, so that
 // one barrier a call is enough.
-__device__ __forceinline__ float row_sum(float v, int lanes, int turn, float (*shared)[32]) {
-  for (int o = 1; o < min(lanes, 32); o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if (lanes <= 32) return v;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (lane == 0) shared[turn & 1][warp] = v;
-  __syncthreads();
-  v = lane < lanes / 32 ? shared[turn & 1][lane] : 0.f;
+template <bool BLOCK> __device__ __forceinline__ float row_sum(float v, int lanes, int turn, float (*shared)[32]) {
+  if (!BLOCK) {
+    for (int o = 1; o < lanes; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  }
 #pragma unroll
   for (int o = 1; o < 32; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if ((threadIdx.x & 31) == 0) shared[turn & 1][threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = shared[turn & 1][0];
+  for (int k = 1; k < lanes / 32; ++k) v += shared[turn & 1][k];
   return v;
 }
 __device__ __forceinline__ float scale_of(float sum, const RmsParams& p) { return rsqrtf(sum * p.inverse_n + p.eps); }
@@ -50,233 +51,286 @@ __device__ __forceinline__ float scale_of(float sum, const RmsParams& p) { retur
 constexpr float RMS_DOWN = 0x1p-80f;
 __device__ __forceinline__ float scale_of_far(float sum, const RmsParams& p) { return rsqrtf(sum * p.inverse_n) * RMS_DOWN; }
 
-// The 8-bit codes of an octet y of the group at column c0 of a row.
-template <int FORMAT, bool FAST>
-__device__ __forceinline__ void keep_octet(const float2 y[4], int64_t row, int c0, int s, const RmsParams& p, bool store) {
+// Which row of a turn of its block a thread works at, which of the row's threads it is, and its columns.
+template <bool BLOCK, int N, bool FAST> struct Place {
+  static constexpr int LANES = KEEP_GROUP / N;
+  int slot, t, s, lanes, n;
+  __device__ __forceinline__ explicit Place(const RmsParams& p) : lanes(p.lanes), n(p.n) {
+    slot = BLOCK ? 0 : threadIdx.x / p.lanes;
+    t = BLOCK ? threadIdx.x : threadIdx.x % p.lanes;
+    s = t % LANES;
+  }
+  __device__ __forceinline__ int per_block() const { return BLOCK ? 1 : RMS_THREADS / lanes; }
+  // the first column of the thread's i-th unit, and how many columns are left from there on
+  __device__ __forceinline__ int column(int i) const { return (t / LANES) * KEEP_GROUP + i * lanes * N + unit_first<N, FAST>(s); }
+  __device__ __forceinline__ int left(int i) const { return n - column(i); }
+};
+template <int FORMAT, bool FAST, int N>
+__device__ __forceinline__ void keep_unit(const float2 y[N / 2], int64_t row, int column, int left, int s, const RmsParams& p, bool store) {
   float m = 0.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m = larger_magnitude(m, larger_magnitude(y[i].x, y[i].y));
-  const uint32_t top = group_top(m), byte = keep_scale_byte<FORMAT>(top);
+  for (int i = 0; i < N / 2; ++i) m = larger_of(m, y[i]);
+  const uint32_t top = group_top<KEEP_GROUP / N>(m), byte = keep_scale_byte<FORMAT>(top);
   const float inverse = keep_scale_inverse(byte);
-  const bool cut = __any_sync(0xffffffffu, keep_needs_cut<FORMAT>(top));
-  uint32_t q[4];
+  // (rarely: a group whose largest value could round up to 128, or one that is not finite)
+  const bool rare = __any_sync(0xffffffffu, byte == 255u || keep_needs_cut<FORMAT>(top));
+  uint32_t q[N / 4];
+  encode_unit<FORMAT, N>(q, y, inverse, rare);
+  if (rare && byte == 255u) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) q[i] = byte == 255u ? 0u : keep_encode2<FORMAT>(y[i], inverse, cut);
+    for (int i = 0; i < N / 4; ++i) q[i] = 0u;
+  }
   if (!store) return;
-  store_codes<FAST>(p.codes + row * p.n, c0, s, p.n, q);
-  if (s == 0 && c0 < p.n) p.scales[row * ((p.n + KEEP_GROUP - 1) / KEEP_GROUP) + c0 / KEEP_GROUP] = (uint8_t)byte;
+  store_codes<FAST, N>(p.codes + row * p.n + column, q, left);
+  if (s == 0 && left > 0) p.scales[row * p.groups + column / KEEP_GROUP] = (uint8_t)byte;
 }
-
-// y of one octet of h, as values, as codes, or both.
-template <typename IO, typename WT, bool FAST>
-__device__ __forceinline__ void finish_octet(const Octet<IO, FAST>& h, float scale, int64_t row, int c0, int s, const RmsParams& p, bool store) {
-  float2 y[4];
+// y of one unit of h, as values, as codes, or both.
+template <typename IO, typename WT, bool FAST, int N>
+__device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT, N>& w, float scale, int64_t row, int column, int left, int s, const RmsParams& p,
+                                            bool store) {
+  float2 y[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) y[i] = mul_pair(h.pair(i), both(scale));
   if (p.weight) {
-    Octet<WT, FAST> w;
-    w.load((const WT*)p.weight, c0, s, p.n);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = mul2(mul2(h.pair(i), both(scale)), w.pair(i));
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = mul2(h.pair(i), both(scale));
+    for (int i = 0; i < N / 2; ++i) y[i] = mul_pair(y[i], w.pair(i));
   }
-  if (p.y) {
-    Octet<IO, FAST> out;
+  if (p.y && store) {
+    Unit<IO, N> out;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out.set(i, y[i]);
-    if (store) out.store((IO*)p.y + row * p.y_stride, c0, s, p.n);
+    for (int i = 0; i < N / 2; ++i) out.set(i, y[i]);
+    store_unit<FAST>(out, (IO*)p.y + row * p.y_stride + column, left);
   }
-  if (p.keep_format == SNN_KEEP_INT8) keep_octet<SNN_KEEP_INT8, FAST>(y, row, c0, s, p, store);
-  if (p.keep_format == SNN_KEEP_E4M3) keep_octet<SNN_KEEP_E4M3, FAST>(y, row, c0, s, p, store);
+  if (p.keep_format == SNN_KEEP_INT8) keep_unit<SNN_KEEP_INT8, FAST, N>(y, row, column, left, s, p, store);
+  if (p.keep_format == SNN_KEEP_E4M3) keep_unit<SNN_KEEP_E4M3, FAST, N>(y, row, column, left, s, p, store);
 }
-// An octet of h: that of x, or its sum with the residual's, which is stored.
-template <typename IO, bool FAST>
-__device__ __forceinline__ void sum_octet(Octet<IO, FAST>& h, const Octet<IO, FAST>& r, int64_t row, int c0, int s, const RmsParams& p, bool store) {
-  if (!p.residual) return;
+// A unit of h: that of x, or its sum with the residual's; and its squares.
+template <typename IO, int N> __device__ __forceinline__ void sum_unit(Unit<IO, N>& h, const Unit<IO, N>& r, bool residual, float2& sum) {
+  if (residual) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) h.set(i, add2(h.pair(i), r.pair(i)));
-  if (store) h.store((IO*)p.h + row * p.h_stride, c0, s, p.n);
+    for (int i = 0; i < N / 2; ++i) h.set(i, add_pair(h.pair(i), r.pair(i)));
+  }
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) sum = fma_pair(h.pair(i), h.pair(i), sum);
+}
+template <typename IO, int N> __device__ __forceinline__ void sum_unit_far(const Unit<IO, N>& h, float2& sum) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    const float2 v = mul_pair(h.pair(i), both(RMS_DOWN));
+    sum = fma_pair(v, v, sum);
+  }
 }
 
-template <typename IO, typename WT, bool FAST, int OCTETS>
-__global__ void __launch_bounds__(RMS_MOST_LANES) rms_forward_kernel(const RmsParams p) {
+// BLOCK: a row per block and turn; otherwise a warp holds whole rows.  The loads of the next row are on their way while a row
+// is finished; the weight stays in registers.
+template <typename IO, typename WT, bool FAST, int UNITS, bool BLOCK>
+__global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK && FAST && UNITS == 1 ? 2 : 1) rms_forward_kernel(const RmsParams p) {
+  constexpr int N = UNIT<IO>;
   __shared__ float shared[2][32];
-  const int slot = threadIdx.x / p.lanes, t = threadIdx.x % p.lanes, s = t & 7, per_block = blockDim.x / p.lanes;
+  const Place<BLOCK, N, FAST> at(p);
+  const int64_t step = (int64_t)gridDim.x * at.per_block();
+  const bool residual = p.residual != nullptr;
   int turn = 0;
-  for (int64_t base = (int64_t)blockIdx.x * per_block; base < p.rows; base += (int64_t)gridDim.x * per_block) {
-    const bool store = base + slot < p.rows;   // (a slot without a row repeats the last one and stores nothing)
-    const int64_t row = min(base + slot, p.rows - 1);
-    Octet<IO, FAST> h[OCTETS], r[OCTETS];
+  Unit<WT, N> w[UNITS];
+  Unit<IO, N> x[UNITS], r[UNITS];
 #pragma unroll
-    for (int o = 0; o < OCTETS; ++o) h[o].load((const IO*)p.x + row * p.x_stride, (t / 8 + o * (p.lanes / 8)) * KEEP_GROUP, s, p.n);
-    if (p.residual) {
+  for (int i = 0; i < UNITS; ++i) {
+    x[i].zero(), r[i].zero();   // (and stay so behind the row's end)
+    if (!p.weight) continue;
+    w[i].zero();
+    load_unit<FAST>(w[i], (const WT*)p.weight + at.column(i), at.left(i));
+  }
+  auto load = [&](int64_t row) {
+    const IO* const from = (const IO*)p.x + row * p.x_stride;
 #pragma unroll
-      for (int o = 0; o < OCTETS; ++o) r[o].load((const IO*)p.residual + row * p.residual_stride, (t / 8 + o * (p.lanes / 8)) * KEEP_GROUP, s, p.n);
-    }
+    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(x[i], from + at.column(i), at.left(i));
+    if (!residual) return;
+    const IO* const other = (const IO*)p.residual + row * p.residual_stride;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(r[i], other + at.column(i), at.left(i));
+  };
+  const int64_t first = (int64_t)blockIdx.x * at.per_block();
+  if (first < p.rows) load(min(first + at.slot, p.rows - 1));
+  for (int64_t base = first; base < p.rows; base += step) {
+    const bool store = base + at.slot < p.rows;   // (a slot without a row repeats the last one and stores nothing)
+    const int64_t row = min(base + at.slot, p.rows - 1);
+    Unit<IO, N> h[UNITS];
     float2 sum = both(0.f);
 #pragma unroll
-    for (int o = 0; o < OCTETS; ++o) {
-      sum_octet<IO, FAST>(h[o], r[o], row, (t / 8 + o * (p.lanes / 8)) * KEEP_GROUP, s, p, store);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum = fma2(h[o].pair(i), h[o].pair(i), sum);
+    for (int i = 0; i < UNITS; ++i) {
+      h[i] = x[i];
+      sum_unit(h[i], r[i], residual, sum);
+      if (residual && store) store_unit<FAST>(h[i], (IO*)p.h + row * p.h_stride + at.column(i), at.left(i));
     }
-    float total = row_sum(sum.x + sum.y, p.lanes, turn++, shared), scale = scale_of(total, p);
+    if (base + step < p.rows) load(min(base + step + at.slot, p.rows - 1));
+    float total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared), scale = scale_of(total, p);
     // (lanes of one warp may hold different rows: they all go the same way, as do all threads of a row's warps)
     const bool far = !(total <= largest_finite<float>());
-    if (p.lanes > 32 ? far : __any_sync(0xffffffffu, far)) {
+    if (BLOCK ? far : __any_sync(0xffffffffu, far)) {
       sum = both(0.f);
 #pragma unroll
-      for (int o = 0; o < OCTETS; ++o) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 v = mul2(h[o].pair(i), both(RMS_DOWN));
-          sum = fma2(v, v, sum);
-        }
-      }
-      total = row_sum(sum.x + sum.y, p.lanes, turn++, shared);
+      for (int i = 0; i < UNITS; ++i) sum_unit_far(h[i], sum);
+      total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared);
       if (far) scale = scale_of_far(total, p);
     }
-    if (p.rstd && t == 0 && store) p.rstd[row] = scale;
+    if (p.rstd && at.t == 0 && store) p.rstd[row] = scale;
 #pragma unroll
-    for (int o = 0; o < OCTETS; ++o) finish_octet<IO, WT, FAST>(h[o], scale, row, (t / 8 + o * (p.lanes / 8)) * KEEP_GROUP, s, p, store);
+    for (int i = 0; i < UNITS; ++i) finish_unit<IO, WT, FAST, N>(h[i], w[i], scale, row, at.column(i), at.left(i), at.s, p, store);
   }
 }
 // A block per row, which is read twice.
-template <typename IO, typename WT, bool FAST>
-__global__ void __launch_bounds__(RMS_MOST_LANES) rms_forward_wide_kernel(const RmsParams p) {
+template <typename IO, typename WT, bool FAST> __global__ void __launch_bounds__(RMS_WIDE) rms_forward_wide_kernel(const RmsParams p) {
+  constexpr int N = UNIT<IO>, LANES = KEEP_GROUP / N, STEP = RMS_WIDE / LANES;
   __shared__ float shared[2][32];
-  const int t = threadIdx.x, s = t & 7, groups = (p.n + KEEP_GROUP - 1) / KEEP_GROUP, rounds = (groups + RMS_MOST_LANES / 8 - 1) / (RMS_MOST_LANES / 8);
+  const int t = threadIdx.x, s = t % LANES;
+  const bool residual = p.residual != nullptr;
   int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const IO* const from = (const IO*)p.x + row * p.x_stride;
-    const IO* const again = p.residual ? (const IO*)p.h + row * p.h_stride : from;
+    const IO* const again = residual ? (const IO*)p.h + row * p.h_stride : from;
     float2 sum = both(0.f);
-    for (int o = 0; o < rounds; ++o) {
-      const int64_t c = (int64_t)(t / 8 + o * (RMS_MOST_LANES / 8)) * KEEP_GROUP;
-      const int c0 = (int)min(c, (int64_t)p.n);
-      Octet<IO, FAST> h, r;
-      h.load(from, c0, s, p.n);
-      if (p.residual) r.load((const IO*)p.residual + row * p.residual_stride, c0, s, p.n);
-      sum_octet<IO, FAST>(h, r, row, c0, s, p, true);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum = fma2(h.pair(i), h.pair(i), sum);
-    }
-    float total = row_sum(sum.x + sum.y, RMS_MOST_LANES, turn++, shared), scale = scale_of(total, p);
+    // (groups behind the last one: all threads take the same number of turns, as lanes of a group work together)
+    auto each = [&](auto&& f) {
+      for (int64_t g = t / LANES; g - t / LANES < p.groups; g += STEP) {
+        const int column = (int)min(g * KEEP_GROUP, (int64_t)p.n) + unit_first<N, FAST>(s);
+        f(column, p.n - column);
+      }
+    };
+    each([&](int column, int left) {
+      Unit<IO, N> h, r;
+      h.zero(), r.zero();
+      load_unit<FAST>(h, from + column, left);
+      if (residual) load_unit<FAST>(r, (const IO*)p.residual + row * p.residual_stride + column, left);
+      sum_unit(h, r, residual, sum);
+      if (residual) store_unit<FAST>(h, (IO*)p.h + row * p.h_stride + column, left);
+    });
+    float total = row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared), scale = scale_of(total, p);
     if (!(total <= largest_finite<float>())) {
       sum = both(0.f);
-      for (int o = 0; o < rounds; ++o) {
-        const int c0 = (int)min((int64_t)(t / 8 + o * (RMS_MOST_LANES / 8)) * KEEP_GROUP, (int64_t)p.n);
-        Octet<IO, FAST> h;
-        h.load(again, c0, s, p.n);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 v = mul2(h.pair(i), both(RMS_DOWN));
-          sum = fma2(v, v, sum);
-        }
-      }
-      scale = scale_of_far(row_sum(sum.x + sum.y, RMS_MOST_LANES, turn++, shared), p);
+      each([&](int column, int left) {
+        Unit<IO, N> h;
+        h.zero();
+        load_unit<FAST>(h, again + column, left);
+        sum_unit_far(h, sum);
+      });
+      scale = scale_of_far(row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared), p);
     }
     if (p.rstd && t == 0) p.rstd[row] = scale;
-    for (int o = 0; o < rounds; ++o) {   // (a thread reads back what it stored itself)
-      const int c0 = (int)min((int64_t)(t / 8 + o * (RMS_MOST_LANES / 8)) * KEEP_GROUP, (int64_t)p.n);
-      Octet<IO, FAST> h;
-      h.load(again, c0, s, p.n);
-      finish_octet<IO, WT, FAST>(h, scale, row, c0, s, p, true);
-    }
+    each([&](int column, int left) {   // (a thread reads back what it stored itself)
+      Unit<IO, N> h;
+      Unit<WT, N> w;
+      h.zero(), w.zero();
+      load_unit<FAST>(h, again + column, left);
+      if (p.weight) load_unit<FAST>(w, (const WT*)p.weight + column, left);
+      finish_unit<IO, WT, FAST, N>(h, w, scale, row, column, left, s, p, true);
+    });
   }
 }
 
-// n = h s and g = dy w of pair i of an octet.
-template <typename IO, typename WT, bool FAST>
-__device__ __forceinline__ float2 weighted(const Octet<IO, FAST>& dy, const Octet<WT, FAST>& w, bool has_weight, int i) {
-  return has_weight ? mul2(dy.pair(i), w.pair(i)) : dy.pair(i);
+// g = dy w of pair i of a unit.
+template <typename IO, typename WT, int N> __device__ __forceinline__ float2 weighted(const Unit<IO, N>& dy, const Unit<WT, N>& w, bool has_weight, int i) {
+  return has_weight ? mul_pair(dy.pair(i), w.pair(i)) : dy.pair(i);
 }
-
-template <typename IO, typename WT, bool FAST, int OCTETS>
-__global__ void __launch_bounds__(RMS_MOST_LANES_BACK) rms_backward_kernel(const RmsParams p) {
+template <typename IO, typename WT, bool FAST, int UNITS, bool BLOCK>
+__global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_backward_kernel(const RmsParams p) {
+  constexpr int N = UNIT<IO>;
   __shared__ float shared[2][32];
-  __shared__ float dw_shared[32 * OCTETS * 8];   // rows within a warp only
+  __shared__ float dw_shared[BLOCK ? 1 : 32 * N];
   let_next_kernel_start();
-  const int slot = threadIdx.x / p.lanes, t = threadIdx.x % p.lanes, s = t & 7, per_block = blockDim.x / p.lanes;
-  const int64_t step = (int64_t)gridDim.x * per_block;
+  const Place<BLOCK, N, FAST> at(p);
+  const int64_t step = (int64_t)gridDim.x * at.per_block();
+  const bool has_weight = p.weight != nullptr;
   int turn = 0;
-  float2 dw[OCTETS][4];
+  // the loads of the next row are on their way while a row is worked at, where registers hold both
+  constexpr bool AHEAD = FAST && UNITS == 1;
+  struct Inputs {
+    Unit<IO, N> h[UNITS], dy[UNITS], dh[UNITS];
+    float scale;
+  } now, next;
+  float2 dw[UNITS][N / 2];
+  Unit<WT, N> w[UNITS];
 #pragma unroll
-  for (int o = 0; o < OCTETS; ++o)
+  for (int i = 0; i < UNITS; ++i) {
+    now.h[i].zero(), now.dy[i].zero(), now.dh[i].zero(), w[i].zero();   // (and stay so behind the row's end)
+    if (has_weight) load_unit<FAST>(w[i], (const WT*)p.weight + at.column(i), at.left(i));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) dw[o][i] = both(0.f);
-  auto column = [&](int o) { return (t / 8 + o * (p.lanes / 8)) * KEEP_GROUP; };
-  for (int64_t base = (int64_t)blockIdx.x * per_block; base < p.rows; base += step) {
-    const bool mine = base + slot < p.rows;
-    const int64_t row = min(base + slot, p.rows - 1);
-    Octet<IO, FAST> h[OCTETS], dy[OCTETS], dh[OCTETS];
+    for (int k = 0; k < N / 2; ++k) dw[i][k] = both(0.f);
+  }
+  auto load = [&](Inputs& in, int64_t row) {
+    const IO *const from = (const IO*)p.h + row * p.h_stride, *const from_dy = (const IO*)p.dy + row * p.dy_stride;
+    in.scale = p.rstd[row];
 #pragma unroll
-    for (int o = 0; o < OCTETS; ++o) {
-      h[o].load((const IO*)p.h + row * p.h_stride, column(o), s, p.n);
-      dy[o].load((const IO*)p.dy + row * p.dy_stride, column(o), s, p.n);
-      if (p.dh) dh[o].load((const IO*)p.dh + row * p.dh_stride, column(o), s, p.n);
+    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(in.h[i], from + at.column(i), at.left(i));
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(in.dy[i], from_dy + at.column(i), at.left(i));
+    if (!p.dh) return;
+    const IO* const from_dh = (const IO*)p.dh + row * p.dh_stride;
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(in.dh[i], from_dh + at.column(i), at.left(i));
+  };
+  next = now;
+  if (AHEAD && (int64_t)blockIdx.x * at.per_block() < p.rows) load(next, min((int64_t)blockIdx.x * at.per_block() + at.slot, p.rows - 1));
+  for (int64_t base = (int64_t)blockIdx.x * at.per_block(); base < p.rows; base += step) {
+    const bool mine = base + at.slot < p.rows;
+    const int64_t row = min(base + at.slot, p.rows - 1);
+    if (AHEAD) {
+      now = next;
+      if (base + step < p.rows) load(next, min(base + step + at.slot, p.rows - 1));
+    } else {
+      load(now, row);
     }
-    const float scale = p.rstd[row];
+    const float scale = now.scale;
     float2 sum = both(0.f);
 #pragma unroll
-    for (int o = 0; o < OCTETS; ++o) {
-      Octet<WT, FAST> w;
-      if (p.weight) w.load((const WT*)p.weight, column(o), s, p.n);
+    for (int i = 0; i < UNITS; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 n = mul2(h[o].pair(i), both(scale));
-        sum = fma2(weighted(dy[o], w, p.weight != nullptr, i), n, sum);
-        if (mine) dw[o][i] = fma2(dy[o].pair(i), n, dw[o][i]);
+      for (int k = 0; k < N / 2; ++k) {
+        const float2 n = mul_pair(now.h[i].pair(k), both(scale));
+        sum = fma_pair(weighted(now.dy[i], w[i], has_weight, k), n, sum);
+        if (BLOCK || mine) dw[i][k] = fma_pair(now.dy[i].pair(k), n, dw[i][k]);
       }
-    }
-    const float c = row_sum(sum.x + sum.y, p.lanes, turn++, shared) * p.inverse_n;
+    const float c = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared) * p.inverse_n;
+    IO* const to = (IO*)p.dx + row * p.dx_stride;
 #pragma unroll
-    for (int o = 0; o < OCTETS; ++o) {
-      Octet<WT, FAST> w;
-      if (p.weight) w.load((const WT*)p.weight, column(o), s, p.n);
-      Octet<IO, FAST> out;
+    for (int i = 0; i < UNITS; ++i) {
+      Unit<IO, N> out;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 n = mul2(h[o].pair(i), both(scale));
-        float2 v = mul2(fma2(n, both(-c), weighted(dy[o], w, p.weight != nullptr, i)), both(scale));
-        if (p.dh) v = add2(v, dh[o].pair(i));
-        out.set(i, v);
+      for (int k = 0; k < N / 2; ++k) {
+        const float2 n = mul_pair(now.h[i].pair(k), both(scale));
+        float2 v = mul_pair(fma_pair(n, both(-c), weighted(now.dy[i], w[i], has_weight, k)), both(scale));
+        if (p.dh) v = add_pair(v, now.dh[i].pair(k));
+        out.set(k, v);
       }
-      if (mine) out.store((IO*)p.dx + row * p.dx_stride, column(o), s, p.n);
+      if (mine) store_unit<FAST>(out, to + at.column(i), at.left(i));
     }
   }
   if (!p.partial) return;
   float* const to = p.partial + (int64_t)blockIdx.x * p.n;
-  if (p.lanes > 32) {
+  auto each = [&](auto&& f) {
 #pragma unroll
-    for (int o = 0; o < OCTETS; ++o)
+    for (int i = 0; i < UNITS; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int at = column(o) + octet_place<FAST>(s, j);
-        if (at < p.n) to[at] = j % 2 ? dw[o][j / 2].y : dw[o][j / 2].x;
-      }
+      for (int j = 0; j < N; ++j) f(at.column(i) + unit_place<N, FAST>(j), j % 2 ? dw[i][j / 2].y : dw[i][j / 2].x);
+  };
+  if (BLOCK) {
+    each([&](int c, float v) {
+      if (c < p.n) to[c] = v;
+    });
     return;
   }
   // the rows of a block one behind the other
-  for (int k = 0; k < per_block; ++k) {
-    if (slot == k) {
-#pragma unroll
-      for (int o = 0; o < OCTETS; ++o)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int at = column(o) + octet_place<FAST>(s, j);
-          const float v = j % 2 ? dw[o][j / 2].y : dw[o][j / 2].x;
-          dw_shared[at] = k == 0 ? v : dw_shared[at] + v;
-        }
-    }
+  for (int k = 0; k < at.per_block(); ++k) {
+    if (at.slot == k) each([&](int c, float v) { dw_shared[c] = k == 0 ? v : dw_shared[c] + v; });
     __syncthreads();
   }
   for (int i = threadIdx.x; i < p.n; i += blockDim.x) to[i] = dw_shared[i];
 }
-template <typename IO, typename WT, bool FAST>
-__global__ void __launch_bounds__(RMS_MOST_LANES) rms_backward_wide_kernel(const RmsParams p) {
+template <typename IO, typename WT, bool FAST> __global__ void __launch_bounds__(RMS_WIDE) rms_backward_wide_kernel(const RmsParams p) {
+  constexpr int N = UNIT<IO>, LANES = KEEP_GROUP / N, STEP = RMS_WIDE / LANES;
   __shared__ float shared[2][32];
-  const int t = threadIdx.x, s = t & 7, groups = (p.n + KEEP_GROUP - 1) / KEEP_GROUP, rounds = (groups + RMS_MOST_LANES / 8 - 1) / (RMS_MOST_LANES / 8);
+  let_next_kernel_start();
+  const int t = threadIdx.x, s = t % LANES;
+  const bool has_weight = p.weight != nullptr;
   int turn = 0;
   float* const to = p.partial ? p.partial + (int64_t)blockIdx.x * p.n : nullptr;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
@@ -284,76 +338,84 @@ __global__ void __launch_bounds__(RMS_MOST_LANES) rms_backward_wide_kernel(const
     float2 sum = both(0.f);
     float c = 0.f;
     for (int pass = 0; pass < 2; ++pass) {
-      for (int o = 0; o < rounds; ++o) {
-        const int c0 = (int)min((int64_t)(t / 8 + o * (RMS_MOST_LANES / 8)) * KEEP_GROUP, (int64_t)p.n);
-        Octet<IO, FAST> h, dy, dh, out;
-        Octet<WT, FAST> w;
-        h.load((const IO*)p.h + row * p.h_stride, c0, s, p.n);
-        dy.load((const IO*)p.dy + row * p.dy_stride, c0, s, p.n);
-        if (p.weight) w.load((const WT*)p.weight, c0, s, p.n);
-        if (p.dh && pass) dh.load((const IO*)p.dh + row * p.dh_stride, c0, s, p.n);
+      for (int64_t g = t / LANES; g < p.groups; g += STEP) {
+        const int column = (int)(g * KEEP_GROUP) + unit_first<N, FAST>(s), left = p.n - column;
+        Unit<IO, N> h, dy, dh, out;
+        Unit<WT, N> w;
+        h.zero(), dy.zero(), dh.zero(), w.zero();
+        load_unit<FAST>(h, (const IO*)p.h + row * p.h_stride + column, left);
+        load_unit<FAST>(dy, (const IO*)p.dy + row * p.dy_stride + column, left);
+        if (has_weight) load_unit<FAST>(w, (const WT*)p.weight + column, left);
+        if (p.dh && pass) load_unit<FAST>(dh, (const IO*)p.dh + row * p.dh_stride + column, left);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 n = mul2(h.pair(i), both(scale)), g = weighted(dy, w, p.weight != nullptr, i);
+        for (int k = 0; k < N / 2; ++k) {
+          const float2 n = mul_pair(h.pair(k), both(scale)), gw = weighted(dy, w, has_weight, k);
           if (!pass) {
-            sum = fma2(g, n, sum);
+            sum = fma_pair(gw, n, sum);
             continue;
           }
-          float2 v = mul2(fma2(n, both(-c), g), both(scale));
-          if (p.dh) v = add2(v, dh.pair(i));
-          out.set(i, v);
+          float2 v = mul_pair(fma_pair(n, both(-c), gw), both(scale));
+          if (p.dh) v = add_pair(v, dh.pair(k));
+          out.set(k, v);
           if (!to) continue;
-          const float2 d = mul2(dy.pair(i), n);   // (every place of a block's share belongs to one thread)
-          const int at = c0 + octet_place<FAST>(s, 2 * i), next = c0 + octet_place<FAST>(s, 2 * i + 1);
-          if (at < p.n) to[at] = row == blockIdx.x ? d.x : to[at] + d.x;
-          if (next < p.n) to[next] = row == blockIdx.x ? d.y : to[next] + d.y;
+          const float2 d = mul_pair(dy.pair(k), n);   // (every place of a block's share belongs to one thread)
+          const int a = unit_place<N, FAST>(2 * k), b = unit_place<N, FAST>(2 * k + 1);
+          if (a < left) to[column + a] = row == blockIdx.x ? d.x : to[column + a] + d.x;
+          if (b < left) to[column + b] = row == blockIdx.x ? d.y : to[column + b] + d.y;
         }
-        if (pass) out.store((IO*)p.dx + row * p.dx_stride, c0, s, p.n);
+        if (pass) store_unit<FAST>(out, (IO*)p.dx + row * p.dx_stride + column, left);
       }
-      if (!pass) c = row_sum(sum.x + sum.y, RMS_MOST_LANES, turn++, shared) * p.inverse_n;
+      if (!pass) c = row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared) * p.inverse_n;
     }
   }
 }
-// dw from the blocks' shares, in their order: 32 columns a block, eight rows of shares at a time.
-template <typename WT> __global__ void __launch_bounds__(256) rms_dweight_kernel(const float* partial, int blocks, int n, WT* dw) {
-  __shared__ float shared[8][32];
+// dw from the blocks' shares, in an order of its own: 32 columns a block, 32 rows of shares at a time.
+template <typename WT> __global__ void __launch_bounds__(1024) rms_dweight_kernel(const float* partial, int blocks, int n, WT* dw) {
+  __shared__ float shared[32][33];
   wait_for_kernel_before();
   const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
   float sum = 0.f;
   if (c < n) {
 #pragma unroll 8
-    for (int b = y; b < blocks; b += 8) sum += partial[(int64_t)b * n + c];
+    for (int b = y; b < blocks; b += 32) sum += partial[(int64_t)b * n + c];
   }
   shared[y][x] = sum;
   __syncthreads();
-  if (y > 0 || c >= n) return;
+  sum = shared[x][y];   // column y of the block, share x
 #pragma unroll
-  for (int k = 1; k < 8; ++k) sum += shared[k][x];
-  dw[c] = from_f32<WT>(sum);
+  for (int o = 1; o < 32; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (x == 0 && blockIdx.x * 32 + y < n) dw[blockIdx.x * 32 + y] = from_f32<WT>(sum);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------
+int unit_of(int dtype) { return 32 / (int)dtype_size(dtype); }
 struct Shape {
-  int lanes, octets, threads;   // octets 0: rows that do not fit registers
+  int lanes, units, threads, blocks;   // units 0: rows that do not fit registers
+  bool block;                          // a row per block
 };
-Shape shape_of(int n, int most_lanes) {
-  const int groups = (n + KEEP_GROUP - 1) / KEEP_GROUP;
-  for (int octets = 1; octets <= 2; ++octets) {
-    const int need = 8 * ((groups + octets - 1) / octets);
-    const int lanes = need > 32 ? (need + 31) / 32 * 32 : need > 16 ? 32 : need;
-    if (lanes <= (octets == 1 ? 256 : most_lanes)) return {lanes, octets, lanes > 32 ? lanes : RMS_THREADS};
+// One unit a thread where rows are few, so that a row is spread over many threads; two where the rows fill the device with half
+// the threads each, so that what a row costs beside its values is shared by more of them.  (Value by value, without vectors,
+// a second unit only means more registers.)
+Shape shape_of(const snn_rms_norm_args* a, bool fast, bool two, int resident) {
+  const int groups = (a->n + KEEP_GROUP - 1) / KEEP_GROUP, per_group = KEEP_GROUP * (int)dtype_size(a->dtype) / 32;
+  Shape s{RMS_WIDE, 0, RMS_WIDE, 0, true};
+  for (int units = 1; units <= 2; ++units) {
+    const int64_t need = (int64_t)per_group * ((groups + units - 1) / units);
+    int lanes = per_group;
+    while (lanes < need && lanes < 32) lanes *= 2;
+    if (need > 32) lanes = (int)std::min<int64_t>((need + 31) / 32 * 32, INT32_MAX - 31);
+    if (lanes > RMS_MOST_LANES) continue;
+    if (s.units && (!fast || !two || need < 32 || a->rows * lanes < 148 * 512)) break;
+    const bool block = units > 1 || lanes > 32;
+    s = {lanes, units, block ? lanes : RMS_THREADS, 0, block};
   }
-  return {RMS_MOST_LANES, 0, RMS_MOST_LANES};
+  const int64_t per_block = s.threads / s.lanes, turns = (a->rows + per_block - 1) / per_block;
+  s.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(turns, (int64_t)148 * std::max(1, (s.units == 2 ? 512 : resident) / s.threads)));
+  return s;
 }
-unsigned blocks_of(const Shape& s, int64_t rows, int per_sm) {
-  const int64_t per_block = s.threads / s.lanes, want = (rows + per_block - 1) / per_block;
-  return (unsigned)std::max<int64_t>(1, std::min<int64_t>(want, (int64_t)148 * per_sm));
-}
-// blocks of the backward pass: two thousand threads of an SM at most, and no more than rows
-unsigned backward_blocks(int n, int64_t rows) {
-  const Shape s = shape_of(n, RMS_MOST_LANES_BACK);
-  return blocks_of(s, rows, std::max(1, 1024 / s.threads));
-}
+Shape shape_forward(const snn_rms_norm_args* a, bool fast) { return shape_of(a, fast, true, 1024); }
+Shape shape_back(const snn_rms_norm_args* a, bool fast) { return shape_of(a, fast, false, 512); }
+
 snn_status check(const snn_rms_norm_args* a) {
   if (!a || a->rows < 0 || a->n < 1 || !dtype_known(a->dtype)) return SNN_ERR_INVALID_ARG;
   if (a->weight_dtype != a->dtype && a->weight_dtype != SNN_DTYPE_FP32) return SNN_ERR_INVALID_ARG;
@@ -373,7 +435,9 @@ extern "C" snn_status snn_rms_norm_workspace(const snn_rms_norm_args* a, size_t*
   const snn_status st = check(a);
   if (st != SNN_OK) return st;
   if (!bytes) return SNN_ERR_INVALID_ARG;
-  *bytes = a->rows == 0 ? 0 : ((size_t)backward_blocks(a->n, a->rows) * a->n * 4 + 255) / 256 * 256;
+  // (whether rows can be accessed by vectors is not asked here)
+  const int blocks = std::max(shape_back(a, true).blocks, shape_back(a, false).blocks);
+  *bytes = a->rows == 0 ? 0 : ((size_t)blocks * a->n * 4 + 255) / 256 * 256;
   return SNN_OK;
 }
 
@@ -387,21 +451,23 @@ extern "C" snn_status snn_rms_norm_forward(const snn_rms_norm_args* a, void* str
   if (!a->x || (a->residual && !a->h) || (!a->y && !keeps) || (keeps && (!a->codes || !a->scales))) return SNN_ERR_INVALID_ARG;
   if ((a->residual && !no_overlap(a, a->h_stride)) || (a->y && !no_overlap(a, a->y_stride))) return SNN_ERR_INVALID_ARG;
   RmsParams p{};
-  const Shape s = shape_of(a->n, RMS_MOST_LANES);
-  p.rows = a->rows, p.n = a->n, p.lanes = s.lanes, p.keep_format = a->keep_format, p.eps = a->eps, p.inverse_n = 1.f / (float)a->n;
+  p.rows = a->rows, p.n = a->n, p.groups = (a->n + KEEP_GROUP - 1) / KEEP_GROUP, p.keep_format = a->keep_format, p.eps = a->eps, p.inverse_n = 1.f / (float)a->n;
   p.x = a->x, p.x_stride = a->x_stride, p.residual = a->residual, p.residual_stride = a->residual_stride, p.weight = a->weight;
   p.h = a->h, p.h_stride = a->h_stride, p.y = a->y, p.y_stride = a->y_stride, p.rstd = a->rstd, p.codes = a->codes, p.scales = a->scales;
-  const bool fast = a->n % 8 == 0 && octet_rows(a->x, a->x_stride, a->dtype) && octet_rows(a->residual, a->residual_stride, a->dtype) &&
-                    octet_rows(a->residual ? a->h : nullptr, a->h_stride, a->dtype) && octet_rows(a->y, a->y_stride, a->dtype) &&
-                    octet_rows(a->weight, 0, a->weight_dtype) && (!keeps || aligned_to(a->codes, 8));
+  const bool fast = a->n % unit_of(a->dtype) == 0 && rows_of_32(a->x, a->x_stride, a->dtype) && rows_of_32(a->residual, a->residual_stride, a->dtype) &&
+                    rows_of_32(a->residual ? a->h : nullptr, a->h_stride, a->dtype) && rows_of_32(a->y, a->y_stride, a->dtype) &&
+                    rows_of_32(a->weight, 0, a->weight_dtype) && (!keeps || aligned_to(a->codes, 16));
+  const Shape s = shape_forward(a, fast);
+  p.lanes = s.lanes;
   return by_types(a->dtype, a->weight_dtype, fast, [&](auto io, auto wt, auto is_fast) {
     using IO = decltype(io);
     using WT = decltype(wt);
     constexpr bool FAST = decltype(is_fast)::value;
-    const auto kernel = s.octets == 0   ? rms_forward_wide_kernel<IO, WT, FAST>
-                        : s.octets == 1 ? rms_forward_kernel<IO, WT, FAST, 1>
-                        : rms_forward_kernel<IO, WT, FAST, 2>;
-    return launch_behind(kernel, blocks_of(s, a->rows, 1 << 16), s.threads, 0, (cudaStream_t)stream, false, p);
+    const auto kernel = s.units == 0   ? rms_forward_wide_kernel<IO, WT, FAST>
+                        : !s.block     ? rms_forward_kernel<IO, WT, FAST, 1, false>
+                        : s.units == 1 ? rms_forward_kernel<IO, WT, FAST, 1, true>
+                                       : rms_forward_kernel<IO, WT, FAST, 2, true>;
+    return launch_behind(kernel, (unsigned)s.blocks, s.threads, 0, (cudaStream_t)stream, false, p);
   });
 }
 
@@ -414,31 +480,31 @@ extern "C" snn_status snn_rms_norm_backward(const snn_rms_norm_args* a, void* st
     return cudaMemsetAsync(a->dweight, 0, (size_t)a->n * dtype_size(a->weight_dtype), on) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
   }
   if (!a->h || !a->rstd || !a->dy || !a->dx || !no_overlap(a, a->dx_stride)) return SNN_ERR_INVALID_ARG;
-  const unsigned blocks = backward_blocks(a->n, a->rows);
+  const bool fast = a->n % unit_of(a->dtype) == 0 && rows_of_32(a->h, a->h_stride, a->dtype) && rows_of_32(a->dy, a->dy_stride, a->dtype) &&
+                    rows_of_32(a->dh, a->dh_stride, a->dtype) && rows_of_32(a->dx, a->dx_stride, a->dtype) && rows_of_32(a->weight, 0, a->weight_dtype);
+  const Shape s = shape_back(a, fast);
   if (a->dweight) {
     if (!a->workspace || !aligned_to(a->workspace, 256)) return SNN_ERR_INVALID_ARG;
-    if (a->workspace_bytes < (size_t)blocks * a->n * 4) return SNN_ERR_WORKSPACE_TOO_SMALL;
+    if (a->workspace_bytes < (size_t)s.blocks * a->n * 4) return SNN_ERR_WORKSPACE_TOO_SMALL;
   }
   RmsParams p{};
-  const Shape s = shape_of(a->n, RMS_MOST_LANES_BACK);
-  p.rows = a->rows, p.n = a->n, p.lanes = s.lanes, p.inverse_n = 1.f / (float)a->n, p.weight = a->weight;
+  p.rows = a->rows, p.n = a->n, p.groups = (a->n + KEEP_GROUP - 1) / KEEP_GROUP, p.lanes = s.lanes, p.inverse_n = 1.f / (float)a->n, p.weight = a->weight;
   p.h = a->h, p.h_stride = a->h_stride, p.rstd = a->rstd, p.dy = a->dy, p.dy_stride = a->dy_stride, p.dh = a->dh, p.dh_stride = a->dh_stride;
   p.dx = a->dx, p.dx_stride = a->dx_stride, p.partial = a->dweight ? (float*)a->workspace : nullptr;
-  const bool fast = a->n % 8 == 0 && octet_rows(a->h, a->h_stride, a->dtype) && octet_rows(a->dy, a->dy_stride, a->dtype) &&
-                    octet_rows(a->dh, a->dh_stride, a->dtype) && octet_rows(a->dx, a->dx_stride, a->dtype) && octet_rows(a->weight, 0, a->weight_dtype);
   const snn_status done = by_types(a->dtype, a->weight_dtype, fast, [&](auto io, auto wt, auto is_fast) {
     using IO = decltype(io);
     using WT = decltype(wt);
     constexpr bool FAST = decltype(is_fast)::value;
-    const auto kernel = s.octets == 0   ? rms_backward_wide_kernel<IO, WT, FAST>
-                        : s.octets == 1 ? rms_backward_kernel<IO, WT, FAST, 1>
-                        : rms_backward_kernel<IO, WT, FAST, 2>;
-    return launch_behind(kernel, blocks, s.threads, 0, on, false, p);
+    const auto kernel = s.units == 0   ? rms_backward_wide_kernel<IO, WT, FAST>
+                        : !s.block     ? rms_backward_kernel<IO, WT, FAST, 1, false>
+                        : s.units == 1 ? rms_backward_kernel<IO, WT, FAST, 1, true>
+                                       : rms_backward_kernel<IO, WT, FAST, 2, true>;
+    return launch_behind(kernel, (unsigned)s.blocks, s.threads, 0, on, false, p);
   });
   if (done != SNN_OK || !a->dweight) return done;
   const unsigned tiles = (unsigned)((a->n + 31) / 32);
-  if (a->weight_dtype == SNN_DTYPE_FP32) return launch_behind(rms_dweight_kernel<float>, tiles, 256, 0, on, true, p.partial, (int)blocks, a->n, (float*)a->dweight);
+  if (a->weight_dtype == SNN_DTYPE_FP32) return launch_behind(rms_dweight_kernel<float>, tiles, 1024, 0, on, true, p.partial, s.blocks, a->n, (float*)a->dweight);
   if (a->weight_dtype == SNN_DTYPE_BF16)
-    return launch_behind(rms_dweight_kernel<__nv_bfloat16>, tiles, 256, 0, on, true, p.partial, (int)blocks, a->n, (__nv_bfloat16*)a->dweight);
-  return launch_behind(rms_dweight_kernel<__half>, tiles, 256, 0, on, true, p.partial, (int)blocks, a->n, (__half*)a->dweight);
+    return launch_behind(rms_dweight_kernel<__nv_bfloat16>, tiles, 1024, 0, on, true, p.partial, s.blocks, a->n, (__nv_bfloat16*)a->dweight);
+  return launch_behind(rms_dweight_kernel<__half>, tiles, 1024, 0, on, true, p.partial, s.blocks, a->n, (__half*)a->dweight);
 }

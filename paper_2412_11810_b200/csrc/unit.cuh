@@ -1,0 +1,209 @@
+// 32 bytes of a row per thread, and what kernels that move such units share.
+//
+// A unit is N values of a lane: 8 of fp32, 16 of a 16-bit type, so that a unit of the type is one 256-bit access and the lanes
+// of a warp cover whole lines with it.  A group of 64 values (KEEP_GROUP) belongs to 64 / N neighbouring lanes.  FAST: lane s
+// holds values N s .. N s + N - 1; it needs rows of multiples of N values at addresses of multiples of 32 bytes.  Otherwise
+// it holds s, s + 64 / N, ..: single values, neighbouring lanes at neighbouring addresses.
+#pragma once
+#include <string.h>
+
+#include <type_traits>
+
+#include "seq_common.cuh"
+
+namespace snnk {
+
+template <typename T> constexpr int UNIT = 32 / (int)sizeof(T);
+
+// ---- pairs of fp32 values in two registers -------------------------------------------------------------------
+__device__ __forceinline__ float2 fma_pair(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul_pair(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add_pair(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+// The largest magnitude of m and a pair; NaN if one of them is.
+__device__ __forceinline__ float larger_of(float m, float2 v) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(m), "f"(fabsf(v.x)), "f"(fabsf(v.y)));
+  return d;
+}
+
+// ---- units -----------------------------------------------------------------------------------------------------
+// (volatile keeps the order of these accesses among one another; a store that depends on a load comes behind it anyway)
+__device__ __forceinline__ void get_32(uint32_t* u, const void* p) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+               : "l"(p));
+}
+__device__ __forceinline__ void put_32(void* p, const uint32_t* u) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]),
+               "r"(u[5]), "r"(u[6]), "r"(u[7])
+               : "memory");
+}
+__device__ __forceinline__ void get_16(uint32_t* u, const void* p) {
+  asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]) : "l"(p));
+}
+__device__ __forceinline__ void put_16(void* p, const uint32_t* u) {
+  asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]) : "memory");
+}
+template <typename T> __device__ __forceinline__ float2 pair_of(const uint32_t* u, int i) {
+  if constexpr (sizeof(T) == 4) {
+    return make_float2(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+  } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {   // the upper half of an fp32 value
+    return make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+  } else {
+    __half2 r;
+    memcpy(&r, &u[i], 4);
+    return __half22float2(r);
+  }
+}
+template <typename T> __device__ __forceinline__ void set_pair(uint32_t* u, int i, float2 v) {
+  if constexpr (sizeof(T) == 4) {
+    u[2 * i] = __float_as_uint(v.x), u[2 * i + 1] = __float_as_uint(v.y);
+  } else {
+    typename Pair<T>::raw r;
+    set_raw(r, v);
+    memcpy(&u[i], &r, 4);
+  }
+}
+// N values of type T: 16 or 32 bytes, or a multiple of that.
+template <typename T, int N> struct Unit {
+  static constexpr int WORDS = N * (int)sizeof(T) / 4, LANES = KEEP_GROUP / N;
+  uint32_t u[WORDS];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) u[i] = 0u;
+  }
+  __device__ __forceinline__ float2 pair(int i) const { return pair_of<T>(u, i); }
+  __device__ __forceinline__ void set(int i, float2 v) { set_pair<T>(u, i, v); }
+  __device__ __forceinline__ void get(const T* p) {
+    if constexpr (WORDS == 4) {
+      get_16(u, p);
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 8) get_32(u + i, (const uint32_t*)p + i);
+    }
+  }
+  __device__ __forceinline__ void put(T* p) const {
+    if constexpr (WORDS == 4) {
+      put_16(p, u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; i += 8) put_32((uint32_t*)p + i, u + i);
+    }
+  }
+  // Value by value, LANES apart from p on, of which `left` places exist; the others are zero.
+  __device__ __forceinline__ void get_each(const T* p, int left) {
+    T v[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = LANES * j < left ? p[LANES * j] : from_f32<T>(0.f);
+    memcpy(u, v, sizeof(v));
+  }
+  __device__ __forceinline__ void put_each(T* p, int left) const {
+    T v[N];
+    memcpy(v, u, sizeof(v));
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (LANES * j < left) p[LANES * j] = v[j];
+  }
+};
+// Where a lane's values of a group lie: the first one, and the others behind it.
+template <int N, bool FAST> __device__ __forceinline__ constexpr int unit_first(int s) { return FAST ? N * s : s; }
+template <int N, bool FAST> __device__ __forceinline__ constexpr int unit_place(int j) { return FAST ? j : j * (KEEP_GROUP / N); }
+// The unit at p, the place of a lane's first value in a row of which `left` places are left.
+template <bool FAST, typename T, int N> __device__ __forceinline__ void load_unit(Unit<T, N>& v, const T* p, int left) {
+  if (!FAST)
+    v.get_each(p, left);
+  else if (left > 0)
+    v.get(p);
+}
+template <bool FAST, typename T, int N> __device__ __forceinline__ void store_unit(const Unit<T, N>& v, T* p, int left) {
+  if (!FAST)
+    v.put_each(p, left);
+  else if (left > 0)
+    v.put(p);
+}
+
+// ---- 8-bit codes of a group ------------------------------------------------------------------------------------
+// Largest magnitude of a group as a bit pattern, from that of its lanes; NaN sorts above infinity above the rest.
+template <int LANES> __device__ __forceinline__ uint32_t group_top(float m) {
+  uint32_t top = __float_as_uint(m);
+#pragma unroll
+  for (int o = 1; o < LANES; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  return top;
+}
+// Codes of N values, four per word, rounded to nearest.  rare: whether a code of the warp could round up to 128.
+template <int FORMAT, int N> __device__ __forceinline__ void encode_unit(uint32_t q[N / 4], const float2 v[N / 2], float inverse, bool rare) {
+#pragma unroll
+  for (int k = 0; k < N / 4; ++k) {
+    if (FORMAT == SNN_KEEP_INT8) {
+      // 1.5 x 2^23 + v / scale, rounded once: the integer stands in the low bits
+      const float magic = 12582912.f;
+      float2 a = fma_pair(v[2 * k], both(inverse), both(magic)), b = fma_pair(v[2 * k + 1], both(inverse), both(magic));
+      if (rare) {
+        a = make_float2(fminf(fmaxf(a.x, magic - 127.f), magic + 127.f), fminf(fmaxf(a.y, magic - 127.f), magic + 127.f));
+        b = make_float2(fminf(fmaxf(b.x, magic - 127.f), magic + 127.f), fminf(fmaxf(b.y, magic - 127.f), magic + 127.f));
+      }
+      q[k] = __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+    } else {
+      const float2 a = mul_pair(v[2 * k], both(inverse)), b = mul_pair(v[2 * k + 1], both(inverse));
+      q[k] = (uint32_t)__nv_cvt_float2_to_fp8x2(a, __NV_SATFINITE, __NV_E4M3) | (uint32_t)__nv_cvt_float2_to_fp8x2(b, __NV_SATFINITE, __NV_E4M3) << 16;
+    }
+  }
+}
+template <bool FAST, int N> __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t q[N / 4], int left) {
+  if (FAST) {
+    if (left <= 0) return;
+    if (N == 16)
+      *reinterpret_cast<uint4*>(p) = make_uint4(q[0], q[1], q[N / 4 - 2], q[N / 4 - 1]);
+    else
+      *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+    if (j * (KEEP_GROUP / N) < left) p[j * (KEEP_GROUP / N)] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+}
+
+// ---- launches behind one another's start ---------------------------------------------------------------------
+__device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;"); }
+
+// behind: the kernel may be set up while the one before it in the stream runs; it calls wait_for_kernel_before() before it
+// touches anything that one writes or reads.
+template <typename... P, typename... A>
+snn_status launch_behind(void (*kernel)(P...), unsigned grid, int threads, size_t smem, cudaStream_t stream, bool behind, const A&... args) {
+  cudaLaunchConfig_t cfg{};
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = &at;
+  cfg.numAttrs = behind ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+}
+
+inline bool aligned_to(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
+// whether rows can be accessed 32 bytes at a time (rows that do not exist do not stand in the way)
+inline bool rows_of_32(const void* p, int64_t stride, int dtype) { return !p || (stride * (int64_t)dtype_size(dtype) % 32 == 0 && aligned_to(p, 32)); }
+
+}  // namespace snnk

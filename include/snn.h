@@ -531,7 +531,7 @@ typedef struct {
   int32_t moment_format;           /* SNN_KEEP_RAW or SNN_KEEP_E4M3                                      */
   const snn_adamw_tensor* tensors; /* [count], host; read before the call returns                        */
   float *m, *v;                    /* SNN_KEEP_RAW; 32-byte aligned                                      */
-  uint8_t *m_codes, *m_scales, *v_codes, *v_scales;   /* SNN_KEEP_E4M3; codes 16-byte aligned            */
+  uint8_t *m_codes, *m_scales, *v_codes, *v_scales;   /* SNN_KEEP_E4M3; codes 8-byte aligned             */
   int64_t* step;                   /* device: steps done so far; the call adds one                       */
   double lr, beta1, beta2, eps, weight_decay;   /* lr, weight_decay >= 0; 0 <= beta < 1; 1e-30 <= eps <= 1 */
   const float* lr_device;          /* or NULL: used in place of lr                                       */

@@ -3,7 +3,7 @@
 //   m' = b1 m + (1 - b1) g,  v' = b2 v + (1 - b2) g^2,  p' = p (1 - lr wd) - lr / (1 - b1^t) m' / (sqrt(v' / (1 - b2^t)) + eps)
 //
 // Bound by HBM (28 bytes a parameter with everything in fp32, 10 with bf16 parameters and gradients and moments in 8 bits).
-// A thread block takes tiles of a tensor, eight (16 with moments in 8 bits) neighbouring parameters a thread and turn; where a
+// A thread block takes tiles of a tensor, eight neighbouring parameters a thread and turn; where a
 // tile's tensor lies is found by bisection in a table that comes with the launch, so that nothing is copied to the device first
 // and a graph holds it.
 //
@@ -20,7 +20,8 @@ using namespace snnk;
 
 namespace {
 
-constexpr int AW_THREADS = 256, AW_MOST_TURNS = 4;   // of a tile
+constexpr int AW_THREADS = 256, AW_VALUES = 8;   // values of a thread and turn: eight lanes a group
+constexpr int AW_TURNS = 8;                       // of a tile, where there is enough to do
 constexpr int AW_NORM_BLOCKS = 148 * 4;
 
 struct AwTensor {
@@ -52,7 +53,7 @@ struct AwBegin {
 template <int COUNT> struct AwParams {
   int count;
   int64_t tiles;
-  int turns;                    // of a tile: AW_THREADS times 8 or 16 values each
+  int turns;                    // of a tile, AW_THREADS times AW_VALUES each
   float beta1, one_less_beta1, beta2, one_less_beta2, eps;
   float *m, *v;
   uint8_t *m_codes, *m_scales, *v_codes, *v_scales;
@@ -127,6 +128,13 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t x) {
   x = (x ^ x >> 15) * 0x5DE0A3B7u;
   return x ^ x >> 16;
 }
+// mix(place ^ key) of place = first + j, first a multiple of 8 and j below it, from base = mix_base(first ^ key)
+__device__ __forceinline__ uint32_t mix_base(uint32_t x) { return x ^ x >> 16; }
+__device__ __forceinline__ uint32_t mix_from(uint32_t base, uint32_t j) {
+  uint32_t x = (base ^ j) * 0xEE1F5725u;
+  x = (x ^ x >> 15) * 0x5DE0A3B7u;
+  return x ^ x >> 16;
+}
 __device__ __forceinline__ uint32_t key_of(uint64_t seed, uint64_t step) {
   uint32_t key = mix(0x2545F491u ^ (uint32_t)seed);
   key = mix(key ^ (uint32_t)(seed >> 32));
@@ -135,7 +143,12 @@ __device__ __forceinline__ uint32_t key_of(uint64_t seed, uint64_t step) {
 }
 
 // ---- moments in 8 bits -----------------------------------------------------------------------------------------
-constexpr int AW_PACKED = 16;   // values of a lane: four lanes a group
+constexpr int AW_LANES = KEEP_GROUP / AW_VALUES;
+struct AwCodes {
+  uint32_t q[AW_VALUES / 4];
+  __device__ __forceinline__ void get(const uint8_t* p) { memcpy(q, __builtin_assume_aligned(p, 8), 8); }
+  __device__ __forceinline__ void put(uint8_t* p) const { memcpy(__builtin_assume_aligned(p, 8), q, 8); }
+};
 // A value times 2^-120 over its group's scale has the e4m3 code in bits 20 to 26 of its fp32 pattern, subnormal codes among
 // them (they are subnormal there as well), and the fraction of a step in the 20 bits below.  The pattern moved up by four bits
 // plus 2^8 r, with r of 16 bits, has the rounded code in its highest byte.
@@ -143,29 +156,28 @@ constexpr uint32_t AW_BITS_LOW = 0x4104u, AW_BITS_HIGH = 0x4324u;   // selectors
 __device__ __forceinline__ uint32_t highest_bytes(const uint32_t y[4]) {
   return __byte_perm(__byte_perm(y[0], y[1], 0x0073), __byte_perm(y[2], y[3], 0x0073), 0x5410);
 }
-// Codes of a lane's 16 values; byte: their group's scale byte.  ROOT: nothing is negative, and what is above zero stays above zero.
-template <bool ROOT> __device__ __forceinline__ uint4 encode_at_random(float2 f[AW_PACKED / 2], const uint32_t r[AW_PACKED], uint32_t byte) {
+// Codes of a lane's values; byte: their group's scale byte.  ROOT: nothing is negative, and what is above zero stays above zero.
+template <bool ROOT> __device__ __forceinline__ AwCodes encode_at_random(float2 f[AW_VALUES / 2], const uint32_t r[AW_VALUES], uint32_t byte) {
   // 2^-120 over the scale, 2^(7 - byte); where that is subnormal, 2^-126 of it beforehand
   const bool far = byte > 133u;
   if (__any_sync(0xffffffffu, far)) {
 #pragma unroll
-    for (int k = 0; k < AW_PACKED / 2; ++k) {
+    for (int k = 0; k < AW_VALUES / 2; ++k) {
       const float2 down = mul_pair(f[k], both(0x1p-126f));
-      const float2 least = ROOT ? make_float2(f[k].x > 0.f ? 0x1p-100f : 0.f, f[k].y > 0.f ? 0x1p-100f : 0.f) : both(0.f);
+      const float2 least = make_float2(f[k].x > 0.f ? 0x1p-100f : 0.f, f[k].y > 0.f ? 0x1p-100f : 0.f);
       if (far) f[k] = ROOT ? make_float2(fmaxf(down.x, least.x), fmaxf(down.y, least.y)) : down;
     }
   }
   const float factor = __uint_as_float((far ? 260u - byte : 134u - byte) << 23);
-  uint32_t q[AW_PACKED / 4];
+  AwCodes c;
 #pragma unroll
-  for (int k = 0; k < AW_PACKED / 4; ++k) {
+  for (int k = 0; k < AW_VALUES / 4; ++k) {
     uint32_t y[4];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const float2 u = mul_pair(f[2 * k + j], both(factor));
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t t = __float_as_uint(h ? u.y : u.x), random = __byte_perm(r[4 * k + 2 * j + h], 0u, ROOT ? AW_BITS_HIGH : AW_BITS_LOW);
+        const uint32_t t = __float_as_uint((h ? f[2 * k + j].y : f[2 * k + j].x) * factor), random = __byte_perm(r[4 * k + 2 * j + h], 0u, ROOT ? AW_BITS_HIGH : AW_BITS_LOW);
         uint32_t v = (t << 4) + random;
         if (ROOT)
           v = max(v, min(__float_as_uint(h ? f[2 * k + j].y : f[2 * k + j].x), 1u << 24));
@@ -174,23 +186,23 @@ template <bool ROOT> __device__ __forceinline__ uint4 encode_at_random(float2 f[
         y[2 * j + h] = v;
       }
     }
-    q[k] = highest_bytes(y);
+    c.q[k] = byte == 255u ? 0u : highest_bytes(y);
   }
-  return byte == 255u ? make_uint4(0u, 0u, 0u, 0u) : make_uint4(q[0], q[1], q[2], q[3]);
+  return c;
 }
-__device__ __forceinline__ void decode(float2 f[AW_PACKED / 2], const uint32_t codes[AW_PACKED / 4], uint32_t byte) {
-  const float scale = keep_scale_value(byte);
+// The e4m3 values of codes, without their scale.
+__device__ __forceinline__ void decode(float2 f[AW_VALUES / 2], const AwCodes& codes) {
 #pragma unroll
-  for (int k = 0; k < AW_PACKED / 2; ++k) {
-    const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes[k / 2] >> (16 * (k & 1))), __NV_E4M3)));
-    f[k] = mul_pair(v, both(scale));
+  for (int k = 0; k < AW_VALUES / 2; ++k) {
+    const uint32_t two = codes.q[k / 2] >> (16 * (k & 1));
+    f[k] = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3)));
   }
 }
-__device__ __forceinline__ uint32_t top_of(const float2 f[AW_PACKED / 2]) {
+__device__ __forceinline__ uint32_t top_of(const float2 f[AW_VALUES / 2]) {
   float m = 0.f;
 #pragma unroll
-  for (int k = 0; k < AW_PACKED / 2; ++k) m = larger_of(m, f[k]);
-  return group_top<KEEP_GROUP / AW_PACKED>(m);
+  for (int k = 0; k < AW_VALUES / 2; ++k) m = larger_of(m, f[k]);
+  return group_top<AW_LANES>(m);
 }
 // Square roots by the hardware's approximation of 1 / sqrt(v) and one step of Newton's iteration from the residual v - s^2, which
 // leaves them correctly rounded but for a few; of numbers below 2^-126 they are too small.
@@ -198,8 +210,8 @@ __device__ __forceinline__ float2 root_of(float2 v) {
   float2 y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, 0x1p-126f)));
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(v.y, 0x1p-126f)));
-  const float2 s = mul_pair(v, y), off = fma_pair(make_float2(-s.x, -s.y), s, v);
-  return fma_pair(mul_pair(off, both(0.5f)), y, s);
+  const float2 s = mul_pair(v, y);
+  return fma_pair(make_float2(fmaf(-s.x, s.x, v.x) * 0.5f, fmaf(-s.y, s.y, v.y) * 0.5f), y, s);
 }
 __device__ __forceinline__ float reciprocal(float v) {
   float r;
@@ -208,27 +220,43 @@ __device__ __forceinline__ float reciprocal(float v) {
 }
 
 // ---- kernels -------------------------------------------------------------------------------------------------
+// Where a block's values lie: tiles of tensors, the turns of each.
+template <int COUNT> struct AwWalk {
+  int64_t tile, first;   // first place of the tile
+  int turn, tensor;
+  __device__ __forceinline__ void seek(const AwParams<COUNT>& a) {
+    if (tile < 0 || tile >= a.tiles) return;
+    tensor = tensor_of(a, tile);
+    first = (tile - a.t[tensor].tile) * a.turns * (AW_THREADS * AW_VALUES);
+    turn = 0;
+  }
+  __device__ __forceinline__ AwWalk(const AwParams<COUNT>& a, int64_t from) : tile(from), first(0), turn(0), tensor(0) { seek(a); }
+  __device__ __forceinline__ int64_t place() const { return first + (turn * AW_THREADS + (int)threadIdx.x) * AW_VALUES; }
+  // (a turn in which the warp has no values ends the tile)
+  __device__ __forceinline__ void go_on(const AwParams<COUNT>& a, int64_t step) {
+    if (++turn < a.turns && first + (turn * AW_THREADS + (int)(threadIdx.x & ~31u)) * AW_VALUES < a.t[tensor].n) return;
+    tile += step;
+    seek(a);
+  }
+};
+
 // Sums of squares of the gradients, a block's share in 64 bits.
-template <int COUNT, int N> __global__ void __launch_bounds__(AW_THREADS) adamw_norm_kernel(const __grid_constant__ AwParams<COUNT> a, int first) {
+template <int COUNT> __global__ void __launch_bounds__(AW_THREADS) adamw_norm_kernel(const __grid_constant__ AwParams<COUNT> a, int first) {
   let_next_kernel_start();
   double sum = 0.0;
-  for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-    const AwTensor& t = a.t[tensor_of(a, tile)];
-    const int64_t n = t.n;
-    int64_t i = ((tile - t.tile) * a.turns * AW_THREADS + threadIdx.x) * N;
-    for (int turn = 0; turn < a.turns && i < n; ++turn, i += AW_THREADS * N) {
-      float2 g[N / 2];
-      load_values<N>(g, t.g, t.g_dtype, i, n, t.vectors);
-      float2 s = both(0.f);
+  for (AwWalk<COUNT> at(a, blockIdx.x); at.tile < a.tiles; at.go_on(a, gridDim.x)) {
+    const AwTensor& t = a.t[at.tensor];
+    float2 g[AW_VALUES / 2];
+    load_values<AW_VALUES>(g, t.g, t.g_dtype, at.place(), t.n, t.vectors);
+    float2 s = both(0.f);
 #pragma unroll
-      for (int k = 0; k < N / 2; ++k) s = fma_pair(g[k], g[k], s);
-      const float here = s.x + s.y;
-      if (here >= 0x1p-100f && here <= 0x1p126f) {
-        sum += (double)here;
-        continue;
-      }
+    for (int k = 0; k < AW_VALUES / 2; ++k) s = fma_pair(g[k], g[k], s);
+    const float here = s.x + s.y;
+    if (here >= 0x1p-100f && here <= 0x1p126f) {
+      sum += (double)here;
+    } else {   // squares beyond the range of fp32
 #pragma unroll
-      for (int k = 0; k < N / 2; ++k) sum += (double)g[k].x * g[k].x + (double)g[k].y * g[k].y;   // squares beyond the range of fp32
+      for (int k = 0; k < AW_VALUES / 2; ++k) sum += (double)g[k].x * g[k].x + (double)g[k].y * g[k].y;
     }
   }
 #pragma unroll
@@ -277,102 +305,220 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_begin_kernel(const AwBegin b
   *b.out = s;
 }
 
-// EIGHT: moments in 8 bits.
-template <int COUNT, bool EIGHT> __global__ void __launch_bounds__(AW_THREADS) adamw_update_kernel(const __grid_constant__ AwParams<COUNT> a) {
-  constexpr int N = EIGHT ? AW_PACKED : 8;
+__device__ __forceinline__ float2 times(float2 v, float factor) { return mul_pair(v, both(factor)); }
+
+// The step of a thread's parameters and their moments, of which b1 m and b2 v are at hand; g is spent.  On return v holds roots where
+// EIGHT.  Products and sums are rounded one by one: what is rounded at random afterwards is then what tensor operations, one after
+// the other, give as well.
+template <bool EIGHT, int N, int COUNT>
+__device__ __forceinline__ void step_values(const AwParams<COUNT>& a, const AwStep& step, float2 p[N / 2], float2 g[N / 2], float2 m[N / 2], float2 v[N / 2]) {
+  float2 root[N / 2];
+  if (step.factor != 1.f) {
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) g[k] = times(g[k], step.factor);
+  }
+#pragma unroll
+  for (int k = 0; k < N / 2; ++k) {
+    m[k] = add_pair(m[k], times(g[k], a.one_less_beta1));
+    v[k] = add_pair(v[k], times(mul_pair(g[k], g[k]), a.one_less_beta2));
+    root[k] = EIGHT ? root_of(v[k]) : make_float2(__fsqrt_rn(v[k].x), __fsqrt_rn(v[k].y));
+  }
+  if constexpr (EIGHT) {
+    // where all of a thread's roots are below 2^-44, squares may be subnormal (one that is beside a larger root has the smallest
+    // code or none either way)
+    float top = 0.f;
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) top = larger_of(top, root[k]);
+    if (top > 0.f && top < 0x1p-44f) {
+#pragma unroll
+      for (int k = 0; k < N / 2; ++k) root[k] = make_float2(__fsqrt_rn(v[k].x), __fsqrt_rn(v[k].y));
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < N / 2; ++k) {
+    const float2 below = fma_pair(root[k], both(step.root), both(a.eps)), up = times(m[k], -step.rate);
+    const float2 update = EIGHT ? mul_pair(up, make_float2(reciprocal(below.x), reciprocal(below.y)))
+                                : make_float2(__fdividef(up.x, below.x), __fdividef(up.y, below.y));
+    p[k] = fma_pair(p[k], both(step.keep), update);
+    if (EIGHT) v[k] = root[k];
+  }
+}
+
+// Moments in fp32.
+template <int COUNT> __global__ void __launch_bounds__(AW_THREADS, 4) adamw_update_kernel(const __grid_constant__ AwParams<COUNT> a) {
   wait_for_kernel_before();
   const AwStep step = *a.step;
   if (step.skip) return;
   // from the last tile to the first: where the gradients have just been read for their norm, the last of them are in L2
+  for (AwWalk<COUNT> at(a, a.tiles - 1 - blockIdx.x); at.tile >= 0; at.go_on(a, -(int64_t)gridDim.x)) {
+    const AwTensor& t = a.t[at.tensor];
+    const int64_t i = at.place(), state = t.state + i, n = t.n;
+    if (i >= n) continue;
+    float2 p[AW_VALUES / 2], g[AW_VALUES / 2], m[AW_VALUES / 2], v[AW_VALUES / 2];
+    load_values<AW_VALUES>(p, t.p, t.p_dtype, i, n, t.vectors);
+    load_values<AW_VALUES>(g, t.g, t.g_dtype, i, n, t.vectors);
+    Unit<float, AW_VALUES> b;
+    b.get(a.m + state);
+#pragma unroll
+    for (int k = 0; k < AW_VALUES / 2; ++k) m[k] = times(b.pair(k), a.beta1);
+    b.get(a.v + state);
+#pragma unroll
+    for (int k = 0; k < AW_VALUES / 2; ++k) v[k] = times(b.pair(k), a.beta2);
+    step_values<false, AW_VALUES>(a, step, p, g, m, v);
+    store_values<AW_VALUES>(p, t.p, t.p_dtype, i, n, t.vectors);
+    if (t.copy) store_values<AW_VALUES>(p, t.copy, t.copy_dtype, i, n, t.vectors);
+#pragma unroll
+    for (int k = 0; k < AW_VALUES / 2; ++k) b.set(k, m[k]);
+    b.put(a.m + state);
+#pragma unroll
+    for (int k = 0; k < AW_VALUES / 2; ++k) b.set(k, v[k]);
+    b.put(a.v + state);
+  }
+}
+
+// Moments in 8 bits: bound by instructions (50 a parameter) rather than by HBM.
+// b1 m and b2 v from their codes.  The scale is a power of two, so that it can be multiplied by b1 or b2 first: the product with a
+// value (or with its square, which is exact) is rounded once either way.  Where the square of a scale leaves the range, one
+// by one.
+template <int COUNT>
+__device__ __forceinline__ void read_moments(const AwParams<COUNT>& a, float2 m[AW_VALUES / 2], float2 v[AW_VALUES / 2], const AwCodes& m_codes, const AwCodes& v_codes, uint32_t m_byte, uint32_t v_byte) {
+  decode(m, m_codes);
+  decode(v, v_codes);
+  const float m_scale = keep_scale_value(m_byte) * a.beta1, v_scale = keep_scale_value(v_byte);
+#pragma unroll
+  for (int k = 0; k < AW_VALUES / 2; ++k) m[k] = times(m[k], m_scale), v[k] = mul_pair(v[k], v[k]);
+  if (v_byte - 80u < 96u) {   // scales from 2^-47 to 2^48
+    const float square = v_scale * v_scale * a.beta2;
+#pragma unroll
+    for (int k = 0; k < AW_VALUES / 2; ++k) v[k] = times(v[k], square);
+  } else {
+#pragma unroll
+    for (int k = 0; k < AW_VALUES / 2; ++k) v[k] = times(times(times(v[k], v_scale), v_scale), a.beta2);
+  }
+}
+// The moments back to codes and scale bytes; the lanes of a warp do this together.
+struct AwPacked {
+  AwCodes m, v;
+  uint32_t m_byte, v_byte;
+};
+__device__ __forceinline__ AwPacked pack_moments(const AwStep& step, int64_t at, float2 m[AW_VALUES / 2], float2 root[AW_VALUES / 2]) {
+  AwPacked k;
+  k.v_byte = keep_scale_byte<SNN_KEEP_E4M3>(top_of(root)), k.m_byte = keep_scale_byte<SNN_KEEP_E4M3>(top_of(m));
+  uint32_t r[AW_VALUES];
+  const uint32_t base = mix_base((uint32_t)at ^ step.key ^ mix((uint32_t)(at >> 32)));
+#pragma unroll
+  for (int j = 0; j < AW_VALUES; ++j) r[j] = mix_from(base, j);
+  k.m = encode_at_random<false>(m, r, k.m_byte), k.v = encode_at_random<true>(root, r, k.v_byte);
+  return k;
+}
+constexpr int AW_STEP = 32 * AW_VALUES;   // of a warp and turn
+static_assert(AW_TURNS * AW_STEP == 32 * KEEP_GROUP, "a scale byte of a part for each lane");
+// A warp's part of a tile: 2048 values one behind the other (AW_TURNS a tile, where there are that many turns), or what a tensor's
+// end leaves of them.  types: those of parameters and gradients where all values exist and vectors fit them, otherwise -1.
+template <int COUNT> struct AwPart {
+  const AwTensor* t;
+  int64_t tile, first;
+  int types;
+  __device__ __forceinline__ AwPart(const AwParams<COUNT>& a, int64_t at) : t(nullptr), tile(at), first(0), types(-1) {
+    if (tile < 0) return;
+    t = &a.t[tensor_of(a, tile)];
+    const int64_t part = (int64_t)a.turns * AW_STEP;
+    first = ((tile - t->tile) * (AW_THREADS / 32) + (threadIdx.x >> 5)) * part;
+    if (a.turns == AW_TURNS && t->vectors && first + part <= t->n) types = t->p_dtype * 3 + t->g_dtype;
+  }
+  __device__ __forceinline__ static constexpr int of(int p, int g) { return p * 3 + g; }
+};
+// A whole part in these types.  The 32 scale bytes are read and written at once, lane by lane: stores of parts of a 32-byte sector
+// cost L2 so much that 70 M parameters took 199 us with four bytes a warp and turn (119 us against 351 where nothing was
+// computed).
+template <typename PT, typename GT, int COUNT>
+__device__ __forceinline__ void update_part(const AwParams<COUNT>& a, const AwStep& step, const AwPart<COUNT>& part) {
+  const AwTensor& t = *part.t;
+  const int lane = threadIdx.x & 31;
+  const int64_t begin = part.first + lane * AW_VALUES, group0 = (t.state + part.first) / KEEP_GROUP + lane;
+  PT* to = (PT*)t.p + begin;
+  const GT* from = (const GT*)t.g + begin;
+  int64_t at = t.state + begin;
+  const uint32_t m_bytes = a.m_scales[group0], v_bytes = a.v_scales[group0];
+  uint32_t m_new = 0u, v_new = 0u;
+#pragma unroll 1
+  for (int turn = 0; turn < AW_TURNS; ++turn) {
+    constexpr int GROUPS = 32 / AW_LANES;   // of a turn
+    Unit<PT, AW_VALUES> up;
+    Unit<GT, AW_VALUES> ug;
+    AwCodes m_codes, v_codes;
+    up.get(to);
+    ug.get(from);
+    m_codes.get(a.m_codes + at);
+    v_codes.get(a.v_codes + at);
+    float2 p[AW_VALUES / 2], g[AW_VALUES / 2], m[AW_VALUES / 2], v[AW_VALUES / 2];
+#pragma unroll
+    for (int k = 0; k < AW_VALUES / 2; ++k) p[k] = up.pair(k), g[k] = ug.pair(k);
+    const int group = turn * GROUPS + lane / AW_LANES;
+    read_moments(a, m, v, m_codes, v_codes, __shfl_sync(0xffffffffu, m_bytes, group), __shfl_sync(0xffffffffu, v_bytes, group));
+    step_values<true, AW_VALUES>(a, step, p, g, m, v);
+#pragma unroll
+    for (int k = 0; k < AW_VALUES / 2; ++k) up.set(k, p[k]);
+    up.put(to);
+    if (t.copy) store_values<AW_VALUES>(p, t.copy, t.copy_dtype, begin + turn * AW_STEP, t.n, true);
+    const AwPacked k = pack_moments(step, at, m, v);
+    k.m.put(a.m_codes + at);
+    k.v.put(a.v_codes + at);
+    const uint32_t m_here = __shfl_sync(0xffffffffu, k.m_byte, lane % GROUPS * AW_LANES), v_here = __shfl_sync(0xffffffffu, k.v_byte, lane % GROUPS * AW_LANES);
+    if (lane / GROUPS == turn) m_new = m_here, v_new = v_here;
+    to += AW_STEP, from += AW_STEP, at += AW_STEP;
+  }
+  a.m_scales[group0] = (uint8_t)m_new;
+  a.v_scales[group0] = (uint8_t)v_new;
+}
+// A thread's values up to place n: at a tensor's end, or where vectors do not fit, or another mixture of types.  What lies behind
+// n is zero, also to the group.
+template <int COUNT> __device__ __noinline__ void update_any(const AwParams<COUNT>& a, const AwStep& step, const AwTensor& t, int64_t i, int64_t n) {
+  const int64_t at = t.state + i;
+  float2 p[AW_VALUES / 2], g[AW_VALUES / 2], m[AW_VALUES / 2], v[AW_VALUES / 2];
+#pragma unroll
+  for (int k = 0; k < AW_VALUES / 2; ++k) m[k] = v[k] = both(0.f);
+  if (i < n) {
+    load_values<AW_VALUES>(p, t.p, t.p_dtype, i, n, t.vectors);
+    load_values<AW_VALUES>(g, t.g, t.g_dtype, i, n, t.vectors);
+    AwCodes m_codes, v_codes;
+    m_codes.get(a.m_codes + at);
+    v_codes.get(a.v_codes + at);
+    read_moments(a, m, v, m_codes, v_codes, a.m_scales[at / KEEP_GROUP], a.v_scales[at / KEEP_GROUP]);
+    step_values<true, AW_VALUES>(a, step, p, g, m, v);
+    store_values<AW_VALUES>(p, t.p, t.p_dtype, i, n, t.vectors);
+    if (t.copy) store_values<AW_VALUES>(p, t.copy, t.copy_dtype, i, n, t.vectors);
+  }
+#pragma unroll
+  for (int k = 0; k < AW_VALUES / 2; ++k) {
+    if (i + 2 * k >= n) m[k].x = v[k].x = 0.f;
+    if (i + 2 * k + 1 >= n) m[k].y = v[k].y = 0.f;
+  }
+  const AwPacked k = pack_moments(step, at, m, v);
+  if ((i & ~(int64_t)(KEEP_GROUP - 1)) >= n) return;
+  k.m.put(a.m_codes + at);
+  k.v.put(a.v_codes + at);
+  if (threadIdx.x % AW_LANES == 0) a.m_scales[at / KEEP_GROUP] = (uint8_t)k.m_byte, a.v_scales[at / KEEP_GROUP] = (uint8_t)k.v_byte;
+}
+template <int COUNT> __global__ void __launch_bounds__(AW_THREADS, 4) adamw_update_packed_kernel(const __grid_constant__ AwParams<COUNT> a) {
+  using BF = __nv_bfloat16;
+  using Part = AwPart<COUNT>;
+  wait_for_kernel_before();
+  const AwStep step = *a.step;
+  if (step.skip) return;
   for (int64_t tile = a.tiles - 1 - blockIdx.x; tile >= 0; tile -= gridDim.x) {
-    const AwTensor& t = a.t[tensor_of(a, tile)];
-    const int64_t n = t.n, first = (tile - t.tile) * a.turns * (AW_THREADS * N), state = t.state;
-    for (int turn = 0; turn < a.turns; ++turn) {
-      const int64_t i = first + (turn * AW_THREADS + (int)threadIdx.x) * N, at = state + i;
-      // (in 8 bits the lanes of a group work together: those behind the tensor's end hold zeros)
-      const bool here = i < n, group = (i & ~(int64_t)(KEEP_GROUP - 1)) < n;
-      if (!__any_sync(0xffffffffu, group)) break;
-      float2 p[N / 2], g[N / 2], m[N / 2], v[N / 2];
-#pragma unroll
-      for (int k = 0; k < N / 2; ++k) p[k] = g[k] = m[k] = v[k] = both(0.f);
-      if (here) {
-        load_values<N>(p, t.p, t.p_dtype, i, n, t.vectors);
-        load_values<N>(g, t.g, t.g_dtype, i, n, t.vectors);
-      }
-      if constexpr (EIGHT) {
-        if (group) {
-          uint32_t m_codes[4], v_codes[4];
-          get_16(m_codes, a.m_codes + at);
-          get_16(v_codes, a.v_codes + at);
-          const uint32_t m_byte = a.m_scales[at / KEEP_GROUP], v_byte = a.v_scales[at / KEEP_GROUP];
-          decode(m, m_codes, m_byte);
-          decode(v, v_codes, v_byte);
-        }
-      } else if (here) {
-        Unit<float, N> b;
-        b.get(a.m + at);
-#pragma unroll
-        for (int k = 0; k < N / 2; ++k) m[k] = b.pair(k);
-        b.get(a.v + at);
-#pragma unroll
-        for (int k = 0; k < N / 2; ++k) v[k] = b.pair(k);
-      }
-#pragma unroll
-      for (int k = 0; k < N / 2; ++k) {
-        g[k] = mul_pair(g[k], both(step.factor));
-        // (products and sums are rounded one by one: what is rounded at random afterwards is then what tensor operations, one
-        // after the other, give as well)
-        m[k] = add_pair(mul_pair(m[k], both(a.beta1)), mul_pair(g[k], both(a.one_less_beta1)));
-        if (EIGHT) v[k] = mul_pair(v[k], v[k]);
-        v[k] = add_pair(mul_pair(v[k], both(a.beta2)), mul_pair(mul_pair(g[k], g[k]), both(a.one_less_beta2)));
-        const float2 root = EIGHT ? root_of(v[k]) : make_float2(__fsqrt_rn(v[k].x), __fsqrt_rn(v[k].y));
-        const float2 below = fma_pair(root, both(step.root), both(a.eps)), up = mul_pair(m[k], both(-step.rate));
-        const float2 update = EIGHT ? mul_pair(up, make_float2(reciprocal(below.x), reciprocal(below.y)))
-                                    : make_float2(__fdividef(up.x, below.x), __fdividef(up.y, below.y));
-        p[k] = fma_pair(p[k], both(step.keep), update);
-        if (EIGHT) g[k] = v[k], v[k] = root;   // (the root is what is kept)
-      }
-      if (here) {
-        store_values<N>(p, t.p, t.p_dtype, i, n, t.vectors);
-        if (t.copy) store_values<N>(p, t.copy, t.copy_dtype, i, n, t.vectors);
-      }
-      if constexpr (EIGHT) {
-        if (i + N > n) {   // what lies behind the tensor's end is nothing to its group
-#pragma unroll
-          for (int k = 0; k < N / 2; ++k) {
-            if (i + 2 * k >= n) m[k].x = v[k].x = 0.f;
-            if (i + 2 * k + 1 >= n) m[k].y = v[k].y = 0.f;
-          }
-        }
-        uint32_t top = top_of(v);
-        if (__any_sync(0xffffffffu, top - 1u < (83u << 23) - 1u)) {   // roots below 2^-44, but not zero: squares may be subnormal
-#pragma unroll
-          for (int k = 0; k < N / 2; ++k) {
-            if (v[k].x > 0.f) v[k].x = __fsqrt_rn(g[k].x);
-            if (v[k].y > 0.f) v[k].y = __fsqrt_rn(g[k].y);
-          }
-          top = top_of(v);
-        }
-        const uint32_t v_byte = keep_scale_byte<SNN_KEEP_E4M3>(top), m_byte = keep_scale_byte<SNN_KEEP_E4M3>(top_of(m));
-        uint32_t r[N];
-        const uint32_t key = step.key ^ mix((uint32_t)(at >> 32));
-#pragma unroll
-        for (int j = 0; j < N; ++j) r[j] = mix((uint32_t)(at + j) ^ key);
-        const uint4 m_codes = encode_at_random<false>(m, r, m_byte), v_codes = encode_at_random<true>(v, r, v_byte);
-        if (group) {
-          *reinterpret_cast<uint4*>(a.m_codes + at) = m_codes;
-          *reinterpret_cast<uint4*>(a.v_codes + at) = v_codes;
-          if ((threadIdx.x & 3) == 0) a.m_scales[at / KEEP_GROUP] = (uint8_t)m_byte, a.v_scales[at / KEEP_GROUP] = (uint8_t)v_byte;
-        }
-      } else if (here) {
-        Unit<float, N> b;
-#pragma unroll
-        for (int k = 0; k < N / 2; ++k) b.set(k, m[k]);
-        b.put(a.m + at);
-#pragma unroll
-        for (int k = 0; k < N / 2; ++k) b.set(k, v[k]);
-        b.put(a.v + at);
-      }
+    const Part part(a, tile);
+    if (part.types == Part::of(SNN_DTYPE_BF16, SNN_DTYPE_BF16)) {
+      update_part<BF, BF>(a, step, part);
+    } else if (part.types == Part::of(SNN_DTYPE_FP32, SNN_DTYPE_FP32)) {
+      update_part<float, float>(a, step, part);
+    } else if (part.types == Part::of(SNN_DTYPE_FP32, SNN_DTYPE_BF16)) {
+      update_part<float, BF>(a, step, part);
+    } else if (part.types == Part::of(SNN_DTYPE_FP16, SNN_DTYPE_FP16)) {
+      update_part<__half, __half>(a, step, part);
+    } else {
+      const int64_t n = min(part.first + (int64_t)a.turns * AW_STEP, part.t->n);
+      for (int64_t i = part.first; i < n; i += AW_STEP) update_any(a, step, *part.t, i + (threadIdx.x & 31) * AW_VALUES, n);
     }
   }
 }
@@ -398,7 +544,7 @@ static_assert(256 + AW_NORM_BLOCKS * 8 <= AW_WORKSPACE && sizeof(AwStep) <= 256,
 // The launches of one list of tensors, as many at a time as the table holds.
 template <int COUNT, typename F> snn_status in_tables(const snn_adamw_args* a, const AwParams<COUNT>& common, F&& launch) {
   AwParams<COUNT> p = common;
-  const int64_t tile = (int64_t)AW_THREADS * (a->moment_format == SNN_KEEP_RAW ? 8 : AW_PACKED) * p.turns;
+  const int64_t tile = (int64_t)AW_THREADS * AW_VALUES * p.turns;
   int64_t state = 0;
   bool first = true;
   for (int k = 0; k < a->count;) {
@@ -430,12 +576,12 @@ template <int COUNT> snn_status step_of(const snn_adamw_args* a, cudaStream_t st
   // tiles of several turns share what it takes to find them, where there are enough of them for every SM
   int64_t values = 0;
   for (int k = 0; k < a->count; ++k) values += a->tensors[k].n;
-  p.turns = values >= (int64_t)148 * 8 * AW_MOST_TURNS * AW_THREADS * AW_PACKED ? AW_MOST_TURNS : 1;
+  p.turns = values >= (int64_t)148 * 4 * AW_TURNS * AW_THREADS * AW_VALUES ? AW_TURNS : 1;
   if (clips) {
     bool any = false;
     const snn_status st = in_tables(a, p, [&](const AwParams<COUNT>& q, bool first) {
       any = true;
-      return launch_behind(eight ? adamw_norm_kernel<COUNT, AW_PACKED> : adamw_norm_kernel<COUNT, 8>, AW_NORM_BLOCKS, AW_THREADS, 0, stream, false, q, (int)first);
+      return launch_behind(adamw_norm_kernel<COUNT>, AW_NORM_BLOCKS, AW_THREADS, 0, stream, false, q, (int)first);
     });
     if (st != SNN_OK) return st;
     if (!any && cudaMemsetAsync(p.partial, 0, AW_NORM_BLOCKS * 8, stream) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
@@ -445,9 +591,8 @@ template <int COUNT> snn_status step_of(const snn_adamw_args* a, cudaStream_t st
   snn_status st = launch_behind(adamw_begin_kernel, 1, AW_THREADS, 0, stream, false, b);
   if (st != SNN_OK) return st;
   return in_tables(a, p, [&](const AwParams<COUNT>& q, bool first) {
-    const unsigned blocks = (unsigned)std::min<int64_t>(q.tiles, 148 * 8);
-    return eight ? launch_behind(adamw_update_kernel<COUNT, true>, blocks, AW_THREADS, 0, stream, first, q)
-                                             : launch_behind(adamw_update_kernel<COUNT, false>, blocks, AW_THREADS, 0, stream, first, q);
+    if (eight) return launch_behind(adamw_update_packed_kernel<COUNT>, (unsigned)std::min<int64_t>(q.tiles, 148 * 4), AW_THREADS, 0, stream, first, q);
+    return launch_behind(adamw_update_kernel<COUNT>, (unsigned)std::min<int64_t>(q.tiles, 148 * 8), AW_THREADS, 0, stream, first, q);
   });
 }
 }  // namespace
@@ -468,7 +613,7 @@ extern "C" snn_status snn_adamw_step(const snn_adamw_args* a, void* stream) {
   for (int k = 0; k < a->count; ++k) any = any || a->tensors[k].n > 0;
   if (any && a->moment_format == SNN_KEEP_RAW && (!a->m || !a->v || !aligned_to(a->m, 32) || !aligned_to(a->v, 32))) return SNN_ERR_INVALID_ARG;
   if (any && a->moment_format == SNN_KEEP_E4M3 &&
-      (!a->m_codes || !a->v_codes || !a->m_scales || !a->v_scales || !aligned_to(a->m_codes, 16) || !aligned_to(a->v_codes, 16)))
+      (!a->m_codes || !a->v_codes || !a->m_scales || !a->v_scales || !aligned_to(a->m_codes, 8) || !aligned_to(a->v_codes, 8)))
     return SNN_ERR_INVALID_ARG;
   if (a->workspace_bytes < AW_WORKSPACE) return SNN_ERR_WORKSPACE_TOO_SMALL;
   // a launch carries its table of tensors: a small one for the usual lists, a large one for long lists

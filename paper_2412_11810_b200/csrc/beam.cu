@@ -56,11 +56,6 @@ __device__ __forceinline__ bool goes_on(const BeamParams& p, int64_t row) {
   return !(p.ended && p.ended[row]) && fabsf(p.scores[row]) <= largest_finite<float>();
 }
 
-// Copies of 16 bytes from global to shared memory that the thread does not wait for.
-__device__ __forceinline__ void copy_16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
-__device__ __forceinline__ void close_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int OPEN> __device__ __forceinline__ void wait_groups() { asm volatile("cp.async.wait_group %0;" ::"n"(OPEN) : "memory"); }
-
 // A segment's place in shared memory, and the values of a thread: fp32 classes tid + 256 j, 16-bit ones 2 tid + 512 j and the
 // next, whatever the address of the row (so that equal rows have equal sums).  The bytes lie as in the row, 16 by 16: class 0
 // of the segment stands `lead` values behind the start.

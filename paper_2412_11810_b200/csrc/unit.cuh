@@ -140,6 +140,12 @@ template <bool FAST, typename T, int N> __device__ __forceinline__ void store_un
     v.put(p);
 }
 
+// ---- copies to shared memory ----------------------------------------------------------------------------------
+// Copies of 16 bytes from global to shared memory that the thread does not wait for.
+__device__ __forceinline__ void copy_16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void close_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int OPEN> __device__ __forceinline__ void wait_groups() { asm volatile("cp.async.wait_group %0;" ::"n"(OPEN) : "memory"); }
+
 // ---- 8-bit codes of a group ------------------------------------------------------------------------------------
 // Largest magnitude of a group as a bit pattern, from that of its lanes; NaN sorts above infinity above the rest.
 template <int LANES> __device__ __forceinline__ uint32_t group_top(float m) {

@@ -63,8 +63,16 @@ template <typename IO, int VALUES> struct Segment {
   static constexpr int CLASSES = BM_THREADS * VALUES, PER_COPY = 16 / sizeof(IO), BYTES = CLASSES * sizeof(IO) + 32;
   // Starts the copies of classes c0 .. of a row of V; 16 bytes that reach beyond the row's ends are read value by value.
   static __device__ __forceinline__ void fetch(uint8_t* to, const IO* z, int64_t c0, int V) {
-    const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO)), here = (int)min((int64_t)CLASSES, V - c0);
-    const int copies = (lead + here + PER_COPY - 1) / PER_COPY;
+    const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO));
+    if (c0 >= lead && c0 + CLASSES + PER_COPY <= V) {   // all of them lie within the row
+      const uint32_t at = (uint32_t)__cvta_generic_to_shared(to) + 16 * threadIdx.x;
+      const IO* const from = z + c0 - lead + PER_COPY * (int)threadIdx.x;
+#pragma unroll
+      for (int i = 0; i < CLASSES / PER_COPY / BM_THREADS; ++i) copy_16(at + 16 * BM_THREADS * i, from + PER_COPY * BM_THREADS * i);
+      if (lead && threadIdx.x == 0) copy_16(at + 16 * (CLASSES / PER_COPY), from + CLASSES);
+      return;
+    }
+    const int here = (int)min((int64_t)CLASSES, V - c0), copies = (lead + here + PER_COPY - 1) / PER_COPY;
     for (int i = threadIdx.x; i < copies; i += BM_THREADS) {
       const int64_t c = c0 + i * PER_COPY - lead;
       if (c >= 0 && c + PER_COPY <= V) {
@@ -81,9 +89,14 @@ template <typename IO, int VALUES> struct Segment {
     const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO)), here = (int)min((int64_t)CLASSES, V - c0);
     const IO none = from_f32<IO>(__uint_as_float(0xff800000u));
     const IO* const at = reinterpret_cast<const IO*>(from) + lead;
-    if (sizeof(IO) == 2 && lead % 2 == 0 && here == CLASSES) {
+    if (here == CLASSES) {
+      if (sizeof(IO) == 2 && lead % 2 == 0) {
 #pragma unroll
-      for (int i = 0; i < VALUES / 2; ++i) raw[i] = *reinterpret_cast<const Raw*>(at + place(2 * i));
+        for (int i = 0; i < VALUES / 2; ++i) raw[i] = *reinterpret_cast<const Raw*>(at + place(2 * i));
+      } else {
+#pragma unroll
+        for (int i = 0; i < VALUES / 2; ++i) raw[i].x = at[place(2 * i)], raw[i].y = at[place(2 * i + 1)];
+      }
       return;
     }
 #pragma unroll
@@ -104,15 +117,22 @@ __device__ __forceinline__ float exp2_of(float v) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v));
   return e;
 }
+// The largest of m and a pair, without notice of NaN.
+__device__ __forceinline__ float larger_number(float m, float2 v) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(m), "f"(v.x), "f"(v.y));
+  return d;
+}
 constexpr float LOG2_E = 1.4426950408889634f;
 
 // A block: `length` segments of a row, one behind the other through a ring of BM_STAGES places in shared memory.
-template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS, 4) beam_rows_kernel(const BeamParams p) {
+template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS, 3) beam_rows_kernel(const BeamParams p) {
   using Seg = Segment<IO, VALUES>;
   extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ float group_max[BM_GROUPS], warp_part[2][BM_THREADS / 32];
+  __shared__ __align__(16) float group_max[BM_GROUPS];
+  __shared__ float warp_part[2][BM_THREADS / 32];
   __shared__ uint32_t need;            // candidates are values v with rising(v) at or above it
-  __shared__ int count;                // candidates so far, the best `kept` of earlier segments first
+  __shared__ int count;                // candidates so far
   __shared__ uint64_t candidates[BM_CANDIDATES];
   let_next_kernel_start();
   const int64_t row = blockIdx.x / p.splits;
@@ -127,20 +147,40 @@ template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS,
   };
 #pragma unroll
   for (int s = 0; s < BM_STAGES - 1; ++s) fetch(s);
-  if (tid == 0) count = 0;
+  if (tid == 0) count = 0, need = 0;
   const float none = __uint_as_float(0xff800000u);
   float most = none, sum = 0.f;        // of this thread's values: the maximum, and the sum of exp(v - maximum)
-  int kept = 0;
+  int held = 0;                        // candidates before the segment
+  // the best `width` of the first n candidates, each to the place that the number of larger ones gives it
+  auto rank = [&](int n) {
+    uint64_t mine[BM_CANDIDATES / BM_THREADS];
+    int to[BM_CANDIDATES / BM_THREADS];
+#pragma unroll
+    for (int k = 0; k < BM_CANDIDATES / BM_THREADS; ++k) {
+      const int i = tid + k * BM_THREADS;
+      to[k] = p.W;
+      if (i >= n) continue;
+      mine[k] = candidates[i];
+      to[k] = 0;
+      for (int j = 0; j < n; ++j) to[k] += candidates[j] > mine[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < BM_CANDIDATES / BM_THREADS; ++k)
+      if (to[k] < p.W) candidates[to[k]] = mine[k];
+    __syncthreads();
+    return min(n, p.W);
+  };
+  wait_groups<BM_STAGES - 2>();
+  __syncthreads();
   for (int s = 0; s < segments; ++s) {
-    wait_groups<BM_STAGES - 2>();
-    __syncthreads();                   // the segment is there for all, and the one before it has been read by all
-    fetch(s + BM_STAGES - 1);
+    fetch(s + BM_STAGES - 1);          // (the segment before this one has been read by all)
     const int64_t c0 = first + (int64_t)s * Seg::CLASSES;
     Seg g;
     g.read(ring + s % BM_STAGES * Seg::BYTES, z, c0, p.V);
     float here = none;
 #pragma unroll
-    for (int i = 0; i < VALUES / 2; ++i) here = fmaxf(here, fmaxf(g.pair(i).x, g.pair(i).y));
+    for (int i = 0; i < VALUES / 2; ++i) here = larger_number(here, g.pair(i));
     if (here > most) {
       sum *= exp2_of((most - here) * LOG2_E);   // (0 of a sum that is 0)
       most = here;
@@ -150,11 +190,11 @@ template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS,
       float2 more = both(0.f);
 #pragma unroll
       for (int i = 0; i < VALUES / 2; ++i) {
-        const float2 d = mul2(add2(g.pair(i), both(-most)), both(LOG2_E));
-        more = add2(more, make_float2(exp2_of(d.x), exp2_of(d.y)));
+        const float2 d = mul_pair(add_pair(g.pair(i), both(-most)), both(LOG2_E));
+        more = add_pair(more, make_float2(exp2_of(d.x), exp2_of(d.y)));
       }
       sum += more.x + more.y;
-    } else {   // masked places alone, or NaN, of which fmaxf takes no notice
+    } else {   // masked places alone, or NaN, of which the maximum takes no notice
 #pragma unroll
       for (int i = 0; i < VALUES / 2; ++i)
         if (g.pair(i).x != g.pair(i).x || g.pair(i).y != g.pair(i).y) sum = __uint_as_float(0x7fc00000u);
@@ -167,53 +207,52 @@ template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS,
       __syncthreads();
       if (tid < BM_GROUPS) {
         const float mine = group_max[tid];
-        int before = 0;
-#pragma unroll 8
-        for (int j = 0; j < BM_GROUPS; ++j) before += group_max[j] > mine || (group_max[j] == mine && j < tid);
-        if (before == p.W - 1) need = rising(mine);
+        int reach = 0;
+#pragma unroll
+        for (int j = 0; j < BM_GROUPS; j += 4) {
+          const float4 other = *reinterpret_cast<const float4*>(group_max + j);
+          reach += (other.x >= mine) + (other.y >= mine) + (other.z >= mine) + (other.w >= mine);
+        }
+        if (reach >= p.W) atomicMax(&need, rising(mine));
       }
       __syncthreads();
     }
     const uint32_t bound = need;
-    bool pushed = false;
+    bool full = false;
     if (here > none && rising(here) >= bound) {
-      pushed = true;
 #pragma unroll
       for (int j = 0; j < VALUES; ++j) {
         const float v = g.value(j);
         if (v > none && rising(v) >= bound) {
           const int at = atomicAdd(&count, 1);
           if (at < BM_CANDIDATES) candidates[at] = key_of(v, (uint32_t)(c0 + Seg::place(j)));
+          full = full || at >= BM_CANDIDATES / 2;
         }
       }
     }
-    if (!__syncthreads_or(pushed)) continue;
+    wait_groups<BM_STAGES - 2>();      // the next segment is there, for all behind the barrier
+    full = __syncthreads_or(full);
     const int n = count;
+    if (!full) {
+      held = n;
+      continue;
+    }
+    int kept;
     if (n <= BM_CANDIDATES) {
-      // each of them goes to the place that the number of larger ones gives it
-      uint64_t mine[BM_CANDIDATES / BM_THREADS];
-      int to[BM_CANDIDATES / BM_THREADS];
-#pragma unroll
-      for (int k = 0; k < BM_CANDIDATES / BM_THREADS; ++k) {
-        const int i = tid + k * BM_THREADS;
-        to[k] = p.W;
-        if (i >= n) continue;
-        mine[k] = candidates[i];
-        to[k] = 0;
-        for (int j = 0; j < n; ++j) to[k] += candidates[j] > mine[k];
-      }
       __syncthreads();
-#pragma unroll
-      for (int k = 0; k < BM_CANDIDATES / BM_THREADS; ++k)
-        if (to[k] < p.W) candidates[to[k]] = mine[k];
-      kept = min(n, p.W);
+      kept = rank(n);
     } else {
-      // too many at or above the bound (equal values, or rising ones): the next best of all, one after the other
-      const uint64_t held = tid < kept ? candidates[tid] : 0;
+      // too many at or above the bound (equal values, or rising ones): the next best of the candidates that were there before
+      // and of all values of the segment, one after the other
+      uint64_t old[BM_CANDIDATES / 2 / BM_THREADS];
+#pragma unroll
+      for (int k = 0; k < BM_CANDIDATES / 2 / BM_THREADS; ++k) old[k] = tid + k * BM_THREADS < held ? candidates[tid + k * BM_THREADS] : 0;
       uint64_t last = ~(uint64_t)0;
-      int found = 0;
-      for (; found < p.W; ++found) {
-        uint64_t best = held < last ? held : 0;
+      for (kept = 0; kept < p.W; ++kept) {
+        uint64_t best = 0;
+#pragma unroll
+        for (int k = 0; k < BM_CANDIDATES / 2 / BM_THREADS; ++k)
+          if (old[k] < last && old[k] > best) best = old[k];
 #pragma unroll
         for (int j = 0; j < VALUES; ++j) {
           const float v = g.value(j);
@@ -226,18 +265,19 @@ template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS,
         __syncthreads();
         for (int k = 0; k < BM_THREADS / 32; ++k) best = max(best, candidates[BM_MOST + k]);
         if (!best) break;
-        if (tid == 0) candidates[found] = best;   // (what stood there is held by its thread)
+        if (tid == 0) candidates[kept] = best;   // (what stood there is held by its thread)
         last = best;
       }
-      kept = found;
+      __syncthreads();
     }
-    __syncthreads();
     if (tid == 0) {
       count = kept;
       if (kept == p.W) need = (uint32_t)(candidates[p.W - 1] >> 32) + 1;   // a later class has to be larger, not equal
     }
+    held = kept;
     __syncthreads();
   }
+  const int kept = rank(held);
   uint64_t* const out = p.keys + (row * p.splits + split) * p.W;
   if (tid < p.W) out[tid] = tid < kept ? candidates[tid] : 0;
   float m = most;
@@ -259,10 +299,12 @@ template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS,
 
 // A block per sample: the rows of its beams from their segments, a warp each, then the sample from its rows.
 __global__ void __launch_bounds__(32 * BM_JOIN_WARPS) beam_join_kernel(const BeamParams p) {
-  __shared__ uint64_t rows[BM_MOST][BM_MOST];   // the best of each beam
+  __shared__ uint64_t keys_of[BM_MOST * BM_MOST];   // the best of each beam, [K][W]
+  __shared__ uint64_t scores_of[BM_MOST * BM_MOST]; // their scores, as whole numbers that order alike; 0: none
   __shared__ float row_max[BM_MOST];
-  __shared__ double row_base[BM_MOST];          // score less log sum
+  __shared__ double row_base[BM_MOST];              // score less log sum
   __shared__ int64_t found[BM_MOST];
+  __shared__ int valid;
   extern __shared__ uint8_t heads_of_all[];
   let_next_kernel_start();
   wait_for_kernel_before();
@@ -274,7 +316,7 @@ __global__ void __launch_bounds__(32 * BM_JOIN_WARPS) beam_join_kernel(const Bea
     if (!goes_on(p, row)) {
       // an ended beam goes on with the end alone, at its own score
       const bool stays = p.ended && p.ended[row] && fabsf(p.scores[row]) <= largest_finite<float>();
-      for (int r = lane; r < p.W; r += 32) rows[k][r] = r == 0 && stays ? key_of(0.f, (uint32_t)p.end) : 0;
+      for (int r = lane; r < p.W; r += 32) keys_of[k * p.W + r] = r == 0 && stays ? key_of(0.f, (uint32_t)p.end) : 0;
       if (lane == 0) row_max[k] = 0.f, row_base[k] = (double)p.scores[row];
       continue;
     }
@@ -285,13 +327,19 @@ __global__ void __launch_bounds__(32 * BM_JOIN_WARPS) beam_join_kernel(const Bea
     double total = 0.0;
     for (int l = lane; l < p.splits; l += 32) {
       const float2 s = p.stats[row * p.splits + l];
-      if (s.y != 0.f) total += (double)s.y * exp((double)s.x - (double)m);   // (a segment without a value has a sum of zero)
+      if (s.y != 0.f) total += (double)s.y * (double)exp2_of((s.x - m) * LOG2_E);   // (a segment without a value has a sum of zero)
       heads[l] = 0;
     }
 #pragma unroll
     for (int o = 16; o > 0; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
     const bool alive = total > 0.0 && total < INFINITY;   // (not where it is NaN)
-    if (lane == 0) row_max[k] = m, row_base[k] = (double)p.scores[row] - log(total);
+    if (lane == 0) {
+      // log(2^e f) with f from 0.7 to 1.4, where the logarithm in fp32 is off by 2^-25 at most
+      int e;
+      double f = frexp(total, &e);
+      if (f < 0.70710678) f *= 2.0, --e;
+      row_max[k] = m, row_base[k] = (double)p.scores[row] - (e * 0.6931471805599453 + (double)logf((float)f) + (f - (double)(float)f) / f);
+    }
     __syncwarp();
     const uint64_t* const keys = p.keys + row * p.splits * p.W;
     // a lane looks after the lists lane, lane + 32, ..; the largest of their first keys is taken, `width` times.  Where it has
@@ -315,7 +363,7 @@ __global__ void __launch_bounds__(32 * BM_JOIN_WARPS) beam_join_kernel(const Bea
     }
     for (int r = 0; r < p.W; ++r) {
       const uint64_t best = alive ? warp_max(here) : 0;
-      if (lane == 0) rows[k][r] = best;
+      if (lane == 0) keys_of[k * p.W + r] = best;
       if (best && best == here) {
         if (one) {
           here = behind;
@@ -328,20 +376,22 @@ __global__ void __launch_bounds__(32 * BM_JOIN_WARPS) beam_join_kernel(const Bea
       __syncwarp();
     }
   }
+  if (threadIdx.x == 0) valid = 0;
   __syncthreads();
-  if (warp > 0) return;
-  // lane k looks after beam k; the lower beam first among equal scores
-  int next = 0, n = 0;
-  uint64_t here = 0, key = 0;
-  auto look = [&]() {
-    here = 0;
-    if (lane >= p.K || next >= p.W) return;
-    key = rows[lane][next];
-    if (!key) return;
-    const double score = row_base[lane] + ((double)from_rising((uint32_t)(key >> 32)) - (double)row_max[lane]);
-    const uint64_t u = (uint64_t)__double_as_longlong(score + 0.0);
-    here = u ^ ((uint64_t)((int64_t)u >> 63) | (uint64_t)1 << 63);
-  };
+  const int all = p.K * p.W;
+  for (int i = threadIdx.x; i < all; i += blockDim.x) {
+    const uint64_t key = keys_of[i];
+    const int k = i / p.W;
+    uint64_t order = 0;
+    if (key) {
+      const double score = row_base[k] + ((double)from_rising((uint32_t)(key >> 32)) - (double)row_max[k]) + 0.0;
+      const uint64_t u = (uint64_t)__double_as_longlong(score);
+      order = u ^ ((uint64_t)((int64_t)u >> 63) | (uint64_t)1 << 63);
+      atomicAdd(&valid, 1);
+    }
+    scores_of[i] = order;
+  }
+  __syncthreads();
   auto write = [&](int at, int64_t flat, float score) {
     const int64_t k = flat / p.V, c = flat % p.V, to = b * p.W + at;
     p.tokens[to] = c;
@@ -350,20 +400,22 @@ __global__ void __launch_bounds__(32 * BM_JOIN_WARPS) beam_join_kernel(const Bea
     if (p.new_ended) p.new_ended[to] = (p.ended && p.ended[b * p.K + k]) || c == p.end;
     found[at] = flat;
   };
-  look();
-  for (; n < p.W; ++n) {
-    const uint64_t best = warp_max(here);
-    if (!best) break;
-    if (lane == __ffs(__ballot_sync(0xffffffffu, here == best)) - 1) {
-      const uint64_t u = here & (uint64_t)1 << 63 ? here ^ (uint64_t)1 << 63 : ~here;
-      write(n, (int64_t)lane * p.V + class_of(key), (float)__longlong_as_double((int64_t)u));
-      ++next;
-      look();
-    }
-    __syncwarp();
+  // each to the place that the number of better ones gives it; of equal scores the lower beam's is first, and a beam's own list
+  // is in its order
+  for (int i = threadIdx.x; i < all; i += blockDim.x) {
+    const uint64_t order = scores_of[i];
+    if (!order) continue;
+    int before = 0;
+    for (int j = 0; j < all; ++j) before += scores_of[j] > order || (scores_of[j] == order && j < i);
+    if (before >= p.W) continue;
+    const uint64_t u = order & (uint64_t)1 << 63 ? order ^ (uint64_t)1 << 63 : ~order;
+    write(before, (int64_t)(i / p.W) * p.V + class_of(keys_of[i]), (float)__longlong_as_double((int64_t)u));
   }
-  if (n == p.W || lane > 0) return;
+  if (valid >= p.W) return;
+  __syncthreads();
+  if (threadIdx.x > 0) return;
   // fewer continuations than survivors: all of them are here, and the others, at -infinity, follow in their order
+  int n = valid;
   for (int64_t flat = 0; n < p.W; ++flat) {
     bool taken = false;
     for (int i = 0; i < n; ++i) taken = taken || found[i] == flat;
@@ -444,16 +496,16 @@ struct Split {
   int length, splits;
 };
 constexpr int WIDE = 16384 / BM_THREADS, NARROW = 8;   // bytes, values of a thread
-// Parts of four segments of 16 KB where there are rows enough to give every SM several of them, shorter ones for fewer rows: down
-// to one segment of 2048 classes, which are on their way at once in a block of their own.
+// Parts of as many segments of 16 KB as still give every SM a dozen of blocks, down to one; for fewer rows segments of 2048 classes,
+// again as many as still give it four, down to one, which are on their way at once in a block of their own.
 Split split_of(int64_t rows, int V, int dtype) {
-  const int64_t classes = (int64_t)BM_THREADS * WIDE / (int)dtype_size(dtype);
-  const int64_t segments = (V + classes - 1) / classes;
-  for (int64_t length = 4; length >= 1; length /= 2)
-    if (rows * ((segments + length - 1) / length) >= 148 * 4) return {true, (int)length, (int)((segments + length - 1) / length)};
-  const int64_t small = BM_THREADS * NARROW;
+  const int64_t classes = (int64_t)BM_THREADS * WIDE / (int)dtype_size(dtype), segments = (V + classes - 1) / classes;
+  for (int64_t length = 16; length >= 1; length /= 2)
+    if (rows * ((segments + length - 1) / length) >= 148 * (length > 1 ? 12 : 4)) return {true, (int)length, (int)((segments + length - 1) / length)};
+  const int64_t small = BM_THREADS * NARROW, count = (V + small - 1) / small;
   // (no more than 1024 parts, whose lists the joining kernel looks after)
-  const int64_t count = (V + small - 1) / small, length = (count + 1023) / 1024;
+  int64_t length = (count + 1023) / 1024;
+  while (rows * ((count + 2 * length - 1) / (2 * length)) >= 148 * 4) length *= 2;
   return {false, (int)length, (int)((count + length - 1) / length)};
 }
 snn_status check(const snn_beam_args* a) {

@@ -2,13 +2,13 @@
 //
 //   score(k, v) = s_k + (z_kv - m_k) - log sum_v exp(z_kv - m_k),  m_k = max_v z_kv;  the best `width` of a sample, lower k V + v first
 //
-// Bound by HBM: the logits are read once.  A thread block walks through a part of a beam's row, segment by segment, and leaves
+// Bound by HBM: the logits are read once.  A warp walks through a part of a beam's row, segment by segment of 2 KB, and leaves
 // behind its maximum, its sum of exponentials and its `width` best classes; a second kernel, a block per sample, joins the parts
-// of each row and the rows of the sample; a third moves the states.  Each is set up while the one before it runs.
+// of each row and the rows of the sample; a third moves the states.  Each is set up while the one before it runs.  (Blocks of
+// eight warps that worked at segments of 16 KB together waited for one another: 76 us for 512 rows of 131072 fp32 logits.)
 //
-// The best of a part: 64 groups of four lanes have a maximum each in the first segment, and the width-th largest of them is a
-// bound that at least `width` values reach: few more do (a dozen for eight), and those are ranked by comparing each with all.
-// From then on the width-th best so far is the bound, which few values of a later segment pass.
+// The best of a part: maxima that lanes have seen give a bound that at least `width` values of the row reach, and few more do.
+// What reaches it is put aside; where that gets too much, the best of it are kept and are the bound.
 // Keys hold the value above the complement of the class, so that no two are the same and ties go to the lower class.
 #include <algorithm>
 
@@ -18,7 +18,7 @@ using namespace snnk;
 
 namespace {
 
-constexpr int BM_THREADS = 256, BM_GROUPS = BM_THREADS / 4, BM_CANDIDATES = 1024, BM_STAGES = 3;
+constexpr int BM_WARPS = 8, BM_STAGES = 3, BM_CANDIDATES = 128;   // of a block; of a warp
 constexpr int BM_MOST = 32;          // beams of a sample, and survivors
 constexpr int BM_JOIN_WARPS = 8;
 constexpr int BM_TABLE = 64;         // states of one launch
@@ -26,7 +26,7 @@ constexpr int BM_COPY_THREADS = 256;
 constexpr int BM_PIECE = 16 * 1024, BM_PIECE_IN_PLACE = 1024;   // bytes of a row at a time
 
 struct BeamParams {
-  int64_t rows;
+  int64_t rows, parts;
   int K, W, V, splits, length;        // a row is cut into `splits` parts of `length` segments
   int64_t sample_stride, beam_stride, end;
   const void* logits;
@@ -56,24 +56,30 @@ __device__ __forceinline__ bool goes_on(const BeamParams& p, int64_t row) {
   return !(p.ended && p.ended[row]) && fabsf(p.scores[row]) <= largest_finite<float>();
 }
 
-// A segment's place in shared memory, and the values of a thread: fp32 classes tid + 256 j, 16-bit ones 2 tid + 512 j and the
-// next, whatever the address of the row (so that equal rows have equal sums).  The bytes lie as in the row, 16 by 16: class 0
-// of the segment stands `lead` values behind the start.
-template <typename IO, int VALUES> struct Segment {
-  static constexpr int CLASSES = BM_THREADS * VALUES, PER_COPY = 16 / sizeof(IO), BYTES = CLASSES * sizeof(IO) + 32;
+// The largest of m and a pair, without notice of NaN.
+__device__ __forceinline__ float larger_number(float m, float2 v) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(m), "f"(v.x), "f"(v.y));
+  return d;
+}
+// A segment's place in shared memory, and the values of a lane: fp32 classes lane + 32 j, 16-bit ones 2 lane + 64 j and the next,
+// whatever the address of the row (so that equal rows have equal sums).  The bytes lie as in the row, 16 by 16: class 0 of the
+// segment stands `lead` values behind the start.
+template <typename IO> struct Segment {
+  static constexpr int VALUES = 64 / sizeof(IO), CLASSES = 32 * VALUES, PER_COPY = 16 / sizeof(IO), BYTES = CLASSES * sizeof(IO) + 32;
   // Starts the copies of classes c0 .. of a row of V; 16 bytes that reach beyond the row's ends are read value by value.
   static __device__ __forceinline__ void fetch(uint8_t* to, const IO* z, int64_t c0, int V) {
-    const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO));
+    const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO)), lane = threadIdx.x & 31;
     if (c0 >= lead && c0 + CLASSES + PER_COPY <= V) {   // all of them lie within the row
-      const uint32_t at = (uint32_t)__cvta_generic_to_shared(to) + 16 * threadIdx.x;
-      const IO* const from = z + c0 - lead + PER_COPY * (int)threadIdx.x;
+      const uint32_t at = (uint32_t)__cvta_generic_to_shared(to) + 16 * lane;
+      const IO* const from = z + c0 - lead + PER_COPY * lane;
 #pragma unroll
-      for (int i = 0; i < CLASSES / PER_COPY / BM_THREADS; ++i) copy_16(at + 16 * BM_THREADS * i, from + PER_COPY * BM_THREADS * i);
-      if (lead && threadIdx.x == 0) copy_16(at + 16 * (CLASSES / PER_COPY), from + CLASSES);
+      for (int i = 0; i < CLASSES / PER_COPY / 32; ++i) copy_16(at + 16 * 32 * i, from + PER_COPY * 32 * i);
+      if (lead && lane == 0) copy_16(at + 16 * (CLASSES / PER_COPY), from + CLASSES);
       return;
     }
     const int here = (int)min((int64_t)CLASSES, V - c0), copies = (lead + here + PER_COPY - 1) / PER_COPY;
-    for (int i = threadIdx.x; i < copies; i += BM_THREADS) {
+    for (int i = lane; i < copies; i += 32) {
       const int64_t c = c0 + i * PER_COPY - lead;
       if (c >= 0 && c + PER_COPY <= V) {
         copy_16((uint32_t)__cvta_generic_to_shared(to + 16 * i), z + c);
@@ -85,10 +91,13 @@ template <typename IO, int VALUES> struct Segment {
   }
   using Raw = typename Pair<IO>::raw;
   Raw raw[VALUES / 2];    // what does not exist is -infinity: never a candidate, as what is masked
+  const IO* at;           // class 0 of the segment in shared memory
+  int here;               // classes that exist
   __device__ __forceinline__ void read(const uint8_t* from, const IO* z, int64_t c0, int V) {
-    const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO)), here = (int)min((int64_t)CLASSES, V - c0);
+    const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO));
     const IO none = from_f32<IO>(__uint_as_float(0xff800000u));
-    const IO* const at = reinterpret_cast<const IO*>(from) + lead;
+    here = (int)min((int64_t)CLASSES, V - c0);
+    at = reinterpret_cast<const IO*>(from) + lead;
     if (here == CLASSES) {
       if (sizeof(IO) == 2 && lead % 2 == 0) {
 #pragma unroll
@@ -107,39 +116,87 @@ template <typename IO, int VALUES> struct Segment {
     }
   }
   static __device__ __forceinline__ int place(int j) {
-    return sizeof(IO) == 2 ? 2 * (int)threadIdx.x + j / 2 * (2 * BM_THREADS) + j % 2 : (int)threadIdx.x + j * BM_THREADS;
+    const int lane = threadIdx.x & 31;
+    return sizeof(IO) == 2 ? 2 * lane + j / 2 * 64 + j % 2 : lane + j * 32;
   }
   __device__ __forceinline__ float2 pair(int i) const { return to_f32(raw[i]); }
-  __device__ __forceinline__ float value(int j) const { return j % 2 ? pair(j / 2).y : pair(j / 2).x; }
+  // without notice of NaN, but where there is nothing else
+  __device__ __forceinline__ float most_of_eight(int q) const {
+    if constexpr (sizeof(IO) == 4) {
+      return larger_number(larger_number(larger_number(fmaxf(raw[4 * q].x, raw[4 * q].y), raw[4 * q + 1]), raw[4 * q + 2]), raw[4 * q + 3]);
+    } else {
+      const float2 m = to_f32(__hmax2(__hmax2(raw[4 * q], raw[4 * q + 1]), __hmax2(raw[4 * q + 2], raw[4 * q + 3])));
+      return fmaxf(m.x, m.y);
+    }
+  }
+  // Value j once more, from shared memory: few are looked at again, and registers are worth more than they.
+  __device__ __forceinline__ float again(int j) const {
+    const int c = place(j);
+    return c < here ? to_f32(at[c]) : __uint_as_float(0xff800000u);
+  }
 };
 __device__ __forceinline__ float exp2_of(float v) {
   float e;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v));
   return e;
 }
-// The largest of m and a pair, without notice of NaN.
-__device__ __forceinline__ float larger_number(float m, float2 v) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(m), "f"(v.x), "f"(v.y));
-  return d;
-}
 constexpr float LOG2_E = 1.4426950408889634f;
 
-// A block: `length` segments of a row, one behind the other through a ring of BM_STAGES places in shared memory.
-template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS, 3) beam_rows_kernel(const BeamParams p) {
-  using Seg = Segment<IO, VALUES>;
-  extern __shared__ __align__(16) uint8_t ring[];
-  __shared__ __align__(16) float group_max[BM_GROUPS];
-  __shared__ float warp_part[2][BM_THREADS / 32];
-  __shared__ uint32_t need;            // candidates are values v with rising(v) at or above it
-  __shared__ int count;                // candidates so far
-  __shared__ uint64_t candidates[BM_CANDIDATES];
+// The best `width` of a warp's first n candidates, falling, to their beginning: the largest of all, one after the other.
+template <int EACH> __device__ __forceinline__ int best_candidates(uint64_t* candidates, int n, int width) {
+  const int lane = threadIdx.x & 31;
+  uint64_t mine[EACH];
+  __syncwarp();
+#pragma unroll
+  for (int k = 0; k < EACH; ++k) mine[k] = lane + 32 * k < n ? candidates[lane + 32 * k] : 0;
+  __syncwarp();
+  const int found = min(n, width);
+  for (int r = 0; r < found; ++r) {
+    uint64_t best = mine[0];
+#pragma unroll
+    for (int k = 1; k < EACH; ++k) best = max(best, mine[k]);
+    best = warp_max(best);
+    if (lane == 0) candidates[r] = best;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k)
+      if (mine[k] == best) mine[k] = 0;
+  }
+  __syncwarp();
+  return found;
+}
+__device__ __forceinline__ int best_candidates(uint64_t* candidates, int n, int width) {
+  return n <= 64 ? best_candidates<2>(candidates, n, width) : best_candidates<BM_CANDIDATES / 32>(candidates, n, width);
+}
+// The width-th largest of the lanes' numbers.
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v, int width) {
+  const int lane = threadIdx.x & 31;
+  uint32_t best = 0u;
+  for (int r = 0; r < width; ++r) {
+    best = __reduce_max_sync(0xffffffffu, v);
+    if (lane == __ffs(__ballot_sync(0xffffffffu, v == best)) - 1) v = 0u;
+  }
+  return best;
+}
+
+// A warp: `length` segments of a row, one behind the other through a ring of BM_STAGES places of its own in shared memory.
+template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, 3) beam_rows_kernel(const BeamParams p) {
+  using Seg = Segment<IO>;
+  constexpr int VALUES = Seg::VALUES;
+  extern __shared__ __align__(16) uint8_t ring_of_all[];
+  __shared__ uint64_t candidates_of_all[BM_WARPS][BM_CANDIDATES];
+  __shared__ float most_of_all[BM_WARPS][32];   // the lanes' maxima so far
   let_next_kernel_start();
-  const int64_t row = blockIdx.x / p.splits;
-  const int split = blockIdx.x % p.splits, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (!goes_on(p, row)) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t part = (int64_t)blockIdx.x * BM_WARPS + warp, row = part / p.splits;
+  most_of_all[warp][lane] = __uint_as_float(0xff800000u);
+  __syncthreads();
+  if (part >= p.parts || !goes_on(p, row)) return;
+  uint8_t* const ring = ring_of_all + warp * (BM_STAGES * Seg::BYTES);
+  uint64_t* const candidates = candidates_of_all[warp];
   const IO* const z = (const IO*)p.logits + row / p.K * p.sample_stride + row % p.K * p.beam_stride;
-  const int64_t first = (int64_t)split * p.length * Seg::CLASSES;
+  const int64_t first = (part - row * p.splits) * p.length * Seg::CLASSES;
+  // the warps of the block that work at the same row
+  const int from = (int)max((int64_t)0, warp - (part - row * p.splits)), to = (int)min((int64_t)BM_WARPS, warp + (row + 1) * p.splits - part);
   const int segments = (int)min((int64_t)p.length, (p.V - first + Seg::CLASSES - 1) / Seg::CLASSES);
   auto fetch = [&](int s) {
     if (s < segments) Seg::fetch(ring + s % BM_STAGES * Seg::BYTES, z, first + (int64_t)s * Seg::CLASSES, p.V);
@@ -147,40 +204,24 @@ template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS,
   };
 #pragma unroll
   for (int s = 0; s < BM_STAGES - 1; ++s) fetch(s);
-  if (tid == 0) count = 0, need = 0;
   const float none = __uint_as_float(0xff800000u);
-  float most = none, sum = 0.f;        // of this thread's values: the maximum, and the sum of exp(v - maximum)
-  int held = 0;                        // candidates before the segment
-  // the best `width` of the first n candidates, each to the place that the number of larger ones gives it
-  auto rank = [&](int n) {
-    uint64_t mine[BM_CANDIDATES / BM_THREADS];
-    int to[BM_CANDIDATES / BM_THREADS];
-#pragma unroll
-    for (int k = 0; k < BM_CANDIDATES / BM_THREADS; ++k) {
-      const int i = tid + k * BM_THREADS;
-      to[k] = p.W;
-      if (i >= n) continue;
-      mine[k] = candidates[i];
-      to[k] = 0;
-      for (int j = 0; j < n; ++j) to[k] += candidates[j] > mine[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < BM_CANDIDATES / BM_THREADS; ++k)
-      if (to[k] < p.W) candidates[to[k]] = mine[k];
-    __syncthreads();
-    return min(n, p.W);
-  };
-  wait_groups<BM_STAGES - 2>();
-  __syncthreads();
+  float most = none, sum = 0.f;        // of this lane's values: the maximum, and the sum of exp(v - maximum)
+  float bound = none;                  // candidates are values at or above it, all of them finite
+  int count = 0;                       // candidates so far
   for (int s = 0; s < segments; ++s) {
-    fetch(s + BM_STAGES - 1);          // (the segment before this one has been read by all)
+    wait_groups<BM_STAGES - 2>();
+    __syncwarp();                      // the segment is there for all lanes, and the one before it has been read by all
+    fetch(s + BM_STAGES - 1);
     const int64_t c0 = first + (int64_t)s * Seg::CLASSES;
     Seg g;
     g.read(ring + s % BM_STAGES * Seg::BYTES, z, c0, p.V);
+    float eighth[VALUES / 8];          // the maxima of eight values each
     float here = none;
 #pragma unroll
-    for (int i = 0; i < VALUES / 2; ++i) here = larger_number(here, g.pair(i));
+    for (int q = 0; q < VALUES / 8; ++q) {
+      eighth[q] = g.most_of_eight(q);
+      here = fmaxf(here, eighth[q]);
+    }
     if (here > most) {
       sum *= exp2_of((most - here) * LOG2_E);   // (0 of a sum that is 0)
       most = here;
@@ -199,102 +240,68 @@ template <typename IO, int VALUES> __global__ void __launch_bounds__(BM_THREADS,
       for (int i = 0; i < VALUES / 2; ++i)
         if (g.pair(i).x != g.pair(i).x || g.pair(i).y != g.pair(i).y) sum = __uint_as_float(0x7fc00000u);
     }
-    // the first segment: the width-th largest of its groups' maxima is a bound that at least `width` values reach
-    if (s == 0) {
-      float m = fmaxf(here, __shfl_xor_sync(0xffffffffu, here, 1));
-      m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-      if (lane % 4 == 0) group_max[tid / 4] = m;
-      __syncthreads();
-      if (tid < BM_GROUPS) {
-        const float mine = group_max[tid];
-        int reach = 0;
-#pragma unroll
-        for (int j = 0; j < BM_GROUPS; j += 4) {
-          const float4 other = *reinterpret_cast<const float4*>(group_max + j);
-          reach += (other.x >= mine) + (other.y >= mine) + (other.z >= mine) + (other.w >= mine);
-        }
-        if (reach >= p.W) atomicMax(&need, rising(mine));
-      }
-      __syncthreads();
+    // The largest of what lane l of each of the row's warps has seen: the width-th largest of these 32 is a bound that at least
+    // `width` values of the row reach.  It is taken again when the part that has been read has doubled.  (Another warp's maximum
+    // may be an older one: the bound is lower then, not wrong.)
+    reinterpret_cast<volatile float*>(most_of_all[warp])[lane] = most;
+    if ((s & (s + 1)) == 0) {
+      float m = most;
+      for (int w = from; w < to; ++w) m = fmaxf(m, reinterpret_cast<const volatile float*>(most_of_all[w])[lane]);
+      const float least = from_rising(largest_of_lanes(rising(m), p.W));
+      bound = fmaxf(bound, fmaxf(least, -largest_finite<float>()));
     }
-    const uint32_t bound = need;
-    bool full = false;
-    if (here > none && rising(here) >= bound) {
+    if (!__any_sync(0xffffffffu, here >= bound)) continue;
+    const int held = count;
 #pragma unroll
-      for (int j = 0; j < VALUES; ++j) {
-        const float v = g.value(j);
-        if (v > none && rising(v) >= bound) {
-          const int at = atomicAdd(&count, 1);
-          if (at < BM_CANDIDATES) candidates[at] = key_of(v, (uint32_t)(c0 + Seg::place(j)));
-          full = full || at >= BM_CANDIDATES / 2;
-        }
+    for (int q = 0; q < VALUES / 8; ++q) {
+      if (!__any_sync(0xffffffffu, eighth[q] >= bound)) continue;
+#pragma unroll
+      for (int j = 8 * q; j < 8 * q + 8; ++j) {
+        const float v = g.again(j);
+        const uint32_t passed = __ballot_sync(0xffffffffu, v >= bound);
+        if (!passed) continue;
+        const int at = count + __popc(passed & ((1u << lane) - 1u));
+        if (v >= bound && at < BM_CANDIDATES) candidates[at] = key_of(v, (uint32_t)(c0 + Seg::place(j)));
+        count += __popc(passed);
       }
     }
-    wait_groups<BM_STAGES - 2>();      // the next segment is there, for all behind the barrier
-    full = __syncthreads_or(full);
-    const int n = count;
-    if (!full) {
-      held = n;
-      continue;
-    }
-    int kept;
-    if (n <= BM_CANDIDATES) {
-      __syncthreads();
-      kept = rank(n);
+    if (count <= BM_CANDIDATES / 2) continue;
+    if (count <= BM_CANDIDATES) {
+      count = best_candidates(candidates, count, p.W);
     } else {
-      // too many at or above the bound (equal values, or rising ones): the next best of the candidates that were there before
-      // and of all values of the segment, one after the other
-      uint64_t old[BM_CANDIDATES / 2 / BM_THREADS];
-#pragma unroll
-      for (int k = 0; k < BM_CANDIDATES / 2 / BM_THREADS; ++k) old[k] = tid + k * BM_THREADS < held ? candidates[tid + k * BM_THREADS] : 0;
+      // too many at or above the bound (equal values, or rising ones): the next best of the candidates that were there before and of
+      // all values of the segment, one after the other
+      __syncwarp();
+      const uint64_t old[2] = {lane < held ? candidates[lane] : 0, lane + 32 < held ? candidates[lane + 32] : 0};
+      __syncwarp();
       uint64_t last = ~(uint64_t)0;
-      for (kept = 0; kept < p.W; ++kept) {
-        uint64_t best = 0;
-#pragma unroll
-        for (int k = 0; k < BM_CANDIDATES / 2 / BM_THREADS; ++k)
-          if (old[k] < last && old[k] > best) best = old[k];
-#pragma unroll
+      for (count = 0; count < p.W; ++count) {
+        uint64_t best = old[0] < last ? old[0] : 0;
+        if (old[1] < last && old[1] > best) best = old[1];
         for (int j = 0; j < VALUES; ++j) {
-          const float v = g.value(j);
-          const uint64_t key = v > none ? key_of(v, (uint32_t)(c0 + Seg::place(j))) : 0;
+          const float v = g.again(j);
+          const uint64_t key = v >= bound ? key_of(v, (uint32_t)(c0 + Seg::place(j))) : 0;
           if (key < last && key > best) best = key;
         }
-        best = warp_max(best);
-        __syncthreads();
-        if (lane == 0) candidates[BM_MOST + warp] = best;
-        __syncthreads();
-        for (int k = 0; k < BM_THREADS / 32; ++k) best = max(best, candidates[BM_MOST + k]);
-        if (!best) break;
-        if (tid == 0) candidates[kept] = best;   // (what stood there is held by its thread)
-        last = best;
+        last = warp_max(best);
+        if (!last) break;
+        if (lane == 0) candidates[count] = last;
       }
-      __syncthreads();
+      __syncwarp();
     }
-    if (tid == 0) {
-      count = kept;
-      if (kept == p.W) need = (uint32_t)(candidates[p.W - 1] >> 32) + 1;   // a later class has to be larger, not equal
-    }
-    held = kept;
-    __syncthreads();
+    // a later class has to be larger, not equal
+    if (count == p.W) bound = fmaxf(from_rising((uint32_t)(candidates[p.W - 1] >> 32) + 1), -largest_finite<float>());
   }
-  const int kept = rank(held);
-  uint64_t* const out = p.keys + (row * p.splits + split) * p.W;
-  if (tid < p.W) out[tid] = tid < kept ? candidates[tid] : 0;
+  count = best_candidates(candidates, count, p.W);
+  uint64_t* const out = p.keys + part * p.W;
+  if (lane < p.W) out[lane] = lane < count ? candidates[lane] : 0;
   float m = most;
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  if (lane == 0) warp_part[0][warp] = m;
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < BM_THREADS / 32; ++k) m = fmaxf(m, warp_part[0][k]);
   float total = most > none ? sum * exp2_of((most - m) * LOG2_E) : sum;
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) total += __shfl_xor_sync(0xffffffffu, total, o);
-  if (lane == 0) warp_part[1][warp] = total;
-  __syncthreads();
-  if (tid > 0) return;
-  for (int k = 1; k < BM_THREADS / 32; ++k) total += warp_part[1][k];
-  p.stats[row * p.splits + split] = make_float2(m, total);
+  if (lane == 0) p.stats[part] = make_float2(m, total);
 }
 
 // A block per sample: the rows of its beams from their segments, a warp each, then the sample from its rows.
@@ -492,21 +499,17 @@ __global__ void __launch_bounds__(BM_COPY_THREADS) reorder_rows_kernel(const __g
 
 // ---- host ----------------------------------------------------------------------------------------------------
 struct Split {
-  bool wide;                   // segments of 16 KB, otherwise 2048 classes
   int length, splits;
 };
-constexpr int WIDE = 16384 / BM_THREADS, NARROW = 8;   // bytes, values of a thread
-// Parts of as many segments of 16 KB as still give every SM a dozen of blocks, down to one; for fewer rows segments of 2048 classes,
-// again as many as still give it four, down to one, which are on their way at once in a block of their own.
+// Parts of as many segments as still give every warp that the device holds one of them, and no more than 32 (one list of the best for
+// each lane that joins them) where that leaves at least half of them one.
 Split split_of(int64_t rows, int V, int dtype) {
-  const int64_t classes = (int64_t)BM_THREADS * WIDE / (int)dtype_size(dtype), segments = (V + classes - 1) / classes;
-  for (int64_t length = 16; length >= 1; length /= 2)
-    if (rows * ((segments + length - 1) / length) >= 148 * (length > 1 ? 12 : 4)) return {true, (int)length, (int)((segments + length - 1) / length)};
-  const int64_t small = BM_THREADS * NARROW, count = (V + small - 1) / small;
-  // (no more than 1024 parts, whose lists the joining kernel looks after)
-  int64_t length = (count + 1023) / 1024;
-  while (rows * ((count + 2 * length - 1) / (2 * length)) >= 148 * 4) length *= 2;
-  return {false, (int)length, (int)((count + length - 1) / length)};
+  const int64_t classes = 32 * 64 / (int64_t)dtype_size(dtype), segments = (V + classes - 1) / classes;
+  int64_t length = 32;
+  while (length > 1 && rows * ((segments + length - 1) / length) < 148 * 24) length /= 2;
+  while ((segments + length - 1) / length > 32 && rows * ((segments + 2 * length - 1) / (2 * length)) >= 148 * 8) length *= 2;
+  while ((segments + length - 1) / length > 1024) length *= 2;   // (whose heads the joining kernel keeps in shared memory)
+  return {(int)length, (int)((segments + length - 1) / length)};
 }
 snn_status check(const snn_beam_args* a) {
   if (!a || a->B < 0 || a->K < 1 || a->W < 1 || a->V < 1 || !dtype_known(a->dtype)) return SNN_ERR_INVALID_ARG;
@@ -555,13 +558,10 @@ snn_status reorder(const snn_state_rows* t, int32_t count, const int64_t* parent
   }
   return SNN_OK;
 }
-template <typename IO, int VALUES> snn_status launch_segments(const BeamParams& p, cudaStream_t stream) {
-  constexpr int SMEM = BM_STAGES * Segment<IO, VALUES>::BYTES;
-  if (cudaFuncSetAttribute(beam_rows_kernel<IO, VALUES>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
-  return launch_behind(beam_rows_kernel<IO, VALUES>, (unsigned)(p.rows * p.splits), BM_THREADS, SMEM, stream, false, p);
-}
-template <typename IO> snn_status launch_rows(const BeamParams& p, bool wide, cudaStream_t stream) {
-  return wide ? launch_segments<IO, WIDE / (int)sizeof(IO)>(p, stream) : launch_segments<IO, NARROW>(p, stream);
+template <typename IO> snn_status launch_rows(const BeamParams& p, cudaStream_t stream) {
+  constexpr int SMEM = BM_WARPS * BM_STAGES * Segment<IO>::BYTES;
+  if (cudaFuncSetAttribute(beam_rows_kernel<IO>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
+  return launch_behind(beam_rows_kernel<IO>, (unsigned)((p.parts + BM_WARPS - 1) / BM_WARPS), 32 * BM_WARPS, SMEM, stream, false, p);
 }
 }  // namespace
 
@@ -585,14 +585,14 @@ extern "C" snn_status snn_beam_step(const snn_beam_args* a, void* stream) {
   BeamParams p{};
   p.rows = (int64_t)a->B * a->K;
   const Split s = split_of(p.rows, a->V, a->dtype);
-  p.K = a->K, p.W = a->W, p.V = a->V, p.splits = s.splits, p.length = s.length, p.sample_stride = a->sample_stride, p.beam_stride = a->beam_stride, p.end = a->end;
+  p.K = a->K, p.W = a->W, p.V = a->V, p.splits = s.splits, p.length = s.length, p.parts = p.rows * s.splits, p.sample_stride = a->sample_stride, p.beam_stride = a->beam_stride, p.end = a->end;
   p.logits = a->logits, p.scores = a->scores, p.ended = a->ended;
   p.keys = (uint64_t*)a->workspace, p.stats = (float2*)((char*)a->workspace + l.stats);
   p.tokens = a->tokens, p.parents = a->parents, p.new_scores = a->new_scores, p.new_ended = a->new_ended;
   const cudaStream_t on = (cudaStream_t)stream;
-  st = a->dtype == SNN_DTYPE_FP32   ? launch_rows<float>(p, s.wide, on)
-       : a->dtype == SNN_DTYPE_BF16 ? launch_rows<__nv_bfloat16>(p, s.wide, on)
-                                    : launch_rows<__half>(p, s.wide, on);
+  st = a->dtype == SNN_DTYPE_FP32   ? launch_rows<float>(p, on)
+       : a->dtype == SNN_DTYPE_BF16 ? launch_rows<__nv_bfloat16>(p, on)
+                                    : launch_rows<__half>(p, on);
   if (st != SNN_OK) return st;
   const int warps = std::min(a->K, BM_JOIN_WARPS);
   st = launch_behind(beam_join_kernel, (unsigned)a->B, 32 * warps, (size_t)warps * s.splits, on, true, p);

@@ -426,6 +426,11 @@ def _rows_like(t: torch.Tensor, name: str, like: torch.Tensor) -> int:
     return _row_stride(t, name)
 
 
+def _overlap(a: Optional[int], a_stride: int, b: Optional[int], b_stride: int, rows: int, n: int, size: int) -> bool:
+    """Whether the memory between the first and the last value of two arrays of rows has bytes in common."""
+    return bool(a and b and rows) and a < b + ((rows - 1) * b_stride + n) * size and b < a + ((rows - 1) * a_stride + n) * size
+
+
 def _norm_weight(weight: Optional[torch.Tensor], like: torch.Tensor) -> int:
     """Checks a norm's weight and returns its type's number."""
     if weight is None:
@@ -475,6 +480,9 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: O
                 h, a.h_stride = residual, a.residual_stride
                 if a.rows > 1 and a.h_stride < n:
                     raise ValueError("residual: rows overlap")
+                same = a.x == a.residual and a.x_stride == a.residual_stride
+                if not same and _overlap(a.x, a.x_stride, a.residual, a.residual_stride, a.rows, n, x.element_size()):
+                    raise ValueError("residual: overlaps x in memory")
             else:
                 h, a.h_stride = _dense(x), n
             a.h = h.data_ptr()

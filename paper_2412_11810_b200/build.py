@@ -10,9 +10,9 @@ HEADERS = [os.path.join(CSRC, f) for f in ("kernels.cuh", "tma.cuh", "tc_gemm.cu
 LIB = os.path.join(HERE, "libsnnckpt.so")
 LIB_DEBUG = os.path.join(HERE, "libsnnckpt_debug.so")   # the same sources with -DSNN_DEBUG_CHECKS=1 (bounds-checked)
 # -fmad=false: nothing is fused unless the source says fmaf; the forward arithmetic that decides
-# spikes is written with explicit intrinsics anyway.
+# spikes is written with explicit intrinsics anyway.  The sources are compiled side by side.
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-fmad=false",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:

@@ -240,24 +240,51 @@ template <int COUNT> struct AwWalk {
   }
 };
 
+// The sum of squares of a thread's values of a tile of type T, from place i on; four turns at a time, so that as many loads are on
+// their way.
+template <typename T> __device__ __forceinline__ double squares_of(const T* g, int64_t i, int64_t n, int turns, bool vectors) {
+  constexpr int AHEAD = 4, STEP = AW_THREADS * AW_VALUES;
+  double sum = 0.0;
+  for (int turn = 0; turn < turns && i < n; turn += AHEAD, i += AHEAD * STEP) {
+    Unit<T, AW_VALUES> u[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const int64_t at = i + k * STEP, left = turn + k < turns ? n - at : 0;
+      if (vectors && left >= AW_VALUES) {
+        u[k].get(g + at);
+      } else {
+        T v[AW_VALUES];
+#pragma unroll
+        for (int j = 0; j < AW_VALUES; ++j) v[j] = j < left ? g[at + j] : from_f32<T>(0.f);
+        memcpy(u[k].u, v, sizeof(v));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      float2 s = both(0.f);
+#pragma unroll
+      for (int j = 0; j < AW_VALUES / 2; ++j) s = fma_pair(u[k].pair(j), u[k].pair(j), s);
+      const float here = s.x + s.y;
+      if (here >= 0x1p-100f && here <= 0x1p126f) {
+        sum += (double)here;
+      } else {   // squares beyond the range of fp32
+#pragma unroll
+        for (int j = 0; j < AW_VALUES / 2; ++j) sum += (double)u[k].pair(j).x * u[k].pair(j).x + (double)u[k].pair(j).y * u[k].pair(j).y;
+      }
+    }
+  }
+  return sum;
+}
 // Sums of squares of the gradients, a block's share in 64 bits.
 template <int COUNT> __global__ void __launch_bounds__(AW_THREADS) adamw_norm_kernel(const __grid_constant__ AwParams<COUNT> a, int first) {
   let_next_kernel_start();
   double sum = 0.0;
-  for (AwWalk<COUNT> at(a, blockIdx.x); at.tile < a.tiles; at.go_on(a, gridDim.x)) {
-    const AwTensor& t = a.t[at.tensor];
-    float2 g[AW_VALUES / 2];
-    load_values<AW_VALUES>(g, t.g, t.g_dtype, at.place(), t.n, t.vectors);
-    float2 s = both(0.f);
-#pragma unroll
-    for (int k = 0; k < AW_VALUES / 2; ++k) s = fma_pair(g[k], g[k], s);
-    const float here = s.x + s.y;
-    if (here >= 0x1p-100f && here <= 0x1p126f) {
-      sum += (double)here;
-    } else {   // squares beyond the range of fp32
-#pragma unroll
-      for (int k = 0; k < AW_VALUES / 2; ++k) sum += (double)g[k].x * g[k].x + (double)g[k].y * g[k].y;
-    }
+  for (int64_t tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
+    const AwTensor& t = a.t[tensor_of(a, tile)];
+    const int64_t i = ((tile - t.tile) * a.turns * AW_THREADS + threadIdx.x) * AW_VALUES;
+    sum += t.g_dtype == SNN_DTYPE_FP32   ? squares_of((const float*)t.g, i, t.n, a.turns, t.vectors)
+           : t.g_dtype == SNN_DTYPE_BF16 ? squares_of((const __nv_bfloat16*)t.g, i, t.n, a.turns, t.vectors)
+                                         : squares_of((const __half*)t.g, i, t.n, a.turns, t.vectors);
   }
 #pragma unroll
   for (int o = 16; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);

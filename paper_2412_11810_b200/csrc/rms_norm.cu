@@ -7,6 +7,7 @@
 // hold one or two units each (unit.cuh) in registers, so that the second use of h costs no second read.  Within a warp nothing
 // waits for a block.  Rows that do not fit are read a second time, from L2.
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "unit.cuh"
@@ -17,6 +18,7 @@ namespace {
 
 constexpr int RMS_THREADS = 256;      // of a block whose rows need no more than a warp
 constexpr int RMS_MOST_LANES = 512, RMS_WIDE = 1024;   // threads of a row; of one that does not fit registers
+constexpr size_t RMS_SUMS = 192 * 1024;                // bytes of such a row's sums for dw in shared memory
 
 struct RmsParams {
   int64_t rows;
@@ -51,43 +53,68 @@ __device__ __forceinline__ float scale_of(float sum, const RmsParams& p) { retur
 constexpr float RMS_DOWN = 0x1p-80f;
 __device__ __forceinline__ float scale_of_far(float sum, const RmsParams& p) { return rsqrtf(sum * p.inverse_n) * RMS_DOWN; }
 
-// Which row of a turn of its block a thread works at, which of the row's threads it is, and its columns.
-template <bool BLOCK, int N, bool FAST> struct Place {
-  static constexpr int LANES = KEEP_GROUP / N;
-  int slot, t, s, lanes, n;
+// Which row of a turn of its block a thread works at, which of the row's threads it is, and its columns.  (Less than a warp a row: by
+// vectors only.)
+template <bool BLOCK, int ACCESS, int N> struct Place {
+  int slot, t, lanes, n;
   __device__ __forceinline__ explicit Place(const RmsParams& p) : lanes(p.lanes), n(p.n) {
     slot = BLOCK ? 0 : threadIdx.x / p.lanes;
     t = BLOCK ? threadIdx.x : threadIdx.x % p.lanes;
-    s = t % LANES;
   }
   __device__ __forceinline__ int per_block() const { return BLOCK ? 1 : RMS_THREADS / lanes; }
-  // the first column of the thread's i-th unit, and how many columns are left from there on
-  __device__ __forceinline__ int column(int i) const { return (t / LANES) * KEEP_GROUP + i * lanes * N + unit_first<N, FAST>(s); }
-  __device__ __forceinline__ int left(int i) const { return n - column(i); }
-};
-template <int FORMAT, bool FAST, int N>
-__device__ __forceinline__ void keep_unit(const float2 y[N / 2], int64_t row, int column, int left, int s, const RmsParams& p, bool store) {
-  float m = 0.f;
-#pragma unroll
-  for (int i = 0; i < N / 2; ++i) m = larger_of(m, y[i]);
-  const uint32_t top = group_top<KEEP_GROUP / N>(m), byte = keep_scale_byte<FORMAT>(top);
-  const float inverse = keep_scale_inverse(byte);
-  // (rarely: a group whose largest value could round up to 128, or one that is not finite)
-  const bool rare = __any_sync(0xffffffffu, byte == 255u || keep_needs_cut<FORMAT>(top));
-  uint32_t q[N / 4];
-  encode_unit<FORMAT, N>(q, y, inverse, rare);
-  if (rare && byte == 255u) {
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) q[i] = 0u;
+  __device__ __forceinline__ Columns<ACCESS, N> columns(int i) const {   // of the thread's i-th unit
+    return {((t & ~31) + i * lanes) * N + Columns<ACCESS, N>::of_lane(t & 31), n};
   }
-  if (!store) return;
-  store_codes<FAST, N>(p.codes + row * p.n + column, q, left);
-  if (s == 0 && left > 0) p.scales[row * p.groups + column / KEEP_GROUP] = (uint8_t)byte;
+};
+// The 8-bit codes of a unit y; the lanes of a warp do this together.
+template <int FORMAT, int ACCESS, int N> __device__ __forceinline__ void keep_unit(const float2 y[N / 2], int64_t row, Columns<ACCESS, N> at, const RmsParams& p, bool store) {
+  uint8_t* const codes = p.codes + row * p.n + at.first;
+  uint8_t* const scales = p.scales + row * p.groups;
+  if constexpr (ACCESS == VECTORS) {
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) m = larger_of(m, y[i]);
+    const uint32_t top = group_top<KEEP_GROUP / N>(m), byte = keep_scale_byte<FORMAT>(top);
+    const float inverse = keep_scale_inverse(byte);
+    // (rarely: a group whose largest value could round up to 128, or one that is not finite)
+    const bool rare = __any_sync(0xffffffffu, byte == 255u || keep_needs_cut<FORMAT>(top));
+    uint32_t q[N / 4];
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) q[i] = __byte_perm(encode_pair<FORMAT>(y[2 * i], inverse, rare), encode_pair<FORMAT>(y[2 * i + 1], inverse, rare), 0x5410);
+    if (rare && byte == 255u) {
+#pragma unroll
+      for (int i = 0; i < N / 4; ++i) q[i] = 0u;
+    }
+    if (!store || !at.exists(0)) return;
+    if constexpr (N == 16)
+      *reinterpret_cast<uint4*>(codes) = make_uint4(q[0], q[1], q[2], q[3]);
+    else
+      *reinterpret_cast<uint2*>(codes) = make_uint2(q[0], q[1]);
+    if (at.first % KEEP_GROUP == 0) scales[at.first / KEEP_GROUP] = (uint8_t)byte;
+  } else {
+    // group k of the unit: a pair of each lane, or two values 32 places apart.  All lanes know its scale; lane k keeps it.
+    const int lane = threadIdx.x & 31, start = at.first - Columns<ACCESS, N>::of_lane(lane);
+    uint32_t mine = 0u;
+#pragma unroll
+    for (int k = 0; k < N / 2; ++k) {
+      if (start + k * KEEP_GROUP >= p.n) break;
+      const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(larger_of(0.f, y[k]))), byte = keep_scale_byte<FORMAT>(top);
+      const uint32_t q = byte == 255u ? 0u : encode_pair<FORMAT>(y[k], keep_scale_inverse(byte), keep_needs_cut<FORMAT>(top));
+      if (lane == k) mine = byte;
+      if (!store) continue;
+      if (ACCESS == PAIRS) {
+        if (at.exists(2 * k)) *reinterpret_cast<uint16_t*>(codes + at.behind(2 * k)) = (uint16_t)q;
+      } else {
+        if (at.exists(2 * k)) codes[at.behind(2 * k)] = (uint8_t)q;
+        if (at.exists(2 * k + 1)) codes[at.behind(2 * k + 1)] = (uint8_t)(q >> 8);
+      }
+    }
+    if (store && lane < N / 2 && start + lane * KEEP_GROUP < p.n) scales[start / KEEP_GROUP + lane] = (uint8_t)mine;
+  }
 }
 // y of one unit of h, as values, as codes, or both.
-template <typename IO, typename WT, bool FAST, int N>
-__device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT, N>& w, float scale, int64_t row, int column, int left, int s, const RmsParams& p,
-                                            bool store) {
+template <typename IO, typename WT, int ACCESS, int N>
+__device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT, N>& w, float scale, int64_t row, Columns<ACCESS, N> at, const RmsParams& p, bool store) {
   float2 y[N / 2];
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) y[i] = mul_pair(h.pair(i), both(scale));
@@ -99,10 +126,10 @@ __device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT,
     Unit<IO, N> out;
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) out.set(i, y[i]);
-    store_unit<FAST>(out, (IO*)p.y + row * p.y_stride + column, left);
+    at.store(out, (IO*)p.y + row * p.y_stride);
   }
-  if (p.keep_format == SNN_KEEP_INT8) keep_unit<SNN_KEEP_INT8, FAST, N>(y, row, column, left, s, p, store);
-  if (p.keep_format == SNN_KEEP_E4M3) keep_unit<SNN_KEEP_E4M3, FAST, N>(y, row, column, left, s, p, store);
+  if (p.keep_format == SNN_KEEP_INT8) keep_unit<SNN_KEEP_INT8, ACCESS, N>(y, row, at, p, store);
+  if (p.keep_format == SNN_KEEP_E4M3) keep_unit<SNN_KEEP_E4M3, ACCESS, N>(y, row, at, p, store);
 }
 // A unit of h: that of x, or its sum with the residual's; and its squares.
 template <typename IO, int N> __device__ __forceinline__ void sum_unit(Unit<IO, N>& h, const Unit<IO, N>& r, bool residual, float2& sum) {
@@ -123,11 +150,11 @@ template <typename IO, int N> __device__ __forceinline__ void sum_unit_far(const
 
 // BLOCK: a row per block and turn; otherwise a warp holds whole rows.  The loads of the next row are on their way while a row
 // is finished; the weight stays in registers.
-template <typename IO, typename WT, bool FAST, int UNITS, bool BLOCK>
-__global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK && FAST && UNITS == 1 ? 2 : 1) rms_forward_kernel(const RmsParams p) {
+template <typename IO, typename WT, int ACCESS, int UNITS, bool BLOCK>
+__global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK && ACCESS == VECTORS && UNITS == 1 ? 2 : 1) rms_forward_kernel(const RmsParams p) {
   constexpr int N = UNIT<IO>;
   __shared__ float shared[2][32];
-  const Place<BLOCK, N, FAST> at(p);
+  const Place<BLOCK, ACCESS, N> at(p);
   const int64_t step = (int64_t)gridDim.x * at.per_block();
   const bool residual = p.residual != nullptr;
   int turn = 0;
@@ -138,16 +165,16 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
     x[i].zero(), r[i].zero();   // (and stay so behind the row's end)
     if (!p.weight) continue;
     w[i].zero();
-    load_unit<FAST>(w[i], (const WT*)p.weight + at.column(i), at.left(i));
+    at.columns(i).load(w[i], (const WT*)p.weight);
   }
   auto load = [&](int64_t row) {
     const IO* const from = (const IO*)p.x + row * p.x_stride;
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(x[i], from + at.column(i), at.left(i));
+    for (int i = 0; i < UNITS; ++i) at.columns(i).load(x[i], from);
     if (!residual) return;
     const IO* const other = (const IO*)p.residual + row * p.residual_stride;
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(r[i], other + at.column(i), at.left(i));
+    for (int i = 0; i < UNITS; ++i) at.columns(i).load(r[i], other);
   };
   const int64_t first = (int64_t)blockIdx.x * at.per_block();
   if (first < p.rows) load(min(first + at.slot, p.rows - 1));
@@ -160,7 +187,7 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
     for (int i = 0; i < UNITS; ++i) {
       h[i] = x[i];
       sum_unit(h[i], r[i], residual, sum);
-      if (residual && store) store_unit<FAST>(h[i], (IO*)p.h + row * p.h_stride + at.column(i), at.left(i));
+      if (residual && store) at.columns(i).store(h[i], (IO*)p.h + row * p.h_stride);
     }
     if (base + step < p.rows) load(min(base + step + at.slot, p.rows - 1));
     float total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared), scale = scale_of(total, p);
@@ -175,54 +202,52 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
     }
     if (p.rstd && at.t == 0 && store) p.rstd[row] = scale;
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) finish_unit<IO, WT, FAST, N>(h[i], w[i], scale, row, at.column(i), at.left(i), at.s, p, store);
+    for (int i = 0; i < UNITS; ++i) finish_unit<IO, WT, ACCESS, N>(h[i], w[i], scale, row, at.columns(i), p, store);
   }
 }
 // A block per row, which is read twice.
-template <typename IO, typename WT, bool FAST> __global__ void __launch_bounds__(RMS_WIDE) rms_forward_wide_kernel(const RmsParams p) {
-  constexpr int N = UNIT<IO>, LANES = KEEP_GROUP / N, STEP = RMS_WIDE / LANES;
+template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds__(RMS_WIDE) rms_forward_wide_kernel(const RmsParams p) {
+  constexpr int N = UNIT<IO>;
+  using At = Columns<ACCESS, N>;
   __shared__ float shared[2][32];
-  const int t = threadIdx.x, s = t % LANES;
+  const int t = threadIdx.x;
   const bool residual = p.residual != nullptr;
   int turn = 0;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const IO* const from = (const IO*)p.x + row * p.x_stride;
     const IO* const again = residual ? (const IO*)p.h + row * p.h_stride : from;
     float2 sum = both(0.f);
-    // (groups behind the last one: all threads take the same number of turns, as lanes of a group work together)
+    // (a warp whose columns begin behind the last one has nothing to do: its lanes go the same way)
     auto each = [&](auto&& f) {
-      for (int64_t g = t / LANES; g - t / LANES < p.groups; g += STEP) {
-        const int column = (int)min(g * KEEP_GROUP, (int64_t)p.n) + unit_first<N, FAST>(s);
-        f(column, p.n - column);
-      }
+      for (int64_t start = (t & ~31) * N; start < p.n; start += RMS_WIDE * N) f(At{(int)start + At::of_lane(t & 31), p.n});
     };
-    each([&](int column, int left) {
+    each([&](At at) {
       Unit<IO, N> h, r;
       h.zero(), r.zero();
-      load_unit<FAST>(h, from + column, left);
-      if (residual) load_unit<FAST>(r, (const IO*)p.residual + row * p.residual_stride + column, left);
+      at.load(h, from);
+      if (residual) at.load(r, (const IO*)p.residual + row * p.residual_stride);
       sum_unit(h, r, residual, sum);
-      if (residual) store_unit<FAST>(h, (IO*)p.h + row * p.h_stride + column, left);
+      if (residual) at.store(h, (IO*)p.h + row * p.h_stride);
     });
     float total = row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared), scale = scale_of(total, p);
     if (!(total <= largest_finite<float>())) {
       sum = both(0.f);
-      each([&](int column, int left) {
+      each([&](At at) {
         Unit<IO, N> h;
         h.zero();
-        load_unit<FAST>(h, again + column, left);
+        at.load(h, again);
         sum_unit_far(h, sum);
       });
       scale = scale_of_far(row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared), p);
     }
     if (p.rstd && t == 0) p.rstd[row] = scale;
-    each([&](int column, int left) {   // (a thread reads back what it stored itself)
+    each([&](At at) {   // (a thread reads back what it stored itself)
       Unit<IO, N> h;
       Unit<WT, N> w;
       h.zero(), w.zero();
-      load_unit<FAST>(h, again + column, left);
-      if (p.weight) load_unit<FAST>(w, (const WT*)p.weight + column, left);
-      finish_unit<IO, WT, FAST, N>(h, w, scale, row, column, left, s, p, true);
+      at.load(h, again);
+      if (p.weight) at.load(w, (const WT*)p.weight);
+      finish_unit<IO, WT, ACCESS, N>(h, w, scale, row, at, p, true);
     });
   }
 }
@@ -231,18 +256,18 @@ template <typename IO, typename WT, bool FAST> __global__ void __launch_bounds__
 template <typename IO, typename WT, int N> __device__ __forceinline__ float2 weighted(const Unit<IO, N>& dy, const Unit<WT, N>& w, bool has_weight, int i) {
   return has_weight ? mul_pair(dy.pair(i), w.pair(i)) : dy.pair(i);
 }
-template <typename IO, typename WT, bool FAST, int UNITS, bool BLOCK>
+template <typename IO, typename WT, int ACCESS, int UNITS, bool BLOCK>
 __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_backward_kernel(const RmsParams p) {
   constexpr int N = UNIT<IO>;
   __shared__ float shared[2][32];
   __shared__ float dw_shared[BLOCK ? 1 : 32 * N];
   let_next_kernel_start();
-  const Place<BLOCK, N, FAST> at(p);
+  const Place<BLOCK, ACCESS, N> at(p);
   const int64_t step = (int64_t)gridDim.x * at.per_block();
   const bool has_weight = p.weight != nullptr;
   int turn = 0;
   // the loads of the next row are on their way while a row is worked at, where registers hold both
-  constexpr bool AHEAD = FAST && UNITS == 1;
+  constexpr bool AHEAD = ACCESS == VECTORS && UNITS == 1;
   struct Inputs {
     Unit<IO, N> h[UNITS], dy[UNITS], dh[UNITS];
     float scale;
@@ -252,7 +277,7 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_back
 #pragma unroll
   for (int i = 0; i < UNITS; ++i) {
     now.h[i].zero(), now.dy[i].zero(), now.dh[i].zero(), w[i].zero();   // (and stay so behind the row's end)
-    if (has_weight) load_unit<FAST>(w[i], (const WT*)p.weight + at.column(i), at.left(i));
+    if (has_weight) at.columns(i).load(w[i], (const WT*)p.weight);
 #pragma unroll
     for (int k = 0; k < N / 2; ++k) dw[i][k] = both(0.f);
   }
@@ -260,13 +285,13 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_back
     const IO *const from = (const IO*)p.h + row * p.h_stride, *const from_dy = (const IO*)p.dy + row * p.dy_stride;
     in.scale = p.rstd[row];
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(in.h[i], from + at.column(i), at.left(i));
+    for (int i = 0; i < UNITS; ++i) at.columns(i).load(in.h[i], from);
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(in.dy[i], from_dy + at.column(i), at.left(i));
+    for (int i = 0; i < UNITS; ++i) at.columns(i).load(in.dy[i], from_dy);
     if (!p.dh) return;
     const IO* const from_dh = (const IO*)p.dh + row * p.dh_stride;
 #pragma unroll
-    for (int i = 0; i < UNITS; ++i) load_unit<FAST>(in.dh[i], from_dh + at.column(i), at.left(i));
+    for (int i = 0; i < UNITS; ++i) at.columns(i).load(in.dh[i], from_dh);
   };
   next = now;
   if (AHEAD && (int64_t)blockIdx.x * at.per_block() < p.rows) load(next, min((int64_t)blockIdx.x * at.per_block() + at.slot, p.rows - 1));
@@ -301,7 +326,7 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_back
         if (p.dh) v = add_pair(v, now.dh[i].pair(k));
         out.set(k, v);
       }
-      if (mine) store_unit<FAST>(out, to + at.column(i), at.left(i));
+      if (mine) at.columns(i).store(out, to);
     }
   }
   if (!p.partial) return;
@@ -310,7 +335,7 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_back
 #pragma unroll
     for (int i = 0; i < UNITS; ++i)
 #pragma unroll
-      for (int j = 0; j < N; ++j) f(at.column(i) + unit_place<N, FAST>(j), j % 2 ? dw[i][j / 2].y : dw[i][j / 2].x);
+      for (int j = 0; j < N; ++j) f(at.columns(i).first + Columns<ACCESS, N>::behind(j), j % 2 ? dw[i][j / 2].y : dw[i][j / 2].x);
   };
   if (BLOCK) {
     each([&](int c, float v) {
@@ -325,28 +350,34 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_back
   }
   for (int i = threadIdx.x; i < p.n; i += blockDim.x) to[i] = dw_shared[i];
 }
-template <typename IO, typename WT, bool FAST> __global__ void __launch_bounds__(RMS_WIDE) rms_backward_wide_kernel(const RmsParams p) {
-  constexpr int N = UNIT<IO>, LANES = KEEP_GROUP / N, STEP = RMS_WIDE / LANES;
+// A block per row, which is read twice.  Its share of dw lies in shared memory, each thread's sums at places of its own, or where that
+// is too small (in_shared false) in the workspace itself.
+template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds__(RMS_WIDE) rms_backward_wide_kernel(const RmsParams p, bool in_shared) {
+  constexpr int N = UNIT<IO>;
+  using At = Columns<ACCESS, N>;
   __shared__ float shared[2][32];
+  extern __shared__ float sums[];
   let_next_kernel_start();
-  const int t = threadIdx.x, s = t % LANES;
+  const int t = threadIdx.x;
   const bool has_weight = p.weight != nullptr;
   int turn = 0;
   float* const to = p.partial ? p.partial + (int64_t)blockIdx.x * p.n : nullptr;
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+    const bool first = row == blockIdx.x;
     const float scale = p.rstd[row];
     float2 sum = both(0.f);
     float c = 0.f;
     for (int pass = 0; pass < 2; ++pass) {
-      for (int64_t g = t / LANES; g < p.groups; g += STEP) {
-        const int column = (int)(g * KEEP_GROUP) + unit_first<N, FAST>(s), left = p.n - column;
+      float* mine = sums + t;   // value v of round r: RMS_WIDE (N r + v) on
+      for (int64_t start = (t & ~31) * N; start < p.n; start += RMS_WIDE * N, mine += RMS_WIDE * N) {
+        const At at{(int)start + At::of_lane(t & 31), p.n};
         Unit<IO, N> h, dy, dh, out;
         Unit<WT, N> w;
         h.zero(), dy.zero(), dh.zero(), w.zero();
-        load_unit<FAST>(h, (const IO*)p.h + row * p.h_stride + column, left);
-        load_unit<FAST>(dy, (const IO*)p.dy + row * p.dy_stride + column, left);
-        if (has_weight) load_unit<FAST>(w, (const WT*)p.weight + column, left);
-        if (p.dh && pass) load_unit<FAST>(dh, (const IO*)p.dh + row * p.dh_stride + column, left);
+        at.load(h, (const IO*)p.h + row * p.h_stride);
+        at.load(dy, (const IO*)p.dy + row * p.dy_stride);
+        if (has_weight) at.load(w, (const WT*)p.weight);
+        if (p.dh && pass) at.load(dh, (const IO*)p.dh + row * p.dh_stride);
 #pragma unroll
         for (int k = 0; k < N / 2; ++k) {
           const float2 n = mul_pair(h.pair(k), both(scale)), gw = weighted(dy, w, has_weight, k);
@@ -358,15 +389,28 @@ template <typename IO, typename WT, bool FAST> __global__ void __launch_bounds__
           if (p.dh) v = add_pair(v, dh.pair(k));
           out.set(k, v);
           if (!to) continue;
-          const float2 d = mul_pair(dy.pair(k), n);   // (every place of a block's share belongs to one thread)
-          const int a = unit_place<N, FAST>(2 * k), b = unit_place<N, FAST>(2 * k + 1);
-          if (a < left) to[column + a] = row == blockIdx.x ? d.x : to[column + a] + d.x;
-          if (b < left) to[column + b] = row == blockIdx.x ? d.y : to[column + b] + d.y;
+          const float2 d = mul_pair(dy.pair(k), n);
+          if (in_shared) {
+            mine[RMS_WIDE * 2 * k] = first ? d.x : mine[RMS_WIDE * 2 * k] + d.x;
+            mine[RMS_WIDE * (2 * k + 1)] = first ? d.y : mine[RMS_WIDE * (2 * k + 1)] + d.y;
+          } else {   // (every place of a block's share belongs to one thread)
+            const int a = at.first + At::behind(2 * k), b = at.first + At::behind(2 * k + 1);
+            if (at.exists(2 * k)) to[a] = first ? d.x : to[a] + d.x;
+            if (at.exists(2 * k + 1)) to[b] = first ? d.y : to[b] + d.y;
+          }
         }
-        if (pass) store_unit<FAST>(out, (IO*)p.dx + row * p.dx_stride + column, left);
+        if (pass) at.store(out, (IO*)p.dx + row * p.dx_stride);
       }
       if (!pass) c = row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared) * p.inverse_n;
     }
+  }
+  if (!to || !in_shared) return;
+  const float* mine = sums + t;
+  for (int64_t start = (t & ~31) * N; start < p.n; start += RMS_WIDE * N, mine += RMS_WIDE * N) {
+    const At at{(int)start + At::of_lane(t & 31), p.n};
+#pragma unroll
+    for (int v = 0; v < N; ++v)
+      if (at.exists(v)) to[at.first + At::behind(v)] = mine[RMS_WIDE * v];
   }
 }
 // dw from the blocks' shares, in an order of its own: 32 columns a block, 32 rows of shares at a time.
@@ -394,18 +438,18 @@ struct Shape {
   bool block;                          // a row per block
 };
 // One unit a thread where rows are few, so that a row is spread over many threads; two where the rows fill the device with half
-// the threads each, so that what a row costs beside its values is shared by more of them.  (Value by value, without vectors,
-// a second unit only means more registers.)
-Shape shape_of(const snn_rms_norm_args* a, bool fast, bool two, int resident) {
-  const int groups = (a->n + KEEP_GROUP - 1) / KEEP_GROUP, per_group = KEEP_GROUP * (int)dtype_size(a->dtype) / 32;
+// the threads each, so that what a row costs beside its values is shared by more of them.  (Without vectors a second unit only
+// means more registers, and a row has a warp at least.)
+Shape shape_of(const snn_rms_norm_args* a, int access, bool two, int resident) {
+  const int unit = unit_of(a->dtype), groups = (a->n + KEEP_GROUP - 1) / KEEP_GROUP, per_group = KEEP_GROUP / unit;
   Shape s{RMS_WIDE, 0, RMS_WIDE, 0, true};
   for (int units = 1; units <= 2; ++units) {
     const int64_t need = (int64_t)per_group * ((groups + units - 1) / units);
-    int lanes = per_group;
+    int lanes = access == VECTORS ? per_group : 32;
     while (lanes < need && lanes < 32) lanes *= 2;
     if (need > 32) lanes = (int)std::min<int64_t>((need + 31) / 32 * 32, INT32_MAX - 31);
     if (lanes > RMS_MOST_LANES) continue;
-    if (s.units && (!fast || !two || need < 32 || a->rows * lanes < 148 * 512)) break;
+    if (s.units && (access != VECTORS || !two || need < 32 || a->rows * lanes < 148 * 512)) break;
     const bool block = units > 1 || lanes > 32;
     s = {lanes, units, block ? lanes : RMS_THREADS, 0, block};
   }
@@ -413,8 +457,8 @@ Shape shape_of(const snn_rms_norm_args* a, bool fast, bool two, int resident) {
   s.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(turns, (int64_t)148 * std::max(1, (s.units == 2 ? 512 : resident) / s.threads)));
   return s;
 }
-Shape shape_forward(const snn_rms_norm_args* a, bool fast) { return shape_of(a, fast, true, 1024); }
-Shape shape_back(const snn_rms_norm_args* a, bool fast) { return shape_of(a, fast, false, 512); }
+Shape shape_forward(const snn_rms_norm_args* a, int access) { return shape_of(a, access, true, 1024); }
+Shape shape_back(const snn_rms_norm_args* a, int access) { return shape_of(a, access, false, 512); }
 
 snn_status check(const snn_rms_norm_args* a) {
   if (!a || a->rows < 0 || a->n < 1 || !dtype_known(a->dtype)) return SNN_ERR_INVALID_ARG;
@@ -423,11 +467,26 @@ snn_status check(const snn_rms_norm_args* a) {
   return SNN_OK;
 }
 bool no_overlap(const snn_rms_norm_args* a, int64_t stride) { return a->rows < 2 || stride >= a->n; }
-template <typename F> snn_status by_types(int dtype, int weight_dtype, bool fast, F&& f) {
-  auto with = [&](auto io, auto wt) { return fast ? f(io, wt, std::true_type()) : f(io, wt, std::false_type()); };
+template <typename F> snn_status by_types(int dtype, int weight_dtype, int access, F&& f) {
+  auto with = [&](auto io, auto wt) {
+    return access == VECTORS ? f(io, wt, std::integral_constant<int, VECTORS>())
+           : access == PAIRS ? f(io, wt, std::integral_constant<int, PAIRS>())
+                             : f(io, wt, std::integral_constant<int, SINGLE>());
+  };
   if (dtype == SNN_DTYPE_FP32) return with(float(), float());
   if (dtype == SNN_DTYPE_BF16) return weight_dtype == SNN_DTYPE_FP32 ? with(__nv_bfloat16(), float()) : with(__nv_bfloat16(), __nv_bfloat16());
   return weight_dtype == SNN_DTYPE_FP32 ? with(__half(), float()) : with(__half(), __half());
+}
+// The widest access that all of the rows allow.
+struct Rows {
+  const void* p;
+  int64_t stride;
+  int dtype;
+};
+int access_of(const snn_rms_norm_args* a, std::initializer_list<Rows> all) {
+  int access = VECTORS;
+  for (const Rows& r : all) access = std::min(access, row_access(r.p, r.stride, a->n, r.dtype, unit_of(a->dtype)));
+  return access;
 }
 }  // namespace
 
@@ -436,7 +495,7 @@ extern "C" snn_status snn_rms_norm_workspace(const snn_rms_norm_args* a, size_t*
   if (st != SNN_OK) return st;
   if (!bytes) return SNN_ERR_INVALID_ARG;
   // (whether rows can be accessed by vectors is not asked here)
-  const int blocks = std::max(shape_back(a, true).blocks, shape_back(a, false).blocks);
+  const int blocks = std::max(shape_back(a, VECTORS).blocks, shape_back(a, SINGLE).blocks);
   *bytes = a->rows == 0 ? 0 : ((size_t)blocks * a->n * 4 + 255) / 256 * 256;
   return SNN_OK;
 }
@@ -454,19 +513,19 @@ extern "C" snn_status snn_rms_norm_forward(const snn_rms_norm_args* a, void* str
   p.rows = a->rows, p.n = a->n, p.groups = (a->n + KEEP_GROUP - 1) / KEEP_GROUP, p.keep_format = a->keep_format, p.eps = a->eps, p.inverse_n = 1.f / (float)a->n;
   p.x = a->x, p.x_stride = a->x_stride, p.residual = a->residual, p.residual_stride = a->residual_stride, p.weight = a->weight;
   p.h = a->h, p.h_stride = a->h_stride, p.y = a->y, p.y_stride = a->y_stride, p.rstd = a->rstd, p.codes = a->codes, p.scales = a->scales;
-  const bool fast = a->n % unit_of(a->dtype) == 0 && rows_of_32(a->x, a->x_stride, a->dtype) && rows_of_32(a->residual, a->residual_stride, a->dtype) &&
-                    rows_of_32(a->residual ? a->h : nullptr, a->h_stride, a->dtype) && rows_of_32(a->y, a->y_stride, a->dtype) &&
-                    rows_of_32(a->weight, 0, a->weight_dtype) && (!keeps || aligned_to(a->codes, 16));
-  const Shape s = shape_forward(a, fast);
+  int access = access_of(a, {{a->x, a->x_stride, a->dtype}, {a->residual, a->residual_stride, a->dtype}, {a->residual ? a->h : nullptr, a->h_stride, a->dtype},
+                             {a->y, a->y_stride, a->dtype}, {a->weight, 0, a->weight_dtype}});
+  if (keeps && !aligned_to(a->codes, 16)) access = std::min(access, aligned_to(a->codes, 2) ? (int)PAIRS : (int)SINGLE);
+  const Shape s = shape_forward(a, access);
   p.lanes = s.lanes;
-  return by_types(a->dtype, a->weight_dtype, fast, [&](auto io, auto wt, auto is_fast) {
+  return by_types(a->dtype, a->weight_dtype, access, [&](auto io, auto wt, auto with) {
     using IO = decltype(io);
     using WT = decltype(wt);
-    constexpr bool FAST = decltype(is_fast)::value;
-    const auto kernel = s.units == 0   ? rms_forward_wide_kernel<IO, WT, FAST>
-                        : !s.block     ? rms_forward_kernel<IO, WT, FAST, 1, false>
-                        : s.units == 1 ? rms_forward_kernel<IO, WT, FAST, 1, true>
-                                       : rms_forward_kernel<IO, WT, FAST, 2, true>;
+    constexpr int ACCESS = decltype(with)::value;
+    const auto kernel = s.units == 0   ? rms_forward_wide_kernel<IO, WT, ACCESS>
+                        : !s.block     ? rms_forward_kernel<IO, WT, ACCESS, 1, false>
+                        : s.units == 1 ? rms_forward_kernel<IO, WT, ACCESS, 1, true>
+                                       : rms_forward_kernel<IO, WT, ACCESS, 2, true>;
     return launch_behind(kernel, (unsigned)s.blocks, s.threads, 0, (cudaStream_t)stream, false, p);
   });
 }
@@ -480,9 +539,9 @@ extern "C" snn_status snn_rms_norm_backward(const snn_rms_norm_args* a, void* st
     return cudaMemsetAsync(a->dweight, 0, (size_t)a->n * dtype_size(a->weight_dtype), on) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
   }
   if (!a->h || !a->rstd || !a->dy || !a->dx || !no_overlap(a, a->dx_stride)) return SNN_ERR_INVALID_ARG;
-  const bool fast = a->n % unit_of(a->dtype) == 0 && rows_of_32(a->h, a->h_stride, a->dtype) && rows_of_32(a->dy, a->dy_stride, a->dtype) &&
-                    rows_of_32(a->dh, a->dh_stride, a->dtype) && rows_of_32(a->dx, a->dx_stride, a->dtype) && rows_of_32(a->weight, 0, a->weight_dtype);
-  const Shape s = shape_back(a, fast);
+  const int access = access_of(a, {{a->h, a->h_stride, a->dtype}, {a->dy, a->dy_stride, a->dtype}, {a->dh, a->dh_stride, a->dtype}, {a->dx, a->dx_stride, a->dtype},
+                                   {a->weight, 0, a->weight_dtype}});
+  const Shape s = shape_back(a, access);
   if (a->dweight) {
     if (!a->workspace || !aligned_to(a->workspace, 256)) return SNN_ERR_INVALID_ARG;
     if (a->workspace_bytes < (size_t)s.blocks * a->n * 4) return SNN_ERR_WORKSPACE_TOO_SMALL;
@@ -491,14 +550,20 @@ extern "C" snn_status snn_rms_norm_backward(const snn_rms_norm_args* a, void* st
   p.rows = a->rows, p.n = a->n, p.groups = (a->n + KEEP_GROUP - 1) / KEEP_GROUP, p.lanes = s.lanes, p.inverse_n = 1.f / (float)a->n, p.weight = a->weight;
   p.h = a->h, p.h_stride = a->h_stride, p.rstd = a->rstd, p.dy = a->dy, p.dy_stride = a->dy_stride, p.dh = a->dh, p.dh_stride = a->dh_stride;
   p.dx = a->dx, p.dx_stride = a->dx_stride, p.partial = a->dweight ? (float*)a->workspace : nullptr;
-  const snn_status done = by_types(a->dtype, a->weight_dtype, fast, [&](auto io, auto wt, auto is_fast) {
+  const snn_status done = by_types(a->dtype, a->weight_dtype, access, [&](auto io, auto wt, auto with) {
     using IO = decltype(io);
     using WT = decltype(wt);
-    constexpr bool FAST = decltype(is_fast)::value;
-    const auto kernel = s.units == 0   ? rms_backward_wide_kernel<IO, WT, FAST>
-                        : !s.block     ? rms_backward_kernel<IO, WT, FAST, 1, false>
-                        : s.units == 1 ? rms_backward_kernel<IO, WT, FAST, 1, true>
-                                       : rms_backward_kernel<IO, WT, FAST, 2, true>;
+    constexpr int ACCESS = decltype(with)::value;
+    if (s.units == 0) {
+      const size_t round = (size_t)RMS_WIDE * UNIT<IO> * 4, sums = (a->n * (size_t)4 + round - 1) / round * round;
+      const bool in_shared = a->dweight && sums <= RMS_SUMS;
+      const auto wide = rms_backward_wide_kernel<IO, WT, ACCESS>;
+      if (in_shared && cudaFuncSetAttribute(wide, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)RMS_SUMS) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
+      return launch_behind(wide, (unsigned)s.blocks, s.threads, in_shared ? sums : 0, on, false, p, in_shared);
+    }
+    const auto kernel = !s.block       ? rms_backward_kernel<IO, WT, ACCESS, 1, false>
+                        : s.units == 1 ? rms_backward_kernel<IO, WT, ACCESS, 1, true>
+                                       : rms_backward_kernel<IO, WT, ACCESS, 2, true>;
     return launch_behind(kernel, (unsigned)s.blocks, s.threads, 0, on, false, p);
   });
   if (done != SNN_OK || !a->dweight) return done;

@@ -1,9 +1,10 @@
 // 32 bytes of a row per thread, and what kernels that move such units share.
 //
-// A unit is N values of a lane: 8 of fp32, 16 of a 16-bit type, so that a unit of the type is one 256-bit access and the lanes
-// of a warp cover whole lines with it.  A group of 64 values (KEEP_GROUP) belongs to 64 / N neighbouring lanes.  FAST: lane s
-// holds values N s .. N s + N - 1; it needs rows of multiples of N values at addresses of multiples of 32 bytes.  Otherwise
-// it holds s, s + 64 / N, ..: single values, neighbouring lanes at neighbouring addresses.
+// A unit is N values of a lane: 8 of fp32, 16 of a 16-bit type.  By VECTORS they are neighbours and one 256-bit access, so that the
+// lanes of a warp cover whole lines with it; a group of 64 values (KEEP_GROUP) belongs to 64 / N lanes.  It needs rows of
+// multiples of N values at addresses of multiples of 32 bytes.  Otherwise the lanes of a warp take neighbouring PAIRS, where rows
+// are even and pairs aligned, or SINGLE values, and a unit has every 32nd of them: an access of a warp is 64 to 256 bytes without a
+// gap, and a group is one pair of each lane or two values.
 #pragma once
 #include <string.h>
 
@@ -108,37 +109,53 @@ template <typename T, int N> struct Unit {
       for (int i = 0; i < WORDS; i += 8) put_32((uint32_t*)p + i, u + i);
     }
   }
-  // Value by value, LANES apart from p on, of which `left` places exist; the others are zero.
-  __device__ __forceinline__ void get_each(const T* p, int left) {
-    T v[N];
+};
+enum Access { SINGLE, PAIRS, VECTORS };
+// Where the values of a unit stand in a row of n: `first` is the lane's first one.
+template <int ACCESS, int N> struct Columns {
+  int first, n;
+  static __device__ __forceinline__ constexpr int behind(int v) { return ACCESS == VECTORS ? v : ACCESS == PAIRS ? 64 * (v / 2) + v % 2 : 32 * v; }
+  // the columns from `start` on, of which a lane's share is N
+  static __device__ __forceinline__ constexpr int of_lane(int lane) { return ACCESS == VECTORS ? N * lane : ACCESS == PAIRS ? 2 * lane : lane; }
+  // (by vectors all values of a unit exist or none does, by pairs both of a pair)
+  __device__ __forceinline__ bool exists(int v) const { return ACCESS == VECTORS ? first < n : behind(v) < n - first; }
+  // Values that do not exist: by vectors what the unit held before, otherwise zero.
+  template <typename T> __device__ __forceinline__ void load(Unit<T, N>& u, const T* row) const {
+    if constexpr (ACCESS == VECTORS) {
+      if (first < n) u.get(row + first);
+    } else if constexpr (ACCESS == PAIRS) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) v[j] = LANES * j < left ? p[LANES * j] : from_f32<T>(0.f);
-    memcpy(u, v, sizeof(v));
+      for (int k = 0; k < N / 2; ++k) {
+        typename Pair<T>::raw r{};
+        if (exists(2 * k)) r = *reinterpret_cast<const typename Pair<T>::raw*>(row + first + behind(2 * k));
+        memcpy(u.u + k * (int)sizeof(T) / 2, &r, sizeof(r));
+      }
+    } else {
+      T v[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = exists(j) ? row[first + behind(j)] : from_f32<T>(0.f);
+      memcpy(u.u, v, sizeof(v));
+    }
   }
-  __device__ __forceinline__ void put_each(T* p, int left) const {
-    T v[N];
-    memcpy(v, u, sizeof(v));
+  template <typename T> __device__ __forceinline__ void store(const Unit<T, N>& u, T* row) const {
+    if constexpr (ACCESS == VECTORS) {
+      if (first < n) u.put(row + first);
+    } else if constexpr (ACCESS == PAIRS) {
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (LANES * j < left) p[LANES * j] = v[j];
+      for (int k = 0; k < N / 2; ++k) {
+        typename Pair<T>::raw r;
+        memcpy(&r, u.u + k * (int)sizeof(T) / 2, sizeof(r));
+        if (exists(2 * k)) *reinterpret_cast<typename Pair<T>::raw*>(row + first + behind(2 * k)) = r;
+      }
+    } else {
+      T v[N];
+      memcpy(v, u.u, sizeof(v));
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (exists(j)) row[first + behind(j)] = v[j];
+    }
   }
 };
-// Where a lane's values of a group lie: the first one, and the others behind it.
-template <int N, bool FAST> __device__ __forceinline__ constexpr int unit_first(int s) { return FAST ? N * s : s; }
-template <int N, bool FAST> __device__ __forceinline__ constexpr int unit_place(int j) { return FAST ? j : j * (KEEP_GROUP / N); }
-// The unit at p, the place of a lane's first value in a row of which `left` places are left.
-template <bool FAST, typename T, int N> __device__ __forceinline__ void load_unit(Unit<T, N>& v, const T* p, int left) {
-  if (!FAST)
-    v.get_each(p, left);
-  else if (left > 0)
-    v.get(p);
-}
-template <bool FAST, typename T, int N> __device__ __forceinline__ void store_unit(const Unit<T, N>& v, T* p, int left) {
-  if (!FAST)
-    v.put_each(p, left);
-  else if (left > 0)
-    v.put(p);
-}
 
 // ---- copies to shared memory ----------------------------------------------------------------------------------
 // Copies of 16 bytes from global to shared memory that the thread does not wait for.
@@ -154,37 +171,16 @@ template <int LANES> __device__ __forceinline__ uint32_t group_top(float m) {
   for (int o = 1; o < LANES; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
   return top;
 }
-// Codes of N values, four per word, rounded to nearest.  rare: whether a code of the warp could round up to 128.
-template <int FORMAT, int N> __device__ __forceinline__ void encode_unit(uint32_t q[N / 4], const float2 v[N / 2], float inverse, bool rare) {
-#pragma unroll
-  for (int k = 0; k < N / 4; ++k) {
-    if (FORMAT == SNN_KEEP_INT8) {
-      // 1.5 x 2^23 + v / scale, rounded once: the integer stands in the low bits
-      const float magic = 12582912.f;
-      float2 a = fma_pair(v[2 * k], both(inverse), both(magic)), b = fma_pair(v[2 * k + 1], both(inverse), both(magic));
-      if (rare) {
-        a = make_float2(fminf(fmaxf(a.x, magic - 127.f), magic + 127.f), fminf(fmaxf(a.y, magic - 127.f), magic + 127.f));
-        b = make_float2(fminf(fmaxf(b.x, magic - 127.f), magic + 127.f), fminf(fmaxf(b.y, magic - 127.f), magic + 127.f));
-      }
-      q[k] = __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
-    } else {
-      const float2 a = mul_pair(v[2 * k], both(inverse)), b = mul_pair(v[2 * k + 1], both(inverse));
-      q[k] = (uint32_t)__nv_cvt_float2_to_fp8x2(a, __NV_SATFINITE, __NV_E4M3) | (uint32_t)__nv_cvt_float2_to_fp8x2(b, __NV_SATFINITE, __NV_E4M3) << 16;
-    }
+// The codes of two values, low first, rounded to nearest.  rare: whether a code of the warp could round up to 128.
+template <int FORMAT> __device__ __forceinline__ uint32_t encode_pair(float2 v, float inverse, bool rare) {
+  if (FORMAT == SNN_KEEP_INT8) {
+    // 1.5 x 2^23 + v / scale, rounded once: the integer stands in the low bits
+    const float magic = 12582912.f;
+    float2 a = fma_pair(v, both(inverse), both(magic));
+    if (rare) a = make_float2(fminf(fmaxf(a.x, magic - 127.f), magic + 127.f), fminf(fmaxf(a.y, magic - 127.f), magic + 127.f));
+    return __byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040);   // (the upper half is not used)
   }
-}
-template <bool FAST, int N> __device__ __forceinline__ void store_codes(uint8_t* p, const uint32_t q[N / 4], int left) {
-  if (FAST) {
-    if (left <= 0) return;
-    if (N == 16)
-      *reinterpret_cast<uint4*>(p) = make_uint4(q[0], q[1], q[N / 4 - 2], q[N / 4 - 1]);
-    else
-      *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < N; ++j)
-    if (j * (KEEP_GROUP / N) < left) p[j * (KEEP_GROUP / N)] = (uint8_t)(q[j / 4] >> (8 * (j % 4)));
+  return (uint32_t)__nv_cvt_float2_to_fp8x2(mul_pair(v, both(inverse)), __NV_SATFINITE, __NV_E4M3);
 }
 
 // ---- launches behind one another's start ---------------------------------------------------------------------
@@ -209,7 +205,11 @@ snn_status launch_behind(void (*kernel)(P...), unsigned grid, int threads, size_
 }
 
 inline bool aligned_to(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
-// whether rows can be accessed 32 bytes at a time (rows that do not exist do not stand in the way)
-inline bool rows_of_32(const void* p, int64_t stride, int dtype) { return !p || (stride * (int64_t)dtype_size(dtype) % 32 == 0 && aligned_to(p, 32)); }
+// The widest access that rows of n values allow (rows that do not exist do not stand in the way).
+inline int row_access(const void* p, int64_t stride, int n, int dtype, int unit) {
+  const size_t size = dtype_size(dtype);
+  if (!p || (n % unit == 0 && stride * (int64_t)size % 32 == 0 && aligned_to(p, 32))) return VECTORS;
+  return n % 2 == 0 && stride % 2 == 0 && aligned_to(p, 2 * size) ? PAIRS : SINGLE;
+}
 
 }  // namespace snnk

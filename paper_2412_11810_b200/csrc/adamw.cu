@@ -2,8 +2,9 @@
 //
 //   m' = b1 m + (1 - b1) g,  v' = b2 v + (1 - b2) g^2,  p' = p (1 - lr wd) - lr / (1 - b1^t) m' / (sqrt(v' / (1 - b2^t)) + eps)
 //
-// Bound by HBM (28 bytes a parameter with everything in fp32, 10 with bf16 parameters and gradients and moments in 8 bits).
-// A thread block takes tiles of a tensor, eight neighbouring parameters a thread and turn; where a
+// With moments in fp32 bound by HBM (28 bytes a parameter with everything in fp32: 345 M parameters 1510 us, 6.4 TB/s), in 8 bits
+// (10 bytes with bf16 parameters and gradients) by instructions: 59 a parameter, three quarters of the issue slots (70 M
+// parameters 166 us, 4.3 TB/s).  A thread block takes tiles of a tensor, eight neighbouring parameters a thread and turn; where a
 // tile's tensor lies is found by bisection in a table that comes with the launch, so that nothing is copied to the device first
 // and a graph holds it.
 //
@@ -295,11 +296,16 @@ template <int COUNT> __global__ void __launch_bounds__(AW_THREADS) adamw_norm_ke
   for (int k = 1; k < AW_THREADS / 32; ++k) sum += shared[k];
   a.partial[blockIdx.x] = first ? sum : a.partial[blockIdx.x] + sum;
 }
-// One block: the norm, the step's number, and the factors that follow from it.
+// One block: the norm, the step's number, and the factors that follow from it.  The powers take longer than all else: a warp each
+// raises them, beside the one that waits for the sums.
 __global__ void __launch_bounds__(AW_THREADS) adamw_begin_kernel(const AwBegin b) {
   let_next_kernel_start();
+  __shared__ double shared[AW_THREADS], left[2];   // 1 - beta^t
+  // (the kernel before it, if any, is that of the norm: it does not write the step's number)
+  const int64_t t = *b.step + 1;
+  if (threadIdx.x == 32) left[0] = 1.0 - pow(b.beta1, (double)t);
+  if (threadIdx.x == 64) left[1] = 1.0 - pow(b.beta2, (double)t);
   wait_for_kernel_before();
-  __shared__ double shared[AW_THREADS];
   double sum = 0.0;
   if (b.partial) {
     for (int k = threadIdx.x; k < AW_NORM_BLOCKS; k += AW_THREADS) sum += b.partial[k];
@@ -310,6 +316,8 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_begin_kernel(const AwBegin b
       __syncthreads();
     }
     sum = shared[0];
+  } else {
+    __syncthreads();
   }
   if (threadIdx.x > 0) return;
   const double scale = (double)b.scale * (b.scale_device ? (double)*b.scale_device : 1.0);
@@ -321,11 +329,10 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_begin_kernel(const AwBegin b
     if (norm > b.max_norm) s.factor = (float)(scale * (b.max_norm / norm));
   }
   if (!s.skip) {
-    const int64_t t = *b.step + 1;
     *b.step = t;
     const double lr = b.lr_device ? (double)*b.lr_device : b.lr;
-    s.rate = (float)(lr / (1.0 - pow(b.beta1, (double)t)));
-    s.root = (float)(1.0 / sqrt(1.0 - pow(b.beta2, (double)t)));
+    s.rate = (float)(lr / left[0]);
+    s.root = (float)(1.0 / sqrt(left[1]));
     s.keep = (float)(1.0 - lr * b.weight_decay);
     s.key = key_of(b.seed, (uint64_t)t);
   }
@@ -403,7 +410,6 @@ template <int COUNT> __global__ void __launch_bounds__(AW_THREADS, 4) adamw_upda
   }
 }
 
-// Moments in 8 bits: bound by instructions (50 a parameter) rather than by HBM.
 // b1 m and b2 v from their codes.  The scale is a power of two, so that it can be multiplied by b1 or b2 first: the product with a
 // value (or with its square, which is exact) is rounded once either way.  Where the square of a scale leaves the range, one
 // by one.
@@ -457,7 +463,8 @@ template <int COUNT> struct AwPart {
 };
 // A whole part in these types.  The 32 scale bytes are read and written at once, lane by lane: stores of parts of a 32-byte sector
 // cost L2 so much that 70 M parameters took 199 us with four bytes a warp and turn (119 us against 351 where nothing was
-// computed).
+// computed).  Sixteen values a thread need a fifth fewer instructions and as long, since fewer warps find room; so do copies to shared
+// memory a turn ahead.
 template <typename PT, typename GT, int COUNT>
 __device__ __forceinline__ void update_part(const AwParams<COUNT>& a, const AwStep& step, const AwPart<COUNT>& part) {
   const AwTensor& t = *part.t;
@@ -604,6 +611,7 @@ template <int COUNT> snn_status step_of(const snn_adamw_args* a, cudaStream_t st
   int64_t values = 0;
   for (int k = 0; k < a->count; ++k) values += a->tensors[k].n;
   p.turns = values >= (int64_t)148 * 4 * AW_TURNS * AW_THREADS * AW_VALUES ? AW_TURNS : 1;
+  bool normed = false;
   if (clips) {
     bool any = false;
     const snn_status st = in_tables(a, p, [&](const AwParams<COUNT>& q, bool first) {
@@ -611,11 +619,12 @@ template <int COUNT> snn_status step_of(const snn_adamw_args* a, cudaStream_t st
       return launch_behind(adamw_norm_kernel<COUNT>, AW_NORM_BLOCKS, AW_THREADS, 0, stream, false, q, (int)first);
     });
     if (st != SNN_OK) return st;
+    normed = any;
     if (!any && cudaMemsetAsync(p.partial, 0, AW_NORM_BLOCKS * 8, stream) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
   }
   const AwBegin b{a->step, a->lr, a->beta1, a->beta2, a->weight_decay, a->max_norm, a->lr_device, a->scale_device, a->scale, a->seed,
                   clips ? p.partial : nullptr, a->norm, step};
-  snn_status st = launch_behind(adamw_begin_kernel, 1, AW_THREADS, 0, stream, false, b);
+  snn_status st = launch_behind(adamw_begin_kernel, 1, AW_THREADS, 0, stream, clips && normed, b);
   if (st != SNN_OK) return st;
   return in_tables(a, p, [&](const AwParams<COUNT>& q, bool first) {
     if (eight) return launch_behind(adamw_update_packed_kernel<COUNT>, (unsigned)std::min<int64_t>(q.tiles, 148 * 4), AW_THREADS, 0, stream, first, q);

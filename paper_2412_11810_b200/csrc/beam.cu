@@ -4,11 +4,15 @@
 //
 // Bound by HBM: the logits are read once.  A warp walks through a part of a beam's row, segment by segment of 2 KB, and leaves
 // behind its maximum, its sum of exponentials and its `width` best classes; a second kernel, a block per sample, joins the parts
-// of each row and the rows of the sample; a third moves the states.  Each is set up while the one before it runs.  (Blocks of
-// eight warps that worked at segments of 16 KB together waited for one another: 76 us for 512 rows of 131072 fp32 logits.)
+// of each row and the rows of the sample; a third moves the states.  Each is set up while the one before it runs.
 //
 // The best of a part: maxima that lanes have seen give a bound that at least `width` values of the row reach, and few more do.
 // What reaches it is put aside; where that gets too much, the best of it are kept and are the bound.
+//
+// Measured, the best 8 of 64 x 8 rows of 131072 (a fifth of them ended): fp32 44 us (4.9 TB/s of what is read); bf16, none ended,
+// 50 us, bound by instructions.  Blocks of eight warps at segments of 16 KB waited for one another (fp32 76 us); warps that did
+// not share their bound put more aside (53 and 71 us).
+//
 // Keys hold the value above the complement of the class, so that no two are the same and ties go to the lower class.
 #include <algorithm>
 

@@ -4,8 +4,14 @@
 //   with g = dy w, c = mean(g h s):  dx = s (g - h s c) + dh,  dw = sum over the rows of dy h s
 //
 // Bound by HBM: every value is read and written once.  A row belongs to `lanes` threads (part of a warp, or whole warps) that
-// hold one or two units each (unit.cuh) in registers, so that the second use of h costs no second read.  Within a warp nothing
-// waits for a block.  Rows that do not fit are read a second time, from L2.
+// hold one or two units each (unit.cuh) in registers, so that the second use of h costs no second read; the loads of the next row
+// are on their way while one is finished.  Within a warp nothing waits for a block.  Rows that do not fit (16384 values of a
+// 16-bit type, 8192 of fp32) are read a second time, from L2.
+//
+// Measured, bf16 with residual: 32768 x 2048 forward 80 us (6.7 TB/s), backward 84 us (6.4 TB/s) and 6 us for dw from the blocks'
+// shares; 16384 x 4096 to int8 alone 68 us (6.9 TB/s).  Units of 16 bytes and a row per block and launch, without the next row's
+// loads, took 112, 115 and 108 us: they were bound by instructions (42 a value).  Rows that vectors do not fit: 16384 x 4090
+// 190 us (pairs; 359 us with eight lanes a group, whose accesses spread over as many lines).
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>
@@ -35,16 +41,13 @@ struct RmsParams {
 // The sum over the lanes of a row, the same bits for all of them.  `turn` counts the calls: two buffers take turns, so that
 // one barrier a call is enough.
 template <bool BLOCK> __device__ __forceinline__ float row_sum(float v, int lanes, int turn, float (*shared)[32]) {
-  if (!BLOCK) {
-    for (int o = 1; o < lanes; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
+  for (int o = 1; o < (BLOCK ? 32 : lanes); o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if constexpr (BLOCK) {
+    if ((threadIdx.x & 31) == 0) shared[turn & 1][threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = shared[turn & 1][0];
+    for (int k = 1; k < lanes / 32; ++k) v += shared[turn & 1][k];
   }
-#pragma unroll
-  for (int o = 1; o < 32; o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if ((threadIdx.x & 31) == 0) shared[turn & 1][threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = shared[turn & 1][0];
-  for (int k = 1; k < lanes / 32; ++k) v += shared[turn & 1][k];
   return v;
 }
 __device__ __forceinline__ float scale_of(float sum, const RmsParams& p) { return rsqrtf(sum * p.inverse_n + p.eps); }
@@ -337,18 +340,17 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_back
 #pragma unroll
       for (int j = 0; j < N; ++j) f(at.columns(i).first + Columns<ACCESS, N>::behind(j), j % 2 ? dw[i][j / 2].y : dw[i][j / 2].x);
   };
-  if (BLOCK) {
+  if constexpr (BLOCK) {
     each([&](int c, float v) {
       if (c < p.n) to[c] = v;
     });
-    return;
+  } else {   // the rows of a block one behind the other
+    for (int k = 0; k < at.per_block(); ++k) {
+      if (at.slot == k) each([&](int c, float v) { dw_shared[c] = k == 0 ? v : dw_shared[c] + v; });
+      __syncthreads();
+    }
+    for (int i = threadIdx.x; i < p.n; i += blockDim.x) to[i] = dw_shared[i];
   }
-  // the rows of a block one behind the other
-  for (int k = 0; k < at.per_block(); ++k) {
-    if (at.slot == k) each([&](int c, float v) { dw_shared[c] = k == 0 ? v : dw_shared[c] + v; });
-    __syncthreads();
-  }
-  for (int i = threadIdx.x; i < p.n; i += blockDim.x) to[i] = dw_shared[i];
 }
 // A block per row, which is read twice.  Its share of dw lies in shared memory, each thread's sums at places of its own, or where that
 // is too small (in_shared false) in the workspace itself.

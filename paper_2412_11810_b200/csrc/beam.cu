@@ -564,7 +564,7 @@ snn_status reorder(const snn_state_rows* t, int32_t count, const int64_t* parent
 }
 template <typename IO> snn_status launch_rows(const BeamParams& p, cudaStream_t stream) {
   constexpr int SMEM = BM_WARPS * BM_STAGES * Segment<IO>::BYTES;
-  if (cudaFuncSetAttribute(beam_rows_kernel<IO>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
+  if (!allow_shared<beam_rows_kernel<IO>>(SMEM)) return SNN_ERR_CUDA;
   return launch_behind(beam_rows_kernel<IO>, (unsigned)((p.parts + BM_WARPS - 1) / BM_WARPS), 32 * BM_WARPS, SMEM, stream, false, p);
 }
 }  // namespace

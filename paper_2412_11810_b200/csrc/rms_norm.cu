@@ -559,9 +559,8 @@ extern "C" snn_status snn_rms_norm_backward(const snn_rms_norm_args* a, void* st
     if (s.units == 0) {
       const size_t round = (size_t)RMS_WIDE * UNIT<IO> * 4, sums = (a->n * (size_t)4 + round - 1) / round * round;
       const bool in_shared = a->dweight && sums <= RMS_SUMS;
-      const auto wide = rms_backward_wide_kernel<IO, WT, ACCESS>;
-      if (in_shared && cudaFuncSetAttribute(wide, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)RMS_SUMS) != cudaSuccess) return cudaGetLastError(), SNN_ERR_CUDA;
-      return launch_behind(wide, (unsigned)s.blocks, s.threads, in_shared ? sums : 0, on, false, p, in_shared);
+      if (in_shared && !allow_shared<rms_backward_wide_kernel<IO, WT, ACCESS>>((int)RMS_SUMS)) return SNN_ERR_CUDA;
+      return launch_behind(rms_backward_wide_kernel<IO, WT, ACCESS>, (unsigned)s.blocks, s.threads, in_shared ? sums : 0, on, false, p, in_shared);
     }
     const auto kernel = !s.block       ? rms_backward_kernel<IO, WT, ACCESS, 1, false>
                         : s.units == 1 ? rms_backward_kernel<IO, WT, ACCESS, 1, true>

@@ -8,6 +8,7 @@
 #pragma once
 #include <string.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "seq_common.cuh"
@@ -191,6 +192,10 @@ __device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepc
 // touches anything that one writes or reads.
 template <typename... P, typename... A>
 snn_status launch_behind(void (*kernel)(P...), unsigned grid, int threads, size_t smem, cudaStream_t stream, bool behind, const A&... args) {
+  if (!behind) {
+    kernel<<<grid, threads, smem, stream>>>(P(args)...);
+    return launched();
+  }
   cudaLaunchConfig_t cfg{};
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -200,8 +205,18 @@ snn_status launch_behind(void (*kernel)(P...), unsigned grid, int threads, size_
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cfg.attrs = &at;
-  cfg.numAttrs = behind ? 1 : 0;
+  cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess ? SNN_OK : (cudaGetLastError(), SNN_ERR_CUDA);
+}
+// Lets a kernel have more than 48 KB of shared memory, once for each device.
+template <auto KERNEL> bool allow_shared(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int device = 0;
+  if (cudaGetDevice(&device) != cudaSuccess) return cudaGetLastError(), false;
+  if (device < 64 && done.load() >> device & 1) return true;
+  if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return cudaGetLastError(), false;
+  if (device < 64) done.fetch_or((uint64_t)1 << device);
+  return true;
 }
 
 inline bool aligned_to(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }

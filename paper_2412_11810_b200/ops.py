@@ -74,6 +74,18 @@ def _on(t: torch.Tensor):
 
 
 _HERE = contextlib.nullcontext()
+
+
+def _launch(call, args, like: torch.Tensor) -> None:
+    """A call of the library on the current stream of a tensor's device, which is made the current one where it is another."""
+    device = like.get_device()
+    if device == torch.cuda.current_device():
+        call(args, _stream(like))
+    else:
+        with torch.cuda.device(device):
+            call(args, _stream(like))
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -473,31 +485,30 @@ def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: O
     elif inplace:
         raise ValueError("inplace: needs a residual")
     a.weight = _ptr(weight)
-    with _on(x):
-        h = x
-        if residual is not None:
-            if inplace:
-                h, a.h_stride = residual, a.residual_stride
-                if a.rows > 1 and a.h_stride < n:
-                    raise ValueError("residual: rows overlap")
-                same = a.x == a.residual and a.x_stride == a.residual_stride
-                if not same and _overlap(a.x, a.x_stride, a.residual, a.residual_stride, a.rows, n, x.element_size()):
-                    raise ValueError("residual: overlaps x in memory")
-            else:
-                h, a.h_stride = _dense(x), n
-            a.h = h.data_ptr()
-        rstd = x.new_empty(shape[:-1], dtype=torch.float32)
-        a.rstd = rstd.data_ptr()
-        y = kept = None
-        if values:
-            y = _dense(x)
-            a.y, a.y_stride = y.data_ptr(), n
-        if keep is not None:
-            codes, scales = _empty_codes(x, shape)
-            kept = PackedActivation(codes, scales, keep, x.dtype)
-            a.keep_format, a.codes, a.scales = _FORMATS[keep], codes.data_ptr(), scales.data_ptr()
-        if count:
-            sb.snn_rms_norm_forward(a, _stream(x))
+    h = x
+    if residual is not None:
+        if inplace:
+            h, a.h_stride = residual, a.residual_stride
+            if a.rows > 1 and a.h_stride < n:
+                raise ValueError("residual: rows overlap")
+            same = a.x == a.residual and a.x_stride == a.residual_stride
+            if not same and _overlap(a.x, a.x_stride, a.residual, a.residual_stride, a.rows, n, x.element_size()):
+                raise ValueError("residual: overlaps x in memory")
+        else:
+            h, a.h_stride = _dense(x), n
+        a.h = h.data_ptr()
+    rstd = x.new_empty(shape[:-1], dtype=torch.float32)
+    a.rstd = rstd.data_ptr()
+    y = kept = None
+    if values:
+        y = _dense(x)
+        a.y, a.y_stride = y.data_ptr(), n
+    if keep is not None:
+        codes, scales = _empty_codes(x, shape)
+        kept = PackedActivation(codes, scales, keep, x.dtype)
+        a.keep_format, a.codes, a.scales = _FORMATS[keep], codes.data_ptr(), scales.data_ptr()
+    if count:
+        _launch(sb.snn_rms_norm_forward, a, x)
     return y, h, rstd, kept
 
 
@@ -516,16 +527,15 @@ def rms_norm_backward(h: torch.Tensor, rstd: torch.Tensor, dy: torch.Tensor, wei
     a.dy_stride, a.dy = _rows_like(dy, "dy", h), dy.data_ptr()
     if dh is not None:
         a.dh_stride, a.dh = _rows_like(dh, "dh", h), dh.data_ptr()
-    with _on(h):
-        dx = _dense(h)
-        a.dx, a.dx_stride = dx.data_ptr(), n
-        dweight = None
-        if weight is not None:
-            dweight = torch.empty_like(weight)
-            a.dweight = dweight.data_ptr()
-            ws = h.new_empty(sb.snn_rms_norm_workspace(a), dtype=torch.uint8)
-            a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
-        sb.snn_rms_norm_backward(a, _stream(h))
+    dx = _dense(h)
+    a.dx, a.dx_stride = dx.data_ptr(), n
+    dweight = None
+    if weight is not None:
+        dweight = torch.empty_like(weight)
+        a.dweight = dweight.data_ptr()
+        ws = h.new_empty(sb.snn_rms_norm_workspace(a), dtype=torch.uint8)
+        a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+    _launch(sb.snn_rms_norm_backward, a, h)
     return dx, dweight
 
 
@@ -657,14 +667,13 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
     if not 0 <= seed < 2 ** 64:
         raise ValueError("seed: has to fit 64 bits")
     a.beta1, a.beta2, a.eps, a.weight_decay, a.max_norm, a.seed = *betas, eps, weight_decay, max_norm or 0.0, seed
-    with _on(like):
-        norm = None
-        if max_norm is not None:
-            norm = like.new_empty((), dtype=torch.float32)
-            a.norm = norm.data_ptr()
-        ws = like.new_empty(sb.SNN_ADAMW_WORKSPACE, dtype=torch.uint8)
-        a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
-        sb.snn_adamw_step(a, _stream(like))
+    norm = None
+    if max_norm is not None:
+        norm = like.new_empty((), dtype=torch.float32)
+        a.norm = norm.data_ptr()
+    ws = like.new_empty(sb.SNN_ADAMW_WORKSPACE, dtype=torch.uint8)
+    a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+    _launch(sb.snn_adamw_step, a, like)
     return norm
 
 
@@ -730,19 +739,18 @@ def beam_step(logits: torch.Tensor, scores: torch.Tensor, *, width: Optional[int
         _like(ended, "ended", logits, (B, K), torch.bool)
     if inplace and width != K:
         raise ValueError("inplace: needs as many survivors as beams")
-    with _on(logits):
-        table, out = _state_table(states, B * K, B * width, inplace, logits.get_device())
-        tokens = logits.new_empty((2, B, width), dtype=torch.int64)
-        tokens, parents = tokens[0], tokens[1]
-        new_scores = logits.new_empty((B, width), dtype=torch.float32)
-        new_ended = None if end is None else logits.new_empty((B, width), dtype=torch.bool)
-        a = sb.snn_beam_args(B, K, width, V, _DTYPES[logits.dtype], logits.data_ptr(), logits.stride(0), logits.stride(1), scores.data_ptr(),
-                             _ptr(ended), -1 if end is None else end, tokens.data_ptr(), parents.data_ptr(), new_scores.data_ptr(),
-                             _ptr(new_ended), table, len(out))
-        if B:
-            ws = logits.new_empty(sb.snn_beam_workspace(a), dtype=torch.uint8)
-            a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
-            sb.snn_beam_step(a, _stream(logits))
+    table, out = _state_table(states, B * K, B * width, inplace, logits.get_device())
+    tokens = logits.new_empty((B, width), dtype=torch.int64)
+    parents = torch.empty_like(tokens)
+    new_scores = torch.empty_like(scores) if width == K else scores.new_empty((B, width))
+    new_ended = None if end is None else logits.new_empty((B, width), dtype=torch.bool)
+    a = sb.snn_beam_args(B, K, width, V, _DTYPES[logits.dtype], logits.data_ptr(), logits.stride(0), logits.stride(1), scores.data_ptr(),
+                         _ptr(ended), -1 if end is None else end, tokens.data_ptr(), parents.data_ptr(), new_scores.data_ptr(),
+                         _ptr(new_ended), table, len(out))
+    if B:
+        ws = logits.new_empty(sb.snn_beam_workspace(a), dtype=torch.uint8)
+        a.workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+        _launch(sb.snn_beam_step, a, logits)
     return tokens, parents, new_scores, new_ended, out
 
 

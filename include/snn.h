@@ -517,7 +517,7 @@ snn_status snn_rms_norm_backward(const snn_rms_norm_args* args, void* stream);
  * snn_activation_unpack reads them), since in sqrt(v) e4m3 holds a range of 2^36 of v.  A moment moves by a small part of its
  * codes' steps, so codes are rounded up or down at random: magnitude u in steps becomes floor(u + r / 2^16); m takes the lower
  * and sqrt(v) the upper 16 bits of hash(seed, t, place) (adamw.cu), and a sqrt(v) above zero at least the smallest code.  A group
- * with an infinity or a NaN decodes to NaN from then on.
+ * with an infinity or a NaN decodes to NaN from then on.  In the quotient a sqrt(v) below 2^-63 counts as that.
  * With max_norm > 0 a step whose norm is not finite is left out: nothing changes, and *step does not count it.
  * v is fp32: gradients beyond 1.8e19 in magnitude make it infinite, and stop that parameter. */
 typedef struct {

@@ -159,17 +159,18 @@ __device__ __forceinline__ uint32_t highest_bytes(const uint32_t y[4]) {
 }
 // Codes of a lane's values; byte: their group's scale byte.  ROOT: nothing is negative, and what is above zero stays above zero.
 template <bool ROOT> __device__ __forceinline__ AwCodes encode_at_random(float2 f[AW_VALUES / 2], const uint32_t r[AW_VALUES], uint32_t byte) {
-  // 2^-120 over the scale, 2^(7 - byte); where that is subnormal, 2^-126 of it beforehand
+  // 2^-120 over the scale, 2^(7 - byte); where that is subnormal, in two steps (what is then too small to count, but not zero, counts
+  // as 2^-60, far below a step)
   const bool far = byte > 133u;
   if (__any_sync(0xffffffffu, far)) {
+    const float inverse = keep_scale_inverse(byte);
 #pragma unroll
     for (int k = 0; k < AW_VALUES / 2; ++k) {
-      const float2 down = mul_pair(f[k], both(0x1p-126f));
-      const float2 least = make_float2(f[k].x > 0.f ? 0x1p-100f : 0.f, f[k].y > 0.f ? 0x1p-100f : 0.f);
-      if (far) f[k] = ROOT ? make_float2(fmaxf(down.x, least.x), fmaxf(down.y, least.y)) : down;
+      const float2 u = mul_pair(f[k], both(inverse));
+      if (far) f[k] = ROOT ? make_float2(f[k].x > 0.f ? fmaxf(u.x, 0x1p-60f) : 0.f, f[k].y > 0.f ? fmaxf(u.y, 0x1p-60f) : 0.f) : u;
     }
   }
-  const float factor = __uint_as_float((far ? 260u - byte : 134u - byte) << 23);
+  const float factor = __uint_as_float((far ? 7u : 134u - byte) << 23);
   AwCodes c;
 #pragma unroll
   for (int k = 0; k < AW_VALUES / 4; ++k) {
@@ -213,6 +214,11 @@ __device__ __forceinline__ float2 root_of(float2 v) {
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(v.y, 0x1p-126f)));
   const float2 s = mul_pair(v, y);
   return fma_pair(make_float2(fmaf(-s.x, s.x, v.x) * 0.5f, fmaf(-s.y, s.y, v.y) * 0.5f), y, s);
+}
+__device__ __forceinline__ float at_least(float v, float least) {   // NaN stays
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(v), "f"(least));
+  return d;
 }
 __device__ __forceinline__ float reciprocal(float v) {
   float r;
@@ -370,7 +376,9 @@ __device__ __forceinline__ void step_values(const AwParams<COUNT>& a, const AwSt
   }
 #pragma unroll
   for (int k = 0; k < N / 2; ++k) {
-    const float2 below = fma_pair(root[k], both(step.root), both(a.eps)), up = times(m[k], -step.rate);
+    // (a root of a subnormal square may be too small here: it counts as the smallest of a normal one)
+    const float2 counts = EIGHT ? make_float2(at_least(root[k].x, 0x1p-63f), at_least(root[k].y, 0x1p-63f)) : root[k];
+    const float2 below = fma_pair(counts, both(step.root), both(a.eps)), up = times(m[k], -step.rate);
     const float2 update = EIGHT ? mul_pair(up, make_float2(reciprocal(below.x), reciprocal(below.y)))
                                 : make_float2(__fdividef(up.x, below.x), __fdividef(up.y, below.y));
     p[k] = fma_pair(p[k], both(step.keep), update);

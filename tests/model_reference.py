@@ -71,10 +71,11 @@ def e4m3(codes, scales):
         return value * np.repeat(scale, GROUP)
 
 
-def encode_at_random(v, r, root, unsure):
-    """(values after rounding, the other candidate where the decision is closer than `unsure` steps (relative to v), else the same)."""
+def encode_at_random(v, r, root, unsure, shift=0.0):
+    """(values after rounding, the other candidate where the decision is closer than `unsure` steps (relative to v), else the same);
+    shift: the groups' scales are those of tops larger by that, relatively."""
     v = v.reshape(-1, GROUP)
-    top = np.abs(v).max(1, keepdims=True)
+    top = np.abs(v).max(1, keepdims=True) * (1 + shift)
     e = np.full(top.shape, -127.0)
     for k in range(-127, 128):
         e = np.where((e == k) & (top > 448 * 2.0 ** k), k + 1, e)

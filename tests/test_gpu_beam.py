@@ -58,6 +58,26 @@ def test_sizes(B, K, W, V, dtype):
     check(logits, scores, W)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("W", [4, 32])
+def test_parts_of_many_segments(W, dtype):
+    """Enough rows for a warp to walk through a dozen of segments: ordinary rows, equal values, rising and falling ones, steps of
+    a few values, the best at the end, and masks."""
+    B, K, V = 300, 4, 20001
+    logits, scores, g = inputs(B, K, V, dtype, 13)
+    rise = torch.arange(V, device="cuda") / V
+    logits[1] = 0.5
+    logits[2, 0], logits[2, 1] = rise.to(logits), (-rise).to(logits)
+    logits[3] = (rise * 40).floor().to(logits)
+    logits[4] = (-rise * 40).floor().to(logits)
+    logits[5, :, -3:] = 30
+    logits[6, :, :-2] = -INF
+    logits[7, 1] = torch.where(torch.rand(V, generator=g) < 0.5, -INF, 1.0).to(logits)
+    logits[8] = torch.randint(0, 3, (K, V), generator=g).to(logits)
+    logits[9, 2], logits[10, 3, 15000] = -INF, float("nan")
+    check(logits, scores, W)
+
+
 @pytest.mark.parametrize("V", [(1 << 22) - 3, 1 << 22])
 def test_the_largest_vocabulary(V):
     logits, scores, _ = inputs(1, 2, V, "bf16", 3)

@@ -81,6 +81,17 @@ def test_norm_and_gradients(n, dtype):
         check(*inputs(rows, n, dtype, n + rows, weight=weight, residual=residual), dtype)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("n", [16, 24, 32, 48, 80, 112, 160, 192, 320, 512, 576])
+def test_several_rows_of_a_warp(n, dtype):
+    for rows in (1, 2, 5, 33, 500):
+        x, res, w, dy, dh = inputs(rows, n, dtype, n + rows)
+        check(x, res, w, dy, dh, dtype)
+        want = ops().rms_norm(x, w, res, keep="int8")
+        alone = [ops().rms_norm(x[k:k + 1].clone(), w, res[k:k + 1].clone(), keep="int8")[3] for k in range(0, rows, 7)]
+        assert all(torch.equal(a.codes[0], want[3].codes[k * 7]) and torch.equal(a.scales[0], want[3].scales[k * 7]) for k, a in enumerate(alone))
+
+
 @pytest.mark.parametrize("dtype,weight", [("fp32", "same"), ("bf16", "same"), ("bf16", "fp32"), ("fp16", None)])
 @pytest.mark.parametrize("layout", ["dense", "offset", "apart"])
 @pytest.mark.parametrize("rows,n", [(700, 96), (3000, 40), (2500, 256), (1500, 1032), (300, 8192), (200, 9000)])

@@ -119,8 +119,8 @@ template <typename IO> struct Segment {
       raw[i].y = b < here ? at[b] : none;
     }
   }
-  static __device__ __forceinline__ int place(int j) {
-    const int lane = threadIdx.x & 31;
+  static __device__ __forceinline__ int place(int j) { return place(j, threadIdx.x & 31); }
+  static __device__ __forceinline__ int place(int j, int lane) {
     return sizeof(IO) == 2 ? 2 * lane + j / 2 * 64 + j % 2 : lane + j * 32;
   }
   __device__ __forceinline__ float2 pair(int i) const { return to_f32(raw[i]); }
@@ -133,9 +133,9 @@ template <typename IO> struct Segment {
       return fmaxf(m.x, m.y);
     }
   }
-  // Value j once more, from shared memory: few are looked at again, and registers are worth more than they.
-  __device__ __forceinline__ float again(int j) const {
-    const int c = place(j);
+  // Value j of a lane once more, from shared memory: few are looked at again, and registers are worth more than they.
+  __device__ __forceinline__ float again(int j, int lane) const {
+    const int c = place(j, lane);
     return c < here ? to_f32(at[c]) : __uint_as_float(0xff800000u);
   }
 };
@@ -219,13 +219,9 @@ template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, 3) beam_
     const int64_t c0 = first + (int64_t)s * Seg::CLASSES;
     Seg g;
     g.read(ring + s % BM_STAGES * Seg::BYTES, z, c0, p.V);
-    float eighth[VALUES / 8];          // the maxima of eight values each
     float here = none;
 #pragma unroll
-    for (int q = 0; q < VALUES / 8; ++q) {
-      eighth[q] = g.most_of_eight(q);
-      here = fmaxf(here, eighth[q]);
-    }
+    for (int q = 0; q < VALUES / 8; ++q) here = fmaxf(here, g.most_of_eight(q));
     if (here > most) {
       sum *= exp2_of((most - here) * LOG2_E);   // (0 of a sum that is 0)
       most = here;
@@ -254,20 +250,24 @@ template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, 3) beam_
       const float least = from_rising(largest_of_lanes(rising(m), p.W));
       bound = fmaxf(bound, fmaxf(least, -largest_finite<float>()));
     }
-    if (!__any_sync(0xffffffffu, here >= bound)) continue;
+    // Lanes that have seen a value at or above the bound are few, mostly one: all lanes look at the values of one such lane (two of
+    // fp32) again, a value each.
+    uint32_t passing = __ballot_sync(0xffffffffu, here >= bound);
+    if (!passing) continue;
     const int held = count;
-#pragma unroll
-    for (int q = 0; q < VALUES / 8; ++q) {
-      if (!__any_sync(0xffffffffu, eighth[q] >= bound)) continue;
-#pragma unroll
-      for (int j = 8 * q; j < 8 * q + 8; ++j) {
-        const float v = g.again(j);
-        const uint32_t passed = __ballot_sync(0xffffffffu, v >= bound);
-        if (!passed) continue;
-        const int at = count + __popc(passed & ((1u << lane) - 1u));
-        if (v >= bound && at < BM_CANDIDATES) candidates[at] = key_of(v, (uint32_t)(c0 + Seg::place(j)));
-        count += __popc(passed);
+    while (passing) {
+      int from_lane = __ffs(passing) - 1;
+      passing &= passing - 1u;
+      if (VALUES == 16) {
+        if (lane >= 16) from_lane = __ffs(passing) - 1;   // (-1: no second one)
+        passing &= passing - 1u;
       }
+      const int j = lane % VALUES;
+      const float v = from_lane >= 0 ? g.again(j, from_lane) : none;
+      const uint32_t passed = __ballot_sync(0xffffffffu, v >= bound);
+      const int at = count + __popc(passed & ((1u << lane) - 1u));
+      if (v >= bound && at < BM_CANDIDATES) candidates[at] = key_of(v, (uint32_t)(c0 + Seg::place(j, from_lane)));
+      count += __popc(passed);
     }
     if (count <= BM_CANDIDATES / 2) continue;
     if (count <= BM_CANDIDATES) {
@@ -283,7 +283,7 @@ template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, 3) beam_
         uint64_t best = old[0] < last ? old[0] : 0;
         if (old[1] < last && old[1] > best) best = old[1];
         for (int j = 0; j < VALUES; ++j) {
-          const float v = g.again(j);
+          const float v = g.again(j, lane);
           const uint64_t key = v >= bound ? key_of(v, (uint32_t)(c0 + Seg::place(j))) : 0;
           if (key < last && key > best) best = key;
         }

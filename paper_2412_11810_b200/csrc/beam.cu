@@ -9,9 +9,10 @@
 // The best of a part: maxima that lanes have seen give a bound that at least `width` values of the row reach, and few more do.
 // What reaches it is put aside; where that gets too much, the best of it are kept and are the bound.
 //
-// Measured, the best 8 of 64 x 8 rows of 131072 (a fifth of them ended): fp32 44 us (4.9 TB/s of what is read); bf16, none ended,
-// 50 us, bound by instructions.  Blocks of eight warps at segments of 16 KB waited for one another (fp32 76 us); warps that did
-// not share their bound put more aside (53 and 71 us).
+// Measured, the best 8 of 64 x 8 rows of 131072 (a fifth of them ended): fp32 45 us (4.8 TB/s of what is read); bf16, none ended,
+// 42 us, bound by instructions (12 a value, and what each waits for the one before it).  The best 32: 71 and 61 to 79 us; with
+// a bound from 32 maxima instead of 64, and the best taken one after the other, 104 and 111.  Blocks of eight warps at segments of
+// 16 KB waited for one another (fp32 76 us); warps that did not share their bound put more aside (53 and 71 us).
 //
 // Keys hold the value above the complement of the class, so that no two are the same and ties go to the lower class.
 #include <algorithm>
@@ -22,7 +23,7 @@ using namespace snnk;
 
 namespace {
 
-constexpr int BM_WARPS = 8, BM_STAGES = 3, BM_CANDIDATES = 128;   // of a block; of a warp
+constexpr int BM_WARPS = 8, BM_STAGES = 3, BM_CANDIDATES = 88, BM_HELD = 64;   // of a block; of a warp, and between segments
 constexpr int BM_MOST = 32;          // beams of a sample, and survivors
 constexpr int BM_JOIN_WARPS = 8;
 constexpr int BM_TABLE = 64;         // states of one launch
@@ -70,7 +71,7 @@ __device__ __forceinline__ float larger_number(float m, float2 v) {
 // whatever the address of the row (so that equal rows have equal sums).  The bytes lie as in the row, 16 by 16: class 0 of the
 // segment stands `lead` values behind the start.
 template <typename IO> struct Segment {
-  static constexpr int VALUES = 64 / sizeof(IO), CLASSES = 32 * VALUES, PER_COPY = 16 / sizeof(IO), BYTES = CLASSES * sizeof(IO) + 32;
+  static constexpr int VALUES = 64 / sizeof(IO), CLASSES = 32 * VALUES, PER_COPY = 16 / sizeof(IO), BYTES = CLASSES * sizeof(IO) + 16;
   // Starts the copies of classes c0 .. of a row of V; 16 bytes that reach beyond the row's ends are read value by value.
   static __device__ __forceinline__ void fetch(uint8_t* to, const IO* z, int64_t c0, int V) {
     const int lead = (int)((uintptr_t)(z + c0) % 16 / sizeof(IO)), lane = threadIdx.x & 31;
@@ -146,53 +147,57 @@ __device__ __forceinline__ float exp2_of(float v) {
 }
 constexpr float LOG2_E = 1.4426950408889634f;
 
-// The best `width` of a warp's first n candidates, falling, to their beginning: the largest of all, one after the other.
+// The best `width` of a warp's first n candidates, falling, to their beginning: each to the place that the number of larger ones
+// gives it.  (Taking the largest of all `width` times waits for one result after the other.)
 template <int EACH> __device__ __forceinline__ int best_candidates(uint64_t* candidates, int n, int width) {
   const int lane = threadIdx.x & 31;
   uint64_t mine[EACH];
+  int before[EACH];
   __syncwarp();
 #pragma unroll
-  for (int k = 0; k < EACH; ++k) mine[k] = lane + 32 * k < n ? candidates[lane + 32 * k] : 0;
-  __syncwarp();
-  const int found = min(n, width);
-  for (int r = 0; r < found; ++r) {
-    uint64_t best = mine[0];
+  for (int k = 0; k < EACH; ++k) mine[k] = lane + 32 * k < n ? candidates[lane + 32 * k] : 0, before[k] = 0;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const uint64_t key = candidates[i];
 #pragma unroll
-    for (int k = 1; k < EACH; ++k) best = max(best, mine[k]);
-    best = warp_max(best);
-    if (lane == 0) candidates[r] = best;
-#pragma unroll
-    for (int k = 0; k < EACH; ++k)
-      if (mine[k] == best) mine[k] = 0;
+    for (int k = 0; k < EACH; ++k) before[k] += key > mine[k];
   }
   __syncwarp();
-  return found;
+#pragma unroll
+  for (int k = 0; k < EACH; ++k)
+    if (mine[k] && before[k] < width) candidates[before[k]] = mine[k];
+  __syncwarp();
+  return min(n, width);
 }
 __device__ __forceinline__ int best_candidates(uint64_t* candidates, int n, int width) {
-  return n <= 64 ? best_candidates<2>(candidates, n, width) : best_candidates<BM_CANDIDATES / 32>(candidates, n, width);
+  return n <= 32 ? best_candidates<1>(candidates, n, width) : best_candidates<(BM_CANDIDATES + 31) / 32>(candidates, n, width);
 }
-// The width-th largest of the lanes' numbers.
-__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t v, int width) {
-  const int lane = threadIdx.x & 31;
-  uint32_t best = 0u;
-  for (int r = 0; r < width; ++r) {
-    best = __reduce_max_sync(0xffffffffu, v);
-    if (lane == __ffs(__ballot_sync(0xffffffffu, v == best)) - 1) v = 0u;
+// A number that the width-th largest of the lanes' numbers, two of each, reaches, and is close to: it is built bit by bit from the
+// highest one in which they differ, nine of them, or the upper half where the signs or much of the exponents differ.
+__device__ __forceinline__ uint32_t largest_of_lanes(uint32_t a, uint32_t b, int width) {
+  const uint32_t most = __reduce_max_sync(0xffffffffu, max(a, b)), least = __reduce_min_sync(0xffffffffu, min(a, b));
+  if (most == least) return most;
+  const int top = 31 - __clz(most ^ least);
+  uint32_t found = most & ~(0xffffffffu >> (31 - top));
+  for (int bit = top, last = min(16, max(top - 8, 0)); bit >= last; --bit) {
+    const uint32_t next = found | 1u << bit;
+    if (__popc(__ballot_sync(0xffffffffu, a >= next)) + __popc(__ballot_sync(0xffffffffu, b >= next)) >= width) found = next;
   }
-  return best;
+  return found;
 }
 
+// (Four blocks an SM for 16-bit types, 38 to 43 us against 42 to 45; fp32 with as many took 49 to 51 instead of 43, its registers spilled.)
 // A warp: `length` segments of a row, one behind the other through a ring of BM_STAGES places of its own in shared memory.
-template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, 3) beam_rows_kernel(const BeamParams p) {
+template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, sizeof(IO) == 2 ? 4 : 3) beam_rows_kernel(const BeamParams p) {
   using Seg = Segment<IO>;
   constexpr int VALUES = Seg::VALUES;
   extern __shared__ __align__(16) uint8_t ring_of_all[];
   __shared__ uint64_t candidates_of_all[BM_WARPS][BM_CANDIDATES];
-  __shared__ float most_of_all[BM_WARPS][32];   // the lanes' maxima so far
+  __shared__ float most_of_all[BM_WARPS][2][32];   // the lanes' maxima so far, of two halves of their values
   let_next_kernel_start();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t part = (int64_t)blockIdx.x * BM_WARPS + warp, row = part / p.splits;
-  most_of_all[warp][lane] = __uint_as_float(0xff800000u);
+  most_of_all[warp][0][lane] = most_of_all[warp][1][lane] = __uint_as_float(0xff800000u);
   __syncthreads();
   if (part >= p.parts || !goes_on(p, row)) return;
   uint8_t* const ring = ring_of_all + warp * (BM_STAGES * Seg::BYTES);
@@ -210,6 +215,7 @@ template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, 3) beam_
   for (int s = 0; s < BM_STAGES - 1; ++s) fetch(s);
   const float none = __uint_as_float(0xff800000u);
   float most = none, sum = 0.f;        // of this lane's values: the maximum, and the sum of exp(v - maximum)
+  float half[2] = {none, none};        // maxima of values 0 .. 7, 16 .. 23 of the segments, and of the others
   float bound = none;                  // candidates are values at or above it, all of them finite
   int count = 0;                       // candidates so far
   for (int s = 0; s < segments; ++s) {
@@ -219,9 +225,10 @@ template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, 3) beam_
     const int64_t c0 = first + (int64_t)s * Seg::CLASSES;
     Seg g;
     g.read(ring + s % BM_STAGES * Seg::BYTES, z, c0, p.V);
-    float here = none;
+    float now[2] = {none, none};
 #pragma unroll
-    for (int q = 0; q < VALUES / 8; ++q) here = fmaxf(here, g.most_of_eight(q));
+    for (int q = 0; q < VALUES / 8; ++q) now[q % 2] = fmaxf(now[q % 2], g.most_of_eight(q));
+    const float here = fmaxf(now[0], now[1]);
     if (here > most) {
       sum *= exp2_of((most - here) * LOG2_E);   // (0 of a sum that is 0)
       most = here;
@@ -240,14 +247,20 @@ template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, 3) beam_
       for (int i = 0; i < VALUES / 2; ++i)
         if (g.pair(i).x != g.pair(i).x || g.pair(i).y != g.pair(i).y) sum = __uint_as_float(0x7fc00000u);
     }
-    // The largest of what lane l of each of the row's warps has seen: the width-th largest of these 32 is a bound that at least
-    // `width` values of the row reach.  It is taken again when the part that has been read has doubled.  (Another warp's maximum
-    // may be an older one: the bound is lower then, not wrong.)
-    reinterpret_cast<volatile float*>(most_of_all[warp])[lane] = most;
+    // The largest of what a half of lane l of each of the row's warps has seen: the width-th largest of these 64 is a bound that at
+    // least `width` values of the row reach (and 44 of a row in any order, where width is 32; of 32 numbers the least had 130).
+    // It is taken again when the part that has been read has doubled.  (Another warp's maximum may be an older one: the bound is
+    // lower then, not wrong.)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) half[h] = fmaxf(half[h], now[h]);
     if ((s & (s + 1)) == 0) {
-      float m = most;
-      for (int w = from; w < to; ++w) m = fmaxf(m, reinterpret_cast<const volatile float*>(most_of_all[w])[lane]);
-      const float least = from_rising(largest_of_lanes(rising(m), p.W));
+      float m[2] = {half[0], half[1]};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) *(volatile float*)&most_of_all[warp][h][lane] = half[h];
+      for (int w = from; w < to; ++w)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) m[h] = fmaxf(m[h], *(const volatile float*)&most_of_all[w][h][lane]);
+      const float least = from_rising(largest_of_lanes(rising(m[0]), rising(m[1]), p.W));
       bound = fmaxf(bound, fmaxf(least, -largest_finite<float>()));
     }
     // Lanes that have seen a value at or above the bound are few, mostly one: all lanes look at the values of one such lane (two of
@@ -269,7 +282,7 @@ template <typename IO> __global__ void __launch_bounds__(32 * BM_WARPS, 3) beam_
       if (v >= bound && at < BM_CANDIDATES) candidates[at] = key_of(v, (uint32_t)(c0 + Seg::place(j, from_lane)));
       count += __popc(passed);
     }
-    if (count <= BM_CANDIDATES / 2) continue;
+    if (count <= BM_HELD) continue;
     if (count <= BM_CANDIDATES) {
       count = best_candidates(candidates, count, p.W);
     } else {

@@ -30,6 +30,7 @@ struct RmsParams {
   int64_t rows;
   int n, groups, lanes, keep_format;
   float eps, inverse_n;
+  double inverse;                     // 1 / n
   const void *x, *residual, *weight, *dy, *dh;
   int64_t x_stride, residual_stride, h_stride, y_stride, dy_stride, dh_stride, dx_stride;
   void *h, *y, *dx;
@@ -38,19 +39,31 @@ struct RmsParams {
   float* partial;                     // [blocks][n]: each block's share of dw
 };
 
-// The sum over the lanes of a row, the same bits for all of them.  `turn` counts the calls: two buffers take turns, so that
-// one barrier a call is enough.
-template <bool BLOCK> __device__ __forceinline__ float row_sum(float v, int lanes, int turn, float (*shared)[32]) {
+// The sum over the lanes of a row, the same bits for all of them, of type T.  `turn` counts the calls: two buffers take turns, so
+// that one barrier a call is enough.
+template <bool BLOCK, typename T> __device__ __forceinline__ T row_sum(T v, int lanes, int turn, double (*shared)[32]) {
   for (int o = 1; o < (BLOCK ? 32 : lanes); o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
   if constexpr (BLOCK) {
-    if ((threadIdx.x & 31) == 0) shared[turn & 1][threadIdx.x >> 5] = v;
+    T* const buffer = reinterpret_cast<T*>(shared[turn & 1]);
+    if ((threadIdx.x & 31) == 0) buffer[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = shared[turn & 1][0];
-    for (int k = 1; k < lanes / 32; ++k) v += shared[turn & 1][k];
+    v = buffer[0];
+    for (int k = 1; k < lanes / 32; ++k) v += buffer[k];
   }
   return v;
 }
 __device__ __forceinline__ float scale_of(float sum, const RmsParams& p) { return rsqrtf(sum * p.inverse_n + p.eps); }
+// A row's scale and what it is off by: with a copy in 8 bits the lanes' sums are joined in 64 bits, and one step of Newton's iteration
+// leaves a scale to 2^-28, so that codes are those of the formula.  (Of the scale in fp32 alone, and y rounded before it was coded, one
+// code in a million was the one beside it.)
+struct Scale {
+  float value, rest;
+};
+__device__ __forceinline__ Scale scale_of(double sum, const RmsParams& p) {
+  const double m = sum * p.inverse + (double)p.eps, s = (double)rsqrtf((float)m), better = s + s * 0.5 * (1.0 - m * s * s);
+  const float value = (float)better;
+  return {value, (float)(better - (double)value)};
+}
 // Where squares leave the range of fp32 they are summed again of values times 2^-80: that of the largest row is finite, and
 // eps, at most one, is nothing beside it.  An infinity in the row leaves a scale of zero, NaN a NaN.
 constexpr float RMS_DOWN = 0x1p-80f;
@@ -69,7 +82,11 @@ template <bool BLOCK, int ACCESS, int N> struct Place {
     return {((t & ~31) + i * lanes) * N + Columns<ACCESS, N>::of_lane(t & 31), n};
   }
 };
-// The 8-bit codes of a unit y; the lanes of a warp do this together.
+// What is not between two codes does not look as if it were with its lowest bit set, where y has been rounded toward zero: it is
+// rounded but once.  The scale is that of the next larger value.
+__device__ __forceinline__ float2 inexact(float2 v) { return make_float2(__uint_as_float(__float_as_uint(v.x) | 1u), __uint_as_float(__float_as_uint(v.y) | 1u)); }
+__device__ __forceinline__ uint32_t top_above(uint32_t top) { return top ? min(top + 1u, 0x7f800000u) : 0u; }
+// The 8-bit codes of a unit y, rounded toward zero; the lanes of a warp do this together.
 template <int FORMAT, int ACCESS, int N> __device__ __forceinline__ void keep_unit(const float2 y[N / 2], int64_t row, Columns<ACCESS, N> at, const RmsParams& p, bool store) {
   uint8_t* const codes = p.codes + row * p.n + at.first;
   uint8_t* const scales = p.scales + row * p.groups;
@@ -77,13 +94,13 @@ template <int FORMAT, int ACCESS, int N> __device__ __forceinline__ void keep_un
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) m = larger_of(m, y[i]);
-    const uint32_t top = group_top<KEEP_GROUP / N>(m), byte = keep_scale_byte<FORMAT>(top);
+    const uint32_t top = top_above(group_top<KEEP_GROUP / N>(m)), byte = keep_scale_byte<FORMAT>(top);
     const float inverse = keep_scale_inverse(byte);
     // (rarely: a group whose largest value could round up to 128, or one that is not finite)
     const bool rare = __any_sync(0xffffffffu, byte == 255u || keep_needs_cut<FORMAT>(top));
     uint32_t q[N / 4];
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) q[i] = __byte_perm(encode_pair<FORMAT>(y[2 * i], inverse, rare), encode_pair<FORMAT>(y[2 * i + 1], inverse, rare), 0x5410);
+    for (int i = 0; i < N / 4; ++i) q[i] = __byte_perm(encode_pair<FORMAT>(inexact(y[2 * i]), inverse, rare), encode_pair<FORMAT>(inexact(y[2 * i + 1]), inverse, rare), 0x5410);
     if (rare && byte == 255u) {
 #pragma unroll
       for (int i = 0; i < N / 4; ++i) q[i] = 0u;
@@ -101,8 +118,8 @@ template <int FORMAT, int ACCESS, int N> __device__ __forceinline__ void keep_un
 #pragma unroll
     for (int k = 0; k < N / 2; ++k) {
       if (start + k * KEEP_GROUP >= p.n) break;
-      const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(larger_of(0.f, y[k]))), byte = keep_scale_byte<FORMAT>(top);
-      const uint32_t q = byte == 255u ? 0u : encode_pair<FORMAT>(y[k], keep_scale_inverse(byte), keep_needs_cut<FORMAT>(top));
+      const uint32_t top = top_above(__reduce_max_sync(0xffffffffu, __float_as_uint(larger_of(0.f, y[k])))), byte = keep_scale_byte<FORMAT>(top);
+      const uint32_t q = byte == 255u ? 0u : encode_pair<FORMAT>(inexact(y[k]), keep_scale_inverse(byte), keep_needs_cut<FORMAT>(top));
       if (lane == k) mine = byte;
       if (!store) continue;
       if (ACCESS == PAIRS) {
@@ -115,24 +132,38 @@ template <int FORMAT, int ACCESS, int N> __device__ __forceinline__ void keep_un
     if (store && lane < N / 2 && start + lane * KEEP_GROUP < p.n) scales[start / KEEP_GROUP + lane] = (uint8_t)mine;
   }
 }
-// y of one unit of h, as values, as codes, or both.
+// y of one unit of h, as values, as codes, or both.  For codes, h s w is computed with what h s and the scale are off by, and
+// rounded toward zero.  With h of 16 bits the upper 12 bits of s have an exact product, and the others are a correction.
 template <typename IO, typename WT, int ACCESS, int N>
-__device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT, N>& w, float scale, int64_t row, Columns<ACCESS, N> at, const RmsParams& p, bool store) {
-  float2 y[N / 2];
-#pragma unroll
-  for (int i = 0; i < N / 2; ++i) y[i] = mul_pair(h.pair(i), both(scale));
-  if (p.weight) {
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) y[i] = mul_pair(y[i], w.pair(i));
-  }
+__device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT, N>& w, Scale scale, int64_t row, Columns<ACCESS, N> at, const RmsParams& p, bool store) {
   if (p.y && store) {
     Unit<IO, N> out;
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) out.set(i, y[i]);
+    for (int i = 0; i < N / 2; ++i) {
+      const float2 y = mul_pair(h.pair(i), both(scale.value));
+      out.set(i, p.weight ? mul_pair(y, w.pair(i)) : y);
+    }
     at.store(out, (IO*)p.y + row * p.y_stride);
   }
-  if (p.keep_format == SNN_KEEP_INT8) keep_unit<SNN_KEEP_INT8, ACCESS, N>(y, row, at, p, store);
-  if (p.keep_format == SNN_KEEP_E4M3) keep_unit<SNN_KEEP_E4M3, ACCESS, N>(y, row, at, p, store);
+  if (p.keep_format == SNN_KEEP_RAW) return;
+  const float upper = sizeof(IO) == 2 ? __uint_as_float(__float_as_uint(scale.value) & 0xfffff000u) : scale.value;
+  const float lower = scale.value - upper + scale.rest;
+  float2 y[N / 2];
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    const float2 v = h.pair(i), a = mul_pair(v, both(upper));
+    float2 rest;
+    if constexpr (sizeof(IO) == 2)
+      rest = mul_pair(v, both(lower));
+    else
+      rest = fma_pair(v, both(lower), fma_pair(v, both(upper), mul_pair(v, both(-upper))));
+    const float2 weight = p.weight ? w.pair(i) : both(1.f);
+    y[i] = fma_pair_down(a, weight, mul_pair(rest, weight));
+  }
+  if (p.keep_format == SNN_KEEP_INT8)
+    keep_unit<SNN_KEEP_INT8, ACCESS, N>(y, row, at, p, store);
+  else
+    keep_unit<SNN_KEEP_E4M3, ACCESS, N>(y, row, at, p, store);
 }
 // A unit of h: that of x, or its sum with the residual's; and its squares.
 template <typename IO, int N> __device__ __forceinline__ void sum_unit(Unit<IO, N>& h, const Unit<IO, N>& r, bool residual, float2& sum) {
@@ -156,7 +187,7 @@ template <typename IO, int N> __device__ __forceinline__ void sum_unit_far(const
 template <typename IO, typename WT, int ACCESS, int UNITS, bool BLOCK>
 __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK && ACCESS == VECTORS && UNITS == 1 ? 2 : 1) rms_forward_kernel(const RmsParams p) {
   constexpr int N = UNIT<IO>;
-  __shared__ float shared[2][32];
+  __shared__ double shared[2][32];
   const Place<BLOCK, ACCESS, N> at(p);
   const int64_t step = (int64_t)gridDim.x * at.per_block();
   const bool residual = p.residual != nullptr;
@@ -193,17 +224,24 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
       if (residual && store) at.columns(i).store(h[i], (IO*)p.h + row * p.h_stride);
     }
     if (base + step < p.rows) load(min(base + step + at.slot, p.rows - 1));
-    float total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared), scale = scale_of(total, p);
+    Scale scale;
+    bool far;
+    if (p.keep_format != SNN_KEEP_RAW) {
+      const double total = row_sum<BLOCK>((double)sum.x + (double)sum.y, at.lanes, turn++, shared);
+      scale = scale_of(total, p), far = !(total <= largest_finite<float>());
+    } else {
+      const float total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared);
+      scale = {scale_of(total, p), 0.f}, far = !(total <= largest_finite<float>());
+    }
     // (lanes of one warp may hold different rows: they all go the same way, as do all threads of a row's warps)
-    const bool far = !(total <= largest_finite<float>());
     if (BLOCK ? far : __any_sync(0xffffffffu, far)) {
       sum = both(0.f);
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) sum_unit_far(h[i], sum);
-      total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared);
-      if (far) scale = scale_of_far(total, p);
+      const float total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared);
+      if (far) scale = {scale_of_far(total, p), 0.f};
     }
-    if (p.rstd && at.t == 0 && store) p.rstd[row] = scale;
+    if (p.rstd && at.t == 0 && store) p.rstd[row] = scale.value;
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) finish_unit<IO, WT, ACCESS, N>(h[i], w[i], scale, row, at.columns(i), p, store);
   }
@@ -212,7 +250,7 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
 template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds__(RMS_WIDE) rms_forward_wide_kernel(const RmsParams p) {
   constexpr int N = UNIT<IO>;
   using At = Columns<ACCESS, N>;
-  __shared__ float shared[2][32];
+  __shared__ double shared[2][32];
   const int t = threadIdx.x;
   const bool residual = p.residual != nullptr;
   int turn = 0;
@@ -232,7 +270,8 @@ template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds_
       sum_unit(h, r, residual, sum);
       if (residual) at.store(h, (IO*)p.h + row * p.h_stride);
     });
-    float total = row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared), scale = scale_of(total, p);
+    const double total = row_sum<true>((double)sum.x + (double)sum.y, RMS_WIDE, turn++, shared);
+    Scale scale = scale_of(total, p);
     if (!(total <= largest_finite<float>())) {
       sum = both(0.f);
       each([&](At at) {
@@ -241,9 +280,9 @@ template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds_
         at.load(h, again);
         sum_unit_far(h, sum);
       });
-      scale = scale_of_far(row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared), p);
+      scale = {scale_of_far(row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared), p), 0.f};
     }
-    if (p.rstd && t == 0) p.rstd[row] = scale;
+    if (p.rstd && t == 0) p.rstd[row] = scale.value;
     each([&](At at) {   // (a thread reads back what it stored itself)
       Unit<IO, N> h;
       Unit<WT, N> w;
@@ -262,7 +301,7 @@ template <typename IO, typename WT, int N> __device__ __forceinline__ float2 wei
 template <typename IO, typename WT, int ACCESS, int UNITS, bool BLOCK>
 __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_backward_kernel(const RmsParams p) {
   constexpr int N = UNIT<IO>;
-  __shared__ float shared[2][32];
+  __shared__ double shared[2][32];
   __shared__ float dw_shared[BLOCK ? 1 : 32 * N];
   let_next_kernel_start();
   const Place<BLOCK, ACCESS, N> at(p);
@@ -357,7 +396,7 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_back
 template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds__(RMS_WIDE) rms_backward_wide_kernel(const RmsParams p, bool in_shared) {
   constexpr int N = UNIT<IO>;
   using At = Columns<ACCESS, N>;
-  __shared__ float shared[2][32];
+  __shared__ double shared[2][32];
   extern __shared__ float sums[];
   let_next_kernel_start();
   const int t = threadIdx.x;
@@ -512,7 +551,7 @@ extern "C" snn_status snn_rms_norm_forward(const snn_rms_norm_args* a, void* str
   if (!a->x || (a->residual && !a->h) || (!a->y && !keeps) || (keeps && (!a->codes || !a->scales))) return SNN_ERR_INVALID_ARG;
   if ((a->residual && !no_overlap(a, a->h_stride)) || (a->y && !no_overlap(a, a->y_stride))) return SNN_ERR_INVALID_ARG;
   RmsParams p{};
-  p.rows = a->rows, p.n = a->n, p.groups = (a->n + KEEP_GROUP - 1) / KEEP_GROUP, p.keep_format = a->keep_format, p.eps = a->eps, p.inverse_n = 1.f / (float)a->n;
+  p.rows = a->rows, p.n = a->n, p.groups = (a->n + KEEP_GROUP - 1) / KEEP_GROUP, p.keep_format = a->keep_format, p.eps = a->eps, p.inverse_n = 1.f / (float)a->n, p.inverse = 1.0 / a->n;
   p.x = a->x, p.x_stride = a->x_stride, p.residual = a->residual, p.residual_stride = a->residual_stride, p.weight = a->weight;
   p.h = a->h, p.h_stride = a->h_stride, p.y = a->y, p.y_stride = a->y_stride, p.rstd = a->rstd, p.codes = a->codes, p.scales = a->scales;
   int access = access_of(a, {{a->x, a->x_stride, a->dtype}, {a->residual, a->residual_stride, a->dtype}, {a->residual ? a->h : nullptr, a->h_stride, a->dtype},

@@ -71,6 +71,20 @@ def check(x, res, w, dy, dh, dtype, eps=1e-6, **kw):
         close(dw, b["dw"], b["dw_tol"], "fp32" if w.dtype is torch.float32 else dtype, "dw")
 
 
+@pytest.mark.parametrize("keep", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,weight,n", [("fp32", "same", 512), ("bf16", "same", 512), ("bf16", "fp32", 4096), ("fp16", "same", 1030), ("fp32", None, 321),
+                                            ("bf16", "same", 20000)])
+def test_codes_are_those_of_the_formula(dtype, weight, n, keep):
+    """Codes are rounded once.  The scale is good to 2^-28 or so, and a code of int8 lies 64 steps from zero on average: of 1.2 million
+    64 x 2^-28 x 1.2 million = 0.3 are the ones beside it; products rounded to fp32 before leave a dozen."""
+    rows = 1200000 // n
+    x, res, w, _, _ = inputs(rows, n, dtype, n, weight=weight)
+    _, h, _, kept = ops().rms_norm(x, w, res, keep=keep, values=False)
+    want, _ = eight_bits(ref.norm_forward(f64(h), None if w is None else f64(w), 1e-6)["y"], keep)
+    differ = int((f64(ops().unpack_activation(kept, torch.float32)) != want).sum())
+    assert differ <= 3
+
+
 WIDTHS = [1, 7, 8, 63, 64, 65, 130, 256, 264, 520, 1030, 2048, 2056, 4096, 8192, 8200, 16384, 16392, 20001]
 
 

@@ -517,9 +517,11 @@ snn_status snn_rms_norm_backward(const snn_rms_norm_args* args, void* stream);
  * snn_activation_unpack reads them), since in sqrt(v) e4m3 holds a range of 2^36 of v.  A moment moves by a small part of its
  * codes' steps, so codes are rounded up or down at random: magnitude u in steps becomes floor(u + r / 2^16); m takes the lower
  * and sqrt(v) the upper 16 bits of hash(seed, t, place) (adamw.cu), and a sqrt(v) above zero at least the smallest code.  A group
- * with an infinity or a NaN decodes to NaN from then on.  In the quotient a sqrt(v) below 2^-63 counts as that.
+ * with an infinite or NaN gradient decodes to NaN from then on.  In the quotient a sqrt(v) below 2^-63 counts as that.
  * With max_norm > 0 a step whose norm is not finite is left out: nothing changes, and *step does not count it.
- * v is fp32: gradients beyond 1.8e19 in magnitude make it infinite, and stop that parameter. */
+ * v is fp32: finite gradients beyond 1.8e19 in magnitude make it infinite, and stop that parameter: p (1 - lr weight_decay) is
+ * left of it.  In 8 bits such a place keeps the largest root, 448 x 2^55, and m = 0, which moves it no more than infinity would (and
+ * stands for as long as beta2 takes to let it fall); roots of its group that are above zero are 2^-18 of that at least. */
 typedef struct {
   void* param; const void* grad;   /* device, contiguous; no two tensors overlap                        */
   void* copy;                      /* device, or NULL: p' rounded to copy_dtype                          */

@@ -157,12 +157,14 @@ constexpr uint32_t AW_BITS_LOW = 0x4104u, AW_BITS_HIGH = 0x4324u;   // selectors
 __device__ __forceinline__ uint32_t highest_bytes(const uint32_t y[4]) {
   return __byte_perm(__byte_perm(y[0], y[1], 0x0073), __byte_perm(y[2], y[3], 0x0073), 0x5410);
 }
-// Codes of a lane's values; byte: their group's scale byte.  ROOT: nothing is negative, and what is above zero stays above zero.
-template <bool ROOT> __device__ __forceinline__ AwCodes encode_at_random(float2 f[AW_VALUES / 2], const uint32_t r[AW_VALUES], uint32_t byte) {
+constexpr uint32_t AW_FAR_BYTE = 133;   // 2^-120 over a larger scale is subnormal
+// Codes of a lane's values; byte: their group's scale byte; some_far: whether one of the warp's is above AW_FAR_BYTE.  ROOT: nothing is
+// negative, and what is above zero stays above zero.
+template <bool ROOT> __device__ __forceinline__ AwCodes encode_at_random(float2 f[AW_VALUES / 2], const uint32_t r[AW_VALUES], uint32_t byte, bool some_far) {
   // 2^-120 over the scale, 2^(7 - byte); where that is subnormal, in two steps (what is then too small to count, but not zero, counts
   // as 2^-60, far below a step)
-  const bool far = byte > 133u;
-  if (__any_sync(0xffffffffu, far)) {
+  const bool far = byte > AW_FAR_BYTE;
+  if (some_far) {
     const float inverse = keep_scale_inverse(byte);
 #pragma unroll
     for (int k = 0; k < AW_VALUES / 2; ++k) {
@@ -207,7 +209,7 @@ __device__ __forceinline__ uint32_t top_of(const float2 f[AW_VALUES / 2]) {
   return group_top<AW_LANES>(m);
 }
 // Square roots by the hardware's approximation of 1 / sqrt(v) and one step of Newton's iteration from the residual v - s^2, which
-// leaves them correctly rounded but for a few; of numbers below 2^-126 they are too small.
+// leaves them correctly rounded but for a few; of numbers below 2^-126 they are too small, of infinity NaN.
 __device__ __forceinline__ float2 root_of(float2 v) {
   float2 y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, 0x1p-126f)));
@@ -364,12 +366,12 @@ __device__ __forceinline__ void step_values(const AwParams<COUNT>& a, const AwSt
     root[k] = EIGHT ? root_of(v[k]) : make_float2(__fsqrt_rn(v[k].x), __fsqrt_rn(v[k].y));
   }
   if constexpr (EIGHT) {
-    // where all of a thread's roots are below 2^-44, squares may be subnormal (one that is beside a larger root has the smallest
-    // code or none either way)
+    // Where all of a thread's roots are below 2^-44, squares may be subnormal (one that is beside a larger root has the smallest
+    // code or none either way); where one is NaN, a square may be infinite.
     float top = 0.f;
 #pragma unroll
     for (int k = 0; k < N / 2; ++k) top = larger_of(top, root[k]);
-    if (top > 0.f && top < 0x1p-44f) {
+    if (top != 0.f && !(top >= 0x1p-44f)) {
 #pragma unroll
       for (int k = 0; k < N / 2; ++k) root[k] = make_float2(__fsqrt_rn(v[k].x), __fsqrt_rn(v[k].y));
     }
@@ -437,6 +439,17 @@ __device__ __forceinline__ void read_moments(const AwParams<COUNT>& a, float2 m[
     for (int k = 0; k < AW_VALUES / 2; ++k) v[k] = times(times(times(v[k], v_scale), v_scale), a.beta2);
   }
 }
+// The largest root that is kept, the last code of its scale: squares of what it is rounded to are finite.
+constexpr float AW_LARGEST = 0x1.cp63f;   // 448 x 2^55
+constexpr uint32_t AW_LARGEST_BYTE = 55 + 127;
+// A moment pair that is about to be coded.  Of a finite gradient whose square is infinite the step has been none (m / infinity); the
+// largest root and no first moment stand for that from now on, since a group that holds an infinity is lost.  (NaN and infinite
+// gradients are.)
+__device__ __forceinline__ void keep_finite(float& m, float& root) {
+  if (!(root > AW_LARGEST && fabsf(m) <= largest_finite<float>())) return;
+  if (root > largest_finite<float>()) m = 0.f;
+  root = AW_LARGEST;
+}
 // The moments back to codes and scale bytes; the lanes of a warp do this together.
 struct AwPacked {
   AwCodes m, v;
@@ -445,11 +458,17 @@ struct AwPacked {
 __device__ __forceinline__ AwPacked pack_moments(const AwStep& step, int64_t at, float2 m[AW_VALUES / 2], float2 root[AW_VALUES / 2]) {
   AwPacked k;
   k.v_byte = keep_scale_byte<SNN_KEEP_E4M3>(top_of(root)), k.m_byte = keep_scale_byte<SNN_KEEP_E4M3>(top_of(m));
+  const bool far = __any_sync(0xffffffffu, k.v_byte > AW_FAR_BYTE);
+  if (far && __any_sync(0xffffffffu, k.v_byte > AW_LARGEST_BYTE)) {
+#pragma unroll
+    for (int j = 0; j < AW_VALUES / 2; ++j) keep_finite(m[j].x, root[j].x), keep_finite(m[j].y, root[j].y);
+    k.v_byte = keep_scale_byte<SNN_KEEP_E4M3>(top_of(root)), k.m_byte = keep_scale_byte<SNN_KEEP_E4M3>(top_of(m));
+  }
   uint32_t r[AW_VALUES];
   const uint32_t base = mix_base((uint32_t)at ^ step.key ^ mix((uint32_t)(at >> 32)));
 #pragma unroll
   for (int j = 0; j < AW_VALUES; ++j) r[j] = mix_from(base, j);
-  k.m = encode_at_random<false>(m, r, k.m_byte), k.v = encode_at_random<true>(root, r, k.v_byte);
+  k.m = encode_at_random<false>(m, r, k.m_byte, __any_sync(0xffffffffu, k.m_byte > AW_FAR_BYTE)), k.v = encode_at_random<true>(root, r, k.v_byte, far);
   return k;
 }
 constexpr int AW_STEP = 32 * AW_VALUES;   // of a warp and turn

@@ -37,7 +37,7 @@ struct AwTensor {
 struct AwStep {
   float factor;                 // of the gradients
   float rate, root;             // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
-  float keep;                   // 1 - lr wd
+  float keep, keep_rest;        // 1 - lr wd, the sum of the two
   uint32_t key;
   int32_t skip;
 };
@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_begin_kernel(const AwBegin b
   }
   if (threadIdx.x > 0) return;
   const double scale = (double)b.scale * (b.scale_device ? (double)*b.scale_device : 1.0);
-  AwStep s{(float)scale, 0.f, 0.f, 0.f, 0u, 0};
+  AwStep s{(float)scale, 0.f, 0.f, 0.f, 0.f, 0u, 0};
   if (b.partial) {
     const double norm = sqrt(sum) * fabs(scale);
     if (b.norm) *b.norm = (float)norm;
@@ -341,7 +341,12 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_begin_kernel(const AwBegin b
     const double lr = b.lr_device ? (double)*b.lr_device : b.lr;
     s.rate = (float)(lr / left[0]);
     s.root = (float)(1.0 / sqrt(left[1]));
-    s.keep = (float)(1.0 - lr * b.weight_decay);
+    // In one float a decay of 2e-7 would be 1.8e-7.  Two of the same sign, of which the second is never zero, leave an infinite
+    // parameter infinite.
+    const double keep = 1.0 - lr * b.weight_decay;
+    s.keep = (float)keep;
+    if (keep != 0.0 && fabs((double)s.keep) >= fabs(keep)) s.keep = __uint_as_float(__float_as_uint(s.keep) - 1u);
+    s.keep_rest = (float)(keep - (double)s.keep);
     s.key = key_of(b.seed, (uint64_t)t);
   }
   *b.out = s;
@@ -383,7 +388,7 @@ __device__ __forceinline__ void step_values(const AwParams<COUNT>& a, const AwSt
     const float2 below = fma_pair(counts, both(step.root), both(a.eps)), up = times(m[k], -step.rate);
     const float2 update = EIGHT ? mul_pair(up, make_float2(reciprocal(below.x), reciprocal(below.y)))
                                 : make_float2(__fdividef(up.x, below.x), __fdividef(up.y, below.y));
-    p[k] = fma_pair(p[k], both(step.keep), update);
+    p[k] = fma_pair(p[k], both(step.keep), fma_pair(p[k], both(step.keep_rest), update));
     if (EIGHT) v[k] = root[k];
   }
 }

@@ -53,16 +53,20 @@ template <bool BLOCK, typename T> __device__ __forceinline__ T row_sum(T v, int 
   return v;
 }
 __device__ __forceinline__ float scale_of(float sum, const RmsParams& p) { return rsqrtf(sum * p.inverse_n + p.eps); }
-// A row's scale and what it is off by: with a copy in 8 bits the lanes' sums are joined in 64 bits, and one step of Newton's iteration
-// leaves a scale to 2^-28, so that codes are those of the formula.  (Of the scale in fp32 alone, and y rounded before it was coded, one
-// code in a million was the one beside it.)
+// A row's scale and what it is off by: with a copy in 8 bits the lanes' sums are joined in 64 bits, and two steps of Newton's iteration
+// leave 1 / sqrt of them in 64 bits, so that codes are those of the formula.  (Of the scale in fp32 alone, and y rounded before it was
+// coded, one code in a million was the one beside it.)  Where mean and root are numbers of few bits, they are found: the quotient has
+// its remainder added, and the second step ends at such a root, which the first one passes by 2^-44.
 struct Scale {
   float value, rest;
 };
 __device__ __forceinline__ Scale scale_of(double sum, const RmsParams& p) {
-  const double m = sum * p.inverse + (double)p.eps, s = (double)rsqrtf((float)m), better = s + s * 0.5 * (1.0 - m * s * s);
-  const float value = (float)better;
-  return {value, (float)(better - (double)value)};
+  const double q = sum * p.inverse, m = fma(fma(-q, (double)p.n, sum), p.inverse, q) + (double)p.eps;
+  double s = (double)rsqrtf((float)m);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) s = fma(s * 0.5, fma(-(m * s), s, 1.0), s);
+  const float value = (float)s;
+  return {value, (float)(s - (double)value)};
 }
 // Where squares leave the range of fp32 they are summed again of values times 2^-80: that of the largest row is finite, and
 // eps, at most one, is nothing beside it.  An infinity in the row leaves a scale of zero, NaN a NaN.
@@ -82,11 +86,12 @@ template <bool BLOCK, int ACCESS, int N> struct Place {
     return {((t & ~31) + i * lanes) * N + Columns<ACCESS, N>::of_lane(t & 31), n};
   }
 };
-// What is not between two codes does not look as if it were with its lowest bit set, where y has been rounded toward zero: it is
-// rounded but once.  The scale is that of the next larger value.
+// A number that is not exact has its lowest bit set, where y has been rounded toward zero: it lies neither on a border between two codes
+// nor on that between two scales then, and is rounded but once.
 __device__ __forceinline__ float2 inexact(float2 v) { return make_float2(__uint_as_float(__float_as_uint(v.x) | 1u), __uint_as_float(__float_as_uint(v.y) | 1u)); }
-__device__ __forceinline__ uint32_t top_above(uint32_t top) { return top ? min(top + 1u, 0x7f800000u) : 0u; }
-// The 8-bit codes of a unit y, rounded toward zero; the lanes of a warp do this together.
+// (what left fp32 was cut to its largest value)
+__device__ __forceinline__ uint32_t top_of_cut(uint32_t top) { return top == 0x7f7fffffu ? 0x7f800000u : top; }
+// The 8-bit codes of a unit y, rounded as above; the lanes of a warp do this together.
 template <int FORMAT, int ACCESS, int N> __device__ __forceinline__ void keep_unit(const float2 y[N / 2], int64_t row, Columns<ACCESS, N> at, const RmsParams& p, bool store) {
   uint8_t* const codes = p.codes + row * p.n + at.first;
   uint8_t* const scales = p.scales + row * p.groups;
@@ -94,13 +99,13 @@ template <int FORMAT, int ACCESS, int N> __device__ __forceinline__ void keep_un
     float m = 0.f;
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) m = larger_of(m, y[i]);
-    const uint32_t top = top_above(group_top<KEEP_GROUP / N>(m)), byte = keep_scale_byte<FORMAT>(top);
+    const uint32_t top = top_of_cut(group_top<KEEP_GROUP / N>(m)), byte = keep_scale_byte<FORMAT>(top);
     const float inverse = keep_scale_inverse(byte);
     // (rarely: a group whose largest value could round up to 128, or one that is not finite)
     const bool rare = __any_sync(0xffffffffu, byte == 255u || keep_needs_cut<FORMAT>(top));
     uint32_t q[N / 4];
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i) q[i] = __byte_perm(encode_pair<FORMAT>(inexact(y[2 * i]), inverse, rare), encode_pair<FORMAT>(inexact(y[2 * i + 1]), inverse, rare), 0x5410);
+    for (int i = 0; i < N / 4; ++i) q[i] = __byte_perm(encode_pair<FORMAT>(y[2 * i], inverse, rare), encode_pair<FORMAT>(y[2 * i + 1], inverse, rare), 0x5410);
     if (rare && byte == 255u) {
 #pragma unroll
       for (int i = 0; i < N / 4; ++i) q[i] = 0u;
@@ -118,8 +123,8 @@ template <int FORMAT, int ACCESS, int N> __device__ __forceinline__ void keep_un
 #pragma unroll
     for (int k = 0; k < N / 2; ++k) {
       if (start + k * KEEP_GROUP >= p.n) break;
-      const uint32_t top = top_above(__reduce_max_sync(0xffffffffu, __float_as_uint(larger_of(0.f, y[k])))), byte = keep_scale_byte<FORMAT>(top);
-      const uint32_t q = byte == 255u ? 0u : encode_pair<FORMAT>(inexact(y[k]), keep_scale_inverse(byte), keep_needs_cut<FORMAT>(top));
+      const uint32_t top = top_of_cut(__reduce_max_sync(0xffffffffu, __float_as_uint(larger_of(0.f, y[k])))), byte = keep_scale_byte<FORMAT>(top);
+      const uint32_t q = byte == 255u ? 0u : encode_pair<FORMAT>(y[k], keep_scale_inverse(byte), keep_needs_cut<FORMAT>(top));
       if (lane == k) mine = byte;
       if (!store) continue;
       if (ACCESS == PAIRS) {
@@ -148,17 +153,35 @@ __device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT,
   if (p.keep_format == SNN_KEEP_RAW) return;
   const float upper = sizeof(IO) == 2 ? __uint_as_float(__float_as_uint(scale.value) & 0xfffff000u) : scale.value;
   const float lower = scale.value - upper + scale.rest;
-  float2 y[N / 2];
-#pragma unroll
-  for (int i = 0; i < N / 2; ++i) {
-    const float2 v = h.pair(i), a = mul_pair(v, both(upper));
-    float2 rest;
+  // h s = first + rest
+  auto product = [&](int i, float2& first, float2& rest) {
+    const float2 v = h.pair(i);
+    first = mul_pair(v, both(upper));
     if constexpr (sizeof(IO) == 2)
       rest = mul_pair(v, both(lower));
     else
       rest = fma_pair(v, both(lower), fma_pair(v, both(upper), mul_pair(v, both(-upper))));
-    const float2 weight = p.weight ? w.pair(i) : both(1.f);
-    y[i] = fma_pair_down(a, weight, mul_pair(rest, weight));
+  };
+  float2 y[N / 2];
+  if (scale.rest != 0.f) {
+    // A scale of more than 24 bits: so has every product with it, since that of two odd numbers is at least as long as each.
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      float2 first, rest;
+      product(i, first, rest);
+      const float2 weight = p.weight ? w.pair(i) : both(1.f);
+      y[i] = inexact(fma_pair_down(first, weight, mul_pair(rest, weight)));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      float2 first, rest;
+      product(i, first, rest);
+      const float2 weight = p.weight ? w.pair(i) : both(1.f);
+      rest = mul_pair(rest, weight);
+      const float2 v = fma_pair_down(first, weight, rest), off = add_pair(fma_pair(first, weight, make_float2(-v.x, -v.y)), rest), up = inexact(v);
+      y[i] = make_float2(off.x == 0.f ? v.x : up.x, off.y == 0.f ? v.y : up.y);
+    }
   }
   if (p.keep_format == SNN_KEEP_INT8)
     keep_unit<SNN_KEEP_INT8, ACCESS, N>(y, row, at, p, store);

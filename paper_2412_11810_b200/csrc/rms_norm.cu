@@ -58,20 +58,34 @@ __device__ __forceinline__ float scale_of(float sum, const RmsParams& p) { retur
 // coded, one code in a million was the one beside it.)  Where mean and root are numbers of few bits, they are found: the quotient has
 // its remainder added, and the second step ends at such a root, which the first one passes by 2^-44.
 struct Scale {
-  float value, rest;
+  float value, rest, down;   // 1 / sqrt(mean + eps) = (value + rest) down
+  __device__ __forceinline__ float rounded() const { return value * down; }
 };
-__device__ __forceinline__ Scale scale_of(double sum, const RmsParams& p) {
-  const double q = sum * p.inverse, m = fma(fma(-q, (double)p.n, sum), p.inverse, q) + (double)p.eps;
+__device__ __forceinline__ double root_inverse(double m) {
   double s = (double)rsqrtf((float)m);
 #pragma unroll
   for (int k = 0; k < 2; ++k) s = fma(s * 0.5, fma(-(m * s), s, 1.0), s);
+  return s;
+}
+__device__ __forceinline__ double mean_of(double sum, const RmsParams& p) {
+  const double q = sum * p.inverse;
+  return fma(fma(-q, (double)p.n, sum), p.inverse, q);
+}
+__device__ __forceinline__ Scale scale_of(double sum, const RmsParams& p) {
+  const double s = root_inverse(mean_of(sum, p) + (double)p.eps);
   const float value = (float)s;
-  return {value, (float)(s - (double)value)};
+  return {value, (float)(s - (double)value), 1.f};
 }
 // Where squares leave the range of fp32 they are summed again of values times 2^-80: that of the largest row is finite, and
-// eps, at most one, is nothing beside it.  An infinity in the row leaves a scale of zero, NaN a NaN.
-constexpr float RMS_DOWN = 0x1p-80f;
-__device__ __forceinline__ float scale_of_far(float sum, const RmsParams& p) { return rsqrtf(sum * p.inverse_n) * RMS_DOWN; }
+// eps, at most one, is nothing beside it.  The scale, down to 2^-128, is held times 2^32: as it is it would be subnormal.  An infinity
+// in the row leaves a scale of zero, NaN a NaN.
+constexpr float RMS_DOWN = 0x1p-80f, RMS_SCALE_DOWN = 0x1p-32f;
+__device__ __forceinline__ Scale scale_of_far(double sum, const RmsParams& p) {
+  if (!(sum <= (double)largest_finite<float>())) return {rsqrtf((float)sum), 0.f, 1.f};
+  const double s = root_inverse(mean_of(sum, p)) * 0x1p-48;
+  const float value = (float)s;
+  return {value, (float)(s - (double)value), RMS_SCALE_DOWN};
+}
 
 // Which row of a turn of its block a thread works at, which of the row's threads it is, and its columns.  (Less than a warp a row: by
 // vectors only.)
@@ -145,7 +159,7 @@ __device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT,
     Unit<IO, N> out;
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
-      const float2 y = mul_pair(h.pair(i), both(scale.value));
+      const float2 y = mul_pair(h.pair(i), both(scale.rounded()));
       out.set(i, p.weight ? mul_pair(y, w.pair(i)) : y);
     }
     at.store(out, (IO*)p.y + row * p.y_stride);
@@ -153,9 +167,8 @@ __device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT,
   if (p.keep_format == SNN_KEEP_RAW) return;
   const float upper = sizeof(IO) == 2 ? __uint_as_float(__float_as_uint(scale.value) & 0xfffff000u) : scale.value;
   const float lower = scale.value - upper + scale.rest;
-  // h s = first + rest
-  auto product = [&](int i, float2& first, float2& rest) {
-    const float2 v = h.pair(i);
+  // v s = first + rest
+  auto product = [&](float2 v, float2& first, float2& rest) {
     first = mul_pair(v, both(upper));
     if constexpr (sizeof(IO) == 2)
       rest = mul_pair(v, both(lower));
@@ -163,24 +176,25 @@ __device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT,
       rest = fma_pair(v, both(lower), fma_pair(v, both(upper), mul_pair(v, both(-upper))));
   };
   float2 y[N / 2];
-  if (scale.rest != 0.f) {
+  if (scale.rest != 0.f && scale.down == 1.f) {
     // A scale of more than 24 bits: so has every product with it, since that of two odd numbers is at least as long as each.
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
       float2 first, rest;
-      product(i, first, rest);
+      product(h.pair(i), first, rest);
       const float2 weight = p.weight ? w.pair(i) : both(1.f);
       y[i] = inexact(fma_pair_down(first, weight, mul_pair(rest, weight)));
     }
   } else {
+    const bool exact = scale.rest == 0.f;
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
       float2 first, rest;
-      product(i, first, rest);
+      product(mul_pair(h.pair(i), both(scale.down)), first, rest);
       const float2 weight = p.weight ? w.pair(i) : both(1.f);
       rest = mul_pair(rest, weight);
       const float2 v = fma_pair_down(first, weight, rest), off = add_pair(fma_pair(first, weight, make_float2(-v.x, -v.y)), rest), up = inexact(v);
-      y[i] = make_float2(off.x == 0.f ? v.x : up.x, off.y == 0.f ? v.y : up.y);
+      y[i] = make_float2(off.x == 0.f && exact ? v.x : up.x, off.y == 0.f && exact ? v.y : up.y);
     }
   }
   if (p.keep_format == SNN_KEEP_INT8)
@@ -254,17 +268,17 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
       scale = scale_of(total, p), far = !(total <= largest_finite<float>());
     } else {
       const float total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared);
-      scale = {scale_of(total, p), 0.f}, far = !(total <= largest_finite<float>());
+      scale = {scale_of(total, p), 0.f, 1.f}, far = !(total <= largest_finite<float>());
     }
     // (lanes of one warp may hold different rows: they all go the same way, as do all threads of a row's warps)
     if (BLOCK ? far : __any_sync(0xffffffffu, far)) {
       sum = both(0.f);
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) sum_unit_far(h[i], sum);
-      const float total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared);
-      if (far) scale = {scale_of_far(total, p), 0.f};
+      const double total = row_sum<BLOCK>((double)sum.x + (double)sum.y, at.lanes, turn++, shared);
+      if (far) scale = scale_of_far(total, p);
     }
-    if (p.rstd && at.t == 0 && store) p.rstd[row] = scale.value;
+    if (p.rstd && at.t == 0 && store) p.rstd[row] = scale.rounded();
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) finish_unit<IO, WT, ACCESS, N>(h[i], w[i], scale, row, at.columns(i), p, store);
   }
@@ -303,9 +317,9 @@ template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds_
         at.load(h, again);
         sum_unit_far(h, sum);
       });
-      scale = {scale_of_far(row_sum<true>(sum.x + sum.y, RMS_WIDE, turn++, shared), p), 0.f};
+      scale = scale_of_far(row_sum<true>((double)sum.x + (double)sum.y, RMS_WIDE, turn++, shared), p);
     }
-    if (p.rstd && t == 0) p.rstd[row] = scale.value;
+    if (p.rstd && t == 0) p.rstd[row] = scale.rounded();
     each([&](At at) {   // (a thread reads back what it stored itself)
       Unit<IO, N> h;
       Unit<WT, N> w;

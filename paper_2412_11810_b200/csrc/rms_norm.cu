@@ -41,7 +41,11 @@ struct RmsParams {
 
 // The sum over the lanes of a row, the same bits for all of them, of type T.  `turn` counts the calls: two buffers take turns, so
 // that one barrier a call is enough.
-template <bool BLOCK, typename T> __device__ __forceinline__ T row_sum(T v, int lanes, int turn, double (*shared)[32]) {
+struct Sums {
+  double in64;
+  float in32;
+};
+template <bool BLOCK, typename T> __device__ __forceinline__ T row_sum(T v, int lanes, int turn, Sums (*shared)[32]) {
   for (int o = 1; o < (BLOCK ? 32 : lanes); o *= 2) v += __shfl_xor_sync(0xffffffffu, v, o);
   if constexpr (BLOCK) {
     T* const buffer = reinterpret_cast<T*>(shared[turn & 1]);
@@ -52,14 +56,30 @@ template <bool BLOCK, typename T> __device__ __forceinline__ T row_sum(T v, int 
   }
   return v;
 }
+// The same sum in 32 and in 64 bits: that in 32 has the bits of the one above.
+template <bool BLOCK> __device__ __forceinline__ Sums row_sums(float2 v, int lanes, int turn, Sums (*shared)[32]) {
+  Sums s{(double)v.x + (double)v.y, v.x + v.y};
+  for (int o = 1; o < (BLOCK ? 32 : lanes); o *= 2) s.in64 += __shfl_xor_sync(0xffffffffu, s.in64, o), s.in32 += __shfl_xor_sync(0xffffffffu, s.in32, o);
+  if constexpr (BLOCK) {
+    Sums* const buffer = shared[turn & 1];
+    if ((threadIdx.x & 31) == 0) buffer[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = buffer[0];   // (two at a time: four take 15 registers more, and with 104 fp32 rows by pairs have three blocks an SM instead of four)
+#pragma unroll 2
+    for (int k = 1; k < lanes / 32; ++k) s.in64 += buffer[k].in64, s.in32 += buffer[k].in32;
+  }
+  return s;
+}
 __device__ __forceinline__ float scale_of(float sum, const RmsParams& p) { return rsqrtf(sum * p.inverse_n + p.eps); }
 // A row's scale and what it is off by: with a copy in 8 bits the lanes' sums are joined in 64 bits, and two steps of Newton's iteration
 // leave 1 / sqrt of them in 64 bits, so that codes are those of the formula.  (Of the scale in fp32 alone, and y rounded before it was
 // coded, one code in a million was the one beside it.)  Where mean and root are numbers of few bits, they are found: the quotient has
 // its remainder added, and the second step ends at such a root, which the first one passes by 2^-44.
+// The values and rstd take a scale from sums in 32 bits, with a copy in 8 bits as without one: they have the same bits in both calls.
+// (Sums in 64 bits for all calls cost 1 % of 32768 x 2048, and 4 % where a row's threads wait for one another, 16384 x 4090.)
 struct Scale {
+  float rounded;             // that of the values
   float value, rest, down;   // 1 / sqrt(mean + eps) = (value + rest) down
-  __device__ __forceinline__ float rounded() const { return value * down; }
 };
 __device__ __forceinline__ double root_inverse(double m) {
   double s = (double)rsqrtf((float)m);
@@ -74,17 +94,17 @@ __device__ __forceinline__ double mean_of(double sum, const RmsParams& p) {
 __device__ __forceinline__ Scale scale_of(double sum, const RmsParams& p) {
   const double s = root_inverse(mean_of(sum, p) + (double)p.eps);
   const float value = (float)s;
-  return {value, (float)(s - (double)value), 1.f};
+  return {value, value, (float)(s - (double)value), 1.f};
 }
 // Where squares leave the range of fp32 they are summed again of values times 2^-80: that of the largest row is finite, and
 // eps, at most one, is nothing beside it.  The scale, down to 2^-128, is held times 2^32: as it is it would be subnormal.  An infinity
 // in the row leaves a scale of zero, NaN a NaN.
 constexpr float RMS_DOWN = 0x1p-80f, RMS_SCALE_DOWN = 0x1p-32f;
 __device__ __forceinline__ Scale scale_of_far(double sum, const RmsParams& p) {
-  if (!(sum <= (double)largest_finite<float>())) return {rsqrtf((float)sum), 0.f, 1.f};
+  if (!(sum <= (double)largest_finite<float>())) return {rsqrtf((float)sum), rsqrtf((float)sum), 0.f, 1.f};
   const double s = root_inverse(mean_of(sum, p)) * 0x1p-48;
   const float value = (float)s;
-  return {value, (float)(s - (double)value), RMS_SCALE_DOWN};
+  return {value * RMS_SCALE_DOWN, value, (float)(s - (double)value), RMS_SCALE_DOWN};
 }
 
 // Which row of a turn of its block a thread works at, which of the row's threads it is, and its columns.  (Less than a warp a row: by
@@ -159,7 +179,7 @@ __device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT,
     Unit<IO, N> out;
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) {
-      const float2 y = mul_pair(h.pair(i), both(scale.rounded()));
+      const float2 y = mul_pair(h.pair(i), both(scale.rounded));
       out.set(i, p.weight ? mul_pair(y, w.pair(i)) : y);
     }
     at.store(out, (IO*)p.y + row * p.y_stride);
@@ -224,7 +244,7 @@ template <typename IO, int N> __device__ __forceinline__ void sum_unit_far(const
 template <typename IO, typename WT, int ACCESS, int UNITS, bool BLOCK>
 __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK && ACCESS == VECTORS && UNITS == 1 ? 2 : 1) rms_forward_kernel(const RmsParams p) {
   constexpr int N = UNIT<IO>;
-  __shared__ double shared[2][32];
+  __shared__ Sums shared[2][32];
   const Place<BLOCK, ACCESS, N> at(p);
   const int64_t step = (int64_t)gridDim.x * at.per_block();
   const bool residual = p.residual != nullptr;
@@ -262,23 +282,24 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
     }
     if (base + step < p.rows) load(min(base + step + at.slot, p.rows - 1));
     Scale scale;
-    bool far;
+    float total;
     if (p.keep_format != SNN_KEEP_RAW) {
-      const double total = row_sum<BLOCK>((double)sum.x + (double)sum.y, at.lanes, turn++, shared);
-      scale = scale_of(total, p), far = !(total <= largest_finite<float>());
+      const Sums sums = row_sums<BLOCK>(sum, at.lanes, turn++, shared);
+      scale = scale_of(sums.in64, p), total = sums.in32;
     } else {
-      const float total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared);
-      scale = {scale_of(total, p), 0.f, 1.f}, far = !(total <= largest_finite<float>());
+      scale = {}, total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared);
     }
+    scale.rounded = scale_of(total, p);
+    const bool far = !(total <= largest_finite<float>());
     // (lanes of one warp may hold different rows: they all go the same way, as do all threads of a row's warps)
     if (BLOCK ? far : __any_sync(0xffffffffu, far)) {
       sum = both(0.f);
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) sum_unit_far(h[i], sum);
-      const double total = row_sum<BLOCK>((double)sum.x + (double)sum.y, at.lanes, turn++, shared);
-      if (far) scale = scale_of_far(total, p);
+      const double again = row_sum<BLOCK>((double)sum.x + (double)sum.y, at.lanes, turn++, shared);
+      if (far) scale = scale_of_far(again, p);
     }
-    if (p.rstd && at.t == 0 && store) p.rstd[row] = scale.rounded();
+    if (p.rstd && at.t == 0 && store) p.rstd[row] = scale.rounded;
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) finish_unit<IO, WT, ACCESS, N>(h[i], w[i], scale, row, at.columns(i), p, store);
   }
@@ -287,7 +308,7 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
 template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds__(RMS_WIDE) rms_forward_wide_kernel(const RmsParams p) {
   constexpr int N = UNIT<IO>;
   using At = Columns<ACCESS, N>;
-  __shared__ double shared[2][32];
+  __shared__ Sums shared[2][32];
   const int t = threadIdx.x;
   const bool residual = p.residual != nullptr;
   int turn = 0;
@@ -319,7 +340,7 @@ template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds_
       });
       scale = scale_of_far(row_sum<true>((double)sum.x + (double)sum.y, RMS_WIDE, turn++, shared), p);
     }
-    if (p.rstd && t == 0) p.rstd[row] = scale.rounded();
+    if (p.rstd && t == 0) p.rstd[row] = scale.rounded;
     each([&](At at) {   // (a thread reads back what it stored itself)
       Unit<IO, N> h;
       Unit<WT, N> w;
@@ -338,7 +359,7 @@ template <typename IO, typename WT, int N> __device__ __forceinline__ float2 wei
 template <typename IO, typename WT, int ACCESS, int UNITS, bool BLOCK>
 __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_backward_kernel(const RmsParams p) {
   constexpr int N = UNIT<IO>;
-  __shared__ double shared[2][32];
+  __shared__ Sums shared[2][32];
   __shared__ float dw_shared[BLOCK ? 1 : 32 * N];
   let_next_kernel_start();
   const Place<BLOCK, ACCESS, N> at(p);
@@ -433,7 +454,7 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS) rms_back
 template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds__(RMS_WIDE) rms_backward_wide_kernel(const RmsParams p, bool in_shared) {
   constexpr int N = UNIT<IO>;
   using At = Columns<ACCESS, N>;
-  __shared__ double shared[2][32];
+  __shared__ Sums shared[2][32];
   extern __shared__ float sums[];
   let_next_kernel_start();
   const int t = threadIdx.x;

@@ -38,6 +38,7 @@ class Session:
         self.device_ws: Optional[torch.Tensor] = None
         self.pinned_ws: Optional[torch.Tensor] = None
         self.adamw: Optional[ops.AdamWState] = None
+        self._has_gradients = False      # whether the last step was a training step of these weights
         self.debug_V: Optional[List[torch.Tensor]] = None
         self._last = None
 
@@ -67,6 +68,7 @@ class Session:
         self.dW_rec = [torch.empty_like(w) for w in self.W_rec]
         self.dW_out = torch.empty_like(self.W_out)
         self.adamw = None
+        self._has_gradients = False
 
     def ckpt(self, strategy: int, chunk_size: int = 0, remote_chunk_size: int = 0, nb_local: int = 0) -> sb.snn_ckpt:
         return sb.snn_ckpt(strategy, chunk_size, remote_chunk_size, nb_local)
@@ -124,7 +126,10 @@ class Session:
             a.debug_V = dbg
         self._last = (T, B, input_bits, targets)   # keep inputs alive until the call returns
         torch.cuda.current_stream(self.device).synchronize()
-        return sb.snn_train_step(self.net, a)
+        self._has_gradients = False      # (nor after a step that fails)
+        loss = sb.snn_train_step(self.net, a)
+        self._has_gradients = not flags & sb.SNN_FLAG_FORWARD_ONLY
+        return loss
 
     # ---- the update --------------------------------------------------------------------------
     def parameters(self) -> List[torch.Tensor]:
@@ -133,11 +138,17 @@ class Session:
     def parameter_gradients(self) -> List[torch.Tensor]:
         return [*self.dW_ff, *self.dW_rec, self.dW_out]
 
-    def adamw_step(self, lr, bits: int = 32, **kw) -> Optional[torch.Tensor]:
-        """One AdamW step on all weights with the gradients of the last train step, on the current stream; `bits` (32 or 8)
-        are those of the moments, chosen by the first step, and the other arguments those of `ops.adamw_step`."""
+    def adamw_step(self, lr, bits: Optional[int] = None, **kw) -> Optional[torch.Tensor]:
+        """One AdamW step on all weights with the gradients of the last train step, on the current stream.  That step has to have
+        made some: there are none before the first one, behind one that was forward only or failed, nor for new weights.
+        `bits` (32 or 8) are those of the moments, chosen by the first step (32 if None); later ones take those that there are.
+        The other arguments are those of `ops.adamw_step`."""
+        if not self._has_gradients:
+            raise RuntimeError("adamw_step: the last step made no gradients of these weights")
         if self.adamw is None:
-            self.adamw = ops.adamw_state(self.parameters(), bits)
+            self.adamw = ops.adamw_state(self.parameters(), 32 if bits is None else bits)
+        elif bits is not None and bits != (8 if isinstance(self.adamw.m, ops.PackedActivation) else 32):
+            raise ValueError(f"bits: {bits!r} are not those of the moments, which the first step chose")
         return ops.adamw_step(self.parameters(), self.parameter_gradients(), self.adamw, lr=lr, **kw)
 
     # ---- inspection ------------------------------------------------------------------------

@@ -438,9 +438,14 @@ def _rows_like(t: torch.Tensor, name: str, like: torch.Tensor) -> int:
     return _row_stride(t, name)
 
 
-def _overlap(a: Optional[int], a_stride: int, b: Optional[int], b_stride: int, rows: int, n: int, size: int) -> bool:
-    """Whether the memory between the first and the last value of two arrays of rows has bytes in common."""
-    return bool(a and b and rows) and a < b + ((rows - 1) * b_stride + n) * size and b < a + ((rows - 1) * a_stride + n) * size
+def _overlap(a: int, a_stride: int, b: int, b_stride: int, rows: int, n: int, size: int) -> bool:
+    """Whether two arrays of rows have bytes in common (strides of at least n values; of different strides: whether they could)."""
+    if rows == 0 or a >= b + ((rows - 1) * b_stride + n) * size or b >= a + ((rows - 1) * a_stride + n) * size:
+        return False
+    if a_stride != b_stride or rows == 1:
+        return True
+    apart = (b - a) % (a_stride * size)     # columns of the same rows, beside one another?
+    return apart < n * size or a_stride * size - apart < n * size
 
 
 def _norm_weight(weight: Optional[torch.Tensor], like: torch.Tensor) -> int:

@@ -558,7 +558,7 @@ snn_status snn_adamw_step(const snn_adamw_args* args, void* stream);
  * whose logits are all masked or hold a NaN or +infinity.
  * Limits (SNN_ERR_UNSUPPORTED): K and W up to 32, V up to 2^22. */
 typedef struct {
-  const void* from; void* to;      /* device: rows one behind the other; the same pointer, where W = K: in place; no other overlap */
+  const void* from; void* to;      /* device: rows one behind the other; the same pointer, where W = K: in place; no other overlap, nor with parents */
   int64_t row_bytes;
 } snn_state_rows;
 typedef struct {

@@ -686,11 +686,11 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
 MOST_BEAMS = 32
 
 
-def _state_table(states, rows: int, out_rows: int, inplace: bool, device: int):
-    """(table for the library, tensors that receive the rows)."""
+def _state_table(states, rows: int, out_rows: int, inplace: bool, device: int, read: Optional[torch.Tensor] = None):
+    """(table for the library, tensors that receive the rows); read: what the call reads while it writes them."""
     if isinstance(states, torch.Tensor):
         raise ValueError("states: a sequence of tensors is required")
-    table, out, seen = (sb.snn_state_rows * len(states))(), [], set()
+    table, out, held = (sb.snn_state_rows * len(states))(), [], []
     for k, t in enumerate(states):
         if not isinstance(t, torch.Tensor) or t.get_device() != device or not t.is_contiguous():
             raise ValueError(f"states[{k}]: a contiguous tensor on the device of the beams is required")
@@ -698,15 +698,23 @@ def _state_table(states, rows: int, out_rows: int, inplace: bool, device: int):
             raise ValueError(f"states[{k}]: {rows} rows are required, one for each beam")
         at, size = t.data_ptr(), t.numel() * t.element_size()
         if inplace:
-            if size and at in seen:
-                raise ValueError(f"states[{k}]: given twice")
-            seen.add(at)
+            if size:
+                held.append((at, at + size, k))
             new = t
         else:
             new = torch.empty_like(t) if rows == out_rows else t.new_empty((out_rows, *t.shape[1:]))
         out.append(new)
         e = table[k]
         e.source, e.to, e.row_bytes = at, new.data_ptr(), size // rows if rows else 0
+    held.sort()
+    for (_, end, j), (begin, _, k) in zip(held, held[1:]):
+        if begin < end:
+            raise ValueError(f"states[{max(j, k)}]: shares memory with states[{min(j, k)}], which does not go in place")
+    if read is not None and read.numel():
+        first, last = read.data_ptr(), read.data_ptr() + read.numel() * read.element_size()
+        for begin, end, k in held:
+            if begin < last and first < end:
+                raise ValueError(f"states[{k}]: shares memory with the parents, which does not go in place")
     return table, out
 
 
@@ -722,7 +730,7 @@ def beam_step(logits: torch.Tensor, scores: torch.Tensor, *, width: Optional[int
     Continuations at -infinity come last, in the order of k V + c: classes masked by logits of -infinity, and all of a
     beam whose score is not finite, or whose logits are all masked or hold a NaN or +infinity.
     states: tensors whose rows [B K, ...] belong to the beams (what gated_scan_step carries, tokens so far): they come back
-    as rows [B width, ...] of the beams' parents, with inplace in their own memory (width = K).
+    as rows [B width, ...] of the beams' parents, with inplace in their own memory (width = K), of which no two may share any.
     K and width are at most 32, V at most 2^22.  Returns (tokens int64 [B][width], parents int64 [B][width], the beam of each,
     scores fp32 [B][width], ended bool [B][width] or None without end, list of states)."""
     _values(logits, "logits", 3)
@@ -762,7 +770,8 @@ def beam_step(logits: torch.Tensor, scores: torch.Tensor, *, width: Optional[int
 def reorder_states(states: Sequence[torch.Tensor], parents: torch.Tensor, *, beams: Optional[int] = None, inplace: bool = False) -> List[torch.Tensor]:
     """Rows [B K, ...] of tensors of any type in the order of their parents, int64 [B][W]: row b W + w of a result is row
     b K + parents[b, w]; a parent outside [0, K) leaves zeros.  beams: K, where it is not W.  inplace: in the tensors' own
-    memory (K = W); rows that stay where they are are not written.  K and W are at most 32."""
+    memory (K = W), which they may share neither with one another nor with the parents; rows that stay where they are are not
+    written.  K and W are at most 32."""
     if not (isinstance(parents, torch.Tensor) and parents.is_cuda and parents.dtype is torch.int64 and parents.dim() == 2 and parents.is_contiguous()):
         raise ValueError("parents: a contiguous int64 CUDA tensor of two dimensions is required")
     B, W = parents.shape
@@ -774,7 +783,7 @@ def reorder_states(states: Sequence[torch.Tensor], parents: torch.Tensor, *, bea
     if inplace and K != W:
         raise ValueError("inplace: needs as many survivors as beams")
     with _on(parents):
-        table, out = _state_table(states, B * K, B * W, inplace, parents.get_device())
+        table, out = _state_table(states, B * K, B * W, inplace, parents.get_device(), parents)
         if B and out:
             sb.snn_reorder_rows(table, len(out), parents.data_ptr(), B, K, W, _stream(parents))
     return out

@@ -500,7 +500,8 @@ typedef struct {
   void* workspace; size_t workspace_bytes;      /* device, 256-byte aligned: backward pass with dweight only; calls
                                   that may overlap in time need workspaces of their own                 */
 } snn_rms_norm_args;
-/* Bytes of workspace that the backward pass needs: it depends on rows and n alone, 4 n bytes per thread block. */
+/* Bytes of workspace that the backward pass needs, by rows, n and the size of dtype alone: 4 n per thread block, of which there are at most
+ * 1184, and no more than rows. */
 snn_status snn_rms_norm_workspace(const snn_rms_norm_args* args, size_t* bytes);
 snn_status snn_rms_norm_forward(const snn_rms_norm_args* args, void* stream);
 snn_status snn_rms_norm_backward(const snn_rms_norm_args* args, void* stream);

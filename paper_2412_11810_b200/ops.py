@@ -522,7 +522,7 @@ def rms_norm_backward(h: torch.Tensor, rstd: torch.Tensor, dy: torch.Tensor, wei
     """Gradients of a loss from those by y (dy) and by h (dh, what the residual stream hands back; zero if None), with h and
     rstd as `rms_norm` returned them.  Where y was kept in 8 bits, they are those of the values before.
     Returns (dx, the gradient by x and by the residual alike, of their type; dweight, of weight's type, None without one).
-    Workspace: 4 N bytes per thread block, of which there are at most 592, and no more than rows."""
+    Workspace: 4 N bytes per thread block, of which there are at most 1184, and no more than rows."""
     _rows(h, "h")
     n = h.shape[-1]
     weight_dtype = _norm_weight(weight, h)

@@ -553,7 +553,9 @@ snn_status snn_adamw_step(const snn_adamw_args* args, void* stream);
 
 /* One step of beam search: of the K V continuations of a sample's beams the best W,
  *   score(k, c) = scores[k] + log softmax(logits[k])[c],
- * ranked in 64 bits, classes of one beam by their logits; ties go to the lower beam, then to the lower class.  An ended beam
+ * classes of one beam ranked by their logits, to the bit, and beams by scores that are compared in 64 bits, with exponentials summed in fp32:
+ * they are good to 1e-6 as a rule and 1e-5 at worst, and what is closer than that may come in either order.  Equal beams have equal
+ * scores; ties go to the lower beam, then to the lower class.  An ended beam
  * goes on with `end` alone, at its own score.  Continuations at -infinity come last, in the order of k V + c: all others of an
  * ended beam, masked classes (logits of -infinity), and every one of a beam that is dead, whose score is not finite or
  * whose logits are all masked or hold a NaN or +infinity.

@@ -725,7 +725,9 @@ def beam_step(logits: torch.Tensor, scores: torch.Tensor, *, width: Optional[int
         score(k, c) = scores[b, k] + log_softmax(logits[b, k])[c]
 
     logits: [B][K][V], fp32, bf16 or fp16, with contiguous classes; scores: fp32 [B][K] (a first step from one beam has K = 1).
-    Scores are ranked in 64 bits, classes of one beam by their logits; ties go to the lower beam, then to the lower class.
+    Classes of one beam are ranked by their logits, exactly.  Beams are ranked by scores that are compared in 64 bits, with exponentials
+    summed in fp32: good to 1e-6 as a rule and 1e-5 at worst, and what is closer than that may come in either order.  Equal beams have
+    equal scores; ties go to the lower beam, then to the lower class.
     end: the class that ends a beam; ended: bool [B][K], the beams that have: they go on with `end` alone, at their score.
     Continuations at -infinity come last, in the order of k V + c: classes masked by logits of -infinity, and all of a
     beam whose score is not finite, or whose logits are all masked or hold a NaN or +infinity.

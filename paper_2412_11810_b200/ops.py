@@ -606,7 +606,7 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
     if device < 0:
         raise ValueError("state.step: a CUDA tensor is required")
     table, dtypes, room = (sb.snn_adamw_tensor * count)(), _DTYPES, 0
-    written = set()
+    written = []          # (begin, end, of which list, which one)
     for k in range(count):
         p, g = params[k], grads[k]
         n = p.numel() if isinstance(p, torch.Tensor) else 0
@@ -622,18 +622,18 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
         e = table[k]
         at = p.data_ptr()
         e.param, e.grad, e.n, e.param_dtype, e.grad_dtype = at, g.data_ptr(), n, dtypes[p.dtype], dtypes[g.dtype]
-        if at in written:
-            raise ValueError(f"params[{k}]: given twice")
-        written.add(at)
+        written.append((at, at + n * p.element_size(), "params", k))
         c = None if copies is None else copies[k]
         if c is not None:
             if not isinstance(c, torch.Tensor) or c.get_device() != device or c.dtype not in dtypes or not c.is_contiguous() or c.shape != p.shape:
                 raise ValueError(f"copies[{k}]: a contiguous tensor of fp32, bf16 or fp16 and of the parameter's shape is required")
             at = c.data_ptr()
-            if at in written:
-                raise ValueError(f"copies[{k}]: given twice")
-            written.add(at)
+            written.append((at, at + n * c.element_size(), "copies", k))
             e.copy, e.copy_dtype = at, dtypes[c.dtype]
+    written.sort()
+    for a, b in zip(written, written[1:]):
+        if b[0] < a[1]:
+            raise ValueError(f"{b[2]}[{b[3]}]: shares memory with {a[2]}[{a[3]}], which is written as well")
     if like.dtype is not torch.int64 or like.dim() != 0:
         raise ValueError("state.step: an int64 0-d tensor is required")
     a = sb.snn_adamw_args()

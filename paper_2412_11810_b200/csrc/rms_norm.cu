@@ -56,9 +56,8 @@ template <bool BLOCK, typename T> __device__ __forceinline__ T row_sum(T v, int 
   }
   return v;
 }
-// The same sum in 32 and in 64 bits: that in 32 has the bits of the one above.
-template <bool BLOCK> __device__ __forceinline__ Sums row_sums(float2 v, int lanes, int turn, Sums (*shared)[32]) {
-  Sums s{(double)v.x + (double)v.y, v.x + v.y};
+// The same of both at once: that in 32 bits has the bits of the one above.
+template <bool BLOCK> __device__ __forceinline__ Sums row_sums(Sums s, int lanes, int turn, Sums (*shared)[32]) {
   for (int o = 1; o < (BLOCK ? 32 : lanes); o *= 2) s.in64 += __shfl_xor_sync(0xffffffffu, s.in64, o), s.in32 += __shfl_xor_sync(0xffffffffu, s.in32, o);
   if constexpr (BLOCK) {
     Sums* const buffer = shared[turn & 1];
@@ -222,14 +221,41 @@ __device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT,
   else
     keep_unit<SNN_KEEP_E4M3, ACCESS, N>(y, row, at, p, store);
 }
-// A unit of h: that of x, or its sum with the residual's; and its squares.
-template <typename IO, int N> __device__ __forceinline__ void sum_unit(Unit<IO, N>& h, const Unit<IO, N>& r, bool residual, float2& sum) {
+// Sums of squares of a lane: in 32 bits, and what 64 bits need beside them, so that rows of one magnitude, whose largest y is next to a
+// border, come out on the right side of it.  bf16: squares have 16 bits, and a lane adds up few enough of them.  fp16: they have 22 bits, of
+// which fp32 holds the sums of four.  fp32: what roundings leave out (all of it where no square is larger than the sum before it).
+struct Squares {
+  float2 in32{0.f, 0.f}, lost{0.f, 0.f};
+  double fours = 0.0;
+  template <typename IO> __device__ __forceinline__ double in64() const {
+    if constexpr (std::is_same<IO, __half>::value) return fours;
+    const double sum = (double)in32.x + (double)in32.y;
+    return std::is_same<IO, float>::value ? sum + (double)(lost.x + lost.y) : sum;
+  }
+};
+// A unit of h: that of x, or its sum with the residual's; and its squares, in 64 bits as well where that is asked for.
+template <typename IO, int N> __device__ __forceinline__ void sum_unit(Unit<IO, N>& h, const Unit<IO, N>& r, bool residual, Squares& s, bool in64) {
   if (residual) {
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) h.set(i, add_pair(h.pair(i), r.pair(i)));
   }
+  if constexpr (std::is_same<IO, __half>::value) {
 #pragma unroll
-  for (int i = 0; i < N / 2; ++i) sum = fma_pair(h.pair(i), h.pair(i), sum);
+    for (int i = 0; i < N / 2; i += 4) {
+      float2 four = mul_pair(h.pair(i), h.pair(i));
+#pragma unroll
+      for (int k = 1; k < 4; ++k) four = fma_pair(h.pair(i + k), h.pair(i + k), four);
+      s.in32 = add_pair(s.in32, four);
+      if (in64) s.fours += (double)four.x, s.fours += (double)four.y;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const float2 v = h.pair(i), before = s.in32;
+      s.in32 = fma_pair(v, v, before);
+      if (std::is_same<IO, float>::value && in64) s.lost = add_pair(s.lost, fma_pair(v, v, fma_pair(s.in32, both(-1.f), before)));
+    }
+  }
 }
 template <typename IO, int N> __device__ __forceinline__ void sum_unit_far(const Unit<IO, N>& h, float2& sum) {
 #pragma unroll
@@ -273,27 +299,27 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
     const bool store = base + at.slot < p.rows;   // (a slot without a row repeats the last one and stores nothing)
     const int64_t row = min(base + at.slot, p.rows - 1);
     Unit<IO, N> h[UNITS];
-    float2 sum = both(0.f);
+    Squares squares;
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
       h[i] = x[i];
-      sum_unit(h[i], r[i], residual, sum);
+      sum_unit(h[i], r[i], residual, squares, p.keep_format != SNN_KEEP_RAW);
       if (residual && store) at.columns(i).store(h[i], (IO*)p.h + row * p.h_stride);
     }
     if (base + step < p.rows) load(min(base + step + at.slot, p.rows - 1));
     Scale scale;
     float total;
     if (p.keep_format != SNN_KEEP_RAW) {
-      const Sums sums = row_sums<BLOCK>(sum, at.lanes, turn++, shared);
+      const Sums sums = row_sums<BLOCK>({squares.in64<IO>(), squares.in32.x + squares.in32.y}, at.lanes, turn++, shared);
       scale = scale_of(sums.in64, p), total = sums.in32;
     } else {
-      scale = {}, total = row_sum<BLOCK>(sum.x + sum.y, at.lanes, turn++, shared);
+      scale = {}, total = row_sum<BLOCK>(squares.in32.x + squares.in32.y, at.lanes, turn++, shared);
     }
     scale.rounded = scale_of(total, p);
     const bool far = !(total <= largest_finite<float>());
     // (lanes of one warp may hold different rows: they all go the same way, as do all threads of a row's warps)
     if (BLOCK ? far : __any_sync(0xffffffffu, far)) {
-      sum = both(0.f);
+      float2 sum = both(0.f);
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) sum_unit_far(h[i], sum);
       const double again = row_sum<BLOCK>((double)sum.x + (double)sum.y, at.lanes, turn++, shared);
@@ -315,7 +341,7 @@ template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds_
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const IO* const from = (const IO*)p.x + row * p.x_stride;
     const IO* const again = residual ? (const IO*)p.h + row * p.h_stride : from;
-    float2 sum = both(0.f);
+    Squares squares;
     // (a warp whose columns begin behind the last one has nothing to do: its lanes go the same way)
     auto each = [&](auto&& f) {
       for (int64_t start = (t & ~31) * N; start < p.n; start += RMS_WIDE * N) f(At{(int)start + At::of_lane(t & 31), p.n});
@@ -325,13 +351,13 @@ template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds_
       h.zero(), r.zero();
       at.load(h, from);
       if (residual) at.load(r, (const IO*)p.residual + row * p.residual_stride);
-      sum_unit(h, r, residual, sum);
+      sum_unit(h, r, residual, squares, true);
       if (residual) at.store(h, (IO*)p.h + row * p.h_stride);
     });
-    const double total = row_sum<true>((double)sum.x + (double)sum.y, RMS_WIDE, turn++, shared);
+    const double total = row_sum<true>(squares.in64<IO>(), RMS_WIDE, turn++, shared);
     Scale scale = scale_of(total, p);
     if (!(total <= largest_finite<float>())) {
-      sum = both(0.f);
+      float2 sum = both(0.f);
       each([&](At at) {
         Unit<IO, N> h;
         h.zero();

@@ -3,8 +3,8 @@
 //   m' = b1 m + (1 - b1) g,  v' = b2 v + (1 - b2) g^2,  p' = p (1 - lr wd) - lr / (1 - b1^t) m' / (sqrt(v' / (1 - b2^t)) + eps)
 //
 // With moments in fp32 bound by HBM (28 bytes a parameter with everything in fp32: 345 M parameters 1510 us, 6.4 TB/s), in 8 bits
-// (10 bytes with bf16 parameters and gradients) by instructions: 59 a parameter, three quarters of the issue slots (70 M
-// parameters 166 us, 4.3 TB/s).  A thread block takes tiles of a tensor, eight neighbouring parameters a thread and turn; where a
+// (10 bytes with bf16 parameters and gradients) by instructions: 60 a parameter, three quarters of the issue slots (70 M
+// parameters 170 us, 4.2 TB/s).  A thread block takes tiles of a tensor, eight neighbouring parameters a thread and turn; where a
 // tile's tensor lies is found by bisection in a table that comes with the launch, so that nothing is copied to the device first
 // and a graph holds it.
 //
@@ -494,7 +494,7 @@ template <int COUNT> struct AwPart {
   __device__ __forceinline__ static constexpr int of(int p, int g) { return p * 3 + g; }
 };
 // A whole part in these types.  The 32 scale bytes are read and written at once, lane by lane: stores of parts of a 32-byte sector
-// cost L2 so much that 70 M parameters took 199 us with four bytes a warp and turn (119 us against 351 where nothing was
+// cost L2 so much that 70 M parameters took 199 us instead of 166 with four bytes a warp and turn (351 against 119 us where nothing was
 // computed).  Sixteen values a thread need a fifth fewer instructions and as long, since fewer warps find room; so do copies to shared
 // memory a turn ahead.
 template <typename PT, typename GT, int COUNT>

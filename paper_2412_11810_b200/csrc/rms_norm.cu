@@ -9,8 +9,9 @@
 // 16-bit type, 8192 of fp32) are read a second time, from L2.
 //
 // Measured, bf16 with residual: 32768 x 2048 forward 80 us (6.7 TB/s), backward 84 us (6.4 TB/s) and 6 us for dw from the blocks'
-// shares; 16384 x 4096 to int8 alone 74 us (6.4 TB/s; 68 with codes that were rounded twice).  Units of 16 bytes and a row per block and launch, without the next row's
-// loads, took 112, 115 and 108 us: they were bound by instructions (42 a value).  Rows that vectors do not fit: 16384 x 4090
+// shares; 16384 x 4096 to int8 alone 77 us (6.1 TB/s; 68 with codes that were rounded twice, 73 with ties and limits of scales left to
+// chance).  Units of 16 bytes and a row per block and launch, without the next row's loads, took 112, 115 and 108 us: they were bound by
+// instructions (42 a value).  Rows that vectors do not fit: 16384 x 4090
 // 190 us (pairs; 359 us with eight lanes a group, whose accesses spread over as many lines).
 #include <algorithm>
 #include <initializer_list>

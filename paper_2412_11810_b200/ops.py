@@ -594,6 +594,7 @@ def adamw_step(params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], st
     parameter whose change is less than half a step stays as it is.
     lr and scale: numbers, or fp32 0-d tensors on the device, so that a captured step follows a schedule.
     max_norm: None computes no norm; otherwise a step whose norm is not finite is left out and not counted.
+    A finite gradient beyond 1.8e19 in magnitude, whose square is infinite, stops its parameter (but for the decay).
     Moments in 8 bits are rounded at random, by a hash of seed, t and place: give every list of tensors a seed of its own.
     eps: from 1e-30 to 1.  Returns the norm before the clip (fp32, 0-d), or None without max_norm."""
     if not isinstance(state, AdamWState):

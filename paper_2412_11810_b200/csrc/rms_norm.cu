@@ -225,34 +225,41 @@ __device__ __forceinline__ void finish_unit(const Unit<IO, N>& h, const Unit<WT,
 // Sums of squares of a lane: in 32 bits, and what 64 bits need beside them, so that rows of one magnitude, whose largest y is next to a
 // border, come out on the right side of it.  bf16: squares have 16 bits, and a lane adds up few enough of them.  fp16: they have 22 bits, of
 // which fp32 holds the sums of four.  fp32: what roundings leave out (all of it where no square is larger than the sum before it).
-struct Squares {
-  float2 in32{0.f, 0.f}, lost{0.f, 0.f};
-  double fours = 0.0;
-  template <typename IO> __device__ __forceinline__ double in64() const {
-    if constexpr (std::is_same<IO, __half>::value) return fours;
-    const double sum = (double)in32.x + (double)in32.y;
-    return std::is_same<IO, float>::value ? sum + (double)(lost.x + lost.y) : sum;
+template <typename IO, int UNITS> struct Squares {
+  static constexpr bool FOURS = std::is_same<IO, __half>::value;
+  float2 in32{0.f, 0.f}, lost{0.f, 0.f}, fours[UNITS][2];
+  __device__ __forceinline__ double in64() const {
+    double sum = 0.0;
+    if constexpr (FOURS) {
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) sum += (double)fours[i][0].x + (double)fours[i][0].y + ((double)fours[i][1].x + (double)fours[i][1].y);
+    } else {
+      sum = (double)in32.x + (double)in32.y + (double)(lost.x + lost.y);
+    }
+    return sum;
   }
 };
-// A unit of h: that of x, or its sum with the residual's; and its squares, in 64 bits as well where that is asked for.
-template <typename IO, int N> __device__ __forceinline__ void sum_unit(Unit<IO, N>& h, const Unit<IO, N>& r, bool residual, Squares& s, bool in64) {
+// Unit i of h: that of x, or its sum with the residual's; and its squares, in 64 bits as well where that is asked for.
+template <typename IO, int N, int UNITS>
+__device__ __forceinline__ void sum_unit(Unit<IO, N>& h, const Unit<IO, N>& r, bool residual, Squares<IO, UNITS>& s, int i, bool in64) {
   if (residual) {
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) h.set(i, add_pair(h.pair(i), r.pair(i)));
+    for (int k = 0; k < N / 2; ++k) h.set(k, add_pair(h.pair(k), r.pair(k)));
   }
-  if constexpr (std::is_same<IO, __half>::value) {
+  if constexpr (Squares<IO, UNITS>::FOURS) {
+    static_assert(N == 16, "two times four pairs");
 #pragma unroll
-    for (int i = 0; i < N / 2; i += 4) {
-      float2 four = mul_pair(h.pair(i), h.pair(i));
+    for (int j = 0; j < 2; ++j) {
+      float2 four = mul_pair(h.pair(4 * j), h.pair(4 * j));
 #pragma unroll
-      for (int k = 1; k < 4; ++k) four = fma_pair(h.pair(i + k), h.pair(i + k), four);
+      for (int k = 1; k < 4; ++k) four = fma_pair(h.pair(4 * j + k), h.pair(4 * j + k), four);
       s.in32 = add_pair(s.in32, four);
-      if (in64) s.fours += (double)four.x, s.fours += (double)four.y;
+      s.fours[i][j] = four;
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-      const float2 v = h.pair(i), before = s.in32;
+    for (int k = 0; k < N / 2; ++k) {
+      const float2 v = h.pair(k), before = s.in32;
       s.in32 = fma_pair(v, v, before);
       if (std::is_same<IO, float>::value && in64) s.lost = add_pair(s.lost, fma_pair(v, v, fma_pair(s.in32, both(-1.f), before)));
     }
@@ -300,18 +307,18 @@ __global__ void __launch_bounds__(BLOCK ? RMS_MOST_LANES : RMS_THREADS, BLOCK &&
     const bool store = base + at.slot < p.rows;   // (a slot without a row repeats the last one and stores nothing)
     const int64_t row = min(base + at.slot, p.rows - 1);
     Unit<IO, N> h[UNITS];
-    Squares squares;
+    Squares<IO, UNITS> squares;
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
       h[i] = x[i];
-      sum_unit(h[i], r[i], residual, squares, p.keep_format != SNN_KEEP_RAW);
+      sum_unit(h[i], r[i], residual, squares, i, p.keep_format != SNN_KEEP_RAW);
       if (residual && store) at.columns(i).store(h[i], (IO*)p.h + row * p.h_stride);
     }
     if (base + step < p.rows) load(min(base + step + at.slot, p.rows - 1));
     Scale scale;
     float total;
     if (p.keep_format != SNN_KEEP_RAW) {
-      const Sums sums = row_sums<BLOCK>({squares.in64<IO>(), squares.in32.x + squares.in32.y}, at.lanes, turn++, shared);
+      const Sums sums = row_sums<BLOCK>({squares.in64(), squares.in32.x + squares.in32.y}, at.lanes, turn++, shared);
       scale = scale_of(sums.in64, p), total = sums.in32;
     } else {
       scale = {}, total = row_sum<BLOCK>(squares.in32.x + squares.in32.y, at.lanes, turn++, shared);
@@ -342,7 +349,8 @@ template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds_
   for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
     const IO* const from = (const IO*)p.x + row * p.x_stride;
     const IO* const again = residual ? (const IO*)p.h + row * p.h_stride : from;
-    Squares squares;
+    Squares<IO, 1> squares;
+    double fours = 0.0;
     // (a warp whose columns begin behind the last one has nothing to do: its lanes go the same way)
     auto each = [&](auto&& f) {
       for (int64_t start = (t & ~31) * N; start < p.n; start += RMS_WIDE * N) f(At{(int)start + At::of_lane(t & 31), p.n});
@@ -352,10 +360,11 @@ template <typename IO, typename WT, int ACCESS> __global__ void __launch_bounds_
       h.zero(), r.zero();
       at.load(h, from);
       if (residual) at.load(r, (const IO*)p.residual + row * p.residual_stride);
-      sum_unit(h, r, residual, squares, true);
+      sum_unit(h, r, residual, squares, 0, true);
+      if (Squares<IO, 1>::FOURS) fours += squares.in64();
       if (residual) at.store(h, (IO*)p.h + row * p.h_stride);
     });
-    const double total = row_sum<true>(squares.in64<IO>(), RMS_WIDE, turn++, shared);
+    const double total = row_sum<true>(Squares<IO, 1>::FOURS ? fours : squares.in64(), RMS_WIDE, turn++, shared);
     Scale scale = scale_of(total, p);
     if (!(total <= largest_finite<float>())) {
       float2 sum = both(0.f);
